@@ -60,6 +60,12 @@ typedef enum {
   HYDRA_ERR_HIP = -6          /* the HIP runtime reported an error at launch        */
 } hydra_status;
 
+/* Element type of a tensor that a call takes in either. */
+typedef enum {
+  HYDRA_BF16 = 0, /* bf16 bit patterns, 2-byte aligned */
+  HYDRA_F32 = 1   /* fp32, 4-byte aligned              */
+} hydra_dtype;
+
 /* Largest LoRA rank accepted. */
 #define HYDRA_MAX_RANK 128
 
@@ -539,6 +545,187 @@ hydra_status hydra_lora_linear_backward(const uint16_t* x, const uint16_t* Wt, c
                                         float s, const uint16_t* dy, int64_t M, int64_t N, int64_t K, int64_t r,
                                         float* dx, float* dA, float* dB, void* workspace, size_t workspace_bytes,
                                         void* stream);
+
+/*
+ * hydra_layer_norm -- layer normalisation of M rows of K values (OPT's layers
+ * put one before the attention projections, one before fc1, one before the
+ * heads):
+ *   mean = sum x / K,  var = sum (x - mean)^2 / K,  rstd = 1 / sqrt(var + eps),
+ *   y = (x - mean) rstd weight + bias.
+ *
+ *   x       [M x K] bf16 or fp32 (x_type)
+ *   weight, bias [K] bf16 or fp32 (w_type, both), optional (NULL: ones / zeros)
+ *   eps     > 0, finite
+ *   y       [M x K] bf16 or fp32 (y_type): out; may be x where the types are
+ *           the same
+ *   mean, rstd [M] fp32   out, optional: what the backward takes
+ * Statistics and products are fp32 (the variance from the centred values),
+ * y is rounded once, to nearest even.  A row that holds NaN or an infinity
+ * becomes NaN.  Requires 1 <= M <= 2^20, 1 <= K <= 2^21; K need be no multiple of anything, and
+ * buffers need their element's alignment only (16-byte aligned ones with
+ * K % 8 == 0 are faster).  Outputs distinct (HYDRA_ERR_SHAPE); partial
+ * overlaps are not detected and are not allowed.
+ */
+hydra_status hydra_layer_norm(const void* x, hydra_dtype x_type, const void* weight, const void* bias,
+                              hydra_dtype w_type, float eps, int64_t M, int64_t K, void* y, hydra_dtype y_type,
+                              float* mean, float* rstd, void* stream);
+
+/*
+ * hydra_layer_norm_backward_workspace_bytes -- device workspace that
+ * hydra_layer_norm_backward needs for M rows of K values (writes *bytes).
+ * HYDRA_ERR_NULL for a NULL `bytes`, HYDRA_ERR_SHAPE for M outside [1, 2^20]
+ * or K outside [1, 2^21].
+ */
+hydra_status hydra_layer_norm_backward_workspace_bytes(int64_t M, int64_t K, size_t* bytes);
+
+/*
+ * hydra_layer_norm_backward -- gradients of hydra_layer_norm for an upstream
+ * gradient dy.  With g = dy weight and xh = (x - mean) rstd:
+ *   dx = rstd (g - sum g / K - xh sum (g xh) / K),
+ *   dweight = sum over the rows of dy xh,  dbias = sum over the rows of dy.
+ *
+ *   dy      [M x K] bf16 or fp32 (dy_type; hydra_lora_linear_backward's dx is fp32)
+ *   x       [M x K] bf16 or fp32 (x_type): the forward's input
+ *   weight  [K] bf16 or fp32 (w_type), optional (NULL: ones)
+ *   mean, rstd [M] fp32   the forward's
+ *   dx      [M x K] bf16 or fp32 (dx_type; bf16 is the dy of the linear
+ *           before), optional; may be dy or x where the types are the same
+ *   dweight, dbias [K] fp32   out, optional; overwritten, not added to
+ *   workspace, workspace_bytes  device, 16-byte aligned, at least
+ *           hydra_layer_norm_backward_workspace_bytes(M, K) bytes, contents
+ *           ignored and overwritten
+ * At least one output (HYDRA_ERR_NULL).  Products and sums are fp32, every sum
+ * in a fixed order: repeated calls give the same bits.  Sizes, alignment and
+ * overlaps as in hydra_layer_norm.  Calls that share a workspace on different
+ * streams race.
+ */
+hydra_status hydra_layer_norm_backward(const void* dy, hydra_dtype dy_type, const void* x, hydra_dtype x_type,
+                                       const void* weight, hydra_dtype w_type, const float* mean, const float* rstd,
+                                       int64_t M, int64_t K, void* dx, hydra_dtype dx_type, float* dweight,
+                                       float* dbias, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Most alternatives per token of hydra_token_logprobs. */
+#define HYDRA_MAX_TOP 32
+
+/*
+ * hydra_token_logprobs_workspace_bytes -- device workspace that
+ * hydra_token_logprobs needs for M rows, a vocabulary of V and `top`
+ * alternatives (writes *bytes; 0 when none is needed).  HYDRA_ERR_NULL for a NULL `bytes`,
+ * HYDRA_ERR_SHAPE for M outside [1, 2^20], V outside [1, 2^21] or top outside
+ * [0, min(V, HYDRA_MAX_TOP)].
+ */
+hydra_status hydra_token_logprobs_workspace_bytes(int64_t M, int64_t V, int64_t top, size_t* bytes);
+
+/*
+ * hydra_token_logprobs -- log-probabilities of given tokens under one set of
+ * logits, with the distribution's entropy and the most likely alternatives
+ * (the update stage's new log-probabilities of Sec. 2 Stage 3, over logits
+ * that the program keeps for the backward; and what a generation step reports).
+ *
+ *   logits  [M x V] bf16 or fp32 (logits_type), row m at logits + m * ld
+ *           elements, ld >= V; -inf marks a masked-out entry
+ *   tokens  [M] int32, optional (NULL iff lp is)
+ *   lp      [M] fp32   out: z[token] - lse
+ *   lse     [M] fp32   out, optional: ln sum_j e^z_j
+ *   entropy [M] fp32   out, optional: -sum_j p_j ln p_j, p_j = e^(z_j - lse)
+ *   top     alternatives per row, 0 <= top <= min(V, HYDRA_MAX_TOP)
+ *   top_ids [M x top] int32   out: indices of the row's `top` largest logits,
+ *           the largest first, the lowest index first among equals (+0 and -0
+ *           are equal); NULL iff top == 0
+ *   top_lp  [M x top] fp32    out, optional: their log-probabilities
+ *   workspace, workspace_bytes  device, 16-byte aligned, at least
+ *           hydra_token_logprobs_workspace_bytes(M, V, top) bytes (NULL
+ *           allowed when that is 0), contents ignored and overwritten
+ *   err_flag [1] int32  optional: 1 is OR-ed in for a token outside [0, V),
+ *           whose lp is NaN
+ * At least one output (HYDRA_ERR_NULL).  Masked-out entries have probability 0
+ * and log-probability -inf; a row of nothing else has lse -inf and NaN lp,
+ * entropy and top_lp (top_ids 0, 1, ...).  In a row that holds NaN or +inf lp, lse, entropy and
+ * top_lp are NaN (top_ids then take NaN first, then +inf).  Sums and maxima are
+ * fp32.  Requires 1 <= M <= 2^20, 1 <= V <= 2^21,
+ * ld <= 2^31 - 1; logits need their element's alignment only.  Outputs distinct (HYDRA_ERR_SHAPE).
+ */
+hydra_status hydra_token_logprobs(const void* logits, hydra_dtype logits_type, int64_t ld, const int32_t* tokens,
+                                  int64_t M, int64_t V, int64_t top, float* lp, float* lse, float* entropy,
+                                  int32_t* top_ids, float* top_lp, void* workspace, size_t workspace_bytes,
+                                  int32_t* err_flag, void* stream);
+
+/*
+ * hydra_token_logprobs_backward -- gradient of hydra_token_logprobs' lp and
+ * entropy H with respect to the logits, for upstream gradients d_lp (that of
+ * hydra_ppo_loss) and d_entropy:
+ *   dz_j = d_lp ([j == token] - p_j) - d_entropy p_j (ln p_j + H),  p_j = e^(z_j - lse).
+ *
+ *   logits, logits_type, ld, tokens, M, V   as in hydra_token_logprobs
+ *   lse     [M] fp32   the forward's
+ *   entropy [M] fp32   the forward's (NULL iff d_entropy is)
+ *   d_lp    [M] fp32   optional (NULL: zeros; tokens may then be NULL too)
+ *   d_entropy [M] fp32 optional (NULL: zeros)
+ *   d_logits [M x V] bf16 or fp32 (d_type), row m at d_logits + m * ld_d
+ *           elements, ld_d >= V: out (bf16 and ld_d == V is the dy of
+ *           hydra_lora_linear_backward for the head); may be logits where types
+ *           and strides are the same.  Elements between V and ld_d are left as they are.
+ *   err_flag [1] int32  optional: 1 is OR-ed in for a token outside [0, V) of
+ *           a row whose d_lp is not 0; that row's gradient is NaN
+ * At least one of d_lp and d_entropy (HYDRA_ERR_NULL).  A row whose upstream
+ * gradients are both 0 (a prompt token, padding) gets zeros: its logits, token
+ * and statistics are not read.  Products are fp32, each gradient rounded once, to
+ * nearest even.  Sizes, alignment and overlaps as in hydra_token_logprobs.
+ */
+hydra_status hydra_token_logprobs_backward(const void* logits, hydra_dtype logits_type, int64_t ld,
+                                           const int32_t* tokens, const float* lse, const float* entropy,
+                                           const float* d_lp, const float* d_entropy, int64_t M, int64_t V,
+                                           void* d_logits, hydra_dtype d_type, int64_t ld_d, int32_t* err_flag,
+                                           void* stream);
+
+/* Most tensors of one hydra_grad_norm or hydra_grad_clip call. */
+#define HYDRA_MAX_GRADS 4096
+
+/* hydra_grad_norm_workspace_bytes -- device workspace that hydra_grad_norm and
+ * hydra_grad_clip need, whatever the tensors (writes *bytes; HYDRA_ERR_NULL for NULL). */
+hydra_status hydra_grad_norm_workspace_bytes(size_t* bytes);
+
+/*
+ * hydra_grad_norm -- the norm over all gradients of an update (the dA and dB
+ * of every linear's hydra_lora_linear_backward):
+ *   norm = sqrt(sum over the tensors of sum g^2).
+ *
+ *   n       1 <= n <= HYDRA_MAX_GRADS
+ *   grads   HOST array of n device pointers (an entry may be NULL where its numel is 0)
+ *   types   HOST array of n hydra_dtype values
+ *   numels  HOST array of n element counts, 0 <= numel <= 2^40
+ *   norm    [1] fp32   out
+ *   workspace, workspace_bytes  device, 16-byte aligned, at least
+ *           hydra_grad_norm_workspace_bytes() bytes, contents ignored and overwritten
+ * Squares and sums are 64-bit floats, in a fixed order: gradients whose
+ * squares leave the range of fp32 count, and repeated calls give the same bits.
+ * Tensors need their element's alignment only.  NaN and infinities propagate.
+ * Calls that share a workspace on different streams race.
+ */
+hydra_status hydra_grad_norm(int64_t n, const void* const* grads, const int32_t* types, const int64_t* numels,
+                             float* norm, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * hydra_grad_clip -- hydra_grad_norm, and the gradients scaled to a norm of
+ * at most max_norm:
+ *   out = g c,  c = max_norm / norm where norm > max_norm, else 1.
+ *
+ *   n, grads, types, numels, norm, workspace   as in hydra_grad_norm
+ *   max_norm  >= 0 (infinity: never scaled)
+ *   outs      HOST array of n device pointers, outs[i] of grads[i]'s size (it
+ *             may be grads[i] itself where the types are the same); NULL: the
+ *             gradients are scaled in place
+ *   out_types HOST array of n hydra_dtype values (NULL iff outs is)
+ *   err_flag  [1] int32, optional: 1 is OR-ed in when the norm is not finite;
+ *             c is 1 then, so that a program can leave the step out
+ * c is formed in 64 bits and rounded to fp32; each product is rounded once.
+ * Where c is 1, gradients in place are not written.  A tensor that is
+ * written may not overlap another tensor that is written or read, `norm` or `err_flag`
+ * (HYDRA_ERR_SHAPE): neither may a gradient stand in the list twice.
+ */
+hydra_status hydra_grad_clip(int64_t n, const void* const* grads, const int32_t* types, const int64_t* numels,
+                             float max_norm, float* norm, void* const* outs, const int32_t* out_types,
+                             void* workspace, size_t workspace_bytes, int32_t* err_flag, void* stream);
 
 /* A static, human-readable name for a status code. */
 const char* hydra_status_string(hydra_status status);

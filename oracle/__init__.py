@@ -16,3 +16,11 @@ from .ppo_oracle import (  # noqa: F401
     ppo_rewards_ref,
     value_head_ref,
 )
+from .update_oracle import (  # noqa: F401
+    grad_clip_ref,
+    grad_norm_ref,
+    layer_norm_backward_ref,
+    layer_norm_ref,
+    token_logprobs_backward_ref,
+    token_logprobs_ref,
+)

@@ -33,6 +33,10 @@ HYDRA_MAX_RANK = 128
 HYDRA_MAX_GROUP = 8
 HYDRA_MAX_ADAPTERS = 4
 HYDRA_SCORE_NOALLOC_MAX_BYTES = 48 << 20
+HYDRA_BF16 = 0
+HYDRA_F32 = 1
+HYDRA_MAX_TOP = 32
+HYDRA_MAX_GRADS = 4096
 HYDRA_GROUP_WS_CONTROL_BYTES = 4352
 HYDRA_GROUP_WS_BOUND_WORD = 8
 HYDRA_GROUP_WS_T_BYTES = 65536
@@ -60,6 +64,15 @@ EXPORTED = (
     "hydra_transpose_bf16",
     "hydra_lora_linear_backward_workspace_bytes",
     "hydra_lora_linear_backward",
+    "hydra_layer_norm",
+    "hydra_layer_norm_backward_workspace_bytes",
+    "hydra_layer_norm_backward",
+    "hydra_token_logprobs_workspace_bytes",
+    "hydra_token_logprobs",
+    "hydra_token_logprobs_backward",
+    "hydra_grad_norm_workspace_bytes",
+    "hydra_grad_norm",
+    "hydra_grad_clip",
     "hydra_status_string",
     "hydra_abi_version",
 )
@@ -141,6 +154,23 @@ def lib() -> ctypes.CDLL:
     L.hydra_lora_linear_backward.argtypes = [_vp, _vp, _vp, _vp, _f32, _vp, _i64, _i64, _i64, _i64, _vp, _vp, _vp,
                                              _vp, ctypes.c_size_t, _vp]
     L.hydra_lora_linear_backward.restype = ctypes.c_int
+    _int, _size, _sizep = ctypes.c_int, ctypes.c_size_t, ctypes.POINTER(ctypes.c_size_t)
+    _i32p, _i64p = ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_int64)
+    for name, args in (
+            ("hydra_layer_norm", [_vp, _int, _vp, _vp, _int, _f32, _i64, _i64, _vp, _int, _vp, _vp, _vp]),
+            ("hydra_layer_norm_backward_workspace_bytes", [_i64, _i64, _sizep]),
+            ("hydra_layer_norm_backward", [_vp, _int, _vp, _int, _vp, _int, _vp, _vp, _i64, _i64, _vp, _int, _vp, _vp,
+                                           _vp, _size, _vp]),
+            ("hydra_token_logprobs_workspace_bytes", [_i64, _i64, _i64, _sizep]),
+            ("hydra_token_logprobs", [_vp, _int, _i64, _vp, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _size, _vp,
+                                      _vp]),
+            ("hydra_token_logprobs_backward", [_vp, _int, _i64, _vp, _vp, _vp, _vp, _vp, _i64, _i64, _vp, _int, _i64, _vp,
+                                               _vp]),
+            ("hydra_grad_norm_workspace_bytes", [_sizep]),
+            ("hydra_grad_norm", [_i64, _pp, _i32p, _i64p, _vp, _vp, _size, _vp]),
+            ("hydra_grad_clip", [_i64, _pp, _i32p, _i64p, _f32, _vp, _pp, _i32p, _vp, _size, _vp, _vp])):
+        getattr(L, name).argtypes = args
+        getattr(L, name).restype = ctypes.c_int
     L.hydra_status_string.argtypes = [ctypes.c_int]
     L.hydra_status_string.restype = ctypes.c_char_p
     L.hydra_abi_version.argtypes = []
@@ -763,3 +793,266 @@ def _hydra_lora_linear_backward(x, Wt, A, B, s, dy, dx, dA, dB, workspace, strea
                                           _ptr(dx), _ptr(dA), _ptr(dB), _ptr(workspace), nbytes,
                                           _stream_handle(stream))
     _check(st, "hydra_lora_linear_backward")
+
+
+# ------------------------------------------------------------------ the update step's further operators
+#
+# These calls go to the device that their tensors are on, whichever is current, on `stream` or on that device's
+# current stream.  A workspace that a call allocates itself belongs to that stream.
+
+def _any_types():
+    return _bf16_types() + (_torch().float32,)
+
+
+def _type(t) -> int:
+    return HYDRA_BF16 if t is None or t.dtype != _torch().float32 else HYDRA_F32
+
+
+def _launch(where, tensors, stream, call, workspace=None, need=0) -> None:
+    """call(workspace pointer, its bytes, stream handle) on the tensors' device; allocates a workspace of `need` bytes
+    if none is given."""
+    torch = _torch()
+    _need(workspace, "workspace", (torch.uint8,))
+    devices = {t.device for t in (*tensors, workspace) if t is not None}
+    if len(devices) != 1:
+        raise ValueError(f"{where}: the tensors are on different devices: {sorted(map(str, devices))}")
+    device, = devices
+    if stream is not None and stream.device != device:
+        raise ValueError(f"{where}: the stream belongs to {stream.device}, the tensors are on {device}")
+    with torch.cuda.device(device):
+        if workspace is None and need > 0:
+            with torch.cuda.stream(stream):
+                workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        st = call(_ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_handle(stream))
+    _check(st, where)
+
+
+def hydra_layer_norm(x, weight, bias, y, mean=None, rstd=None, eps: float = 1e-5, stream=None) -> None:
+    """y = (x - mean) rstd weight + bias over the rows of x (see include/hydra.h).
+
+    x, y [M,K]: bf16 (or 16-bit integer tensors holding bf16 bits) or float32 (y may be x); weight, bias [K]: either
+    type, both the same, each may be None; mean, rstd [M] float32 outputs for the backward (each optional).
+    """
+    st = (_nat or _native()).layer_norm(x, weight, bias, y, mean, rstd, eps, stream)
+    if st == _SLOW:
+        return _hydra_layer_norm(x, weight, bias, y, mean, rstd, eps, stream)
+    if st != HYDRA_OK:
+        _check(st, "hydra_layer_norm")
+
+
+def _affine(weight, bias, K) -> None:
+    _need(weight, "weight", _any_types(), (K,))
+    _need(bias, "bias", _any_types(), (K,))
+    if weight is not None and bias is not None and _type(weight) != _type(bias):
+        raise TypeError(f"weight is {weight.dtype}, bias {bias.dtype}")
+
+
+def _hydra_layer_norm(x, weight, bias, y, mean, rstd, eps, stream) -> None:
+    torch = _torch()
+    _need(x, "x", _any_types())
+    M, K = x.shape
+    _affine(weight, bias, K)
+    _need(y, "y", _any_types(), (M, K))
+    _need(mean, "mean", (torch.float32,), (M,))
+    _need(rstd, "rstd", (torch.float32,), (M,))
+    _launch("hydra_layer_norm", (x, weight, bias, y, mean, rstd), stream, lambda ws, n, st: lib().hydra_layer_norm(
+        _ptr(x), _type(x), _ptr(weight), _ptr(bias), _type(bias if weight is None else weight), float(eps), M, K,
+        _ptr(y), _type(y), _ptr(mean), _ptr(rstd), st))
+
+
+def hydra_layer_norm_backward_workspace_bytes(M: int, K: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().hydra_layer_norm_backward_workspace_bytes(int(M), int(K), ctypes.byref(out)),
+           "hydra_layer_norm_backward_workspace_bytes")
+    return int(out.value)
+
+
+def hydra_layer_norm_backward(dy, x, weight, mean, rstd, dx=None, dweight=None, dbias=None, workspace=None,
+                              stream=None) -> None:
+    """dx, dweight, dbias of hydra_layer_norm (see include/hydra.h).
+
+    dy, x, dx [M,K]: bf16 (or 16-bit integer tensors holding bf16 bits) or float32, each of its own type (dx may be dy
+    or x); weight [K]: either type or None; mean, rstd [M] float32, the forward's; dweight, dbias [K] float32 outputs
+    (each output optional).  Allocates the workspace if none is given.
+    """
+    st = (_nat or _native()).layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, workspace, stream)
+    if st == _SLOW:
+        return _hydra_layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, workspace, stream)
+    if st != HYDRA_OK:
+        _check(st, "hydra_layer_norm_backward")
+
+
+def _hydra_layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, workspace, stream) -> None:
+    torch = _torch()
+    _need(x, "x", _any_types())
+    M, K = x.shape
+    _need(dy, "dy", _any_types(), (M, K))
+    _affine(weight, None, K)
+    _need(dx, "dx", _any_types(), (M, K))
+    for name, t, n in (("mean", mean, M), ("rstd", rstd, M), ("dweight", dweight, K), ("dbias", dbias, K)):
+        _need(t, name, (torch.float32,), (n,))
+    need = hydra_layer_norm_backward_workspace_bytes(M, K)
+    _launch("hydra_layer_norm_backward", (dy, x, weight, mean, rstd, dx, dweight, dbias), stream,
+            lambda ws, n, st: lib().hydra_layer_norm_backward(
+                _ptr(dy), _type(dy), _ptr(x), _type(x), _ptr(weight), _type(weight), _ptr(mean), _ptr(rstd), M, K,
+                _ptr(dx), _type(dx), _ptr(dweight), _ptr(dbias), ws, n, st), workspace, need)
+
+
+def hydra_token_logprobs_workspace_bytes(M: int, V: int, top: int = 0) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().hydra_token_logprobs_workspace_bytes(int(M), int(V), int(top), ctypes.byref(out)),
+           "hydra_token_logprobs_workspace_bytes")
+    return int(out.value)
+
+
+def _rows(t, name, shape=None) -> int:
+    """Checks a matrix whose rows may stand apart (each row contiguous, a row's end before the next one's start);
+    returns the distance of its rows in elements."""
+    torch = _torch()
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.device.type != "cuda":
+        raise ValueError(f"{name} must be on a ROCm device, got {t.device}")
+    if t.dtype not in _any_types():
+        raise TypeError(f"{name} has dtype {t.dtype}, expected one of {_any_types()}")
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {'two dimensions' if shape is None else tuple(shape)}")
+    M, V = t.shape
+    ld = t.stride(0) if M > 1 else V
+    if (V > 1 and t.stride(1) != 1) or ld < V:
+        raise ValueError(f"{name} must have contiguous rows, got strides {t.stride()}")
+    return ld
+
+
+def hydra_token_logprobs(logits, tokens, lp, lse=None, entropy=None, top_ids=None, top_lp=None, workspace=None,
+                         err_flag=None, stream=None) -> None:
+    """Log-probabilities of given tokens under one set of logits, with the distribution's entropy and the most likely
+    alternatives (see include/hydra.h).
+
+    logits [M,V]: bf16 (or 16-bit integer tensors holding bf16 bits) or float32, rows contiguous and possibly apart
+    (logits[:, :V] of a padded vocabulary); tokens [M] int32 and lp [M] float32 (both None: alternatives or statistics
+    alone); lse, entropy [M] float32, top_ids [M,top] int32, top_lp [M,top] float32 outputs (each optional; top_lp
+    needs top_ids).  Allocates the workspace if one is needed and none is given.
+    """
+    st = (_nat or _native()).token_logprobs(logits, tokens, lp, lse, entropy, top_ids, top_lp, workspace, err_flag,
+                                            stream)
+    if st == _SLOW:
+        return _hydra_token_logprobs(logits, tokens, lp, lse, entropy, top_ids, top_lp, workspace, err_flag, stream)
+    if st != HYDRA_OK:
+        _check(st, "hydra_token_logprobs")
+
+
+def _hydra_token_logprobs(logits, tokens, lp, lse, entropy, top_ids, top_lp, workspace, err_flag, stream) -> None:
+    torch = _torch()
+    ld = _rows(logits, "logits")
+    M, V = logits.shape
+    top = 0 if top_ids is None else top_ids.shape[-1]
+    _need(tokens, "tokens", (torch.int32,), (M,))
+    for name, t in (("lp", lp), ("lse", lse), ("entropy", entropy)):
+        _need(t, name, (torch.float32,), (M,))
+    _need(top_ids, "top_ids", (torch.int32,), (M, top))
+    _need(top_lp, "top_lp", (torch.float32,), (M, top))
+    _need(err_flag, "err_flag", (torch.int32,), (1,))
+    need = hydra_token_logprobs_workspace_bytes(M, V, top)
+    _launch("hydra_token_logprobs", (logits, tokens, lp, lse, entropy, top_ids, top_lp, err_flag), stream,
+            lambda ws, n, st: lib().hydra_token_logprobs(
+                _ptr(logits), _type(logits), ld, _ptr(tokens), M, V, top, _ptr(lp), _ptr(lse), _ptr(entropy),
+                _ptr(top_ids), _ptr(top_lp), ws, n, _ptr(err_flag), st), workspace, need)
+
+
+def hydra_token_logprobs_backward(logits, tokens, lse, d_logits, d_lp=None, entropy=None, d_entropy=None,
+                                  err_flag=None, stream=None) -> None:
+    """Gradient of hydra_token_logprobs' lp and entropy with respect to the logits (see include/hydra.h).
+
+    logits, d_logits [M,V]: bf16 (or 16-bit integer tensors holding bf16 bits) or float32, rows contiguous and possibly
+    apart (d_logits may be logits); tokens [M] int32; lse, d_lp [M] float32; entropy, d_entropy [M] float32 (both or
+    neither).  Rows whose d_lp and d_entropy are 0 get zeros.
+    """
+    st = (_nat or _native()).token_logprobs_backward(logits, tokens, lse, d_logits, d_lp, entropy, d_entropy, err_flag,
+                                                     stream)
+    if st == _SLOW:
+        return _hydra_token_logprobs_backward(logits, tokens, lse, d_logits, d_lp, entropy, d_entropy, err_flag, stream)
+    if st != HYDRA_OK:
+        _check(st, "hydra_token_logprobs_backward")
+
+
+def _hydra_token_logprobs_backward(logits, tokens, lse, d_logits, d_lp, entropy, d_entropy, err_flag, stream) -> None:
+    torch = _torch()
+    ld = _rows(logits, "logits")
+    M, V = logits.shape
+    ld_d = _rows(d_logits, "d_logits", (M, V))
+    _need(tokens, "tokens", (torch.int32,), (M,))
+    for name, t in (("lse", lse), ("d_lp", d_lp), ("entropy", entropy), ("d_entropy", d_entropy)):
+        _need(t, name, (torch.float32,), (M,))
+    _need(err_flag, "err_flag", (torch.int32,), (1,))
+    _launch("hydra_token_logprobs_backward", (logits, tokens, lse, d_logits, d_lp, entropy, d_entropy, err_flag), stream,
+            lambda ws, n, st: lib().hydra_token_logprobs_backward(
+                _ptr(logits), _type(logits), ld, _ptr(tokens), _ptr(lse), _ptr(entropy), _ptr(d_lp), _ptr(d_entropy), M,
+                V, _ptr(d_logits), _type(d_logits), ld_d, _ptr(err_flag), st))
+
+
+def hydra_grad_norm_workspace_bytes() -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().hydra_grad_norm_workspace_bytes(ctypes.byref(out)), "hydra_grad_norm_workspace_bytes")
+    return int(out.value)
+
+
+def hydra_grad_norm(grads, norm, workspace=None, stream=None) -> None:
+    """norm [1] float32 = the norm over all the tensors of `grads` (see include/hydra.h).
+
+    grads: a sequence of contiguous tensors of any shape, bf16 (or 16-bit integer tensors holding bf16 bits) or
+    float32.  Allocates the workspace (hydra_grad_norm_workspace_bytes()) if none is given.
+    """
+    st = (_nat or _native()).grad_clip(grads, None, norm, None, workspace, None, stream)
+    if st == _SLOW:
+        return _hydra_grad("hydra_grad_norm", grads, None, norm, None, workspace, None, stream)
+    if st != HYDRA_OK:
+        _check(st, "hydra_grad_norm")
+
+
+def hydra_grad_clip(grads, max_norm: float, norm, outs=None, workspace=None, err_flag=None, stream=None) -> None:
+    """hydra_grad_norm, and the gradients scaled to a norm of at most max_norm: in place, or into `outs` (see
+    include/hydra.h).
+
+    outs: None, or a sequence of contiguous tensors of the gradients' shapes, bf16 or float32; err_flag [1] int32 gets
+    1 OR-ed in when the norm is not finite (nothing is scaled then).
+    """
+    if max_norm is None:
+        raise TypeError("max_norm must be a number")
+    st = (_nat or _native()).grad_clip(grads, max_norm, norm, outs, workspace, err_flag, stream)
+    if st == _SLOW:
+        return _hydra_grad("hydra_grad_clip", grads, max_norm, norm, outs, workspace, err_flag, stream)
+    if st != HYDRA_OK:
+        _check(st, "hydra_grad_clip")
+
+
+def _hydra_grad(where, grads, max_norm, norm, outs, workspace, err_flag, stream) -> None:
+    torch = _torch()
+    grads = list(grads)
+    n = len(grads)
+    for i, g in enumerate(grads):
+        if g is None:
+            raise TypeError(f"grads[{i}] must be a torch.Tensor")
+        _need(g, f"grads[{i}]", _any_types())
+    _need(norm, "norm", (torch.float32,), (1,))
+    _need(err_flag, "err_flag", (torch.int32,), (1,))
+    if outs is not None:
+        outs = list(outs)
+        if len(outs) != n:
+            raise ValueError("outs must have one tensor for each gradient")
+        for i, o in enumerate(outs):
+            if o is None:
+                raise TypeError(f"outs[{i}] must be a torch.Tensor")
+            _need(o, f"outs[{i}]", _any_types(), grads[i].shape)
+    types = (ctypes.c_int32 * n)(*[_type(g) for g in grads])
+    numels = (ctypes.c_int64 * n)(*[g.numel() for g in grads])
+    head = (n, _ptr_array(grads), types, numels)
+
+    def call(ws, nbytes, st):
+        if max_norm is None:
+            return lib().hydra_grad_norm(*head, _ptr(norm), ws, nbytes, st)
+        return lib().hydra_grad_clip(*head, float(max_norm), _ptr(norm), None if outs is None else _ptr_array(outs),
+                                     None if outs is None else (ctypes.c_int32 * n)(*[_type(o) for o in outs]), ws,
+                                     nbytes, _ptr(err_flag), st)
+
+    _launch(where, (*grads, norm, *(outs or ()), err_flag), stream, call, workspace, hydra_grad_norm_workspace_bytes())

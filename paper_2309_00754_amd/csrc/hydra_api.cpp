@@ -5,6 +5,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <mutex>
 
 #include "hydra_internal.h"
@@ -822,6 +823,331 @@ hydra_status hydra_score_logits(const float* logits_on, const float* logits_off,
   o.lse_off = lse_off;
   o.err = err_flag;
   return from_hip(hydra::launch_score_logits(o, reinterpret_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"
+
+namespace {
+
+bool type_ok(int t) { return t == HYDRA_BF16 || t == HYDRA_F32; }
+uintptr_t type_align(int t) { return t == HYDRA_BF16 ? 2 : 4; }
+
+// No two of the outputs are one, and none is an input (null: not there).
+template <int NO, int NI>
+bool distinct(const void* const (&outs)[NO], const void* const (&ins)[NI]) {
+  for (int i = 0; i < NO; ++i) {
+    if (!outs[i]) continue;
+    for (int j = 0; j < i; ++j)
+      if (outs[i] == outs[j]) return false;
+    for (const void* p : ins)
+      if (outs[i] == p) return false;
+  }
+  return true;
+}
+
+bool norm_shape_ok(int64_t M, int64_t K) { return M >= 1 && M <= kMaxRows && K >= 1 && K <= kMaxK; }
+
+}  // namespace
+
+extern "C" {
+
+hydra_status hydra_layer_norm(const void* x, hydra_dtype x_type, const void* weight, const void* bias,
+                              hydra_dtype w_type, float eps, int64_t M, int64_t K, void* y, hydra_dtype y_type,
+                              float* mean, float* rstd, void* stream) {
+  if (!x || !y) return HYDRA_ERR_NULL;
+  if (!type_ok(x_type) || !type_ok(w_type) || !type_ok(y_type)) return HYDRA_ERR_UNSUPPORTED;
+  if (!norm_shape_ok(M, K)) return HYDRA_ERR_SHAPE;
+  if (!(eps > 0.f && eps <= 3.4028235e38f)) return HYDRA_ERR_SHAPE;
+  const void* const outs[3] = {y, mean, rstd};
+  const void* const ins[3] = {x == y && x_type == y_type ? nullptr : x, weight, bias};
+  if (!distinct(outs, ins)) return HYDRA_ERR_SHAPE;
+  if (!aligned(x, type_align(x_type)) || !aligned(y, type_align(y_type)) || !aligned(weight, type_align(w_type)) ||
+      !aligned(bias, type_align(w_type)) || !aligned(mean, 4) || !aligned(rstd, 4))
+    return HYDRA_ERR_ALIGN;
+  hydra::LayerNormArgs a{};
+  a.x = x;
+  a.w = weight;
+  a.b = bias;
+  a.y = y;
+  a.mean = mean;
+  a.rstd = rstd;
+  a.x_type = x_type;
+  a.w_type = w_type;
+  a.y_type = y_type;
+  a.eps = eps;
+  a.M = int(M);
+  a.K = int(K);
+  return from_hip(hydra::launch_layer_norm(a, reinterpret_cast<hipStream_t>(stream)));
+}
+
+hydra_status hydra_layer_norm_backward_workspace_bytes(int64_t M, int64_t K, size_t* bytes) {
+  if (!bytes) return HYDRA_ERR_NULL;
+  if (!norm_shape_ok(M, K)) return HYDRA_ERR_SHAPE;
+  *bytes = hydra::layer_norm_back_ws_bytes(int(M), int(K));
+  return HYDRA_OK;
+}
+
+hydra_status hydra_layer_norm_backward(const void* dy, hydra_dtype dy_type, const void* x, hydra_dtype x_type,
+                                       const void* weight, hydra_dtype w_type, const float* mean, const float* rstd,
+                                       int64_t M, int64_t K, void* dx, hydra_dtype dx_type, float* dweight,
+                                       float* dbias, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!dy || !x || !mean || !rstd) return HYDRA_ERR_NULL;
+  if (!dx && !dweight && !dbias) return HYDRA_ERR_NULL;
+  if (!type_ok(dy_type) || !type_ok(x_type) || !type_ok(w_type) || !type_ok(dx_type)) return HYDRA_ERR_UNSUPPORTED;
+  if (!norm_shape_ok(M, K)) return HYDRA_ERR_SHAPE;
+  const void* const outs[3] = {dx, dweight, dbias};
+  const void* const ins[5] = {dx == dy && dx_type == dy_type ? nullptr : dy, dx == x && dx_type == x_type ? nullptr : x,
+                              weight, mean, rstd};
+  if (!distinct(outs, ins)) return HYDRA_ERR_SHAPE;
+  if (!aligned(dy, type_align(dy_type)) || !aligned(x, type_align(x_type)) || !aligned(weight, type_align(w_type)) ||
+      !aligned(mean, 4) || !aligned(rstd, 4) || !aligned(dx, type_align(dx_type)) || !aligned(dweight, 4) ||
+      !aligned(dbias, 4))
+    return HYDRA_ERR_ALIGN;
+  if (!workspace) return HYDRA_ERR_NULL;
+  if (workspace_bytes < hydra::layer_norm_back_ws_bytes(int(M), int(K))) return HYDRA_ERR_WORKSPACE;
+  if (!aligned(workspace, 16)) return HYDRA_ERR_ALIGN;
+  hydra::LayerNormBackArgs a{};
+  a.dy = dy;
+  a.x = x;
+  a.w = weight;
+  a.mean = mean;
+  a.rstd = rstd;
+  a.dx = dx;
+  a.dw = dweight;
+  a.db = dbias;
+  a.dy_type = dy_type;
+  a.x_type = x_type;
+  a.w_type = w_type;
+  a.dx_type = dx_type;
+  a.M = int(M);
+  a.K = int(K);
+  return from_hip(hydra::launch_layer_norm_back(a, workspace, reinterpret_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"
+
+namespace {
+
+hydra_status logits_check(int type, int64_t ld, int64_t M, int64_t V) {
+  if (!type_ok(type)) return HYDRA_ERR_UNSUPPORTED;
+  if (M < 1 || M > kMaxRows || V < 1 || V > kMaxCols || ld < V || ld > kMaxDim) return HYDRA_ERR_SHAPE;
+  return HYDRA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+hydra_status hydra_token_logprobs_workspace_bytes(int64_t M, int64_t V, int64_t top, size_t* bytes) {
+  if (!bytes) return HYDRA_ERR_NULL;
+  if (M < 1 || M > kMaxRows || V < 1 || V > kMaxCols || top < 0 || top > HYDRA_MAX_TOP || top > V)
+    return HYDRA_ERR_SHAPE;
+  *bytes = hydra::token_logp_ws_bytes(int(M), int(V), int(top));
+  return HYDRA_OK;
+}
+
+hydra_status hydra_token_logprobs(const void* logits, hydra_dtype logits_type, int64_t ld, const int32_t* tokens,
+                                  int64_t M, int64_t V, int64_t top, float* lp, float* lse, float* entropy,
+                                  int32_t* top_ids, float* top_lp, void* workspace, size_t workspace_bytes,
+                                  int32_t* err_flag, void* stream) {
+  if (!logits || (lp && !tokens) || (tokens && !lp)) return HYDRA_ERR_NULL;
+  if (!lp && !lse && !entropy && !top_ids) return HYDRA_ERR_NULL;
+  const hydra_status chk = logits_check(logits_type, ld, M, V);
+  if (chk != HYDRA_OK) return chk;
+  if (top < 0 || top > HYDRA_MAX_TOP || top > V) return HYDRA_ERR_SHAPE;
+  if ((top > 0) != (top_ids != nullptr) || (top_lp && top == 0)) return HYDRA_ERR_NULL;
+  const void* const outs[6] = {lp, lse, entropy, top_ids, top_lp, err_flag};
+  const void* const ins[2] = {logits, tokens};
+  if (!distinct(outs, ins)) return HYDRA_ERR_SHAPE;
+  if (!aligned(logits, type_align(logits_type)) || !aligned(tokens, 4)) return HYDRA_ERR_ALIGN;
+  for (const void* p : outs)
+    if (!aligned(p, 4)) return HYDRA_ERR_ALIGN;
+  const size_t need = hydra::token_logp_ws_bytes(int(M), int(V), int(top));
+  if (need > 0) {
+    if (!workspace) return HYDRA_ERR_NULL;
+    if (workspace_bytes < need) return HYDRA_ERR_WORKSPACE;
+    if (!aligned(workspace, 16)) return HYDRA_ERR_ALIGN;
+  }
+  hydra::TokenLogpArgs a{};
+  a.z = logits;
+  a.type = logits_type;
+  a.ld = ld;
+  a.tokens = tokens;
+  a.M = int(M);
+  a.V = int(V);
+  a.top = int(top);
+  a.lp = lp;
+  a.lse = lse;
+  a.entropy = entropy;
+  a.ids = top_ids;
+  a.top_lp = top_lp;
+  a.err = err_flag;
+  return from_hip(hydra::launch_token_logp(a, workspace, reinterpret_cast<hipStream_t>(stream)));
+}
+
+hydra_status hydra_token_logprobs_backward(const void* logits, hydra_dtype logits_type, int64_t ld,
+                                           const int32_t* tokens, const float* lse, const float* entropy,
+                                           const float* d_lp, const float* d_entropy, int64_t M, int64_t V,
+                                           void* d_logits, hydra_dtype d_type, int64_t ld_d, int32_t* err_flag,
+                                           void* stream) {
+  if (!logits || !lse || !d_logits || (!d_lp && !d_entropy) || (d_lp && !tokens)) return HYDRA_ERR_NULL;
+  if ((d_entropy != nullptr) != (entropy != nullptr)) return HYDRA_ERR_NULL;
+  hydra_status chk = logits_check(logits_type, ld, M, V);
+  if (chk == HYDRA_OK) chk = logits_check(d_type, ld_d, M, V);
+  if (chk != HYDRA_OK) return chk;
+  const bool over = d_logits == logits && d_type == logits_type && ld_d == ld;
+  const void* const outs[2] = {d_logits, err_flag};
+  const void* const ins[6] = {over ? nullptr : logits, tokens, lse, entropy, d_lp, d_entropy};
+  if (!distinct(outs, ins)) return HYDRA_ERR_SHAPE;
+  if (!aligned(logits, type_align(logits_type)) || !aligned(d_logits, type_align(d_type)) || !aligned(tokens, 4) ||
+      !aligned(lse, 4) || !aligned(entropy, 4) || !aligned(d_lp, 4) || !aligned(d_entropy, 4) || !aligned(err_flag, 4))
+    return HYDRA_ERR_ALIGN;
+  hydra::TokenLogpBackArgs a{};
+  a.z = logits;
+  a.type = logits_type;
+  a.ld = ld;
+  a.tokens = d_lp ? tokens : nullptr;
+  a.lse = lse;
+  a.entropy = entropy;
+  a.d_lp = d_lp;
+  a.d_entropy = d_entropy;
+  a.M = int(M);
+  a.V = int(V);
+  a.dz = d_logits;
+  a.d_type = d_type;
+  a.ld_d = ld_d;
+  a.err = err_flag;
+  return from_hip(hydra::launch_token_logp_back(a, reinterpret_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"
+
+namespace {
+
+constexpr int64_t kMaxNumel = int64_t(1) << 40;
+
+hydra_status grad_check(int64_t n, const void* const* grads, const int32_t* types, const int64_t* numels, float* norm,
+                        void* workspace, size_t workspace_bytes) {
+  if (n < 1 || n > HYDRA_MAX_GRADS) return HYDRA_ERR_SHAPE;
+  if (!grads || !types || !numels || !norm || !workspace) return HYDRA_ERR_NULL;
+  int64_t all = 0;
+  for (int64_t i = 0; i < n; ++i) {
+    if (!type_ok(types[i])) return HYDRA_ERR_UNSUPPORTED;
+    if (numels[i] < 0 || numels[i] > kMaxNumel || (all += numels[i]) > kMaxNumel) return HYDRA_ERR_SHAPE;
+    if (numels[i] == 0) continue;
+    if (!grads[i]) return HYDRA_ERR_NULL;
+    if (!aligned(grads[i], type_align(types[i]))) return HYDRA_ERR_ALIGN;
+  }
+  if (!aligned(norm, 4) || !aligned(workspace, 16)) return HYDRA_ERR_ALIGN;
+  if (workspace_bytes < hydra::grad_ws_bytes()) return HYDRA_ERR_WORKSPACE;
+  return HYDRA_OK;
+}
+
+struct Range {
+  uintptr_t lo, hi;
+};
+
+// Whether the written tensors are apart from each other and from what is read.
+// The usual lists pass in one sweep: written ranges in ascending order (the
+// views of one buffer, or buffers allocated in turn) that lie wholly on one
+// side of what is read, or are what is read.  Others are sorted (on the stack:
+// the library allocates nothing).
+bool written_apart(int64_t n, const void* const* grads, const int32_t* types, const int64_t* numels, void* const* outs,
+                   const int32_t* out_types, const Range* extra, int n_extra) {
+  Range w[HYDRA_MAX_GRADS];
+  int nw = 0;
+  bool ascending = true, in_place = true;
+  uintptr_t r_lo = ~uintptr_t(0), r_hi = 0;
+  for (int64_t i = 0; i < n; ++i) {
+    if (numels[i] == 0) continue;
+    const uintptr_t g = reinterpret_cast<uintptr_t>(grads[i]), o = outs ? reinterpret_cast<uintptr_t>(outs[i]) : g;
+    const int ot = outs ? out_types[i] : types[i];
+    const uintptr_t g_end = g + uintptr_t(numels[i]) * type_align(types[i]);
+    in_place = in_place && o == g && ot == types[i];
+    r_lo = g < r_lo ? g : r_lo;
+    r_hi = g_end > r_hi ? g_end : r_hi;
+    w[nw] = {o, o + uintptr_t(numels[i]) * type_align(ot)};
+    ascending = ascending && (nw == 0 || w[nw].lo >= w[nw - 1].hi);
+    ++nw;
+  }
+  if (!ascending) {
+    std::sort(w, w + nw, [](const Range& a, const Range& b) { return a.lo < b.lo; });
+    for (int i = 1; i < nw; ++i)
+      if (w[i].lo < w[i - 1].hi) return false;
+  }
+  // the written range that would hold the first byte at or after lo, in order
+  const auto hits = [&](uintptr_t lo, uintptr_t hi, const Range* but) {
+    const Range* p = std::lower_bound(w, w + nw, lo, [](const Range& a, uintptr_t v) { return a.hi <= v; });
+    for (; p != w + nw && p->lo < hi; ++p)
+      if (!but || p->lo != but->lo || p->hi != but->hi) return true;
+    return false;
+  };
+  for (int i = 0; i < n_extra; ++i)
+    if (extra[i].lo && hits(extra[i].lo, extra[i].hi, nullptr)) return false;
+  if (in_place || nw == 0 || w[nw - 1].hi <= r_lo || w[0].lo >= r_hi) return true;
+  for (int64_t i = 0; i < n; ++i) {
+    if (numels[i] == 0) continue;
+    const uintptr_t g = reinterpret_cast<uintptr_t>(grads[i]);
+    const Range own{g, g + uintptr_t(numels[i]) * type_align(types[i])};
+    const bool self = outs[i] == grads[i] && out_types[i] == types[i];
+    if (hits(own.lo, own.hi, self ? &own : nullptr)) return false;
+  }
+  return true;
+}
+
+}  // namespace
+
+extern "C" {
+
+hydra_status hydra_grad_norm_workspace_bytes(size_t* bytes) {
+  if (!bytes) return HYDRA_ERR_NULL;
+  *bytes = hydra::grad_ws_bytes();
+  return HYDRA_OK;
+}
+
+hydra_status hydra_grad_norm(int64_t n, const void* const* grads, const int32_t* types, const int64_t* numels,
+                             float* norm, void* workspace, size_t workspace_bytes, void* stream) {
+  const hydra_status chk = grad_check(n, grads, types, numels, norm, workspace, workspace_bytes);
+  if (chk != HYDRA_OK) return chk;
+  hydra::GradArgs a{};
+  a.n = n;
+  a.g = grads;
+  a.types = types;
+  a.numels = numels;
+  a.norm = norm;
+  return from_hip(hydra::launch_grad_norm(a, workspace, reinterpret_cast<hipStream_t>(stream)));
+}
+
+hydra_status hydra_grad_clip(int64_t n, const void* const* grads, const int32_t* types, const int64_t* numels,
+                             float max_norm, float* norm, void* const* outs, const int32_t* out_types,
+                             void* workspace, size_t workspace_bytes, int32_t* err_flag, void* stream) {
+  const hydra_status chk = grad_check(n, grads, types, numels, norm, workspace, workspace_bytes);
+  if (chk != HYDRA_OK) return chk;
+  if ((outs != nullptr) != (out_types != nullptr)) return HYDRA_ERR_NULL;
+  if (!(max_norm >= 0.f)) return HYDRA_ERR_SHAPE;
+  if (!aligned(err_flag, 4)) return HYDRA_ERR_ALIGN;
+  for (int64_t i = 0; outs && i < n; ++i) {
+    if (!type_ok(out_types[i])) return HYDRA_ERR_UNSUPPORTED;
+    if (numels[i] == 0) continue;
+    if (!outs[i]) return HYDRA_ERR_NULL;
+    if (!aligned(outs[i], type_align(out_types[i]))) return HYDRA_ERR_ALIGN;
+  }
+  if (static_cast<const void*>(err_flag) == norm) return HYDRA_ERR_SHAPE;
+  const uintptr_t pn = reinterpret_cast<uintptr_t>(norm), pe = reinterpret_cast<uintptr_t>(err_flag);
+  const Range extra[2] = {{pn, pn + 4}, {pe, pe + 4}};
+  if (!written_apart(n, grads, types, numels, outs, out_types, extra, 2)) return HYDRA_ERR_SHAPE;
+  hydra::GradArgs a{};
+  a.n = n;
+  a.g = grads;
+  a.types = types;
+  a.numels = numels;
+  a.norm = norm;
+  a.clip = true;
+  a.max_norm = max_norm;
+  a.outs = outs;
+  a.out_types = out_types;
+  a.err = err_flag;
+  return from_hip(hydra::launch_grad_norm(a, workspace, reinterpret_cast<hipStream_t>(stream)));
 }
 
 const char* hydra_status_string(hydra_status status) {

@@ -190,6 +190,91 @@ struct PpoLossArgs {
   float* d_v;            // [M] or nullptr
 };
 
+// Element types, with the values of hydra_dtype.
+enum Type : int { kBf16 = 0, kF32 = 1 };
+inline size_t type_bytes(int t) { return t == kBf16 ? 2 : 4; }
+
+// Layer norm of M rows of K values, and its backward (layer_norm.hip).
+struct LayerNormArgs {
+  const void* x;       // [M x K]
+  const void* w;       // [K] or nullptr
+  const void* b;       // [K] or nullptr
+  void* y;             // [M x K]
+  float* mean;         // [M] or nullptr
+  float* rstd;         // [M] or nullptr
+  int x_type, w_type, y_type;
+  float eps;
+  int M, K;
+};
+struct LayerNormBackArgs {
+  const void* dy;      // [M x K]
+  const void* x;       // [M x K]
+  const void* w;       // [K] or nullptr
+  const float* mean;   // [M]
+  const float* rstd;   // [M]
+  void* dx;            // [M x K] or nullptr
+  float* dw;           // [K] or nullptr
+  float* db;           // [K] or nullptr
+  int dy_type, x_type, w_type, dx_type;
+  int M, K;
+};
+size_t layer_norm_back_ws_bytes(int M, int K);
+hipError_t launch_layer_norm(const LayerNormArgs& a, hipStream_t stream);
+hipError_t launch_layer_norm_back(const LayerNormBackArgs& a, void* ws, hipStream_t stream);
+
+// Log-probabilities of given tokens, entropy and the `top` most likely tokens
+// over materialised logits, and their gradient (token_logprobs.hip).  Row m
+// starts ld elements after row m - 1.
+constexpr int kMaxTop = 32;
+struct TokenLogpArgs {
+  const void* z;
+  int type;
+  int64_t ld;
+  const int32_t* tokens;  // [M] or nullptr
+  int M, V, top;
+  float* lp;              // [M] or nullptr
+  float* lse;             // [M] or nullptr
+  float* entropy;         // [M] or nullptr
+  int32_t* ids;           // [M x top]
+  float* top_lp;          // [M x top] or nullptr
+  int32_t* err;           // optional
+};
+struct TokenLogpBackArgs {
+  const void* z;
+  int type;
+  int64_t ld;
+  const int32_t* tokens;    // [M] or nullptr
+  const float* lse;         // [M]
+  const float* entropy;     // [M] or nullptr
+  const float* d_lp;        // [M] or nullptr
+  const float* d_entropy;   // [M] or nullptr
+  int M, V;
+  void* dz;
+  int d_type;
+  int64_t ld_d;
+  int32_t* err;             // optional
+};
+size_t token_logp_ws_bytes(int M, int V, int top);
+hipError_t launch_token_logp(const TokenLogpArgs& a, void* ws, hipStream_t stream);
+hipError_t launch_token_logp_back(const TokenLogpBackArgs& a, hipStream_t stream);
+
+// The norm over many tensors, and the clipped tensors (grad_norm.hip).
+struct GradArgs {
+  int64_t n;
+  const void* const* g;
+  const int32_t* types;
+  const int64_t* numels;
+  float* norm;            // [1]
+  // clipping; outs nullptr: in place
+  bool clip;
+  float max_norm;
+  void* const* outs;
+  const int32_t* out_types;
+  int32_t* err;           // optional
+};
+size_t grad_ws_bytes();
+hipError_t launch_grad_norm(const GradArgs& a, void* ws, hipStream_t stream);
+
 // Backward of the LoRA-switchable linear with W frozen (see lora_backward.hip).
 struct BackwardArgs {
   const uint16_t* x;   // [M x K]

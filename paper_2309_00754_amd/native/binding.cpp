@@ -12,7 +12,10 @@
 #include <Python.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
+
+#include <vector>
 
 #include "../../include/hydra.h"
 
@@ -20,14 +23,16 @@ namespace {
 
 constexpr long kSlow = -1000;
 
-enum Kind { kBf16, kF32, kI32, kU8 };
+enum Kind { kBf16, kF32, kI32, kU8, kAny };  // kAny: bf16 or fp32
 
 // Collects the arguments of one call; ok turns false at the first that is not
 // of the accepted form.
 struct Take {
   bool ok = true;
+  int device = -1;           // of the tensors so far
+  bool one_device = true;
 
-  const at::Tensor* tensor(PyObject* o, Kind kind) {
+  const at::Tensor* tensor(PyObject* o, Kind kind, bool rows_apart = false) {
     if (!ok || o == Py_None) return nullptr;
     if (!THPVariable_CheckExact(o)) {
       ok = false;
@@ -38,9 +43,63 @@ struct Take {
     const bool dtype = kind == kBf16   ? d == at::kBFloat16 || d == at::kShort || d == at::kUInt16
                        : kind == kF32  ? d == at::kFloat
                        : kind == kI32  ? d == at::kInt
-                                       : d == at::kByte;
-    ok = t.is_cuda() && dtype && t.is_contiguous();
-    return ok ? &t : nullptr;
+                       : kind == kU8   ? d == at::kByte
+                                       : d == at::kBFloat16 || d == at::kFloat || d == at::kShort || d == at::kUInt16;
+    ok = t.is_cuda() && dtype && (rows_apart || t.is_contiguous());
+    if (!ok) return nullptr;
+    const int on = t.get_device();
+    one_device = one_device && (device < 0 || device == on);
+    device = on;
+    return &t;
+  }
+  static hydra_dtype type_of(const at::Tensor* t) {
+    return t && t->scalar_type() == at::kFloat ? HYDRA_F32 : HYDRA_BF16;
+  }
+  // None, or a tensor of bf16 or fp32 of this shape, and its type.
+  void* any1(PyObject* o, int64_t n, hydra_dtype& type) {
+    const at::Tensor* t = tensor(o, kAny);
+    type = type_of(t);
+    return ptr(t, t && t->dim() == 1 && t->size(0) == n);
+  }
+  void* any2(PyObject* o, int64_t n, int64_t m, hydra_dtype& type) {
+    const at::Tensor* t = tensor(o, kAny);
+    type = type_of(t);
+    return ptr(t, t && t->dim() == 2 && t->size(0) == n && t->size(1) == m);
+  }
+  // A matrix of bf16 or fp32 that has to be there, its rows contiguous and
+  // possibly apart: its sizes, type and row distance.
+  void* rows_of(PyObject* o, int64_t& M, int64_t& V, hydra_dtype& type, int64_t& ld) {
+    const at::Tensor* t = tensor(o, kAny, true);
+    if (!t || t->dim() != 2) {
+      ok = false;
+      return nullptr;
+    }
+    M = t->size(0);
+    V = t->size(1);
+    type = type_of(t);
+    ld = M > 1 ? t->stride(0) : V;
+    ok = (V <= 1 || t->stride(1) == 1) && ld >= V;
+    return t->data_ptr();
+  }
+  // None: no workspace.
+  void* maybe_workspace(PyObject* o, size_t& bytes) {
+    bytes = 0;
+    return o == Py_None ? nullptr : workspace(o, bytes);
+  }
+  // The stream of a call that goes where its tensors are: they have to be on
+  // the current device, and so has a given stream.
+  void* stream_here(PyObject* o) {
+    ok = ok && one_device && device == (int)c10::hip::current_device();
+    if (ok && o != Py_None) {
+      PyObject* d = PyObject_GetAttrString(o, "device_index");
+      ok = d && PyLong_Check(d) && PyLong_AsLong(d) == device;
+      Py_XDECREF(d);
+      if (PyErr_Occurred()) {
+        PyErr_Clear();
+        ok = false;
+      }
+    }
+    return stream(o);
   }
   // A matrix that has to be there: its sizes and pointer.
   const uint16_t* matrix(PyObject* o, int64_t& rows, int64_t& cols, Kind kind = kBf16) {
@@ -410,10 +469,155 @@ HYDRA_PY(lora_linear_backward, 11) {
   });
 }
 
+// x weight bias y mean rstd eps stream
+HYDRA_PY(layer_norm, 8) {
+  return guarded([&](Take& a) {
+    const at::Tensor* x = a.tensor(v[0], kAny);
+    a.ok = a.ok && x && x->dim() == 2;
+    const int64_t M = a.ok ? x->size(0) : 0, K = a.ok ? x->size(1) : 0;
+    const void* xp = a.ok ? x->data_ptr() : nullptr;
+    const hydra_dtype xt = Take::type_of(x);
+    hydra_dtype wt, bt, yt;
+    const void* w = a.any1(v[1], K, wt);
+    const void* b = a.any1(v[2], K, bt);
+    a.ok = a.ok && (!w || !b || wt == bt);
+    void* y = a.any2(v[3], M, K, yt);
+    float* mean = a.at1<float>(v[4], kF32, M);
+    float* rstd = a.at1<float>(v[5], kF32, M);
+    const float eps = a.real(v[6]);
+    void* st = a.stream_here(v[7]);
+    return [=]() { return hydra_layer_norm(xp, xt, w, b, w ? wt : bt, eps, M, K, y, yt, mean, rstd, st); };
+  });
+}
+
+// dy x weight mean rstd dx dweight dbias workspace stream
+HYDRA_PY(layer_norm_backward, 10) {
+  return guarded([&](Take& a) {
+    const at::Tensor* x = a.tensor(v[1], kAny);
+    a.ok = a.ok && x && x->dim() == 2;
+    const int64_t M = a.ok ? x->size(0) : 0, K = a.ok ? x->size(1) : 0;
+    const void* xp = a.ok ? x->data_ptr() : nullptr;
+    const hydra_dtype xt = Take::type_of(x);
+    hydra_dtype dyt, wt, dxt;
+    const void* dy = a.any2(v[0], M, K, dyt);
+    const void* w = a.any1(v[2], K, wt);
+    const float* mean = a.at1<float>(v[3], kF32, M);
+    const float* rstd = a.at1<float>(v[4], kF32, M);
+    void* dx = a.any2(v[5], M, K, dxt);
+    float* dw = a.at1<float>(v[6], kF32, K);
+    float* db = a.at1<float>(v[7], kF32, K);
+    size_t bytes = 0;
+    void* ws = a.workspace(v[8], bytes);
+    void* st = a.stream_here(v[9]);
+    return [=]() {
+      return hydra_layer_norm_backward(dy, dyt, xp, xt, w, wt, mean, rstd, M, K, dx, dxt, dw, db, ws, bytes, st);
+    };
+  });
+}
+
+// logits tokens lp lse entropy top_ids top_lp workspace err_flag stream
+HYDRA_PY(token_logprobs, 10) {
+  return guarded([&](Take& a) {
+    int64_t M = 0, V = 0, ld = 0, top = 0;
+    hydra_dtype zt = HYDRA_BF16;
+    const void* z = a.rows_of(v[0], M, V, zt, ld);
+    const int32_t* tok = a.at1<int32_t>(v[1], kI32, M);
+    float* lp = a.at1<float>(v[2], kF32, M);
+    float* lse = a.at1<float>(v[3], kF32, M);
+    float* ent = a.at1<float>(v[4], kF32, M);
+    const at::Tensor* ids = a.tensor(v[5], kI32);
+    if (ids && ids->dim() == 2) top = ids->size(1);
+    int32_t* idp = a.at2<int32_t>(v[5], kI32, M, top);
+    float* tlp = a.at2<float>(v[6], kF32, M, top);
+    size_t bytes = 0, need = 0;
+    void* ws = a.maybe_workspace(v[7], bytes);
+    int32_t* err = a.at1<int32_t>(v[8], kI32, 1);
+    // (one that is needed and missing, or sizes that are refused: the Python path)
+    a.ok = a.ok && (ws || (hydra_token_logprobs_workspace_bytes(M, V, top, &need) == HYDRA_OK && need == 0));
+    void* st = a.stream_here(v[9]);
+    return [=]() {
+      return hydra_token_logprobs(z, zt, ld, tok, M, V, top, lp, lse, ent, idp, tlp, ws, bytes, err, st);
+    };
+  });
+}
+
+// logits tokens lse d_logits d_lp entropy d_entropy err_flag stream
+HYDRA_PY(token_logprobs_backward, 9) {
+  return guarded([&](Take& a) {
+    int64_t M = 0, V = 0, ld = 0, dM = 0, dV = 0, ld_d = 0;
+    hydra_dtype zt = HYDRA_BF16, dt = HYDRA_BF16;
+    const void* z = a.rows_of(v[0], M, V, zt, ld);
+    void* dz = a.ok ? a.rows_of(v[3], dM, dV, dt, ld_d) : nullptr;
+    a.ok = a.ok && dM == M && dV == V;
+    const int32_t* tok = a.at1<int32_t>(v[1], kI32, M);
+    const float* lse = a.at1<float>(v[2], kF32, M);
+    const float* d_lp = a.at1<float>(v[4], kF32, M);
+    const float* ent = a.at1<float>(v[5], kF32, M);
+    const float* d_ent = a.at1<float>(v[6], kF32, M);
+    int32_t* err = a.at1<int32_t>(v[7], kI32, 1);
+    void* st = a.stream_here(v[8]);
+    return [=]() {
+      return hydra_token_logprobs_backward(z, zt, ld, tok, lse, ent, d_lp, d_ent, M, V, dz, dt, ld_d, err, st);
+    };
+  });
+}
+
+// grads max_norm (None: the norm alone) norm outs workspace err_flag stream
+HYDRA_PY(grad_clip, 7) {
+  struct Tensors {
+    std::vector<const void*> g;
+    std::vector<void*> out;
+    std::vector<int32_t> type, out_type;
+    std::vector<int64_t> numel;
+  } m;
+  return guarded([&](Take& a) {
+    const int64_t n = PyList_CheckExact(v[0]) || PyTuple_CheckExact(v[0]) ? PySequence_Fast_GET_SIZE(v[0]) : -1;
+    a.ok = n >= 1 && n <= HYDRA_MAX_GRADS;
+    const bool clip = v[1] != Py_None, own = v[3] != Py_None;
+    if (a.ok) {
+      PyObject *const *gs = a.list(v[0], n), *const *os = own ? a.list(v[3], n) : nullptr;
+      m.g.reserve(n);
+      m.type.reserve(n);
+      m.numel.reserve(n);
+      for (int64_t i = 0; a.ok && i < n; ++i) {
+        const at::Tensor* g = a.tensor(gs[i], kAny);
+        if (!g) {
+          a.ok = false;
+          break;
+        }
+        m.g.push_back(g->data_ptr());
+        m.type.push_back(Take::type_of(g));
+        m.numel.push_back(g->numel());
+        if (!own) continue;
+        const at::Tensor* o = a.tensor(os[i], kAny);
+        if (!o || o->sizes() != g->sizes()) {
+          a.ok = false;
+          break;
+        }
+        m.out.push_back(o->data_ptr());
+        m.out_type.push_back(Take::type_of(o));
+      }
+    }
+    const float max_norm = clip ? a.real(v[1]) : 0.f;
+    float* norm = a.at1<float>(v[2], kF32, 1);
+    size_t bytes = 0;
+    void* ws = a.workspace(v[4], bytes);
+    int32_t* err = a.at1<int32_t>(v[5], kI32, 1);
+    void* st = a.stream_here(v[6]);
+    return [=, &m]() {
+      if (!clip) return hydra_grad_norm(n, m.g.data(), m.type.data(), m.numel.data(), norm, ws, bytes, st);
+      return hydra_grad_clip(n, m.g.data(), m.type.data(), m.numel.data(), max_norm, norm, own ? m.out.data() : nullptr,
+                             own ? m.out_type.data() : nullptr, ws, bytes, err, st);
+    };
+  });
+}
+
 #define HYDRA_DEF(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {HYDRA_DEF(lora_linear),  HYDRA_DEF(lora_linear_group), HYDRA_DEF(lora_linear_multi),
                          HYDRA_DEF(score),        HYDRA_DEF(score_logits),      HYDRA_DEF(value_head),
                          HYDRA_DEF(ppo_advantages), HYDRA_DEF(ppo_loss),        HYDRA_DEF(lora_linear_backward),
+                         HYDRA_DEF(layer_norm),   HYDRA_DEF(layer_norm_backward), HYDRA_DEF(token_logprobs),
+                         HYDRA_DEF(token_logprobs_backward), HYDRA_DEF(grad_clip),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_hydra_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
