@@ -658,7 +658,7 @@ hydra_status hydra_token_logprobs(const void* logits, hydra_dtype logits_type, i
  *
  *   logits, logits_type, ld, tokens, M, V   as in hydra_token_logprobs
  *   lse     [M] fp32   the forward's
- *   entropy [M] fp32   the forward's (NULL iff d_entropy is)
+ *   entropy [M] fp32   the forward's (needed and read with d_entropy alone)
  *   d_lp    [M] fp32   optional (NULL: zeros; tokens may then be NULL too)
  *   d_entropy [M] fp32 optional (NULL: zeros)
  *   d_logits [M x V] bf16 or fp32 (d_type), row m at d_logits + m * ld_d

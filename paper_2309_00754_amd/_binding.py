@@ -965,8 +965,8 @@ def hydra_token_logprobs_backward(logits, tokens, lse, d_logits, d_lp=None, entr
     """Gradient of hydra_token_logprobs' lp and entropy with respect to the logits (see include/hydra.h).
 
     logits, d_logits [M,V]: bf16 (or 16-bit integer tensors holding bf16 bits) or float32, rows contiguous and possibly
-    apart (d_logits may be logits); tokens [M] int32; lse, d_lp [M] float32; entropy, d_entropy [M] float32 (both or
-    neither).  Rows whose d_lp and d_entropy are 0 get zeros.
+    apart (d_logits may be logits); tokens [M] int32; lse, d_lp [M] float32; entropy, d_entropy [M] float32 (d_entropy
+    needs entropy).  Rows whose d_lp and d_entropy are 0 get zeros.
     """
     st = (_nat or _native()).token_logprobs_backward(logits, tokens, lse, d_logits, d_lp, entropy, d_entropy, err_flag,
                                                      stream)

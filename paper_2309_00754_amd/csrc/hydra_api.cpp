@@ -991,7 +991,7 @@ hydra_status hydra_token_logprobs_backward(const void* logits, hydra_dtype logit
                                            void* d_logits, hydra_dtype d_type, int64_t ld_d, int32_t* err_flag,
                                            void* stream) {
   if (!logits || !lse || !d_logits || (!d_lp && !d_entropy) || (d_lp && !tokens)) return HYDRA_ERR_NULL;
-  if ((d_entropy != nullptr) != (entropy != nullptr)) return HYDRA_ERR_NULL;
+  if (d_entropy && !entropy) return HYDRA_ERR_NULL;
   hydra_status chk = logits_check(logits_type, ld, M, V);
   if (chk == HYDRA_OK) chk = logits_check(d_type, ld_d, M, V);
   if (chk != HYDRA_OK) return chk;

@@ -79,7 +79,7 @@ def test_token_logprobs_rejects(kw, code):
 
 @pytest.mark.parametrize("kw,code", [
     (dict(z=None), NULL), (dict(lse=None), NULL), (dict(dz=None), NULL), (dict(tok=None), NULL), (dict(ent=None), NULL),
-    (dict(dh=None), NULL), (dict(dlp=None, ent=None, dh=None), NULL),
+    (dict(dlp=None, dh=None), NULL),
     (dict(zt=2), UNSUP), (dict(dt=-1), UNSUP), (dict(M=0), SHAPE), (dict(M=(1 << 20) + 1), SHAPE), (dict(V=0), SHAPE),
     (dict(V=(1 << 21) + 1, ld=1 << 22, ldd=1 << 22), SHAPE), (dict(ld=99), SHAPE), (dict(ldd=99), SHAPE),
     (dict(ldd=1 << 31), SHAPE),
