@@ -220,10 +220,10 @@ __global__ __launch_bounds__(THREADS) void layer_norm_kernel(LayerNormArgs a, in
   }
 }
 
-// The same layout; part: one [2][K] block (dw, db) per workgroup, nullptr where
-// neither is wanted.
+// The same layout.  Workgroup i writes its part of dw at pw + i 2 K, of db at pb
+// + i 2 K (either may be null).
 template <int TD, int TX, int VEC, int NCH, int THREADS>
-__global__ __launch_bounds__(THREADS) void norm_back_kernel(LayerNormBackArgs a, float* part, int nw) {
+__global__ __launch_bounds__(THREADS) void norm_back_kernel(LayerNormBackArgs a, float* pw, float* pb, int nw) {
   // the groups' columns of dw, then of db, by place in the group: no two lanes on one bank
   __shared__ float acc[THREADS * NCH * VEC];
   __shared__ float red[2][2][kMaxWaves];
@@ -300,22 +300,23 @@ __global__ __launch_bounds__(THREADS) void norm_back_kernel(LayerNormBackArgs a,
       if (k < K) store_chunk<VEC>(orr, a.dx_type, k, f);
     }
   }
-  if (!part) return;
-  float* const p = part + (size_t)blockIdx.x * 2 * K;
   const int lanes = nw * 64, at0 = threadIdx.x - w0 * 64;
   for (int which = 0; which < 2; ++which) {
+    float* const p = which ? pb : pw;
+    if (!p) continue;
 #pragma unroll
     for (int c = 0; c < NCH; ++c)
 #pragma unroll
       for (int e = 0; e < VEC; ++e)
         acc[((group * NCH + c) * VEC + e) * lanes + at0] = which ? db[c][e] : dw[c][e];
     __syncthreads();
+    const int shift = 31 - __builtin_clz(lanes);
     for (int i = threadIdx.x; i < lanes * NCH * VEC; i += THREADS) {
-      const int ce = i / lanes, k = (ce / VEC) * step + (i & (lanes - 1)) * VEC + ce % VEC;
+      const int ce = i >> shift, k = (ce / VEC) * step + (i & (lanes - 1)) * VEC + ce % VEC;
       if (k >= K) continue;
       float v = acc[i];
       for (int g = 1; g < groups; ++g) v += acc[g * NCH * VEC * lanes + i];
-      p[which * K + k] = v;
+      p[(size_t)blockIdx.x * 2 * K + k] = v;
     }
     __syncthreads();
   }
@@ -437,14 +438,14 @@ __global__ __launch_bounds__(COL_THREADS) void norm_back_cols_kernel(LayerNormBa
 
 // ---- plans
 
-// Columns per lane: what the registers hold of x, dy, w, dw and db without
-// spilling (element by element a chunk's address takes a register too).
-template <int VEC>
-constexpr int kLane = VEC == 1 ? 16 : 32;
-template <int VEC>
-constexpr int kRegsK = kMaxWaves * 64 * kLane<VEC>;  // the longest row in registers
+// Columns per lane.  16 as far as 8 waves reach: 4096 x 4096 fp32 forward 26.9
+// us (32: 28.9; 8: 26.4 to 27.7), backward 46.6 (51.1; 49.9); bf16 forward 13.8
+// (14.6; 15.3 to 17.7), backward 32.7 (32.6; 38.1).  32 for rows of up to
+// 16384.  Element by element (rows of odd length or alignment) 16 alone: a
+// chunk's address takes a register too, and 32 spill.
+constexpr int kFew = 16, kMany = 32;
+constexpr int kFewK = kMaxWaves * 64 * kFew, kManyK = kMaxWaves * 64 * kMany;
 constexpr int FWD_THREADS = 256, BACK_THREADS = 512;
-constexpr int kCus = 256;
 
 // Waves per row: enough for `lane` columns a lane.
 int row_waves(int K, int lane) {
@@ -453,10 +454,17 @@ int row_waves(int K, int lane) {
   return nw;
 }
 
-// Workgroups of the backward (each writes a part of dw and db): one a CU.
-int back_blocks(int M, int nw) {
+// Workgroups of the backward.  Each writes a part of dw and db that
+// norm_back_sum_kernel reads again: one a CU, half as many where the rows are
+// few (M K up to 2^22: 700 x 2048 bf16 10.6 us, so 11.5; 333 x 4096 12.8, so
+// 13.8; 4096 x 2048 21.1, so 18.7), and a single one, which needs no second
+// launch, where that takes it two rounds of rows at most (8 x 2048: 7.7 us with
+// the launch).
+int back_blocks(int M, int K, int nw) {
   const int groups = BACK_THREADS / 64 / nw, want = (M + groups - 1) / groups;
-  return want < kCus ? want : kCus;
+  if (want <= 2) return 1;
+  const int most = (int64_t)M * K <= (1 << 22) ? 128 : 256;
+  return want < most ? want : most;
 }
 
 // Row chunks of the backward of long rows: about 1024 workgroups over columns and rows.
@@ -475,29 +483,51 @@ bool aligned16(std::initializer_list<const void*> ps) {
   return true;
 }
 
-template <int TX, int VEC>
-bool forward(const LayerNormArgs& a, hipStream_t stream) {
-  if (a.K > kRegsK<VEC>) return false;
-  constexpr int NCH = kLane<VEC> / VEC;
-  const int nw = row_waves(a.K, kLane<VEC>);
+// At most 1024 workgroups, which then take several rows each: 8192 x 2048 fp32 to
+// bf16 22.0 us (2048 of them: 22.5; one for each row group at 32 columns a lane: 24.5).
+template <int TX, int VEC, int LANE>
+void forward_of(const LayerNormArgs& a, hipStream_t stream) {
+  const int nw = row_waves(a.K, LANE);
   if (nw <= FWD_THREADS / 64) {
     const int groups = FWD_THREADS / 64 / nw, want = (a.M + groups - 1) / groups;
-    hipLaunchKernelGGL((layer_norm_kernel<TX, VEC, NCH, FWD_THREADS>), dim3(want < 8 * kCus ? want : 8 * kCus),
+    hipLaunchKernelGGL((layer_norm_kernel<TX, VEC, LANE / VEC, FWD_THREADS>), dim3(want < 1024 ? want : 1024),
                        dim3(FWD_THREADS), 0, stream, a, nw);
   } else {
-    hipLaunchKernelGGL((layer_norm_kernel<TX, VEC, NCH, 512>), dim3(a.M < 4 * kCus ? a.M : 4 * kCus), dim3(512), 0, stream, a,
+    hipLaunchKernelGGL((layer_norm_kernel<TX, VEC, LANE / VEC, 512>), dim3(a.M < 512 ? a.M : 512), dim3(512), 0, stream, a,
                        nw);
   }
-  return true;
 }
 
-// The number of parts written, 0 where the row does not fit.
+template <int TX, int VEC>
+bool forward(const LayerNormArgs& a, hipStream_t stream) {
+  if (a.K <= kFewK) {
+    forward_of<TX, VEC, kFew>(a, stream);
+    return true;
+  }
+  if constexpr (VEC > 1)
+    if (a.K <= kManyK) {
+      forward_of<TX, VEC, kMany>(a, stream);
+      return true;
+    }
+  return false;
+}
+
+// The number of parts written (1: straight to dw and db), 0 where the row does
+// not fit.
 template <int TD, int TX, int VEC>
 int backward(const LayerNormBackArgs& a, float* part, hipStream_t stream) {
-  if (a.K > kRegsK<VEC>) return 0;
-  const int nw = row_waves(a.K, kLane<VEC>), blocks = back_blocks(a.M, nw);
-  hipLaunchKernelGGL((norm_back_kernel<TD, TX, VEC, kLane<VEC> / VEC, BACK_THREADS>), dim3(blocks), dim3(BACK_THREADS), 0,
-                     stream, a, part, nw);
+  const bool few = a.K <= kFewK;
+  if (!few && (VEC == 1 || a.K > kManyK)) return 0;
+  const int nw = row_waves(a.K, few ? kFew : kMany), blocks = back_blocks(a.M, a.K, nw);
+  float* const pw = blocks > 1 ? part : a.dw;
+  float* const pb = blocks > 1 && part ? part + a.K : a.db;
+  if (few) {
+    hipLaunchKernelGGL((norm_back_kernel<TD, TX, VEC, kFew / VEC, BACK_THREADS>), dim3(blocks), dim3(BACK_THREADS), 0, stream,
+                       a, pw, pb, nw);
+  } else if constexpr (VEC > 1) {
+    hipLaunchKernelGGL((norm_back_kernel<TD, TX, VEC, kMany / VEC, BACK_THREADS>), dim3(blocks), dim3(BACK_THREADS), 0,
+                       stream, a, pw, pb, nw);
+  }
   return blocks;
 }
 
@@ -514,12 +544,9 @@ int backward_of(const LayerNormBackArgs& a, float* part, hipStream_t stream) {
 size_t layer_norm_back_ws_bytes(int M, int K) {
   // (whatever the types and the alignment of the call)
   size_t need = 0;
-  if (K <= kRegsK<1>) need = (size_t)back_blocks(M, row_waves(K, kLane<1>)) * 2 * K * sizeof(float);
-  if (K <= kRegsK<8>) {
-    const size_t n = (size_t)back_blocks(M, row_waves(K, kLane<8>)) * 2 * K * sizeof(float);
-    need = n > need ? n : need;
-  }
-  if (K > kRegsK<1>) {
+  if (K <= kManyK)
+    need = (size_t)back_blocks(M, K, row_waves(K, K <= kFewK ? kFew : kMany)) * 2 * K * sizeof(float);
+  if (K > kFewK) {
     int nch, rows;
     long_plan(M, K, nch, rows);
     const size_t n = sums_bytes(M) + (size_t)nch * 2 * K * sizeof(float);
@@ -546,7 +573,9 @@ hipError_t launch_layer_norm_back(const LayerNormBackArgs& a, void* ws, hipStrea
   // 16 bytes of bf16 per lane and load where both are bf16, of fp32 where one is
   const bool vec = al && a.K % (a.dy_type == kBf16 && a.x_type == kBf16 ? 8 : 4) == 0;
   int n = vec ? backward_of<4>(a, p, stream) : backward_of<1>(a, p, stream);
+  bool add = sums && n > 1;
   if (n == 0) {
+    add = sums;
     int rows;
     long_plan(a.M, a.K, n, rows);
     float2* rs = static_cast<float2*>(ws);
@@ -555,7 +584,7 @@ hipError_t launch_layer_norm_back(const LayerNormBackArgs& a, void* ws, hipStrea
     if (a.dx) hipLaunchKernelGGL(norm_back_rows_kernel, dim3(a.M), dim3(LONG_THREADS), 0, stream, a, rs);
     hipLaunchKernelGGL(norm_back_cols_kernel, dim3(cols, n), dim3(COL_THREADS), 0, stream, a, rs, part, rows);
   }
-  if (sums)
+  if (add)
     hipLaunchKernelGGL(norm_back_sum_kernel, dim3((2 * a.K + 63) / 64), dim3(SUM_WAVES * 64), 0, stream, part, n, a.K, a.dw,
                        a.db);
   return hipGetLastError();
