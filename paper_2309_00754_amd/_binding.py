@@ -997,12 +997,23 @@ def hydra_grad_norm_workspace_bytes() -> int:
     return int(out.value)
 
 
+def _grad_workspace(workspace, norm, stream):
+    """The workspace given, or one on the current stream's device where the call goes there: hundreds of tensors take
+    the Python checks a millisecond, the native ones tens of microseconds."""
+    torch = _torch()
+    if workspace is None and stream is None and isinstance(norm, torch.Tensor) and norm.is_cuda and \
+            norm.get_device() == torch.cuda.current_device():
+        return torch.empty(hydra_grad_norm_workspace_bytes(), dtype=torch.uint8, device=norm.device)
+    return workspace
+
+
 def hydra_grad_norm(grads, norm, workspace=None, stream=None) -> None:
     """norm [1] float32 = the norm over all the tensors of `grads` (see include/hydra.h).
 
     grads: a sequence of contiguous tensors of any shape, bf16 (or 16-bit integer tensors holding bf16 bits) or
     float32.  Allocates the workspace (hydra_grad_norm_workspace_bytes()) if none is given.
     """
+    workspace = _grad_workspace(workspace, norm, stream)
     st = (_nat or _native()).grad_clip(grads, None, norm, None, workspace, None, stream)
     if st == _SLOW:
         return _hydra_grad("hydra_grad_norm", grads, None, norm, None, workspace, None, stream)
@@ -1019,6 +1030,7 @@ def hydra_grad_clip(grads, max_norm: float, norm, outs=None, workspace=None, err
     """
     if max_norm is None:
         raise TypeError("max_norm must be a number")
+    workspace = _grad_workspace(workspace, norm, stream)
     st = (_nat or _native()).grad_clip(grads, max_norm, norm, outs, workspace, err_flag, stream)
     if st == _SLOW:
         return _hydra_grad("hydra_grad_clip", grads, max_norm, norm, outs, workspace, err_flag, stream)

@@ -8,11 +8,21 @@
 //    adds the squares of its chunks in 64 bits and writes its part.
 //  * grad_norm_kernel: one workgroup adds the parts.
 //  * grad_scale_kernel: every workgroup adds the parts itself (the same order:
-//    the same c), then scales its chunks.
-// Pointers and sizes travel as kernel arguments, kSegs tensors a launch.
-// Squares are formed and added in 64 bits: an fp32 product of two gradients
-// below 1e-19 or above 1e19 would leave the range, and the conversion and the
-// 64-bit FMA run beside the loads.
+//    the same c), then scales its share.  The shares run backwards, so that the
+//    first to be read are what the sums read last and the memory-side cache
+//    (256 MB) still holds, and neither these last reads nor the results take
+//    its place: every adapter of OPT-1.3b at rank 128 (453 MB) 283 us, with the
+//    results past the cache 265, backwards 254, with the reads too 229; of
+//    Llama-7B at rank 16 into bf16 (160 MB) 92, 83, 82, 79.  The sums alone run
+//    at 5.3 TB/s.
+// Pointers and sizes travel as kernel arguments, kSegs runs a launch; tensors
+// that lie side by side, as views of one buffer do, are one run.  A workgroup
+// takes an equal share of a launch's chunks, one stretch of them: chunks dealt
+// in turn, each with its own search for the tensor and its own wait, took 303
+// us where this takes 283.
+// Squares are formed and added in 64 bits: an fp32 square of a gradient below
+// 1e-19 or above 1e19 would leave the range, and the conversion and the 64-bit
+// FMA run beside the loads.
 #include "hydra_device.h"
 #include "hydra_internal.h"
 
@@ -20,34 +30,39 @@ namespace hydra {
 namespace {
 
 constexpr int GN_THREADS = 256;
-constexpr int GN_CHUNK = 16384;  // elements
-constexpr int kSegs = 120;       // (28 bytes each: below the 4 KB of arguments of a launch)
-constexpr int kMaxParts = 2048;
+constexpr int kSegs = 128;       // (28 bytes each: below the 4 KB of arguments of a launch)
+constexpr int kMaxParts = 2048;  // of all launches of a call
+constexpr int kWorkgroups = 1024;  // of a launch at most
+constexpr int kLogChunk = 11;    // elements of a chunk
 
 struct GradSegs {
   const void* g[kSegs];
   void* out[kSegs];
   int64_t numel[kSegs];
-  int chunk0[kSegs];     // first chunk of the tensor
+  int chunk0[kSegs];  // first chunk of the run
   uint8_t g_type[kSegs], out_type[kSegs];
   int n, chunks;
 };
+static_assert(sizeof(GradSegs) <= 4000, "kernel arguments");
 
 __device__ __forceinline__ float load1(const void* p, int type, int64_t i) {
   return type == kF32 ? static_cast<const float*>(p)[i] : bf16_to_f32(static_cast<const uint16_t*>(p)[i]);
 }
 
-// The tensor that chunk c belongs to.
+__device__ __forceinline__ void store1(void* p, int type, int64_t i, float v) {
+  if (type == kF32)
+    static_cast<float*>(p)[i] = v;
+  else
+    static_cast<uint16_t*>(p)[i] = f32_to_bf16_any(v);
+}
+
+// The run that chunk c belongs to: every lane compares the starts of some.
 __device__ __forceinline__ int seg_of(const GradSegs& s, int c) {
-  int lo = 0, hi = s.n - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (s.chunk0[mid] <= c)
-      lo = mid;
-    else
-      hi = mid - 1;
-  }
-  return lo;
+  const int lane = threadIdx.x & 63;
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < kSegs; i += 64) n += __popcll(__ballot(i + lane < s.n && s.chunk0[i + lane] <= c));
+  return __builtin_amdgcn_readfirstlane(n - 1);
 }
 
 // Sum over the workgroup in a fixed order, in every thread.
@@ -64,20 +79,99 @@ __device__ __forceinline__ double block_sum(double v) {
   return v;
 }
 
-__global__ __launch_bounds__(GN_THREADS) void grad_sum_kernel(GradSegs s, double* part) {
-  const int t = threadIdx.x;
-  double sum = 0.0;
-  for (int c = blockIdx.x; c < s.chunks; c += gridDim.x) {
-    const int i = seg_of(s, c);
-    const int64_t e0 = (int64_t)(c - s.chunk0[i]) * GN_CHUNK;
-    const int64_t e1 = min(s.numel[i], e0 + GN_CHUNK);
-    for (int64_t e = e0 + t; e < e1; e += GN_THREADS) {
-      const double v = (double)load1(s.g[i], s.g_type[i], e);
-      sum = fma(v, v, sum);
+// Chunks [c0, c1) of a run: elements [e0, e1), of which the whole groups of VEC
+// from b0 on start at 16-byte boundaries of g.
+struct Piece {
+  int64_t e0, e1, b0, groups;
+};
+template <int VEC>
+__device__ __forceinline__ Piece piece_of(const void* g, int64_t numel, int64_t c0, int64_t c1) {
+  constexpr int BYTES = 16 / VEC;
+  const int64_t head = (int64_t)((-reinterpret_cast<uintptr_t>(g)) & 15) / BYTES;  // before the first boundary
+  Piece p;
+  p.b0 = head + (c0 << kLogChunk);
+  p.e0 = c0 == 0 ? 0 : p.b0;
+  p.e1 = min(numel, head + (c1 << kLogChunk));
+  p.groups = p.e1 > p.b0 ? (p.e1 - p.b0) / VEC : 0;
+  return p;
+}
+
+// f(run, first chunk, end) for this workgroup's chunks: an equal share of all of
+// them, in order (k: which share).
+template <class F>
+__device__ __forceinline__ void each_piece(const GradSegs& s, int k, F f) {
+  const int64_t all = s.chunks;
+  int c = (int)(all * k / gridDim.x);
+  const int end = (int)(all * (k + 1) / gridDim.x);
+  for (int i = seg_of(s, c); c < end; ++i) {
+    const int stop = i + 1 < s.n ? min(end, s.chunk0[i + 1]) : end;
+    f(i, (int64_t)(c - s.chunk0[i]), (int64_t)(stop - s.chunk0[i]));
+    c = stop;
+  }
+}
+
+template <int T>
+__device__ __forceinline__ void unpack(const uint4& u, float (&f)[16 / (T == kF32 ? 4 : 2)]) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (T == kF32) {
+      f[i] = __uint_as_float(w[i]);
+    } else {
+      f[2 * i] = __uint_as_float(w[i] << 16);
+      f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
     }
   }
-  sum = block_sum(sum);
-  if (t == 0) part[blockIdx.x] = sum;
+}
+
+constexpr int GN_U = 8;  // 16-byte loads of a thread under way
+
+typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4_t;
+typedef __attribute__((__vector_size__(2 * sizeof(uint32_t)))) uint32_t u32x2_t;
+
+// The elements of a piece that are in no whole group: those before b0 and those
+// after the last group, fewer than 16 of each.
+template <int VEC, class F>
+__device__ __forceinline__ void edges(const Piece& p, F f) {
+  const int t = threadIdx.x;
+  const int64_t front = min(p.b0, p.e1) - p.e0, back = p.groups > 0 || p.e1 > p.b0 ? p.b0 + p.groups * VEC : p.e1;
+  if (t < front) f(p.e0 + t);
+  if (t < p.e1 - back) f(back + t);
+}
+
+template <int T>
+__device__ __forceinline__ void sum_piece(const void* g, int64_t numel, int64_t c0, int64_t c1, double (&sum)[4]) {
+  constexpr int VEC = T == kF32 ? 4 : 8;
+  const Piece p = piece_of<VEC>(g, numel, c0, c1);
+  const uint4* const v = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(g) + p.b0 * (16 / VEC));
+  for (int64_t i = threadIdx.x; i < p.groups; i += GN_THREADS * GN_U) {
+    uint4 u[GN_U];
+#pragma unroll
+    for (int q = 0; q < GN_U; ++q) u[q] = i + q * GN_THREADS < p.groups ? v[i + q * GN_THREADS] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int q = 0; q < GN_U; ++q) {
+      float f[VEC];
+      unpack<T>(u[q], f);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) sum[e & 3] = fma((double)f[e], (double)f[e], sum[e & 3]);
+    }
+  }
+  edges<VEC>(p, [&](int64_t e) {
+    const double x = (double)load1(g, T, e);
+    sum[0] = fma(x, x, sum[0]);
+  });
+}
+
+__global__ __launch_bounds__(GN_THREADS) void grad_sum_kernel(GradSegs s, double* part) {
+  double sum[4] = {0.0, 0.0, 0.0, 0.0};
+  each_piece(s, blockIdx.x, [&](int i, int64_t c0, int64_t c1) __attribute__((always_inline)) {
+    if (s.g_type[i] == kF32)
+      sum_piece<kF32>(s.g[i], s.numel[i], c0, c1, sum);
+    else
+      sum_piece<kBf16>(s.g[i], s.numel[i], c0, c1, sum);
+  });
+  const double v = block_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
+  if (threadIdx.x == 0) part[blockIdx.x] = v;
 }
 
 __device__ __forceinline__ double norm_of(const double* part, int parts) {
@@ -91,45 +185,107 @@ __global__ __launch_bounds__(GN_THREADS) void grad_norm_kernel(const double* par
   if (threadIdx.x == 0) *norm = (float)v;
 }
 
+template <int TG, int TO>
+__device__ __forceinline__ void scale_piece(const void* g, void* out, int64_t numel, int64_t c0, int64_t c1,
+                                            float c) {
+  constexpr int VEC = TG == kF32 ? 4 : 8, OB = TO == kF32 ? 4 : 2;
+  constexpr int OUT = VEC * OB < 16 ? VEC * OB : 16;  // bytes of a store
+  const Piece p = piece_of<VEC>(g, numel, c0, c1);
+  if ((reinterpret_cast<uintptr_t>(out) + p.b0 * OB) % OUT != 0) {  // (the same for every chunk of a run)
+    for (int64_t e = p.e0 + threadIdx.x; e < p.e1; e += GN_THREADS) store1(out, TO, e, load1(g, TG, e) * c);
+    return;
+  }
+  const u32x4_t* const v = reinterpret_cast<const u32x4_t*>(static_cast<const uint8_t*>(g) + p.b0 * (16 / VEC));
+  uint8_t* const o = static_cast<uint8_t*>(out) + p.b0 * OB;
+  for (int64_t i = threadIdx.x; i < p.groups; i += GN_THREADS * GN_U) {
+    u32x4_t u[GN_U];
+#pragma unroll
+    for (int q = 0; q < GN_U; ++q)
+      u[q] = i + q * GN_THREADS < p.groups ? __builtin_nontemporal_load(v + i + q * GN_THREADS) : u32x4_t{0, 0, 0, 0};
+#pragma unroll
+    for (int q = 0; q < GN_U; ++q) {
+      const int64_t k = i + q * GN_THREADS;
+      if (k >= p.groups) break;
+      float f[VEC];
+      unpack<TG>(__builtin_bit_cast(uint4, u[q]), f);
+      uint32_t w[VEC * OB / 4];
+#pragma unroll
+      for (int e = 0; e < VEC * OB / 4; ++e) {
+        if constexpr (TO == kF32)
+          w[e] = __float_as_uint(f[e] * c);
+        else
+          w[e] = (uint32_t)f32_to_bf16_any(f[2 * e] * c) | ((uint32_t)f32_to_bf16_any(f[2 * e + 1] * c) << 16);
+      }
+      if constexpr (VEC * OB == 8) {
+        __builtin_nontemporal_store(u32x2_t{w[0], w[1]}, reinterpret_cast<u32x2_t*>(o) + k);
+      } else {
+#pragma unroll
+        for (int e = 0; e < VEC * OB / 16; ++e)
+          __builtin_nontemporal_store(u32x4_t{w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]},
+                                      reinterpret_cast<u32x4_t*>(o) + k * (VEC * OB / 16) + e);
+      }
+    }
+  }
+  edges<VEC>(p, [&](int64_t e) { store1(out, TO, e, load1(g, TG, e) * c); });
+}
+
 __global__ __launch_bounds__(GN_THREADS) void grad_scale_kernel(GradSegs s, const double* part, int parts,
                                                                 float max_norm, float* norm, int32_t* err) {
-  const int t = threadIdx.x;
   const double v = norm_of(part, parts);
   const bool finite = (float)v <= 3.4028235e38f;
   const float c = finite && v > (double)max_norm ? (float)((double)max_norm / v) : 1.f;
-  if (norm && blockIdx.x == 0 && t == 0) {
+  if (norm && blockIdx.x == 0 && threadIdx.x == 0) {
     *norm = (float)v;
     if (!finite && err) atomicOr(err, 1);
   }
-  for (int k = blockIdx.x; k < s.chunks; k += gridDim.x) {
-    const int i = seg_of(s, k);
-    if (c == 1.f && s.out[i] == s.g[i]) continue;
-    const int64_t e0 = (int64_t)(k - s.chunk0[i]) * GN_CHUNK;
-    const int64_t e1 = min(s.numel[i], e0 + GN_CHUNK);
-    for (int64_t e = e0 + t; e < e1; e += GN_THREADS) {
-      const float v = load1(s.g[i], s.g_type[i], e) * c;
+  each_piece(s, gridDim.x - 1 - blockIdx.x, [&](int i, int64_t c0, int64_t c1) __attribute__((always_inline)) {
+    const void* const g = s.g[i];
+    void* const out = s.out[i];
+    const int64_t numel = s.numel[i];
+    if (c == 1.f && out == g) return;
+    if (s.g_type[i] == kF32) {
       if (s.out_type[i] == kF32)
-        static_cast<float*>(s.out[i])[e] = v;
+        scale_piece<kF32, kF32>(g, out, numel, c0, c1, c);
       else
-        static_cast<uint16_t*>(s.out[i])[e] = f32_to_bf16_any(v);
+        scale_piece<kF32, kBf16>(g, out, numel, c0, c1, c);
+    } else {
+      if (s.out_type[i] == kF32)
+        scale_piece<kBf16, kF32>(g, out, numel, c0, c1, c);
+      else
+        scale_piece<kBf16, kBf16>(g, out, numel, c0, c1, c);
     }
-  }
+  });
 }
 
-// The next tensors of the list, from i on (empty ones left out).
+// The next runs of the list, from tensor i on (empty tensors left out, tensors
+// side by side joined).
 int64_t take(const GradArgs& a, int64_t i, GradSegs& s) {
-  s.n = s.chunks = 0;
-  for (; i < a.n && s.n < kSegs; ++i) {
+  s.n = 0;
+  for (; i < a.n; ++i) {
     if (a.numels[i] == 0) continue;
-    const int64_t chunks = (a.numels[i] + GN_CHUNK - 1) / GN_CHUNK;
+    const uint8_t gt = (uint8_t)a.types[i], ot = a.clip && a.outs ? (uint8_t)a.out_types[i] : gt;
+    void* const out = a.clip && a.outs ? a.outs[i] : const_cast<void*>(a.g[i]);
+    if (s.n > 0) {
+      const int p = s.n - 1;
+      if (s.g_type[p] == gt && s.out_type[p] == ot &&
+          static_cast<const uint8_t*>(s.g[p]) + s.numel[p] * type_bytes(gt) == a.g[i] &&
+          static_cast<uint8_t*>(s.out[p]) + s.numel[p] * type_bytes(ot) == out) {
+        s.numel[p] += a.numels[i];
+        continue;
+      }
+    }
+    if (s.n == kSegs) break;
     s.g[s.n] = a.g[i];
-    s.out[s.n] = a.clip ? (a.outs ? a.outs[i] : const_cast<void*>(a.g[i])) : nullptr;
+    s.out[s.n] = out;
     s.numel[s.n] = a.numels[i];
-    s.g_type[s.n] = (uint8_t)a.types[i];
-    s.out_type[s.n] = (uint8_t)(a.outs ? a.out_types[i] : a.types[i]);
-    s.chunk0[s.n] = s.chunks;
-    s.chunks += (int)chunks;
+    s.g_type[s.n] = gt;
+    s.out_type[s.n] = ot;
     ++s.n;
+  }
+  s.chunks = 0;
+  for (int k = 0; k < s.n; ++k) {
+    s.chunk0[k] = s.chunks;
+    s.chunks += (int)((s.numel[k] + (int64_t(1) << kLogChunk) - 1) >> kLogChunk);
   }
   return i;
 }
@@ -140,29 +296,30 @@ size_t grad_ws_bytes() { return kMaxParts * sizeof(double); }
 
 hipError_t launch_grad_norm(const GradArgs& a, void* ws, hipStream_t stream) {
   double* part = static_cast<double*>(ws);
-  const int launches = (int)((a.n + kSegs - 1) / kSegs);
-  const int most = kMaxParts / launches < 1024 ? kMaxParts / launches : 1024;
   GradSegs s;
-  int parts = 0;
+  int64_t first[kMaxGrads / kSegs + 1];  // tensor that each launch starts with
+  int runs = 0, parts = 0;
   for (int64_t i = 0; i < a.n;) {
+    first[runs] = i;
     i = take(a, i, s);
-    if (s.chunks == 0) continue;
+    if (s.n > 0) ++runs;
+  }
+  const int most = runs > 2 ? kMaxParts / runs : kWorkgroups;
+  for (int r = 0; r < runs; ++r) {
+    if (runs > 1) take(a, first[r], s);
     const int grid = s.chunks < most ? s.chunks : most;
     hipLaunchKernelGGL(grad_sum_kernel, dim3(grid), dim3(GN_THREADS), 0, stream, s, part + parts);
     parts += grid;
   }
-  if (!a.clip || parts == 0) {
+  if (!a.clip || runs == 0) {
     hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(GN_THREADS), 0, stream, part, parts, a.norm);
     return hipGetLastError();
   }
-  bool first = true;
-  for (int64_t i = 0; i < a.n;) {
-    i = take(a, i, s);
-    if (s.chunks == 0) continue;
-    const int grid = s.chunks < 2048 ? s.chunks : 2048;
+  for (int r = runs - 1; r >= 0; --r) {
+    if (runs > 1) take(a, first[r], s);
+    const int grid = s.chunks < kWorkgroups ? s.chunks : kWorkgroups;
     hipLaunchKernelGGL(grad_scale_kernel, dim3(grid), dim3(GN_THREADS), 0, stream, s, part, parts, a.max_norm,
-                       first ? a.norm : nullptr, a.err);
-    first = false;
+                       r == 0 ? a.norm : nullptr, a.err);
   }
   return hipGetLastError();
 }

@@ -226,6 +226,7 @@ hipError_t launch_layer_norm_back(const LayerNormBackArgs& a, void* ws, hipStrea
 // over materialised logits, and their gradient (token_logprobs.hip).  Row m
 // starts ld elements after row m - 1.
 constexpr int kMaxTop = 32;
+constexpr int kMaxGrads = 4096;  // tensors of a gradient norm
 struct TokenLogpArgs {
   const void* z;
   int type;
