@@ -611,8 +611,8 @@ hydra_status hydra_layer_norm_backward(const void* dy, hydra_dtype dy_type, cons
  * hydra_token_logprobs_workspace_bytes -- device workspace that
  * hydra_token_logprobs needs for M rows, a vocabulary of V and `top`
  * alternatives (writes *bytes; 0 when none is needed).  HYDRA_ERR_NULL for a NULL `bytes`,
- * HYDRA_ERR_SHAPE for M outside [1, 2^20], V outside [1, 2^21] or top outside
- * [0, min(V, HYDRA_MAX_TOP)].
+ * HYDRA_ERR_SHAPE for M outside [1, 2^20], V outside [1, 2^21], M V above 2^38
+ * or top outside [0, min(V, HYDRA_MAX_TOP)].
  */
 hydra_status hydra_token_logprobs_workspace_bytes(int64_t M, int64_t V, int64_t top, size_t* bytes);
 
@@ -642,7 +642,7 @@ hydra_status hydra_token_logprobs_workspace_bytes(int64_t M, int64_t V, int64_t 
  * and log-probability -inf; a row of nothing else has lse -inf and NaN lp,
  * entropy and top_lp (top_ids 0, 1, ...).  In a row that holds NaN or +inf lp, lse, entropy and
  * top_lp are NaN (top_ids then take NaN first, then +inf).  Sums and maxima are
- * fp32.  Requires 1 <= M <= 2^20, 1 <= V <= 2^21,
+ * fp32.  Requires 1 <= M <= 2^20, 1 <= V <= 2^21, M V <= 2^38,
  * ld <= 2^31 - 1; logits need their element's alignment only.  Outputs distinct (HYDRA_ERR_SHAPE).
  */
 hydra_status hydra_token_logprobs(const void* logits, hydra_dtype logits_type, int64_t ld, const int32_t* tokens,

@@ -928,9 +928,15 @@ hydra_status hydra_layer_norm_backward(const void* dy, hydra_dtype dy_type, cons
 
 namespace {
 
+// Logits are at most what the card's memory could hold in bf16, which keeps the
+// workgroups of a launch (one per row and 57344 logits) within a dispatch.
+bool logits_shape_ok(int64_t M, int64_t V) {
+  return M >= 1 && M <= kMaxRows && V >= 1 && V <= kMaxCols && M * V <= (int64_t(1) << 38);
+}
+
 hydra_status logits_check(int type, int64_t ld, int64_t M, int64_t V) {
   if (!type_ok(type)) return HYDRA_ERR_UNSUPPORTED;
-  if (M < 1 || M > kMaxRows || V < 1 || V > kMaxCols || ld < V || ld > kMaxDim) return HYDRA_ERR_SHAPE;
+  if (!logits_shape_ok(M, V) || ld < V || ld > kMaxDim) return HYDRA_ERR_SHAPE;
   return HYDRA_OK;
 }
 
@@ -940,8 +946,7 @@ extern "C" {
 
 hydra_status hydra_token_logprobs_workspace_bytes(int64_t M, int64_t V, int64_t top, size_t* bytes) {
   if (!bytes) return HYDRA_ERR_NULL;
-  if (M < 1 || M > kMaxRows || V < 1 || V > kMaxCols || top < 0 || top > HYDRA_MAX_TOP || top > V)
-    return HYDRA_ERR_SHAPE;
+  if (!logits_shape_ok(M, V) || top < 0 || top > HYDRA_MAX_TOP || top > V) return HYDRA_ERR_SHAPE;
   *bytes = hydra::token_logp_ws_bytes(int(M), int(V), int(top));
   return HYDRA_OK;
 }

@@ -7,11 +7,20 @@
 //   H = ln S - W / S,  W = sum_j e^(z_j - m) (z_j - m)
 //   dz_j = d_lp ([j == token] - p_j) - d_H p_j (ln p_j + H), p_j = e^(z_j - lse)
 //
-//  * token_logp_kernel: one workgroup per row keeps a running (m, S, W) per
-//    thread and joins them in a fixed tree; the alternatives are extracted one
-//    after the other, each by a maximum over the workgroup.
-//  * token_logp_back_kernel: a workgroup per row; a row without a gradient is
-//    filled with zeros unread.
+//  * token_logp_kernel: a workgroup per row, or per segment of a long one,
+//    reads it once in 16-byte groups, each thread with a running (m, S, W); the
+//    threads meet in a fixed tree.  For the alternatives it keeps the maximum
+//    of every group in LDS.
+//  * token_logp_join_kernel: one wave per row joins the segments.
+//  * token_logp_back_kernel: a workgroup per stretch of a row; rows without a
+//    gradient are filled with zeros unread.
+//
+// The k largest of a row: every wave finds the j-th largest of its threads'
+// maxima, j = k over the waves; the smallest of these is a bound that at least
+// k logits reach.  The groups whose maximum reaches it are read again (from the
+// cache), and what reaches it there, some tens of logits, is ranked by counting.
+// Ties, masks and values out of order can leave too many for that: then the k
+// are extracted one after the other.
 #include "hydra_device.h"
 #include "hydra_internal.h"
 
@@ -20,18 +29,49 @@ namespace {
 
 constexpr int TL_THREADS = 512;
 constexpr int TL_WAVES = TL_THREADS / 64;
+constexpr int TL_U = 4;             // 16-byte loads of a thread under way
+constexpr int kSegMost = 57344;     // elements of a segment (its groups' maxima, 4 bytes each, beside 6 KB in 64 KB of LDS)
+constexpr int kSegs = 64;           // segments of a row at most
+constexpr int kCand = 512;          // logits ranked by counting at most
 
-__device__ __forceinline__ float load_z(const void* p, int type, size_t i) {
-  return type == kF32 ? static_cast<const float*>(p)[i] : bf16_to_f32(static_cast<const uint16_t*>(p)[i]);
+template <int T>
+constexpr int kVec = T == kF32 ? 4 : 8;  // elements of 16 bytes
+
+template <int T>
+__device__ __forceinline__ float load_z(const void* p, size_t i) {
+  return T == kF32 ? static_cast<const float*>(p)[i] : bf16_to_f32(static_cast<const uint16_t*>(p)[i]);
+}
+
+template <int T>
+__device__ __forceinline__ void unpack(const uint4& u, float (&f)[kVec<T>]) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (T == kF32) {
+      f[i] = __uint_as_float(w[i]);
+    } else {
+      f[2 * i] = __uint_as_float(w[i] << 16);
+      f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+  }
+}
+
+// Elements before the first 16-byte boundary of a row.
+template <int T>
+__device__ __forceinline__ int head_of(const void* row, int V) {
+  return min(V, (int)((-reinterpret_cast<uintptr_t>(row)) & 15) / (16 / kVec<T>));
 }
 
 // A whole number that orders logits by value, then by index (the lower one the
-// greater): NaN first, then +inf.  +0 and -0 are one value.
+// greater): NaN first, then +inf.  +0 and -0 are one value.  No logit gives 0.
 __device__ __forceinline__ uint64_t order_key(float z, int idx) {
   const uint32_t u = __float_as_uint(z + 0.f);
   const uint32_t o = z != z ? 0xFFFFFFFEu : (int)u < 0 ? ~u : u | 0x80000000u;
   return ((uint64_t)o << 32) | (uint32_t)~idx;
 }
+__device__ __forceinline__ int index_of(uint64_t key) { return (int)~(uint32_t)key; }
+// (of -inf and below: masked out, or no logit)
+__device__ __forceinline__ bool masked_out(uint64_t key) { return (uint32_t)(key >> 32) <= 0x007FFFFFu; }
 
 // The statistics of a part of a row.  Differences to the maximum are formed
 // before anything else is done with them, so that logits up to the type's
@@ -52,33 +92,59 @@ __device__ __forceinline__ void rescale(Stat& a, float m) {
   a.m = m;
 }
 
-__device__ __forceinline__ void absorb(Stat& a, float z) {
-  rescale(a, fmaxf(a.m, z));
-  if (z == -INFINITY) return;
-  const float d = z - a.m, e = exp_e(d);
-  a.s += e;
-  a.w = fmaf(e, fmaxf(d, kFar), a.w);
+// n logits whose maximum (NaN aside) is `most`.
+template <int N>
+__device__ __forceinline__ void absorb(Stat& a, const float (&z)[N], float most) {
+  rescale(a, fmaxf(a.m, most));
+  if (a.m == -INFINITY) {  // nothing but -inf so far, or NaN
+#pragma unroll
+    for (int i = 0; i < N; ++i) a.s += z[i] == -INFINITY ? 0.f : z[i];
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float d = z[i] - a.m, e = exp_e(d);
+    a.s += e;
+    a.w = fmaf(e, fmaxf(d, kFar), a.w);
+  }
+}
+
+template <bool MAX>
+__device__ __forceinline__ float combine(float a, float b) {
+  return MAX ? fmaxf(a, b) : a + b;
+}
+
+// Maximum or sum over the wave's lanes in a fixed order, in every lane: each row
+// of 16 lanes by shifts, then the rows one after the other.
+template <bool MAX>
+__device__ __forceinline__ float wave_all(float v) {
+  const uint32_t none = __float_as_uint(MAX ? -INFINITY : 0.f);
+#define HYDRA_DPP(ctrl, rows) \
+  v = combine<MAX>(v, __uint_as_float(__builtin_amdgcn_update_dpp(none, __float_as_uint(v), ctrl, rows, 0xF, false)))
+  HYDRA_DPP(0x111, 0xF);
+  HYDRA_DPP(0x112, 0xF);
+  HYDRA_DPP(0x114, 0xF);
+  HYDRA_DPP(0x118, 0xF);
+  HYDRA_DPP(0x142, 0xA);
+  HYDRA_DPP(0x143, 0xC);
+#undef HYDRA_DPP
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
 }
 
 __device__ __forceinline__ Stat block_stat(Stat a) {
   __shared__ float red[3][TL_WAVES];
-  const int t = threadIdx.x;
-  float m = a.m;
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-  if ((t & 63) == 0) red[0][t >> 6] = m;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  float m = wave_all<true>(a.m);
+  if (lane == 0) red[0][wave] = m;
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < TL_WAVES; ++i) m = fmaxf(m, red[0][i]);
   rescale(a, m);
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) {
-    a.s += __shfl_xor(a.s, o);
-    a.w += __shfl_xor(a.w, o);
-  }
-  if ((t & 63) == 0) {
-    red[1][t >> 6] = a.s;
-    red[2][t >> 6] = a.w;
+  a.s = wave_all<false>(a.s);
+  a.w = wave_all<false>(a.w);
+  if (lane == 0) {
+    red[1][wave] = a.s;
+    red[2][wave] = a.w;
   }
   __syncthreads();
   a.s = red[1][0];
@@ -109,84 +175,388 @@ __device__ __forceinline__ uint64_t block_max(uint64_t v) {
 
 // lp of a logit, by way of the maximum: of the rounding of lse that of ln S
 // alone remains.
-__device__ __forceinline__ float logp_of(float z, const Stat& a, float ln_s) { return (z - a.m) - ln_s; }
+__device__ __forceinline__ float logp_of(float z, float m, float ln_s) { return (z - m) - ln_s; }
 
-__global__ __launch_bounds__(TL_THREADS) void token_logp_kernel(TokenLogpArgs a) {
-  const int row = blockIdx.x, t = threadIdx.x, V = a.V;
-  const size_t r0 = (size_t)row * a.ld;
-  Stat st{-INFINITY, 0.f, 0.f};
-  for (int j = t; j < V; j += TL_THREADS) absorb(st, load_z(a.z, a.type, r0 + j));
-  st = block_stat(st);
+// One thread: the row's statistics.
+template <int T>
+__device__ __forceinline__ void finish_row(const TokenLogpArgs& a, int row, const Stat& st) {
   const float ln_s = log_e(st.s);
-  if (t == 0) {
-    if (a.lse) a.lse[row] = st.m + ln_s;
-    if (a.entropy) a.entropy[row] = ln_s - st.w / st.s;
-    if (a.lp) {
-      const int tk = a.tokens[row];
-      const bool ok = tk >= 0 && tk < V;
-      a.lp[row] = ok ? logp_of(load_z(a.z, a.type, r0 + tk), st, ln_s) : __builtin_nanf("");
-      if (!ok && a.err) atomicOr(a.err, 1);
-    }
-  }
-  uint64_t last = ~0ull;
-  for (int r = 0; r < a.top; ++r) {
-    uint64_t best = 0;
-    for (int j = t; j < V; j += TL_THREADS) {
-      const uint64_t k = order_key(load_z(a.z, a.type, r0 + j), j);
-      best = k < last && k > best ? k : best;
-    }
-    last = block_max(best);
-    if (t == 0) {
-      const int id = (int)~(uint32_t)last;
-      a.ids[(size_t)row * a.top + r] = id;
-      if (a.top_lp) a.top_lp[(size_t)row * a.top + r] = logp_of(load_z(a.z, a.type, r0 + id), st, ln_s);
-    }
+  if (a.lse) a.lse[row] = st.m + ln_s;
+  if (a.entropy) a.entropy[row] = ln_s - st.w / st.s;
+  if (a.lp) {
+    const int tk = a.tokens[row];
+    const bool ok = tk >= 0 && tk < a.V;
+    a.lp[row] = ok ? logp_of(load_z<T>(a.z, (size_t)row * a.ld + tk), st.m, ln_s) : __builtin_nanf("");
+    if (!ok && a.err) atomicOr(a.err, 1);
   }
 }
 
-__global__ __launch_bounds__(TL_THREADS) void token_logp_back_kernel(TokenLogpBackArgs a) {
-  const int row = blockIdx.x, t = threadIdx.x, V = a.V;
-  const size_t r0 = (size_t)row * a.ld, d0 = (size_t)row * a.ld_d;
-  const float d_lp = a.d_lp ? a.d_lp[row] : 0.f, d_h = a.d_entropy ? a.d_entropy[row] : 0.f;
-  const bool live = d_lp != 0.f || d_h != 0.f;
-  int tk = -1;
-  float lse = 0.f, h = 0.f, scale = 1.f;
-  if (live) {
-    lse = a.lse[row];
-    h = d_h != 0.f ? a.entropy[row] : 0.f;
+// One wave: the row's alternatives from the n keys at `key` (LDS), which hold
+// all logits of the first k that are not masked out.
+template <int T>
+__device__ __forceinline__ void finish_top(const TokenLogpArgs& a, int row, const Stat& st, const uint64_t* key, int n) {
+  const int lane = threadIdx.x & 63, k = a.top;
+  const size_t r0 = (size_t)row * a.ld, o0 = (size_t)row * k;
+  const float ln_s = log_e(st.s);
+  for (int i = lane; i < n; i += 64) {
+    const uint64_t mine = key[i];
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += key[j] > mine;
+    if (rank < k) {
+      const int id = index_of(mine);
+      a.ids[o0 + rank] = id;
+      if (a.top_lp) a.top_lp[o0 + rank] = logp_of(load_z<T>(a.z, r0 + id), st.m, ln_s);
+    }
+  }
+  if (n >= k) return;
+  // Fewer than k <= 32 logits are not masked out: of the first 64 entries (or of
+  // all, at least k) enough are.
+  const bool out = lane < a.V && load_z<T>(a.z, r0 + lane) == -INFINITY;
+  const uint64_t outs = __ballot(out);
+  const int rank = n + __popcll(outs & ((1ull << lane) - 1));
+  if (out && rank < k) {
+    a.ids[o0 + rank] = lane;
+    if (a.top_lp) a.top_lp[o0 + rank] = logp_of(-INFINITY, st.m, ln_s);
+  }
+}
+
+// Partial results of a segment in the workspace: all statistics [M][nseg], then
+// all keys [M][nseg][top], the greatest first, 0 behind the last.
+struct Parts {
+  Stat* stat;
+  uint64_t* key;
+};
+
+// The groups (of kVec elements from the first boundary on) of a segment.
+struct Span {
+  int head, g0, g1;    // elements before the first group; the segment's groups
+  int tail0;           // elements [tail0, V) behind the last group
+  bool first, last;
+};
+template <int T>
+__device__ __forceinline__ Span span_of(const void* row, int V, int seg, int nseg) {
+  constexpr int VEC = kVec<T>;
+  Span s;
+  s.head = head_of<T>(row, V);
+  const int groups = (V - s.head) / VEC, per = (groups + nseg - 1) / nseg;
+  s.g0 = min(groups, seg * per);
+  s.g1 = min(groups, s.g0 + per);
+  s.tail0 = s.head + groups * VEC;
+  s.first = seg == 0;
+  s.last = seg == nseg - 1;
+  return s;
+}
+
+// Grid: M * nseg workgroups.
+template <int T, bool TOP>
+__global__ __launch_bounds__(TL_THREADS) void token_logp_kernel(TokenLogpArgs a, int nseg, Parts parts) {
+  constexpr int VEC = kVec<T>;
+  extern __shared__ float most_of[];  // TOP: the maxima of the segment's groups
+  const int row = blockIdx.x / nseg, seg = blockIdx.x - row * nseg, t = threadIdx.x, V = a.V;
+  const uint8_t* const z = static_cast<const uint8_t*>(a.z) + (size_t)row * a.ld * (16 / VEC);
+  const Span sp = span_of<T>(z, V, seg, nseg);
+  const uint4* const v = reinterpret_cast<const uint4*>(z + (size_t)sp.head * (16 / VEC));
+  Stat st{-INFINITY, 0.f, 0.f};
+  for (int g = sp.g0 + t; g < sp.g1; g += TL_THREADS * TL_U) {
+    uint4 u[TL_U];
+#pragma unroll
+    for (int q = 0; q < TL_U; ++q)
+      if (g + q * TL_THREADS < sp.g1) u[q] = v[g + q * TL_THREADS];
+#pragma unroll
+    for (int q = 0; q < TL_U; ++q) {
+      if (g + q * TL_THREADS >= sp.g1) break;
+      float f[VEC];
+      unpack<T>(u[q], f);
+      float most = f[0];
+#pragma unroll
+      for (int e = 1; e < VEC; ++e) most = fmaxf(most, f[e]);
+      if constexpr (TOP) most_of[g + q * TL_THREADS - sp.g0] = most;
+      absorb(st, f, most);
+    }
+  }
+  // the elements in no group: a thread each
+  float edge = -INFINITY;
+  int edge_at = -1;
+  if (sp.first && t < sp.head) edge_at = t;
+  if (sp.last && t >= 64 && t - 64 < V - sp.tail0) edge_at = sp.tail0 + t - 64;
+  if (edge_at >= 0) {
+    const float f[1] = {edge = load_z<T>(z, edge_at)};
+    absorb(st, f, edge);
+  }
+  const float mine = st.m;
+  st = block_stat(st);
+  if (nseg == 1) {
+    if (t == 0) finish_row<T>(a, row, st);
+  } else if (t == 0) {
+    parts.stat[blockIdx.x] = st;
+  }
+  if constexpr (TOP) {
+    __shared__ uint64_t cand[kCand];
+    __shared__ float bound_of[TL_WAVES];
+    __shared__ int slot[kCand], count[2];
+    const int lane = t & 63, wave = t >> 6, k = a.top, groups = sp.g1 - sp.g0;
+    int n = kCand + 1;  // too many
+    if (st.s >= 0.f && st.m != INFINITY) {  // (no NaN and no +inf)
+      // waves that have a group, and the bound
+      const int waves = min(TL_WAVES, (groups + 63) / 64), j = waves > 0 ? (k + waves - 1) / waves : 0;
+      float left = mine, bound = -INFINITY;
+      if (wave < waves)
+        for (int i = 0; i < j; ++i) {
+          bound = wave_all<true>(left);
+          const uint64_t have = __ballot(left == bound);
+          if (lane == __ffsll((unsigned long long)have) - 1) left = -INFINITY;
+        }
+      if (t < 2) count[t] = 0;
+      if (lane == 0) bound_of[wave] = bound;
+      __syncthreads();
+      bound = bound_of[0];
+      for (int i = 1; i < waves; ++i) bound = fminf(bound, bound_of[i]);
+      const auto reaches = [&](float x) __attribute__((always_inline)) { return x >= bound && x != -INFINITY; };
+      for (int g = t; g < groups; g += TL_THREADS)
+        if (reaches(most_of[g])) {
+          const int i = atomicAdd(&count[0], 1);
+          if (i < kCand) slot[i] = g;
+        }
+      if (edge_at >= 0 && reaches(edge)) cand[atomicAdd(&count[1], 1)] = order_key(edge, edge_at);
+      __syncthreads();
+      const int slots = count[0];
+      if (slots <= kCand) {
+        for (int i = t; i < slots * VEC; i += TL_THREADS) {
+          const int e = sp.head + (sp.g0 + slot[i / VEC]) * VEC + i % VEC;
+          const float x = load_z<T>(z, e);
+          if (reaches(x)) {
+            const int p = atomicAdd(&count[1], 1);
+            if (p < kCand) cand[p] = order_key(x, e);
+          }
+        }
+        __syncthreads();
+        n = count[1];
+      }
+      __syncthreads();
+    }
+    if (n > kCand) {
+      // one after the other: each thread's greatest below the last one
+      uint64_t last = ~0ull;
+      for (n = 0; n < k; ++n) {
+        uint64_t best = 0;
+        const auto see = [&](int e) __attribute__((always_inline)) {
+          const uint64_t key = order_key(load_z<T>(z, e), e);
+          best = key < last && key > best ? key : best;
+        };
+        for (int e = sp.head + sp.g0 * VEC + t; e < sp.head + sp.g1 * VEC; e += TL_THREADS) see(e);
+        if (edge_at >= 0) see(edge_at);
+        last = block_max(best);
+        if (masked_out(last)) break;
+        if (t == 0) cand[n] = last;
+      }
+      __syncthreads();
+    }
+    if (wave != 0) return;
+    if (nseg == 1) {
+      finish_top<T>(a, row, st, cand, n);
+      return;
+    }
+    uint64_t* const out = parts.key + (size_t)blockIdx.x * k;
+    for (int i = lane; i < n; i += 64) {
+      const uint64_t me = cand[i];
+      int rank = 0;
+      for (int q = 0; q < n; ++q) rank += cand[q] > me;
+      if (rank < k) out[rank] = me;
+    }
+    for (int i = n + lane; i < k; i += 64) out[i] = 0;
+  }
+}
+
+// One wave per row.
+template <int T>
+__global__ __launch_bounds__(64) void token_logp_join_kernel(TokenLogpArgs a, int nseg, Parts parts) {
+  __shared__ uint64_t cand[kSegs * kMaxTop];
+  const int row = blockIdx.x, lane = threadIdx.x, k = a.top;
+  const Stat* const ps = parts.stat + (size_t)row * nseg;
+  Stat st{-INFINITY, 0.f, 0.f};
+  if (lane < nseg) st = ps[lane];
+  rescale(st, wave_all<true>(st.m));
+  st.s = wave_all<false>(st.s);
+  st.w = wave_all<false>(st.w);
+  if (lane == 0) finish_row<T>(a, row, st);
+  if (k == 0) return;
+  // what reaches the greatest of the segments' k-th keys
+  const uint64_t* const pk = parts.key + (size_t)row * nseg * k;
+  uint64_t bound = lane < nseg ? pk[lane * k + k - 1] : 0;
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) {
+    const uint64_t u = __shfl_xor((unsigned long long)bound, o);
+    bound = u > bound ? u : bound;
+  }
+  int n = 0;
+  for (int i = lane; i - lane < nseg * k; i += 64) {
+    const uint64_t key = i < nseg * k ? pk[i] : 0;
+    const bool in = key != 0 && key >= bound;
+    const uint64_t ins = __ballot(in);
+    if (in) cand[n + __popcll(ins & ((1ull << lane) - 1))] = key;
+    n += __popcll(ins);
+  }
+  __syncthreads();
+  finish_top<T>(a, row, st, cand, n);
+}
+
+// ---- gradient
+
+constexpr int TB_THREADS = 256;
+constexpr int TB_U = 4;
+
+// Stretches of `per` groups; workgroup b takes stretches b, b + gridDim.x, ...
+// of the M * n of all rows.
+template <int TZ, int TD>
+__global__ __launch_bounds__(TB_THREADS) void token_logp_back_kernel(TokenLogpBackArgs a, int n, int per) {
+  constexpr int VEC = kVec<TZ>, ZB = 16 / VEC, DB = TD == kF32 ? 4 : 2;
+  constexpr int STORE = VEC * DB < 16 ? VEC * DB : 16;  // bytes
+  const int t = threadIdx.x, V = a.V;
+  for (int64_t b = blockIdx.x; b < (int64_t)a.M * n; b += gridDim.x) {
+    const int row = (int)(b / n), part = (int)(b - (int64_t)row * n);
+    const uint8_t* const z = static_cast<const uint8_t*>(a.z) + (size_t)row * a.ld * ZB;
+    uint8_t* const d = static_cast<uint8_t*>(a.dz) + (size_t)row * a.ld_d * DB;
+    float d_lp = a.d_lp ? a.d_lp[row] : 0.f;
+    const float d_h = a.d_entropy ? a.d_entropy[row] : 0.f;
+    const bool live = d_lp != 0.f || d_h != 0.f;
+    const float lse = a.lse[row], h = d_h != 0.f ? a.entropy[row] : 0.f;
+    int tk = -1;
     if (d_lp != 0.f) {
       tk = a.tokens[row];
       if (tk < 0 || tk >= V) {
-        scale = __builtin_nanf("");
-        if (t == 0 && a.err) atomicOr(a.err, 1);
+        d_lp = __builtin_nanf("");  // (all of the row's gradient)
+        if (part == 0 && t == 0 && a.err) atomicOr(a.err, 1);
       }
     }
-  }
-  for (int j = t; j < V; j += TL_THREADS) {
-    float d = 0.f;
-    if (live) {
-      const float lp = load_z(a.z, a.type, r0 + j) - lse, p = exp_e(lp);
-      // (p = 0 where lp is -inf)
-      d = scale * fmaf(-p, fmaf(d_h, fmaxf(lp, kFar) + h, d_lp), j == tk ? d_lp : 0.f);
+    const auto gradient = [&](float x) __attribute__((always_inline)) {  // of every logit but the token's
+      const float lp = x - lse, p = exp_e(lp);
+      return -p * (d_h == 0.f ? d_lp : fmaf(d_h, fmaxf(lp, kFar) + h, d_lp));  // (p = 0 where lp is -inf)
+    };
+    const auto one = [&](int e) __attribute__((always_inline)) {
+      const float f = live ? gradient(load_z<TZ>(z, e)) + (e == tk ? d_lp : 0.f) : 0.f;
+      if constexpr (TD == kF32)
+        reinterpret_cast<float*>(d)[e] = f;
+      else
+        reinterpret_cast<uint16_t*>(d)[e] = f32_to_bf16_any(f);
+    };
+    const int head = head_of<TZ>(z, V), groups = (V - head) / VEC;
+    const int g0 = min(groups, part * per), g1 = min(groups, g0 + per);
+    if ((reinterpret_cast<uintptr_t>(d) + head * DB) % STORE != 0) {  // input and output never on a boundary together
+      const int e0 = part == 0 ? 0 : head + g0 * VEC, e1 = part == n - 1 ? V : head + g1 * VEC;
+      for (int e = e0 + t; e < e1; e += TB_THREADS) one(e);
+      continue;
     }
-    if (a.d_type == kF32)
-      static_cast<float*>(a.dz)[d0 + j] = d;
-    else
-      static_cast<uint16_t*>(a.dz)[d0 + j] = f32_to_bf16_any(d);
+    const uint4* const zv = reinterpret_cast<const uint4*>(z + (size_t)head * ZB);
+    uint8_t* const dv = d + (size_t)head * DB;
+    for (int g = g0 + t; g < g1; g += TB_THREADS * TB_U) {
+      uint4 u[TB_U];
+      if (live) {
+#pragma unroll
+        for (int q = 0; q < TB_U; ++q)
+          if (g + q * TB_THREADS < g1) u[q] = zv[g + q * TB_THREADS];
+      }
+#pragma unroll
+      for (int q = 0; q < TB_U; ++q) {
+        const int at = g + q * TB_THREADS;
+        if (at >= g1) break;
+        float f[VEC];
+        if (live) {
+          unpack<TZ>(u[q], f);
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) f[e] = gradient(f[e]);
+          const int mine = tk - head - at * VEC;  // the token's place in this group
+          if ((unsigned)mine < (unsigned)VEC) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) f[e] += e == mine ? d_lp : 0.f;
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) f[e] = 0.f;
+        }
+        uint32_t w[VEC * DB / 4];
+#pragma unroll
+        for (int e = 0; e < VEC * DB / 4; ++e) {
+          if constexpr (TD == kF32)
+            w[e] = __float_as_uint(f[e]);
+          else
+            w[e] = (uint32_t)f32_to_bf16_any(f[2 * e]) | ((uint32_t)f32_to_bf16_any(f[2 * e + 1]) << 16);
+        }
+        if constexpr (VEC * DB == 8) {
+          reinterpret_cast<uint2*>(dv)[at] = make_uint2(w[0], w[1]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < VEC * DB / 16; ++e)
+            reinterpret_cast<uint4*>(dv)[at * (VEC * DB / 16) + e] =
+                make_uint4(w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]);
+        }
+      }
+    }
+    if (part == 0 && t < head) one(t);
+    if (part == n - 1 && t < V - head - groups * VEC) one(head + groups * VEC + t);
   }
+}
+
+// Segments of a row: none longer than kSegMost; more where the rows alone are
+// too few for the chip.
+int segments(int M, int V) {
+  int n = (V + kSegMost - 1) / kSegMost;
+  while (n < kSegs && (int64_t)M * n < 256 && V / (2 * n) >= 4096) n *= 2;
+  return n < kSegs ? n : kSegs;
+}
+
+size_t stat_bytes(int M, int nseg) { return ((size_t)M * nseg * sizeof(Stat) + 15) & ~size_t(15); }
+
+template <int T>
+void forward(const TokenLogpArgs& a, int nseg, const Parts& p, hipStream_t stream) {
+  const dim3 grid((unsigned)(a.M * nseg)), block(TL_THREADS);
+  if (a.top > 0) {
+    const int groups = (a.V / kVec<T> + nseg - 1) / nseg + 1;
+    hipLaunchKernelGGL((token_logp_kernel<T, true>), grid, block, groups * sizeof(float), stream, a, nseg, p);
+  } else {
+    hipLaunchKernelGGL((token_logp_kernel<T, false>), grid, block, 0, stream, a, nseg, p);
+  }
+  if (nseg > 1) hipLaunchKernelGGL((token_logp_join_kernel<T>), dim3(a.M), dim3(64), 0, stream, a, nseg, p);
 }
 
 }  // namespace
 
-size_t token_logp_ws_bytes(int, int, int) { return 0; }
+size_t token_logp_ws_bytes(int M, int V, int top) {
+  const int nseg = segments(M, V);
+  return nseg == 1 ? 0 : stat_bytes(M, nseg) + (size_t)M * nseg * top * sizeof(uint64_t);
+}
 
-hipError_t launch_token_logp(const TokenLogpArgs& a, void*, hipStream_t stream) {
-  hipLaunchKernelGGL(token_logp_kernel, dim3(a.M), dim3(TL_THREADS), 0, stream, a);
+hipError_t launch_token_logp(const TokenLogpArgs& a, void* ws, hipStream_t stream) {
+  const int nseg = segments(a.M, a.V);
+  Parts p{static_cast<Stat*>(ws), reinterpret_cast<uint64_t*>(static_cast<uint8_t*>(ws) + stat_bytes(a.M, nseg))};
+  if (a.type == kF32)
+    forward<kF32>(a, nseg, p, stream);
+  else
+    forward<kBf16>(a, nseg, p, stream);
   return hipGetLastError();
 }
 
+template <int TZ>
+static void back_of(const TokenLogpBackArgs& a, hipStream_t stream) {
+  // a stretch is one round of the workgroup's loads, or several where there are many
+  constexpr int ROUND = TB_THREADS * TB_U;
+  const int groups = a.V / kVec<TZ> > 0 ? a.V / kVec<TZ> : 1;
+  const int64_t rounds = (int64_t)a.M * ((groups + ROUND - 1) / ROUND);
+  int per = ROUND;
+  while (per < 8 * ROUND && rounds * ROUND / per > 8192) per *= 2;
+  const int n = (groups + per - 1) / per;
+  const int64_t all = (int64_t)a.M * n;
+  const dim3 grid((unsigned)(all < (1 << 20) ? all : 1 << 20)), block(TB_THREADS);
+  if (a.d_type == kF32)
+    hipLaunchKernelGGL((token_logp_back_kernel<TZ, kF32>), grid, block, 0, stream, a, n, per);
+  else
+    hipLaunchKernelGGL((token_logp_back_kernel<TZ, kBf16>), grid, block, 0, stream, a, n, per);
+}
+
 hipError_t launch_token_logp_back(const TokenLogpBackArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL(token_logp_back_kernel, dim3(a.M), dim3(TL_THREADS), 0, stream, a);
+  if (a.type == kF32)
+    back_of<kF32>(a, stream);
+  else
+    back_of<kBf16>(a, stream);
   return hipGetLastError();
 }
 

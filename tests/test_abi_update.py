@@ -62,7 +62,7 @@ def test_layer_norm_backward_rejects(kw, code):
     (dict(tok=None, lp=None, lse=None, ent=None, top=0, ids=None, tlp=None), NULL),
     (dict(ids=None), NULL), (dict(ids=None, tlp=None), NULL), (dict(top=0), NULL), (dict(top=0, ids=None), NULL),
     (dict(zt=2), UNSUP), (dict(M=0), SHAPE), (dict(M=(1 << 20) + 1), SHAPE), (dict(V=0), SHAPE),
-    (dict(V=(1 << 21) + 1, ld=1 << 22), SHAPE), (dict(ld=99), SHAPE), (dict(ld=1 << 31), SHAPE),
+    (dict(V=(1 << 21) + 1, ld=1 << 22), SHAPE), (dict(M=1 << 18, V=(1 << 20) + 1, ld=1 << 21), SHAPE), (dict(ld=99), SHAPE), (dict(ld=1 << 31), SHAPE),
     (dict(top=33), SHAPE), (dict(top=-1), SHAPE), (dict(V=7, top=8), SHAPE),
     (dict(lp=at(0)), SHAPE), (dict(lse=at(1)), SHAPE), (dict(ent=at(3)), SHAPE), (dict(tlp=at(5)), SHAPE),
     (dict(err=at(2)), SHAPE),
@@ -81,7 +81,7 @@ def test_token_logprobs_rejects(kw, code):
     (dict(z=None), NULL), (dict(lse=None), NULL), (dict(dz=None), NULL), (dict(tok=None), NULL), (dict(ent=None), NULL),
     (dict(dlp=None, dh=None), NULL),
     (dict(zt=2), UNSUP), (dict(dt=-1), UNSUP), (dict(M=0), SHAPE), (dict(M=(1 << 20) + 1), SHAPE), (dict(V=0), SHAPE),
-    (dict(V=(1 << 21) + 1, ld=1 << 22, ldd=1 << 22), SHAPE), (dict(ld=99), SHAPE), (dict(ldd=99), SHAPE),
+    (dict(V=(1 << 21) + 1, ld=1 << 22, ldd=1 << 22), SHAPE), (dict(M=1 << 20, V=1 << 19, ld=1 << 21, ldd=1 << 21), SHAPE), (dict(ld=99), SHAPE), (dict(ldd=99), SHAPE),
     (dict(ldd=1 << 31), SHAPE),
     (dict(dz=at(0), dt=BF), SHAPE), (dict(dz=at(0), ldd=104), SHAPE), (dict(dz=at(2)), SHAPE), (dict(err=at(5)), SHAPE),
     (dict(dz=at(0), err=at(0)), SHAPE),
@@ -154,6 +154,7 @@ def test_workspace_sizes():
     assert L.hydra_layer_norm_backward_workspace_bytes(8, (1 << 21) + 1, ctypes.byref(b)) == SHAPE
     assert L.hydra_layer_norm_backward_workspace_bytes(8, 8, None) == NULL
     assert L.hydra_token_logprobs_workspace_bytes(8, 7, 8, ctypes.byref(b)) == SHAPE
+    assert L.hydra_token_logprobs_workspace_bytes(1 << 20, 1 << 19, 8, ctypes.byref(b)) == SHAPE
     assert L.hydra_token_logprobs_workspace_bytes(8, 100, 33, ctypes.byref(b)) == SHAPE
     assert L.hydra_token_logprobs_workspace_bytes(8, 100, 8, None) == NULL
     assert L.hydra_grad_norm_workspace_bytes(None) == NULL
