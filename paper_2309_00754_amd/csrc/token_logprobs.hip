@@ -32,7 +32,7 @@ constexpr int TL_WAVES = TL_THREADS / 64;
 constexpr int TL_U = 4;             // 16-byte loads of a thread under way
 constexpr int kSegMost = 57344;     // elements of a segment (its groups' maxima, 4 bytes each, beside 6 KB in 64 KB of LDS)
 constexpr int kSegs = 64;           // segments of a row at most
-constexpr int kCand = 512;          // logits ranked by counting at most
+constexpr int kCand = 576;          // logits ranked by counting at most
 
 template <int T>
 constexpr int kVec = T == kF32 ? 4 : 8;  // elements of 16 bytes
@@ -70,6 +70,10 @@ __device__ __forceinline__ uint64_t order_key(float z, int idx) {
   return ((uint64_t)o << 32) | (uint32_t)~idx;
 }
 __device__ __forceinline__ int index_of(uint64_t key) { return (int)~(uint32_t)key; }
+__device__ __forceinline__ float logit_of(uint64_t key) {  // (of -0: +0)
+  const uint32_t o = (uint32_t)(key >> 32);
+  return __uint_as_float((int)o < 0 ? o & 0x7FFFFFFFu : ~o);
+}
 // (of -inf and below: masked out, or no logit)
 __device__ __forceinline__ bool masked_out(uint64_t key) { return (uint32_t)(key >> 32) <= 0x007FFFFFu; }
 
@@ -131,30 +135,24 @@ __device__ __forceinline__ float wave_all(float v) {
   return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
 }
 
-__device__ __forceinline__ Stat block_stat(Stat a) {
-  __shared__ float red[3][TL_WAVES];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  float m = wave_all<true>(a.m);
-  if (lane == 0) red[0][wave] = m;
-  __syncthreads();
+// The waves' maxima, then their sums, met by the workgroup.
+struct Meet {
+  float m[TL_WAVES], s[TL_WAVES], w[TL_WAVES];
+};
+__device__ __forceinline__ void meet_max(Stat& a, const Meet& meet) {
+  float m = meet.m[0];
 #pragma unroll
-  for (int i = 0; i < TL_WAVES; ++i) m = fmaxf(m, red[0][i]);
+  for (int i = 1; i < TL_WAVES; ++i) m = fmaxf(m, meet.m[i]);
   rescale(a, m);
-  a.s = wave_all<false>(a.s);
-  a.w = wave_all<false>(a.w);
-  if (lane == 0) {
-    red[1][wave] = a.s;
-    red[2][wave] = a.w;
-  }
-  __syncthreads();
-  a.s = red[1][0];
-  a.w = red[2][0];
+}
+__device__ __forceinline__ void meet_sums(Stat& a, const Meet& meet) {
+  a.s = meet.s[0];
+  a.w = meet.w[0];
 #pragma unroll
   for (int i = 1; i < TL_WAVES; ++i) {
-    a.s += red[1][i];
-    a.w += red[2][i];
+    a.s += meet.s[i];
+    a.w += meet.w[i];
   }
-  return a;
 }
 
 __device__ __forceinline__ uint64_t block_max(uint64_t v) {
@@ -177,47 +175,73 @@ __device__ __forceinline__ uint64_t block_max(uint64_t v) {
 // alone remains.
 __device__ __forceinline__ float logp_of(float z, float m, float ln_s) { return (z - m) - ln_s; }
 
-// One thread: the row's statistics.
+// The token of a row and its logit, loaded ahead of the row (by one thread).
+struct Token {
+  int tk;
+  float z;
+};
 template <int T>
-__device__ __forceinline__ void finish_row(const TokenLogpArgs& a, int row, const Stat& st) {
+__device__ __forceinline__ Token token_of(const TokenLogpArgs& a, int row) {
+  Token k{0, 0.f};
+  if (a.lp) {
+    k.tk = a.tokens[row];
+    if (k.tk >= 0 && k.tk < a.V) k.z = load_z<T>(a.z, (size_t)row * a.ld + k.tk);
+  }
+  return k;
+}
+
+// One thread: the row's statistics.
+__device__ __forceinline__ void finish_row(const TokenLogpArgs& a, int row, const Stat& st, const Token& k) {
   const float ln_s = log_e(st.s);
   if (a.lse) a.lse[row] = st.m + ln_s;
   if (a.entropy) a.entropy[row] = ln_s - st.w / st.s;
   if (a.lp) {
-    const int tk = a.tokens[row];
-    const bool ok = tk >= 0 && tk < a.V;
-    a.lp[row] = ok ? logp_of(load_z<T>(a.z, (size_t)row * a.ld + tk), st.m, ln_s) : __builtin_nanf("");
+    const bool ok = k.tk >= 0 && k.tk < a.V;
+    a.lp[row] = ok ? logp_of(k.z, st.m, ln_s) : __builtin_nanf("");
     if (!ok && a.err) atomicOr(a.err, 1);
   }
 }
 
-// One wave: the row's alternatives from the n keys at `key` (LDS), which hold
-// all logits of the first k that are not masked out.
-template <int T>
-__device__ __forceinline__ void finish_top(const TokenLogpArgs& a, int row, const Stat& st, const uint64_t* key, int n) {
-  const int lane = threadIdx.x & 63, k = a.top;
-  const size_t r0 = (size_t)row * a.ld, o0 = (size_t)row * k;
-  const float ln_s = log_e(st.s);
-  for (int i = lane; i < n; i += 64) {
-    const uint64_t mine = key[i];
+// One wave: f(rank, key) for each of the n keys at `key` (LDS, 16-byte aligned,
+// room for a multiple of 8), the rank counted over all of them.
+template <class F>
+__device__ __forceinline__ void each_ranked(uint64_t* key, int n, F f) {
+  const int lane = threadIdx.x & 63, n8 = (n + 7) & ~7;
+  if (lane < n8 - n) key[n + lane] = 0;
+  __builtin_amdgcn_wave_barrier();
+  for (int i = lane; i - lane < n; i += 64) {
+    const uint64_t mine = i < n ? key[i] : ~0ull;
     int rank = 0;
-    for (int j = 0; j < n; ++j) rank += key[j] > mine;
-    if (rank < k) {
-      const int id = index_of(mine);
-      a.ids[o0 + rank] = id;
-      if (a.top_lp) a.top_lp[o0 + rank] = logp_of(load_z<T>(a.z, r0 + id), st.m, ln_s);
+    for (int j = 0; j < n8; j += 8) {
+      uint64_t other[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) other[q] = key[j + q];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) rank += other[q] > mine;
     }
+    if (i < n) f(rank, mine);
   }
+}
+
+// One wave: the row's alternatives from n keys, which hold all logits of the
+// first k that are not masked out.
+template <int T>
+__device__ __forceinline__ void finish_top(const TokenLogpArgs& a, int row, const Stat& st, uint64_t* key, int n) {
+  const int lane = threadIdx.x & 63, k = a.top;
+  const size_t o0 = (size_t)row * k;
+  const float ln_s = log_e(st.s);
+  const auto put = [&](int rank, int id, float z) __attribute__((always_inline)) {
+    if (rank >= k) return;
+    a.ids[o0 + rank] = id;
+    if (a.top_lp) a.top_lp[o0 + rank] = logp_of(z, st.m, ln_s);
+  };
+  each_ranked(key, n, [&](int rank, uint64_t mine) __attribute__((always_inline)) { put(rank, index_of(mine), logit_of(mine)); });
   if (n >= k) return;
   // Fewer than k <= 32 logits are not masked out: of the first 64 entries (or of
   // all, at least k) enough are.
-  const bool out = lane < a.V && load_z<T>(a.z, r0 + lane) == -INFINITY;
+  const bool out = lane < a.V && load_z<T>(a.z, (size_t)row * a.ld + lane) == -INFINITY;
   const uint64_t outs = __ballot(out);
-  const int rank = n + __popcll(outs & ((1ull << lane) - 1));
-  if (out && rank < k) {
-    a.ids[o0 + rank] = lane;
-    if (a.top_lp) a.top_lp[o0 + rank] = logp_of(-INFINITY, st.m, ln_s);
-  }
+  if (out) put(n + __popcll(outs & ((1ull << lane) - 1)), lane, -INFINITY);
 }
 
 // Partial results of a segment in the workspace: all statistics [M][nseg], then
@@ -252,10 +276,18 @@ template <int T, bool TOP>
 __global__ __launch_bounds__(TL_THREADS) void token_logp_kernel(TokenLogpArgs a, int nseg, Parts parts) {
   constexpr int VEC = kVec<T>;
   extern __shared__ float most_of[];  // TOP: the maxima of the segment's groups
+  __shared__ Meet meet;
+  // TOP: the waves' bounds, the groups that reach the bound, the logits that do
+  __shared__ float bound_of[TOP ? TL_WAVES : 1];
+  __shared__ int slot[TOP ? kCand : 1], count[2];
+  __shared__ __align__(16) uint64_t cand[TOP ? kCand : 1];
   const int row = blockIdx.x / nseg, seg = blockIdx.x - row * nseg, t = threadIdx.x, V = a.V;
   const uint8_t* const z = static_cast<const uint8_t*>(a.z) + (size_t)row * a.ld * (16 / VEC);
   const Span sp = span_of<T>(z, V, seg, nseg);
   const uint4* const v = reinterpret_cast<const uint4*>(z + (size_t)sp.head * (16 / VEC));
+  Token token{0, 0.f};
+  if (t == 0 && nseg == 1) token = token_of<T>(a, row);
+  if (TOP && t < 2) count[t] = 0;
   Stat st{-INFINITY, 0.f, 0.f};
   for (int g = sp.g0 + t; g < sp.g1; g += TL_THREADS * TL_U) {
     uint4 u[TL_U];
@@ -283,56 +315,71 @@ __global__ __launch_bounds__(TL_THREADS) void token_logp_kernel(TokenLogpArgs a,
     const float f[1] = {edge = load_z<T>(z, edge_at)};
     absorb(st, f, edge);
   }
+  // First meeting: the maxima, and (TOP) each wave's bound.
   const float mine = st.m;
-  st = block_stat(st);
-  if (nseg == 1) {
-    if (t == 0) finish_row<T>(a, row, st);
-  } else if (t == 0) {
-    parts.stat[blockIdx.x] = st;
+  const int lane = t & 63, wave = t >> 6;
+  const float wave_most = wave_all<true>(mine);
+  if (lane == 0) meet.m[wave] = wave_most;
+  const int groups = sp.g1 - sp.g0;
+  // whole waves of groups, or the only one (where the last wave's few threads cannot
+  // bound anything, and what is left to others is few)
+  const int waves = groups >= 64 ? min(TL_WAVES, groups / 64) : groups > 0;
+  if constexpr (TOP) {
+    float left = mine, bound = -INFINITY;
+    if (wave < waves) {
+      const int j = (a.top + waves - 1) / waves;
+      bound = wave_most;
+      for (int i = 1; i < j; ++i) {
+        const uint64_t have = __ballot(left == bound);
+        if (lane == __ffsll((unsigned long long)have) - 1) left = -INFINITY;
+        bound = wave_all<true>(left);
+      }
+    }
+    if (lane == 0) bound_of[wave] = bound;
+  }
+  __syncthreads();
+  meet_max(st, meet);
+  st.s = wave_all<false>(st.s);
+  st.w = wave_all<false>(st.w);
+  if (lane == 0) {
+    meet.s[wave] = st.s;
+    meet.w[wave] = st.w;
+  }
+  // Second meeting: the sums, and (TOP) the groups that reach the bound.
+  float bound = -INFINITY;
+  const auto reaches = [&](float x) __attribute__((always_inline)) { return x >= bound && x != -INFINITY; };
+  if constexpr (TOP) {
+    if (waves > 0) bound = bound_of[0];
+    for (int i = 1; i < waves; ++i) bound = fminf(bound, bound_of[i]);
+    for (int g = t; g < groups; g += TL_THREADS)
+      if (reaches(most_of[g])) {
+        const int i = atomicAdd(&count[0], 1);
+        if (i < kCand) slot[i] = g;
+      }
+    if (edge_at >= 0 && reaches(edge)) cand[atomicAdd(&count[1], 1)] = order_key(edge, edge_at);
+  }
+  __syncthreads();
+  meet_sums(st, meet);
+  if (t == 0) {
+    if (nseg == 1)
+      finish_row(a, row, st, token);
+    else
+      parts.stat[blockIdx.x] = st;
   }
   if constexpr (TOP) {
-    __shared__ uint64_t cand[kCand];
-    __shared__ float bound_of[TL_WAVES];
-    __shared__ int slot[kCand], count[2];
-    const int lane = t & 63, wave = t >> 6, k = a.top, groups = sp.g1 - sp.g0;
+    const int k = a.top, slots = count[0];
     int n = kCand + 1;  // too many
-    if (st.s >= 0.f && st.m != INFINITY) {  // (no NaN and no +inf)
-      // waves that have a group, and the bound
-      const int waves = min(TL_WAVES, (groups + 63) / 64), j = waves > 0 ? (k + waves - 1) / waves : 0;
-      float left = mine, bound = -INFINITY;
-      if (wave < waves)
-        for (int i = 0; i < j; ++i) {
-          bound = wave_all<true>(left);
-          const uint64_t have = __ballot(left == bound);
-          if (lane == __ffsll((unsigned long long)have) - 1) left = -INFINITY;
+    if (slots <= kCand && st.s >= 0.f && st.m != INFINITY) {  // (no NaN and no +inf)
+      for (int i = t; i < slots * VEC; i += TL_THREADS) {
+        const int e = sp.head + (sp.g0 + slot[i / VEC]) * VEC + i % VEC;
+        const float x = load_z<T>(z, e);
+        if (reaches(x)) {
+          const int p = atomicAdd(&count[1], 1);
+          if (p < kCand) cand[p] = order_key(x, e);
         }
-      if (t < 2) count[t] = 0;
-      if (lane == 0) bound_of[wave] = bound;
-      __syncthreads();
-      bound = bound_of[0];
-      for (int i = 1; i < waves; ++i) bound = fminf(bound, bound_of[i]);
-      const auto reaches = [&](float x) __attribute__((always_inline)) { return x >= bound && x != -INFINITY; };
-      for (int g = t; g < groups; g += TL_THREADS)
-        if (reaches(most_of[g])) {
-          const int i = atomicAdd(&count[0], 1);
-          if (i < kCand) slot[i] = g;
-        }
-      if (edge_at >= 0 && reaches(edge)) cand[atomicAdd(&count[1], 1)] = order_key(edge, edge_at);
-      __syncthreads();
-      const int slots = count[0];
-      if (slots <= kCand) {
-        for (int i = t; i < slots * VEC; i += TL_THREADS) {
-          const int e = sp.head + (sp.g0 + slot[i / VEC]) * VEC + i % VEC;
-          const float x = load_z<T>(z, e);
-          if (reaches(x)) {
-            const int p = atomicAdd(&count[1], 1);
-            if (p < kCand) cand[p] = order_key(x, e);
-          }
-        }
-        __syncthreads();
-        n = count[1];
       }
       __syncthreads();
+      n = count[1];
     }
     if (n > kCand) {
       // one after the other: each thread's greatest below the last one
@@ -357,12 +404,9 @@ __global__ __launch_bounds__(TL_THREADS) void token_logp_kernel(TokenLogpArgs a,
       return;
     }
     uint64_t* const out = parts.key + (size_t)blockIdx.x * k;
-    for (int i = lane; i < n; i += 64) {
-      const uint64_t me = cand[i];
-      int rank = 0;
-      for (int q = 0; q < n; ++q) rank += cand[q] > me;
+    each_ranked(cand, n, [&](int rank, uint64_t me) __attribute__((always_inline)) {
       if (rank < k) out[rank] = me;
-    }
+    });
     for (int i = n + lane; i < k; i += 64) out[i] = 0;
   }
 }
@@ -370,15 +414,17 @@ __global__ __launch_bounds__(TL_THREADS) void token_logp_kernel(TokenLogpArgs a,
 // One wave per row.
 template <int T>
 __global__ __launch_bounds__(64) void token_logp_join_kernel(TokenLogpArgs a, int nseg, Parts parts) {
-  __shared__ uint64_t cand[kSegs * kMaxTop];
+  __shared__ __align__(16) uint64_t cand[kSegs * kMaxTop];
   const int row = blockIdx.x, lane = threadIdx.x, k = a.top;
+  Token token{0, 0.f};
+  if (lane == 0) token = token_of<T>(a, row);
   const Stat* const ps = parts.stat + (size_t)row * nseg;
   Stat st{-INFINITY, 0.f, 0.f};
   if (lane < nseg) st = ps[lane];
   rescale(st, wave_all<true>(st.m));
   st.s = wave_all<false>(st.s);
   st.w = wave_all<false>(st.w);
-  if (lane == 0) finish_row<T>(a, row, st);
+  if (lane == 0) finish_row(a, row, st, token);
   if (k == 0) return;
   // what reaches the greatest of the segments' k-th keys
   const uint64_t* const pk = parts.key + (size_t)row * nseg * k;
@@ -496,12 +542,17 @@ __global__ __launch_bounds__(TB_THREADS) void token_logp_back_kernel(TokenLogpBa
   }
 }
 
-// Segments of a row: none longer than kSegMost; more where the rows alone are
-// too few for the chip.
-int segments(int M, int V) {
-  int n = (V + kSegMost - 1) / kSegMost;
-  while (n < kSegs && (int64_t)M * n < 256 && V / (2 * n) >= 4096) n *= 2;
-  return n < kSegs ? n : kSegs;
+// Segments of a row: none longer than kSegMost; more, of 24 KB, where a row is
+// longer than 128 KB and there are fewer than 256 of them.  One row of 50272 fp32
+// logits takes 5.7 us in eight segments (their join is a second launch), so 7.7
+// in one, 64 rows 7.4 and 9.2, 250 rows 12.4 and 10.5; 32000 fp32 6.1 and 5.6,
+// 50272 bf16 5.7 and 6.4 (with alternatives, from 16 rows on, 10.7 and 10.0).
+int segments(int M, int V, int type) {
+  const int64_t least = (V + kSegMost - 1) / kSegMost, bytes = V * (int64_t)type_bytes(type);
+  int64_t n = bytes > (128 << 10) ? bytes / (24 << 10) : 1;
+  n = n < 256 / M ? n : 256 / M;
+  n = n > least ? n : least;
+  return (int)(n < kSegs ? n : kSegs);
 }
 
 size_t stat_bytes(int M, int nseg) { return ((size_t)M * nseg * sizeof(Stat) + 15) & ~size_t(15); }
@@ -521,12 +572,12 @@ void forward(const TokenLogpArgs& a, int nseg, const Parts& p, hipStream_t strea
 }  // namespace
 
 size_t token_logp_ws_bytes(int M, int V, int top) {
-  const int nseg = segments(M, V);
+  const int nseg = segments(M, V, kF32);  // (the most of the two types)
   return nseg == 1 ? 0 : stat_bytes(M, nseg) + (size_t)M * nseg * top * sizeof(uint64_t);
 }
 
 hipError_t launch_token_logp(const TokenLogpArgs& a, void* ws, hipStream_t stream) {
-  const int nseg = segments(a.M, a.V);
+  const int nseg = segments(a.M, a.V, a.type);
   Parts p{static_cast<Stat*>(ws), reinterpret_cast<uint64_t*>(static_cast<uint8_t*>(ws) + stat_bytes(a.M, nseg))};
   if (a.type == kF32)
     forward<kF32>(a, nseg, p, stream);
