@@ -143,7 +143,7 @@ __device__ __forceinline__ float wave_sum(float v) {
   return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
 }
 
-constexpr int kMaxWaves = 8;  // of a workgroup
+constexpr int kMaxWaves = 8;  // of a row
 
 // Sum over the `nw` waves of a row group (nw a power of two; this wave's group
 // starts at wave w0), in every thread.  `red` is used by this call alone until
@@ -226,7 +226,7 @@ template <int TD, int TX, int VEC, int NCH, int THREADS>
 __global__ __launch_bounds__(THREADS) void norm_back_kernel(LayerNormBackArgs a, float* pw, float* pb, int nw) {
   // the groups' columns of dw, then of db, by place in the group: no two lanes on one bank
   __shared__ float acc[THREADS * NCH * VEC];
-  __shared__ float red[2][2][kMaxWaves];
+  __shared__ float red[2][2][THREADS / 64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int w0 = wave & -nw, groups = THREADS / 64 / nw, group = w0 / nw, K = a.K;
   const int k0 = ((wave - w0) * 64 + lane) * VEC, step = nw * 64 * VEC;
@@ -445,7 +445,7 @@ __global__ __launch_bounds__(COL_THREADS) void norm_back_cols_kernel(LayerNormBa
 // chunk's address takes a register too, and 32 spill.
 constexpr int kFew = 16, kMany = 32;
 constexpr int kFewK = kMaxWaves * 64 * kFew, kManyK = kMaxWaves * 64 * kMany;
-constexpr int FWD_THREADS = 256, BACK_THREADS = 512;
+constexpr int FWD_THREADS = 256;
 
 // Waves per row: enough for `lane` columns a lane.
 int row_waves(int K, int lane) {
@@ -454,14 +454,23 @@ int row_waves(int K, int lane) {
   return nw;
 }
 
+// Threads of the backward's workgroups: 1024 from 512 rows on (700 x 2048 fp32 11.8
+// us, with 512 threads 12.5; 1024 x 4096 bf16 16.0 and 17.6, 8192 x 4096 48.6 and
+// 53.1; but 333 x 4096 13.3 and 12.8), save for much fp32 on both sides (8192 x
+// 4096 87.4 and 81.5).  Element by element that many registers are not there.
+int back_threads(const LayerNormBackArgs& a, int vec) {
+  const bool both32 = a.dy_type == kF32 && a.x_type == kF32;
+  return vec > 1 && a.K <= kFewK && a.M >= 512 && (!both32 || (int64_t)a.M * a.K <= (1 << 23)) ? 1024 : 512;
+}
+
 // Workgroups of the backward.  Each writes a part of dw and db that
 // norm_back_sum_kernel reads again: one a CU, half as many where the rows are
 // few (M K up to 2^22: 700 x 2048 bf16 10.6 us, so 11.5; 333 x 4096 12.8, so
 // 13.8; 4096 x 2048 21.1, so 18.7), and a single one, which needs no second
 // launch, where that takes it two rounds of rows at most (8 x 2048: 7.7 us with
 // the launch).
-int back_blocks(int M, int K, int nw) {
-  const int groups = BACK_THREADS / 64 / nw, want = (M + groups - 1) / groups;
+int back_blocks(int M, int K, int nw, int threads) {
+  const int groups = threads / 64 / nw, want = (M + groups - 1) / groups;
   if (want <= 2) return 1;
   const int most = (int64_t)M * K <= (1 << 22) ? 128 : 256;
   return want < most ? want : most;
@@ -518,16 +527,22 @@ template <int TD, int TX, int VEC>
 int backward(const LayerNormBackArgs& a, float* part, hipStream_t stream) {
   const bool few = a.K <= kFewK;
   if (!few && (VEC == 1 || a.K > kManyK)) return 0;
-  const int nw = row_waves(a.K, few ? kFew : kMany), blocks = back_blocks(a.M, a.K, nw);
+  const int nw = row_waves(a.K, few ? kFew : kMany), threads = back_threads(a, VEC);
+  const int blocks = back_blocks(a.M, a.K, nw, threads);
   float* const pw = blocks > 1 ? part : a.dw;
   float* const pb = blocks > 1 && part ? part + a.K : a.db;
-  if (few) {
-    hipLaunchKernelGGL((norm_back_kernel<TD, TX, VEC, kFew / VEC, BACK_THREADS>), dim3(blocks), dim3(BACK_THREADS), 0, stream,
-                       a, pw, pb, nw);
-  } else if constexpr (VEC > 1) {
-    hipLaunchKernelGGL((norm_back_kernel<TD, TX, VEC, kMany / VEC, BACK_THREADS>), dim3(blocks), dim3(BACK_THREADS), 0,
-                       stream, a, pw, pb, nw);
+  if constexpr (VEC > 1) {
+    if (!few) {
+      hipLaunchKernelGGL((norm_back_kernel<TD, TX, VEC, kMany / VEC, 512>), dim3(blocks), dim3(512), 0, stream, a, pw, pb, nw);
+      return blocks;
+    }
+    if (threads == 1024) {
+      hipLaunchKernelGGL((norm_back_kernel<TD, TX, VEC, kFew / VEC, 1024>), dim3(blocks), dim3(1024), 0, stream, a, pw, pb,
+                         nw);
+      return blocks;
+    }
   }
+  hipLaunchKernelGGL((norm_back_kernel<TD, TX, VEC, kFew / VEC, 512>), dim3(blocks), dim3(512), 0, stream, a, pw, pb, nw);
   return blocks;
 }
 
@@ -545,7 +560,7 @@ size_t layer_norm_back_ws_bytes(int M, int K) {
   // (whatever the types and the alignment of the call)
   size_t need = 0;
   if (K <= kManyK)
-    need = (size_t)back_blocks(M, K, row_waves(K, K <= kFewK ? kFew : kMany)) * 2 * K * sizeof(float);
+    need = (size_t)back_blocks(M, K, row_waves(K, K <= kFewK ? kFew : kMany), 512) * 2 * K * sizeof(float);  // (the more)
   if (K > kFewK) {
     int nch, rows;
     long_plan(M, K, nch, rows);
