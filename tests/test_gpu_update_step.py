@@ -1,0 +1,319 @@
+"""An update step put together from the library's calls, as a program would: layer norm, the CLM head with its adapter,
+log-probabilities of the sampled tokens, the PPO losses, and back through all of them to the clipped gradients; the same
+captured in a HIP graph, on another stream and from two threads; the native call path against the Python one."""
+import threading
+
+import numpy as np
+import pytest
+
+import paper_2309_00754_amd as H
+from paper_2309_00754_amd import _binding as Bd
+from gpu_helpers import host, say
+from update_helpers import U, f64, near, put
+
+pytestmark = pytest.mark.gpu
+
+N_SEQ, T, START, K, V, R, S = 3, 40, 11, 264, 1000, 8, 2.0
+M = N_SEQ * T
+
+
+class Step:
+    """The buffers of one update step, and the step itself."""
+
+    def __init__(self, dev, seed=0):
+        import torch
+        r = np.random.default_rng(seed)
+        bf, f = "bf16", "f32"
+        self.h = put(r.normal(0, 1, (M, K)) * r.uniform(0.5, 2, K), f, dev)  # the residual stream
+        self.w, self.b = put(r.normal(1, 0.2, K), bf, dev), put(r.normal(0, 0.1, K), bf, dev)
+        self.W, self.A = put(r.normal(0, K ** -0.5, (V, K)), bf, dev), put(r.normal(0, K ** -0.5, (R, K)), bf, dev)
+        self.B = put(r.normal(0, R ** -0.5, (V, R)), bf, dev)
+        self.Wt = torch.empty((K, V), dtype=torch.bfloat16, device=dev)
+        H.hydra_transpose_bf16(self.W, self.Wt)
+        self.tokens = torch.as_tensor(r.integers(0, V, M).astype(np.int32)).to(dev)
+        self.adv, self.values, self.returns = (put(r.normal(0, 1, M), f, dev) for _ in range(3))
+        self.noise = put(r.normal(0, 0.1, M), f, dev)
+
+        def out(*shape, dtype=torch.float32):
+            return torch.full(shape, float("nan"), device=dev).to(dtype)
+
+        self.x, self.mean, self.rstd = out(M, K, dtype=torch.bfloat16), out(M), out(M)
+        self.z = out(M, V)
+        self.lp, self.lse, self.entropy = out(M), out(M), out(M)
+        self.ids, self.top_lp = torch.zeros((M, 5), dtype=torch.int32, device=dev), out(M, 5)
+        self.lp_old, self.losses, self.d_lp, self.d_v = out(M), out(3), out(M), out(M)
+        self.d_h = torch.zeros(M, device=dev)
+        self.d_h.view(N_SEQ, T)[:, START:] = -0.01 / (N_SEQ * (T - START))
+        self.dz = out(M, V, dtype=torch.bfloat16)
+        self.dx, self.dA, self.dB = out(M, K), out(R, K), out(V, R)
+        self.dh, self.dw, self.db = out(M, K), out(K), out(K)
+        self.flat = out(R * K + V * R + 2 * K)
+        self.outs = [t.view(g.shape) for t, g in zip(self.flat.split([R * K, V * R, K, K]), (self.dA, self.dB, self.dw, self.db))]
+        self.norm = out(1)
+        self.err = torch.zeros(1, dtype=torch.int32, device=dev)
+
+        def ws(n):
+            return torch.full((max(n, 16),), 0xFF, dtype=torch.uint8, device=dev)
+
+        self.ws_lin = ws(H.hydra_lora_linear_backward_workspace_bytes(M, V, K, R))
+        self.ws_norm = ws(H.hydra_layer_norm_backward_workspace_bytes(M, K))
+        self.ws_lp = ws(H.hydra_token_logprobs_workspace_bytes(M, V, 5))
+        self.ws_grad = ws(H.hydra_grad_norm_workspace_bytes())
+
+    def run(self, stream=None, own_workspaces=True):
+        st = dict(stream=stream)
+        w = (lambda t: t) if own_workspaces else (lambda t: None)
+        H.hydra_layer_norm(self.h, self.w, self.b, self.x, self.mean, self.rstd, **st)
+        H.hydra_lora_linear(self.x, self.W, self.A, self.B, S, None, self.z, **st)
+        H.hydra_token_logprobs(self.z, self.tokens, self.lp, self.lse, self.entropy, self.ids, self.top_lp, w(self.ws_lp),
+                               self.err, **st)
+        # the sampling policy's log-probabilities: the new ones and some noise
+        import torch
+        with torch.cuda.stream(stream):
+            torch.add(self.lp, self.noise, out=self.lp_old)
+        H.hydra_ppo_loss(self.lp, self.lp_old, self.adv, self.values, self.returns, N_SEQ, T, self.losses, self.d_lp,
+                         self.d_v, start=START, **st)
+        H.hydra_token_logprobs_backward(self.z, self.tokens, self.lse, self.dz, self.d_lp, self.entropy, self.d_h, self.err,
+                                        **st)
+        H.hydra_lora_linear_backward(self.x, self.Wt, self.A, self.B, S, self.dz, self.dx, self.dA, self.dB, self.ws_lin, **st)
+        H.hydra_layer_norm_backward(self.dx, self.h, self.w, self.mean, self.rstd, self.dh, self.dw, self.db,
+                                    w(self.ws_norm), **st)
+        H.hydra_grad_clip([self.dA, self.dB, self.dw, self.db], 0.05, self.norm, self.outs, w(self.ws_grad), self.err, **st)
+
+    def results(self):
+        names = ("x", "mean", "rstd", "z", "lp", "lse", "entropy", "ids", "top_lp", "losses", "d_lp", "d_v", "dz", "dx", "dA",
+                 "dB", "dh", "dw", "db", "norm", "flat", "err")
+        return {k: host(getattr(self, k).float()).copy() for k in names}
+
+    def clear(self):
+        for k in ("x", "z", "lp", "lse", "entropy", "top_lp", "d_lp", "dz", "dx", "dA", "dB", "dh", "dw", "db", "norm", "flat"):
+            getattr(self, k).fill_(float("nan"))
+
+
+def test_step_against_autograd_in_64_bits(dev):
+    """The loss of the whole step, differentiated by torch in float64 on the CPU at the bf16 rows that the linear read.
+    The library rounds dz to bf16 once on the way back (2^-8 of each element); everything after it is linear, so its
+    effect is bounded by the same products over magnitudes, with the fp32 sums' share on top (below 2^-12 of them)."""
+    import torch
+    say("update step")
+    s = Step(dev)
+    s.run()
+    torch.cuda.synchronize()
+    h, w, b, A, B = (torch.tensor(f64(t), requires_grad=True) for t in (s.h, s.w, s.b, s.A, s.B))
+    W = torch.tensor(f64(s.W))
+    mean = h.mean(1, keepdim=True)
+    y = (h - mean) * ((h - mean).square().mean(1, keepdim=True) + 1e-5).rsqrt() * w + b
+    x = y + (torch.tensor(f64(s.x)) - y).detach()
+    assert ((x - y).abs() <= (2 ** -8 + 2 ** -18) * y.abs() + 1e-6).all()
+    z = x @ W.t() + S * (x @ A.t()) @ B.t()
+    lp = torch.log_softmax(z, 1)
+    mine = lp.gather(1, torch.tensor(host(s.tokens)).long()[:, None])[:, 0]
+    ent = -(lp.exp() * lp).sum(1)
+    # (the ratio as the library saw it)
+    ratio = torch.exp(mine - torch.tensor(f64(s.lp_old)))
+    live = (torch.arange(T) >= START).repeat(N_SEQ)
+    adv, n = torch.tensor(f64(s.adv)), N_SEQ * (T - START)
+    loss = -(torch.minimum(ratio * adv, ratio.clamp(0.8, 1.2) * adv) * live).sum() / n - 0.01 * (ent * live).sum() / n
+    loss.backward()
+    near(f64(s.lp), mine.detach().numpy(), 2e-5, "lp")
+    near(f64(s.entropy), ent.detach().numpy(), 2e-5, "entropy")
+    step = 2 ** -8 + 2 ** -12
+    with torch.no_grad():
+        lpv = lp
+        p = lpv.exp()
+        d_lp, d_h = torch.tensor(f64(s.d_lp)), torch.tensor(f64(s.d_h))
+        dz = -p * (d_lp[:, None] + d_h[:, None] * (lpv + ent[:, None]))
+        dz[torch.arange(M), torch.tensor(host(s.tokens)).long()] += d_lp
+        # what a relative error of `step` in every element of dz can do
+        t_dz = step * dz.abs() + 1e-12
+        t_dA = S * (t_dz @ B.abs()).t() @ x.abs() + 2 ** -12 * S * (dz.abs() @ B.abs()).t() @ x.abs()
+        t_dB = S * t_dz.t() @ (x.abs() @ A.abs().t()) * (1 + 2 ** -4)
+        t_dx = t_dz @ W.abs() + S * (t_dz @ B.abs()) @ A.abs()
+        rstd = torch.tensor(f64(s.rstd))[:, None]
+        xh = (h - mean) * rstd
+        g = t_dx * w.abs()
+        t_dh = rstd * (g + g.mean(1, keepdim=True) + xh.abs() * (g * xh.abs()).mean(1, keepdim=True))
+        t_dw, t_db = (t_dx * xh.abs()).sum(0), t_dx.sum(0)
+    near(f64(s.dz), dz.numpy(), t_dz.numpy() * 1.5 + 1e-9, "dz")
+    for got, ref, tol, what in ((s.dA, A.grad, t_dA, "dA"), (s.dB, B.grad, t_dB, "dB"), (s.dh, h.grad, t_dh, "dh"),
+                                (s.dw, w.grad, t_dw, "dw"), (s.db, b.grad, t_db, "db")):
+        near(f64(got), ref.numpy(), tol.numpy() * 1.1 + 1e-9, what)
+    norm = np.sqrt(sum((f64(t) ** 2).sum() for t in (s.dA, s.dB, s.dw, s.db)))
+    near(f64(s.norm), [norm], 2 * U * norm, "norm")
+    assert norm > 0.05  # clipped
+    flat = np.concatenate([f64(t).ravel() for t in (s.dA, s.dB, s.dw, s.db)]) * (0.05 / norm)
+    near(f64(s.flat), flat, 4 * U * np.abs(flat) + 1e-38, "clipped gradients")
+    assert np.all(f64(s.dz).reshape(N_SEQ, T, V)[:, :START] == 0) and s.err.item() == 0
+
+
+def test_step_replays_in_a_hip_graph(dev):
+    import torch
+    say("update step in a graph")
+    s, other = Step(dev, 1), Step(dev, 2)
+    s.run()
+    other.run()
+    torch.cuda.synchronize()
+    eager, eager_other = s.results(), other.results()
+    g, g2 = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        s.run()
+    with torch.cuda.graph(g2):  # without workspaces: the capture's own memory
+        s.run(own_workspaces=False)
+    torch.cuda.synchronize()
+    for rep in range(3):
+        for graph in (g, g2):
+            s.clear()
+            other.run()  # eager work between the replays
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            for k, v in s.results().items():
+                assert np.array_equal(v, eager[k]), f"replay {rep}: {k}"
+    for k, v in other.results().items():
+        assert np.array_equal(v, eager_other[k]), k
+
+
+def test_step_on_another_stream(dev):
+    import torch
+    say("update step on another stream")
+    s = Step(dev, 3)
+    s.run()
+    torch.cuda.synchronize()
+    want = s.results()
+    side = torch.cuda.Stream(dev)
+    for own in (True, False):
+        s.clear()
+        side.wait_stream(torch.cuda.current_stream())
+        s.run(stream=side, own_workspaces=own)
+        side.synchronize()
+        for k, v in s.results().items():
+            assert np.array_equal(v, want[k]), k
+
+
+def test_two_threads_on_two_streams(dev):
+    import torch
+    say("two threads")
+    steps = [Step(dev, 4), Step(dev, 5)]
+    for s in steps:
+        s.run()
+    torch.cuda.synchronize()
+    want = [s.results() for s in steps]
+    fail = []
+
+    def work(i):
+        try:
+            st = torch.cuda.Stream(dev)
+            for _ in range(5):
+                steps[i].run(stream=st)
+            st.synchronize()
+        except Exception as e:  # noqa: BLE001
+            fail.append(e)
+
+    for s in steps:
+        s.clear()
+    torch.cuda.synchronize()
+    ts = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in ts:
+        t.start()
+    for t in ts:
+        t.join()
+    assert not fail, fail
+    for s, w in zip(steps, want):
+        for k, v in s.results().items():
+            assert np.array_equal(v, w[k]), k
+
+
+def test_python_path_has_the_bits_of_the_native_one(dev, monkeypatch):
+    import torch
+    say("python path")
+    assert not isinstance(Bd._native(), Bd._NoNative)
+    s = Step(dev, 6)
+    s.run()
+    torch.cuda.synchronize()
+    want = s.results()
+    monkeypatch.setattr(Bd, "_nat", Bd._NoNative())
+    for own in (True, False):
+        s.clear()
+        s.run(own_workspaces=own)
+        torch.cuda.synchronize()
+        for k, v in s.results().items():
+            assert np.array_equal(v, want[k]), k
+    norm = torch.empty(1, device=dev)
+    H.hydra_grad_norm([s.dA, s.dB, s.dw, s.db], norm)
+    assert norm.item() == s.norm.item()
+
+
+def test_16_bit_integer_views_are_bf16(dev):
+    import torch
+    s = Step(dev, 7)
+    s.run()
+    i16 = torch.int16
+    y, dx = torch.empty((M, K), dtype=i16, device=dev), torch.empty((M, K), dtype=i16, device=dev)
+    H.hydra_layer_norm(s.x.view(i16), s.w.view(i16), s.b.view(i16), y)
+    z = torch.empty((M, K), dtype=torch.bfloat16, device=dev)
+    H.hydra_layer_norm(s.x, s.w, s.b, z)
+    assert torch.equal(y.view(torch.bfloat16), z)
+    d = torch.empty_like(s.dz)
+    zb = s.z.bfloat16()
+    H.hydra_token_logprobs_backward(zb, s.tokens, s.lse, d, s.d_lp)
+    d2 = torch.empty((M, V), dtype=i16, device=dev)
+    H.hydra_token_logprobs_backward(zb.view(i16), s.tokens, s.lse, d2, s.d_lp)
+    assert torch.equal(d, d2.view(torch.bfloat16))
+    H.hydra_layer_norm_backward(s.x.view(i16), s.x.view(i16), s.w, s.mean, s.rstd, dx)
+    assert torch.isfinite(dx.view(torch.bfloat16).float()).all()
+
+
+@pytest.mark.parametrize("what", ["host_x", "half_x", "w_and_b", "short_mean", "strided_y", "one_row_short"])
+def test_layer_norm_refusals(what, dev):
+    import torch
+    s = Step(dev, 8)
+    a = dict(x=s.h, weight=s.w, bias=s.b, y=torch.full((M, K), 7.0, device=dev), mean=s.mean, rstd=s.rstd)
+    exc = ValueError
+    if what == "host_x":
+        a["x"] = a["x"].cpu()
+    elif what == "half_x":
+        a["x"], exc = a["x"].half(), TypeError
+    elif what == "w_and_b":
+        a["bias"], exc = a["bias"].float(), TypeError
+    elif what == "short_mean":
+        a["mean"] = a["mean"][:-1]
+    elif what == "strided_y":
+        a["y"] = torch.full((M, 2 * K), 7.0, device=dev)[:, ::2]
+    elif what == "one_row_short":
+        a["y"] = a["y"][:-1]
+    with pytest.raises(exc):
+        H.hydra_layer_norm(**a)
+    torch.cuda.synchronize()
+    assert (a["y"] == 7).all()
+
+
+@pytest.mark.parametrize("what", ["tokens_64", "transposed", "top_shape", "small_workspace", "d_shape", "overlapping_rows",
+                                  "stream_of_another_kind"])
+def test_token_logprob_refusals(what, dev):
+    import torch
+    z = torch.randn(4, 200000, device=dev)
+    tok = torch.zeros(4, dtype=torch.int32, device=dev)
+    lp = torch.full((4,), 7.0, device=dev)
+    ids = torch.zeros((4, 3), dtype=torch.int32, device=dev)
+    exc, kw = ValueError, {}
+    args = [z, tok, lp]
+    if what == "tokens_64":
+        args[1], exc = tok.long(), TypeError
+    elif what == "transposed":
+        args[0] = torch.randn(200000, 4, device=dev).t()
+    elif what == "top_shape":
+        kw = dict(top_ids=ids, top_lp=torch.zeros(4, 2, device=dev))
+    elif what == "small_workspace":
+        kw, exc = dict(top_ids=ids, workspace=torch.zeros(16, dtype=torch.uint8, device=dev)), H.HydraError
+    elif what == "d_shape":
+        with pytest.raises(ValueError):
+            H.hydra_token_logprobs_backward(z, tok, lp, z[:3], lp)
+        return
+    elif what == "overlapping_rows":
+        args[0] = z.view(-1).as_strided((4, 100), (50, 1))
+    elif what == "stream_of_another_kind":
+        kw, exc = dict(stream=12345), AttributeError
+    with pytest.raises(exc):
+        H.hydra_token_logprobs(*args, **kw)
+    torch.cuda.synchronize()
+    assert (lp == 7).all()
