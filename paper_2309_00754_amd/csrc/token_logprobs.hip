@@ -448,12 +448,30 @@ __global__ __launch_bounds__(64) void token_logp_join_kernel(TokenLogpArgs a, in
 
 // ---- gradient
 
+constexpr int64_t kCacheBytes = int64_t(256) << 20;  // the memory-side cache
 constexpr int TB_THREADS = 256;
-constexpr int TB_U = 4;
+constexpr int TB_U = 2;  // (4: 2048 x 32000 56.5 us, so 52.3; 250 x 50272 bf16 10.5 and 9.8)
 
+typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4_t;
+typedef __attribute__((__vector_size__(2 * sizeof(uint32_t)))) uint32_t u32x2_t;
+template <bool FAR, class V>
+__device__ __forceinline__ V fetch(const V* p) {
+  return FAR ? __builtin_nontemporal_load(p) : *p;
+}
+template <bool FAR, class V>
+__device__ __forceinline__ void put(V* p, V v) {
+  if constexpr (FAR)
+    __builtin_nontemporal_store(v, p);
+  else
+    *p = v;
+}
+
+// FAR: past the caches, for logits and gradient that they cannot hold together
+// anyway (2048 x 32000 fp32 into bf16, 393 MB: 47.6 us, so 52.3; but 250 x 50272
+// bf16, 50 MB: 11.6 and 9.8).
 // Stretches of `per` groups; workgroup b takes stretches b, b + gridDim.x, ...
 // of the M * n of all rows.
-template <int TZ, int TD>
+template <int TZ, int TD, bool FAR>
 __global__ __launch_bounds__(TB_THREADS) void token_logp_back_kernel(TokenLogpBackArgs a, int n, int per) {
   constexpr int VEC = kVec<TZ>, ZB = 16 / VEC, DB = TD == kF32 ? 4 : 2;
   constexpr int STORE = VEC * DB < 16 ? VEC * DB : 16;  // bytes
@@ -492,14 +510,14 @@ __global__ __launch_bounds__(TB_THREADS) void token_logp_back_kernel(TokenLogpBa
       for (int e = e0 + t; e < e1; e += TB_THREADS) one(e);
       continue;
     }
-    const uint4* const zv = reinterpret_cast<const uint4*>(z + (size_t)head * ZB);
+    const u32x4_t* const zv = reinterpret_cast<const u32x4_t*>(z + (size_t)head * ZB);
     uint8_t* const dv = d + (size_t)head * DB;
     for (int g = g0 + t; g < g1; g += TB_THREADS * TB_U) {
-      uint4 u[TB_U];
+      u32x4_t u[TB_U];
       if (live) {
 #pragma unroll
         for (int q = 0; q < TB_U; ++q)
-          if (g + q * TB_THREADS < g1) u[q] = zv[g + q * TB_THREADS];
+          if (g + q * TB_THREADS < g1) u[q] = fetch<FAR>(zv + g + q * TB_THREADS);
       }
 #pragma unroll
       for (int q = 0; q < TB_U; ++q) {
@@ -507,7 +525,7 @@ __global__ __launch_bounds__(TB_THREADS) void token_logp_back_kernel(TokenLogpBa
         if (at >= g1) break;
         float f[VEC];
         if (live) {
-          unpack<TZ>(u[q], f);
+          unpack<TZ>(__builtin_bit_cast(uint4, u[q]), f);
 #pragma unroll
           for (int e = 0; e < VEC; ++e) f[e] = gradient(f[e]);
           const int mine = tk - head - at * VEC;  // the token's place in this group
@@ -528,12 +546,12 @@ __global__ __launch_bounds__(TB_THREADS) void token_logp_back_kernel(TokenLogpBa
             w[e] = (uint32_t)f32_to_bf16_any(f[2 * e]) | ((uint32_t)f32_to_bf16_any(f[2 * e + 1]) << 16);
         }
         if constexpr (VEC * DB == 8) {
-          reinterpret_cast<uint2*>(dv)[at] = make_uint2(w[0], w[1]);
+          put<FAR>(reinterpret_cast<u32x2_t*>(dv) + at, u32x2_t{w[0], w[1]});
         } else {
 #pragma unroll
           for (int e = 0; e < VEC * DB / 16; ++e)
-            reinterpret_cast<uint4*>(dv)[at * (VEC * DB / 16) + e] =
-                make_uint4(w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]);
+            put<FAR>(reinterpret_cast<u32x4_t*>(dv) + at * (VEC * DB / 16) + e,
+                     u32x4_t{w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]});
         }
       }
     }
@@ -586,7 +604,7 @@ hipError_t launch_token_logp(const TokenLogpArgs& a, void* ws, hipStream_t strea
   return hipGetLastError();
 }
 
-template <int TZ>
+template <int TZ, int TD>
 static void back_of(const TokenLogpBackArgs& a, hipStream_t stream) {
   // a stretch is one round of the workgroup's loads, or several where there are many
   constexpr int ROUND = TB_THREADS * TB_U;
@@ -597,17 +615,17 @@ static void back_of(const TokenLogpBackArgs& a, hipStream_t stream) {
   const int n = (groups + per - 1) / per;
   const int64_t all = (int64_t)a.M * n;
   const dim3 grid((unsigned)(all < (1 << 20) ? all : 1 << 20)), block(TB_THREADS);
-  if (a.d_type == kF32)
-    hipLaunchKernelGGL((token_logp_back_kernel<TZ, kF32>), grid, block, 0, stream, a, n, per);
+  if ((int64_t)a.M * a.V * (int64_t)(type_bytes(TZ) + type_bytes(TD)) > kCacheBytes)
+    hipLaunchKernelGGL((token_logp_back_kernel<TZ, TD, true>), grid, block, 0, stream, a, n, per);
   else
-    hipLaunchKernelGGL((token_logp_back_kernel<TZ, kBf16>), grid, block, 0, stream, a, n, per);
+    hipLaunchKernelGGL((token_logp_back_kernel<TZ, TD, false>), grid, block, 0, stream, a, n, per);
 }
 
 hipError_t launch_token_logp_back(const TokenLogpBackArgs& a, hipStream_t stream) {
   if (a.type == kF32)
-    back_of<kF32>(a, stream);
+    a.d_type == kF32 ? back_of<kF32, kF32>(a, stream) : back_of<kF32, kBf16>(a, stream);
   else
-    back_of<kBf16>(a, stream);
+    a.d_type == kF32 ? back_of<kBf16, kF32>(a, stream) : back_of<kBf16, kBf16>(a, stream);
   return hipGetLastError();
 }
 
