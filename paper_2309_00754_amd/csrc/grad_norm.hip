@@ -15,8 +15,9 @@
 //    results past the cache 265, backwards 254, with the reads too 229; of
 //    Llama-7B at rank 16 into bf16 (160 MB) 92, 83, 82, 79.  The sums alone run
 //    at 5.3 TB/s.
-// Pointers and sizes travel as kernel arguments, kSegs runs a launch; tensors
-// that lie side by side, as views of one buffer do, are one run.  A workgroup
+// Pointers and sizes travel as kernel arguments, 256 runs a launch of the sums
+// and 176 of the scaling; tensors that lie side by side, as views of one buffer
+// do, are one run.  A workgroup
 // takes an equal share of a launch's chunks, one stretch of them: chunks dealt
 // in turn, each with its own search for the tensor and its own wait, took 303
 // us where this takes 283.
@@ -30,20 +31,50 @@ namespace hydra {
 namespace {
 
 constexpr int GN_THREADS = 256;
-constexpr int kSegs = 128;       // (28 bytes each: below the 4 KB of arguments of a launch)
 constexpr int kMaxParts = 2048;  // of all launches of a call
 constexpr int kWorkgroups = 1024;  // of a launch at most
 constexpr int kLogChunk = 11;    // elements of a chunk
 
-struct GradSegs {
-  const void* g[kSegs];
-  void* out[kSegs];
-  int64_t numel[kSegs];
-  int chunk0[kSegs];  // first chunk of the run
-  uint8_t g_type[kSegs], out_type[kSegs];
-  int n, chunks;
+// Tensors side by side in memory, as one.
+struct Run {
+  const void* g;
+  void* out;
+  int64_t numel;
+  int g_type, out_type;
 };
-static_assert(sizeof(GradSegs) <= 4000, "kernel arguments");
+
+// The runs of a launch.  `last` holds the elements of a run's last chunk less
+// one, and above them its two types.
+template <int N, bool OUT>
+struct GradSegs {
+  static constexpr int kMost = N;
+  const void* g[N];
+  void* out[OUT ? N : 1];
+  int chunk0[N + 1];  // first chunk of each run, and the end
+  uint16_t last[N];
+  int n;
+  __device__ __forceinline__ int64_t numel(int i) const {
+    return ((int64_t)(chunk0[i + 1] - chunk0[i] - 1) << kLogChunk) + (last[i] & ((1 << kLogChunk) - 1)) + 1;
+  }
+  __device__ __forceinline__ int g_type(int i) const { return (last[i] >> kLogChunk) & 1; }
+  __device__ __forceinline__ int out_type(int i) const { return (last[i] >> (kLogChunk + 1)) & 1; }
+  // The next runs, from `r` on; returns how many.
+  int fill(const Run* r, int64_t left) {
+    chunk0[0] = 0;
+    for (n = 0; n < N && n < left; ++n) {
+      g[n] = r[n].g;
+      if constexpr (OUT) out[n] = r[n].out;
+      chunk0[n + 1] = chunk0[n] + (int)((r[n].numel + (int64_t(1) << kLogChunk) - 1) >> kLogChunk);
+      last[n] = (uint16_t)(((r[n].numel - 1) & ((1 << kLogChunk) - 1)) | r[n].g_type << kLogChunk |
+                           r[n].out_type << (kLogChunk + 1));
+    }
+    return n;
+  }
+  __host__ __device__ int chunks() const { return chunk0[n]; }
+};
+using SumSegs = GradSegs<256, false>;
+using ScaleSegs = GradSegs<176, true>;
+static_assert(sizeof(SumSegs) <= 4000 && sizeof(ScaleSegs) <= 4000, "kernel arguments");
 
 __device__ __forceinline__ float load1(const void* p, int type, int64_t i) {
   return type == kF32 ? static_cast<const float*>(p)[i] : bf16_to_f32(static_cast<const uint16_t*>(p)[i]);
@@ -57,11 +88,11 @@ __device__ __forceinline__ void store1(void* p, int type, int64_t i, float v) {
 }
 
 // The run that chunk c belongs to: every lane compares the starts of some.
-__device__ __forceinline__ int seg_of(const GradSegs& s, int c) {
+template <class Segs>
+__device__ __forceinline__ int seg_of(const Segs& s, int c) {
   const int lane = threadIdx.x & 63;
   int n = 0;
-#pragma unroll
-  for (int i = 0; i < kSegs; i += 64) n += __popcll(__ballot(i + lane < s.n && s.chunk0[i + lane] <= c));
+  for (int i = 0; i < s.n; i += 64) n += __popcll(__ballot(i + lane < s.n && s.chunk0[i + lane] <= c));
   return __builtin_amdgcn_readfirstlane(n - 1);
 }
 
@@ -98,13 +129,13 @@ __device__ __forceinline__ Piece piece_of(const void* g, int64_t numel, int64_t 
 
 // f(run, first chunk, end) for this workgroup's chunks: an equal share of all of
 // them, in order (k: which share).
-template <class F>
-__device__ __forceinline__ void each_piece(const GradSegs& s, int k, F f) {
-  const int64_t all = s.chunks;
+template <class Segs, class F>
+__device__ __forceinline__ void each_piece(const Segs& s, int k, F f) {
+  const int64_t all = s.chunks();
   int c = (int)(all * k / gridDim.x);
   const int end = (int)(all * (k + 1) / gridDim.x);
   for (int i = seg_of(s, c); c < end; ++i) {
-    const int stop = i + 1 < s.n ? min(end, s.chunk0[i + 1]) : end;
+    const int stop = min(end, s.chunk0[i + 1]);
     f(i, (int64_t)(c - s.chunk0[i]), (int64_t)(stop - s.chunk0[i]));
     c = stop;
   }
@@ -162,13 +193,13 @@ __device__ __forceinline__ void sum_piece(const void* g, int64_t numel, int64_t 
   });
 }
 
-__global__ __launch_bounds__(GN_THREADS) void grad_sum_kernel(GradSegs s, double* part) {
+__global__ __launch_bounds__(GN_THREADS) void grad_sum_kernel(SumSegs s, double* part) {
   double sum[4] = {0.0, 0.0, 0.0, 0.0};
   each_piece(s, blockIdx.x, [&](int i, int64_t c0, int64_t c1) __attribute__((always_inline)) {
-    if (s.g_type[i] == kF32)
-      sum_piece<kF32>(s.g[i], s.numel[i], c0, c1, sum);
+    if (s.g_type(i) == kF32)
+      sum_piece<kF32>(s.g[i], s.numel(i), c0, c1, sum);
     else
-      sum_piece<kBf16>(s.g[i], s.numel[i], c0, c1, sum);
+      sum_piece<kBf16>(s.g[i], s.numel(i), c0, c1, sum);
   });
   const double v = block_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
   if (threadIdx.x == 0) part[blockIdx.x] = v;
@@ -229,7 +260,7 @@ __device__ __forceinline__ void scale_piece(const void* g, void* out, int64_t nu
   edges<VEC>(p, [&](int64_t e) { store1(out, TO, e, load1(g, TG, e) * c); });
 }
 
-__global__ __launch_bounds__(GN_THREADS) void grad_scale_kernel(GradSegs s, const double* part, int parts,
+__global__ __launch_bounds__(GN_THREADS) void grad_scale_kernel(ScaleSegs s, const double* part, int parts,
                                                                 float max_norm, float* norm, int32_t* err) {
   const double v = norm_of(part, parts);
   const bool finite = (float)v <= 3.4028235e38f;
@@ -241,15 +272,15 @@ __global__ __launch_bounds__(GN_THREADS) void grad_scale_kernel(GradSegs s, cons
   each_piece(s, gridDim.x - 1 - blockIdx.x, [&](int i, int64_t c0, int64_t c1) __attribute__((always_inline)) {
     const void* const g = s.g[i];
     void* const out = s.out[i];
-    const int64_t numel = s.numel[i];
+    const int64_t numel = s.numel(i);
     if (c == 1.f && out == g) return;
-    if (s.g_type[i] == kF32) {
-      if (s.out_type[i] == kF32)
+    if (s.g_type(i) == kF32) {
+      if (s.out_type(i) == kF32)
         scale_piece<kF32, kF32>(g, out, numel, c0, c1, c);
       else
         scale_piece<kF32, kBf16>(g, out, numel, c0, c1, c);
     } else {
-      if (s.out_type[i] == kF32)
+      if (s.out_type(i) == kF32)
         scale_piece<kBf16, kF32>(g, out, numel, c0, c1, c);
       else
         scale_piece<kBf16, kBf16>(g, out, numel, c0, c1, c);
@@ -257,37 +288,24 @@ __global__ __launch_bounds__(GN_THREADS) void grad_scale_kernel(GradSegs s, cons
   });
 }
 
-// The next runs of the list, from tensor i on (empty tensors left out, tensors
-// side by side joined).
-int64_t take(const GradArgs& a, int64_t i, GradSegs& s) {
-  s.n = 0;
-  for (; i < a.n; ++i) {
+// The list as runs (empty tensors left out, tensors side by side joined).
+int join(const GradArgs& a, Run* runs) {
+  int n = 0;
+  for (int64_t i = 0; i < a.n; ++i) {
     if (a.numels[i] == 0) continue;
-    const uint8_t gt = (uint8_t)a.types[i], ot = a.clip && a.outs ? (uint8_t)a.out_types[i] : gt;
-    void* const out = a.clip && a.outs ? a.outs[i] : const_cast<void*>(a.g[i]);
-    if (s.n > 0) {
-      const int p = s.n - 1;
-      if (s.g_type[p] == gt && s.out_type[p] == ot &&
-          static_cast<const uint8_t*>(s.g[p]) + s.numel[p] * type_bytes(gt) == a.g[i] &&
-          static_cast<uint8_t*>(s.out[p]) + s.numel[p] * type_bytes(ot) == out) {
-        s.numel[p] += a.numels[i];
+    const int gt = a.types[i], ot = a.outs ? a.out_types[i] : gt;
+    void* const out = a.outs ? a.outs[i] : const_cast<void*>(a.g[i]);
+    if (n > 0) {
+      Run& p = runs[n - 1];
+      if (p.g_type == gt && p.out_type == ot && static_cast<const uint8_t*>(p.g) + p.numel * type_bytes(gt) == a.g[i] &&
+          static_cast<uint8_t*>(p.out) + p.numel * type_bytes(ot) == out) {
+        p.numel += a.numels[i];
         continue;
       }
     }
-    if (s.n == kSegs) break;
-    s.g[s.n] = a.g[i];
-    s.out[s.n] = out;
-    s.numel[s.n] = a.numels[i];
-    s.g_type[s.n] = gt;
-    s.out_type[s.n] = ot;
-    ++s.n;
+    runs[n++] = Run{a.g[i], out, a.numels[i], gt, ot};
   }
-  s.chunks = 0;
-  for (int k = 0; k < s.n; ++k) {
-    s.chunk0[k] = s.chunks;
-    s.chunks += (int)((s.numel[k] + (int64_t(1) << kLogChunk) - 1) >> kLogChunk);
-  }
-  return i;
+  return n;
 }
 
 }  // namespace
@@ -296,30 +314,28 @@ size_t grad_ws_bytes() { return kMaxParts * sizeof(double); }
 
 hipError_t launch_grad_norm(const GradArgs& a, void* ws, hipStream_t stream) {
   double* part = static_cast<double*>(ws);
-  GradSegs s;
-  int64_t first[kMaxGrads / kSegs + 1];  // tensor that each launch starts with
-  int runs = 0, parts = 0;
-  for (int64_t i = 0; i < a.n;) {
-    first[runs] = i;
-    i = take(a, i, s);
-    if (s.n > 0) ++runs;
-  }
-  const int most = runs > 2 ? kMaxParts / runs : kWorkgroups;
-  for (int r = 0; r < runs; ++r) {
-    if (runs > 1) take(a, first[r], s);
-    const int grid = s.chunks < most ? s.chunks : most;
+  Run runs[kMaxGrads];  // (on the stack: the library allocates nothing)
+  const int n = join(a, runs);
+  const int sums = (n + SumSegs::kMost - 1) / SumSegs::kMost;
+  const int most = sums > 2 ? kMaxParts / sums : kWorkgroups;
+  int parts = 0;
+  SumSegs s;
+  for (int r = 0; r < n;) {
+    r += s.fill(runs + r, n - r);
+    const int grid = s.chunks() < most ? s.chunks() : most;
     hipLaunchKernelGGL(grad_sum_kernel, dim3(grid), dim3(GN_THREADS), 0, stream, s, part + parts);
     parts += grid;
   }
-  if (!a.clip || runs == 0) {
+  if (!a.clip || n == 0) {
     hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(GN_THREADS), 0, stream, part, parts, a.norm);
     return hipGetLastError();
   }
-  for (int r = runs - 1; r >= 0; --r) {
-    if (runs > 1) take(a, first[r], s);
-    const int grid = s.chunks < kWorkgroups ? s.chunks : kWorkgroups;
-    hipLaunchKernelGGL(grad_scale_kernel, dim3(grid), dim3(GN_THREADS), 0, stream, s, part, parts, a.max_norm,
-                       r == 0 ? a.norm : nullptr, a.err);
+  ScaleSegs o;
+  for (int l = (n - 1) / ScaleSegs::kMost; l >= 0; --l) {
+    o.fill(runs + l * ScaleSegs::kMost, n - l * ScaleSegs::kMost);
+    const int grid = o.chunks() < kWorkgroups ? o.chunks() : kWorkgroups;
+    hipLaunchKernelGGL(grad_scale_kernel, dim3(grid), dim3(GN_THREADS), 0, stream, o, part, parts, a.max_norm,
+                       l == 0 ? a.norm : nullptr, a.err);
   }
   return hipGetLastError();
 }

@@ -293,6 +293,34 @@ def test_gradient_against_differences_of_the_forward(dev):
     near(f64(dz)[0], (f[:12] - f[12:]) / (2 * h), 4e-4, "gradient")
 
 
+@pytest.mark.parametrize("kind,d_kind,M", [("f32", "f32", 700), ("f32", "bf16", 930), ("bf16", "f32", 930),
+                                           ("bf16", "bf16", 1400)])
+def test_gradient_larger_than_the_caches(kind, d_kind, M, dev):
+    """Logits and gradient of more than 256 MB together go past the caches: the bits of the same rows in smaller calls,
+    and a few rows against the oracle."""
+    import torch
+    say("large gradient", kind, d_kind, M)
+    V = 50001  # (rows at every alignment)
+    gen = torch.Generator(device=dev)
+    gen.manual_seed(M)
+    z = torch.randn(M, V, generator=gen, device=dev).to(empty(1, kind, dev).dtype)
+    tok = torch.randint(0, V, (M,), generator=gen, device=dev, dtype=torch.int32)
+    lse, d_lp = torch.logsumexp(z.float(), 1), torch.randn(M, generator=gen, device=dev)
+    d_lp[::3] = 0
+    dz = torch.full((M, V), float("nan"), device=dev, dtype=empty(1, d_kind, dev).dtype)
+    assert z.numel() * (z.element_size() + dz.element_size()) > 1 << 28
+    H.hydra_token_logprobs_backward(z, tok, lse, dz, d_lp)
+    part = torch.empty_like(dz)
+    for m in range(0, M, 280):
+        r = slice(m, m + 280)
+        H.hydra_token_logprobs_backward(z[r], tok[r], lse[r], part[r], d_lp[r])
+    assert torch.equal(dz, part)
+    rows = [0, 1, 2, M - 1]
+    zz, t = f64(z[rows]), [f64(v[rows]) for v in (lse, d_lp)]
+    ref = token_logprobs_backward_ref(zz, tok[rows].cpu().numpy(), *t)
+    near(f64(dz[rows]), ref, logp_back_bounds(zz, t[0], t[1], None, None, ref, d_kind), "d_logits")
+
+
 def test_rows_past_2_to_the_31_elements(dev):
     """Rows so far apart that their offsets leave 32 bits (a strided view of one large bf16 buffer)."""
     import torch
