@@ -310,13 +310,18 @@ __global__ __launch_bounds__(THREADS) void norm_back_kernel(LayerNormBackArgs a,
       for (int e = 0; e < VEC; ++e)
         acc[((group * NCH + c) * VEC + e) * lanes + at0] = which ? db[c][e] : dw[c][e];
     __syncthreads();
+    const __amdgpu_buffer_rsrc_t pr = make_rsrc(p + (size_t)blockIdx.x * 2 * K, (uint32_t)K * 4u);
     const int shift = 31 - __builtin_clz(lanes);
-    for (int i = threadIdx.x; i < lanes * NCH * VEC; i += THREADS) {
-      const int ce = i >> shift, k = (ce / VEC) * step + (i & (lanes - 1)) * VEC + ce % VEC;
+    for (int i = threadIdx.x; i < lanes * NCH; i += THREADS) {  // a lane's place and chunk: whole chunks go out
+      const int c = i >> shift, at = i & (lanes - 1), k = c * step + at * VEC;
       if (k >= K) continue;
-      float v = acc[i];
-      for (int g = 1; g < groups; ++g) v += acc[g * NCH * VEC * lanes + i];
-      p[(size_t)blockIdx.x * 2 * K + k] = v;
+      float f[VEC];
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        f[e] = acc[(c * VEC + e) * lanes + at];
+        for (int g = 1; g < groups; ++g) f[e] += acc[((g * NCH + c) * VEC + e) * lanes + at];
+      }
+      store_chunk<VEC>(pr, kF32, k, f);
     }
     __syncthreads();
   }
@@ -445,7 +450,7 @@ __global__ __launch_bounds__(COL_THREADS) void norm_back_cols_kernel(LayerNormBa
 // chunk's address takes a register too, and 32 spill.
 constexpr int kFew = 16, kMany = 32;
 constexpr int kFewK = kMaxWaves * 64 * kFew, kManyK = kMaxWaves * 64 * kMany;
-constexpr int FWD_THREADS = 256;
+constexpr int FWD_THREADS = 256, BACK_THREADS = 512;
 
 // Waves per row: enough for `lane` columns a lane.
 int row_waves(int K, int lane) {
@@ -454,23 +459,15 @@ int row_waves(int K, int lane) {
   return nw;
 }
 
-// Threads of the backward's workgroups: 1024 from 512 rows on (700 x 2048 fp32 11.8
-// us, with 512 threads 12.5; 1024 x 4096 bf16 16.0 and 17.6, 8192 x 4096 48.6 and
-// 53.1; but 333 x 4096 13.3 and 12.8), save for much fp32 on both sides (8192 x
-// 4096 87.4 and 81.5).  Element by element that many registers are not there.
-int back_threads(const LayerNormBackArgs& a, int vec) {
-  const bool both32 = a.dy_type == kF32 && a.x_type == kF32;
-  return vec > 1 && a.K <= kFewK && a.M >= 512 && (!both32 || (int64_t)a.M * a.K <= (1 << 23)) ? 1024 : 512;
-}
-
 // Workgroups of the backward.  Each writes a part of dw and db that
 // norm_back_sum_kernel reads again: one a CU, half as many where the rows are
-// few (M K up to 2^22: 700 x 2048 bf16 10.6 us, so 11.5; 333 x 4096 12.8, so
-// 13.8; 4096 x 2048 21.1, so 18.7), and a single one, which needs no second
-// launch, where that takes it two rounds of rows at most (8 x 2048: 7.7 us with
-// the launch).
-int back_blocks(int M, int K, int nw, int threads) {
-  const int groups = threads / 64 / nw, want = (M + groups - 1) / groups;
+// few (M K up to 2^22: 700 x 2048 fp32 and bf16 11.3 us, so 11.8; 700 x 4096 bf16
+// 13.9, so 15.4; but 4096 x 4096 42.3, so 30.4), and a single one, which needs no
+// second launch, where that takes it two rounds of rows at most (8 x 2048: 7.7 us
+// with the launch).  Workgroups of 1024 threads gain up to 6% on much bf16 (8192
+// x 4096 47.1 us, so 50.2) and lose as much on fp32 (86.6, so 81.0) and few rows.
+int back_blocks(int M, int K, int nw) {
+  const int groups = BACK_THREADS / 64 / nw, want = (M + groups - 1) / groups;
   if (want <= 2) return 1;
   const int most = (int64_t)M * K <= (1 << 22) ? 128 : 256;
   return want < most ? want : most;
@@ -527,22 +524,16 @@ template <int TD, int TX, int VEC>
 int backward(const LayerNormBackArgs& a, float* part, hipStream_t stream) {
   const bool few = a.K <= kFewK;
   if (!few && (VEC == 1 || a.K > kManyK)) return 0;
-  const int nw = row_waves(a.K, few ? kFew : kMany), threads = back_threads(a, VEC);
-  const int blocks = back_blocks(a.M, a.K, nw, threads);
+  const int nw = row_waves(a.K, few ? kFew : kMany), blocks = back_blocks(a.M, a.K, nw);
   float* const pw = blocks > 1 ? part : a.dw;
   float* const pb = blocks > 1 && part ? part + a.K : a.db;
-  if constexpr (VEC > 1) {
-    if (!few) {
-      hipLaunchKernelGGL((norm_back_kernel<TD, TX, VEC, kMany / VEC, 512>), dim3(blocks), dim3(512), 0, stream, a, pw, pb, nw);
-      return blocks;
-    }
-    if (threads == 1024) {
-      hipLaunchKernelGGL((norm_back_kernel<TD, TX, VEC, kFew / VEC, 1024>), dim3(blocks), dim3(1024), 0, stream, a, pw, pb,
-                         nw);
-      return blocks;
-    }
+  if (few) {
+    hipLaunchKernelGGL((norm_back_kernel<TD, TX, VEC, kFew / VEC, BACK_THREADS>), dim3(blocks), dim3(BACK_THREADS), 0, stream,
+                       a, pw, pb, nw);
+  } else if constexpr (VEC > 1) {
+    hipLaunchKernelGGL((norm_back_kernel<TD, TX, VEC, kMany / VEC, BACK_THREADS>), dim3(blocks), dim3(BACK_THREADS), 0,
+                       stream, a, pw, pb, nw);
   }
-  hipLaunchKernelGGL((norm_back_kernel<TD, TX, VEC, kFew / VEC, 512>), dim3(blocks), dim3(512), 0, stream, a, pw, pb, nw);
   return blocks;
 }
 
@@ -560,7 +551,7 @@ size_t layer_norm_back_ws_bytes(int M, int K) {
   // (whatever the types and the alignment of the call)
   size_t need = 0;
   if (K <= kManyK)
-    need = (size_t)back_blocks(M, K, row_waves(K, K <= kFewK ? kFew : kMany), 512) * 2 * K * sizeof(float);  // (the more)
+    need = (size_t)back_blocks(M, K, row_waves(K, K <= kFewK ? kFew : kMany)) * 2 * K * sizeof(float);
   if (K > kFewK) {
     int nch, rows;
     long_plan(M, K, nch, rows);
