@@ -329,7 +329,7 @@ __global__ __launch_bounds__(THREADS) void norm_back_kernel(LayerNormBackArgs a,
 
 // dw and db from n parts of [2][K], in order: a workgroup takes 64 of the 2 K
 // columns, each of its waves a run of the parts.
-constexpr int SUM_WAVES = 8;
+constexpr int SUM_WAVES = 16;
 __global__ __launch_bounds__(SUM_WAVES * 64) void norm_back_sum_kernel(const float* part, int n, int K, float* dw,
                                                                       float* db) {
   __shared__ float red[SUM_WAVES][64];

@@ -419,6 +419,8 @@ __global__ __launch_bounds__(64) void token_logp_join_kernel(TokenLogpArgs a, in
   Token token{0, 0.f};
   if (lane == 0) token = token_of<T>(a, row);
   const Stat* const ps = parts.stat + (size_t)row * nseg;
+  const uint64_t* const pk = parts.key + (size_t)row * nseg * k;
+  const uint64_t early = lane < nseg * k ? pk[lane] : 0;
   Stat st{-INFINITY, 0.f, 0.f};
   if (lane < nseg) st = ps[lane];
   rescale(st, wave_all<true>(st.m));
@@ -426,17 +428,24 @@ __global__ __launch_bounds__(64) void token_logp_join_kernel(TokenLogpArgs a, in
   st.w = wave_all<false>(st.w);
   if (lane == 0) finish_row(a, row, st, token);
   if (k == 0) return;
-  // what reaches the greatest of the segments' k-th keys
-  const uint64_t* const pk = parts.key + (size_t)row * nseg * k;
-  uint64_t bound = lane < nseg ? pk[lane * k + k - 1] : 0;
+  uint64_t bound = 0;
+  if (nseg * k > 64) {
+    // of many, what reaches a bound that k keys reach: the greatest of the
+    // segments' k-th keys or the least of their j-th, j = k over the segments
+    // (8 segments of 32 keys: of the first alone 13.2 us)
+    const int j = (k + nseg - 1) / nseg;
+    uint64_t most = lane < nseg ? pk[lane * k + k - 1] : 0, least = lane < nseg ? pk[lane * k + j - 1] : ~0ull;
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) {
-    const uint64_t u = __shfl_xor((unsigned long long)bound, o);
-    bound = u > bound ? u : bound;
+    for (int o = 32; o >= 1; o >>= 1) {
+      const uint64_t u = __shfl_xor((unsigned long long)most, o), v = __shfl_xor((unsigned long long)least, o);
+      most = u > most ? u : most;
+      least = v < least ? v : least;
+    }
+    bound = most > least ? most : least;
   }
   int n = 0;
   for (int i = lane; i - lane < nseg * k; i += 64) {
-    const uint64_t key = i < nseg * k ? pk[i] : 0;
+    const uint64_t key = i < 64 ? early : i < nseg * k ? pk[i] : 0;
     const bool in = key != 0 && key >= bound;
     const uint64_t ins = __ballot(in);
     if (in) cand[n + __popcll(ins & ((1ull << lane) - 1))] = key;
