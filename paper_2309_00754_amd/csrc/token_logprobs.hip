@@ -19,8 +19,12 @@
 // maxima, j = k over the waves; the smallest of these is a bound that at least
 // k logits reach.  The groups whose maximum reaches it are read again (from the
 // cache), and what reaches it there, some tens of logits, is ranked by counting.
-// Ties, masks and values out of order can leave too many for that: then the k
-// are extracted one after the other.
+// Ties, masks of one value and sorted rows can leave too many for that.  Then
+// the k greatest groups by (maximum, lower index) are found exactly, by their
+// maxima's bits from the highest down: they hold the k largest logits, since any
+// logit in another group has one in each of these before it.  (32000 zeros or
+// sorted logits, 32 alternatives, one row: extracting them one after the other
+// took 335 us.)
 #include "hydra_device.h"
 #include "hydra_internal.h"
 
@@ -64,10 +68,12 @@ __device__ __forceinline__ int head_of(const void* row, int V) {
 
 // A whole number that orders logits by value, then by index (the lower one the
 // greater): NaN first, then +inf.  +0 and -0 are one value.  No logit gives 0.
-__device__ __forceinline__ uint64_t order_key(float z, int idx) {
+__device__ __forceinline__ uint32_t order_bits(float z) {
   const uint32_t u = __float_as_uint(z + 0.f);
-  const uint32_t o = z != z ? 0xFFFFFFFEu : (int)u < 0 ? ~u : u | 0x80000000u;
-  return ((uint64_t)o << 32) | (uint32_t)~idx;
+  return z != z ? 0xFFFFFFFEu : (int)u < 0 ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ uint64_t order_key(float z, int idx) {
+  return ((uint64_t)order_bits(z) << 32) | (uint32_t)~idx;
 }
 __device__ __forceinline__ int index_of(uint64_t key) { return (int)~(uint32_t)key; }
 __device__ __forceinline__ float logit_of(uint64_t key) {  // (of -0: +0)
@@ -155,20 +161,78 @@ __device__ __forceinline__ void meet_sums(Stat& a, const Meet& meet) {
   }
 }
 
-__device__ __forceinline__ uint64_t block_max(uint64_t v) {
-  __shared__ uint64_t red[TL_WAVES];
+// How many of n numbers (LDS) are at least `bound` (> 0), in every thread.  `tally`:
+// this call's alone until the workgroup's next barrier but one.
+__device__ __forceinline__ int count_from(const uint32_t* v, int n, uint32_t bound, int* tally) {
+  constexpr int U = 8;
+  int c = 0;
+  for (int i0 = 0; i0 < n; i0 += TL_THREADS * U) {
+    uint32_t x[U];
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) {
-    const uint64_t u = __shfl_xor((unsigned long long)v, o);
-    v = u > v ? u : v;
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * TL_THREADS + threadIdx.x;
+      x[u] = i < n ? v[i] : 0;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) c += __popcll(__ballot(x[u] >= bound));
+  }
+  if ((threadIdx.x & 63) == 0) tally[threadIdx.x >> 6] = c;
+  __syncthreads();
+  c = tally[0];
+#pragma unroll
+  for (int i = 1; i < TL_WAVES; ++i) c += tally[i];
+  return c;
+}
+
+// The `want` greatest of n > want numbers (LDS), the lower index first among
+// equals: their indices to `slot`, in any order (*count of them, 0 before);
+// returns a bound that they and no others but equals of it reach.  `start`: a
+// bound to try first (where ties are what made this necessary it is mostly the
+// one); if fewer than `want` reach it, those alone are taken.
+__device__ __forceinline__ uint32_t greatest(const uint32_t* v, int n, int want, uint32_t start, int* slot, int* count,
+                                             int (*tally)[TL_WAVES]) {
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  uint32_t bound = start;
+  int have = n, turn = 1, above = count_from(v, n, start + 1, tally[0]);
+  if (above >= want) {
+    bound = 0;
+    for (int bit = 31; bit >= 0 && have > want; --bit, turn ^= 1) {
+      const int c = count_from(v, n, bound | (1u << bit), tally[turn]);
+      if (c >= want) {
+        bound |= 1u << bit;
+        have = c;
+      }
+    }
+    if (have > want) {
+      above = count_from(v, n, bound + 1, tally[turn]);
+      turn ^= 1;
+    }
+  }
+  // all above the bound; of its equals (where they are too many) the first
+  int left = want - above;
+  for (int i0 = 0; i0 < n; i0 += TL_THREADS, turn ^= 1) {
+    const int i = i0 + t;
+    const uint32_t x = i < n ? v[i] : 0;
+    bool take = i < n && x > bound;
+    const bool equal = i < n && x == bound;
+    const uint64_t equals = __ballot(equal);
+    if (have > want) {
+      if (lane == 0) tally[turn][wave] = __popcll(equals);
+      __syncthreads();
+      int before = __popcll(equals & ((1ull << lane) - 1)), all = 0;
+      for (int w = 0; w < TL_WAVES; ++w) {
+        before += w < wave ? tally[turn][w] : 0;
+        all += tally[turn][w];
+      }
+      take = take || (equal && before < left);
+      left -= all < left ? all : left;
+    } else {
+      take = take || equal;
+    }
+    if (take) slot[atomicAdd(count, 1)] = i;
   }
   __syncthreads();
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = red[0];
-#pragma unroll
-  for (int i = 1; i < TL_WAVES; ++i) v = red[i] > v ? red[i] : v;
-  return v;
+  return bound;
 }
 
 // lp of a logit, by way of the maximum: of the rounding of lse that of ln S
@@ -279,7 +343,7 @@ __global__ __launch_bounds__(TL_THREADS) void token_logp_kernel(TokenLogpArgs a,
   __shared__ Meet meet;
   // TOP: the waves' bounds, the groups that reach the bound, the logits that do
   __shared__ float bound_of[TOP ? TL_WAVES : 1];
-  __shared__ int slot[TOP ? kCand : 1], count[2];
+  __shared__ int slot[TOP ? kCand : 1], count[2], tally[TOP ? 2 : 1][TL_WAVES];
   __shared__ __align__(16) uint64_t cand[TOP ? kCand : 1];
   const int row = blockIdx.x / nseg, seg = blockIdx.x - row * nseg, t = threadIdx.x, V = a.V;
   const uint8_t* const z = static_cast<const uint8_t*>(a.z) + (size_t)row * a.ld * (16 / VEC);
@@ -382,21 +446,44 @@ __global__ __launch_bounds__(TL_THREADS) void token_logp_kernel(TokenLogpArgs a,
       n = count[1];
     }
     if (n > kCand) {
-      // one after the other: each thread's greatest below the last one
-      uint64_t last = ~0ull;
-      for (n = 0; n < k; ++n) {
-        uint64_t best = 0;
-        const auto see = [&](int e) __attribute__((always_inline)) {
-          const uint64_t key = order_key(load_z<T>(z, e), e);
-          best = key < last && key > best ? key : best;
-        };
-        for (int e = sp.head + sp.g0 * VEC + t; e < sp.head + sp.g1 * VEC; e += TL_THREADS) see(e);
-        if (edge_at >= 0) see(edge_at);
-        last = block_max(best);
-        if (masked_out(last)) break;
-        if (t == 0) cand[n] = last;
+      // by the groups' maxima as whole numbers; of a row with NaN they are formed again
+      __syncthreads();
+      uint32_t* const key = reinterpret_cast<uint32_t*>(most_of);
+      const bool again = !(st.s >= 0.f) || st.m == INFINITY;
+      for (int g = t; g < groups; g += TL_THREADS) {
+        uint32_t most = 0;
+        if (again) {
+          float f[VEC];
+          unpack<T>(v[sp.g0 + g], f);
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) most = max(most, order_bits(f[e]));
+        } else {
+          most = order_bits(most_of[g]);
+        }
+        key[g] = most;
+      }
+      if (t < 2) count[t] = 0;
+      __syncthreads();
+      uint32_t least = 0;
+      if (groups > k) {
+        // (logits in no group can be among those that reach the waves' bound)
+        least = greatest(key, groups, k, again ? 0 : order_bits(bound), slot, &count[0], tally);
+      } else {
+        if (t < groups) slot[t] = t;
+        if (t == 0) count[0] = groups;
+        __syncthreads();
+      }
+      for (int i = t; i < count[0] * VEC; i += TL_THREADS) {
+        const int e = sp.head + (sp.g0 + slot[i / VEC]) * VEC + i % VEC;
+        const uint64_t x = order_key(load_z<T>(z, e), e);
+        if ((uint32_t)(x >> 32) >= least && !masked_out(x)) cand[atomicAdd(&count[1], 1)] = x;
+      }
+      if (edge_at >= 0) {
+        const uint64_t x = order_key(edge, edge_at);
+        if (!masked_out(x)) cand[atomicAdd(&count[1], 1)] = x;
       }
       __syncthreads();
+      n = count[1];
     }
     if (wave != 0) return;
     if (nseg == 1) {
