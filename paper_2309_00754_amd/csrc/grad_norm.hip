@@ -24,8 +24,7 @@
 // Squares are formed and added in 64 bits: an fp32 square of a gradient below
 // 1e-19 or above 1e19 would leave the range, and the conversion and the 64-bit
 // FMA run beside the loads.
-#include "hydra_device.h"
-#include "hydra_internal.h"
+#include "hydra_elem.h"
 
 namespace hydra {
 namespace {
@@ -75,17 +74,6 @@ struct GradSegs {
 using SumSegs = GradSegs<256, false>;
 using ScaleSegs = GradSegs<176, true>;
 static_assert(sizeof(SumSegs) <= 4000 && sizeof(ScaleSegs) <= 4000, "kernel arguments");
-
-__device__ __forceinline__ float load1(const void* p, int type, int64_t i) {
-  return type == kF32 ? static_cast<const float*>(p)[i] : bf16_to_f32(static_cast<const uint16_t*>(p)[i]);
-}
-
-__device__ __forceinline__ void store1(void* p, int type, int64_t i, float v) {
-  if (type == kF32)
-    static_cast<float*>(p)[i] = v;
-  else
-    static_cast<uint16_t*>(p)[i] = f32_to_bf16_any(v);
-}
 
 // The run that chunk c belongs to: every lane compares the starts of some.
 template <class Segs>
@@ -141,24 +129,7 @@ __device__ __forceinline__ void each_piece(const Segs& s, int k, F f) {
   }
 }
 
-template <int T>
-__device__ __forceinline__ void unpack(const uint4& u, float (&f)[16 / (T == kF32 ? 4 : 2)]) {
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (T == kF32) {
-      f[i] = __uint_as_float(w[i]);
-    } else {
-      f[2 * i] = __uint_as_float(w[i] << 16);
-      f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-    }
-  }
-}
-
 constexpr int GN_U = 8;  // 16-byte loads of a thread under way
-
-typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4_t;
-typedef __attribute__((__vector_size__(2 * sizeof(uint32_t)))) uint32_t u32x2_t;
 
 // The elements of a piece that are in no whole group: those before b0 and those
 // after the last group, fewer than 16 of each.
@@ -172,7 +143,7 @@ __device__ __forceinline__ void edges(const Piece& p, F f) {
 
 template <int T>
 __device__ __forceinline__ void sum_piece(const void* g, int64_t numel, int64_t c0, int64_t c1, double (&sum)[4]) {
-  constexpr int VEC = T == kF32 ? 4 : 8;
+  constexpr int VEC = kVec<T>;
   const Piece p = piece_of<VEC>(g, numel, c0, c1);
   const uint4* const v = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(g) + p.b0 * (16 / VEC));
   for (int64_t i = threadIdx.x; i < p.groups; i += GN_THREADS * GN_U) {
@@ -188,7 +159,7 @@ __device__ __forceinline__ void sum_piece(const void* g, int64_t numel, int64_t 
     }
   }
   edges<VEC>(p, [&](int64_t e) {
-    const double x = (double)load1(g, T, e);
+    const double x = (double)load_elem(g, T, e);
     sum[0] = fma(x, x, sum[0]);
   });
 }
@@ -219,11 +190,11 @@ __global__ __launch_bounds__(GN_THREADS) void grad_norm_kernel(const double* par
 template <int TG, int TO>
 __device__ __forceinline__ void scale_piece(const void* g, void* out, int64_t numel, int64_t c0, int64_t c1,
                                             float c) {
-  constexpr int VEC = TG == kF32 ? 4 : 8, OB = TO == kF32 ? 4 : 2;
+  constexpr int VEC = kVec<TG>, OB = TO == kF32 ? 4 : 2;
   constexpr int OUT = VEC * OB < 16 ? VEC * OB : 16;  // bytes of a store
   const Piece p = piece_of<VEC>(g, numel, c0, c1);
   if ((reinterpret_cast<uintptr_t>(out) + p.b0 * OB) % OUT != 0) {  // (the same for every chunk of a run)
-    for (int64_t e = p.e0 + threadIdx.x; e < p.e1; e += GN_THREADS) store1(out, TO, e, load1(g, TG, e) * c);
+    for (int64_t e = p.e0 + threadIdx.x; e < p.e1; e += GN_THREADS) store_elem(out, TO, e, load_elem(g, TG, e) * c);
     return;
   }
   const u32x4_t* const v = reinterpret_cast<const u32x4_t*>(static_cast<const uint8_t*>(g) + p.b0 * (16 / VEC));
@@ -245,7 +216,7 @@ __device__ __forceinline__ void scale_piece(const void* g, void* out, int64_t nu
         if constexpr (TO == kF32)
           w[e] = __float_as_uint(f[e] * c);
         else
-          w[e] = (uint32_t)f32_to_bf16_any(f[2 * e] * c) | ((uint32_t)f32_to_bf16_any(f[2 * e + 1] * c) << 16);
+          w[e] = f32_to_bf16_pair(f[2 * e] * c, f[2 * e + 1] * c);
       }
       if constexpr (VEC * OB == 8) {
         __builtin_nontemporal_store(u32x2_t{w[0], w[1]}, reinterpret_cast<u32x2_t*>(o) + k);
@@ -257,7 +228,7 @@ __device__ __forceinline__ void scale_piece(const void* g, void* out, int64_t nu
       }
     }
   }
-  edges<VEC>(p, [&](int64_t e) { store1(out, TO, e, load1(g, TG, e) * c); });
+  edges<VEC>(p, [&](int64_t e) { store_elem(out, TO, e, load_elem(g, TG, e) * c); });
 }
 
 __global__ __launch_bounds__(GN_THREADS) void grad_scale_kernel(ScaleSegs s, const double* part, int parts,

@@ -85,9 +85,6 @@ __device__ __forceinline__ uint32_t f32_to_bf16_rne(float f) {
   return u >> 16;
 }
 
-// The same for any value (NaN stays NaN), by the hardware's conversion.
-__device__ __forceinline__ uint16_t f32_to_bf16_any(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
-
 // e^x and ln x from the hardware base-2 transcendental units:
 // e^x = 2^(x log2 e), ln x = log2(x) ln 2.
 constexpr float kLog2e = 1.4426950408889634f;

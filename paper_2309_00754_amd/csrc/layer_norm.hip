@@ -18,24 +18,12 @@
 //    norm_back_cols_kernel, a thread per column over a chunk of rows, and
 //    norm_back_sum_kernel.
 // Statistics, products and sums are fp32; results are rounded once.
-#include "hydra_device.h"
-#include "hydra_internal.h"
+#include "hydra_elem.h"
 
 #include <initializer_list>
 
 namespace hydra {
 namespace {
-
-__device__ __forceinline__ float load1(const void* p, int type, size_t i) {
-  return type == kF32 ? static_cast<const float*>(p)[i] : bf16_to_f32(static_cast<const uint16_t*>(p)[i]);
-}
-
-__device__ __forceinline__ void store1(void* p, int type, size_t i, float v) {
-  if (type == kF32)
-    static_cast<float*>(p)[i] = v;
-  else
-    static_cast<uint16_t*>(p)[i] = f32_to_bf16_any(v);
-}
 
 // VEC elements of type T at element `i` of a buffer (zeros where `i` is out of
 // its range), as loaded and as fp32.
@@ -69,8 +57,6 @@ struct Chunk {
 
 template <int VEC>
 __device__ __forceinline__ void store_chunk(__amdgpu_buffer_rsrc_t r, int type, int k, const float (&f)[VEC]) {
-  typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4_t;
-  typedef __attribute__((__vector_size__(2 * sizeof(uint32_t)))) uint32_t u32x2_t;
   if (type == kF32) {
     if constexpr (VEC == 1) {
       __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(f[0]), r, k * 4, 0, 0);
@@ -88,7 +74,7 @@ __device__ __forceinline__ void store_chunk(__amdgpu_buffer_rsrc_t r, int type, 
     uint32_t u[VEC / 2];
 #pragma unroll
     for (int e = 0; e < VEC / 2; ++e)
-      u[e] = (uint32_t)f32_to_bf16_any(f[2 * e]) | ((uint32_t)f32_to_bf16_any(f[2 * e + 1]) << 16);
+      u[e] = f32_to_bf16_pair(f[2 * e], f[2 * e + 1]);
     if constexpr (VEC == 8)
       __builtin_amdgcn_raw_buffer_store_b128(u32x4_t{u[0], u[1], u[2], u[3]}, r, k * 2, 0, 0);
     else
@@ -126,21 +112,6 @@ __device__ __forceinline__ void load_vector(const void* p, int type, int K, int 
       for (int e = 0; e < VEC; ++e) f[c][e] = u.at(e);
     }
   }
-}
-
-// Sum over the wave's lanes in a fixed order, in every lane: each row of 16
-// lanes by shifted adds, then the rows one after the other.
-__device__ __forceinline__ float wave_sum(float v) {
-#define HYDRA_DPP_ADD(ctrl, rows) \
-  v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), ctrl, rows, 0xF, false))
-  HYDRA_DPP_ADD(0x111, 0xF);  // lanes 1, 2, 4 and 8 to the left
-  HYDRA_DPP_ADD(0x112, 0xF);
-  HYDRA_DPP_ADD(0x114, 0xF);
-  HYDRA_DPP_ADD(0x118, 0xF);
-  HYDRA_DPP_ADD(0x142, 0xA);  // the last lane of rows 0 and 2 into rows 1 and 3
-  HYDRA_DPP_ADD(0x143, 0xC);  // that of row 1 into rows 2 and 3
-#undef HYDRA_DPP_ADD
-  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
 }
 
 constexpr int kMaxWaves = 8;  // of a row
@@ -382,17 +353,17 @@ __global__ __launch_bounds__(LONG_THREADS) void layer_norm_long_kernel(LayerNorm
   const int row = blockIdx.x, t = threadIdx.x, K = a.K;
   const size_t r0 = (size_t)row * K;
   float s = 0.f;
-  for (int k = t; k < K; k += LONG_THREADS) s += load1(a.x, a.x_type, r0 + k);
+  for (int k = t; k < K; k += LONG_THREADS) s += load_elem(a.x, a.x_type, r0 + k);
   const float mean = block_sum(s) / (float)K;
   s = 0.f;
   for (int k = t; k < K; k += LONG_THREADS) {
-    const float c = load1(a.x, a.x_type, r0 + k) - mean;
+    const float c = load_elem(a.x, a.x_type, r0 + k) - mean;
     s = fmaf(c, c, s);
   }
   const float rstd = 1.f / sqrtf(block_sum(s) / (float)K + a.eps);
   for (int k = t; k < K; k += LONG_THREADS) {
-    const float w = a.w ? load1(a.w, a.w_type, k) : 1.f, b = a.b ? load1(a.b, a.w_type, k) : 0.f;
-    store1(a.y, a.y_type, r0 + k, fmaf((load1(a.x, a.x_type, r0 + k) - mean) * rstd, w, b));
+    const float w = a.w ? load_elem(a.w, a.w_type, k) : 1.f, b = a.b ? load_elem(a.b, a.w_type, k) : 0.f;
+    store_elem(a.y, a.y_type, r0 + k, fmaf((load_elem(a.x, a.x_type, r0 + k) - mean) * rstd, w, b));
   }
   if (t == 0) {
     if (a.mean) a.mean[row] = mean;
@@ -406,9 +377,9 @@ __global__ __launch_bounds__(LONG_THREADS) void norm_back_rows_kernel(LayerNormB
   const float mean = a.mean[row], rstd = a.rstd[row];
   float s0 = 0.f, s1 = 0.f;
   for (int k = t; k < K; k += LONG_THREADS) {
-    const float g = load1(a.dy, a.dy_type, r0 + k) * (a.w ? load1(a.w, a.w_type, k) : 1.f);
+    const float g = load_elem(a.dy, a.dy_type, r0 + k) * (a.w ? load_elem(a.w, a.w_type, k) : 1.f);
     s0 += g;
-    s1 = fmaf(g, (load1(a.x, a.x_type, r0 + k) - mean) * rstd, s1);
+    s1 = fmaf(g, (load_elem(a.x, a.x_type, r0 + k) - mean) * rstd, s1);
   }
   s0 = block_sum(s0);
   s1 = block_sum(s1);
@@ -423,17 +394,17 @@ __global__ __launch_bounds__(COL_THREADS) void norm_back_cols_kernel(LayerNormBa
   const int k = blockIdx.x * COL_THREADS + threadIdx.x, K = a.K;
   if (k >= K) return;
   const int m0 = blockIdx.y * rows, m1 = min(a.M, m0 + rows);
-  const float w = a.w ? load1(a.w, a.w_type, k) : 1.f;
+  const float w = a.w ? load_elem(a.w, a.w_type, k) : 1.f;
   float dw = 0.f, db = 0.f;
   for (int m = m0; m < m1; ++m) {
     const size_t i = (size_t)m * K + k;
-    const float dy = load1(a.dy, a.dy_type, i), rstd = a.rstd[m];
-    const float xh = (load1(a.x, a.x_type, i) - a.mean[m]) * rstd;
+    const float dy = load_elem(a.dy, a.dy_type, i), rstd = a.rstd[m];
+    const float xh = (load_elem(a.x, a.x_type, i) - a.mean[m]) * rstd;
     dw = fmaf(dy, xh, dw);
     db += dy;
     if (a.dx) {
       const float2 s = sums[m];
-      store1(a.dx, a.dx_type, i, rstd * (fmaf(dy, w, -s.x) - xh * s.y));
+      store_elem(a.dx, a.dx_type, i, rstd * (fmaf(dy, w, -s.x) - xh * s.y));
     }
   }
   float* p = part + (size_t)blockIdx.y * 2 * K;

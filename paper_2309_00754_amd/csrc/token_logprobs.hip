@@ -25,8 +25,7 @@
 // logit in another group has one in each of these before it.  (32000 zeros or
 // sorted logits, 32 alternatives, one row: extracting them one after the other
 // took 335 us.)
-#include "hydra_device.h"
-#include "hydra_internal.h"
+#include "hydra_elem.h"
 
 namespace hydra {
 namespace {
@@ -39,25 +38,8 @@ constexpr int kSegs = 64;           // segments of a row at most
 constexpr int kCand = 576;          // logits ranked by counting at most
 
 template <int T>
-constexpr int kVec = T == kF32 ? 4 : 8;  // elements of 16 bytes
-
-template <int T>
 __device__ __forceinline__ float load_z(const void* p, size_t i) {
-  return T == kF32 ? static_cast<const float*>(p)[i] : bf16_to_f32(static_cast<const uint16_t*>(p)[i]);
-}
-
-template <int T>
-__device__ __forceinline__ void unpack(const uint4& u, float (&f)[kVec<T>]) {
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (T == kF32) {
-      f[i] = __uint_as_float(w[i]);
-    } else {
-      f[2 * i] = __uint_as_float(w[i] << 16);
-      f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-    }
-  }
+  return load_elem(p, T, i);
 }
 
 // Elements before the first 16-byte boundary of a row.
@@ -117,28 +99,6 @@ __device__ __forceinline__ void absorb(Stat& a, const float (&z)[N], float most)
     a.s += e;
     a.w = fmaf(e, fmaxf(d, kFar), a.w);
   }
-}
-
-template <bool MAX>
-__device__ __forceinline__ float combine(float a, float b) {
-  return MAX ? fmaxf(a, b) : a + b;
-}
-
-// Maximum or sum over the wave's lanes in a fixed order, in every lane: each row
-// of 16 lanes by shifts, then the rows one after the other.
-template <bool MAX>
-__device__ __forceinline__ float wave_all(float v) {
-  const uint32_t none = __float_as_uint(MAX ? -INFINITY : 0.f);
-#define HYDRA_DPP(ctrl, rows) \
-  v = combine<MAX>(v, __uint_as_float(__builtin_amdgcn_update_dpp(none, __float_as_uint(v), ctrl, rows, 0xF, false)))
-  HYDRA_DPP(0x111, 0xF);
-  HYDRA_DPP(0x112, 0xF);
-  HYDRA_DPP(0x114, 0xF);
-  HYDRA_DPP(0x118, 0xF);
-  HYDRA_DPP(0x142, 0xA);
-  HYDRA_DPP(0x143, 0xC);
-#undef HYDRA_DPP
-  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
 }
 
 // The waves' maxima, then their sums, met by the workgroup.
@@ -382,7 +342,7 @@ __global__ __launch_bounds__(TL_THREADS) void token_logp_kernel(TokenLogpArgs a,
   // First meeting: the maxima, and (TOP) each wave's bound.
   const float mine = st.m;
   const int lane = t & 63, wave = t >> 6;
-  const float wave_most = wave_all<true>(mine);
+  const float wave_most = wave_max(mine);
   if (lane == 0) meet.m[wave] = wave_most;
   const int groups = sp.g1 - sp.g0;
   // whole waves of groups, or the only one (where the last wave's few threads cannot
@@ -396,15 +356,15 @@ __global__ __launch_bounds__(TL_THREADS) void token_logp_kernel(TokenLogpArgs a,
       for (int i = 1; i < j; ++i) {
         const uint64_t have = __ballot(left == bound);
         if (lane == __ffsll((unsigned long long)have) - 1) left = -INFINITY;
-        bound = wave_all<true>(left);
+        bound = wave_max(left);
       }
     }
     if (lane == 0) bound_of[wave] = bound;
   }
   __syncthreads();
   meet_max(st, meet);
-  st.s = wave_all<false>(st.s);
-  st.w = wave_all<false>(st.w);
+  st.s = wave_sum(st.s);
+  st.w = wave_sum(st.w);
   if (lane == 0) {
     meet.s[wave] = st.s;
     meet.w[wave] = st.w;
@@ -510,9 +470,9 @@ __global__ __launch_bounds__(64) void token_logp_join_kernel(TokenLogpArgs a, in
   const uint64_t early = lane < nseg * k ? pk[lane] : 0;
   Stat st{-INFINITY, 0.f, 0.f};
   if (lane < nseg) st = ps[lane];
-  rescale(st, wave_all<true>(st.m));
-  st.s = wave_all<false>(st.s);
-  st.w = wave_all<false>(st.w);
+  rescale(st, wave_max(st.m));
+  st.s = wave_sum(st.s);
+  st.w = wave_sum(st.w);
   if (lane == 0) finish_row(a, row, st, token);
   if (k == 0) return;
   uint64_t bound = 0;
@@ -548,8 +508,6 @@ constexpr int64_t kCacheBytes = int64_t(256) << 20;  // the memory-side cache
 constexpr int TB_THREADS = 256;
 constexpr int TB_U = 2;  // (4: 2048 x 32000 56.5 us, so 52.3; 250 x 50272 bf16 10.5 and 9.8)
 
-typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4_t;
-typedef __attribute__((__vector_size__(2 * sizeof(uint32_t)))) uint32_t u32x2_t;
 template <bool FAR, class V>
 __device__ __forceinline__ V fetch(const V* p) {
   return FAR ? __builtin_nontemporal_load(p) : *p;
@@ -594,10 +552,7 @@ __global__ __launch_bounds__(TB_THREADS) void token_logp_back_kernel(TokenLogpBa
     };
     const auto one = [&](int e) __attribute__((always_inline)) {
       const float f = live ? gradient(load_z<TZ>(z, e)) + (e == tk ? d_lp : 0.f) : 0.f;
-      if constexpr (TD == kF32)
-        reinterpret_cast<float*>(d)[e] = f;
-      else
-        reinterpret_cast<uint16_t*>(d)[e] = f32_to_bf16_any(f);
+      store_elem(d, TD, e, f);
     };
     const int head = head_of<TZ>(z, V), groups = (V - head) / VEC;
     const int g0 = min(groups, part * per), g1 = min(groups, g0 + per);
@@ -639,7 +594,7 @@ __global__ __launch_bounds__(TB_THREADS) void token_logp_back_kernel(TokenLogpBa
           if constexpr (TD == kF32)
             w[e] = __float_as_uint(f[e]);
           else
-            w[e] = (uint32_t)f32_to_bf16_any(f[2 * e]) | ((uint32_t)f32_to_bf16_any(f[2 * e + 1]) << 16);
+            w[e] = f32_to_bf16_pair(f[2 * e], f[2 * e + 1]);
         }
         if constexpr (VEC * DB == 8) {
           put<FAR>(reinterpret_cast<u32x2_t*>(dv) + at, u32x2_t{w[0], w[1]});
