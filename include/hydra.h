@@ -561,10 +561,11 @@ hydra_status hydra_lora_linear_backward(const uint16_t* x, const uint16_t* Wt, c
  *   mean, rstd [M] fp32   out, optional: what the backward takes
  * Statistics and products are fp32 (the variance from the centred values),
  * y is rounded once, to nearest even.  A row that holds NaN or an infinity
- * becomes NaN.  Requires 1 <= M <= 2^20, 1 <= K <= 2^21; K need be no multiple of anything, and
- * buffers need their element's alignment only (16-byte aligned ones with
- * K % 8 == 0 are faster).  Outputs distinct (HYDRA_ERR_SHAPE); partial
- * overlaps are not detected and are not allowed.
+ * becomes NaN; the squares of values from about 1e19 on leave the range of fp32.
+ * Requires 1 <= M <= 2^20, 1 <= K <= 2^21; K need be no multiple of anything,
+ * and buffers need their element's alignment only (16-byte aligned ones with
+ * K % 8 == 0 are faster).  Outputs distinct (HYDRA_ERR_SHAPE); partial overlaps
+ * are not detected and are not allowed.
  */
 hydra_status hydra_layer_norm(const void* x, hydra_dtype x_type, const void* weight, const void* bias,
                               hydra_dtype w_type, float eps, int64_t M, int64_t K, void* y, hydra_dtype y_type,
@@ -640,10 +641,12 @@ hydra_status hydra_token_logprobs_workspace_bytes(int64_t M, int64_t V, int64_t 
  *           whose lp is NaN
  * At least one output (HYDRA_ERR_NULL).  Masked-out entries have probability 0
  * and log-probability -inf; a row of nothing else has lse -inf and NaN lp,
- * entropy and top_lp (top_ids 0, 1, ...).  In a row that holds NaN or +inf lp, lse, entropy and
- * top_lp are NaN (top_ids then take NaN first, then +inf).  Sums and maxima are
- * fp32.  Requires 1 <= M <= 2^20, 1 <= V <= 2^21, M V <= 2^38,
- * ld <= 2^31 - 1; logits need their element's alignment only.  Outputs distinct (HYDRA_ERR_SHAPE).
+ * entropy and top_lp (top_ids 0, 1, ...).  In a row that holds NaN or +inf lp,
+ * lse, entropy and top_lp are NaN (top_ids then take NaN first, then +inf).
+ * Sums and maxima are fp32, in an order that depends on M, V and the type alone.
+ * Requires 1 <= M <= 2^20, 1 <= V <= 2^21, M V <= 2^38, ld <= 2^31 - 1; logits
+ * need their element's alignment only.  Outputs distinct (HYDRA_ERR_SHAPE).
+ * Calls that share a workspace on different streams race.
  */
 hydra_status hydra_token_logprobs(const void* logits, hydra_dtype logits_type, int64_t ld, const int32_t* tokens,
                                   int64_t M, int64_t V, int64_t top, float* lp, float* lse, float* entropy,
@@ -668,8 +671,10 @@ hydra_status hydra_token_logprobs(const void* logits, hydra_dtype logits_type, i
  *   err_flag [1] int32  optional: 1 is OR-ed in for a token outside [0, V) of
  *           a row whose d_lp is not 0; that row's gradient is NaN
  * At least one of d_lp and d_entropy (HYDRA_ERR_NULL).  A row whose upstream
- * gradients are both 0 (a prompt token, padding) gets zeros: its logits, token
- * and statistics are not read.  Products are fp32, each gradient rounded once, to
+ * gradients are both 0 (a prompt token, padding) gets zeros, whatever its
+ * logits, token and statistics hold.  p_j goes by the lse given: where that has
+ * lost ln V to its rounding (a row of logits near the type's lowest value alone)
+ * the p_j do not add up to 1.  Products are fp32, each gradient rounded once, to
  * nearest even.  Sizes, alignment and overlaps as in hydra_token_logprobs.
  */
 hydra_status hydra_token_logprobs_backward(const void* logits, hydra_dtype logits_type, int64_t ld,

@@ -82,6 +82,29 @@ def test_clip_in_place(kinds, count, dev):
     assert all(torch.equal(a, b) for a, b in zip(before, grads))
 
 
+@pytest.mark.parametrize("count", [900, 4096])
+def test_many_tensors(count, dev):
+    """Up to the most that a call takes: several launches of the sums and of the scaling."""
+    import torch
+    say("many tensors", count)
+    gen = torch.Generator(device=dev)
+    gen.manual_seed(count)
+    sizes = [1 + (i * 37) % 300 for i in range(count)]
+    flat = torch.randn(sum(sizes) + count, generator=gen, device=dev)
+    grads, at = [], 0
+    for n in sizes:  # one element apart: no two are one run
+        grads.append(flat[at:at + n])
+        at += n + 1
+    v = torch.cat(grads).double().cpu()
+    ref = float(v.square().sum().sqrt())
+    ends = torch.tensor(sizes).cumsum(0) + torch.arange(count)  # the elements between
+    between = flat[ends].clone()
+    norm, err = _clip(dev, grads, 2.0)
+    near([norm], [ref], 1.5 * U * ref, "norm")
+    _check(torch.cat(grads), v.numpy() * (2.0 / ref), "f32", "clipped")
+    assert err == 0 and torch.equal(flat[ends], between)
+
+
 def test_the_same_outs_as_gradients_is_in_place(dev):
     import torch
     a = _tensors(dev, [1000, 70000, 3], ("f32", "bf16"), 8)

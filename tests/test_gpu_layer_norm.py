@@ -144,6 +144,23 @@ def test_bad_values_stay_in_their_row(K, dev):
     assert np.isnan(f64(dx)[bad]).all() and np.isfinite(f64(dx)[good]).all() and np.isnan(f64(dw)).all()
 
 
+@pytest.mark.parametrize("M", [3, 300])
+def test_sums_at_any_alignment(M, dev):
+    """dweight and dbias need 4-byte alignment alone, also where the rows are read 16 bytes at a time."""
+    import torch
+    for K in (264, 2048, 4096, 12000):
+        say("sums at any alignment", M, K)
+        x, w, _, dy = _inputs(M, K, 700 + K, "f32")
+        v, (dx, dw, db) = _backward(dev, dy, x, w, "bf16", "bf16", "bf16", "bf16")
+        flat = torch.full((2 * K + 16,), 7.0, device=dev)
+        dw2, db2 = flat[1:K + 1], flat[K + 3:2 * K + 3]
+        dx2 = torch.empty_like(dx)
+        H.hydra_layer_norm_backward(put(dy, "bf16", dev), put(x, "bf16", dev), put(w, "bf16", dev), put(v[3], "f32", dev),
+                                    put(v[4], "f32", dev), dx2, dw2, db2)
+        assert torch.equal(dx2, dx) and torch.equal(dw2, dw) and torch.equal(db2, db)
+        assert (flat[[0, K + 1, K + 2]] == 7).all() and (flat[2 * K + 3:] == 7).all()
+
+
 def test_repeated_calls_give_the_same_bits(dev):
     import torch
     x, w, _, dy = _inputs(700, 2048, 7, "f32")
