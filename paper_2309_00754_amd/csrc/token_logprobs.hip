@@ -8,9 +8,9 @@
 //   dz_j = d_lp ([j == token] - p_j) - d_H p_j (ln p_j + H), p_j = e^(z_j - lse)
 //
 //  * token_logp_kernel: a workgroup per row, or per segment of a long one,
-//    reads it once in 16-byte groups, each thread with a running (m, S, W); the
-//    threads meet in a fixed tree.  For the alternatives it keeps the maximum
-//    of every group in LDS.
+//    reads it once in 16-byte groups, each thread with running sums relative to
+//    a power of two that follows its maximum; the threads meet in a fixed tree.
+//    For the alternatives it keeps the maximum of every group in LDS.
 //  * token_logp_join_kernel: one wave per row joins the segments.
 //  * token_logp_back_kernel: a workgroup per stretch of a row; rows without a
 //    gradient are filled with zeros unread.
@@ -65,59 +65,98 @@ __device__ __forceinline__ float logit_of(uint64_t key) {  // (of -0: +0)
 // (of -inf and below: masked out, or no logit)
 __device__ __forceinline__ bool masked_out(uint64_t key) { return (uint32_t)(key >> 32) <= 0x007FFFFFu; }
 
-// The statistics of a part of a row.  Differences to the maximum are formed
-// before anything else is done with them, so that logits up to the type's
-// largest and lowest values (masks) keep their meaning.
-struct Stat {
-  float m, s, w;  // max z, sum e^(z - m), sum e^(z - m) (z - m)
+// A thread's running statistics: the largest logit m, and relative to a whole
+// exponent r (that of the largest so far, kLow before) s = sum 2^t and w = sum
+// 2^t t, t = z log2 e - r in one FMA.  A change of r scales by a power of two.
+// Logits below -2^21 (masks) add nothing beside others; a row or segment whose
+// largest lies outside +-2^21, where t would lose its fraction, is summed again
+// relative to that logit itself.  (Bound by these instructions, not by memory,
+// where few rows or 16-bit ones are read: with the sums relative to the maximum
+// of every 16 bytes, twice the instructions, 32000 logits of one row took 5.7 us
+// in place of 4.8, 900 rows of 40000 with 16 alternatives 36.8 in place of 33.0;
+// rows shorter than one round lose: 4000 of 5000 15.5, now 16.0.)
+constexpr float kLow = -4194304.f, kRange = 2097152.f;
+constexpr float kFar = -1000.f;  // 2^kFar is 0, and a product of the two is (with -inf it would not be)
+
+struct Run {
+  float m = -INFINITY, r = kLow;
+  float s[4] = {0.f, 0.f, 0.f, 0.f}, w[4] = {0.f, 0.f, 0.f, 0.f};  // (four chains of additions)
 };
 
-constexpr float kFar = -1000.f;  // e^kFar is 0, and a product of the two is (with -inf it would not be)
+__device__ __forceinline__ float exponent_of(float m) { return fminf(fmaxf(rintf(m * kLog2e), kLow), -kLow); }
 
-__device__ __forceinline__ void rescale(Stat& a, float m) {
-  // (nothing so far: s = w = 0; and a NaN sum stays one)
-  if (a.m != -INFINITY && a.m != m) {
-    const float d = a.m - m, e = exp_e(d);
-    a.w = fmaf(a.s, fmaxf(d, kFar), a.w) * e;
-    a.s *= e;
+__device__ __forceinline__ void rescale(Run& a, float r) {
+  if (r > a.r) {
+    const float d = a.r - r, e = __builtin_amdgcn_exp2f(d);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      a.w[i] = fmaf(a.s[i], fmaxf(d, kFar), a.w[i]) * e;
+      a.s[i] *= e;
+    }
+    a.r = r;
   }
-  a.m = m;
 }
 
-// n logits whose maximum (NaN aside) is `most`.
+// Logits up to `most` are to be added.
+__device__ __forceinline__ void make_room(Run& a, float most) {
+  a.m = fmaxf(a.m, most);
+  rescale(a, exponent_of(most));
+}
 template <int N>
-__device__ __forceinline__ void absorb(Stat& a, const float (&z)[N], float most) {
-  rescale(a, fmaxf(a.m, most));
-  if (a.m == -INFINITY) {  // nothing but -inf so far, or NaN
-#pragma unroll
-    for (int i = 0; i < N; ++i) a.s += z[i] == -INFINITY ? 0.f : z[i];
-    return;
-  }
+__device__ __forceinline__ void add(Run& a, const float* z) {
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const float d = z[i] - a.m, e = exp_e(d);
-    a.s += e;
-    a.w = fmaf(e, fmaxf(d, kFar), a.w);
+    const float t = fmaf(z[i], kLog2e, -a.r), e = __builtin_amdgcn_exp2f(t);
+    a.s[i & 3] += e;
+    a.w[i & 3] = fmaf(e, fmaxf(t, kFar), a.w[i & 3]);
   }
+}
+
+// The statistics of a row or segment: lse = hi + lo + ln s, the sum s = sum
+// e^(z - hi - lo) and w = sum e^(z - hi - lo) (z - hi - lo).  hi is -inf where
+// there is nothing but -inf.
+struct Stat {
+  float hi, lo, s, w;
+};
+constexpr float kLn2 = 0.693147182464599609375f, kLn2Rest = -1.904654299957767e-9f;  // ln 2 as two floats
+constexpr float kLog2eRest = 1.3349759e-8f;  // (log2 e - kLog2e) ln 2: the base is off by m times that
+__device__ __forceinline__ Stat stat_of(float m, float r, float s, float w) {
+  Stat st;
+  st.hi = r * kLn2;
+  st.lo = fmaf(r, kLn2, -st.hi) + fmaf(r, kLn2Rest, m * kLog2eRest);
+  if (m == -INFINITY) st.hi = -INFINITY, st.lo = 0.f;
+  st.s = s;
+  st.w = w * kLn2;
+  return st;
+}
+// Relative to another base.
+__device__ __forceinline__ void rebase(Stat& a, float hi, float lo) {
+  const float d = a.hi == -INFINITY ? -INFINITY : (a.hi - hi) + (a.lo - lo);
+  const float e = exp_e(d);
+  a.w = fmaf(a.s, fmaxf(d, kFar), a.w) * e;
+  a.s *= e;
+  a.hi = hi;
+  a.lo = lo;
 }
 
 // The waves' maxima, then their sums, met by the workgroup.
 struct Meet {
   float m[TL_WAVES], s[TL_WAVES], w[TL_WAVES];
 };
-__device__ __forceinline__ void meet_max(Stat& a, const Meet& meet) {
+__device__ __forceinline__ void meet_max(Run& a, const Meet& meet) {
   float m = meet.m[0];
 #pragma unroll
   for (int i = 1; i < TL_WAVES; ++i) m = fmaxf(m, meet.m[i]);
-  rescale(a, m);
+  a.m = m;
+  rescale(a, exponent_of(m));
 }
-__device__ __forceinline__ void meet_sums(Stat& a, const Meet& meet) {
-  a.s = meet.s[0];
-  a.w = meet.w[0];
+__device__ __forceinline__ void meet_sums(float& s, float& w, const Meet& meet) {
+  s = meet.s[0];
+  w = meet.w[0];
 #pragma unroll
   for (int i = 1; i < TL_WAVES; ++i) {
-    a.s += meet.s[i];
-    a.w += meet.w[i];
+    s += meet.s[i];
+    w += meet.w[i];
   }
 }
 
@@ -195,9 +234,9 @@ __device__ __forceinline__ uint32_t greatest(const uint32_t* v, int n, int want,
   return bound;
 }
 
-// lp of a logit, by way of the maximum: of the rounding of lse that of ln S
-// alone remains.
-__device__ __forceinline__ float logp_of(float z, float m, float ln_s) { return (z - m) - ln_s; }
+// lp of a logit, by way of the base: of the rounding of lse that of ln s alone
+// remains.
+__device__ __forceinline__ float logp_of(float z, const Stat& st, float ln_s) { return ((z - st.hi) - st.lo) - ln_s; }
 
 // The token of a row and its logit, loaded ahead of the row (by one thread).
 struct Token {
@@ -217,33 +256,41 @@ __device__ __forceinline__ Token token_of(const TokenLogpArgs& a, int row) {
 // One thread: the row's statistics.
 __device__ __forceinline__ void finish_row(const TokenLogpArgs& a, int row, const Stat& st, const Token& k) {
   const float ln_s = log_e(st.s);
-  if (a.lse) a.lse[row] = st.m + ln_s;
+  if (a.lse) a.lse[row] = st.hi + (st.lo + ln_s);
   if (a.entropy) a.entropy[row] = ln_s - st.w / st.s;
   if (a.lp) {
     const bool ok = k.tk >= 0 && k.tk < a.V;
-    a.lp[row] = ok ? logp_of(k.z, st.m, ln_s) : __builtin_nanf("");
+    a.lp[row] = ok ? logp_of(k.z, st, ln_s) : __builtin_nanf("");
     if (!ok && a.err) atomicOr(a.err, 1);
   }
 }
 
 // One wave: f(rank, key) for each of the n keys at `key` (LDS, 16-byte aligned,
-// room for a multiple of 8), the rank counted over all of them.
+// room for a multiple of 16), the rank counted over all of them; 128 keys at a
+// time, two to a lane.  (One to a lane, 8 keys loaded at a time: 85 rows of 3186
+// with 32 alternatives 10.0 us, not 9.0.)
 template <class F>
 __device__ __forceinline__ void each_ranked(uint64_t* key, int n, F f) {
-  const int lane = threadIdx.x & 63, n8 = (n + 7) & ~7;
-  if (lane < n8 - n) key[n + lane] = 0;
+  constexpr int U = 16;
+  const int lane = threadIdx.x & 63, padded = (n + U - 1) / U * U;
+  if (lane < padded - n) key[n + lane] = 0;
   __builtin_amdgcn_wave_barrier();
-  for (int i = lane; i - lane < n; i += 64) {
-    const uint64_t mine = i < n ? key[i] : ~0ull;
-    int rank = 0;
-    for (int j = 0; j < n8; j += 8) {
-      uint64_t other[8];
+  for (int i = lane; i - lane < n; i += 128) {
+    const uint64_t a = i < n ? key[i] : ~0ull, b = i + 64 < n ? key[i + 64] : ~0ull;
+    int rank_a = 0, rank_b = 0;
+    for (int j = 0; j < padded; j += U) {
+      uint64_t other[U];
 #pragma unroll
-      for (int q = 0; q < 8; ++q) other[q] = key[j + q];
+      for (int q = 0; q < U; ++q) other[q] = key[j + q];
 #pragma unroll
-      for (int q = 0; q < 8; ++q) rank += other[q] > mine;
+      for (int q = 0; q < U; ++q) rank_a += other[q] > a;
+      if (n - i + lane > 64) {
+#pragma unroll
+        for (int q = 0; q < U; ++q) rank_b += other[q] > b;
+      }
     }
-    if (i < n) f(rank, mine);
+    if (i < n) f(rank_a, a);
+    if (i + 64 < n) f(rank_b, b);
   }
 }
 
@@ -257,7 +304,7 @@ __device__ __forceinline__ void finish_top(const TokenLogpArgs& a, int row, cons
   const auto put = [&](int rank, int id, float z) __attribute__((always_inline)) {
     if (rank >= k) return;
     a.ids[o0 + rank] = id;
-    if (a.top_lp) a.top_lp[o0 + rank] = logp_of(z, st.m, ln_s);
+    if (a.top_lp) a.top_lp[o0 + rank] = logp_of(z, st, ln_s);
   };
   each_ranked(key, n, [&](int rank, uint64_t mine) __attribute__((always_inline)) { put(rank, index_of(mine), logit_of(mine)); });
   if (n >= k) return;
@@ -312,23 +359,44 @@ __global__ __launch_bounds__(TL_THREADS) void token_logp_kernel(TokenLogpArgs a,
   Token token{0, 0.f};
   if (t == 0 && nseg == 1) token = token_of<T>(a, row);
   if (TOP && t < 2) count[t] = 0;
-  Stat st{-INFINITY, 0.f, 0.f};
-  for (int g = sp.g0 + t; g < sp.g1; g += TL_THREADS * TL_U) {
+  const int groups = sp.g1 - sp.g0;
+  const __amdgpu_buffer_rsrc_t rs = make_rsrc(v + sp.g0, (uint32_t)groups * 16u);
+  const int first_of_wave = __builtin_amdgcn_readfirstlane(t & ~63);
+  Run run;
+  constexpr int ROUND = TL_THREADS * TL_U;
+  for (int g0 = 0; g0 < groups; g0 += ROUND) {
     uint4 u[TL_U];
 #pragma unroll
-    for (int q = 0; q < TL_U; ++q)
-      if (g + q * TL_THREADS < sp.g1) u[q] = v[g + q * TL_THREADS];
+    for (int q = 0; q < TL_U; ++q) {
+      const int g = g0 + q * TL_THREADS + t;
+      u[q] = buf_load16(rs, g < groups ? g * 16 : kOutOfRange);
+    }
+    if (g0 + ROUND > groups) {  // the last round: -inf where there is no group
+      constexpr uint32_t none = T == kF32 ? 0xFF800000u : 0xFF80FF80u;
+#pragma unroll
+      for (int q = 0; q < TL_U; ++q)
+        if (g0 + q * TL_THREADS + t >= groups) u[q] = make_uint4(none, none, none, none);
+    }
+    float f[TL_U * VEC], most = -INFINITY;
 #pragma unroll
     for (int q = 0; q < TL_U; ++q) {
-      if (g + q * TL_THREADS >= sp.g1) break;
-      float f[VEC];
-      unpack<T>(u[q], f);
-      float most = f[0];
+      float x[VEC];
+      unpack<T>(u[q], x);
+      float m = x[0];
 #pragma unroll
-      for (int e = 1; e < VEC; ++e) most = fmaxf(most, f[e]);
-      if constexpr (TOP) most_of[g + q * TL_THREADS - sp.g0] = most;
-      absorb(st, f, most);
+      for (int e = 1; e < VEC; ++e) m = fmaxf(m, x[e]);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) f[q * VEC + e] = x[e];
+      if constexpr (TOP) {
+        const int g = g0 + q * TL_THREADS + t;
+        if (g < groups) most_of[g] = m;
+      }
+      most = fmaxf(most, m);
     }
+    make_room(run, most);
+#pragma unroll
+    for (int q = 0; q < TL_U; ++q)
+      if (g0 + q * TL_THREADS + first_of_wave < groups) add<VEC>(run, f + q * VEC);
   }
   // the elements in no group: a thread each
   float edge = -INFINITY;
@@ -336,15 +404,15 @@ __global__ __launch_bounds__(TL_THREADS) void token_logp_kernel(TokenLogpArgs a,
   if (sp.first && t < sp.head) edge_at = t;
   if (sp.last && t >= 64 && t - 64 < V - sp.tail0) edge_at = sp.tail0 + t - 64;
   if (edge_at >= 0) {
-    const float f[1] = {edge = load_z<T>(z, edge_at)};
-    absorb(st, f, edge);
+    edge = load_z<T>(z, edge_at);
+    make_room(run, edge);
+    add<1>(run, &edge);
   }
   // First meeting: the maxima, and (TOP) each wave's bound.
-  const float mine = st.m;
+  const float mine = run.m;
   const int lane = t & 63, wave = t >> 6;
   const float wave_most = wave_max(mine);
   if (lane == 0) meet.m[wave] = wave_most;
-  const int groups = sp.g1 - sp.g0;
   // whole waves of groups, or the only one (where the last wave's few threads cannot
   // bound anything, and what is left to others is few)
   const int waves = groups >= 64 ? min(TL_WAVES, groups / 64) : groups > 0;
@@ -362,12 +430,12 @@ __global__ __launch_bounds__(TL_THREADS) void token_logp_kernel(TokenLogpArgs a,
     if (lane == 0) bound_of[wave] = bound;
   }
   __syncthreads();
-  meet_max(st, meet);
-  st.s = wave_sum(st.s);
-  st.w = wave_sum(st.w);
+  meet_max(run, meet);
+  float sum = wave_sum((run.s[0] + run.s[1]) + (run.s[2] + run.s[3]));
+  float mean = wave_sum((run.w[0] + run.w[1]) + (run.w[2] + run.w[3]));
   if (lane == 0) {
-    meet.s[wave] = st.s;
-    meet.w[wave] = st.w;
+    meet.s[wave] = sum;
+    meet.w[wave] = mean;
   }
   // Second meeting: the sums, and (TOP) the groups that reach the bound.
   float bound = -INFINITY;
@@ -375,15 +443,45 @@ __global__ __launch_bounds__(TL_THREADS) void token_logp_kernel(TokenLogpArgs a,
   if constexpr (TOP) {
     if (waves > 0) bound = bound_of[0];
     for (int i = 1; i < waves; ++i) bound = fminf(bound, bound_of[i]);
-    for (int g = t; g < groups; g += TL_THREADS)
-      if (reaches(most_of[g])) {
-        const int i = atomicAdd(&count[0], 1);
-        if (i < kCand) slot[i] = g;
-      }
+    constexpr int U = 4;  // (loads from LDS under way; with 8, 4000 rows of 5000 took 28.1 us, not 26.7)
+    for (int g0 = t; g0 < groups; g0 += TL_THREADS * U) {
+      float x[U];
+#pragma unroll
+      for (int q = 0; q < U; ++q) x[q] = g0 + q * TL_THREADS < groups ? most_of[g0 + q * TL_THREADS] : -INFINITY;
+#pragma unroll
+      for (int q = 0; q < U; ++q)
+        if (reaches(x[q])) {
+          const int i = atomicAdd(&count[0], 1);
+          if (i < kCand) slot[i] = g0 + q * TL_THREADS;
+        }
+    }
     if (edge_at >= 0 && reaches(edge)) cand[atomicAdd(&count[1], 1)] = order_key(edge, edge_at);
   }
   __syncthreads();
-  meet_sums(st, meet);
+  meet_sums(sum, mean, meet);
+  Stat st = stat_of(run.m, run.r, sum, mean);
+  if (run.m != -INFINITY && !(fabsf(run.m) <= kRange)) {
+    // far from zero: the sums relative to the largest logit itself
+    sum = mean = 0.f;
+    const auto add = [&](float x) __attribute__((always_inline)) {
+      const float d = x - run.m, e = exp_e(d);
+      sum += e;
+      mean = fmaf(e, fmaxf(d, kFar), mean);
+    };
+    for (int e = sp.head + sp.g0 * VEC + t; e < sp.head + sp.g1 * VEC; e += TL_THREADS) add(load_z<T>(z, e));
+    if (edge_at >= 0) add(edge);
+    __syncthreads();
+    sum = wave_sum(sum);
+    mean = wave_sum(mean);
+    if (lane == 0) {
+      meet.s[wave] = sum;
+      meet.w[wave] = mean;
+    }
+    __syncthreads();
+    st.hi = run.m;
+    st.lo = 0.f;
+    meet_sums(st.s, st.w, meet);
+  }
   if (t == 0) {
     if (nseg == 1)
       finish_row(a, row, st, token);
@@ -393,7 +491,7 @@ __global__ __launch_bounds__(TL_THREADS) void token_logp_kernel(TokenLogpArgs a,
   if constexpr (TOP) {
     const int k = a.top, slots = count[0];
     int n = kCand + 1;  // too many
-    if (slots <= kCand && st.s >= 0.f && st.m != INFINITY) {  // (no NaN and no +inf)
+    if (slots <= kCand && st.s >= 0.f) {  // (no NaN and no +inf)
       for (int i = t; i < slots * VEC; i += TL_THREADS) {
         const int e = sp.head + (sp.g0 + slot[i / VEC]) * VEC + i % VEC;
         const float x = load_z<T>(z, e);
@@ -409,7 +507,7 @@ __global__ __launch_bounds__(TL_THREADS) void token_logp_kernel(TokenLogpArgs a,
       // by the groups' maxima as whole numbers; of a row with NaN they are formed again
       __syncthreads();
       uint32_t* const key = reinterpret_cast<uint32_t*>(most_of);
-      const bool again = !(st.s >= 0.f) || st.m == INFINITY;
+      const bool again = !(st.s >= 0.f);
       for (int g = t; g < groups; g += TL_THREADS) {
         uint32_t most = 0;
         if (again) {
@@ -468,9 +566,12 @@ __global__ __launch_bounds__(64) void token_logp_join_kernel(TokenLogpArgs a, in
   const Stat* const ps = parts.stat + (size_t)row * nseg;
   const uint64_t* const pk = parts.key + (size_t)row * nseg * k;
   const uint64_t early = lane < nseg * k ? pk[lane] : 0;
-  Stat st{-INFINITY, 0.f, 0.f};
+  Stat st{-INFINITY, 0.f, 0.f, 0.f};
   if (lane < nseg) st = ps[lane];
-  rescale(st, wave_max(st.m));
+  // relative to the greatest base; its lo goes with it
+  const float hi = wave_max(st.hi);
+  const float lo = wave_max(st.hi == hi ? st.lo : -INFINITY);
+  if (hi != -INFINITY) rebase(st, hi, lo);
   st.s = wave_sum(st.s);
   st.w = wave_sum(st.w);
   if (lane == 0) finish_row(a, row, st, token);

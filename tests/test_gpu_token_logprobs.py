@@ -8,7 +8,7 @@ import pytest
 import paper_2309_00754_amd as H
 from oracle import token_logprobs_backward_ref, token_logprobs_ref
 from gpu_helpers import say
-from update_helpers import TYPES, empty, f64, logp_back_bounds, logp_bounds, near, put
+from update_helpers import TYPES, U, empty, f64, logp_back_bounds, logp_bounds, near, put
 
 pytestmark = pytest.mark.gpu
 INF, LOW = float("inf"), float(np.finfo(np.float32).min)
@@ -147,6 +147,27 @@ def test_extreme_logits(dev):
                   [2.5e38, 2.5e38, -2.5e38, 2.5e38]])
     zt, o = _forward(dev, z, [0, 1, 0, 2, 3], 4, "f32")
     _check(f64(zt), [0, 1, 0, 2, 3], 4, o)
+
+
+@pytest.mark.parametrize("offset", [0, 2 ** 12, -2 ** 16, 2 ** 20, 2 ** 21, -2 ** 21, 2 ** 23, -2 ** 23])
+@pytest.mark.parametrize("V", [600, 70000])
+def test_common_offset(V, offset, dev):
+    """A log-probability does not depend on what all logits of its row have in common: the difference to the rounded base
+    is exact or off by U (d + 1), that to its rest by as much, that to ln s by U |lp|, whatever the offset is.  The logits
+    are whole numbers, which fp32 holds with each offset; sorted, some segments lie on either side of it."""
+    say("common offset", V, offset)
+    z = np.random.default_rng(V).integers(-8, 0, (3, V)).astype(np.float64)
+    z[1], z[2] = np.sort(z[1]), -np.sort(z[2])
+    z[2, : V // 2] = -z[2, : V // 2]
+    tokens = [V // 3, V - 1, 1]
+    zt, o = _forward(dev, z + offset, tokens, 0, "f32")
+    assert np.array_equal(f64(zt), z + offset)
+    ref = token_logprobs_ref(z, tokens, 0)
+    e_lse, e_h, _ = logp_bounds(z, ref)
+    asked = np.take_along_axis(z, np.array(tokens)[:, None], 1)[:, 0]
+    near(f64(o["lp"]), ref["lp"], e_lse + U * (2 * (z.max(1) - asked + 1) + np.abs(ref["lp"])), "lp")
+    near(f64(o["entropy"]), ref["entropy"], e_h, "entropy")
+    near(f64(o["lse"]), ref["lse"] + offset, e_lse + U * np.abs(ref["lse"] + offset), "lse")
 
 
 def test_tokens_out_of_range(dev):
