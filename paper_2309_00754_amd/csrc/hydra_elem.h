@@ -46,6 +46,16 @@ __device__ __forceinline__ void unpack(const uint4& u, float (&f)[kVec<T>]) {
   }
 }
 
+// Four bf16 elements (for results that are twice as wide: a lane that loads 16
+// bytes and stores 32 leaves gaps of 16 bytes in each of its two stores).
+__device__ __forceinline__ void unpack(const u32x2_t& u, float (&f)[4]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    f[2 * i] = __uint_as_float(u[i] << 16);
+    f[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+  }
+}
+
 template <bool MAX>
 __device__ __forceinline__ float combine(float a, float b) {
   return MAX ? fmaxf(a, b) : a + b;
