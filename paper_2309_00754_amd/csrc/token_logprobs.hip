@@ -27,6 +27,8 @@
 // took 335 us.)
 #include "hydra_elem.h"
 
+#include <type_traits>
+
 namespace hydra {
 namespace {
 
@@ -626,10 +628,22 @@ __device__ __forceinline__ void put(V* p, V v) {
 // bf16, 50 MB: 11.6 and 9.8).
 // Stretches of `per` groups; workgroup b takes stretches b, b + gridDim.x, ...
 // of the M * n of all rows.
+template <int TZ, int TD>
+struct BackGroup {
+  // 16 bytes of logits, or of the gradient where it is wider: a lane that loads 16
+  // bytes and stores 32 leaves gaps in each of its two stores (2048 x 32000 bf16
+  // into fp32 with half of the rows live 102 us, so 64.5)
+  static constexpr bool WIDER = TZ == kBf16 && TD == kF32;
+  static constexpr int VEC = WIDER ? 4 : kVec<TZ>, U = WIDER ? 2 * TB_U : TB_U;
+};
+
 template <int TZ, int TD, bool FAR>
 __global__ __launch_bounds__(TB_THREADS) void token_logp_back_kernel(TokenLogpBackArgs a, int n, int per) {
-  constexpr int VEC = kVec<TZ>, ZB = 16 / VEC, DB = TD == kF32 ? 4 : 2;
-  constexpr int STORE = VEC * DB < 16 ? VEC * DB : 16;  // bytes
+  using G = BackGroup<TZ, TD>;
+  constexpr bool WIDER = G::WIDER;
+  constexpr int VEC = G::VEC, U = G::U, ZB = TZ == kF32 ? 4 : 2, DB = TD == kF32 ? 4 : 2;
+  using in_t = typename std::conditional<WIDER, u32x2_t, u32x4_t>::type;
+  using out_t = typename std::conditional<VEC * DB == 8, u32x2_t, u32x4_t>::type;
   const int t = threadIdx.x, V = a.V;
   for (int64_t b = blockIdx.x; b < (int64_t)a.M * n; b += gridDim.x) {
     const int row = (int)(b / n), part = (int)(b - (int64_t)row * n);
@@ -657,27 +671,30 @@ __global__ __launch_bounds__(TB_THREADS) void token_logp_back_kernel(TokenLogpBa
     };
     const int head = head_of<TZ>(z, V), groups = (V - head) / VEC;
     const int g0 = min(groups, part * per), g1 = min(groups, g0 + per);
-    if ((reinterpret_cast<uintptr_t>(d) + head * DB) % STORE != 0) {  // input and output never on a boundary together
+    if ((reinterpret_cast<uintptr_t>(d) + head * DB) % sizeof(out_t) != 0) {  // input and output never on a boundary together
       const int e0 = part == 0 ? 0 : head + g0 * VEC, e1 = part == n - 1 ? V : head + g1 * VEC;
       for (int e = e0 + t; e < e1; e += TB_THREADS) one(e);
       continue;
     }
-    const u32x4_t* const zv = reinterpret_cast<const u32x4_t*>(z + (size_t)head * ZB);
-    uint8_t* const dv = d + (size_t)head * DB;
-    for (int g = g0 + t; g < g1; g += TB_THREADS * TB_U) {
-      u32x4_t u[TB_U];
+    const in_t* const zv = reinterpret_cast<const in_t*>(z + (size_t)head * ZB);
+    out_t* const dv = reinterpret_cast<out_t*>(d + (size_t)head * DB);
+    for (int g = g0 + t; g < g1; g += TB_THREADS * U) {
+      in_t u[U];
       if (live) {
 #pragma unroll
-        for (int q = 0; q < TB_U; ++q)
+        for (int q = 0; q < U; ++q)
           if (g + q * TB_THREADS < g1) u[q] = fetch<FAR>(zv + g + q * TB_THREADS);
       }
 #pragma unroll
-      for (int q = 0; q < TB_U; ++q) {
+      for (int q = 0; q < U; ++q) {
         const int at = g + q * TB_THREADS;
         if (at >= g1) break;
         float f[VEC];
         if (live) {
-          unpack<TZ>(__builtin_bit_cast(uint4, u[q]), f);
+          if constexpr (WIDER)
+            unpack(u[q], f);
+          else
+            unpack<TZ>(__builtin_bit_cast(uint4, u[q]), f);
 #pragma unroll
           for (int e = 0; e < VEC; ++e) f[e] = gradient(f[e]);
           const int mine = tk - head - at * VEC;  // the token's place in this group
@@ -689,7 +706,7 @@ __global__ __launch_bounds__(TB_THREADS) void token_logp_back_kernel(TokenLogpBa
 #pragma unroll
           for (int e = 0; e < VEC; ++e) f[e] = 0.f;
         }
-        uint32_t w[VEC * DB / 4];
+        out_t w;
 #pragma unroll
         for (int e = 0; e < VEC * DB / 4; ++e) {
           if constexpr (TD == kF32)
@@ -697,14 +714,7 @@ __global__ __launch_bounds__(TB_THREADS) void token_logp_back_kernel(TokenLogpBa
           else
             w[e] = f32_to_bf16_pair(f[2 * e], f[2 * e + 1]);
         }
-        if constexpr (VEC * DB == 8) {
-          put<FAR>(reinterpret_cast<u32x2_t*>(dv) + at, u32x2_t{w[0], w[1]});
-        } else {
-#pragma unroll
-          for (int e = 0; e < VEC * DB / 16; ++e)
-            put<FAR>(reinterpret_cast<u32x4_t*>(dv) + at * (VEC * DB / 16) + e,
-                     u32x4_t{w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]});
-        }
+        put<FAR>(dv + at, w);
       }
     }
     if (part == 0 && t < head) one(t);
@@ -759,8 +769,9 @@ hipError_t launch_token_logp(const TokenLogpArgs& a, void* ws, hipStream_t strea
 template <int TZ, int TD>
 static void back_of(const TokenLogpBackArgs& a, hipStream_t stream) {
   // a stretch is one round of the workgroup's loads, or several where there are many
-  constexpr int ROUND = TB_THREADS * TB_U;
-  const int groups = a.V / kVec<TZ> > 0 ? a.V / kVec<TZ> : 1;
+  using G = BackGroup<TZ, TD>;
+  constexpr int ROUND = TB_THREADS * G::U;
+  const int groups = a.V / G::VEC > 0 ? a.V / G::VEC : 1;
   const int64_t rounds = (int64_t)a.M * ((groups + ROUND - 1) / ROUND);
   int per = ROUND;
   while (per < 8 * ROUND && rounds * ROUND / per > 8192) per *= 2;
