@@ -643,7 +643,8 @@ hydra_status hydra_token_logprobs_workspace_bytes(int64_t M, int64_t V, int64_t 
  * and log-probability -inf; a row of nothing else has lse -inf and NaN lp,
  * entropy and top_lp (top_ids 0, 1, ...).  In a row that holds NaN or +inf lp,
  * lse, entropy and top_lp are NaN (top_ids then take NaN first, then +inf).
- * Sums and maxima are fp32, in an order that depends on M, V and the type alone.
+ * Sums and maxima are fp32, in an order that depends on M, V, the type and how
+ * the rows lie to 16-byte boundaries alone.
  * Requires 1 <= M <= 2^20, 1 <= V <= 2^21, M V <= 2^38, ld <= 2^31 - 1; logits
  * need their element's alignment only.  Outputs distinct (HYDRA_ERR_SHAPE).
  * Calls that share a workspace on different streams race.
@@ -672,7 +673,8 @@ hydra_status hydra_token_logprobs(const void* logits, hydra_dtype logits_type, i
  *           a row whose d_lp is not 0; that row's gradient is NaN
  * At least one of d_lp and d_entropy (HYDRA_ERR_NULL).  A row whose upstream
  * gradients are both 0 (a prompt token, padding) gets zeros, whatever its
- * logits, token and statistics hold.  p_j goes by the lse given: where that has
+ * logits, token and statistics hold; another row of -inf alone gets NaN.  p_j
+ * goes by the lse given: where that has
  * lost ln V to its rounding (a row of logits near the type's lowest value alone)
  * the p_j do not add up to 1.  Products are fp32, each gradient rounded once, to
  * nearest even.  Sizes, alignment and overlaps as in hydra_token_logprobs.

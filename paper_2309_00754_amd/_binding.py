@@ -946,7 +946,7 @@ def _hydra_token_logprobs(logits, tokens, lp, lse, entropy, top_ids, top_lp, wor
     torch = _torch()
     ld = _rows(logits, "logits")
     M, V = logits.shape
-    top = 0 if top_ids is None else top_ids.shape[-1]
+    top = top_ids.shape[1] if isinstance(top_ids, torch.Tensor) and top_ids.dim() == 2 else 0
     _need(tokens, "tokens", (torch.int32,), (M,))
     for name, t in (("lp", lp), ("lse", lse), ("entropy", entropy)):
         _need(t, name, (torch.float32,), (M,))

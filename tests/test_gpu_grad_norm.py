@@ -64,6 +64,25 @@ def test_clip_into_other_buffers(kind, out_kind, max_norm, dev):
         assert np.array_equal(f64(g), a)  # the gradients themselves stay
 
 
+@pytest.mark.parametrize("kind,out_kind", list(itertools.product(TYPES, TYPES)))
+def test_clip_at_any_alignment(kind, out_kind, dev):
+    """Gradients and results that lie apart to 16-byte boundaries; what lies around the results is left as it was."""
+    import torch
+    say("clip alignments", kind, out_kind)
+    for n in (5, 9001):
+        a = np.random.default_rng(n).normal(0, 1, n)
+        for shift, out_shift in itertools.product(range(8), range(8)):
+            g = put(a, kind, dev, shift)
+            flat = torch.full((out_shift + n + 9,), 9.0, device=dev, dtype=empty(1, out_kind, dev).dtype)
+            out = flat[out_shift:out_shift + n]
+            norm, err = _clip(dev, [g], 0.5, [out])
+            ref, scaled = grad_clip_ref([f64(g)], 0.5)
+            near([norm], [ref], 1.5 * U * ref, "norm")
+            _check(out, scaled[0], out_kind, f"out {n} {shift} {out_shift}")
+            out.fill_(9.0)
+            assert err == 0 and (flat == 9).all()
+
+
 @pytest.mark.parametrize("kinds", [("f32",), ("bf16",), ("f32", "bf16")])
 @pytest.mark.parametrize("count", [1, 9, 130, 500])
 def test_clip_in_place(kinds, count, dev):

@@ -234,6 +234,46 @@ def test_gradient(M, V, kind, d_kind, dev):
         assert err.item() == 0
 
 
+@pytest.mark.parametrize("kind,d_kind", list(itertools.product(TYPES, TYPES)))
+def test_gradient_at_any_alignment(kind, d_kind, dev):
+    """Rows and results that lie apart to 16-byte boundaries, and what lies around the results is left as it was."""
+    import torch
+    say("gradient alignments", kind, d_kind)
+    M, V, ld = 3, 1061, 1070
+    z, tokens, d_lp = _logits(M, V, 8), [1060, 0, 7], np.array([0.5, -1.0, 2.0])
+    for shift, d_shift in itertools.product(range(8), range(8)):
+        zt = put(z, kind, dev, shift, ld)
+        zz = f64(zt)
+        lse = put(token_logprobs_ref(zz)["lse"], "f32", dev)
+        flat = torch.full((d_shift + M * ld + 8,), 7.0, dtype=empty(1, d_kind, dev).dtype, device=dev)
+        dz = flat.as_strided((M, V), (ld, 1), d_shift)
+        H.hydra_token_logprobs_backward(zt, torch.tensor(tokens, dtype=torch.int32, device=dev), lse, dz,
+                                        put(d_lp, "f32", dev))
+        _check_backward(zz, tokens, {"lse": f64(lse), "d_lp": d_lp, "entropy": None, "d_entropy": None}, dz, d_kind)
+        dz.fill_(7.0)
+        assert (flat == 7).all()
+
+
+@pytest.mark.parametrize("kind", TYPES)
+def test_rows_of_masked_entries_alone_have_no_gradient(kind, dev):
+    """(NaN, as their log-probabilities; zeros where nothing is asked for; the rows beside them as ever)"""
+    import torch
+    say("rows of masked entries alone", kind)
+    z = _logits(4, 3001, 3)
+    z[1], z[2] = -INF, -INF
+    zt = put(z, kind, dev)
+    zz = f64(zt)
+    lse = torch.tensor(token_logprobs_ref(zz)["lse"], dtype=torch.float32, device=dev)
+    assert lse[1] == -INF
+    d_lp, dz = np.array([1.0, 1.0, 0.0, -2.0]), empty((4, 3001), kind, dev)
+    H.hydra_token_logprobs_backward(zt, torch.arange(4, dtype=torch.int32, device=dev), lse, dz, put(d_lp, "f32", dev))
+    got = f64(dz)
+    assert np.isnan(got[1]).all() and (got[2] == 0).all()
+    live = [0, 3]
+    ref = token_logprobs_backward_ref(zz[live], live, f64(lse)[live], d_lp[live])
+    near(got[live], ref, logp_back_bounds(zz[live], f64(lse)[live], d_lp[live], None, None, ref, kind), "d_logits")
+
+
 @pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("V", [75, 32000])
 def test_rows_without_a_gradient_are_zeros(V, kind, dev):

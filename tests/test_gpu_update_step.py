@@ -317,3 +317,14 @@ def test_token_logprob_refusals(what, dev):
         H.hydra_token_logprobs(*args, **kw)
     torch.cuda.synchronize()
     assert (lp == 7).all()
+
+
+def test_alternatives_of_another_shape_are_refused(dev):
+    import torch
+    z, lp = torch.randn(4, 100, device=dev), torch.zeros(4, device=dev)
+    tok = torch.zeros(4, dtype=torch.int32, device=dev)
+    for ids in (torch.zeros((), dtype=torch.int32, device=dev), torch.zeros(4, dtype=torch.int32, device=dev)):
+        with pytest.raises(ValueError):
+            H.hydra_token_logprobs(z, tok, lp, top_ids=ids)
+    with pytest.raises(TypeError):
+        H.hydra_token_logprobs(z, tok, lp, top_ids=[1, 2, 3, 4])
