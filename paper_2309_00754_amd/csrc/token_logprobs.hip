@@ -723,14 +723,15 @@ __global__ __launch_bounds__(TB_THREADS) void token_logp_back_kernel(TokenLogpBa
 }
 
 // Segments of a row: none longer than kSegMost; more, of 24 KB, where a row is
-// longer than 128 KB and there are fewer than 256 of them.  One row of 50272 fp32
-// logits takes 5.7 us in eight segments (their join is a second launch), so 7.7
-// in one, 64 rows 7.4 and 9.2, 250 rows 12.4 and 10.5; 32000 fp32 6.1 and 5.6,
-// 50272 bf16 5.7 and 6.4 (with alternatives, from 16 rows on, 10.7 and 10.0).
+// longer than 128 KB and there are few enough rows for three each on 256 workgroups
+// (their join is a second launch).  50272 fp32 logits with 8 alternatives: 6 rows
+// 8.6 us in eight segments, 9.9 in one; 64 rows 10.5 in four and 11.1; 100 rows 12.7
+// in two and 11.8.  One row 6.2 and 6.4; of 32000 fp32 5.6 in five and 4.9.
 int segments(int M, int V, int type) {
   const int64_t least = (V + kSegMost - 1) / kSegMost, bytes = V * (int64_t)type_bytes(type);
   int64_t n = bytes > (128 << 10) ? bytes / (24 << 10) : 1;
   n = n < 256 / M ? n : 256 / M;
+  n = n < 3 ? 1 : n;
   n = n > least ? n : least;
   return (int)(n < kSegs ? n : kSegs);
 }
