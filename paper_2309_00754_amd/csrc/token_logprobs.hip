@@ -7,7 +7,8 @@
 //   H = ln S - W / S,  W = sum_j e^(z_j - m) (z_j - m)
 //   dz_j = d_lp ([j == token] - p_j) - d_H p_j (ln p_j + H), p_j = e^(z_j - lse)
 //
-//  * token_logp_kernel: a workgroup per row, or per segment of a long one,
+//  * token_logp_kernel: a workgroup of 512 threads per row or segment of a long
+//    one, of 128 per row where many are short,
 //    reads it once in 16-byte groups, each thread with running sums relative to
 //    a power of two that follows its maximum; the threads meet in a fixed tree.
 //    For the alternatives it keeps the maximum of every group in LDS.
@@ -32,8 +33,7 @@
 namespace hydra {
 namespace {
 
-constexpr int TL_THREADS = 512;
-constexpr int TL_WAVES = TL_THREADS / 64;
+constexpr int TL_THREADS = 512, TL_FEW = 128;  // threads of a row or segment, of a short row
 constexpr int TL_U = 4;             // 16-byte loads of a thread under way
 constexpr int kSegMost = 57344;     // elements of a segment (its groups' maxima, 4 bytes each, beside 6 KB in 64 KB of LDS)
 constexpr int kSegs = 64;           // segments of a row at most
@@ -75,8 +75,7 @@ __device__ __forceinline__ bool masked_out(uint64_t key) { return (uint32_t)(key
 // relative to that logit itself.  (Bound by these instructions, not by memory,
 // where few rows or 16-bit ones are read: with the sums relative to the maximum
 // of every 16 bytes, twice the instructions, 32000 logits of one row took 5.7 us
-// in place of 4.8, 900 rows of 40000 with 16 alternatives 36.8 in place of 33.0;
-// rows shorter than one round lose: 4000 of 5000 15.5, now 16.0.)
+// in place of 4.8, 900 rows of 40000 with 16 alternatives 36.8 in place of 33.0.)
 constexpr float kLow = -4194304.f, kRange = 2097152.f;
 constexpr float kFar = -1000.f;  // 2^kFar is 0, and a product of the two is (with -inf it would not be)
 
@@ -142,21 +141,24 @@ __device__ __forceinline__ void rebase(Stat& a, float hi, float lo) {
 }
 
 // The waves' maxima, then their sums, met by the workgroup.
+template <int WAVES>
 struct Meet {
-  float m[TL_WAVES], s[TL_WAVES], w[TL_WAVES];
+  float m[WAVES], s[WAVES], w[WAVES];
 };
-__device__ __forceinline__ void meet_max(Run& a, const Meet& meet) {
+template <int WAVES>
+__device__ __forceinline__ void meet_max(Run& a, const Meet<WAVES>& meet) {
   float m = meet.m[0];
 #pragma unroll
-  for (int i = 1; i < TL_WAVES; ++i) m = fmaxf(m, meet.m[i]);
+  for (int i = 1; i < WAVES; ++i) m = fmaxf(m, meet.m[i]);
   a.m = m;
   rescale(a, exponent_of(m));
 }
-__device__ __forceinline__ void meet_sums(float& s, float& w, const Meet& meet) {
+template <int WAVES>
+__device__ __forceinline__ void meet_sums(float& s, float& w, const Meet<WAVES>& meet) {
   s = meet.s[0];
   w = meet.w[0];
 #pragma unroll
-  for (int i = 1; i < TL_WAVES; ++i) {
+  for (int i = 1; i < WAVES; ++i) {
     s += meet.s[i];
     w += meet.w[i];
   }
@@ -164,14 +166,15 @@ __device__ __forceinline__ void meet_sums(float& s, float& w, const Meet& meet) 
 
 // How many of n numbers (LDS) are at least `bound` (> 0), in every thread.  `tally`:
 // this call's alone until the workgroup's next barrier but one.
+template <int WAVES>
 __device__ __forceinline__ int count_from(const uint32_t* v, int n, uint32_t bound, int* tally) {
   constexpr int U = 8;
   int c = 0;
-  for (int i0 = 0; i0 < n; i0 += TL_THREADS * U) {
+  for (int i0 = 0; i0 < n; i0 += WAVES * 64 * U) {
     uint32_t x[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int i = i0 + u * TL_THREADS + threadIdx.x;
+      const int i = i0 + u * WAVES * 64 + threadIdx.x;
       x[u] = i < n ? v[i] : 0;
     }
 #pragma unroll
@@ -181,7 +184,7 @@ __device__ __forceinline__ int count_from(const uint32_t* v, int n, uint32_t bou
   __syncthreads();
   c = tally[0];
 #pragma unroll
-  for (int i = 1; i < TL_WAVES; ++i) c += tally[i];
+  for (int i = 1; i < WAVES; ++i) c += tally[i];
   return c;
 }
 
@@ -190,28 +193,29 @@ __device__ __forceinline__ int count_from(const uint32_t* v, int n, uint32_t bou
 // returns a bound that they and no others but equals of it reach.  `start`: a
 // bound to try first (where ties are what made this necessary it is mostly the
 // one); if fewer than `want` reach it, those alone are taken.
+template <int WAVES>
 __device__ __forceinline__ uint32_t greatest(const uint32_t* v, int n, int want, uint32_t start, int* slot, int* count,
-                                             int (*tally)[TL_WAVES]) {
+                                             int (*tally)[WAVES]) {
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   uint32_t bound = start;
-  int have = n, turn = 1, above = count_from(v, n, start + 1, tally[0]);
+  int have = n, turn = 1, above = count_from<WAVES>(v, n, start + 1, tally[0]);
   if (above >= want) {
     bound = 0;
     for (int bit = 31; bit >= 0 && have > want; --bit, turn ^= 1) {
-      const int c = count_from(v, n, bound | (1u << bit), tally[turn]);
+      const int c = count_from<WAVES>(v, n, bound | (1u << bit), tally[turn]);
       if (c >= want) {
         bound |= 1u << bit;
         have = c;
       }
     }
     if (have > want) {
-      above = count_from(v, n, bound + 1, tally[turn]);
+      above = count_from<WAVES>(v, n, bound + 1, tally[turn]);
       turn ^= 1;
     }
   }
   // all above the bound; of its equals (where they are too many) the first
   int left = want - above;
-  for (int i0 = 0; i0 < n; i0 += TL_THREADS, turn ^= 1) {
+  for (int i0 = 0; i0 < n; i0 += WAVES * 64, turn ^= 1) {
     const int i = i0 + t;
     const uint32_t x = i < n ? v[i] : 0;
     bool take = i < n && x > bound;
@@ -221,7 +225,7 @@ __device__ __forceinline__ uint32_t greatest(const uint32_t* v, int n, int want,
       if (lane == 0) tally[turn][wave] = __popcll(equals);
       __syncthreads();
       int before = __popcll(equals & ((1ull << lane) - 1)), all = 0;
-      for (int w = 0; w < TL_WAVES; ++w) {
+      for (int w = 0; w < WAVES; ++w) {
         before += w < wave ? tally[turn][w] : 0;
         all += tally[turn][w];
       }
@@ -345,14 +349,14 @@ __device__ __forceinline__ Span span_of(const void* row, int V, int seg, int nse
 }
 
 // Grid: M * nseg workgroups.
-template <int T, bool TOP>
-__global__ __launch_bounds__(TL_THREADS) void token_logp_kernel(TokenLogpArgs a, int nseg, Parts parts) {
-  constexpr int VEC = kVec<T>;
+template <int T, bool TOP, int THREADS>
+__global__ __launch_bounds__(THREADS) void token_logp_kernel(TokenLogpArgs a, int nseg, Parts parts) {
+  constexpr int VEC = kVec<T>, WAVES = THREADS / 64;
   extern __shared__ float most_of[];  // TOP: the maxima of the segment's groups
-  __shared__ Meet meet;
+  __shared__ Meet<WAVES> meet;
   // TOP: the waves' bounds, the groups that reach the bound, the logits that do
-  __shared__ float bound_of[TOP ? TL_WAVES : 1];
-  __shared__ int slot[TOP ? kCand : 1], count[2], tally[TOP ? 2 : 1][TL_WAVES];
+  __shared__ float bound_of[TOP ? WAVES : 1];
+  __shared__ int slot[TOP ? kCand : 1], count[2], tally[TOP ? 2 : 1][WAVES];
   __shared__ __align__(16) uint64_t cand[TOP ? kCand : 1];
   const int row = blockIdx.x / nseg, seg = blockIdx.x - row * nseg, t = threadIdx.x, V = a.V;
   const uint8_t* const z = static_cast<const uint8_t*>(a.z) + (size_t)row * a.ld * (16 / VEC);
@@ -365,19 +369,19 @@ __global__ __launch_bounds__(TL_THREADS) void token_logp_kernel(TokenLogpArgs a,
   const __amdgpu_buffer_rsrc_t rs = make_rsrc(v + sp.g0, (uint32_t)groups * 16u);
   const int first_of_wave = __builtin_amdgcn_readfirstlane(t & ~63);
   Run run;
-  constexpr int ROUND = TL_THREADS * TL_U;
+  constexpr int ROUND = THREADS * TL_U;
   for (int g0 = 0; g0 < groups; g0 += ROUND) {
     uint4 u[TL_U];
 #pragma unroll
     for (int q = 0; q < TL_U; ++q) {
-      const int g = g0 + q * TL_THREADS + t;
+      const int g = g0 + q * THREADS + t;
       u[q] = buf_load16(rs, g < groups ? g * 16 : kOutOfRange);
     }
     if (g0 + ROUND > groups) {  // the last round: -inf where there is no group
       constexpr uint32_t none = T == kF32 ? 0xFF800000u : 0xFF80FF80u;
 #pragma unroll
       for (int q = 0; q < TL_U; ++q)
-        if (g0 + q * TL_THREADS + t >= groups) u[q] = make_uint4(none, none, none, none);
+        if (g0 + q * THREADS + t >= groups) u[q] = make_uint4(none, none, none, none);
     }
     float f[TL_U * VEC], most = -INFINITY;
 #pragma unroll
@@ -390,7 +394,7 @@ __global__ __launch_bounds__(TL_THREADS) void token_logp_kernel(TokenLogpArgs a,
 #pragma unroll
       for (int e = 0; e < VEC; ++e) f[q * VEC + e] = x[e];
       if constexpr (TOP) {
-        const int g = g0 + q * TL_THREADS + t;
+        const int g = g0 + q * THREADS + t;
         if (g < groups) most_of[g] = m;
       }
       most = fmaxf(most, m);
@@ -398,7 +402,7 @@ __global__ __launch_bounds__(TL_THREADS) void token_logp_kernel(TokenLogpArgs a,
     make_room(run, most);
 #pragma unroll
     for (int q = 0; q < TL_U; ++q)
-      if (g0 + q * TL_THREADS + first_of_wave < groups) add<VEC>(run, f + q * VEC);
+      if (g0 + q * THREADS + first_of_wave < groups) add<VEC>(run, f + q * VEC);
   }
   // the elements in no group: a thread each
   float edge = -INFINITY;
@@ -417,7 +421,7 @@ __global__ __launch_bounds__(TL_THREADS) void token_logp_kernel(TokenLogpArgs a,
   if (lane == 0) meet.m[wave] = wave_most;
   // whole waves of groups, or the only one (where the last wave's few threads cannot
   // bound anything, and what is left to others is few)
-  const int waves = groups >= 64 ? min(TL_WAVES, groups / 64) : groups > 0;
+  const int waves = groups >= 64 ? min(WAVES, groups / 64) : groups > 0;
   if constexpr (TOP) {
     float left = mine, bound = -INFINITY;
     if (wave < waves) {
@@ -446,15 +450,15 @@ __global__ __launch_bounds__(TL_THREADS) void token_logp_kernel(TokenLogpArgs a,
     if (waves > 0) bound = bound_of[0];
     for (int i = 1; i < waves; ++i) bound = fminf(bound, bound_of[i]);
     constexpr int U = 4;  // (loads from LDS under way; with 8, 4000 rows of 5000 took 28.1 us, not 26.7)
-    for (int g0 = t; g0 < groups; g0 += TL_THREADS * U) {
+    for (int g0 = t; g0 < groups; g0 += THREADS * U) {
       float x[U];
 #pragma unroll
-      for (int q = 0; q < U; ++q) x[q] = g0 + q * TL_THREADS < groups ? most_of[g0 + q * TL_THREADS] : -INFINITY;
+      for (int q = 0; q < U; ++q) x[q] = g0 + q * THREADS < groups ? most_of[g0 + q * THREADS] : -INFINITY;
 #pragma unroll
       for (int q = 0; q < U; ++q)
         if (reaches(x[q])) {
           const int i = atomicAdd(&count[0], 1);
-          if (i < kCand) slot[i] = g0 + q * TL_THREADS;
+          if (i < kCand) slot[i] = g0 + q * THREADS;
         }
     }
     if (edge_at >= 0 && reaches(edge)) cand[atomicAdd(&count[1], 1)] = order_key(edge, edge_at);
@@ -470,7 +474,7 @@ __global__ __launch_bounds__(TL_THREADS) void token_logp_kernel(TokenLogpArgs a,
       sum += e;
       mean = fmaf(e, fmaxf(d, kFar), mean);
     };
-    for (int e = sp.head + sp.g0 * VEC + t; e < sp.head + sp.g1 * VEC; e += TL_THREADS) add(load_z<T>(z, e));
+    for (int e = sp.head + sp.g0 * VEC + t; e < sp.head + sp.g1 * VEC; e += THREADS) add(load_z<T>(z, e));
     if (edge_at >= 0) add(edge);
     __syncthreads();
     sum = wave_sum(sum);
@@ -494,7 +498,7 @@ __global__ __launch_bounds__(TL_THREADS) void token_logp_kernel(TokenLogpArgs a,
     const int k = a.top, slots = count[0];
     int n = kCand + 1;  // too many
     if (slots <= kCand && st.s >= 0.f) {  // (no NaN and no +inf)
-      for (int i = t; i < slots * VEC; i += TL_THREADS) {
+      for (int i = t; i < slots * VEC; i += THREADS) {
         const int e = sp.head + (sp.g0 + slot[i / VEC]) * VEC + i % VEC;
         const float x = load_z<T>(z, e);
         if (reaches(x)) {
@@ -510,7 +514,7 @@ __global__ __launch_bounds__(TL_THREADS) void token_logp_kernel(TokenLogpArgs a,
       __syncthreads();
       uint32_t* const key = reinterpret_cast<uint32_t*>(most_of);
       const bool again = !(st.s >= 0.f);
-      for (int g = t; g < groups; g += TL_THREADS) {
+      for (int g = t; g < groups; g += THREADS) {
         uint32_t most = 0;
         if (again) {
           float f[VEC];
@@ -533,7 +537,7 @@ __global__ __launch_bounds__(TL_THREADS) void token_logp_kernel(TokenLogpArgs a,
         if (t == 0) count[0] = groups;
         __syncthreads();
       }
-      for (int i = t; i < count[0] * VEC; i += TL_THREADS) {
+      for (int i = t; i < count[0] * VEC; i += THREADS) {
         const int e = sp.head + (sp.g0 + slot[i / VEC]) * VEC + i % VEC;
         const uint64_t x = order_key(load_z<T>(z, e), e);
         if ((uint32_t)(x >> 32) >= least && !masked_out(x)) cand[atomicAdd(&count[1], 1)] = x;
@@ -736,17 +740,32 @@ int segments(int M, int V, int type) {
   return (int)(n < kSegs ? n : kSegs);
 }
 
+// Whether 128 threads take a row, not 512: rows of up to five of their rounds of
+// loads, and enough of them to fill the chip that way.  2000 fp32 logits, 400 rows
+// 3.4 us, so 3.9 with 512; 5000 bf16 with 8 alternatives, 900 rows 7.4 and 9.5;
+// 10000 fp32, 900 rows 8.2 and 9.1, 400 rows 6.9 and 5.9; 14000 with 8, 1800 rows
+// 29.7 and 22.7.  (256 threads lie between the two.)
+bool short_rows(int M, int groups) { return groups <= 2560 && M >= 256 + groups / 4; }
+
 size_t stat_bytes(int M, int nseg) { return ((size_t)M * nseg * sizeof(Stat) + 15) & ~size_t(15); }
+
+template <int T, int THREADS>
+void rows_of(const TokenLogpArgs& a, int nseg, const Parts& p, hipStream_t stream) {
+  const dim3 grid((unsigned)(a.M * nseg)), block(THREADS);
+  if (a.top > 0) {
+    const int groups = (a.V / kVec<T> + nseg - 1) / nseg + 1;
+    hipLaunchKernelGGL((token_logp_kernel<T, true, THREADS>), grid, block, groups * sizeof(float), stream, a, nseg, p);
+  } else {
+    hipLaunchKernelGGL((token_logp_kernel<T, false, THREADS>), grid, block, 0, stream, a, nseg, p);
+  }
+}
 
 template <int T>
 void forward(const TokenLogpArgs& a, int nseg, const Parts& p, hipStream_t stream) {
-  const dim3 grid((unsigned)(a.M * nseg)), block(TL_THREADS);
-  if (a.top > 0) {
-    const int groups = (a.V / kVec<T> + nseg - 1) / nseg + 1;
-    hipLaunchKernelGGL((token_logp_kernel<T, true>), grid, block, groups * sizeof(float), stream, a, nseg, p);
-  } else {
-    hipLaunchKernelGGL((token_logp_kernel<T, false>), grid, block, 0, stream, a, nseg, p);
-  }
+  if (short_rows(a.M, a.V / kVec<T>))
+    rows_of<T, TL_FEW>(a, nseg, p, stream);
+  else
+    rows_of<T, TL_THREADS>(a, nseg, p, stream);
   if (nseg > 1) hipLaunchKernelGGL((token_logp_join_kernel<T>), dim3(a.M), dim3(64), 0, stream, a, nseg, p);
 }
 

@@ -129,6 +129,41 @@ def test_ties_go_to_the_lowest_index(V, kind, dev):
 
 
 @pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("V,shift,top", [(1, 0, 1), (40, 1, 32), (511, 0, 0), (1003, 3, 7), (2050, 0, 32), (4099, 2, 20),
+                                         (10241, 0, 32), (10247, 5, 0)])
+def test_rows_of_every_sort_many_times(V, shift, top, kind, dev):
+    """Short rows in numbers: each sort against the oracle, its repetitions to the bit."""
+    import torch
+    say("rows many times", V, shift, top, kind)
+    r = np.random.default_rng(V)
+    z = r.normal(0, 2, (14, V))
+    z[1], z[2], z[3] = 0.0, np.sort(z[2]), -np.sort(z[3])
+    z[4, V // 2:], z[5, :], z[6, :] = -INF, -INF, LOW
+    z[7, r.integers(0, V, max(1, V // 9))] = LOW
+    z[8, :], z[8, V // 3] = LOW, 1.0
+    z[9, V // 2], z[10, V - 1] = np.nan, INF
+    z[11] = np.round(z[11])
+    z[12] += 4.0e6
+    z[13, ::2] = -INF
+    tokens = list(r.integers(0, V, 13)) + [V]
+    n = 64 if V < 3000 else 80
+    zt = put(np.tile(z, (n, 1)), kind, dev, shift, (V + 15) // 8 * 8)
+    M = zt.shape[0]
+    tok = torch.tensor(tokens * n, dtype=torch.int32, device=dev)
+    o = {k: empty(M, "f32", dev) for k in ("lp", "lse", "entropy")}
+    o["ids"] = torch.full((M, top), -7, dtype=torch.int32, device=dev) if top else None
+    o["top_lp"] = empty((M, top), "f32", dev) if top else None
+    o["err"] = torch.zeros(1, dtype=torch.int32, device=dev)
+    H.hydra_token_logprobs(zt, tok, o["lp"], o["lse"], o["entropy"], o["ids"], o["top_lp"], None, o["err"])
+    for k, v in o.items():
+        if v is not None and k != "err":
+            bits = v.view(torch.int32).view(n, 14, -1)
+            assert (bits == bits[:1]).all(), k
+            o[k] = v[:14]
+    _check(f64(zt)[:14], tokens, top, o, err=1)
+
+
+@pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("V", [33, 4000, 70000])
 def test_nan_and_infinities(V, kind, dev):
     say("nan and infinities", V, kind)
