@@ -17,9 +17,10 @@
 //    gradient are filled with zeros unread.
 //
 // The k largest of a row: every wave finds the j-th largest of its threads'
-// maxima, j = k over the waves; the smallest of these is a bound that at least
-// k logits reach.  The groups whose maximum reaches it are read again (from the
-// cache), and what reaches it there, some tens of logits, is ranked by counting.
+// maxima, j = k over the waves, or a number between it and the next; the smallest
+// of these is a bound that at least k logits reach.  The groups whose maximum
+// reaches it are read again (from the cache), and what reaches it there, some tens
+// of logits, is ranked by counting.
 // Ties, masks of one value and sorted rows can leave too many for that.  Then
 // the k greatest groups by (maximum, lower index) are found exactly, by their
 // maxima's bits from the highest down: they hold the k largest logits, since any
@@ -423,14 +424,30 @@ __global__ __launch_bounds__(THREADS) void token_logp_kernel(TokenLogpArgs a, in
   // bound anything, and what is left to others is few)
   const int waves = groups >= 64 ? min(WAVES, groups / 64) : groups > 0;
   if constexpr (TOP) {
-    float left = mine, bound = -INFINITY;
+    float bound = -INFINITY;
     if (wave < waves) {
       const int j = (a.top + waves - 1) / waves;
       bound = wave_most;
-      for (int i = 1; i < j; ++i) {
-        const uint64_t have = __ballot(left == bound);
-        if (lane == __ffsll((unsigned long long)have) - 1) left = -INFINITY;
-        bound = wave_max(left);
+      if (j >= 5) {
+        // bit by bit, until j lanes reach it (what lies between the j-th and the
+        // next is as good a bound) or it is found; extracted one by one, 3361 rows
+        // of 1508 bf16 with 32 alternatives 16.5 us, not 12.3
+        const uint32_t key = order_bits(mine);
+        uint32_t least = 0;
+        for (int bit = 31; bit >= 0; --bit) {
+          const uint32_t next = least | (1u << bit);
+          const int c = __popcll(__ballot(key >= next));
+          if (c >= j) least = next;
+          if (c == j) break;
+        }
+        bound = least > 0x007FFFFFu ? logit_of((uint64_t)least << 32) : -INFINITY;  // (0x007FFFFF: -inf)
+      } else {
+        float left = mine;
+        for (int i = 1; i < j; ++i) {
+          const uint64_t have = __ballot(left == bound);
+          if (lane == __ffsll((unsigned long long)have) - 1) left = -INFINITY;
+          bound = wave_max(left);
+        }
       }
     }
     if (lane == 0) bound_of[wave] = bound;
