@@ -6,7 +6,7 @@
 //   g = dy w, xh = (x - mean) rstd
 //   dx = rstd (g - sum g / K - xh sum (g xh) / K), dw = sum_m dy xh, db = sum_m dy
 //
-// Up to K = 16384 a row is held in the registers of 1 to 8 waves and read once:
+// Up to K = 16384 a row is held in the registers of 1 to 16 waves and read once:
 //  * layer_norm_kernel: sum, centred squares and result from the registers; a
 //    row group goes on to further rows with its w and b in registers.
 //  * norm_back_kernel: the two sums of dx, dx, and each lane's columns of dw
@@ -114,7 +114,7 @@ __device__ __forceinline__ void load_vector(const void* p, int type, int K, int 
   }
 }
 
-constexpr int kMaxWaves = 8;  // of a row
+constexpr int kMaxWaves = 16;  // of a row
 
 // Sum over the `nw` waves of a row group (nw a power of two; this wave's group
 // starts at wave w0), in every thread.  `red` is used by this call alone until
@@ -417,11 +417,13 @@ __global__ __launch_bounds__(COL_THREADS) void norm_back_cols_kernel(LayerNormBa
 // Columns per lane.  16 as far as 8 waves reach: 4096 x 4096 fp32 forward 26.9
 // us (32: 28.9; 8: 26.4 to 27.7), backward 46.6 (51.1; 49.9); bf16 forward 13.8
 // (14.6; 15.3 to 17.7), backward 32.7 (32.6; 38.1).  32 for rows of up to
-// 16384.  Element by element (rows of odd length or alignment) 16 alone: a
-// chunk's address takes a register too, and 32 spill.
+// 16384.  Element by element (rows of odd length or alignment) 16 alone, in 16
+// waves above 8192: a chunk's address takes a register too, and 32 spill (of 16
+// the backward keeps some 30 in scratch memory there, yet 3552 x 9445 fp32 takes 106
+// us, where the long rows' kernels take 198; bf16 81 and 251; forward 65 and 115).
 constexpr int kFew = 16, kMany = 32;
-constexpr int kFewK = kMaxWaves * 64 * kFew, kManyK = kMaxWaves * 64 * kMany;
-constexpr int FWD_THREADS = 256, BACK_THREADS = 512;
+constexpr int kFewK = 8 * 64 * kFew, kManyK = 8 * 64 * kMany;
+constexpr int FWD_THREADS = 256, BACK_THREADS = 512, ODD_THREADS = kMaxWaves * 64;
 
 // Waves per row: enough for `lane` columns a lane.
 int row_waves(int K, int lane) {
@@ -438,7 +440,7 @@ int row_waves(int K, int lane) {
 // with the launch).  Workgroups of 1024 threads gain up to 6% on much bf16 (8192
 // x 4096 47.1 us, so 50.2) and lose as much on fp32 (86.6, so 81.0) and few rows.
 int back_blocks(int M, int K, int nw) {
-  const int groups = BACK_THREADS / 64 / nw, want = (M + groups - 1) / groups;
+  const int groups = nw < BACK_THREADS / 64 ? BACK_THREADS / 64 / nw : 1, want = (M + groups - 1) / groups;
   if (want <= 2) return 1;
   const int most = (int64_t)M * K <= (1 << 22) ? 128 : 256;
   return want < most ? want : most;
@@ -481,12 +483,13 @@ bool forward(const LayerNormArgs& a, hipStream_t stream) {
     forward_of<TX, VEC, kFew>(a, stream);
     return true;
   }
+  if (a.K > kManyK) return false;
   if constexpr (VEC > 1)
-    if (a.K <= kManyK) {
-      forward_of<TX, VEC, kMany>(a, stream);
-      return true;
-    }
-  return false;
+    forward_of<TX, VEC, kMany>(a, stream);
+  else
+    hipLaunchKernelGGL((layer_norm_kernel<TX, 1, kFew, ODD_THREADS>), dim3(a.M < 512 ? a.M : 512), dim3(ODD_THREADS), 0, stream,
+                       a, kMaxWaves);
+  return true;
 }
 
 // The number of parts written (1: straight to dw and db), 0 where the row does
@@ -494,8 +497,8 @@ bool forward(const LayerNormArgs& a, hipStream_t stream) {
 template <int TD, int TX, int VEC>
 int backward(const LayerNormBackArgs& a, float* part, hipStream_t stream) {
   const bool few = a.K <= kFewK;
-  if (!few && (VEC == 1 || a.K > kManyK)) return 0;
-  const int nw = row_waves(a.K, few ? kFew : kMany), blocks = back_blocks(a.M, a.K, nw);
+  if (a.K > kManyK) return 0;
+  const int nw = row_waves(a.K, few || VEC == 1 ? kFew : kMany), blocks = back_blocks(a.M, a.K, nw);
   float* const pw = blocks > 1 ? part : a.dw;
   float* const pb = blocks > 1 && part ? part + a.K : a.db;
   if (few) {
@@ -504,6 +507,9 @@ int backward(const LayerNormBackArgs& a, float* part, hipStream_t stream) {
   } else if constexpr (VEC > 1) {
     hipLaunchKernelGGL((norm_back_kernel<TD, TX, VEC, kMany / VEC, BACK_THREADS>), dim3(blocks), dim3(BACK_THREADS), 0,
                        stream, a, pw, pb, nw);
+  } else {
+    hipLaunchKernelGGL((norm_back_kernel<TD, TX, 1, kFew, ODD_THREADS>), dim3(blocks), dim3(ODD_THREADS), 0, stream, a, pw, pb,
+                       nw);
   }
   return blocks;
 }
@@ -520,16 +526,10 @@ int backward_of(const LayerNormBackArgs& a, float* part, hipStream_t stream) {
 
 size_t layer_norm_back_ws_bytes(int M, int K) {
   // (whatever the types and the alignment of the call)
-  size_t need = 0;
-  if (K <= kManyK)
-    need = (size_t)back_blocks(M, K, row_waves(K, K <= kFewK ? kFew : kMany)) * 2 * K * sizeof(float);
-  if (K > kFewK) {
-    int nch, rows;
-    long_plan(M, K, nch, rows);
-    const size_t n = sums_bytes(M) + (size_t)nch * 2 * K * sizeof(float);
-    need = n > need ? n : need;
-  }
-  return need;
+  if (K <= kManyK) return (size_t)back_blocks(M, K, row_waves(K, K <= kFewK ? kFew : kMany)) * 2 * K * sizeof(float);
+  int nch, rows;
+  long_plan(M, K, nch, rows);
+  return sums_bytes(M) + (size_t)nch * 2 * K * sizeof(float);
 }
 
 hipError_t launch_layer_norm(const LayerNormArgs& a, hipStream_t stream) {

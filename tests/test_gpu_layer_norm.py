@@ -83,6 +83,18 @@ def test_many_rows(M, K, dev):
     _check_backward(*_backward(dev, dy, x, w, "bf16", "f32", "bf16", "f32"), "f32")
 
 
+@pytest.mark.parametrize("dy_type,x_type", list(itertools.product(TYPES, TYPES)))
+@pytest.mark.parametrize("M,K,shift", [(1, 8193, 0), (2, 8200, 1), (3, 9445, 0), (600, 8195, 3), (2, 16383, 0), (3, 16384, 1)])
+def test_odd_rows_in_sixteen_waves(M, K, shift, dy_type, x_type, dev):
+    """Rows between 8192 and 16384 that no 16-byte access can take."""
+    say("odd rows", M, K, shift, dy_type, x_type)
+    x, w, b, dy = _inputs(M, K, 600 + K, "f32")
+    _check_forward(*_forward(dev, x, w, b, x_type, "bf16", dy_type, shift), dy_type)
+    _check_backward(*_backward(dev, dy, x, w, dy_type, x_type, "f32", x_type, shift), x_type)
+    _check_backward(*_backward(dev, dy, x, None, dy_type, x_type, "f32", x_type, shift, (False, True, True)), x_type)
+    _check_backward(*_backward(dev, dy, x, w, dy_type, x_type, "f32", x_type, shift, (True, False, False)), x_type)
+
+
 @pytest.mark.parametrize("want", [w for w in itertools.product((True, False), repeat=3) if any(w)])
 def test_each_output_is_optional(want, dev):
     say("outputs", want)
