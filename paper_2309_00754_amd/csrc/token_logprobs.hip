@@ -7,11 +7,10 @@
 //   H = ln S - W / S,  W = sum_j e^(z_j - m) (z_j - m)
 //   dz_j = d_lp ([j == token] - p_j) - d_H p_j (ln p_j + H), p_j = e^(z_j - lse)
 //
-//  * token_logp_kernel: a workgroup of 512 threads per row or segment of a long
-//    one, of 128 per row where many are short,
-//    reads it once in 16-byte groups, each thread with running sums relative to
-//    a power of two that follows its maximum; the threads meet in a fixed tree.
-//    For the alternatives it keeps the maximum of every group in LDS.
+//  * token_logp_kernel: a workgroup of 128 to 512 threads per row, or per segment
+//    of a long one, reads it once in 16-byte groups, each thread with running sums
+//    relative to a power of two that follows its maximum; the threads meet in a
+//    fixed tree.  For the alternatives it keeps the maximum of every group in LDS.
 //  * token_logp_join_kernel: one wave per row joins the segments.
 //  * token_logp_back_kernel: a workgroup per stretch of a row; rows without a
 //    gradient are filled with zeros unread.
@@ -34,7 +33,6 @@
 namespace hydra {
 namespace {
 
-constexpr int TL_THREADS = 512, TL_FEW = 128;  // threads of a row or segment, of a short row
 constexpr int TL_U = 4;             // 16-byte loads of a thread under way
 constexpr int kSegMost = 57344;     // elements of a segment (its groups' maxima, 4 bytes each, beside 6 KB in 64 KB of LDS)
 constexpr int kSegs = 64;           // segments of a row at most
@@ -757,12 +755,19 @@ int segments(int M, int V, int type) {
   return (int)(n < kSegs ? n : kSegs);
 }
 
-// Whether 128 threads take a row, not 512: rows of up to five of their rounds of
-// loads, and enough of them to fill the chip that way.  2000 fp32 logits, 400 rows
-// 3.4 us, so 3.9 with 512; 5000 bf16 with 8 alternatives, 900 rows 7.4 and 9.5;
-// 10000 fp32, 900 rows 8.2 and 9.1, 400 rows 6.9 and 5.9; 14000 with 8, 1800 rows
-// 29.7 and 22.7.  (256 threads lie between the two.)
-bool short_rows(int M, int groups) { return groups <= 2560 && M >= 256 + groups / 4; }
+// Threads of a row or segment.  128 for rows of up to five of their rounds of
+// loads, where there are enough to fill the chip that way: 2000 fp32 logits, 400
+// rows 3.4 us, so 3.9 with 512; 5000 bf16 with 8 alternatives, 900 rows 7.4 and
+// 9.5; 10000 fp32, 900 rows 8.2 and 9.1, 400 rows 6.9 and 5.9.  256 for rows of up
+// to five of theirs, or three where the logits are more than the caches turn over:
+// 1000 rows of 32000 bf16 with 20 alternatives 17.9 us, so 19.6 with 512, but 300
+// rows with 8 10.9 and 10.3; 2000 rows of 12000 fp32 with 20 21.2 and 25.4, of
+// 24000 with 8 41.6 and 37.8.
+int threads_of(int M, int groups) {
+  if (groups <= 2560 && M >= 256 + groups / 4) return 128;
+  const bool much = (int64_t)M * groups > (6 << 20);  // 96 MB
+  return M >= 400 && groups <= (much ? 3200 : 5120) ? 256 : 512;
+}
 
 size_t stat_bytes(int M, int nseg) { return ((size_t)M * nseg * sizeof(Stat) + 15) & ~size_t(15); }
 
@@ -779,10 +784,11 @@ void rows_of(const TokenLogpArgs& a, int nseg, const Parts& p, hipStream_t strea
 
 template <int T>
 void forward(const TokenLogpArgs& a, int nseg, const Parts& p, hipStream_t stream) {
-  if (short_rows(a.M, a.V / kVec<T>))
-    rows_of<T, TL_FEW>(a, nseg, p, stream);
-  else
-    rows_of<T, TL_THREADS>(a, nseg, p, stream);
+  switch (nseg == 1 ? threads_of(a.M, a.V / kVec<T>) : 512) {
+    case 128: rows_of<T, 128>(a, nseg, p, stream); break;
+    case 256: rows_of<T, 256>(a, nseg, p, stream); break;
+    default: rows_of<T, 512>(a, nseg, p, stream);
+  }
   if (nseg > 1) hipLaunchKernelGGL((token_logp_join_kernel<T>), dim3(a.M), dim3(64), 0, stream, a, nseg, p);
 }
 

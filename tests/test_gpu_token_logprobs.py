@@ -130,7 +130,7 @@ def test_ties_go_to_the_lowest_index(V, kind, dev):
 
 @pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("V,shift,top", [(1, 0, 1), (40, 1, 32), (511, 0, 0), (1003, 3, 7), (2050, 0, 32), (4099, 2, 20),
-                                         (10241, 0, 32), (10247, 5, 0)])
+                                         (10241, 0, 32), (10247, 5, 0), (12290, 0, 32), (16005, 1, 5), (19999, 0, 0)])
 def test_rows_of_every_sort_many_times(V, shift, top, kind, dev):
     """Short rows in numbers: each sort against the oracle, its repetitions to the bit."""
     import torch
@@ -146,7 +146,7 @@ def test_rows_of_every_sort_many_times(V, shift, top, kind, dev):
     z[12] += 4.0e6
     z[13, ::2] = -INF
     tokens = list(r.integers(0, V, 13)) + [V]
-    n = 64 if V < 3000 else 80
+    n = 64 if V < 3000 else 80 if V < 11000 else 32
     zt = put(np.tile(z, (n, 1)), kind, dev, shift, (V + 15) // 8 * 8)
     M = zt.shape[0]
     tok = torch.tensor(tokens * n, dtype=torch.int32, device=dev)
