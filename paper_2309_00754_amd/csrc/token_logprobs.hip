@@ -33,8 +33,10 @@
 namespace hydra {
 namespace {
 
-constexpr int TL_U = 4;             // 16-byte loads of a thread under way
-constexpr int kSegMost = 57344;     // elements of a segment (its groups' maxima, 4 bytes each, beside 6 KB in 64 KB of LDS)
+// 16-byte loads of a thread under way (2: 900 x 40000 fp32 with 16 alternatives
+// 38.4 us, so 33.2; 8: 1500 x 50272 bf16 with 8 alternatives 38.7, so 33.9).
+constexpr int TL_U = 4;
+constexpr int kSegMost = 57344;     // elements of a segment (its groups' maxima, 4 bytes each, beside 7 KB in 64 KB of LDS)
 constexpr int kSegs = 64;           // segments of a row at most
 constexpr int kCand = 576;          // logits ranked by counting at most
 
@@ -464,7 +466,7 @@ __global__ __launch_bounds__(THREADS) void token_logp_kernel(TokenLogpArgs a, in
   if constexpr (TOP) {
     if (waves > 0) bound = bound_of[0];
     for (int i = 1; i < waves; ++i) bound = fminf(bound, bound_of[i]);
-    constexpr int U = 4;  // (loads from LDS under way; with 8, 4000 rows of 5000 took 28.1 us, not 26.7)
+    constexpr int U = 4;  // (loads from LDS under way; with 8, 4000 x 5000 fp32 with 8 alternatives 21.1 us, not 20.8)
     for (int g0 = t; g0 < groups; g0 += THREADS * U) {
       float x[U];
 #pragma unroll
