@@ -328,3 +328,35 @@ def test_alternatives_of_another_shape_are_refused(dev):
             H.hydra_token_logprobs(z, tok, lp, top_ids=ids)
     with pytest.raises(TypeError):
         H.hydra_token_logprobs(z, tok, lp, top_ids=[1, 2, 3, 4])
+
+
+def test_rows_in_segments_in_a_hip_graph(dev):
+    """Few long rows take two launches and a workspace: replays, with other eager calls on the same workspace between."""
+    import torch
+    say("segments in a graph")
+    rows, vocabulary, top = 3, 70000, 20
+    r = np.random.default_rng(9)
+    z, z2 = (put(r.normal(0, 2, (rows, vocabulary)), "f32", dev) for _ in range(2))
+    tok = torch.tensor([5, 69999, 40000], dtype=torch.int32, device=dev)
+    ws = torch.full((H.hydra_token_logprobs_workspace_bytes(rows, vocabulary, top),), 0xFF, dtype=torch.uint8, device=dev)
+
+    def outputs():
+        return [torch.empty(rows, device=dev) for _ in range(3)] + [
+            torch.empty((rows, top), dtype=torch.int32, device=dev), torch.empty((rows, top), device=dev)]
+
+    want, got, other = outputs(), outputs(), outputs()
+    H.hydra_token_logprobs(z, tok, *want, ws)
+    torch.cuda.synchronize()
+    graphs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()]
+    for g, w in zip(graphs, (ws, None)):
+        with torch.cuda.graph(g):
+            H.hydra_token_logprobs(z, tok, *got, w)
+    for _ in range(3):
+        for g in graphs:
+            for t in got:
+                t.fill_(-5)
+            H.hydra_token_logprobs(z2, tok, *other, ws)
+            torch.cuda.synchronize()
+            g.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
