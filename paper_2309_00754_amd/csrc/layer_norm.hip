@@ -210,23 +210,45 @@ __global__ __launch_bounds__(THREADS) void norm_back_kernel(LayerNormBackArgs a,
 #pragma unroll
     for (int e = 0; e < VEC; ++e) dw[c][e] = db[c][e] = 0.f;
   const float inv_k = 1.f / (float)K;
+  // the next row's loads before this row's sums meet, where registers allow it: 4096
+  // x 4096 bf16 30.2 us without, so 26.9; 4096 x 2048 fp32 26.9 and 25.1; 2000 x 11008
+  // bf16 43.4 and 37.8 (with fp32 at 32 columns a lane it spills: 64.5, so 122)
+  constexpr bool AHEAD = (NCH * VEC <= 16 || VEC == 8) && THREADS <= 512;
   const int per = gridDim.x * groups;
   int turn = 0;
-  for (int r0 = blockIdx.x * groups; r0 < a.M; r0 += per, turn ^= 1) {
-    const int row = r0 + group;
+  Chunk<TD, VEC> dn[NCH];
+  Chunk<TX, VEC> xn[NCH];
+  float mean_n = 0.f, rstd_n = 0.f;
+  const auto fetch = [&](int row) __attribute__((always_inline)) {
     const bool live = row < a.M;
     const size_t at = (size_t)(live ? row : 0) * K;
     const __amdgpu_buffer_rsrc_t dr = make_rsrc(static_cast<const uint8_t*>(a.dy) + at * DB, live ? (uint32_t)K * DB : 0u);
     const __amdgpu_buffer_rsrc_t xr = make_rsrc(static_cast<const uint8_t*>(a.x) + at * XB, live ? (uint32_t)K * XB : 0u);
-    Chunk<TD, VEC> d[NCH];
-    Chunk<TX, VEC> x[NCH];
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
       const int k = k0 + c * step;
-      d[c].load(dr, k < K ? k * DB : kOutOfRange);
-      x[c].load(xr, k < K ? k * XB : kOutOfRange);
+      dn[c].load(dr, k < K ? k * DB : kOutOfRange);
+      xn[c].load(xr, k < K ? k * XB : kOutOfRange);
     }
-    const float mean = live ? a.mean[row] : 0.f, rstd = live ? a.rstd[row] : 0.f;
+    mean_n = live ? a.mean[row] : 0.f;
+    rstd_n = live ? a.rstd[row] : 0.f;
+  };
+  if constexpr (AHEAD) fetch(blockIdx.x * groups + group);
+  for (int r0 = blockIdx.x * groups; r0 < a.M; r0 += per, turn ^= 1) {
+    const int row = r0 + group;
+    const bool live = row < a.M;
+    const size_t at = (size_t)(live ? row : 0) * K;
+    if constexpr (!AHEAD) fetch(row);
+    Chunk<TD, VEC> dc[NCH];
+    Chunk<TX, VEC> xc[NCH];
+    if constexpr (AHEAD) {
+#pragma unroll
+      for (int c = 0; c < NCH; ++c) dc[c] = dn[c], xc[c] = xn[c];
+    }
+    const Chunk<TD, VEC>* const d = AHEAD ? dc : dn;
+    const Chunk<TX, VEC>* const x = AHEAD ? xc : xn;
+    const float mean = mean_n, rstd = rstd_n;
+    if (AHEAD && r0 + per < a.M) fetch(row + per);
     // (columns past K have dy = 0)
     float s0 = 0.f, s1 = 0.f;
 #pragma unroll
@@ -419,7 +441,7 @@ __global__ __launch_bounds__(COL_THREADS) void norm_back_cols_kernel(LayerNormBa
 // (14.6; 15.3 to 17.7), backward 32.7 (32.6; 38.1).  32 for rows of up to
 // 16384.  Element by element (rows of odd length or alignment) 16 alone, in 16
 // waves above 8192: a chunk's address takes a register too, and 32 spill (of 16
-// the backward keeps some 30 in scratch memory there, yet 3552 x 9445 fp32 takes 106
+// the backward keeps some 30 in scratch memory there, yet 3552 x 9445 fp32 takes 116
 // us, where the long rows' kernels take 198; bf16 81 and 251; forward 65 and 115).
 constexpr int kFew = 16, kMany = 32;
 constexpr int kFewK = 8 * 64 * kFew, kManyK = 8 * 64 * kMany;
