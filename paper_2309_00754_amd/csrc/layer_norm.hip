@@ -456,11 +456,10 @@ int row_waves(int K, int lane) {
 
 // Workgroups of the backward.  Each writes a part of dw and db that
 // norm_back_sum_kernel reads again: one a CU, half as many where the rows are
-// few (M K up to 2^22: 700 x 2048 fp32 and bf16 11.3 us, so 11.8; 700 x 4096 bf16
-// 13.9, so 15.4; but 4096 x 4096 42.3, so 30.4), and a single one, which needs no
-// second launch, where that takes it two rounds of rows at most (8 x 2048: 7.7 us
-// with the launch).  Workgroups of 1024 threads gain up to 6% on much bf16 (8192
-// x 4096 47.1 us, so 50.2) and lose as much on fp32 (86.6, so 81.0) and few rows.
+// few (M K up to 2^22: 1500 x 2048 fp32 13.0 us, so 13.5; but 3000 x 2048 18.8, so
+// 17.9, 4096 x 2048 27.2 and 24.9), and a single one, which needs no second
+// launch, where that takes it two rounds of rows at most (8 x 2048: 7.7 us with
+// the launch).
 int back_blocks(int M, int K, int nw) {
   const int groups = nw < BACK_THREADS / 64 ? BACK_THREADS / 64 / nw : 1, want = (M + groups - 1) / groups;
   if (want <= 2) return 1;
