@@ -727,8 +727,10 @@ hydra_status hydra_grad_norm(int64_t n, const void* const* grads, const int32_t*
  *             c is 1 then, so that a program can leave the step out
  * c is formed in 64 bits and rounded to fp32; each product is rounded once.
  * Where c is 1, gradients in place are not written.  A tensor that is
- * written may not overlap another tensor that is written or read, `norm` or `err_flag`
- * (HYDRA_ERR_SHAPE): neither may a gradient stand in the list twice.
+ * written may not overlap another tensor that is written or read
+ * (HYDRA_ERR_SHAPE): neither may a gradient that is scaled in place stand in the
+ * list twice.  `norm` and `err_flag` may not lie in a tensor that is written or
+ * read (HYDRA_ERR_SHAPE).
  */
 hydra_status hydra_grad_clip(int64_t n, const void* const* grads, const int32_t* types, const int64_t* numels,
                              float max_norm, float* norm, void* const* outs, const int32_t* out_types,

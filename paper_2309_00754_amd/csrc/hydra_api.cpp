@@ -1052,7 +1052,8 @@ struct Range {
   uintptr_t lo, hi;
 };
 
-// Whether the written tensors are apart from each other and from what is read.
+// Whether the written tensors are apart from each other and from what is read,
+// and the extra ranges (written too) from both.
 // The usual lists pass in one sweep: written ranges in ascending order (the
 // views of one buffer, or buffers allocated in turn) that lie wholly on one
 // side of what is read, or are what is read.  Others are sorted (on the stack:
@@ -1087,8 +1088,16 @@ bool written_apart(int64_t n, const void* const* grads, const int32_t* types, co
       if (!but || p->lo != but->lo || p->hi != but->hi) return true;
     return false;
   };
-  for (int i = 0; i < n_extra; ++i)
-    if (extra[i].lo && hits(extra[i].lo, extra[i].hi, nullptr)) return false;
+  for (int i = 0; i < n_extra; ++i) {
+    const Range& x = extra[i];
+    if (!x.lo) continue;
+    if (hits(x.lo, x.hi, nullptr)) return false;
+    // (the scaling may still read what is only read when it writes these)
+    for (int64_t k = 0; !in_place && x.lo < r_hi && x.hi > r_lo && k < n; ++k) {
+      const uintptr_t g = reinterpret_cast<uintptr_t>(grads[k]);
+      if (numels[k] > 0 && x.lo < g + uintptr_t(numels[k]) * type_align(types[k]) && x.hi > g) return false;
+    }
+  }
   if (in_place || nw == 0 || w[nw - 1].hi <= r_lo || w[0].lo >= r_hi) return true;
   for (int64_t i = 0; i < n; ++i) {
     if (numels[i] == 0) continue;
