@@ -59,17 +59,13 @@ struct GradSegs {
   }
   __device__ __forceinline__ int g_type(int i) const { return (last[i] >> kLogChunk) & 1; }
   __device__ __forceinline__ int out_type(int i) const { return (last[i] >> (kLogChunk + 1)) & 1; }
-  // The next runs, from `r` on; returns how many.
-  int fill(const Run* r, int64_t left) {
-    chunk0[0] = 0;
-    for (n = 0; n < N && n < left; ++n) {
-      g[n] = r[n].g;
-      if constexpr (OUT) out[n] = r[n].out;
-      chunk0[n + 1] = chunk0[n] + (int)((r[n].numel + (int64_t(1) << kLogChunk) - 1) >> kLogChunk);
-      last[n] = (uint16_t)(((r[n].numel - 1) & ((1 << kLogChunk) - 1)) | r[n].g_type << kLogChunk |
-                           r[n].out_type << (kLogChunk + 1));
-    }
-    return n;
+  // Run n.
+  void add(const Run& r) {
+    g[n] = r.g;
+    if constexpr (OUT) out[n] = r.out;
+    chunk0[n + 1] = chunk0[n] + (int)((r.numel + (int64_t(1) << kLogChunk) - 1) >> kLogChunk);
+    last[n] = (uint16_t)(((r.numel - 1) & ((1 << kLogChunk) - 1)) | r.g_type << kLogChunk |
+                         r.out_type << (kLogChunk + 1));
   }
   __host__ __device__ int chunks() const { return chunk0[n]; }
 };
@@ -261,24 +257,47 @@ __global__ __launch_bounds__(GN_THREADS) void grad_scale_kernel(ScaleSegs s, con
   });
 }
 
-// The list as runs (empty tensors left out, tensors side by side joined).
-int join(const GradArgs& a, Run* runs) {
+// The list as runs: empty tensors left out, tensors side by side joined.  Kept as
+// the runs' first tensors, 8 KB of the caller's stack (the library allocates
+// nothing; the runs themselves would be 128 KB).
+struct Runs {
+  const GradArgs& a;
   int n = 0;
-  for (int64_t i = 0; i < a.n; ++i) {
-    if (a.numels[i] == 0) continue;
-    const int gt = a.types[i], ot = a.outs ? a.out_types[i] : gt;
-    void* const out = a.outs ? a.outs[i] : const_cast<void*>(a.g[i]);
-    if (n > 0) {
-      Run& p = runs[n - 1];
-      if (p.g_type == gt && p.out_type == ot && static_cast<const uint8_t*>(p.g) + p.numel * type_bytes(gt) == a.g[i] &&
-          static_cast<uint8_t*>(p.out) + p.numel * type_bytes(ot) == out) {
-        p.numel += a.numels[i];
+  uint16_t first[kMaxGrads];
+
+  explicit Runs(const GradArgs& args) : a(args) {
+    Run p{};
+    for (int64_t i = 0; i < a.n; ++i) {
+      if (a.numels[i] == 0) continue;
+      const Run t = tensor(i);
+      if (n > 0 && p.g_type == t.g_type && p.out_type == t.out_type &&
+          static_cast<const uint8_t*>(p.g) + p.numel * type_bytes(p.g_type) == t.g &&
+          static_cast<uint8_t*>(p.out) + p.numel * type_bytes(p.out_type) == t.out) {
+        p.numel += t.numel;
         continue;
       }
+      p = t;
+      first[n++] = (uint16_t)i;
     }
-    runs[n++] = Run{a.g[i], out, a.numels[i], gt, ot};
   }
-  return n;
+  Run tensor(int64_t i) const {
+    const int gt = a.types[i];
+    return Run{a.g[i], a.outs ? a.outs[i] : const_cast<void*>(a.g[i]), a.numels[i], gt, a.outs ? a.out_types[i] : gt};
+  }
+  Run operator[](int r) const {
+    Run p = tensor(first[r]);
+    for (int64_t i = first[r] + 1, end = r + 1 < n ? first[r + 1] : a.n; i < end; ++i) p.numel += a.numels[i];
+    return p;
+  }
+};
+static_assert(kMaxGrads <= 1 << 16, "tensors by 16-bit numbers");
+
+// The launch's runs, from run `r0` on; returns how many.
+template <class Segs>
+int fill(Segs& s, const Runs& runs, int r0) {
+  s.chunk0[0] = 0;
+  for (s.n = 0; s.n < Segs::kMost && r0 + s.n < runs.n; ++s.n) s.add(runs[r0 + s.n]);
+  return s.n;
 }
 
 }  // namespace
@@ -287,14 +306,14 @@ size_t grad_ws_bytes() { return kMaxParts * sizeof(double); }
 
 hipError_t launch_grad_norm(const GradArgs& a, void* ws, hipStream_t stream) {
   double* part = static_cast<double*>(ws);
-  Run runs[kMaxGrads];  // (on the stack: the library allocates nothing)
-  const int n = join(a, runs);
+  const Runs runs(a);
+  const int n = runs.n;
   const int sums = (n + SumSegs::kMost - 1) / SumSegs::kMost;
   const int most = sums > 2 ? kMaxParts / sums : kWorkgroups;
   int parts = 0;
   SumSegs s;
   for (int r = 0; r < n;) {
-    r += s.fill(runs + r, n - r);
+    r += fill(s, runs, r);
     const int grid = s.chunks() < most ? s.chunks() : most;
     hipLaunchKernelGGL(grad_sum_kernel, dim3(grid), dim3(GN_THREADS), 0, stream, s, part + parts);
     parts += grid;
@@ -305,7 +324,7 @@ hipError_t launch_grad_norm(const GradArgs& a, void* ws, hipStream_t stream) {
   }
   ScaleSegs o;
   for (int l = (n - 1) / ScaleSegs::kMost; l >= 0; --l) {
-    o.fill(runs + l * ScaleSegs::kMost, n - l * ScaleSegs::kMost);
+    fill(o, runs, l * ScaleSegs::kMost);
     const int grid = o.chunks() < kWorkgroups ? o.chunks() : kWorkgroups;
     hipLaunchKernelGGL(grad_scale_kernel, dim3(grid), dim3(GN_THREADS), 0, stream, o, part, parts, a.max_norm,
                        l == 0 ? a.norm : nullptr, a.err);

@@ -1052,40 +1052,49 @@ struct Range {
   uintptr_t lo, hi;
 };
 
+Range range_of(const void* p, int64_t numel, int type) {
+  const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
+  return {lo, lo + uintptr_t(numel) * type_align(type)};
+}
+
 // Whether the written tensors are apart from each other and from what is read,
 // and the extra ranges (written too) from both.
 // The usual lists pass in one sweep: written ranges in ascending order (the
 // views of one buffer, or buffers allocated in turn) that lie wholly on one
-// side of what is read, or are what is read.  Others are sorted (on the stack:
-// the library allocates nothing).
+// side of what is read, or are what is read.  Others are sorted, by their
+// numbers (8 KB of the caller's stack: the library allocates nothing).
 bool written_apart(int64_t n, const void* const* grads, const int32_t* types, const int64_t* numels, void* const* outs,
                    const int32_t* out_types, const Range* extra, int n_extra) {
-  Range w[HYDRA_MAX_GRADS];
+  static_assert(HYDRA_MAX_GRADS <= 1 << 16, "tensors by 16-bit numbers");
+  uint16_t w[HYDRA_MAX_GRADS];
+  const auto read = [&](int64_t i) { return range_of(grads[i], numels[i], types[i]); };
+  const auto written = [&](int64_t i) { return outs ? range_of(outs[i], numels[i], out_types[i]) : read(i); };
   int nw = 0;
   bool ascending = true, in_place = true;
-  uintptr_t r_lo = ~uintptr_t(0), r_hi = 0;
+  uintptr_t r_lo = ~uintptr_t(0), r_hi = 0, end = 0;
   for (int64_t i = 0; i < n; ++i) {
     if (numels[i] == 0) continue;
-    const uintptr_t g = reinterpret_cast<uintptr_t>(grads[i]), o = outs ? reinterpret_cast<uintptr_t>(outs[i]) : g;
-    const int ot = outs ? out_types[i] : types[i];
-    const uintptr_t g_end = g + uintptr_t(numels[i]) * type_align(types[i]);
-    in_place = in_place && o == g && ot == types[i];
-    r_lo = g < r_lo ? g : r_lo;
-    r_hi = g_end > r_hi ? g_end : r_hi;
-    w[nw] = {o, o + uintptr_t(numels[i]) * type_align(ot)};
-    ascending = ascending && (nw == 0 || w[nw].lo >= w[nw - 1].hi);
-    ++nw;
+    const Range g = read(i), o = written(i);
+    in_place = in_place && o.lo == g.lo && o.hi == g.hi;
+    r_lo = g.lo < r_lo ? g.lo : r_lo;
+    r_hi = g.hi > r_hi ? g.hi : r_hi;
+    ascending = ascending && o.lo >= end;
+    end = o.hi;
+    w[nw++] = uint16_t(i);
   }
   if (!ascending) {
-    std::sort(w, w + nw, [](const Range& a, const Range& b) { return a.lo < b.lo; });
+    std::sort(w, w + nw, [&](uint16_t a, uint16_t b) { return written(a).lo < written(b).lo; });
     for (int i = 1; i < nw; ++i)
-      if (w[i].lo < w[i - 1].hi) return false;
+      if (written(w[i]).lo < written(w[i - 1]).hi) return false;
   }
-  // the written range that would hold the first byte at or after lo, in order
+  // whether [lo, hi) meets a written range that is not `but`
   const auto hits = [&](uintptr_t lo, uintptr_t hi, const Range* but) {
-    const Range* p = std::lower_bound(w, w + nw, lo, [](const Range& a, uintptr_t v) { return a.hi <= v; });
-    for (; p != w + nw && p->lo < hi; ++p)
-      if (!but || p->lo != but->lo || p->hi != but->hi) return true;
+    const uint16_t* p = std::lower_bound(w, w + nw, lo, [&](uint16_t i, uintptr_t v) { return written(i).hi <= v; });
+    for (; p != w + nw; ++p) {
+      const Range o = written(*p);
+      if (o.lo >= hi) break;
+      if (!but || o.lo != but->lo || o.hi != but->hi) return true;
+    }
     return false;
   };
   for (int i = 0; i < n_extra; ++i) {
@@ -1094,15 +1103,14 @@ bool written_apart(int64_t n, const void* const* grads, const int32_t* types, co
     if (hits(x.lo, x.hi, nullptr)) return false;
     // (the scaling may still read what is only read when it writes these)
     for (int64_t k = 0; !in_place && x.lo < r_hi && x.hi > r_lo && k < n; ++k) {
-      const uintptr_t g = reinterpret_cast<uintptr_t>(grads[k]);
-      if (numels[k] > 0 && x.lo < g + uintptr_t(numels[k]) * type_align(types[k]) && x.hi > g) return false;
+      const Range g = read(k);
+      if (numels[k] > 0 && x.lo < g.hi && x.hi > g.lo) return false;
     }
   }
-  if (in_place || nw == 0 || w[nw - 1].hi <= r_lo || w[0].lo >= r_hi) return true;
+  if (in_place || nw == 0 || written(w[nw - 1]).hi <= r_lo || written(w[0]).lo >= r_hi) return true;
   for (int64_t i = 0; i < n; ++i) {
     if (numels[i] == 0) continue;
-    const uintptr_t g = reinterpret_cast<uintptr_t>(grads[i]);
-    const Range own{g, g + uintptr_t(numels[i]) * type_align(types[i])};
+    const Range own = read(i);
     const bool self = outs[i] == grads[i] && out_types[i] == types[i];
     if (hits(own.lo, own.hi, self ? &own : nullptr)) return false;
   }
