@@ -129,14 +129,20 @@ __device__ __forceinline__ float group_sum(float v, float* red, int nw, int w0, 
   return v;
 }
 
-// s / K, from inv_k = 1 / K rounded: the product alone misses whole quotients by a
+// A number that is the same in every lane, in a scalar register.
+__device__ __forceinline__ float uniform(float v) {
+  return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v)));
+}
+
+// s / count, from inv_k = 1 / count rounded: the product alone misses whole quotients by a
 // step (a row of 1000 values of 1000 gets a mean of 1000.00006, and with a small
 // eps its result is not the bias), and one correction by the remainder, which is
-// exact, gives them.  16384 x 128 bf16 takes 7.4 us, 3552 x 9445 bf16 56.1 (the
-// product alone: 7.2 and 55.8; a division: 7.8 and 59.1).
-__device__ __forceinline__ float quotient(float s, int K, float inv_k) {
+// exact, gives them.  16384 x 128 bf16 forward takes 7.4 us, 3552 x 9445 57.4 (the
+// product alone: 7.2 and 56.4; a division, before both numbers were in scalar
+// registers: 7.8 and 59.1).
+__device__ __forceinline__ float quotient(float s, float count, float inv_k) {
   const float q = s * inv_k;
-  const float c = fmaf(fmaf(-q, (float)K, s), inv_k, q);
+  const float c = fmaf(fmaf(-q, count, s), inv_k, q);
   return fabsf(q) < INFINITY ? c : q;  // (of an infinite sum the remainder is no number)
 }
 
@@ -153,7 +159,7 @@ __global__ __launch_bounds__(THREADS) void layer_norm_kernel(LayerNormArgs a, in
   float w[NCH][VEC], b[NCH][VEC];
   load_vector<VEC, NCH>(a.w, a.w_type, K, k0, step, 1.f, w);
   load_vector<VEC, NCH>(a.b, a.w_type, K, k0, step, 0.f, b);
-  const float inv_k = 1.f / (float)K;
+  const float count = uniform((float)K), inv_k = uniform(1.f / (float)K);
   const int per = gridDim.x * groups;
   // (the same number of rounds for every group of the workgroup: it has barriers)
   for (int r0 = blockIdx.x * groups; r0 < a.M; r0 += per) {
@@ -172,7 +178,7 @@ __global__ __launch_bounds__(THREADS) void layer_norm_kernel(LayerNormArgs a, in
     for (int c = 0; c < NCH; ++c)
 #pragma unroll
       for (int e = 0; e < VEC; ++e) s += x[c].at(e);
-    const float mean = quotient(group_sum(s, red[0], nw, w0, wave), K, inv_k);
+    const float mean = quotient(group_sum(s, red[0], nw, w0, wave), count, inv_k);
     s = 0.f;
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
@@ -184,7 +190,7 @@ __global__ __launch_bounds__(THREADS) void layer_norm_kernel(LayerNormArgs a, in
       }
       s += k0 + c * step < K ? q : 0.f;
     }
-    const float rstd = 1.f / sqrtf(quotient(group_sum(s, red[1], nw, w0, wave), K, inv_k) + a.eps);
+    const float rstd = 1.f / sqrtf(quotient(group_sum(s, red[1], nw, w0, wave), count, inv_k) + a.eps);
     if (!live) continue;
     const __amdgpu_buffer_rsrc_t yr = make_rsrc(static_cast<uint8_t*>(a.y) + at * yb, (uint32_t)K * yb);
 #pragma unroll
@@ -220,15 +226,15 @@ __global__ __launch_bounds__(THREADS) void norm_back_kernel(LayerNormBackArgs a,
   for (int c = 0; c < NCH; ++c)
 #pragma unroll
     for (int e = 0; e < VEC; ++e) dw[c][e] = db[c][e] = 0.f;
-  const float inv_k = 1.f / (float)K;
+  const float count = uniform((float)K), inv_k = uniform(1.f / (float)K);
   // the next row's loads before this row's sums meet, where registers allow it: 4096
   // x 4096 bf16 30.2 us without, so 26.9; 4096 x 2048 fp32 26.9 and 25.1; 2000 x 11008
   // bf16 43.4 and 37.8 (with fp32 at 32 columns a lane it spills: 64.5, so 122)
   constexpr bool AHEAD = (NCH * VEC <= 16 || VEC == 8) && THREADS <= 512;
   const int per = gridDim.x * groups;
   int turn = 0;
-  Chunk<TD, VEC> dn[NCH];
-  Chunk<TX, VEC> xn[NCH];
+  Chunk<TD, VEC> dn[AHEAD ? NCH : 1];
+  Chunk<TX, VEC> xn[AHEAD ? NCH : 1];
   float mean_n = 0.f, rstd_n = 0.f;
   const auto fetch = [&](int row) __attribute__((always_inline)) {
     const bool live = row < a.M;
@@ -249,17 +255,28 @@ __global__ __launch_bounds__(THREADS) void norm_back_kernel(LayerNormBackArgs a,
     const int row = r0 + group;
     const bool live = row < a.M;
     const size_t at = (size_t)(live ? row : 0) * K;
-    if constexpr (!AHEAD) fetch(row);
-    Chunk<TD, VEC> dc[NCH];
-    Chunk<TX, VEC> xc[NCH];
+    Chunk<TD, VEC> d[NCH];
+    Chunk<TX, VEC> x[NCH];
+    float mean, rstd;
     if constexpr (AHEAD) {
 #pragma unroll
-      for (int c = 0; c < NCH; ++c) dc[c] = dn[c], xc[c] = xn[c];
+      for (int c = 0; c < NCH; ++c) d[c] = dn[c], x[c] = xn[c];
+      mean = mean_n, rstd = rstd_n;
+      if (r0 + per < a.M) fetch(row + per);
+    } else {
+      // (not by fetch: 3552 x 9445 fp32 takes 116 us by a function, whose chunks' offsets are
+      // formed anew for the stores, 107 here)
+      const __amdgpu_buffer_rsrc_t dr = make_rsrc(static_cast<const uint8_t*>(a.dy) + at * DB, live ? (uint32_t)K * DB : 0u);
+      const __amdgpu_buffer_rsrc_t xr = make_rsrc(static_cast<const uint8_t*>(a.x) + at * XB, live ? (uint32_t)K * XB : 0u);
+#pragma unroll
+      for (int c = 0; c < NCH; ++c) {
+        const int k = k0 + c * step;
+        d[c].load(dr, k < K ? k * DB : kOutOfRange);
+        x[c].load(xr, k < K ? k * XB : kOutOfRange);
+      }
+      mean = live ? a.mean[row] : 0.f;
+      rstd = live ? a.rstd[row] : 0.f;
     }
-    const Chunk<TD, VEC>* const d = AHEAD ? dc : dn;
-    const Chunk<TX, VEC>* const x = AHEAD ? xc : xn;
-    const float mean = mean_n, rstd = rstd_n;
-    if (AHEAD && r0 + per < a.M) fetch(row + per);
     // (columns past K have dy = 0)
     float s0 = 0.f, s1 = 0.f;
 #pragma unroll
@@ -289,8 +306,8 @@ __global__ __launch_bounds__(THREADS) void norm_back_kernel(LayerNormBackArgs a,
       }
     }
     if (!live) continue;
-    s0 = quotient(s0, K, inv_k);
-    s1 = quotient(s1, K, inv_k);
+    s0 = quotient(s0, count, inv_k);
+    s1 = quotient(s1, count, inv_k);
     const __amdgpu_buffer_rsrc_t orr = make_rsrc(static_cast<uint8_t*>(a.dx) + at * ob, (uint32_t)K * ob);
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
@@ -452,7 +469,7 @@ __global__ __launch_bounds__(COL_THREADS) void norm_back_cols_kernel(LayerNormBa
 // (14.6; 15.3 to 17.7), backward 32.7 (32.6; 38.1).  32 for rows of up to
 // 16384.  Element by element (rows of odd length or alignment) 16 alone, in 16
 // waves above 8192: a chunk's address takes a register too, and 32 spill (of 16
-// the backward keeps some 30 in scratch memory there, yet 3552 x 9445 fp32 takes 116
+// the backward keeps some 30 in scratch memory there, yet 3552 x 9445 fp32 takes 107
 // us, where the long rows' kernels take 198; bf16 81 and 251; forward 65 and 115).
 constexpr int kFew = 16, kMany = 32;
 constexpr int kFewK = 8 * 64 * kFew, kManyK = 8 * 64 * kMany;
