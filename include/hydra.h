@@ -674,9 +674,12 @@ hydra_status hydra_token_logprobs(const void* logits, hydra_dtype logits_type, i
  * At least one of d_lp and d_entropy (HYDRA_ERR_NULL).  A row whose upstream
  * gradients are both 0 (a prompt token, padding) gets zeros, whatever its
  * logits, token and statistics hold; another row of -inf alone gets NaN.  p_j
- * goes by the lse given: where that has
- * lost ln V to its rounding (a row of logits near the type's lowest value alone)
- * the p_j do not add up to 1.  Products are fp32, each gradient rounded once, to
+ * goes by the lse given, one fp32: half a step of it, up to 2^-24 |lse|, makes
+ * every p_j of the row larger or smaller by the factor e^(2^-24 |lse|) at most
+ * (2.4e-4 at 4096, 6% at 2^20) and shifts ln p_j by as much; where it has lost
+ * ln V (a row of logits near the type's lowest value alone) the p_j are not
+ * probabilities any more.  Logits with such an offset in common are to be shifted
+ * before both calls.  Products are fp32, each gradient rounded once, to
  * nearest even.  Sizes, alignment and overlaps as in hydra_token_logprobs.
  */
 hydra_status hydra_token_logprobs_backward(const void* logits, hydra_dtype logits_type, int64_t ld,
