@@ -516,14 +516,15 @@ bool aligned16(std::initializer_list<const void*> ps) {
 template <int TX, int VEC, int LANE>
 void forward_of(const LayerNormArgs& a, hipStream_t stream) {
   const int nw = row_waves(a.K, LANE);
-  if (nw <= FWD_THREADS / 64) {
-    const int groups = FWD_THREADS / 64 / nw, want = (a.M + groups - 1) / groups;
-    hipLaunchKernelGGL((layer_norm_kernel<TX, VEC, LANE / VEC, FWD_THREADS>), dim3(want < 1024 ? want : 1024),
-                       dim3(FWD_THREADS), 0, stream, a, nw);
-  } else {
-    hipLaunchKernelGGL((layer_norm_kernel<TX, VEC, LANE / VEC, 512>), dim3(a.M < 512 ? a.M : 512), dim3(512), 0, stream, a,
-                       nw);
+  if constexpr (LANE == kFew) {  // (of 32 columns a lane rows have 8 waves)
+    if (nw <= FWD_THREADS / 64) {
+      const int groups = FWD_THREADS / 64 / nw, want = (a.M + groups - 1) / groups;
+      hipLaunchKernelGGL((layer_norm_kernel<TX, VEC, LANE / VEC, FWD_THREADS>), dim3(want < 1024 ? want : 1024),
+                         dim3(FWD_THREADS), 0, stream, a, nw);
+      return;
+    }
   }
+  hipLaunchKernelGGL((layer_norm_kernel<TX, VEC, LANE / VEC, 512>), dim3(a.M < 512 ? a.M : 512), dim3(512), 0, stream, a, nw);
 }
 
 template <int TX, int VEC>
