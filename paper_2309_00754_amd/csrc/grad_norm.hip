@@ -11,16 +11,17 @@
 //    the same c), then scales its share.  The shares run backwards, so that the
 //    first to be read are what the sums read last and the memory-side cache
 //    (256 MB) still holds, and neither these last reads nor the results take
-//    its place: every adapter of OPT-1.3b at rank 128 (453 MB) 283 us, with the
-//    results past the cache 265, backwards 254, with the reads too 229; of
-//    Llama-7B at rank 16 into bf16 (160 MB) 92, 83, 82, 79.  The sums alone run
-//    at 5.3 TB/s.
+//    its place.  Every adapter of OPT-1.3b at rank 128 (453 MB) in place: 223 us,
+//    forwards 235, with the reads through the cache 281, with the results 276;
+//    into others 222, 222, 254 and 275; of Llama-7B at rank 16 into bf16 (160 MB,
+//    which the cache holds) 70, 66, 72 and 89.  The sums alone run at 5.1 TB/s
+//    (those 160 MB) to 5.6 (453 MB).
 // Pointers and sizes travel as kernel arguments, 256 runs a launch of the sums
 // and 176 of the scaling; tensors that lie side by side, as views of one buffer
 // do, are one run.  A workgroup
 // takes an equal share of a launch's chunks, one stretch of them: chunks dealt
-// in turn, each with its own search for the tensor and its own wait, took 303
-// us where this takes 283.
+// in turn, each with its own search for the tensor and its own wait, took the 453
+// MB 7% longer.
 // Squares are formed and added in 64 bits: an fp32 square of a gradient below
 // 1e-19 or above 1e19 would leave the range, and the conversion and the 64-bit
 // FMA run beside the loads.

@@ -228,8 +228,8 @@ __global__ __launch_bounds__(THREADS) void norm_back_kernel(LayerNormBackArgs a,
     for (int e = 0; e < VEC; ++e) dw[c][e] = db[c][e] = 0.f;
   const float count = uniform((float)K), inv_k = uniform(1.f / (float)K);
   // the next row's loads before this row's sums meet, where registers allow it: 4096
-  // x 4096 bf16 30.2 us without, so 26.9; 4096 x 2048 fp32 26.9 and 25.1; 2000 x 11008
-  // bf16 43.4 and 37.8 (with fp32 at 32 columns a lane it spills: 64.5, so 122)
+  // x 4096 bf16 27.2 us, 31.0 without; 4096 x 2048 fp32 24.9, 26.6 without; 2000 x 11008
+  // bf16 38.8, 43.9 without (fp32 at 32 columns a lane spills with it: 122, 64.5 without)
   constexpr bool AHEAD = (NCH * VEC <= 16 || VEC == 8) && THREADS <= 512;
   const int per = gridDim.x * groups;
   int turn = 0;
@@ -464,13 +464,14 @@ __global__ __launch_bounds__(COL_THREADS) void norm_back_cols_kernel(LayerNormBa
 
 // ---- plans
 
-// Columns per lane.  16 as far as 8 waves reach: 4096 x 4096 fp32 forward 26.9
-// us (32: 28.9; 8: 26.4 to 27.7), backward 46.6 (51.1; 49.9); bf16 forward 13.8
-// (14.6; 15.3 to 17.7), backward 32.7 (32.6; 38.1).  32 for rows of up to
-// 16384.  Element by element (rows of odd length or alignment) 16 alone, in 16
-// waves above 8192: a chunk's address takes a register too, and 32 spill (of 16
-// the backward keeps some 30 in scratch memory there, yet 3552 x 9445 fp32 takes 107
-// us, where the long rows' kernels take 198; bf16 81 and 251; forward 65 and 115).
+// Columns per lane.  16 as far as 8 waves reach: 4096 x 4096 fp32 forward 26.6
+// us (of 32: 28.6; of 8: 26.3), backward 44.1 (of 32: 50.7; of 8: 43.2); bf16
+// forward 13.7 (of 32: 12.4; of 8: 18.3), backward 27.2 (of 32: 29.3; of 8: 27.7).
+// 32 for rows of up to 16384.  Element by element (rows of odd length or alignment) 16 alone, in 16
+// waves above 8192: a chunk's address takes a register too, and 32 spill.  (Of 16
+// the backward keeps 20, with two types 35, in scratch memory there; yet 3552 x 9445
+// fp32 takes 107 us, by the long rows' kernels 198; bf16 81, by those 251; the
+// forward 66, by those 115.)
 constexpr int kFew = 16, kMany = 32;
 constexpr int kFewK = 8 * 64 * kFew, kManyK = 8 * 64 * kMany;
 constexpr int FWD_THREADS = 256, BACK_THREADS = 512, ODD_THREADS = kMaxWaves * 64;
@@ -483,11 +484,14 @@ int row_waves(int K, int lane) {
 }
 
 // Workgroups of the backward.  Each writes a part of dw and db that
-// norm_back_sum_kernel reads again: one a CU, half as many where the rows are
-// few (M K up to 2^22: 1500 x 2048 fp32 13.0 us, so 13.5; but 3000 x 2048 18.8, so
-// 17.9, 4096 x 2048 27.2 and 24.9), and a single one, which needs no second
-// launch, where that takes it two rounds of rows at most (8 x 2048: 7.7 us with
-// the launch).
+// norm_back_sum_kernel reads again: one a CU, or half as many where the rows are
+// few, M K up to 2^22.  Small side, with 128 (with 256): K = 2048, 700 rows of bf16
+// 10.8 us (11.0), 1500 12.6 (12.8), of fp32 11.0 (11.2) and 13.5 (14.0); K = 4096,
+// 333 rows of bf16 11.1 (11.5), 700 12.4 (12.8), of fp32 11.7 (11.7) and 13.9
+// (14.5).  Large side, with 256 (with 128): 3000 x 2048 bf16 14.6 (16.4), fp32 18.5
+// (19.5); 1500 x 4096 14.8 (16.4) and 19.1 (20.1).  A single one, which needs no
+// second launch, where that takes it two rounds of rows at most (8 x 2048 bf16 7.3
+// us, 8.5 with the launch; but 16 x 2048, four rounds, 9.6 and 8.5).
 int back_blocks(int M, int K, int nw) {
   const int groups = nw < BACK_THREADS / 64 ? BACK_THREADS / 64 / nw : 1, want = (M + groups - 1) / groups;
   if (want <= 2) return 1;

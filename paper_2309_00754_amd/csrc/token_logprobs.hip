@@ -33,8 +33,8 @@
 namespace hydra {
 namespace {
 
-// 16-byte loads of a thread under way (2: 900 x 40000 fp32 with 16 alternatives
-// 38.4 us, so 33.2; 8: 1500 x 50272 bf16 with 8 alternatives 38.7, so 33.9).
+// 16-byte loads of a thread under way: 900 x 40000 fp32 with 16 alternatives 33.2
+// us (2: 38.3; 8: 31.6), 1500 x 50272 bf16 with 8 alternatives 34.4 (2: 37.3; 8: 38.6).
 constexpr int TL_U = 4;
 constexpr int kSegMost = 57344;     // elements of a segment (its groups' maxima, 4 bytes each, beside 7 KB in 64 KB of LDS)
 constexpr int kSegs = 64;           // segments of a row at most
@@ -603,7 +603,7 @@ __global__ __launch_bounds__(64) void token_logp_join_kernel(TokenLogpArgs a, in
   if (nseg * k > 64) {
     // of many, what reaches a bound that k keys reach: the greatest of the
     // segments' k-th keys or the least of their j-th, j = k over the segments
-    // (8 segments of 32 keys: of the first alone 13.2 us)
+    // (6 x 50272 fp32, 8 segments of 32 keys: 12.1 us; by the first alone 20.0)
     const int j = (k + nseg - 1) / nseg;
     uint64_t most = lane < nseg ? pk[lane * k + k - 1] : 0, least = lane < nseg ? pk[lane * k + j - 1] : ~0ull;
 #pragma unroll
@@ -630,7 +630,7 @@ __global__ __launch_bounds__(64) void token_logp_join_kernel(TokenLogpArgs a, in
 
 constexpr int64_t kCacheBytes = int64_t(256) << 20;  // the memory-side cache
 constexpr int TB_THREADS = 256;
-constexpr int TB_U = 2;  // (4: 2048 x 32000 56.5 us, so 52.3; 250 x 50272 bf16 10.5 and 9.8)
+constexpr int TB_U = 2;  // (2048 x 32000 fp32 into bf16 48.4 us, with 4 50.4; 250 x 50272 bf16 9.8 and 10.5)
 
 template <bool FAR, class V>
 __device__ __forceinline__ V fetch(const V* p) {
@@ -645,15 +645,15 @@ __device__ __forceinline__ void put(V* p, V v) {
 }
 
 // FAR: past the caches, for logits and gradient that they cannot hold together
-// anyway (2048 x 32000 fp32 into bf16, 393 MB: 47.6 us, so 52.3; but 250 x 50272
-// bf16, 50 MB: 11.6 and 9.8).
+// anyway (2048 x 32000 fp32 into bf16, 393 MB: 48.4 us, through them 55.2; but 250 x
+// 50272 bf16, 50 MB: 11.2, through them 9.8).
 // Stretches of `per` groups; workgroup b takes stretches b, b + gridDim.x, ...
 // of the M * n of all rows.
 template <int TZ, int TD>
 struct BackGroup {
   // 16 bytes of logits, or of the gradient where it is wider: a lane that loads 16
   // bytes and stores 32 leaves gaps in each of its two stores (2048 x 32000 bf16
-  // into fp32 with half of the rows live 102 us, so 64.5)
+  // into fp32 with half of the rows live: 102 us that way, 64.5 this way)
   static constexpr bool WIDER = TZ == kBf16 && TD == kF32;
   static constexpr int VEC = WIDER ? 4 : kVec<TZ>, U = WIDER ? 2 * TB_U : TB_U;
 };
@@ -759,12 +759,12 @@ int segments(int M, int V, int type) {
 
 // Threads of a row or segment.  128 for rows of up to five of their rounds of
 // loads, where there are enough to fill the chip that way: 2000 fp32 logits, 400
-// rows 3.4 us, so 3.9 with 512; 5000 bf16 with 8 alternatives, 900 rows 7.4 and
-// 9.5; 10000 fp32, 900 rows 8.2 and 9.1, 400 rows 6.9 and 5.9.  256 for rows of up
+// rows 3.4 us (with 512 threads 3.9); 5000 bf16 with 8 alternatives, 900 rows 7.4
+// (9.5); 10000 fp32, 900 rows 8.2 (9.1), but 400 rows 6.9 (5.9).  256 for rows of up
 // to five of theirs, or three where the logits are more than the caches turn over:
-// 1000 rows of 32000 bf16 with 20 alternatives 17.9 us, so 19.6 with 512, but 300
-// rows with 8 10.9 and 10.3; 2000 rows of 12000 fp32 with 20 21.2 and 25.4, of
-// 24000 with 8 41.6 and 37.8.
+// 1000 rows of 32000 bf16 with 20 alternatives 17.9 us (with 512 threads 19.6), but
+// 300 rows with 8 10.9 (10.3); 2000 rows of 12000 fp32 with 20 21.2 (25.4), but of
+// 24000 with 8 41.6 (37.8).
 int threads_of(int M, int groups) {
   if (groups <= 2560 && M >= 256 + groups / 4) return 128;
   const bool much = (int64_t)M * groups > (6 << 20);  // 96 MB
