@@ -739,6 +739,177 @@ hydra_status hydra_grad_clip(int64_t n, const void* const* grads, const int32_t*
                              float max_norm, float* norm, void* const* outs, const int32_t* out_types,
                              void* workspace, size_t workspace_bytes, int32_t* err_flag, void* stream);
 
+/*
+ * hydra_fp8_quantize -- a matrix in 8 bits: e4m3 values (OCP: 1 sign, 4 exponent
+ * and 3 fraction bits, largest 448, no infinities) with a power-of-two scale for
+ * each block of 128 consecutive values of a row (block_rows 1: activations), or of
+ * 128 x 128 values (block_rows 128: a frozen weight).  In 8 bits the base takes
+ * half the memory of bf16, which is what Hydra-PPO keeps once for all its roles
+ * (Sec. 3).  Per block, a its largest finite magnitude:
+ *   e = the least integer >= -127 with a <= 448 2^e,  q = the e4m3 value nearest
+ *   to x 2^-e (ties to even),  scale = e + 127, one byte (E8M0).
+ *
+ *   x        [M x K] bf16 or fp32 (x_type)
+ *   q        [M x K] e4m3    out
+ *   scale    [M or ceil(M / 128) x ceil(K / 128)] bytes   out
+ *   qt       [K x M] e4m3    out, optional, block_rows 128 only: q transposed, which
+ *            hydra_fp8_lora_linear_backward reads
+ *   scale_t  [ceil(K / 128) x ceil(M / 128)] bytes   out, NULL iff qt is: scale transposed
+ * Values below 2^-10 of the scale become 0; NaN and infinities become NaN and
+ * do not count for the scale.  Requires 1 <= M, K <= 2^21 (no multiple of
+ * anything) and M ceil(K / 128) < 2^28, or ceil(M / 128) ceil(K / 128) < 2^24;
+ * x at its element's alignment (K % 8 == 0 and 16-byte aligned: faster).
+ * HYDRA_ERR_UNSUPPORTED for another block_rows, or qt with block_rows 1.
+ */
+hydra_status hydra_fp8_quantize(const void* x, hydra_dtype x_type, int64_t M, int64_t K, int64_t block_rows, uint8_t* q,
+                                uint8_t* scale, uint8_t* qt, uint8_t* scale_t, void* stream);
+
+/* hydra_fp8_lora_linear_workspace_bytes -- device workspace that hydra_fp8_lora_linear
+ * needs at most for M rows, K inputs and rank r (writes *bytes).  HYDRA_ERR_NULL for a
+ * NULL `bytes`, HYDRA_ERR_SHAPE for sizes outside that call's limits. */
+hydra_status hydra_fp8_lora_linear_workspace_bytes(int64_t M, int64_t K, int64_t r, size_t* bytes);
+
+/*
+ * hydra_fp8_lora_linear -- hydra_lora_linear over a frozen weight in 8 bits:
+ *   y_off = xh Wh^T,  y_on = xh Wh^T + s (xa A^T) B^T,
+ * xh and Wh what the bytes of the quantized x and W stand for, xa the adapter's
+ * input in bf16 (x, or x after dropout).
+ *
+ *   x         [M x K] bf16   input rows; quantized by the call as hydra_fp8_quantize
+ *             with block_rows 1 does (NULL allowed where xq is given)
+ *   x_adapter [M x K] bf16   the adapter's own input, optional (NULL: x)
+ *   xq, x_scale   x already quantized (several linears may share an input), optional
+ *   Wq, w_scale   [N x K] and [ceil(N / 128) x ceil(K / 128)]: W quantized with block_rows 128
+ *   A, B, s   as in hydra_lora_linear
+ *   y_off, y_on  [M x N] bf16 or fp32 (y_type, both)   out, each optional, at least one
+ *   workspace, workspace_bytes  device, 16-byte aligned, contents ignored and
+ *             overwritten; hydra_fp8_lora_linear_workspace_bytes(M, K, r) bytes are
+ *             always enough (less, down to NULL, where xq is given, outputs are bf16 and no update is computed)
+ * x, x_adapter, xq, Wq and A 16-byte aligned, B 2-byte, outputs at their element's
+ * alignment.  Into fp32 outputs, and up to 16 rows, every product is exact and
+ * added in fp32; into bf16 outputs of more rows the 8-bit matrix instructions run,
+ * whose sums are about 2e-5 off (a step of bf16 is 8e-3).  The update enters in
+ * fp32 up to 16 rows, above as two bf16 parts (2^-17 of s x A^T).  Outputs are
+ * rounded once, to nearest even.  A scale byte 255 stands for NaN.
+ * NaN and infinities in x make their row's outputs NaN.  With r == 0 y_on equals
+ * y_off.  Requires 1 <= M <= 2^20, 1 <= N <= 2^21, 16 <= K <= 2^21, K % 16 == 0,
+ * 0 <= r <= HYDRA_MAX_RANK, ceil(M / 128) ceil(N / 256) < 2^23; outputs distinct
+ * (HYDRA_ERR_SHAPE).  Repeated calls give the same bits.  Calls that share a
+ * workspace on different streams race.
+ */
+hydra_status hydra_fp8_lora_linear(const uint16_t* x, const uint16_t* x_adapter, const uint8_t* xq,
+                                   const uint8_t* x_scale, const uint8_t* Wq, const uint8_t* w_scale,
+                                   const uint16_t* A, const uint16_t* B, float s, int64_t M, int64_t N, int64_t K,
+                                   int64_t r, void* y_off, void* y_on, hydra_dtype y_type, void* workspace,
+                                   size_t workspace_bytes, void* stream);
+
+/* hydra_fp8_lora_linear_backward_workspace_bytes -- device workspace that
+ * hydra_fp8_lora_linear_backward needs (writes *bytes); errors as above. */
+hydra_status hydra_fp8_lora_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t r, size_t* bytes);
+
+/*
+ * hydra_fp8_lora_linear_backward -- gradients of hydra_fp8_lora_linear's y_on, with
+ * W frozen in 8 bits and dropout of probability p on the adapter's input
+ * (xa = m x, m the mask of hydra_dropout over [M x K] with the same p and rng):
+ *   dx = q(dy) Wh + m (s (dy B) A),  dA = s (dy B)^T xa,  dB = s dy^T (xa A^T),
+ * q(dy) what dy stands for after quantizing (block_rows 1).
+ *
+ *   x        [M x K] bf16   the adapter's input xa of the forward
+ *   Wqt, wt_scale   [K x N] and [ceil(K / 128) x ceil(N / 128)]: W's transpose in 8 bits
+ *            (qt and scale_t of hydra_fp8_quantize); only read when dx is wanted
+ *   A, B, s, dy   as in hydra_lora_linear_backward
+ *   p, rng   as in hydra_dropout (p == 0: no dropout, rng may be NULL)
+ *   dx       [M x K] bf16 or fp32 (dx_type)   out, optional
+ *   dA, dB   [r x K], [N x r] fp32            out, optional (ignored for r == 0)
+ *   workspace, workspace_bytes  device, 16-byte aligned, at least
+ *            hydra_fp8_lora_linear_backward_workspace_bytes(M, N, K, r) bytes,
+ *            contents ignored and overwritten
+ * The quantized x of the forward's base product counts as x itself (its
+ * rounding has no gradient).  Requires N and K multiples of 16, other limits as in
+ * hydra_fp8_lora_linear with N and K exchanged.  At least one output
+ * (HYDRA_ERR_NULL).  Every sum has a fixed order.
+ */
+hydra_status hydra_fp8_lora_linear_backward(const uint16_t* x, const uint8_t* Wqt, const uint8_t* wt_scale,
+                                            const uint16_t* A, const uint16_t* B, float s, const uint16_t* dy, int64_t M,
+                                            int64_t N, int64_t K, int64_t r, double p, const uint64_t* rng, void* dx,
+                                            hydra_dtype dx_type, float* dA, float* dB, void* workspace,
+                                            size_t workspace_bytes, void* stream);
+
+/*
+ * hydra_dropout -- dropout whose mask is never stored (on the input of an
+ * adapter; on a layer's output before it joins the residual stream):
+ *   y = residual + m x,  m = 65536 / (65536 - d) where the element is kept, else 0,
+ * d = p 65536 rounded to the nearest whole number: what is kept is scaled for the
+ * probability d / 65536 that is in force, so y's mean is x.
+ *
+ *   x        [n] bf16 or fp32 (x_type)
+ *   residual [n] bf16 or fp32 (residual_type), optional
+ *   p        0 <= p <= 1 (1: everything dropped)
+ *   rng      [2] 64-bit numbers in DEVICE memory, 8-byte aligned: seed and offset.  A
+ *            program (or a captured graph) changes the offset from call to call; the
+ *            same two numbers give the same mask.
+ *   y        [n] bf16 or fp32 (y_type): out; may be x or residual where the types are the same
+ * Element i is dropped iff its sixteen bits of Philox4x32-10 are below d: key =
+ * seed, counter = (i / 8, offset), low 64 bits first; of the block's four words element
+ * i takes word (i % 8) / 2, its lower half where i is even.  The gradient with
+ * respect to x is this call on the upstream gradient, without (or with another) residual.
+ * A dropped element does not count, be it NaN or infinite.  fp32 inside, rounded
+ * once.  Requires 1 <= n <= 2^34; element's alignment (16-byte aligned: faster).
+ */
+hydra_status hydra_dropout(const void* x, hydra_dtype x_type, const void* residual, hydra_dtype residual_type, double p,
+                           const uint64_t* rng, int64_t n, void* y, hydra_dtype y_type, void* stream);
+
+/* Most drafted tokens per sequence of hydra_verify_drafts. */
+#define HYDRA_MAX_DRAFTS 128
+
+/* hydra_verify_drafts_workspace_bytes -- device workspace that hydra_verify_drafts needs
+ * for n sequences, up to k drafts and a vocabulary of V (writes *bytes).  HYDRA_ERR_NULL
+ * for a NULL `bytes`, HYDRA_ERR_SHAPE for sizes outside that call's limits. */
+hydra_status hydra_verify_drafts_workspace_bytes(int64_t n, int64_t k, int64_t V, size_t* bytes);
+
+/*
+ * hydra_verify_drafts -- drafted tokens of a rollout against the target's
+ * probabilities, and the next token (App. A, Alg. 1 and 2, the generation step; a
+ * decode step of up to 8 rows costs one read of the weights, so the k drafts of a
+ * sequence are scored in the step that its next token needs anyway).
+ * With p_j = softmax(target row j / temperature), q_j = softmax(draft row j / temperature):
+ *   draft t_j is accepted iff u_j q_j(t_j) < p_j(t_j) and all before it are;
+ *   at the first position a that is not accepted the next token is drawn from
+ *   max(p_a - q_a, 0), after the last draft from p_a; with draft == NULL (tokens
+ *   looked up, no distribution) q_j is 1 at t_j.
+ * Drawn means: the lowest v where the running sum over 0 ... v exceeds u_k times the
+ * total.  For uniform u the tokens are distributed as the target's own samples.
+ *
+ *   target  n (k + 1) rows of V, bf16 or fp32 (target_type), row i at target + i * ld elements,
+ *           ld >= V: for sequence b rows b (k + 1) ... b (k + 1) + k, the logits of the positions
+ *           of its drafts and of the one after; -inf marks a masked-out entry
+ *   draft   n k rows of V (draft_type, ld_draft): the logits that the drafts were drawn from; optional
+ *   drafts  [n x k] int32    (NULL allowed for k == 0: one sample of each sequence's row)
+ *   lens    [n] int32, optional: how many of the k drafts a sequence has (NULL: all); rows past them are not read
+ *   u       [n x (k + 1)] fp32   random numbers in [0, 1): one for each draft, the last for the next token
+ *   temperature   > 0
+ *   accepted [n] int32           out: how many drafts are accepted
+ *   tokens  [n x (k + 1)] int32  out: the accepted drafts, the next token, then -1
+ *   lp      [n x (k + 1)] fp32   out, optional: ln p_j of those tokens (lp_old of hydra_ppo_loss at
+ *           temperature 1), 0 past the next token
+ *   workspace, workspace_bytes   device, 16-byte aligned, at least
+ *           hydra_verify_drafts_workspace_bytes(n, k, V) bytes, contents ignored and overwritten
+ *   err_flag [1] int32   optional: 1 is OR-ed in for a target row (of an accepted draft or the next token)
+ *           without a distribution (NaN, +inf, or -inf alone: the next token there is -1, its lp
+ *           NaN); for a draft outside [0, V) or with such a draft row, if the drafts before it are accepted
+ *           (it counts as no draft: the next token is drawn from p_j); for a length outside [0, k] (the nearest is taken)
+ * Exponentials and sums are 64-bit, in a fixed order; where rounding leaves nothing of
+ * p_a - q_a, the next token is drawn from p_a.  Requires n >= 1, 0 <= k <= HYDRA_MAX_DRAFTS,
+ * n (k + 1) <= 2^20, 1 <= V <= 2^21, n (2 k + 1) ceil(V / 4096) < 2^24, ld <= 2^31 - 1; logits at their
+ * element's alignment; outputs distinct (HYDRA_ERR_SHAPE).  Calls that share a workspace on
+ * different streams race.
+ */
+hydra_status hydra_verify_drafts(const void* target, hydra_dtype target_type, int64_t ld, const void* draft,
+                                 hydra_dtype draft_type, int64_t ld_draft, const int32_t* drafts, const int32_t* lens,
+                                 const float* u, int64_t n, int64_t k, int64_t V, double temperature, int32_t* accepted,
+                                 int32_t* tokens, float* lp, void* workspace, size_t workspace_bytes, int32_t* err_flag,
+                                 void* stream);
+
 /* A static, human-readable name for a status code. */
 const char* hydra_status_string(hydra_status status);
 

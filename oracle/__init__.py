@@ -1,4 +1,15 @@
 """CPU float64 oracle for the Hydra-PPO hot path (test infrastructure only; see hydra_oracle)."""
+from .base8_oracle import (  # noqa: F401
+    dequantize_ref,
+    dropout_bits_ref,
+    dropout_factor_ref,
+    e4m3_values,
+    fp8_linear_backward_ref,
+    fp8_linear_ref,
+    philox_ref,
+    quantize_ref,
+    verify_ref,
+)
 from .hydra_oracle import (  # noqa: F401
     bf16_to_f64,
     lora_linear_ref,

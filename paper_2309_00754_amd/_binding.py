@@ -37,6 +37,7 @@ HYDRA_BF16 = 0
 HYDRA_F32 = 1
 HYDRA_MAX_TOP = 32
 HYDRA_MAX_GRADS = 4096
+HYDRA_MAX_DRAFTS = 128
 HYDRA_GROUP_WS_CONTROL_BYTES = 4352
 HYDRA_GROUP_WS_BOUND_WORD = 8
 HYDRA_GROUP_WS_T_BYTES = 65536
@@ -73,6 +74,14 @@ EXPORTED = (
     "hydra_grad_norm_workspace_bytes",
     "hydra_grad_norm",
     "hydra_grad_clip",
+    "hydra_fp8_quantize",
+    "hydra_fp8_lora_linear_workspace_bytes",
+    "hydra_fp8_lora_linear",
+    "hydra_fp8_lora_linear_backward_workspace_bytes",
+    "hydra_fp8_lora_linear_backward",
+    "hydra_dropout",
+    "hydra_verify_drafts_workspace_bytes",
+    "hydra_verify_drafts",
     "hydra_status_string",
     "hydra_abi_version",
 )
@@ -156,6 +165,7 @@ def lib() -> ctypes.CDLL:
     L.hydra_lora_linear_backward.restype = ctypes.c_int
     _int, _size, _sizep = ctypes.c_int, ctypes.c_size_t, ctypes.POINTER(ctypes.c_size_t)
     _i32p, _i64p = ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_int64)
+    _f64 = ctypes.c_double
     for name, args in (
             ("hydra_layer_norm", [_vp, _int, _vp, _vp, _int, _f32, _i64, _i64, _vp, _int, _vp, _vp, _vp]),
             ("hydra_layer_norm_backward_workspace_bytes", [_i64, _i64, _sizep]),
@@ -168,7 +178,18 @@ def lib() -> ctypes.CDLL:
                                                _vp]),
             ("hydra_grad_norm_workspace_bytes", [_sizep]),
             ("hydra_grad_norm", [_i64, _pp, _i32p, _i64p, _vp, _vp, _size, _vp]),
-            ("hydra_grad_clip", [_i64, _pp, _i32p, _i64p, _f32, _vp, _pp, _i32p, _vp, _size, _vp, _vp])):
+            ("hydra_grad_clip", [_i64, _pp, _i32p, _i64p, _f32, _vp, _pp, _i32p, _vp, _size, _vp, _vp]),
+            ("hydra_fp8_quantize", [_vp, _int, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp]),
+            ("hydra_fp8_lora_linear_workspace_bytes", [_i64, _i64, _i64, _sizep]),
+            ("hydra_fp8_lora_linear", [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _f32, _i64, _i64, _i64, _i64, _vp, _vp, _int,
+                                       _vp, _size, _vp]),
+            ("hydra_fp8_lora_linear_backward_workspace_bytes", [_i64, _i64, _i64, _i64, _sizep]),
+            ("hydra_fp8_lora_linear_backward", [_vp, _vp, _vp, _vp, _vp, _f32, _vp, _i64, _i64, _i64, _i64, _f64, _vp, _vp,
+                                                _int, _vp, _vp, _vp, _size, _vp]),
+            ("hydra_dropout", [_vp, _int, _vp, _int, _f64, _vp, _i64, _vp, _int, _vp]),
+            ("hydra_verify_drafts_workspace_bytes", [_i64, _i64, _i64, _sizep]),
+            ("hydra_verify_drafts", [_vp, _int, _i64, _vp, _int, _i64, _vp, _vp, _vp, _i64, _i64, _i64, _f64, _vp, _vp, _vp,
+                                     _vp, _size, _vp, _vp])):
         getattr(L, name).argtypes = args
         getattr(L, name).restype = ctypes.c_int
     L.hydra_status_string.argtypes = [ctypes.c_int]
@@ -1068,3 +1089,226 @@ def _hydra_grad(where, grads, max_norm, norm, outs, workspace, err_flag, stream)
                                      nbytes, _ptr(err_flag), st)
 
     _launch(where, (*grads, norm, *(outs or ()), err_flag), stream, call, workspace, hydra_grad_norm_workspace_bytes())
+
+
+# ------------------------------------------------------------------ the base in 8 bits, dropout, drafted tokens
+#
+# As above, these calls go to the device that their tensors are on.
+
+def _fp8_types():
+    torch = _torch()
+    return (torch.float8_e4m3fn, torch.uint8)
+
+
+def _scale_types():
+    torch = _torch()
+    return (torch.uint8, torch.float8_e8m0fnu)
+
+
+def _blocks(n, rows=128) -> int:
+    return -(-n // rows)
+
+
+def hydra_fp8_quantize(x, q, scale, block_rows: int = 1, qt=None, scale_t=None, stream=None) -> None:
+    """e4m3 values and power-of-two scales of a matrix, 128 values of a row (block_rows 1) or 128 x 128 (block_rows 128)
+    to a scale (see include/hydra.h).
+
+    x [M,K]: bf16 (or 16-bit integer tensors holding bf16 bits) or float32; q [M,K]: float8_e4m3fn (or uint8); scale
+    [M or ceil(M/128), ceil(K/128)]: uint8 (or float8_e8m0fnu); qt [K,M], scale_t [ceil(K/128), ceil(M/128)]: the
+    transposed copy, with block_rows 128 (both optional, together).
+    """
+    st = (_nat or _native()).fp8_quantize(x, q, scale, block_rows, qt, scale_t, stream)
+    if st == _SLOW:
+        return _hydra_fp8_quantize(x, q, scale, block_rows, qt, scale_t, stream)
+    if st != HYDRA_OK:
+        _check(st, "hydra_fp8_quantize")
+
+
+def _hydra_fp8_quantize(x, q, scale, block_rows, qt, scale_t, stream) -> None:
+    _need(x, "x", _any_types())
+    M, K = x.shape
+    rows = int(block_rows)
+    if rows not in (1, 128):
+        raise ValueError(f"block_rows must be 1 or 128, got {block_rows}")
+    _need(q, "q", _fp8_types(), (M, K))
+    _need(scale, "scale", _scale_types(), (_blocks(M, rows), _blocks(K)))
+    _need(qt, "qt", _fp8_types(), (K, M))
+    _need(scale_t, "scale_t", _scale_types(), (_blocks(K), _blocks(M, rows)))
+    _launch("hydra_fp8_quantize", (x, q, scale, qt, scale_t), stream, lambda ws, n, st: lib().hydra_fp8_quantize(
+        _ptr(x), _type(x), M, K, rows, _ptr(q), _ptr(scale), _ptr(qt), _ptr(scale_t), st))
+
+
+def hydra_fp8_lora_linear_workspace_bytes(M: int, K: int, r: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().hydra_fp8_lora_linear_workspace_bytes(int(M), int(K), int(r), ctypes.byref(out)),
+           "hydra_fp8_lora_linear_workspace_bytes")
+    return int(out.value)
+
+
+def hydra_fp8_lora_linear(x, Wq, w_scale, A, B, s: float, y_off=None, y_on=None, x_adapter=None, xq=None, x_scale=None,
+                          workspace=None, stream=None) -> None:
+    """y_off = x W^T and/or y_on = x W^T + s (x_adapter A^T) B^T over a weight in 8 bits (see include/hydra.h).
+
+    x [M,K] bf16 (or 16-bit integer tensors holding bf16 bits; may be None where xq is given and x_adapter is not
+    needed or given); Wq [N,K], w_scale [ceil(N/128), ceil(K/128)] from hydra_fp8_quantize with block_rows 128; A [r,K],
+    B [N,r] bf16; y_off, y_on [M,N]: bf16 or float32, both the same (either may be None); x_adapter [M,K] bf16: the
+    adapter's own input (None: x); xq [M,K], x_scale [M, ceil(K/128)]: x already quantized.  Allocates the workspace if
+    none is given.
+    """
+    st = (_nat or _native()).fp8_lora_linear(x, Wq, w_scale, A, B, s, y_off, y_on, x_adapter, xq, x_scale, workspace,
+                                             stream)
+    if st == _SLOW:
+        return _hydra_fp8_lora_linear(x, Wq, w_scale, A, B, s, y_off, y_on, x_adapter, xq, x_scale, workspace, stream)
+    if st != HYDRA_OK:
+        _check(st, "hydra_fp8_lora_linear")
+
+
+def _hydra_fp8_lora_linear(x, Wq, w_scale, A, B, s, y_off, y_on, x_adapter, xq, x_scale, workspace, stream) -> None:
+    bf = _bf16_types()
+    if x is None and xq is None:
+        raise ValueError("x or xq is needed")
+    _need(Wq, "Wq", _fp8_types())
+    N, K = Wq.shape
+    M = (xq if x is None else x).shape[0]
+    r = 0 if A is None else A.shape[0]
+    _need(w_scale, "w_scale", _scale_types(), (_blocks(N), _blocks(K)))
+    for name, t in (("x", x), ("x_adapter", x_adapter)):
+        _need(t, name, bf, (M, K))
+    _need(xq, "xq", _fp8_types(), (M, K))
+    _need(x_scale, "x_scale", _scale_types(), (M, _blocks(K)))
+    _need(A, "A", bf, (r, K))
+    _need(B, "B", bf, (N, r))
+    for name, t in (("y_off", y_off), ("y_on", y_on)):
+        _need(t, name, _any_types(), (M, N))
+    if y_off is not None and y_on is not None and _type(y_off) != _type(y_on):
+        raise TypeError(f"y_off is {y_off.dtype}, y_on {y_on.dtype}")
+    y_type = _type(y_on if y_off is None else y_off)
+    _launch("hydra_fp8_lora_linear", (x, Wq, w_scale, A, B, y_off, y_on, x_adapter, xq, x_scale), stream,
+            lambda ws, n, st: lib().hydra_fp8_lora_linear(
+                _ptr(x), _ptr(x_adapter), _ptr(xq), _ptr(x_scale), _ptr(Wq), _ptr(w_scale), _ptr(A), _ptr(B), float(s), M,
+                N, K, r, _ptr(y_off), _ptr(y_on), y_type, ws, n, st),
+            workspace, hydra_fp8_lora_linear_workspace_bytes(M, K, r))
+
+
+def hydra_fp8_lora_linear_backward_workspace_bytes(M: int, N: int, K: int, r: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().hydra_fp8_lora_linear_backward_workspace_bytes(int(M), int(N), int(K), int(r), ctypes.byref(out)),
+           "hydra_fp8_lora_linear_backward_workspace_bytes")
+    return int(out.value)
+
+
+def hydra_fp8_lora_linear_backward(x, Wqt, wt_scale, A, B, s: float, dy, dx=None, dA=None, dB=None, p: float = 0.0,
+                                   rng=None, workspace=None, stream=None) -> None:
+    """dx, dA, dB of hydra_fp8_lora_linear's y_on, with dropout of probability p on the adapter's input (see
+    include/hydra.h).
+
+    x [M,K] bf16: the adapter's input of the forward (after dropout); Wqt [K,N], wt_scale [ceil(K/128), ceil(N/128)]: qt
+    and scale_t of hydra_fp8_quantize (needed for dx alone); A [r,K], B [N,r], dy [M,N] bf16; dx [M,K]: bf16 or float32,
+    dA [r,K], dB [N,r] float32 outputs (each optional); rng [2] int64: the forward's seed and offset, on the device.
+    Allocates the workspace if none is given.
+    """
+    st = (_nat or _native()).fp8_lora_linear_backward(x, Wqt, wt_scale, A, B, s, dy, dx, dA, dB, p, rng, workspace, stream)
+    if st == _SLOW:
+        return _hydra_fp8_lora_linear_backward(x, Wqt, wt_scale, A, B, s, dy, dx, dA, dB, p, rng, workspace, stream)
+    if st != HYDRA_OK:
+        _check(st, "hydra_fp8_lora_linear_backward")
+
+
+def _hydra_fp8_lora_linear_backward(x, Wqt, wt_scale, A, B, s, dy, dx, dA, dB, p, rng, workspace, stream) -> None:
+    torch = _torch()
+    bf = _bf16_types()
+    _need(dy, "dy", bf)
+    M, N = dy.shape
+    if A is None and x is None and Wqt is None:
+        raise ValueError("A, x or Wqt is needed")
+    K = A.shape[1] if A is not None else (x.shape[1] if x is not None else Wqt.shape[0])
+    r = 0 if A is None else A.shape[0]
+    _need(x, "x", bf, (M, K))
+    _need(Wqt, "Wqt", _fp8_types(), (K, N))
+    _need(wt_scale, "wt_scale", _scale_types(), (_blocks(K), _blocks(N)))
+    _need(A, "A", bf, (r, K))
+    _need(B, "B", bf, (N, r))
+    _need(dx, "dx", _any_types(), (M, K))
+    _need(dA, "dA", (torch.float32,), (r, K))
+    _need(dB, "dB", (torch.float32,), (N, r))
+    _need(rng, "rng", (torch.int64, torch.uint64), (2,))
+    _launch("hydra_fp8_lora_linear_backward", (x, Wqt, wt_scale, A, B, dy, dx, dA, dB, rng), stream,
+            lambda ws, n, st: lib().hydra_fp8_lora_linear_backward(
+                _ptr(x), _ptr(Wqt), _ptr(wt_scale), _ptr(A), _ptr(B), float(s), _ptr(dy), M, N, K, r, float(p), _ptr(rng),
+                _ptr(dx), _type(dx), _ptr(dA), _ptr(dB), ws, n, st),
+            workspace, hydra_fp8_lora_linear_backward_workspace_bytes(M, N, K, r))
+
+
+def hydra_dropout(x, y, p: float, rng, residual=None, stream=None) -> None:
+    """y = residual + (x scaled where it is kept, else 0), the mask from seed and offset alone (see include/hydra.h).
+
+    x, y and residual: contiguous tensors of one shape, bf16 (or 16-bit integer tensors holding bf16 bits) or float32, each
+    of its own type (y may be x or residual); rng [2] int64 on the device: seed and offset.  The gradient with respect
+    to x is the same call on dy.
+    """
+    st = (_nat or _native()).dropout(x, y, p, rng, residual, stream)
+    if st == _SLOW:
+        return _hydra_dropout(x, y, p, rng, residual, stream)
+    if st != HYDRA_OK:
+        _check(st, "hydra_dropout")
+
+
+def _hydra_dropout(x, y, p, rng, residual, stream) -> None:
+    torch = _torch()
+    _need(x, "x", _any_types())
+    if x is None or y is None:
+        raise TypeError("x and y must be torch.Tensors")
+    _need(y, "y", _any_types(), x.shape)
+    _need(residual, "residual", _any_types(), x.shape)
+    _need(rng, "rng", (torch.int64, torch.uint64), (2,))
+    _launch("hydra_dropout", (x, y, rng, residual), stream, lambda ws, n, st: lib().hydra_dropout(
+        _ptr(x), _type(x), _ptr(residual), _type(residual), float(p), _ptr(rng), x.numel(), _ptr(y), _type(y), st))
+
+
+def hydra_verify_drafts_workspace_bytes(n: int, k: int, V: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().hydra_verify_drafts_workspace_bytes(int(n), int(k), int(V), ctypes.byref(out)),
+           "hydra_verify_drafts_workspace_bytes")
+    return int(out.value)
+
+
+def hydra_verify_drafts(target, draft, drafts, u, accepted, tokens, lp=None, lens=None, temperature: float = 1.0,
+                        workspace=None, err_flag=None, stream=None) -> None:
+    """Drafted tokens against the target's probabilities, and the next token, from given random numbers (see
+    include/hydra.h).
+
+    target [n*(k+1),V], draft [n*k,V] (None: drafts without a distribution): bf16 (or 16-bit integer tensors holding
+    bf16 bits) or float32, each of its own type, rows contiguous and possibly apart; drafts [n,k] int32 (None for k = 0);
+    u [n,k+1] float32; accepted [n], tokens [n,k+1] int32, lp [n,k+1] float32 (optional) outputs; lens [n] int32: how many
+    drafts each sequence has (None: all).  Allocates the workspace if none is given.
+    """
+    st = (_nat or _native()).verify_drafts(target, draft, drafts, u, accepted, tokens, lp, lens, temperature, workspace,
+                                           err_flag, stream)
+    if st == _SLOW:
+        return _hydra_verify_drafts(target, draft, drafts, u, accepted, tokens, lp, lens, temperature, workspace, err_flag,
+                                    stream)
+    if st != HYDRA_OK:
+        _check(st, "hydra_verify_drafts")
+
+
+def _hydra_verify_drafts(target, draft, drafts, u, accepted, tokens, lp, lens, temperature, workspace, err_flag,
+                         stream) -> None:
+    torch = _torch()
+    _need(u, "u", (torch.float32,))
+    if u is None or u.dim() != 2 or u.shape[1] < 1:
+        raise ValueError("u must have the shape [n, k + 1]")
+    n, k = u.shape[0], u.shape[1] - 1
+    ld = _rows(target, "target")
+    V = target.shape[1]
+    _rows(target, "target", (n * (k + 1), V))
+    ld_d = 0 if draft is None else _rows(draft, "draft", (n * k, V))
+    _need(drafts, "drafts", (torch.int32,), (n, k))
+    for name, t, shape in (("accepted", accepted, (n,)), ("tokens", tokens, (n, k + 1)), ("lens", lens, (n,)),
+                           ("err_flag", err_flag, (1,))):
+        _need(t, name, (torch.int32,), shape)
+    _need(lp, "lp", (torch.float32,), (n, k + 1))
+    _launch("hydra_verify_drafts", (target, draft, drafts, u, accepted, tokens, lp, lens, err_flag), stream,
+            lambda ws, nb, st: lib().hydra_verify_drafts(
+                _ptr(target), _type(target), ld, _ptr(draft), _type(draft), ld_d, _ptr(drafts), _ptr(lens), _ptr(u), n, k, V,
+                float(temperature), _ptr(accepted), _ptr(tokens), _ptr(lp), ws, nb, _ptr(err_flag), st),
+            workspace, hydra_verify_drafts_workspace_bytes(n, k, V))

@@ -1,0 +1,723 @@
+// The dual-output linear over a frozen weight held in e4m3 with power-of-two
+// scales (128 values of a row of x, 128 x 128 of W):
+//   y_off = xh Wh^T,  y_on = y_off + s (x A^T) B^T,
+// xh and Wh what the bytes stand for.
+//
+// Two ways to form the base product, by where it ends:
+//  * into bf16 (above 16 rows): the scaled 8-bit matrix instructions, which take
+//    bytes and scales as they are at twice bf16's rate, and whose sums are 2e-5 off
+//    (hydra_fp8.h);
+//  * into fp32, and up to 16 rows, where reading W is what costs: bf16 matrix
+//    instructions on the exact values (four fraction bits of bf16's eight), W's
+//    bytes converted in registers, sums in fp32.
+// Kernels:
+//  * fp8_prep_kernel reads x once: its bytes and scales, or the bf16 values that
+//    they stand for, and partial sums of T = x A^T for the update;
+//  * fp8_stream_kernel (up to 16 rows) is bound by reading W: every wave takes
+//    blocks of 128 k values of 16 or more rows of W straight into registers;
+//  * fp8_gemm_kernel (more rows): tiles through LDS.
+#include <type_traits>
+
+#include "hydra_fp8.h"
+#include "hydra_philox.h"
+
+namespace hydra {
+namespace {
+
+// ------------------------------------------------------------------ before the product
+
+constexpr int P_WAVES = 4;
+
+// What sixteen bytes stand for, to memory as bf16.
+__device__ __forceinline__ void put_values(uint16_t* to, const uint4& q, int byte) {
+  uint4 v[2];
+  fp8_to_bf16(q, byte, v);
+  reinterpret_cast<uint4*>(to)[0] = v[0];
+  reinterpret_cast<uint4*>(to)[1] = v[1];
+}
+
+// 16 rows and one chunk of K a workgroup; a wave takes the chunk's blocks in
+// turn.  Lane l holds values 32 (l / 16) ... + 31 of the block of row l % 16, in
+// four pieces of eight: a block's maximum is over four lanes, its bytes are two
+// 16-byte stores a lane, and piece j of all lanes is one 16x16x32 product of T
+// (with its values of k in another order, the same for A).
+template <int RP>
+__global__ __launch_bounds__(P_WAVES * 64) void fp8_prep_kernel(Fp8PrepArgs g) {
+  constexpr int TJ = RP / 16, TJ1 = TJ > 0 ? TJ : 1;
+  const int t = threadIdx.x, lane = t & 63, l16 = lane & 15, lg = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int K = g.K, kb_n = (K + kFp8Block - 1) / kFp8Block;
+  const int m0 = blockIdx.x * 16, rows = min(16, g.M - m0);
+  const uint32_t bytes = (uint32_t)rows * K * 2u;
+  const bool quantize = g.x != nullptr, convert = g.q_in != nullptr;
+  const bool same = g.xa == g.x;
+  const __amdgpu_buffer_rsrc_t xr = make_rsrc(quantize ? g.x + (size_t)m0 * K : nullptr, quantize ? bytes : 0u);
+  const __amdgpu_buffer_rsrc_t ar = make_rsrc(TJ > 0 ? g.xa + (size_t)m0 * K : nullptr, TJ > 0 ? bytes : 0u);
+  const __amdgpu_buffer_rsrc_t Ar = make_rsrc(TJ > 0 ? g.A : nullptr, TJ > 0 ? (uint32_t)g.r * K * 2u : 0u);
+  f32x4_t acc[TJ1];
+#pragma unroll
+  for (int j = 0; j < TJ1; ++j) acc[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  const int kb1 = min(kb_n, (int)(blockIdx.y + 1) * g.kch);
+  for (int kb = blockIdx.y * g.kch + wave; kb < kb1; kb += P_WAVES) {
+    const int k = kb * kFp8Block + 32 * lg;
+    uint4 v[4], a[4];
+    uint4 w[4][TJ1];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = buf_load16(xr, k + 8 * j < K ? (l16 * K + k + 8 * j) * 2 : kOutOfRange);
+    if constexpr (TJ > 0) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bool ok = k + 8 * j < K;
+        a[j] = quantize && same ? v[j] : buf_load16(ar, ok ? (l16 * K + k + 8 * j) * 2 : kOutOfRange);
+#pragma unroll
+        for (int i = 0; i < TJ; ++i)
+          w[j][i] = buf_load16(Ar, ok ? ((i * 16 + l16) * K + k + 8 * j) * 2 : kOutOfRange);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < TJ; ++i) acc[i] = mfma16(a[j], w[j][i], acc[i]);
+    }
+    if (quantize) {
+      float f[4][8];
+      float most = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        unpack<kBf16>(v[j], f[j]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) most = fmaxf(most, fp8_magnitude(f[j][i]));
+      }
+      most = fmaxf(most, __shfl_xor(most, 16));
+      most = fmaxf(most, __shfl_xor(most, 32));
+      const int byte = fp8_scale_byte(most);
+      const float p = fp8_inverse(byte);
+      if (l16 < rows) {
+        const size_t at = (size_t)(m0 + l16) * K + k;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (k + 16 * h >= K) continue;
+          const uint4 q = make_uint4(fp8_pack4(f[2 * h], p), fp8_pack4(f[2 * h] + 4, p), fp8_pack4(f[2 * h + 1], p),
+                                     fp8_pack4(f[2 * h + 1] + 4, p));
+          if (g.xh)
+            put_values(g.xh + at + 16 * h, q, byte);
+          else
+            *reinterpret_cast<uint4*>(g.xq + at + 16 * h) = q;
+        }
+        if (lg == 0 && !g.xh) g.xs[(size_t)(m0 + l16) * kb_n + kb] = (uint8_t)byte;
+      }
+    }
+    if (convert && l16 < rows) {
+      const size_t at = (size_t)(m0 + l16) * K + k;
+      const int byte = g.s_in[(size_t)(m0 + l16) * kb_n + kb];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if (k + 16 * h < K)
+          put_values(g.xh + at + 16 * h, *reinterpret_cast<const uint4*>(g.q_in + at + 16 * h), byte);
+    }
+  }
+  if constexpr (TJ > 0) {
+    // acc[j] of lane l: T[m0 + 4 lg + e][16 j + l16], to be added over the waves
+    __shared__ float red[P_WAVES][16][RP];
+#pragma unroll
+    for (int j = 0; j < TJ; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) red[wave][4 * lg + e][16 * j + l16] = acc[j][e];
+    __syncthreads();
+    for (int e = t; e < rows * RP; e += P_WAVES * 64) {
+      const int row = e / RP, j = e % RP;
+      float sum = red[0][row][j];
+#pragma unroll
+      for (int w = 1; w < P_WAVES; ++w) sum += red[w][row][j];
+      g.part[((size_t)blockIdx.y * g.M + m0 + row) * RP + j] = sum;
+    }
+  }
+}
+
+// T[row][j] as the sum of its chunks, in their order.
+__device__ __forceinline__ float t_sum(const Fp8LinearArgs& a, int row, int j) {
+  const size_t stride = (size_t)a.M * a.rp;
+  const float* p = a.part + (size_t)row * a.rp + j;
+  float v = 0.f;
+  for (int c = 0; c < a.nch; ++c) v += p[c * stride];
+  return v;
+}
+
+// ------------------------------------------------------------------ few rows
+
+constexpr int kFewRows = 16;
+constexpr int S_WAVES = 8;
+
+// 16 NB rows of W a workgroup, the blocks of K dealt to its waves; their partial
+// sums meet in LDS in wave order.
+template <int NB>
+__global__ __launch_bounds__(S_WAVES * 64) void fp8_stream_kernel(Fp8LinearArgs a) {
+  constexpr int U = 4;
+  __shared__ f32x4_t red[S_WAVES][NB][64];
+  __shared__ float T[16][129];
+  __shared__ uint16_t Bs[16 * NB][130];
+  const int t = threadIdx.x, lane = t & 63, l16 = lane & 15, lg = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int M = a.M, N = a.N, K = a.K, kb_n = (K + kFp8Block - 1) / kFp8Block;
+  const int n0 = blockIdx.x * 16 * NB;
+  const __amdgpu_buffer_rsrc_t xr = make_rsrc(a.xh, (uint32_t)M * K * 2u);
+  const __amdgpu_buffer_rsrc_t wr = make_rsrc(a.wq + (size_t)n0 * K, (uint32_t)min(16 * NB, N - n0) * K);
+  const uint8_t* ws = a.ws + (size_t)(n0 / kFp8Block) * kb_n;  // (16 NB rows lie in one block of 128)
+  f32x4_t acc[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) acc[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  for (int kb0 = wave; kb0 < kb_n; kb0 += S_WAVES * U) {
+    uint4 x[U][4], w[U][NB][2];
+    int sw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int kb = kb0 + u * S_WAVES, k = kb * kFp8Block + 32 * lg;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const bool ok = k + 16 * h < K;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+          w[u][b][h] = buf_load16(wr, ok ? (b * 16 + l16) * K + k + 16 * h : kOutOfRange);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          x[u][2 * h + i] = buf_load16(xr, ok ? (l16 * K + k + 16 * h + 8 * i) * 2 : kOutOfRange);
+      }
+      sw[u] = ws[min(kb, kb_n - 1)];
+    }
+    // lane l has values 32 (l / 16) ... + 31 of a block; the products take eight of
+    // every lane at a time
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint4 v[2];
+          fp8_to_bf16(w[u][b][h], sw[u], v);
+          acc[b] = mfma16(v[0], x[u][2 * h], acc[b]);
+          acc[b] = mfma16(v[1], x[u][2 * h + 1], acc[b]);
+        }
+  }
+#pragma unroll
+  for (int b = 0; b < NB; ++b) red[wave][b][lane] = acc[b];
+  const bool lora = a.y_on && a.rp > 0;
+  if (lora) {
+    for (int e = t; e < M * a.rp; e += S_WAVES * 64) T[e / a.rp][e % a.rp] = a.s * t_sum(a, e / a.rp, e % a.rp);
+    const int rows = min(16 * NB, N - n0);
+    for (int e = t; e < rows * a.r; e += S_WAVES * 64)
+      Bs[e / a.r][e % a.r] = a.B[(size_t)(n0 + e / a.r) * a.ldb + e % a.r];
+  }
+  __syncthreads();
+  for (int e = t; e < 16 * NB * M; e += S_WAVES * 64) {
+    const int nl = e % (16 * NB), m = e / (16 * NB), n = n0 + nl;
+    if (n >= N) continue;
+    const int b = nl / 16, src = (nl % 16) / 4 * 16 + m, i = nl % 4;
+    float v = red[0][b][src][i];
+#pragma unroll
+    for (int w = 1; w < S_WAVES; ++w) v += red[w][b][src][i];
+    const size_t at = (size_t)m * N + n;
+    if (a.y_off) store_elem(a.y_off, a.y_type, at, v);
+    if (!a.y_on) continue;
+    if (lora) {
+      float u = 0.f;
+      for (int j = 0; j < a.r; ++j) u = fmaf(T[m][j], bf16_to_f32(Bs[nl][j]), u);
+      if (a.drop > 0) u = dropout_keeps(dropout_words(a.rng, at >> 3), (int)(at & 7), a.drop) ? u * a.keep : 0.f;
+      v += u;
+    }
+    store_elem(a.y_on, a.y_type, at, v);
+  }
+}
+
+// ------------------------------------------------------------------ tiles
+
+struct GemmArgs {
+  Fp8LinearArgs a;
+  int ntm, ntn, total;
+  int vec4;   // outputs in stores of four values
+  int bvec;   // B in 16-byte loads
+  int64_t xs_bytes, ws_bytes;
+};
+
+// TM x TN tile, WM x WN sub-tile a wave, KS waves a sub-tile (each takes its share
+// of every slab), slabs of BK values of K in a ring of NS; four more waves copy.
+// WIDE: x in bf16 and bf16 products, in steps of 32 values of K; else steps of 64.
+template <bool WIDE_, int TM_, int TN_, int WM_, int WN_, int KS_, int BK_, int NS_>
+struct Tile {
+  static constexpr bool WIDE = WIDE_;
+  static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, KS = KS_, BK = BK_, NS = NS_;
+  static constexpr int NWN = TN / WN, NMW = TM / WM * NWN * KS, NW = NMW + 4, NT = NW * 64;
+  static constexpr int MT = WM / 32, NTL = WN / 32, NQ = MT * NTL, NU = NQ * 4;
+  static constexpr int XCPR = BK * (WIDE ? 2 : 1) / 16, WCPR = BK / 16;  // 16-byte chunks of an LDS row
+  static constexpr int XRPB = 64 / XCPR, WRPB = 64 / WCPR;               // rows of a copy instruction
+  static constexpr int XJ = TM / XRPB / 4, WJ = TN / WRPB / 4, DPW = XJ + WJ;  // copies per copy wave and slab
+  static constexpr int STAGE = TM * XCPR + TN * WCPR;  // uint4
+  static constexpr int STEP = WIDE ? 32 : 64;
+  static constexpr int SPW = BK / STEP / KS;           // steps per wave and slab
+  static constexpr int WR = WIDE ? 1 : 2;              // 16-byte reads of a step's row of W (x: always two)
+  static constexpr int EX = KS > 1 ? NMW * NQ * 4096 : 0;  // bytes of the partial sums
+  // rows of s T (hi | lo) and of B, 16 bytes apart from the next, at padded rank rp
+  static constexpr int lora_bytes(int rp) { return TM * (4 * rp + 16) + TN * (2 * rp + 16); }
+  static constexpr size_t cmax(size_t x, size_t y) { return x > y ? x : y; }
+  static constexpr size_t LDS = cmax(cmax(size_t(NS) * STAGE * 16, EX), lora_bytes(128));
+  static_assert(TM % (XRPB * 4) == 0 && TN % (WRPB * 4) == 0 && SPW >= 1 && NU % KS == 0, "whole copies, steps and units");
+  static_assert(SPW <= 4 && (SPW == 1 || SPW % 2 == 0), "steps listed below");
+  static_assert(WN <= kFp8Block && LDS <= 160 * 1024 && (NS - 2) * DPW < 64, "one scale a sub-tile and slab; LDS; waits");
+};
+
+template <int V>
+using IC = std::integral_constant<int, V>;
+
+// s_waitcnt for at most N vector-memory operations in flight.
+template <int N>
+__device__ __forceinline__ void wait_vm() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (0xF << 8) | (((N >> 4) & 3) << 14));
+  asm volatile("" ::: "memory");
+}
+// LDS operations of this wave complete, then the workgroup barrier.
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// Four scale bytes from `at` on (at < bytes); bytes past the array read as
+// anything.
+__device__ __forceinline__ uint32_t load_scales(const uint8_t* p, int64_t at, int64_t bytes) {
+  if (bytes < 4) {
+    uint32_t v = 0;
+    for (int i = 0; i < 4; ++i)
+      if (at + i < bytes) v |= (uint32_t)p[at + i] << (8 * i);
+    return v;
+  }
+  const int64_t from = at < bytes - 4 ? at : bytes - 4;
+  uint32_t v;
+  __builtin_memcpy(&v, p + from, 4);
+  return v >> (8 * (int)(at - from));
+}
+
+template <class G>
+__global__ __launch_bounds__(G::NT) void fp8_gemm_kernel(GemmArgs g) {
+  constexpr int TM = G::TM, TN = G::TN, WM = G::WM, WN = G::WN, KS = G::KS, BK = G::BK, NS = G::NS;
+  constexpr int MT = G::MT, NTL = G::NTL, NQ = G::NQ, NU = G::NU, SPW = G::SPW;
+  constexpr int XCPR = G::XCPR, WCPR = G::WCPR, WBASE = TM * XCPR;  // (W's rows follow x's)
+  __shared__ uint4 sm[G::LDS / 16];
+  const Fp8LinearArgs& a = g.a;
+  const int M = a.M, N = a.N, K = a.K, kb_n = (K + kFp8Block - 1) / kFp8Block;
+  const int t = threadIdx.x, lane = t & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int l32 = lane & 31, lh = lane >> 5;
+
+  // Consecutive workgroups go to consecutive XCDs; each takes a contiguous range
+  // of an order that walks up to 8 row tiles per column tile.
+  int tmi, tni;
+  {
+    const int q = g.total >> 3, rem = g.total & 7, xcd = blockIdx.x & 7;
+    const int lid = xcd * q + min(xcd, rem) + (blockIdx.x >> 3);
+    const int per_group = 8 * g.ntn, group = lid / per_group, first_m = group * 8, gsize = min(g.ntm - first_m, 8);
+    const int in = lid - group * per_group;
+    tmi = first_m + in % gsize;
+    tni = in / gsize;
+  }
+  const int m0 = __builtin_amdgcn_readfirstlane(tmi * TM), n0 = __builtin_amdgcn_readfirstlane(tni * TN);
+  const int nkt = (K + BK - 1) / BK;
+
+  // LDS chunk of (row, 16-byte chunk c) in rows of `cpr` chunks: c is XOR-ed with
+  // bits of the row, so that 16 consecutive rows' chunks c lie in different banks.
+  auto swz = [](int cpr, int row) __attribute__((always_inline)) {
+    return cpr == 4 ? (row >> 2) & 3 : cpr == 8 ? (row >> 1) & 7 : row & 15;
+  };
+  auto lds_idx = [&](int cpr, int row, int c) __attribute__((always_inline)) { return row * cpr + (c ^ swz(cpr, row)); };
+
+  f32x16_t acc[MT][NTL];
+  const int mw = wave < G::NMW ? wave : 0;
+  const int kg = mw % KS, wt = mw / KS, wr = wt / G::NWN, wc = wt % G::NWN;
+
+  if (wave >= G::NMW) {
+    // -------------------------------------------------------------- copy waves
+    const int cw = wave - G::NMW;
+    // (a lane's chunk is the same for every block of rows cw + 4 j)
+    const int xl = lane / XCPR, xc = (lane % XCPR) ^ swz(XCPR, cw * G::XRPB + xl);
+    const int wl = lane / WCPR, wch = (lane % WCPR) ^ swz(WCPR, cw * G::WRPB + wl);
+    constexpr int XE = G::WIDE ? 2 : 1;  // bytes of a value of x
+    const char* const xp = G::WIDE ? reinterpret_cast<const char*>(a.xh) : reinterpret_cast<const char*>(a.xq);
+    const i32x4_t xr = make_rsrc_raw(xp + (size_t)m0 * K * XE, (uint32_t)min(TM, M - m0) * K * XE);
+    const i32x4_t wrs = make_rsrc_raw(a.wq + (size_t)n0 * K, (uint32_t)min(TN, N - n0) * K);
+    auto issue = [&](int stage, int kt) __attribute__((always_inline)) {
+      const int xk = kt * BK * XE + xc * 16, wk = kt * BK + wch * 16;  // bytes
+      const bool xok = xk < K * XE, wok = wk < K;
+#pragma unroll
+      for (int j = 0; j < G::XJ; ++j) {
+        const int row = (cw + 4 * j) * G::XRPB;
+        dma16(xr, sm + stage * G::STAGE + row * XCPR, xok ? (row + xl) * K * XE + xk : kOutOfRange);
+      }
+#pragma unroll
+      for (int j = 0; j < G::WJ; ++j) {
+        const int row = (cw + 4 * j) * G::WRPB;
+        dma16(wrs, sm + stage * G::STAGE + WBASE + row * WCPR, wok ? (row + wl) * K + wk : kOutOfRange);
+      }
+    };
+    // slabs past the last read zeros, so that the waits count the same throughout
+#pragma unroll
+    for (int s = 0; s < NS; ++s) issue(s, s);
+    wait_vm<(NS - 1) * G::DPW < 63 ? (NS - 1) * G::DPW : 63>();
+    lds_barrier();  // slab 0 is in LDS
+    int stage = 0;
+    for (int kt = 0; kt < nkt; ++kt) {
+      wait_vm<(NS - 2) * G::DPW>();
+      lds_barrier();  // slab kt + 1 has landed, slab kt is in registers everywhere
+      issue(stage, kt + NS);
+      stage = stage + 1 == NS ? 0 : stage + 1;
+    }
+    wait_vm<0>();
+  } else {
+    // -------------------------------------------------------------- matrix waves
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < NTL; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+    constexpr int WR = G::WR, NR = WR * NTL + 2 * MT;
+    struct Frag {
+      uint4 w[NTL][WR], x[MT][2];
+    };
+    Frag F[2];
+    // the r-th 16-byte read of step st (of this wave's) of a stage: W rows as the A
+    // operand, x rows as the B operand
+    auto read = [&](Frag& f, int stage, int st, int r) __attribute__((always_inline)) {
+      const uint4* s = sm + stage * G::STAGE;
+      const int own = 2 * (kg * SPW + st) + lh;  // this lane's half step
+      if (r < WR * NTL) {
+        const int q = r / WR, h = r % WR;
+        f.w[q][h] = s[WBASE + lds_idx(WCPR, wc * WN + q * 32 + l32, own * WR + h)];
+      } else {
+        const int q = (r - WR * NTL) / 2, h = (r - WR * NTL) % 2;
+        f.x[q][h] = s[lds_idx(XCPR, wr * WM + q * 32 + l32, own * 2 + h)];
+      }
+    };
+    // scales: four blocks of K at a time, the next four requested ahead (WIDE: x has none)
+    const uint8_t* const xs = a.xs;
+    const uint8_t* const ws = a.ws;
+    constexpr int MS = G::WIDE ? 0 : MT;
+    int64_t xrow[MT];
+#pragma unroll
+    for (int i = 0; i < MS; ++i) xrow[i] = (int64_t)min(m0 + wr * WM + i * 32 + l32, M - 1) * kb_n;
+    const int64_t wrow = (int64_t)(min(n0 + wc * WN, N - 1) / kFp8Block) * kb_n;
+    uint32_t sx[MT], sxn[MT], sw, swn;
+    auto load_four = [&](int kb) __attribute__((always_inline)) {
+      kb = min(kb, kb_n - 1);
+#pragma unroll
+      for (int i = 0; i < MS; ++i) sxn[i] = load_scales(xs, xrow[i] + kb, g.xs_bytes);
+      swn = load_scales(ws, wrow + kb, g.ws_bytes);
+    };
+    int four = -1;  // the four blocks that sx and sw are of
+    auto next_four = [&](int f) __attribute__((always_inline)) {
+      four = f;
+#pragma unroll
+      for (int i = 0; i < MS; ++i) sx[i] = sxn[i];
+      sw = swn;
+      load_four(4 * f + 4);
+    };
+    load_four(0);
+    auto kstep = [&](auto S, const Frag& fc, Frag& fn, int st, int kt) __attribute__((always_inline)) {
+      constexpr int sp = decltype(S)::value;
+      constexpr bool last = sp == SPW - 1;
+      const int kb = (kt * (BK / G::STEP) + kg * SPW + sp) / (kFp8Block / G::STEP);
+      if (kb >> 2 != four) next_four(kb >> 2);  // (each four in turn: a slab is no longer)
+      const int shift = 8 * (kb & 3);
+      // (the second half of a last slab may lie past the scales: zeros times any number)
+      const bool past = BK > kFp8Block && kb >= kb_n;
+      const int rst = last ? (st + 1 == NS ? 0 : st + 1) : st;
+      constexpr int rsp = last ? 0 : sp + 1;
+      if constexpr (last) lds_barrier();
+      if constexpr (G::WIDE) {
+        const int byte = (sw >> shift) & 0xFF;
+#pragma unroll
+        for (int ni = 0; ni < NTL; ++ni) {
+          uint4 v[2];
+          fp8_to_bf16(fc.w[ni][0], byte, v);
+#pragma unroll
+          for (int mi = 0; mi < MT; ++mi)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) acc[mi][ni] = mfma32(v[h], fc.x[mi][h], acc[mi][ni]);
+#pragma unroll
+          for (int r = ni * NR / NTL; r < (ni + 1) * NR / NTL; ++r) read(fn, rst, rsp, r);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      } else {
+#pragma unroll
+        for (int m = 0; m < NQ; ++m) {
+          const int mi = m / NTL, ni = m % NTL;
+          acc[mi][ni] = mfma32_fp8(fc.w[ni][0], fc.w[ni][WR - 1], fc.x[mi][0], fc.x[mi][1], acc[mi][ni],
+                                   past ? 127 : (int)(sw >> shift), past ? 127 : (int)(sx[mi] >> shift));
+#pragma unroll
+          for (int r = m * NR / NQ; r < (m + 1) * NR / NQ; ++r) read(fn, rst, rsp, r);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    };
+    lds_barrier();  // slab 0 is in LDS
+#pragma unroll
+    for (int r = 0; r < NR; ++r) read(F[0], 0, 0, r);
+    // Past the last slab the reads fill registers that are never used.
+    constexpr int UN = SPW % 2 ? 2 : 1;  // slabs until the two fragment sets are back in place
+    int stage = 0;
+    for (int kt = 0; kt < nkt; kt += UN) {
+#pragma unroll
+      for (int u = 0; u < UN; ++u) {
+        if (u > 0 && kt + u >= nkt) break;
+        constexpr int one = SPW > 1 ? 1 : 0, two = SPW > 2 ? 2 : 0, three = SPW > 3 ? 3 : 0;
+        kstep(IC<0>{}, F[u & 1], F[(u & 1) ^ 1], stage, kt + u);
+        if constexpr (SPW > 1) kstep(IC<one>{}, F[1], F[0], stage, kt + u);
+        if constexpr (SPW > 2) {
+          kstep(IC<two>{}, F[0], F[1], stage, kt + u);
+          kstep(IC<three>{}, F[1], F[0], stage, kt + u);
+        }
+        stage = stage + 1 == NS ? 0 : stage + 1;
+      }
+    }
+  }
+  lds_barrier();  // every copy has landed, every wave is done with the ring
+
+  // ---------------------------------------------------------------- epilogue
+  // The KS partial sums of a sub-tile, in units of four registers (unit 4 q + i of
+  // block q = mi NTL + ni), are added in wave order; a wave then holds NU / KS units.
+  constexpr int MYU = NU / KS;
+  const int u0 = kg * MYU;
+  f32x4_t un[MYU];
+  if constexpr (KS > 1) {
+    f32x4_t* const ex = reinterpret_cast<f32x4_t*>(sm);
+    if (wave < G::NMW) {
+#pragma unroll
+      for (int q = 0; q < NQ; ++q)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const f32x16_t& v = acc[q / NTL][q % NTL];
+          ex[(mw * NU + q * 4 + i) * 64 + lane] = f32x4_t{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
+        }
+    }
+    __syncthreads();
+    if (wave < G::NMW) {
+#pragma unroll
+      for (int u = 0; u < MYU; ++u) {
+        un[u] = ex[((wt * KS) * NU + u0 + u) * 64 + lane];
+#pragma unroll
+        for (int k = 1; k < KS; ++k) un[u] += ex[((wt * KS + k) * NU + u0 + u) * 64 + lane];
+      }
+    }
+    __syncthreads();
+  } else if (wave < G::NMW) {
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+      const f32x16_t& v = acc[u / 4 / NTL][u / 4 % NTL];
+      const int i = u % 4;
+      un[u] = f32x4_t{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
+    }
+  }
+  // The rows of s T as bf16 hi and lo parts (2^-17 of a value together) and those
+  // of B, zero padded to rp, to LDS.
+  const bool lora = a.y_on && a.rp > 0;
+  const int rp = a.rp, lrp = 31 - __builtin_clz(rp | 1), ldt = 2 * rp + 8, ldb = rp + 8;  // (in values)
+  uint16_t* const Ts = reinterpret_cast<uint16_t*>(sm);
+  uint16_t* const Bs = Ts + TM * ldt;
+  if (lora) {
+    const int rows = min(TM, M - m0), cols = min(TN, N - n0);
+    if (a.ts) {
+      for (int e = t; e < TM * rp / 4; e += G::NT) {  // 16 bytes each
+        const int row = e >> (lrp - 2), c = (e & (rp / 4 - 1)) * 8;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (row < rows) v = *reinterpret_cast<const uint4*>(a.ts + (size_t)(m0 + row) * 2 * rp + c);
+        *reinterpret_cast<uint4*>(Ts + row * ldt + c) = v;
+      }
+    } else {
+      const size_t stride = (size_t)M * rp;
+      for (int e = t; e < TM * rp / 4; e += G::NT) {
+        const int row = e >> (lrp - 2), j = (e & (rp / 4 - 1)) * 4;
+        f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+        if (row < rows) {
+          const float* p = a.part + (size_t)(m0 + row) * rp + j;
+          for (int c = 0; c < a.nch; ++c) v += *reinterpret_cast<const f32x4_t*>(p + c * stride);
+        }
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float f = a.s * v[i];
+          hi[i] = f32_to_bf16_any(f);
+          lo[i] = (hi[i] & 0x7FFF) < 0x7F80 ? f32_to_bf16_any(f - bf16_to_f32(hi[i])) : 0;  // (none of an infinity)
+        }
+        *reinterpret_cast<uint2*>(Ts + row * ldt + j) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
+        *reinterpret_cast<uint2*>(Ts + row * ldt + rp + j) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+      }
+    }
+    if (g.bvec) {
+      for (int e = t; e < TN * rp / 8; e += G::NT) {
+        const int row = e >> (lrp - 3), j = (e & (rp / 8 - 1)) * 8;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (row < cols && j < a.r) v = *reinterpret_cast<const uint4*>(a.B + (size_t)(n0 + row) * a.ldb + j);
+        *reinterpret_cast<uint4*>(Bs + row * ldb + j) = v;
+      }
+    } else {
+      for (int e = t; e < TN * rp; e += G::NT) {
+        const int row = e >> lrp, j = e & (rp - 1);
+        Bs[row * ldb + j] = row < cols && j < a.r ? a.B[(size_t)(n0 + row) * a.ldb + j] : (uint16_t)0;
+      }
+    }
+    __syncthreads();
+  }
+  if (wave >= G::NMW) return;
+
+  constexpr int MYQ = MYU >= 4 ? MYU / 4 : 1, UPQ = MYU / MYQ;
+  auto finish = [&](auto BI) __attribute__((always_inline)) {
+    constexpr int b = decltype(BI)::value;
+    const int q = (u0 >> 2) + b, i0 = MYU >= 4 ? 0 : (u0 & 3);
+    const int mi = q / NTL, ni = q % NTL;
+    const int row = m0 + wr * WM + mi * 32 + l32;
+    const int colb = n0 + wc * WN + ni * 32 + 4 * lh;
+    auto store = [&](void* y, const f32x4_t (&v)[UPQ]) __attribute__((always_inline)) {
+      if (row >= M) return;
+#pragma unroll
+      for (int k = 0; k < UPQ; ++k) {
+        const int col = colb + 8 * (i0 + k);
+        const size_t at = (size_t)row * N + col;
+        if (g.vec4 && col + 3 < N) {
+          if (a.y_type == kF32)
+            *reinterpret_cast<f32x4_t*>(static_cast<float*>(y) + at) = v[k];
+          else
+            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(y) + at) =
+                make_uint2(f32_to_bf16_pair(v[k][0], v[k][1]), f32_to_bf16_pair(v[k][2], v[k][3]));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (col + e < N) store_elem(y, a.y_type, at + e, v[k][e]);
+        }
+      }
+    };
+    f32x4_t v[UPQ];
+#pragma unroll
+    for (int k = 0; k < UPQ; ++k) v[k] = un[b * UPQ + k];
+    if (a.y_off) store(a.y_off, v);
+    if (!a.y_on) return;
+    if (lora) {
+      // s T B^T of the block: rows of [B | B] against rows of [hi | lo]
+      f32x16_t L;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) L[e] = 0.f;
+      const uint16_t* tr = Ts + (wr * WM + mi * 32 + l32) * ldt + 8 * lh;
+      const uint16_t* br = Bs + (wc * WN + ni * 32 + l32) * ldb + 8 * lh;
+      for (int k0 = 0; k0 < rp; k0 += 16) {
+        const uint4 bf = *reinterpret_cast<const uint4*>(br + k0);
+        L = mfma32(bf, *reinterpret_cast<const uint4*>(tr + k0), L);
+        L = mfma32(bf, *reinterpret_cast<const uint4*>(tr + rp + k0), L);
+      }
+#pragma unroll
+      for (int k = 0; k < UPQ; ++k) {
+        f32x4_t l;
+        if constexpr (MYU >= 4) {
+          l = f32x4_t{L[4 * k], L[4 * k + 1], L[4 * k + 2], L[4 * k + 3]};
+        } else {
+          l = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (i == i0 + k) l = f32x4_t{L[4 * i], L[4 * i + 1], L[4 * i + 2], L[4 * i + 3]};
+        }
+        if (a.drop > 0) {
+          const uint64_t at = (uint64_t)row * N + colb + 8 * (i0 + k);  // (a multiple of 4: N % 8 == 0)
+          const uint4 w = dropout_words(a.rng, at >> 3);
+          const int j0 = (int)(at & 4);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) l[e] = dropout_keeps(w, j0 + e, a.drop) ? l[e] * a.keep : 0.f;
+        }
+        v[k] += l;
+      }
+    }
+    store(a.y_on, v);
+  };
+  static_assert(MYQ <= 8 && UPQ * MYQ == MYU, "blocks listed below");
+  finish(IC<0>{});
+  if constexpr (MYQ > 1) finish(IC<1>{});
+  if constexpr (MYQ > 2) finish(IC<2>{});
+  if constexpr (MYQ > 3) finish(IC<3>{});
+  if constexpr (MYQ > 4) finish(IC<4>{});
+  if constexpr (MYQ > 5) finish(IC<5>{});
+  if constexpr (MYQ > 6) finish(IC<6>{});
+  if constexpr (MYQ > 7) finish(IC<7>{});
+}
+
+bool at_multiple(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+template <class G>
+hipError_t launch_tile(GemmArgs& g, hipStream_t stream) {
+  g.ntm = (g.a.M + G::TM - 1) / G::TM;
+  g.ntn = (g.a.N + G::TN - 1) / G::TN;
+  const int64_t total = (int64_t)g.ntm * g.ntn;
+  if (total * G::NT >= (int64_t(1) << 32)) return hipErrorInvalidValue;
+  g.total = (int)total;
+  hipLaunchKernelGGL(fp8_gemm_kernel<G>, dim3(g.total), dim3(G::NT), 0, stream, g);
+  return hipGetLastError();
+}
+
+// The tile: the largest that gives most CUs one.
+template <bool WIDE>
+hipError_t launch_rows(GemmArgs& g, hipStream_t stream) {
+  const auto tiles = [&](int tm, int tn) {
+    return (int64_t)((g.a.M + tm - 1) / tm) * ((g.a.N + tn - 1) / tn);
+  };
+  constexpr int D = WIDE ? 2 : 1;  // (a slab of bf16 rows holds half the values)
+  if (tiles(128, 256) >= 200) return launch_tile<Tile<WIDE, 128, 256, 64, 128, 1, 128 / D, WIDE ? 4 : 3>>(g, stream);
+  if (tiles(128, 128) >= 200) return launch_tile<Tile<WIDE, 128, 128, 64, 64, 2, 128 / D, 5>>(g, stream);
+  if (tiles(64, 128) >= 200) return launch_tile<Tile<WIDE, 64, 128, 64, 64, 2, 128 / D, 6>>(g, stream);
+  if (tiles(64, 64) >= 200) return launch_tile<Tile<WIDE, 64, 64, 32, 64, 4, 256 / D, 4>>(g, stream);
+  return launch_tile<Tile<WIDE, 32, 32, 32, 32, 4, 256 / D, 8>>(g, stream);
+}
+
+template <int RP>
+void launch_prep(const Fp8PrepArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL(fp8_prep_kernel<RP>, dim3((a.M + 15) / 16, a.nch), dim3(P_WAVES * 64), 0, stream, a);
+}
+
+}  // namespace
+
+// Chunks of K: about 512 workgroups, each at least a block a wave, and no more
+// partial sums of T than the product can add up on the side.
+void fp8_prep_chunks(int M, int K, int rp, int& nch, int& kch) {
+  const int kb = (K + kFp8Block - 1) / kFp8Block, mb = (M + 15) / 16;
+  int want = (512 + mb - 1) / mb;
+  const int most = rp == 0 ? 64 : M <= 16 ? 32 : rp <= 32 ? 8 : 4;
+  want = want < most ? want : most;
+  kch = (kb + want - 1) / want;
+  kch = kch < P_WAVES ? P_WAVES : kch;
+  nch = (kb + kch - 1) / kch;
+}
+
+hipError_t launch_fp8_prep(const Fp8PrepArgs& a, hipStream_t stream) {
+  switch (a.A ? a.rp : 0) {
+    case 0: launch_prep<0>(a, stream); break;
+    case 16: launch_prep<16>(a, stream); break;
+    case 32: launch_prep<32>(a, stream); break;
+    case 64: launch_prep<64>(a, stream); break;
+    case 128: launch_prep<128>(a, stream); break;
+    default: return hipErrorInvalidValue;
+  }
+  return hipGetLastError();
+}
+
+bool fp8_wide(int M, int y_type) { return M <= kFewRows || y_type == kF32; }
+
+hipError_t launch_fp8_linear(const Fp8LinearArgs& a, hipStream_t stream) {
+  if (a.M <= kFewRows && !a.ts) {
+    hipLaunchKernelGGL(fp8_stream_kernel<2>, dim3((a.N + 31) / 32), dim3(S_WAVES * 64), 0, stream, a);
+    return hipGetLastError();
+  }
+  GemmArgs g{};
+  g.a = a;
+  const int64_t kb = (a.K + kFp8Block - 1) / kFp8Block;
+  g.xs_bytes = a.M * kb;
+  g.ws_bytes = (int64_t)((a.N + kFp8Block - 1) / kFp8Block) * kb;
+  const uintptr_t four = a.y_type == kF32 ? 16 : 8;
+  g.vec4 = a.N % 4 == 0 && at_multiple(a.y_off, four) && at_multiple(a.y_on, four);
+  g.bvec = a.r % 8 == 0 && a.ldb % 8 == 0 && at_multiple(a.B, 16);
+  return fp8_wide(a.M, a.y_type) ? launch_rows<true>(g, stream) : launch_rows<false>(g, stream);
+}
+
+}  // namespace hydra

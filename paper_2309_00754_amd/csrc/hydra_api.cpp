@@ -1172,6 +1172,306 @@ hydra_status hydra_grad_clip(int64_t n, const void* const* grads, const int32_t*
   return from_hip(hydra::launch_grad_norm(a, workspace, reinterpret_cast<hipStream_t>(stream)));
 }
 
+}  // extern "C"
+
+namespace {
+
+int64_t blocks128(int64_t n) { return (n + 127) / 128; }
+size_t up256(size_t v) { return (v + 255) / 256 * 256; }
+// Workspace of a product over an 8-bit weight: the rows' values in bf16, or their
+// bytes and scales in the same place.
+size_t fp8_rows_bytes(int64_t M, int64_t K) { return up256((size_t)M * K * 2) + up256((size_t)M * blocks128(K)); }
+
+hydra_status fp8_shape(int64_t M, int64_t N, int64_t K, int64_t r) {
+  if (M < 1 || M > kMaxRows || N < 1 || N > kMaxCols || K < 1 || K > kMaxK || K % 16 != 0) return HYDRA_ERR_SHAPE;
+  if (r < 0 || r > HYDRA_MAX_RANK) return HYDRA_ERR_SHAPE;
+  if (((M + 127) / 128) * ((N + 255) / 256) >= (int64_t(1) << 23)) return HYDRA_ERR_SHAPE;
+  return HYDRA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+hydra_status hydra_fp8_quantize(const void* x, hydra_dtype x_type, int64_t M, int64_t K, int64_t block_rows, uint8_t* q,
+                                uint8_t* scale, uint8_t* qt, uint8_t* scale_t, void* stream) {
+  if (!x || !q || !scale || (qt != nullptr) != (scale_t != nullptr)) return HYDRA_ERR_NULL;
+  if (!type_ok(x_type)) return HYDRA_ERR_UNSUPPORTED;
+  if (block_rows != 1 && block_rows != 128) return HYDRA_ERR_UNSUPPORTED;
+  if (qt && block_rows != 128) return HYDRA_ERR_UNSUPPORTED;
+  if (M < 1 || M > kMaxCols || K < 1 || K > kMaxK) return HYDRA_ERR_SHAPE;
+  // (one dispatch: 16 lanes a block of 128 values, 256 a block of 128 x 128)
+  if (block_rows == 1 ? M * blocks128(K) >= (int64_t(1) << 28) : blocks128(M) * blocks128(K) >= (int64_t(1) << 24))
+    return HYDRA_ERR_SHAPE;
+  const void* const outs[4] = {q, scale, qt, scale_t};
+  const void* const ins[1] = {x};
+  if (!distinct(outs, ins)) return HYDRA_ERR_SHAPE;
+  if (!aligned(x, type_align(x_type))) return HYDRA_ERR_ALIGN;
+  hydra::Fp8QuantArgs a{};
+  a.x = x;
+  a.x_type = x_type;
+  a.M = int(M);
+  a.K = int(K);
+  a.tiles = block_rows == 128;
+  a.q = q;
+  a.scale = scale;
+  a.qt = qt;
+  a.scale_t = scale_t;
+  return from_hip(hydra::launch_fp8_quantize(a, reinterpret_cast<hipStream_t>(stream)));
+}
+
+hydra_status hydra_fp8_lora_linear_workspace_bytes(int64_t M, int64_t K, int64_t r, size_t* bytes) {
+  if (!bytes) return HYDRA_ERR_NULL;
+  const hydra_status chk = fp8_shape(M, 1, K, r);
+  if (chk != HYDRA_OK) return chk;
+  int nch = 0, kch = 0;
+  const int rp = hydra::padded_rank(int(r));
+  hydra::fp8_prep_chunks(int(M), int(K), rp, nch, kch);
+  *bytes = fp8_rows_bytes(M, K) + (rp ? up256((size_t)nch * M * rp * 4) : 0);
+  return HYDRA_OK;
+}
+
+hydra_status hydra_fp8_lora_linear(const uint16_t* x, const uint16_t* x_adapter, const uint8_t* xq,
+                                   const uint8_t* x_scale, const uint8_t* Wq, const uint8_t* w_scale,
+                                   const uint16_t* A, const uint16_t* B, float s, int64_t M, int64_t N, int64_t K,
+                                   int64_t r, void* y_off, void* y_on, hydra_dtype y_type, void* workspace,
+                                   size_t workspace_bytes, void* stream) {
+  if (!Wq || !w_scale || (!y_off && !y_on) || (!x && !xq) || (xq != nullptr) != (x_scale != nullptr)) return HYDRA_ERR_NULL;
+  if (!type_ok(y_type)) return HYDRA_ERR_UNSUPPORTED;
+  const hydra_status chk = fp8_shape(M, N, K, r);
+  if (chk != HYDRA_OK) return chk;
+  const bool lora = y_on && r > 0;
+  const uint16_t* xa = x_adapter ? x_adapter : x;
+  if (lora && (!A || !B || !xa)) return HYDRA_ERR_NULL;
+  const void* const outs[2] = {y_off, y_on};
+  const void* const ins[8] = {x, x_adapter, xq, x_scale, Wq, w_scale, A, B};
+  if (!distinct(outs, ins)) return HYDRA_ERR_SHAPE;
+  if (!aligned(x, 16) || !aligned(x_adapter, 16) || !aligned(xq, 16) || !aligned(Wq, 16) ||
+      (lora && (!aligned(A, 16) || !aligned(B, 2))) || !aligned(y_off, type_align(y_type)) ||
+      !aligned(y_on, type_align(y_type)))
+    return HYDRA_ERR_ALIGN;
+  const int rp = lora ? hydra::padded_rank(int(r)) : 0;
+  int nch = 0, kch = 0;
+  hydra::fp8_prep_chunks(int(M), int(K), rp, nch, kch);
+  const bool wide = hydra::fp8_wide(int(M), y_type);
+  const size_t rows = xq && !wide ? 0 : fp8_rows_bytes(M, K), need = rows + (rp ? up256((size_t)nch * M * rp * 4) : 0);
+  if (need > 0) {
+    if (!workspace) return HYDRA_ERR_NULL;
+    if (workspace_bytes < need) return HYDRA_ERR_WORKSPACE;
+    if (!aligned(workspace, 16)) return HYDRA_ERR_ALIGN;
+  }
+  uint8_t* const w = static_cast<uint8_t*>(workspace);
+  hydra::Fp8PrepArgs p{};
+  p.x = xq ? nullptr : x;
+  p.xa = xa;
+  p.A = lora ? A : nullptr;
+  p.M = int(M);
+  p.K = int(K);
+  p.r = int(r);
+  p.rp = rp;
+  if (wide) {
+    p.xh = reinterpret_cast<uint16_t*>(w);
+    p.q_in = xq;
+    p.s_in = x_scale;
+  } else {
+    p.xq = w;
+    p.xs = rows > 0 ? w + up256((size_t)M * K * 2) : nullptr;
+  }
+  p.part = reinterpret_cast<float*>(w + rows);
+  p.nch = nch;
+  p.kch = kch;
+  const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  if (need > 0) {
+    const hipError_t e = hydra::launch_fp8_prep(p, st);
+    if (e != hipSuccess) return from_hip(e);
+  }
+  hydra::Fp8LinearArgs a{};
+  a.xh = p.xh;
+  a.xq = xq ? xq : p.xq;
+  a.xs = xq ? x_scale : p.xs;
+  a.wq = Wq;
+  a.ws = w_scale;
+  a.M = int(M);
+  a.N = int(N);
+  a.K = int(K);
+  a.y_off = y_off;
+  a.y_on = y_on;
+  a.y_type = y_type;
+  a.r = lora ? int(r) : 0;
+  a.rp = rp;
+  a.s = s;
+  a.part = p.part;
+  a.nch = nch;
+  a.B = B;
+  a.ldb = int(r);
+  return from_hip(hydra::launch_fp8_linear(a, st));
+}
+
+hydra_status hydra_fp8_lora_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t r, size_t* bytes) {
+  if (!bytes) return HYDRA_ERR_NULL;
+  const hydra_status chk = fp8_shape(M, K, N, r);
+  if (chk != HYDRA_OK) return chk;
+  if (K % 16 != 0) return HYDRA_ERR_SHAPE;
+  *bytes = fp8_rows_bytes(M, N) + hydra::backward_ws_bytes(int(M), int(N), int(K), hydra::padded_rank(int(r)));
+  return HYDRA_OK;
+}
+
+hydra_status hydra_fp8_lora_linear_backward(const uint16_t* x, const uint8_t* Wqt, const uint8_t* wt_scale,
+                                            const uint16_t* A, const uint16_t* B, float s, const uint16_t* dy, int64_t M,
+                                            int64_t N, int64_t K, int64_t r, double p, const uint64_t* rng, void* dx,
+                                            hydra_dtype dx_type, float* dA, float* dB, void* workspace,
+                                            size_t workspace_bytes, void* stream) {
+  if (!dy) return HYDRA_ERR_NULL;
+  if (r == 0) dA = dB = nullptr;
+  if (!dx && !dA && !dB) return HYDRA_ERR_NULL;
+  if (!type_ok(dx_type)) return HYDRA_ERR_UNSUPPORTED;
+  const hydra_status chk = fp8_shape(M, K, N, r);
+  if (chk != HYDRA_OK) return chk;
+  if (K % 16 != 0) return HYDRA_ERR_SHAPE;
+  if (!(p >= 0.0 && p <= 1.0)) return HYDRA_ERR_SHAPE;
+  uint32_t drop;
+  float keep;
+  hydra::dropout_numbers(p, drop, keep);
+  if (dx && (!Wqt || !wt_scale || (drop > 0 && !rng))) return HYDRA_ERR_NULL;
+  if (r > 0 && (((dx || dB) && !A) || ((dx || dA) && !B) || ((dA || dB) && !x))) return HYDRA_ERR_NULL;
+  const void* const outs[3] = {dx, dA, dB};
+  const void* const ins[7] = {x, Wqt, wt_scale, A, B, dy, rng};
+  if (!distinct(outs, ins)) return HYDRA_ERR_SHAPE;
+  if (!aligned(x, 16) || !aligned(Wqt, 16) || !aligned(A, 16) || !aligned(B, 2) || !aligned(dy, 16) || !aligned(rng, 8) ||
+      !aligned(dx, type_align(dx_type)) || !aligned(dA, 4) || !aligned(dB, 4))
+    return HYDRA_ERR_ALIGN;
+  const int rp = hydra::padded_rank(int(r));
+  const size_t rows = fp8_rows_bytes(M, N), need = rows + hydra::backward_ws_bytes(int(M), int(N), int(K), rp);
+  if (!workspace) return HYDRA_ERR_NULL;
+  if (workspace_bytes < need) return HYDRA_ERR_WORKSPACE;
+  if (!aligned(workspace, 16)) return HYDRA_ERR_ALIGN;
+  uint8_t* const w = static_cast<uint8_t*>(workspace);
+  hydra::Fp8LinearArgs g{};
+  if (hydra::fp8_wide(int(M), dx_type)) {
+    g.xh = reinterpret_cast<uint16_t*>(w);
+  } else {
+    g.xq = w;
+    g.xs = w + up256((size_t)M * N * 2);
+  }
+  g.wq = Wqt;
+  g.ws = wt_scale;
+  g.M = int(M);
+  g.N = int(K);
+  g.K = int(N);
+  (r > 0 ? g.y_on : g.y_off) = dx;
+  g.y_type = dx_type;
+  g.s = s;
+  g.drop = drop;
+  g.keep = keep;
+  g.rng = rng;
+  hydra::BackwardArgs a{};
+  a.x = x;
+  a.A = A;
+  a.B = B;
+  a.dy = dy;
+  a.s = s;
+  a.M = int(M);
+  a.N = int(N);
+  a.K = int(K);
+  a.r = int(r);
+  a.dA = dA;
+  a.dB = dB;
+  a.base8 = dx ? &g : nullptr;
+  return from_hip(hydra::launch_lora_backward(a, w + rows, reinterpret_cast<hipStream_t>(stream)));
+}
+
+hydra_status hydra_dropout(const void* x, hydra_dtype x_type, const void* residual, hydra_dtype residual_type, double p,
+                           const uint64_t* rng, int64_t n, void* y, hydra_dtype y_type, void* stream) {
+  if (!x || !rng || !y) return HYDRA_ERR_NULL;
+  if (!type_ok(x_type) || !type_ok(residual_type) || !type_ok(y_type)) return HYDRA_ERR_UNSUPPORTED;
+  if (n < 1 || n > (int64_t(1) << 34) || !(p >= 0.0 && p <= 1.0)) return HYDRA_ERR_SHAPE;
+  const void* const outs[1] = {y};
+  const void* const ins[3] = {x == y && x_type == y_type ? nullptr : x,
+                              residual == y && residual_type == y_type ? nullptr : residual, rng};
+  if (!distinct(outs, ins)) return HYDRA_ERR_SHAPE;
+  if (!aligned(x, type_align(x_type)) || !aligned(residual, type_align(residual_type)) || !aligned(y, type_align(y_type)) ||
+      !aligned(rng, 8))
+    return HYDRA_ERR_ALIGN;
+  hydra::DropoutArgs a{};
+  a.x = x;
+  a.res = residual;
+  a.y = y;
+  a.x_type = x_type;
+  a.res_type = residual_type;
+  a.y_type = y_type;
+  a.n = n;
+  hydra::dropout_numbers(p, a.drop, a.keep);
+  a.rng = rng;
+  return from_hip(hydra::launch_dropout(a, reinterpret_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"
+
+namespace {
+
+hydra_status verify_shape(int64_t n, int64_t k, int64_t V) {
+  if (n < 1 || k < 0 || k > HYDRA_MAX_DRAFTS || V < 1 || V > kMaxCols || n > kMaxRows || n * (k + 1) > kMaxRows)
+    return HYDRA_ERR_SHAPE;
+  // (one dispatch of 256 threads a row and 4096 logits)
+  return n * (2 * k + 1) * ((V + 4095) / 4096) < (int64_t(1) << 24) ? HYDRA_OK : HYDRA_ERR_SHAPE;
+}
+
+}  // namespace
+
+extern "C" {
+
+hydra_status hydra_verify_drafts_workspace_bytes(int64_t n, int64_t k, int64_t V, size_t* bytes) {
+  if (!bytes) return HYDRA_ERR_NULL;
+  const hydra_status chk = verify_shape(n, k, V);
+  if (chk != HYDRA_OK) return chk;
+  *bytes = hydra::verify_ws_bytes(int(n), int(k), int(V));
+  return HYDRA_OK;
+}
+
+hydra_status hydra_verify_drafts(const void* target, hydra_dtype target_type, int64_t ld, const void* draft,
+                                 hydra_dtype draft_type, int64_t ld_draft, const int32_t* drafts, const int32_t* lens,
+                                 const float* u, int64_t n, int64_t k, int64_t V, double temperature, int32_t* accepted,
+                                 int32_t* tokens, float* lp, void* workspace, size_t workspace_bytes, int32_t* err_flag,
+                                 void* stream) {
+  if (!target || !u || !accepted || !tokens || (k > 0 && !drafts)) return HYDRA_ERR_NULL;
+  if (!type_ok(target_type) || !type_ok(draft_type)) return HYDRA_ERR_UNSUPPORTED;
+  hydra_status chk = verify_shape(n, k, V);
+  if (chk != HYDRA_OK) return chk;
+  if (ld < V || ld > kMaxDim || (draft && (ld_draft < V || ld_draft > kMaxDim))) return HYDRA_ERR_SHAPE;
+  const double inv_t = 1.0 / temperature;
+  if (!(temperature > 0.0 && temperature <= 1e30 && inv_t <= 1e30)) return HYDRA_ERR_SHAPE;
+  const void* const outs[4] = {accepted, tokens, lp, err_flag};
+  const void* const ins[5] = {target, draft, drafts, lens, u};
+  if (!distinct(outs, ins)) return HYDRA_ERR_SHAPE;
+  if (!aligned(target, type_align(target_type)) || !aligned(draft, type_align(draft_type)) || !aligned(drafts, 4) ||
+      !aligned(lens, 4) || !aligned(u, 4))
+    return HYDRA_ERR_ALIGN;
+  for (const void* p : outs)
+    if (!aligned(p, 4)) return HYDRA_ERR_ALIGN;
+  if (!workspace) return HYDRA_ERR_NULL;
+  if (workspace_bytes < hydra::verify_ws_bytes(int(n), int(k), int(V))) return HYDRA_ERR_WORKSPACE;
+  if (!aligned(workspace, 16)) return HYDRA_ERR_ALIGN;
+  hydra::VerifyArgs a{};
+  a.z = target;
+  a.zd = k > 0 ? draft : nullptr;
+  a.z_type = target_type;
+  a.d_type = draft_type;
+  a.ld = ld;
+  a.ld_d = ld_draft;
+  a.drafts = drafts;
+  a.lens = lens;
+  a.u = u;
+  a.n = int(n);
+  a.k = int(k);
+  a.V = int(V);
+  a.inv_t = inv_t;
+  a.accepted = accepted;
+  a.tokens = tokens;
+  a.lp = lp;
+  a.err = err_flag;
+  return from_hip(hydra::launch_verify(a, workspace, reinterpret_cast<hipStream_t>(stream)));
+}
+
 const char* hydra_status_string(hydra_status status) {
   switch (status) {
     case HYDRA_OK: return "HYDRA_OK";

@@ -276,6 +276,106 @@ struct GradArgs {
 size_t grad_ws_bytes();
 hipError_t launch_grad_norm(const GradArgs& a, void* ws, hipStream_t stream);
 
+// bf16 or fp32 to e4m3 with power-of-two scales (fp8_quantize.hip): blocks of
+// 128 values of a row, or (tiles) of 128 x 128, with the transpose on request.
+struct Fp8QuantArgs {
+  const void* x;     // [M x K]
+  int x_type;
+  int M, K;
+  bool tiles;
+  uint8_t* q;        // [M x K]
+  uint8_t* scale;    // [M or ceil(M / 128) x ceil(K / 128)]
+  uint8_t* qt;       // [K x M] or nullptr
+  uint8_t* scale_t;  // [ceil(K / 128) x ceil(M / 128)]
+};
+hipError_t launch_fp8_quantize(const Fp8QuantArgs& a, hipStream_t stream);
+
+// The dual-output linear over an 8-bit weight (fp8_linear.hip).  Where the LoRA
+// update's s T comes from: `part`, nch partial sums [nch][M][rp] of T, or `ts`,
+// hi and lo parts of s T [M x 2 rp].  drop > 0: the update goes through the
+// dropout mask of rng (an element's 16 bits below `drop`: 0, else times keep).
+struct Fp8LinearArgs {
+  const uint16_t* xh;  // [M x K] bf16 values of x (fp8_wide), or
+  const uint8_t* xq;   // [M x K] their bytes
+  const uint8_t* xs;   // [M x ceil(K / 128)] and scales
+  const uint8_t* wq;   // [N x K]
+  const uint8_t* ws;   // [ceil(N / 128) x ceil(K / 128)]
+  int M, N, K;
+  void* y_off;         // [M x N] or nullptr
+  void* y_on;          // [M x N] or nullptr
+  int y_type;
+  int r, rp;           // rank and padded rank (0: no update)
+  float s;
+  const float* part;
+  int nch;
+  const uint16_t* ts;
+  const uint16_t* B;   // [N x ldb], the first r columns
+  int ldb;
+  uint32_t drop;
+  float keep;
+  const uint64_t* rng;
+};
+// Whether the product takes the values of x as bf16, or bytes and scales.
+bool fp8_wide(int M, int y_type);
+// What the linear needs before its product: x quantized, as bytes and scales or
+// (xh) as the values that they stand for; or values from bytes (q_in, s_in) that
+// are there; and the partial sums of T = xa A^T (A nullptr: not).
+struct Fp8PrepArgs {
+  const uint16_t* x;   // [M x K] bf16, or nullptr
+  const uint8_t* q_in; // [M x K], or nullptr
+  const uint8_t* s_in;
+  const uint16_t* xa;  // [M x K] bf16: x itself, or the adapter's own input
+  const uint16_t* A;   // [r x K] bf16
+  int M, K, r, rp;
+  uint16_t* xh;
+  uint8_t* xq;
+  uint8_t* xs;
+  float* part;         // [nch][M][rp]
+  int nch, kch;        // chunks of K, of kch blocks of 128
+};
+void fp8_prep_chunks(int M, int K, int rp, int& nch, int& kch);
+hipError_t launch_fp8_prep(const Fp8PrepArgs& a, hipStream_t stream);
+hipError_t launch_fp8_linear(const Fp8LinearArgs& a, hipStream_t stream);
+
+// Dropout (dropout.hip): y = res + keep x where the element's 16 random bits are
+// `drop` or more, else res.
+struct DropoutArgs {
+  const void* x;
+  const void* res;       // or nullptr
+  void* y;
+  int x_type, res_type, y_type;
+  int64_t n;
+  uint32_t drop;         // 0 ... 65536
+  float keep;
+  const uint64_t* rng;   // seed, offset
+};
+hipError_t launch_dropout(const DropoutArgs& a, hipStream_t stream);
+// The two numbers of a probability p: drop = round(65536 p), keep = 65536 / (65536 - drop).
+inline void dropout_numbers(double p, uint32_t& drop, float& keep) {
+  drop = (uint32_t)__builtin_rint(p * 65536.0);
+  keep = drop < 65536 ? (float)(65536.0 / (double)(65536 - drop)) : 0.f;
+}
+
+// Drafted tokens against the target's probabilities (verify_drafts.hip).
+constexpr int kMaxDrafts = 128;
+struct VerifyArgs {
+  const void* z;           // n (k + 1) rows of V
+  const void* zd;          // n k rows of V, or nullptr: drafts without a distribution
+  int z_type, d_type;
+  int64_t ld, ld_d;
+  const int32_t* drafts;   // [n x k]
+  const int32_t* lens;     // [n] or nullptr
+  const float* u;          // [n x (k + 1)]
+  int n, k, V;
+  double inv_t;            // 1 / temperature
+  int32_t* accepted;       // [n]
+  int32_t* tokens;         // [n x (k + 1)]
+  float* lp;               // [n x (k + 1)] or nullptr
+  int32_t* err;            // optional
+};
+size_t verify_ws_bytes(int n, int k, int V);
+hipError_t launch_verify(const VerifyArgs& a, void* ws, hipStream_t stream);
+
 // Backward of the LoRA-switchable linear with W frozen (see lora_backward.hip).
 struct BackwardArgs {
   const uint16_t* x;   // [M x K]
@@ -288,6 +388,9 @@ struct BackwardArgs {
   float* dx;           // [M x K] or nullptr
   float* dA;           // [r x K] or nullptr
   float* dB;           // [N x r] or nullptr
+  // W in 8 bits: Wt and dx null, and what the product over it takes in their
+  // place (xh, or xq and xs: room for dy's; y_on: dx, of y_type; drop: the mask)
+  const Fp8LinearArgs* base8;
 };
 // Workspace bytes of the backward, and the launcher (which assumes a
 // workspace of at least that size, 16-byte aligned).

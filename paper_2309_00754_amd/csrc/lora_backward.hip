@@ -346,6 +346,25 @@ size_t backward_ws_bytes(int M, int N, int K, int rp) { return rp == 0 ? 0 : lay
 hipError_t launch_lora_backward(const BackwardArgs& a, void* ws, hipStream_t stream) {
   const int rp = padded_rank(a.r);
   hipError_t e;
+  // dx over a weight in 8 bits: dy's bytes, then the product with its update
+  auto dx_over_8 = [&](const uint16_t* ts, const uint16_t* at) {
+    Fp8LinearArgs g = *a.base8;
+    Fp8PrepArgs q{};
+    q.x = q.xa = a.dy;
+    q.M = a.M;
+    q.K = a.N;
+    q.xh = const_cast<uint16_t*>(g.xh);
+    q.xq = const_cast<uint8_t*>(g.xq);
+    q.xs = const_cast<uint8_t*>(g.xs);
+    fp8_prep_chunks(q.M, q.K, 0, q.nch, q.kch);
+    const hipError_t err = launch_fp8_prep(q, stream);
+    if (err != hipSuccess) return err;
+    g.ts = ts;
+    g.B = at;
+    g.r = g.rp = g.ldb = rp;
+    return launch_fp8_linear(g, stream);
+  };
+  if (rp == 0 && a.base8) return dx_over_8(nullptr, nullptr);
   if (rp == 0) {  // no adapter: dx = dy W only
     if (!a.dx) return hipSuccess;
     LinearArgs g{};
@@ -361,7 +380,8 @@ hipError_t launch_lora_backward(const BackwardArgs& a, void* ws, hipStream_t str
   uint8_t* w = static_cast<uint8_t*>(ws);
   uint16_t* bt = reinterpret_cast<uint16_t*>(w + l.bt);
   uint16_t* at = reinterpret_cast<uint16_t*>(w + l.at);
-  const bool want_u = a.dx || a.dA;  // s U = s dy B
+  const bool want_dx = a.dx || a.base8;
+  const bool want_u = want_dx || a.dA;  // s U = s dy B
   const bool want_t = a.dB != nullptr;  // s T = s x A^T
 
   // 1. B^T [RP x N] (for s U) and A^T [K x RP] (the dx GEMM's LoRA rows), one launch
@@ -369,7 +389,7 @@ hipError_t launch_lora_backward(const BackwardArgs& a, void* ws, hipStream_t str
     int n0 = 0, n1 = 0;
     TransposeJob j0{}, j1{};
     if (want_u) j0 = transpose_job(a.B, a.N, a.r, bt, a.N, rp, n0);
-    if (a.dx) j1 = transpose_job(a.A, a.r, a.K, at, rp, a.K, n1);
+    if (want_dx) j1 = transpose_job(a.A, a.r, a.K, at, rp, a.K, n1);
     if (n0 + n1 > 0) {
       hipLaunchKernelGGL(transpose_pad_kernel, dim3(n0 + n1), dim3(256), 0, stream, j0, n0, j1);
       if ((e = hipGetLastError()) != hipSuccess) return e;
@@ -385,7 +405,7 @@ hipError_t launch_lora_backward(const BackwardArgs& a, void* ws, hipStream_t str
   u.r = a.r;
   u.Kform = tt.Kform = std::max(a.N, a.K);
   u.Kall = tt.Kall = a.N + a.K;
-  u.ts = a.dx ? reinterpret_cast<uint16_t*>(w + l.tsu) : nullptr;
+  u.ts = want_dx ? reinterpret_cast<uint16_t*>(w + l.tsu) : nullptr;
   u.part = reinterpret_cast<float*>(w + l.tpart);
   u.tT = a.dA ? reinterpret_cast<uint16_t*>(w + l.uT) : nullptr;
   u.Mp = padded_rows(a.M);
@@ -404,7 +424,9 @@ hipError_t launch_lora_backward(const BackwardArgs& a, void* ws, hipStream_t str
     e = launch_lora_tpre(want_u ? u : tt, rp, nullptr, stream);
   if (e != hipSuccess) return e;
   // 3. dx = dy W + s U A: the GEMM over W^T with slabs ([hi | lo](s U), A^T)
-  if (a.dx) {
+  if (a.base8) {
+    if ((e = dx_over_8(u.ts, at)) != hipSuccess) return e;
+  } else if (a.dx) {
     LinearArgs g{};
     g.x = a.dy;
     g.W = a.Wt;

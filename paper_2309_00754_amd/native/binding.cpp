@@ -23,7 +23,8 @@ namespace {
 
 constexpr long kSlow = -1000;
 
-enum Kind { kBf16, kF32, kI32, kU8, kAny };  // kAny: bf16 or fp32
+// kAny: bf16 or fp32; kFp8: e4m3; kScale: a scale byte; kI64: 64-bit whole numbers
+enum Kind { kBf16, kF32, kI32, kU8, kAny, kFp8, kScale, kI64 };
 
 // Collects the arguments of one call; ok turns false at the first that is not
 // of the accepted form.
@@ -44,6 +45,9 @@ struct Take {
                        : kind == kF32  ? d == at::kFloat
                        : kind == kI32  ? d == at::kInt
                        : kind == kU8   ? d == at::kByte
+                       : kind == kFp8  ? d == at::kFloat8_e4m3fn || d == at::kByte
+                       : kind == kScale ? d == at::kFloat8_e8m0fnu || d == at::kByte
+                       : kind == kI64  ? d == at::kLong || d == at::kUInt64
                                        : d == at::kBFloat16 || d == at::kFloat || d == at::kShort || d == at::kUInt16;
     ok = t.is_cuda() && dtype && (rows_apart || t.is_contiguous());
     if (!ok) return nullptr;
@@ -148,18 +152,19 @@ struct Take {
     bytes = (size_t)t->numel();
     return t->data_ptr();
   }
-  float real(PyObject* o) {
+  double number(PyObject* o) {
     if (!PyFloat_Check(o) && !PyLong_CheckExact(o)) {
       ok = false;
-      return 0.f;
+      return 0.0;
     }
     const double v = PyFloat_AsDouble(o);
     if (v == -1.0 && PyErr_Occurred()) {
       PyErr_Clear();
       ok = false;
     }
-    return (float)v;
+    return v;
   }
+  float real(PyObject* o) { return (float)number(o); }
   int64_t whole(PyObject* o) {
     if (!PyLong_CheckExact(o)) {
       ok = false;
@@ -612,12 +617,148 @@ HYDRA_PY(grad_clip, 7) {
   });
 }
 
+// x q scale block_rows qt scale_t stream
+HYDRA_PY(fp8_quantize, 7) {
+  return guarded([&](Take& a) {
+    const at::Tensor* x = a.tensor(v[0], kAny);
+    a.ok = a.ok && x && x->dim() == 2;
+    const int64_t M = a.ok ? x->size(0) : 0, K = a.ok ? x->size(1) : 0;
+    const void* xp = a.ok ? x->data_ptr() : nullptr;
+    const hydra_dtype xt = Take::type_of(x);
+    const int64_t rows = a.whole(v[3]);
+    a.ok = a.ok && (rows == 1 || rows == 128);
+    const int64_t kb = (K + 127) / 128, mb = a.ok ? (M + rows - 1) / rows : 0;
+    uint8_t* q = a.at2<uint8_t>(v[1], kFp8, M, K);
+    uint8_t* scale = a.at2<uint8_t>(v[2], kScale, mb, kb);
+    uint8_t* qt = a.at2<uint8_t>(v[4], kFp8, K, M);
+    uint8_t* st = a.at2<uint8_t>(v[5], kScale, kb, mb);
+    void* stream = a.stream_here(v[6]);
+    return [=]() { return hydra_fp8_quantize(xp, xt, M, K, rows, q, scale, qt, st, stream); };
+  });
+}
+
+// x Wq w_scale A B s y_off y_on x_adapter xq x_scale workspace stream
+HYDRA_PY(fp8_lora_linear, 13) {
+  return guarded([&](Take& a) {
+    const int64_t N = a.rows(v[1]), r = a.rows(v[3]);
+    const at::Tensor* W = a.tensor(v[1], kFp8);
+    a.ok = a.ok && W && W->dim() == 2;
+    const int64_t K = a.ok ? W->size(1) : 0, kb = (K + 127) / 128;
+    const uint8_t* Wp = a.ok ? static_cast<const uint8_t*>(W->data_ptr()) : nullptr;
+    const int64_t M = a.rows(v[0] != Py_None ? v[0] : v[9]);
+    const uint16_t* x = a.at2<uint16_t>(v[0], kBf16, M, K);
+    const uint8_t* ws = a.at2<uint8_t>(v[2], kScale, (N + 127) / 128, kb);
+    const uint16_t* A = a.at2<uint16_t>(v[3], kBf16, r, K);
+    const uint16_t* B = a.at2<uint16_t>(v[4], kBf16, N, r);
+    const float s = a.real(v[5]);
+    hydra_dtype ot, nt;
+    void* yo = a.any2(v[6], M, N, ot);
+    void* yn = a.any2(v[7], M, N, nt);
+    a.ok = a.ok && (!yo || !yn || ot == nt);
+    const uint16_t* xa = a.at2<uint16_t>(v[8], kBf16, M, K);
+    const uint8_t* xq = a.at2<uint8_t>(v[9], kFp8, M, K);
+    const uint8_t* xs = a.at2<uint8_t>(v[10], kScale, M, kb);
+    size_t bytes = 0;
+    void* w = a.workspace(v[11], bytes);
+    void* st = a.stream_here(v[12]);
+    return [=]() {
+      return hydra_fp8_lora_linear(x, xa, xq, xs, Wp, ws, A, B, s, M, N, K, r, yo, yn, yo ? ot : nt, w, bytes, st);
+    };
+  });
+}
+
+// x Wqt wt_scale A B s dy dx dA dB p rng workspace stream
+HYDRA_PY(fp8_lora_linear_backward, 14) {
+  return guarded([&](Take& a) {
+    int64_t M = 0, N = 0, K = 0;
+    const uint16_t* dy = a.matrix(v[6], M, N);
+    const int64_t r = a.rows(v[3]);
+    // K from the first of A, x and Wqt that is there
+    PyObject* const from = v[3] != Py_None ? v[3] : v[0] != Py_None ? v[0] : v[1];
+    a.ok = a.ok && THPVariable_CheckExact(from) && THPVariable_Unpack(from).dim() == 2;
+    if (a.ok) K = THPVariable_Unpack(from).size(from == v[1] ? 0 : 1);
+    const int64_t nb = (N + 127) / 128;
+    const uint16_t* x = a.at2<uint16_t>(v[0], kBf16, M, K);
+    const uint8_t* W = a.at2<uint8_t>(v[1], kFp8, K, N);
+    const uint8_t* ws = a.at2<uint8_t>(v[2], kScale, (K + 127) / 128, nb);
+    const uint16_t* A = a.at2<uint16_t>(v[3], kBf16, r, K);
+    const uint16_t* B = a.at2<uint16_t>(v[4], kBf16, N, r);
+    const float s = a.real(v[5]);
+    hydra_dtype dt;
+    void* dx = a.any2(v[7], M, K, dt);
+    float* dA = a.at2<float>(v[8], kF32, r, K);
+    float* dB = a.at2<float>(v[9], kF32, N, r);
+    const double p = a.number(v[10]);
+    const uint64_t* rng = a.at1<uint64_t>(v[11], kI64, 2);
+    size_t bytes = 0;
+    void* w = a.workspace(v[12], bytes);
+    void* st = a.stream_here(v[13]);
+    return [=]() {
+      return hydra_fp8_lora_linear_backward(x, W, ws, A, B, s, dy, M, N, K, r, p, rng, dx, dt, dA, dB, w, bytes, st);
+    };
+  });
+}
+
+// x y p rng residual stream
+HYDRA_PY(dropout, 6) {
+  return guarded([&](Take& a) {
+    const at::Tensor* x = a.tensor(v[0], kAny);
+    const at::Tensor* y = a.tensor(v[1], kAny);
+    const double p = a.number(v[2]);
+    const uint64_t* rng = a.at1<uint64_t>(v[3], kI64, 2);
+    const at::Tensor* res = a.tensor(v[4], kAny);
+    a.ok = a.ok && x && y && y->sizes() == x->sizes() && (!res || res->sizes() == x->sizes());
+    const void* xp = a.ok ? x->data_ptr() : nullptr;
+    void* yp = a.ok ? y->data_ptr() : nullptr;
+    const void* rp = a.ok && res ? res->data_ptr() : nullptr;
+    const int64_t n = a.ok ? x->numel() : 0;
+    const hydra_dtype xt = Take::type_of(x), yt = Take::type_of(y), rt = Take::type_of(res);
+    void* st = a.stream_here(v[5]);
+    return [=]() { return hydra_dropout(xp, xt, rp, rt, p, rng, n, yp, yt, st); };
+  });
+}
+
+// target draft drafts u accepted tokens lp lens temperature workspace err_flag stream
+HYDRA_PY(verify_drafts, 12) {
+  return guarded([&](Take& a) {
+    int64_t Mt = 0, V = 0, ld = 0, Md = 0, Vd = 0, ld_d = 0;
+    hydra_dtype zt = HYDRA_BF16, dt = HYDRA_BF16;
+    const void* z = a.rows_of(v[0], Mt, V, zt, ld);
+    const at::Tensor* u = a.tensor(v[3], kF32);
+    a.ok = a.ok && u && u->dim() == 2 && u->size(1) >= 1;
+    const int64_t n = a.ok ? u->size(0) : 0, k = a.ok ? u->size(1) - 1 : 0;
+    const void* zd = nullptr;
+    if (a.ok && v[1] != Py_None) {
+      zd = a.rows_of(v[1], Md, Vd, dt, ld_d);
+      a.ok = a.ok && Md == n * k && Vd == V;
+    }
+    a.ok = a.ok && Mt == n * (k + 1);
+    const float* up = a.at2<float>(v[3], kF32, n, k + 1);
+    const int32_t* drafts = a.at2<int32_t>(v[2], kI32, n, k);
+    int32_t* accepted = a.at1<int32_t>(v[4], kI32, n);
+    int32_t* tokens = a.at2<int32_t>(v[5], kI32, n, k + 1);
+    float* lp = a.at2<float>(v[6], kF32, n, k + 1);
+    const int32_t* lens = a.at1<int32_t>(v[7], kI32, n);
+    const double temperature = a.number(v[8]);
+    size_t bytes = 0;
+    void* w = a.workspace(v[9], bytes);
+    int32_t* err = a.at1<int32_t>(v[10], kI32, 1);
+    void* st = a.stream_here(v[11]);
+    return [=]() {
+      return hydra_verify_drafts(z, zt, ld, zd, dt, ld_d, drafts, lens, up, n, k, V, temperature, accepted, tokens, lp, w,
+                                 bytes, err, st);
+    };
+  });
+}
+
 #define HYDRA_DEF(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {HYDRA_DEF(lora_linear),  HYDRA_DEF(lora_linear_group), HYDRA_DEF(lora_linear_multi),
                          HYDRA_DEF(score),        HYDRA_DEF(score_logits),      HYDRA_DEF(value_head),
                          HYDRA_DEF(ppo_advantages), HYDRA_DEF(ppo_loss),        HYDRA_DEF(lora_linear_backward),
                          HYDRA_DEF(layer_norm),   HYDRA_DEF(layer_norm_backward), HYDRA_DEF(token_logprobs),
                          HYDRA_DEF(token_logprobs_backward), HYDRA_DEF(grad_clip),
+                         HYDRA_DEF(fp8_quantize), HYDRA_DEF(fp8_lora_linear), HYDRA_DEF(fp8_lora_linear_backward),
+                         HYDRA_DEF(dropout),      HYDRA_DEF(verify_drafts),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_hydra_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

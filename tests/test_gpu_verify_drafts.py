@@ -1,0 +1,285 @@
+"""hydra_verify_drafts against the oracle: whole numbers exactly, log-probabilities to their rounding; vocabularies that
+end inside a segment, masks, rows without a distribution, drafts and lengths out of order, strides, alignments, graphs."""
+import numpy as np
+import pytest
+
+import paper_2309_00754_amd as H
+from oracle import verify_ref
+from gpu_helpers import say
+from base8_helpers import U, f64, put
+
+pytestmark = pytest.mark.gpu
+
+
+class Case:
+    def __init__(self, seed, n, k, V, dev, zt="f32", dt="f32", ragged=False, draft=True, spread=2.0, shift=0, ld=0, edit=None,
+                 T=1.0):
+        import torch
+        r = np.random.default_rng(seed)
+        self.n, self.k, self.V, self.T = n, k, V, T
+        z = r.normal(0, spread, (n, k + 1, V))
+        zd = z[:, :k] + r.normal(0, 0.7, (n, k, V))
+        g = -np.log(-np.log(r.uniform(1e-12, 1 - 1e-12, (n, k, V))))
+        self.drafts = (zd / T + g).argmax(2).astype(np.int32)
+        self.u = r.uniform(0, 1, (n, k + 1)).astype(np.float32)
+        self.lens = r.integers(0, k + 1, n).astype(np.int32) if ragged else None
+        if edit:
+            edit(self, z, zd)
+        self.dz = put(z.reshape(n * (k + 1), V), zt, dev, shift=shift, stride=ld)
+        self.dzd = put(zd.reshape(n * k, V), dt, dev, shift=shift, stride=ld) if draft and k else None
+        self.dev = dev
+
+        def i32(a):
+            return torch.as_tensor(np.asarray(a, np.int32)).to(dev)
+
+        self.ddrafts, self.dlens = i32(self.drafts), None if self.lens is None else i32(self.lens)
+        self.du = torch.as_tensor(self.u).to(dev)
+        self.acc, self.tok = i32(np.full(n, -7)), i32(np.full((n, k + 1), -7))
+        self.lp, self.err = torch.full((n, k + 1), 9.0, device=dev), i32([0])
+        self.ws = torch.full((H.hydra_verify_drafts_workspace_bytes(n, k, V),), 0xFF, dtype=torch.uint8, device=dev)
+
+    def run(self, stream=None, **kw):
+        H.hydra_verify_drafts(self.dz, self.dzd, self.ddrafts, self.du, self.acc, self.tok, self.lp, self.dlens, self.T,
+                              self.ws, self.err, stream=stream, **kw)
+
+    def check(self, odd=False):
+        import torch
+        torch.cuda.synchronize()
+        n, k, V = self.n, self.k, self.V
+        z = f64(self.dz).reshape(n, k + 1, V)
+        zd = None if self.dzd is None else f64(self.dzd).reshape(n, k, V)
+        acc, tok, lp, was_odd = verify_ref(z, zd, self.drafts, self.lens, self.u, self.T)
+        assert np.array_equal(self.acc.cpu().numpy(), acc), "accepted"
+        assert np.array_equal(self.tok.cpu().numpy(), tok), "tokens"
+        got = f64(self.lp)
+        assert np.array_equal(np.isnan(got), np.isnan(lp))
+        # 64-bit sums of up to 2^21 exponentials, each to 1e-14, then one rounding to fp32
+        assert np.all(np.abs(got - lp)[~np.isnan(lp)] <= (U * np.abs(lp) + 1e-9)[~np.isnan(lp)])
+        assert bool(self.err.item()) == was_odd == odd
+
+
+@pytest.mark.parametrize("n,k,V", [(1, 0, 1), (1, 1, 1), (3, 2, 2), (2, 5, 1000), (5, 3, 4096), (3, 7, 4097), (2, 4, 8191),
+                                   (1, 5, 32000), (2, 3, 50272), (40, 1, 300), (1, 128, 64), (2, 1, 70001)])
+@pytest.mark.parametrize("draft", [True, False])
+def test_verify(dev, n, k, V, draft):
+    say("verify", n, k, V, draft)
+    c = Case(n * 1000 + k, n, k, V, dev, draft=draft)
+    c.run()
+    c.check()
+
+
+@pytest.mark.parametrize("zt", ["bf16", "f32"])
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [0.3, 1.0, 2.5])
+def test_types_temperatures_lengths(dev, zt, dt, T):
+    c = Case(11, 24, 5, 3001, dev, zt, dt, ragged=True, T=T)
+    c.run()
+    c.check()
+
+
+@pytest.mark.parametrize("shift,ld", [(1, 0), (2, 0), (0, 3008), (0, 3003), (3, 3001)])
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+def test_alignments_and_strides(dev, t, shift, ld):
+    """Rows apart (the gaps hold NaN), off their boundaries, of odd length."""
+    c = Case(12, 6, 3, 3000 if ld != 3001 else 3001, dev, t, t, shift=shift, ld=ld)
+    c.run()
+    c.check()
+
+
+def test_many_samples_follow_the_target(dev):
+    """What comes out first, over many sequences of one distribution: the target's own frequencies."""
+    n, V = 20000, 12
+
+    def edit(c, z, zd):
+        z[:], zd[:] = z[:1], zd[:1]
+        r = np.random.default_rng(1)
+        g = -np.log(-np.log(r.uniform(1e-12, 1 - 1e-12, zd.shape)))
+        c.drafts = (zd + g).argmax(2).astype(np.int32)
+
+    c = Case(13, n, 1, V, dev, spread=1.5, edit=edit)
+    c.run()
+    z = f64(c.dz)[0]
+    p = np.exp(z - z.max())
+    p /= p.sum()
+    seen = np.bincount(c.tok.cpu().numpy()[:, 0], minlength=V) / n
+    assert np.all(np.abs(seen - p) <= 6 * np.sqrt(p * (1 - p) / n) + 1e-9)
+
+
+def test_equal_rows_accept_every_draft(dev):
+    def edit(c, z, zd):
+        zd[:] = z[:, :c.k]
+        c.u[:, :c.k] = 1 - 2.0 ** -24
+
+    c = Case(14, 5, 6, 5000, dev, edit=edit)
+    c.run()
+    c.check()
+    assert np.all(c.acc.cpu().numpy() == 6)
+
+
+def test_masks(dev):
+    """Most of the vocabulary masked out of the target, the draft, or both; whole segments of -inf; a single token left;
+    drafts that the target masks (never accepted, at u = 0 either)."""
+    def edit(c, z, zd):
+        r = np.random.default_rng(15)
+        z[0][r.uniform(0, 1, z[0].shape) < 0.99] = -np.inf
+        z[0][:, 77] = 0.0
+        zd[1][r.uniform(0, 1, zd[1].shape) < 0.9] = -np.inf
+        zd[1][:, 5] = 0.0
+        c.drafts[1] = 5
+        z[2][:, :9000] = -np.inf
+        z[3][:, 1:] = -np.inf
+        z[4][:, :4096], zd[4][:, 4096:] = -np.inf, -np.inf
+        c.drafts[4] = 17
+        c.u[3:5, :c.k] = 0.0
+
+    for draft in (True, False):
+        c = Case(15, 6, 3, 9300, dev, draft=draft, edit=edit)
+        c.run()
+        c.check()
+
+
+def test_lowest_values_and_wide_rows(dev):
+    """Logits of the type's lowest value, in place of -inf; rows 1e30 wide."""
+    low = float(np.finfo(np.float32).min)
+
+    def edit(c, z, zd):
+        z[0][:, 3:] = low
+        zd[0][:, 2:] = low
+        c.drafts[0] = [0, 1]
+        z[1] *= 1e30
+        z[2][:] = low  # all alike
+
+    c = Case(16, 4, 2, 5003, dev, edit=edit)
+    c.run()
+    c.check()
+
+
+def test_rows_without_a_distribution(dev):
+    def edit(c, z, zd):
+        z[0, 0, 5] = np.nan
+        z[1, 1] = -np.inf
+        z[2, 3, 4999] = np.inf
+        zd[3, 0, 10] = np.nan
+        zd[4, 1] = -np.inf
+        c.u[:, :c.k] = 0.0  # accepted, where they can be
+
+    c = Case(17, 6, 3, 5000, dev, edit=edit)
+    c.run()
+    c.check(odd=True)
+
+
+@pytest.mark.parametrize("reached", [False, True])
+def test_a_bad_row_that_is_not_reached_does_not_count(dev, reached):
+    def edit(c, z, zd):
+        c.lens = np.array([1, 3], np.int32)
+        z[0, 2:], zd[0, 1:] = np.nan, np.nan
+        c.drafts[0, 1:] = 1 << 30
+        c.u[1, 0] = 0.99999
+        t = c.drafts[1, 0] = z[1, 0].argmin()
+        # the least likely token: of this draft's own distribution less likely still, and accepted; or more, and rejected
+        if not reached:
+            zd[1, 0, t] = z[1, 0, t] + 3
+        z[1, 2], zd[1, 1] = np.nan, np.nan
+
+    c = Case(18, 2, 3, 4000, dev, edit=edit)
+    c.run()
+    c.check(odd=reached)
+
+
+@pytest.mark.parametrize("tok", [-1, 5000, 1 << 30, -(1 << 31)])
+def test_drafts_outside_the_vocabulary(dev, tok):
+    def edit(c, z, zd):
+        c.drafts[1, 2] = tok
+        c.u[:, :c.k] = 0.0
+
+    for draft in (True, False):
+        c = Case(19, 3, 4, 5000, dev, draft=draft, edit=edit)
+        c.run()
+        c.check(odd=True)
+
+
+def test_lengths_outside_their_range(dev):
+    def edit(c, z, zd):
+        c.lens = np.array([-3, 99, 2], np.int32)
+
+    c = Case(20, 3, 4, 1000, dev, edit=edit)
+    c.run()
+    c.check(odd=True)
+
+
+@pytest.mark.parametrize("u", [0.0, 1.0, 2.0, -1.0, float("nan")])
+def test_random_numbers_at_and_past_their_ends(dev, u):
+    """0 takes the first token with a probability, 1 and more (and NaN) the last."""
+    import torch
+
+    def edit(c, z, zd):
+        z[:, :, :3], z[:, :, 4990:] = -np.inf, -np.inf
+
+    c = Case(21, 2, 0, 5000, dev, edit=edit)
+    c.du.fill_(u)
+    c.run()
+    torch.cuda.synchronize()
+    assert np.all(c.tok.cpu().numpy() == (3 if u <= 0 else 4989))
+
+
+def test_outputs_that_are_not_asked_for_and_own_workspace(dev):
+    import torch
+    c = Case(22, 4, 3, 2000, dev, ragged=True)
+    c.run()
+    c.check()
+    acc, tok = torch.empty_like(c.acc), torch.empty_like(c.tok)
+    H.hydra_verify_drafts(c.dz, c.dzd, c.ddrafts, c.du, acc, tok, None, c.dlens)
+    assert torch.equal(acc, c.acc) and torch.equal(tok, c.tok)
+
+
+def test_streams_and_a_replayed_graph(dev):
+    import torch
+    c = Case(23, 6, 4, 9000, dev, "bf16", "f32", ragged=True)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    c.run(stream=side)
+    side.synchronize()
+    c.check()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        c.run()
+    for seed in range(4):
+        o = Case(100 + seed, 6, 4, 9000, dev, "bf16", "f32", ragged=True)
+        for name in ("dz", "dzd", "ddrafts", "du", "dlens"):
+            getattr(c, name).copy_(getattr(o, name))
+        c.drafts, c.u, c.lens = o.drafts, o.u, o.lens
+        c.ws.fill_(0x5A)
+        g.replay()
+        c.check()
+
+
+def test_two_calls_at_once(dev):
+    import torch
+    cs = [Case(30 + i, 8, 5, 20000, dev, ragged=True) for i in range(2)]
+    ss = [torch.cuda.Stream() for _ in cs]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for c, s in zip(cs, ss):
+            c.run(stream=s)
+    torch.cuda.synchronize()
+    for c in cs:
+        c.check()
+
+
+def test_shapes_that_do_not_fit_are_refused(dev):
+    import torch
+    c = Case(24, 2, 2, 100, dev)
+    with pytest.raises(ValueError):
+        H.hydra_verify_drafts(c.dz[:5], c.dzd, c.ddrafts, c.du, c.acc, c.tok)
+    with pytest.raises(ValueError):
+        H.hydra_verify_drafts(c.dz, c.dzd[:, :99], c.ddrafts, c.du, c.acc, c.tok)
+    with pytest.raises(ValueError):
+        H.hydra_verify_drafts(c.dz, c.dzd, c.ddrafts[:, :1].contiguous(), c.du, c.acc, c.tok)
+    with pytest.raises(TypeError):
+        H.hydra_verify_drafts(c.dz, c.dzd, c.ddrafts.long(), c.du, c.acc, c.tok)
+    with pytest.raises(ValueError):
+        H.hydra_verify_drafts(c.dz, c.dzd, c.ddrafts, c.du, c.acc[:1], c.tok)
+    with pytest.raises(H.HydraError):
+        H.hydra_verify_drafts(c.dz, c.dzd, c.ddrafts, c.du, c.acc, c.tok, temperature=0.0)
+    with pytest.raises(H.HydraError):
+        H.hydra_verify_drafts(c.dz, c.dzd, c.ddrafts, c.du, c.acc, c.tok, workspace=c.ws[:16])
