@@ -784,7 +784,7 @@ hydra_status hydra_fp8_lora_linear_workspace_bytes(int64_t M, int64_t K, int64_t
  *   y_off, y_on  [M x N] bf16 or fp32 (y_type, both)   out, each optional, at least one
  *   workspace, workspace_bytes  device, 16-byte aligned, contents ignored and
  *             overwritten; hydra_fp8_lora_linear_workspace_bytes(M, K, r) bytes are
- *             always enough (less, down to NULL, where xq is given, outputs are bf16 and no update is computed)
+ *             always enough (NULL allowed where xq is given and no update is computed)
  * x, x_adapter, xq, Wq and A 16-byte aligned, B 2-byte, outputs at their element's
  * alignment.  Into fp32 outputs, and up to 16 rows, every product is exact and
  * added in fp32; into bf16 outputs of more rows the 8-bit matrix instructions run,
@@ -898,8 +898,9 @@ hydra_status hydra_verify_drafts_workspace_bytes(int64_t n, int64_t k, int64_t V
  *           without a distribution (NaN, +inf, or -inf alone: the next token there is -1, its lp
  *           NaN); for a draft outside [0, V) or with such a draft row, if the drafts before it are accepted
  *           (it counts as no draft: the next token is drawn from p_j); for a length outside [0, k] (the nearest is taken)
- * Exponentials and sums are 64-bit, in a fixed order; where rounding leaves nothing of
- * p_a - q_a, the next token is drawn from p_a.  Requires n >= 1, 0 <= k <= HYDRA_MAX_DRAFTS,
+ * Exponentials and sums are 64-bit, in a fixed order (e^-700 of the largest of a row and
+ * less count as 0); where rounding leaves nothing of p_a - q_a, the next token is drawn
+ * from p_a.  Requires n >= 1, 0 <= k <= HYDRA_MAX_DRAFTS,
  * n (k + 1) <= 2^20, 1 <= V <= 2^21, n (2 k + 1) ceil(V / 4096) < 2^24, ld <= 2^31 - 1; logits at their
  * element's alignment; outputs distinct (HYDRA_ERR_SHAPE).  Calls that share a workspace on
  * different streams race.

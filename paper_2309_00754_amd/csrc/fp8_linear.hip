@@ -4,15 +4,15 @@
 // xh and Wh what the bytes stand for.
 //
 // Two ways to form the base product, by where it ends:
-//  * into bf16 (above 16 rows): the scaled 8-bit matrix instructions, which take
+//  * into bf16 (in fp8_gemm_kernel): the scaled 8-bit matrix instructions, which take
 //    bytes and scales as they are at twice bf16's rate, and whose sums are 2e-5 off
 //    (hydra_fp8.h);
-//  * into fp32, and up to 16 rows, where reading W is what costs: bf16 matrix
-//    instructions on the exact values (four fraction bits of bf16's eight), W's
-//    bytes converted in registers, sums in fp32.
+//  * into fp32, and in fp8_stream_kernel, where reading W is what costs: bf16 matrix
+//    instructions on the exact values (four fraction bits of bf16's eight), the
+//    bytes converted in registers on the way in, sums in fp32.
 // Kernels:
-//  * fp8_prep_kernel reads x once: its bytes and scales, or the bf16 values that
-//    they stand for, and partial sums of T = x A^T for the update;
+//  * fp8_prep_kernel reads x once: its bytes and scales, and partial sums of
+//    T = x A^T for the update;
 //  * fp8_stream_kernel (up to 16 rows) is bound by reading W: every wave takes
 //    blocks of 128 k values of 16 or more rows of W straight into registers;
 //  * fp8_gemm_kernel (more rows): tiles through LDS.
@@ -28,14 +28,6 @@ namespace {
 
 constexpr int P_WAVES = 4;
 
-// What sixteen bytes stand for, to memory as bf16.
-__device__ __forceinline__ void put_values(uint16_t* to, const uint4& q, int byte) {
-  uint4 v[2];
-  fp8_to_bf16(q, byte, v);
-  reinterpret_cast<uint4*>(to)[0] = v[0];
-  reinterpret_cast<uint4*>(to)[1] = v[1];
-}
-
 // 16 rows and one chunk of K a workgroup; a wave takes the chunk's blocks in
 // turn.  Lane l holds values 32 (l / 16) ... + 31 of the block of row l % 16, in
 // four pieces of eight: a block's maximum is over four lanes, its bytes are two
@@ -49,7 +41,7 @@ __global__ __launch_bounds__(P_WAVES * 64) void fp8_prep_kernel(Fp8PrepArgs g) {
   const int K = g.K, kb_n = (K + kFp8Block - 1) / kFp8Block;
   const int m0 = blockIdx.x * 16, rows = min(16, g.M - m0);
   const uint32_t bytes = (uint32_t)rows * K * 2u;
-  const bool quantize = g.x != nullptr, convert = g.q_in != nullptr;
+  const bool quantize = g.x != nullptr;
   const bool same = g.xa == g.x;
   const __amdgpu_buffer_rsrc_t xr = make_rsrc(quantize ? g.x + (size_t)m0 * K : nullptr, quantize ? bytes : 0u);
   const __amdgpu_buffer_rsrc_t ar = make_rsrc(TJ > 0 ? g.xa + (size_t)m0 * K : nullptr, TJ > 0 ? bytes : 0u);
@@ -96,23 +88,12 @@ __global__ __launch_bounds__(P_WAVES * 64) void fp8_prep_kernel(Fp8PrepArgs g) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           if (k + 16 * h >= K) continue;
-          const uint4 q = make_uint4(fp8_pack4(f[2 * h], p), fp8_pack4(f[2 * h] + 4, p), fp8_pack4(f[2 * h + 1], p),
-                                     fp8_pack4(f[2 * h + 1] + 4, p));
-          if (g.xh)
-            put_values(g.xh + at + 16 * h, q, byte);
-          else
-            *reinterpret_cast<uint4*>(g.xq + at + 16 * h) = q;
+          *reinterpret_cast<uint4*>(g.xq + at + 16 * h) =
+              make_uint4(fp8_pack4(f[2 * h], p), fp8_pack4(f[2 * h] + 4, p), fp8_pack4(f[2 * h + 1], p),
+                         fp8_pack4(f[2 * h + 1] + 4, p));
         }
-        if (lg == 0 && !g.xh) g.xs[(size_t)(m0 + l16) * kb_n + kb] = (uint8_t)byte;
+        if (lg == 0) g.xs[(size_t)(m0 + l16) * kb_n + kb] = (uint8_t)byte;
       }
-    }
-    if (convert && l16 < rows) {
-      const size_t at = (size_t)(m0 + l16) * K + k;
-      const int byte = g.s_in[(size_t)(m0 + l16) * kb_n + kb];
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        if (k + 16 * h < K)
-          put_values(g.xh + at + 16 * h, *reinterpret_cast<const uint4*>(g.q_in + at + 16 * h), byte);
     }
   }
   if constexpr (TJ > 0) {
@@ -159,15 +140,16 @@ __global__ __launch_bounds__(S_WAVES * 64) void fp8_stream_kernel(Fp8LinearArgs 
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int M = a.M, N = a.N, K = a.K, kb_n = (K + kFp8Block - 1) / kFp8Block;
   const int n0 = blockIdx.x * 16 * NB;
-  const __amdgpu_buffer_rsrc_t xr = make_rsrc(a.xh, (uint32_t)M * K * 2u);
+  const __amdgpu_buffer_rsrc_t xr = make_rsrc(a.xq, (uint32_t)M * K);
   const __amdgpu_buffer_rsrc_t wr = make_rsrc(a.wq + (size_t)n0 * K, (uint32_t)min(16 * NB, N - n0) * K);
+  const uint8_t* xs = a.xs + (size_t)min(l16, M - 1) * kb_n;
   const uint8_t* ws = a.ws + (size_t)(n0 / kFp8Block) * kb_n;  // (16 NB rows lie in one block of 128)
   f32x4_t acc[NB];
 #pragma unroll
   for (int b = 0; b < NB; ++b) acc[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   for (int kb0 = wave; kb0 < kb_n; kb0 += S_WAVES * U) {
-    uint4 x[U][4], w[U][NB][2];
-    int sw[U];
+    uint4 x[U][2], w[U][NB][2];
+    int sx[U], sw[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int kb = kb0 + u * S_WAVES, k = kb * kFp8Block + 32 * lg;
@@ -177,25 +159,27 @@ __global__ __launch_bounds__(S_WAVES * 64) void fp8_stream_kernel(Fp8LinearArgs 
 #pragma unroll
         for (int b = 0; b < NB; ++b)
           w[u][b][h] = buf_load16(wr, ok ? (b * 16 + l16) * K + k + 16 * h : kOutOfRange);
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-          x[u][2 * h + i] = buf_load16(xr, ok ? (l16 * K + k + 16 * h + 8 * i) * 2 : kOutOfRange);
+        x[u][h] = buf_load16(xr, ok ? l16 * K + k + 16 * h : kOutOfRange);
       }
-      sw[u] = ws[min(kb, kb_n - 1)];
+      const int kc = min(kb, kb_n - 1);
+      sx[u] = xs[kc];
+      sw[u] = ws[kc];
     }
     // lane l has values 32 (l / 16) ... + 31 of a block; the products take eight of
     // every lane at a time
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
+      for (int h = 0; h < 2; ++h) {
+        uint4 xv[2], wv[2];
+        fp8_to_bf16(x[u][h], sx[u], xv);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint4 v[2];
-          fp8_to_bf16(w[u][b][h], sw[u], v);
-          acc[b] = mfma16(v[0], x[u][2 * h], acc[b]);
-          acc[b] = mfma16(v[1], x[u][2 * h + 1], acc[b]);
+        for (int b = 0; b < NB; ++b) {
+          fp8_to_bf16(w[u][b][h], sw[u], wv);
+          acc[b] = mfma16(wv[0], xv[0], acc[b]);
+          acc[b] = mfma16(wv[1], xv[1], acc[b]);
         }
+      }
   }
 #pragma unroll
   for (int b = 0; b < NB; ++b) red[wave][b][lane] = acc[b];
@@ -232,33 +216,35 @@ __global__ __launch_bounds__(S_WAVES * 64) void fp8_stream_kernel(Fp8LinearArgs 
 struct GemmArgs {
   Fp8LinearArgs a;
   int ntm, ntn, total;
-  int vec4;   // outputs in stores of four values
+  int vec;    // outputs in 16-byte stores
   int bvec;   // B in 16-byte loads
   int64_t xs_bytes, ws_bytes;
 };
 
 // TM x TN tile, WM x WN sub-tile a wave, KS waves a sub-tile (each takes its share
 // of every slab), slabs of BK values of K in a ring of NS; four more waves copy.
-// WIDE: x in bf16 and bf16 products, in steps of 32 values of K; else steps of 64.
+// WIDE: bf16 products, in steps of 32 values of K, into fp32 outputs; else 8-bit ones, in
+// steps of 64, into bf16.
 template <bool WIDE_, int TM_, int TN_, int WM_, int WN_, int KS_, int BK_, int NS_>
 struct Tile {
   static constexpr bool WIDE = WIDE_;
   static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, KS = KS_, BK = BK_, NS = NS_;
   static constexpr int NWN = TN / WN, NMW = TM / WM * NWN * KS, NW = NMW + 4, NT = NW * 64;
-  static constexpr int MT = WM / 32, NTL = WN / 32, NQ = MT * NTL, NU = NQ * 4;
-  static constexpr int XCPR = BK * (WIDE ? 2 : 1) / 16, WCPR = BK / 16;  // 16-byte chunks of an LDS row
-  static constexpr int XRPB = 64 / XCPR, WRPB = 64 / WCPR;               // rows of a copy instruction
-  static constexpr int XJ = TM / XRPB / 4, WJ = TN / WRPB / 4, DPW = XJ + WJ;  // copies per copy wave and slab
-  static constexpr int STAGE = TM * XCPR + TN * WCPR;  // uint4
+  static constexpr int MT = WM / 32, NTL = WN / 32, NQ = MT * NTL;
+  static constexpr int CPR = BK / 16;             // 16-byte chunks of an LDS row
+  static constexpr int RPB = 64 / CPR;            // rows of a copy instruction
+  static constexpr int XJ = TM / RPB / 4, WJ = TN / RPB / 4, DPW = XJ + WJ;  // copies per copy wave and slab
+  static constexpr int STAGE = (TM + TN) * CPR;   // uint4
   static constexpr int STEP = WIDE ? 32 : 64;
   static constexpr int SPW = BK / STEP / KS;           // steps per wave and slab
-  static constexpr int WR = WIDE ? 1 : 2;              // 16-byte reads of a step's row of W (x: always two)
-  static constexpr int EX = KS > 1 ? NMW * NQ * 4096 : 0;  // bytes of the partial sums
-  // rows of s T (hi | lo) and of B, 16 bytes apart from the next, at padded rank rp
-  static constexpr int lora_bytes(int rp) { return TM * (4 * rp + 16) + TN * (2 * rp + 16); }
+  static constexpr int RD = STEP / 32;                 // 16-byte reads a lane and row in a step
+  static constexpr int OLD = TN + 4;                   // row of the output tile in LDS (fp32, in values)
+  static constexpr int OUT = KS * TM * OLD * 4;        // bytes of the KS partial sums of it
+  // rows of s T (hi | lo) and of B, 16 bytes apart from the next, at padded rank rp, and a mask
+  static constexpr int lora_bytes(int rp) { return TM * (4 * rp + 16) + TN * (2 * rp + 16) + TM * TN / 8; }
   static constexpr size_t cmax(size_t x, size_t y) { return x > y ? x : y; }
-  static constexpr size_t LDS = cmax(cmax(size_t(NS) * STAGE * 16, EX), lora_bytes(128));
-  static_assert(TM % (XRPB * 4) == 0 && TN % (WRPB * 4) == 0 && SPW >= 1 && NU % KS == 0, "whole copies, steps and units");
+  static constexpr size_t LDS = cmax(cmax(size_t(NS) * STAGE * 16, OUT), lora_bytes(128));
+  static_assert(TM % (RPB * 4) == 0 && TN % (RPB * 4) == 0 && SPW >= 1 && TN % 8 == 0, "whole copies, steps and groups");
   static_assert(SPW <= 4 && (SPW == 1 || SPW % 2 == 0), "steps listed below");
   static_assert(WN <= kFp8Block && LDS <= 160 * 1024 && (NS - 2) * DPW < 64, "one scale a sub-tile and slab; LDS; waits");
 };
@@ -296,11 +282,12 @@ __device__ __forceinline__ uint32_t load_scales(const uint8_t* p, int64_t at, in
   return v >> (8 * (int)(at - from));
 }
 
-template <class G>
+// MASK: the update goes through dropout's mask.
+template <class G, bool MASK>
 __global__ __launch_bounds__(G::NT) void fp8_gemm_kernel(GemmArgs g) {
   constexpr int TM = G::TM, TN = G::TN, WM = G::WM, WN = G::WN, KS = G::KS, BK = G::BK, NS = G::NS;
-  constexpr int MT = G::MT, NTL = G::NTL, NQ = G::NQ, NU = G::NU, SPW = G::SPW;
-  constexpr int XCPR = G::XCPR, WCPR = G::WCPR, WBASE = TM * XCPR;  // (W's rows follow x's)
+  constexpr int MT = G::MT, NTL = G::NTL, NQ = G::NQ, SPW = G::SPW;
+  constexpr int CPR = G::CPR, RPB = G::RPB, RD = G::RD;
   __shared__ uint4 sm[G::LDS / 16];
   const Fp8LinearArgs& a = g.a;
   const int M = a.M, N = a.N, K = a.K, kb_n = (K + kFp8Block - 1) / kFp8Block;
@@ -322,39 +309,232 @@ __global__ __launch_bounds__(G::NT) void fp8_gemm_kernel(GemmArgs g) {
   const int m0 = __builtin_amdgcn_readfirstlane(tmi * TM), n0 = __builtin_amdgcn_readfirstlane(tni * TN);
   const int nkt = (K + BK - 1) / BK;
 
-  // LDS chunk of (row, 16-byte chunk c) in rows of `cpr` chunks: c is XOR-ed with
-  // bits of the row, so that 16 consecutive rows' chunks c lie in different banks.
-  auto swz = [](int cpr, int row) __attribute__((always_inline)) {
-    return cpr == 4 ? (row >> 2) & 3 : cpr == 8 ? (row >> 1) & 7 : row & 15;
-  };
-  auto lds_idx = [&](int cpr, int row, int c) __attribute__((always_inline)) { return row * cpr + (c ^ swz(cpr, row)); };
+  // LDS chunk of (row, 16-byte chunk c): c is XOR-ed with bits of the row, so that
+  // 16 consecutive rows' chunks c lie in different banks.  W's rows follow x's.
+  auto swz = [](int row) __attribute__((always_inline)) { return CPR == 8 ? (row >> 1) & 7 : row & 15; };
+  auto lds_idx = [&](int row, int c) __attribute__((always_inline)) { return row * CPR + (c ^ swz(row)); };
 
-  f32x16_t acc[MT][NTL];
   const int mw = wave < G::NMW ? wave : 0;
   const int kg = mw % KS, wt = mw / KS, wr = wt / G::NWN, wc = wt % G::NWN;
+
+  // ---------------------------------------------------------------- epilogue
+  // The accumulators go to LDS as fp32 rows, one copy for each of the KS waves of a
+  // sub-tile; all waves then add the copies up and store whole rows (straight from
+  // the accumulators a store writes 16-byte pieces of 32 rows: 6 us for 2048 x 4096
+  // bf16 outputs, this way N us).
+  float* const out = reinterpret_cast<float*>(sm);
+  // (this thread's number once more, as a value of the epilogue's own: addresses
+  // formed from it are not kept in registers through the main loop)
+  int te = t;
+  constexpr int OLD = G::OLD;
+  auto put = [&](const f32x16_t (&acc)[MT][NTL]) __attribute__((always_inline)) {
+    // acc[mi][ni][4 i + e]: row mi 32 + l32, column ni 32 + 8 i + 4 lh + e
+    const int l32 = te & 31, lh = te >> 5 & 1;
+    float* o = out + (kg * TM + wr * WM + l32) * OLD + wc * WN + 4 * lh;
+#pragma unroll
+    for (int mi = 0; mi < MT; ++mi)
+#pragma unroll
+      for (int ni = 0; ni < NTL; ++ni)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const f32x16_t& v = acc[mi][ni];
+          *reinterpret_cast<f32x4_t*>(o + mi * 32 * OLD + ni * 32 + 8 * i) =
+              f32x4_t{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
+        }
+  };
+  // A thread's groups of consecutive columns, 16 bytes of the output: f(values, row, column).
+  constexpr int w = G::WIDE ? 4 : 8;
+  auto each = [&](auto f) __attribute__((always_inline)) {
+    constexpr int per_row = TN / w, n = TM * per_row;
+#pragma unroll 4
+    for (int i = 0; i < (n + G::NT - 1) / G::NT; ++i) {
+      const int at = i * G::NT + te;
+      if (n % G::NT != 0 && at >= n) break;
+      const int row = at / per_row, col = at % per_row * w;
+      float v[w];
+#pragma unroll
+      for (int q = 0; q < w / 4; ++q) {
+        f32x4_t s = *reinterpret_cast<const f32x4_t*>(out + row * OLD + col + 4 * q);
+#pragma unroll
+        for (int k = 1; k < KS; ++k)
+          s += *reinterpret_cast<const f32x4_t*>(out + (k * TM + row) * OLD + col + 4 * q);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[4 * q + e] = s[e];
+      }
+      f(v, row, col);
+    }
+  };
+  auto store = [&](void* y, const float* v, int row, int col) __attribute__((always_inline)) {
+    if (m0 + row >= M || n0 + col >= N) return;
+    const size_t at = (size_t)(m0 + row) * N + n0 + col;
+    if (g.vec) {
+      if constexpr (w == 4)
+        *reinterpret_cast<f32x4_t*>(static_cast<float*>(y) + at) = f32x4_t{v[0], v[1], v[2], v[3]};
+      else
+        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(y) + at) =
+            make_uint4(f32_to_bf16_pair(v[0], v[1]), f32_to_bf16_pair(v[2], v[3]), f32_to_bf16_pair(v[4], v[5]),
+                       f32_to_bf16_pair(v[6], v[7]));
+    } else {
+#pragma unroll
+      for (int e = 0; e < w; ++e)
+        if (n0 + col + e < N) store_elem(y, w == 4 ? kF32 : kBf16, at + e, v[e]);
+    }
+  };
+  // The rows of s T as bf16 hi and lo parts (2^-17 of a value together) and those
+  // of B, zero padded to rp, to LDS.
+  const int rp = a.rp, lrp = 31 - __builtin_clz(rp | 1), ldt = 2 * rp + 8, ldb = rp + 8;  // (in values)
+  uint16_t* const Ts = reinterpret_cast<uint16_t*>(sm);
+  uint16_t* const Bs = Ts + TM * ldt;
+  auto put_update = [&]() __attribute__((always_inline)) {
+    const int rows = min(TM, M - m0), cols = min(TN, N - n0);
+    if (a.ts) {
+#pragma unroll 1
+      for (int e = te; e < TM * rp / 4; e += G::NT) {  // 16 bytes each
+        const int row = e >> (lrp - 2), c = (e & (rp / 4 - 1)) * 8;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (row < rows) v = *reinterpret_cast<const uint4*>(a.ts + (size_t)(m0 + row) * 2 * rp + c);
+        *reinterpret_cast<uint4*>(Ts + row * ldt + c) = v;
+      }
+    } else {
+      const size_t stride = (size_t)M * rp;
+#pragma unroll 1
+      for (int e = te; e < TM * rp / 4; e += G::NT) {
+        const int row = e >> (lrp - 2), j = (e & (rp / 4 - 1)) * 4;
+        f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+        if (row < rows) {
+          const float* p = a.part + (size_t)(m0 + row) * rp + j;
+#pragma unroll 2
+          for (int c = 0; c < a.nch; ++c) v += *reinterpret_cast<const f32x4_t*>(p + c * stride);
+        }
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float f = a.s * v[i];
+          hi[i] = f32_to_bf16_any(f);
+          lo[i] = (hi[i] & 0x7FFF) < 0x7F80 ? f32_to_bf16_any(f - bf16_to_f32(hi[i])) : 0;  // (none of an infinity)
+        }
+        *reinterpret_cast<uint2*>(Ts + row * ldt + j) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
+        *reinterpret_cast<uint2*>(Ts + row * ldt + rp + j) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+      }
+    }
+    if (g.bvec) {
+#pragma unroll 1
+      for (int e = te; e < TN * rp / 8; e += G::NT) {
+        const int row = e >> (lrp - 3), j = (e & (rp / 8 - 1)) * 8;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (row < cols && j < a.r) v = *reinterpret_cast<const uint4*>(a.B + (size_t)(n0 + row) * a.ldb + j);
+        *reinterpret_cast<uint4*>(Bs + row * ldb + j) = v;
+      }
+    } else {
+#pragma unroll 1
+      for (int e = te; e < TN * rp; e += G::NT) {
+        const int row = e >> lrp, j = e & (rp - 1);
+        Bs[row * ldb + j] = row < cols && j < a.r ? a.B[(size_t)(n0 + row) * a.ldb + j] : (uint16_t)0;
+      }
+    }
+  };
+  // Dropout's mask of the update (N % 8 == 0 here): a bit a column, a byte a block of
+  // the generator.
+  uint8_t* const mask = reinterpret_cast<uint8_t*>(Bs + TN * ldb);
+  auto put_mask = [&]() __attribute__((always_inline)) {
+#pragma unroll 1
+    for (int e = te; e < TM * TN / 8; e += G::NT) {
+      const int row = e / (TN / 8), col = e % (TN / 8) * 8;
+      const uint4 bits = dropout_words(a.rng, ((uint64_t)(m0 + row) * N + n0 + col) >> 3);
+      uint32_t m = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) m |= dropout_keeps(bits, j, a.drop) ? 1u << j : 0u;
+      mask[e] = (uint8_t)m;
+    }
+  };
+  // s T B^T onto the accumulators (of the first of a sub-tile's KS waves): rows of
+  // [B | B] against rows of [hi | lo]
+  auto add_update = [&](f32x16_t (&acc)[MT][NTL]) __attribute__((always_inline)) {
+    if (KS > 1 && kg != 0) return;
+    const int l32 = te & 31, lh = te >> 5 & 1;
+    const uint16_t* const tr = Ts + (wr * WM + l32) * ldt + 8 * lh;
+    const uint16_t* const br = Bs + (wc * WN + l32) * ldb + 8 * lh;
+    if constexpr (!MASK) {
+      for (int k0 = 0; k0 < rp; k0 += 16) {
+        uint4 bf[NTL];
+#pragma unroll
+        for (int ni = 0; ni < NTL; ++ni) bf[ni] = *reinterpret_cast<const uint4*>(br + ni * 32 * ldb + k0);
+#pragma unroll
+        for (int mi = 0; mi < MT; ++mi) {
+          const uint4 hi = *reinterpret_cast<const uint4*>(tr + mi * 32 * ldt + k0);
+          const uint4 lo = *reinterpret_cast<const uint4*>(tr + mi * 32 * ldt + rp + k0);
+#pragma unroll
+          for (int ni = 0; ni < NTL; ++ni) acc[mi][ni] = mfma32(bf[ni], hi, acc[mi][ni]);
+#pragma unroll
+          for (int ni = 0; ni < NTL; ++ni) acc[mi][ni] = mfma32(bf[ni], lo, acc[mi][ni]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int mi = 0; mi < MT; ++mi)
+#pragma unroll
+        for (int ni = 0; ni < NTL; ++ni) {
+          f32x16_t L;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) L[e] = 0.f;
+          for (int k0 = 0; k0 < rp; k0 += 16) {
+            const uint4 bf = *reinterpret_cast<const uint4*>(br + ni * 32 * ldb + k0);
+            L = mfma32(bf, *reinterpret_cast<const uint4*>(tr + mi * 32 * ldt + k0), L);
+            L = mfma32(bf, *reinterpret_cast<const uint4*>(tr + mi * 32 * ldt + rp + k0), L);
+          }
+          // the block's four bytes of this lane's row; elements 4 i + e: bit 4 lh + e of byte i
+          const int at = ((wr * WM + mi * 32 + l32) * TN + wc * WN + ni * 32) / 8;
+          const uint32_t bits = *reinterpret_cast<const uint32_t*>(mask + at) >> (4 * lh);
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            acc[mi][ni][e] += (bits >> (8 * (e / 4) + e % 4)) & 1 ? L[e] * a.keep : 0.f;
+          __builtin_amdgcn_sched_barrier(0);  // (one block's L at a time)
+        }
+    }
+  };
+  // By the role of the wave: `do_put` and `do_add` are nothing on a copy wave.
+  auto finish = [&](auto do_put, auto do_add) __attribute__((always_inline)) {
+    asm volatile("" : "+v"(te));
+    const bool lora = a.y_on && rp > 0;
+    if (a.y_off || !lora) {
+      do_put();
+      __syncthreads();
+      each([&](const float* v, int row, int col) __attribute__((always_inline)) {
+        if (a.y_off) store(a.y_off, v, row, col);
+        if (a.y_on && !lora) store(a.y_on, v, row, col);
+      });
+      if (!lora) return;
+      __syncthreads();
+    }
+    put_update();
+    if constexpr (MASK) put_mask();
+    __syncthreads();
+    do_add();
+    __syncthreads();
+    do_put();
+    __syncthreads();
+    each([&](const float* v, int row, int col) __attribute__((always_inline)) { store(a.y_on, v, row, col); });
+  };
 
   if (wave >= G::NMW) {
     // -------------------------------------------------------------- copy waves
     const int cw = wave - G::NMW;
-    // (a lane's chunk is the same for every block of rows cw + 4 j)
-    const int xl = lane / XCPR, xc = (lane % XCPR) ^ swz(XCPR, cw * G::XRPB + xl);
-    const int wl = lane / WCPR, wch = (lane % WCPR) ^ swz(WCPR, cw * G::WRPB + wl);
-    constexpr int XE = G::WIDE ? 2 : 1;  // bytes of a value of x
-    const char* const xp = G::WIDE ? reinterpret_cast<const char*>(a.xh) : reinterpret_cast<const char*>(a.xq);
-    const i32x4_t xr = make_rsrc_raw(xp + (size_t)m0 * K * XE, (uint32_t)min(TM, M - m0) * K * XE);
+    const int rl = lane / CPR;
+    const int c = (lane % CPR) ^ swz(cw * RPB + rl);  // (the same for every block of rows cw + 4 j)
+    const i32x4_t xr = make_rsrc_raw(a.xq + (size_t)m0 * K, (uint32_t)min(TM, M - m0) * K);
     const i32x4_t wrs = make_rsrc_raw(a.wq + (size_t)n0 * K, (uint32_t)min(TN, N - n0) * K);
     auto issue = [&](int stage, int kt) __attribute__((always_inline)) {
-      const int xk = kt * BK * XE + xc * 16, wk = kt * BK + wch * 16;  // bytes
-      const bool xok = xk < K * XE, wok = wk < K;
+      const int k = kt * BK + c * 16;
+      const bool ok = k < K;
 #pragma unroll
       for (int j = 0; j < G::XJ; ++j) {
-        const int row = (cw + 4 * j) * G::XRPB;
-        dma16(xr, sm + stage * G::STAGE + row * XCPR, xok ? (row + xl) * K * XE + xk : kOutOfRange);
+        const int row = (cw + 4 * j) * RPB;
+        dma16(xr, sm + stage * G::STAGE + row * CPR, ok ? (row + rl) * K + k : kOutOfRange);
       }
 #pragma unroll
       for (int j = 0; j < G::WJ; ++j) {
-        const int row = (cw + 4 * j) * G::WRPB;
-        dma16(wrs, sm + stage * G::STAGE + WBASE + row * WCPR, wok ? (row + wl) * K + wk : kOutOfRange);
+        const int row = (cw + 4 * j) * RPB;
+        dma16(wrs, sm + stage * G::STAGE + (TM + row) * CPR, ok ? (row + rl) * K + k : kOutOfRange);
       }
     };
     // slabs past the last read zeros, so that the waits count the same throughout
@@ -370,52 +550,59 @@ __global__ __launch_bounds__(G::NT) void fp8_gemm_kernel(GemmArgs g) {
       stage = stage + 1 == NS ? 0 : stage + 1;
     }
     wait_vm<0>();
+    lds_barrier();  // every copy has landed, every wave is done with the ring
+    finish([] {}, [] {});
   } else {
     // -------------------------------------------------------------- matrix waves
+    f32x16_t acc[MT][NTL];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
       for (int j = 0; j < NTL; ++j)
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-    constexpr int WR = G::WR, NR = WR * NTL + 2 * MT;
     struct Frag {
-      uint4 w[NTL][WR], x[MT][2];
+      uint4 w[NTL][RD], x[MT][RD];
     };
-    Frag F[2];
+    // Two sets, the next step's reads spread over this step's products; on the largest
+    // sub-tile one, where a fragment is read again right after its last use (two sets
+    // next to its accumulators spill), four products ahead of the next.
+    constexpr bool ONE = NQ >= 8;
+    Frag F[ONE ? 1 : 2];
+    constexpr int NR = RD * (NTL + MT);
     // the r-th 16-byte read of step st (of this wave's) of a stage: W rows as the A
     // operand, x rows as the B operand
     auto read = [&](Frag& f, int stage, int st, int r) __attribute__((always_inline)) {
       const uint4* s = sm + stage * G::STAGE;
-      const int own = 2 * (kg * SPW + st) + lh;  // this lane's half step
-      if (r < WR * NTL) {
-        const int q = r / WR, h = r % WR;
-        f.w[q][h] = s[WBASE + lds_idx(WCPR, wc * WN + q * 32 + l32, own * WR + h)];
-      } else {
-        const int q = (r - WR * NTL) / 2, h = (r - WR * NTL) % 2;
-        f.x[q][h] = s[lds_idx(XCPR, wr * WM + q * 32 + l32, own * 2 + h)];
-      }
+      const int q = r / RD, h = r % RD, ch = (2 * (kg * SPW + st) + lh) * RD + h;
+      if (q < NTL)
+        f.w[q][h] = s[lds_idx(TM + wc * WN + q * 32 + l32, ch)];
+      else
+        f.x[q - NTL][h] = s[lds_idx(wr * WM + (q - NTL) * 32 + l32, ch)];
     };
-    // scales: four blocks of K at a time, the next four requested ahead (WIDE: x has none)
+    auto read_row = [&](Frag& f, int stage, int st, int q) __attribute__((always_inline)) {
+#pragma unroll
+      for (int h = 0; h < RD; ++h) read(f, stage, st, q * RD + h);
+    };
+    // scales: four blocks of K at a time, the next four requested ahead
     const uint8_t* const xs = a.xs;
     const uint8_t* const ws = a.ws;
-    constexpr int MS = G::WIDE ? 0 : MT;
     int64_t xrow[MT];
 #pragma unroll
-    for (int i = 0; i < MS; ++i) xrow[i] = (int64_t)min(m0 + wr * WM + i * 32 + l32, M - 1) * kb_n;
+    for (int i = 0; i < MT; ++i) xrow[i] = (int64_t)min(m0 + wr * WM + i * 32 + l32, M - 1) * kb_n;
     const int64_t wrow = (int64_t)(min(n0 + wc * WN, N - 1) / kFp8Block) * kb_n;
     uint32_t sx[MT], sxn[MT], sw, swn;
     auto load_four = [&](int kb) __attribute__((always_inline)) {
       kb = min(kb, kb_n - 1);
 #pragma unroll
-      for (int i = 0; i < MS; ++i) sxn[i] = load_scales(xs, xrow[i] + kb, g.xs_bytes);
+      for (int i = 0; i < MT; ++i) sxn[i] = load_scales(xs, xrow[i] + kb, g.xs_bytes);
       swn = load_scales(ws, wrow + kb, g.ws_bytes);
     };
     int four = -1;  // the four blocks that sx and sw are of
     auto next_four = [&](int f) __attribute__((always_inline)) {
       four = f;
 #pragma unroll
-      for (int i = 0; i < MS; ++i) sx[i] = sxn[i];
+      for (int i = 0; i < MT; ++i) sx[i] = sxn[i];
       sw = swn;
       load_four(4 * f + 4);
     };
@@ -432,7 +619,13 @@ __global__ __launch_bounds__(G::NT) void fp8_gemm_kernel(GemmArgs g) {
       constexpr int rsp = last ? 0 : sp + 1;
       if constexpr (last) lds_barrier();
       if constexpr (G::WIDE) {
-        const int byte = (sw >> shift) & 0xFF;
+        const int byte = past ? 127 : (sw >> shift) & 0xFF;
+        uint4 xv[MT][2];
+#pragma unroll
+        for (int mi = 0; mi < MT; ++mi) {
+          fp8_to_bf16(fc.x[mi][0], past ? 127 : (sx[mi] >> shift) & 0xFF, xv[mi]);
+          if constexpr (ONE) read_row(fn, rst, rsp, NTL + mi);
+        }
 #pragma unroll
         for (int ni = 0; ni < NTL; ++ni) {
           uint4 v[2];
@@ -440,19 +633,28 @@ __global__ __launch_bounds__(G::NT) void fp8_gemm_kernel(GemmArgs g) {
 #pragma unroll
           for (int mi = 0; mi < MT; ++mi)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) acc[mi][ni] = mfma32(v[h], fc.x[mi][h], acc[mi][ni]);
+            for (int h = 0; h < 2; ++h) acc[mi][ni] = mfma32(v[h], xv[mi][h], acc[mi][ni]);
+          if constexpr (ONE) {
+            read_row(fn, rst, rsp, ni);
+          } else {
 #pragma unroll
-          for (int r = ni * NR / NTL; r < (ni + 1) * NR / NTL; ++r) read(fn, rst, rsp, r);
+            for (int r = ni * NR / NTL; r < (ni + 1) * NR / NTL; ++r) read(fn, rst, rsp, r);
+          }
           __builtin_amdgcn_sched_barrier(0);
         }
       } else {
 #pragma unroll
         for (int m = 0; m < NQ; ++m) {
           const int mi = m / NTL, ni = m % NTL;
-          acc[mi][ni] = mfma32_fp8(fc.w[ni][0], fc.w[ni][WR - 1], fc.x[mi][0], fc.x[mi][1], acc[mi][ni],
+          acc[mi][ni] = mfma32_fp8(fc.w[ni][0], fc.w[ni][RD - 1], fc.x[mi][0], fc.x[mi][RD - 1], acc[mi][ni],
                                    past ? 127 : (int)(sw >> shift), past ? 127 : (int)(sx[mi] >> shift));
+          if constexpr (ONE) {
+            if (mi == MT - 1) read_row(fn, rst, rsp, ni);
+            if (ni == NTL - 1) read_row(fn, rst, rsp, NTL + mi);
+          } else {
 #pragma unroll
-          for (int r = m * NR / NQ; r < (m + 1) * NR / NQ; ++r) read(fn, rst, rsp, r);
+            for (int r = m * NR / NQ; r < (m + 1) * NR / NQ; ++r) read(fn, rst, rsp, r);
+          }
           __builtin_amdgcn_sched_barrier(0);
         }
       }
@@ -461,187 +663,26 @@ __global__ __launch_bounds__(G::NT) void fp8_gemm_kernel(GemmArgs g) {
 #pragma unroll
     for (int r = 0; r < NR; ++r) read(F[0], 0, 0, r);
     // Past the last slab the reads fill registers that are never used.
-    constexpr int UN = SPW % 2 ? 2 : 1;  // slabs until the two fragment sets are back in place
+    constexpr int UN = SPW % 2 && !ONE ? 2 : 1;  // slabs until the two fragment sets are back in place
     int stage = 0;
     for (int kt = 0; kt < nkt; kt += UN) {
 #pragma unroll
       for (int u = 0; u < UN; ++u) {
         if (u > 0 && kt + u >= nkt) break;
         constexpr int one = SPW > 1 ? 1 : 0, two = SPW > 2 ? 2 : 0, three = SPW > 3 ? 3 : 0;
-        kstep(IC<0>{}, F[u & 1], F[(u & 1) ^ 1], stage, kt + u);
-        if constexpr (SPW > 1) kstep(IC<one>{}, F[1], F[0], stage, kt + u);
+        constexpr int other = ONE ? 0 : 1;
+        kstep(IC<0>{}, F[ONE ? 0 : u & 1], F[ONE ? 0 : (u & 1) ^ 1], stage, kt + u);
+        if constexpr (SPW > 1) kstep(IC<one>{}, F[other], F[0], stage, kt + u);
         if constexpr (SPW > 2) {
-          kstep(IC<two>{}, F[0], F[1], stage, kt + u);
-          kstep(IC<three>{}, F[1], F[0], stage, kt + u);
+          kstep(IC<two>{}, F[0], F[other], stage, kt + u);
+          kstep(IC<three>{}, F[other], F[0], stage, kt + u);
         }
         stage = stage + 1 == NS ? 0 : stage + 1;
       }
     }
+    lds_barrier();
+    finish([&] { put(acc); }, [&] { add_update(acc); });
   }
-  lds_barrier();  // every copy has landed, every wave is done with the ring
-
-  // ---------------------------------------------------------------- epilogue
-  // The KS partial sums of a sub-tile, in units of four registers (unit 4 q + i of
-  // block q = mi NTL + ni), are added in wave order; a wave then holds NU / KS units.
-  constexpr int MYU = NU / KS;
-  const int u0 = kg * MYU;
-  f32x4_t un[MYU];
-  if constexpr (KS > 1) {
-    f32x4_t* const ex = reinterpret_cast<f32x4_t*>(sm);
-    if (wave < G::NMW) {
-#pragma unroll
-      for (int q = 0; q < NQ; ++q)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const f32x16_t& v = acc[q / NTL][q % NTL];
-          ex[(mw * NU + q * 4 + i) * 64 + lane] = f32x4_t{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
-        }
-    }
-    __syncthreads();
-    if (wave < G::NMW) {
-#pragma unroll
-      for (int u = 0; u < MYU; ++u) {
-        un[u] = ex[((wt * KS) * NU + u0 + u) * 64 + lane];
-#pragma unroll
-        for (int k = 1; k < KS; ++k) un[u] += ex[((wt * KS + k) * NU + u0 + u) * 64 + lane];
-      }
-    }
-    __syncthreads();
-  } else if (wave < G::NMW) {
-#pragma unroll
-    for (int u = 0; u < NU; ++u) {
-      const f32x16_t& v = acc[u / 4 / NTL][u / 4 % NTL];
-      const int i = u % 4;
-      un[u] = f32x4_t{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
-    }
-  }
-  // The rows of s T as bf16 hi and lo parts (2^-17 of a value together) and those
-  // of B, zero padded to rp, to LDS.
-  const bool lora = a.y_on && a.rp > 0;
-  const int rp = a.rp, lrp = 31 - __builtin_clz(rp | 1), ldt = 2 * rp + 8, ldb = rp + 8;  // (in values)
-  uint16_t* const Ts = reinterpret_cast<uint16_t*>(sm);
-  uint16_t* const Bs = Ts + TM * ldt;
-  if (lora) {
-    const int rows = min(TM, M - m0), cols = min(TN, N - n0);
-    if (a.ts) {
-      for (int e = t; e < TM * rp / 4; e += G::NT) {  // 16 bytes each
-        const int row = e >> (lrp - 2), c = (e & (rp / 4 - 1)) * 8;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (row < rows) v = *reinterpret_cast<const uint4*>(a.ts + (size_t)(m0 + row) * 2 * rp + c);
-        *reinterpret_cast<uint4*>(Ts + row * ldt + c) = v;
-      }
-    } else {
-      const size_t stride = (size_t)M * rp;
-      for (int e = t; e < TM * rp / 4; e += G::NT) {
-        const int row = e >> (lrp - 2), j = (e & (rp / 4 - 1)) * 4;
-        f32x4_t v = {0.f, 0.f, 0.f, 0.f};
-        if (row < rows) {
-          const float* p = a.part + (size_t)(m0 + row) * rp + j;
-          for (int c = 0; c < a.nch; ++c) v += *reinterpret_cast<const f32x4_t*>(p + c * stride);
-        }
-        uint32_t hi[4], lo[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float f = a.s * v[i];
-          hi[i] = f32_to_bf16_any(f);
-          lo[i] = (hi[i] & 0x7FFF) < 0x7F80 ? f32_to_bf16_any(f - bf16_to_f32(hi[i])) : 0;  // (none of an infinity)
-        }
-        *reinterpret_cast<uint2*>(Ts + row * ldt + j) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
-        *reinterpret_cast<uint2*>(Ts + row * ldt + rp + j) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
-      }
-    }
-    if (g.bvec) {
-      for (int e = t; e < TN * rp / 8; e += G::NT) {
-        const int row = e >> (lrp - 3), j = (e & (rp / 8 - 1)) * 8;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (row < cols && j < a.r) v = *reinterpret_cast<const uint4*>(a.B + (size_t)(n0 + row) * a.ldb + j);
-        *reinterpret_cast<uint4*>(Bs + row * ldb + j) = v;
-      }
-    } else {
-      for (int e = t; e < TN * rp; e += G::NT) {
-        const int row = e >> lrp, j = e & (rp - 1);
-        Bs[row * ldb + j] = row < cols && j < a.r ? a.B[(size_t)(n0 + row) * a.ldb + j] : (uint16_t)0;
-      }
-    }
-    __syncthreads();
-  }
-  if (wave >= G::NMW) return;
-
-  constexpr int MYQ = MYU >= 4 ? MYU / 4 : 1, UPQ = MYU / MYQ;
-  auto finish = [&](auto BI) __attribute__((always_inline)) {
-    constexpr int b = decltype(BI)::value;
-    const int q = (u0 >> 2) + b, i0 = MYU >= 4 ? 0 : (u0 & 3);
-    const int mi = q / NTL, ni = q % NTL;
-    const int row = m0 + wr * WM + mi * 32 + l32;
-    const int colb = n0 + wc * WN + ni * 32 + 4 * lh;
-    auto store = [&](void* y, const f32x4_t (&v)[UPQ]) __attribute__((always_inline)) {
-      if (row >= M) return;
-#pragma unroll
-      for (int k = 0; k < UPQ; ++k) {
-        const int col = colb + 8 * (i0 + k);
-        const size_t at = (size_t)row * N + col;
-        if (g.vec4 && col + 3 < N) {
-          if (a.y_type == kF32)
-            *reinterpret_cast<f32x4_t*>(static_cast<float*>(y) + at) = v[k];
-          else
-            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(y) + at) =
-                make_uint2(f32_to_bf16_pair(v[k][0], v[k][1]), f32_to_bf16_pair(v[k][2], v[k][3]));
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (col + e < N) store_elem(y, a.y_type, at + e, v[k][e]);
-        }
-      }
-    };
-    f32x4_t v[UPQ];
-#pragma unroll
-    for (int k = 0; k < UPQ; ++k) v[k] = un[b * UPQ + k];
-    if (a.y_off) store(a.y_off, v);
-    if (!a.y_on) return;
-    if (lora) {
-      // s T B^T of the block: rows of [B | B] against rows of [hi | lo]
-      f32x16_t L;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) L[e] = 0.f;
-      const uint16_t* tr = Ts + (wr * WM + mi * 32 + l32) * ldt + 8 * lh;
-      const uint16_t* br = Bs + (wc * WN + ni * 32 + l32) * ldb + 8 * lh;
-      for (int k0 = 0; k0 < rp; k0 += 16) {
-        const uint4 bf = *reinterpret_cast<const uint4*>(br + k0);
-        L = mfma32(bf, *reinterpret_cast<const uint4*>(tr + k0), L);
-        L = mfma32(bf, *reinterpret_cast<const uint4*>(tr + rp + k0), L);
-      }
-#pragma unroll
-      for (int k = 0; k < UPQ; ++k) {
-        f32x4_t l;
-        if constexpr (MYU >= 4) {
-          l = f32x4_t{L[4 * k], L[4 * k + 1], L[4 * k + 2], L[4 * k + 3]};
-        } else {
-          l = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (i == i0 + k) l = f32x4_t{L[4 * i], L[4 * i + 1], L[4 * i + 2], L[4 * i + 3]};
-        }
-        if (a.drop > 0) {
-          const uint64_t at = (uint64_t)row * N + colb + 8 * (i0 + k);  // (a multiple of 4: N % 8 == 0)
-          const uint4 w = dropout_words(a.rng, at >> 3);
-          const int j0 = (int)(at & 4);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) l[e] = dropout_keeps(w, j0 + e, a.drop) ? l[e] * a.keep : 0.f;
-        }
-        v[k] += l;
-      }
-    }
-    store(a.y_on, v);
-  };
-  static_assert(MYQ <= 8 && UPQ * MYQ == MYU, "blocks listed below");
-  finish(IC<0>{});
-  if constexpr (MYQ > 1) finish(IC<1>{});
-  if constexpr (MYQ > 2) finish(IC<2>{});
-  if constexpr (MYQ > 3) finish(IC<3>{});
-  if constexpr (MYQ > 4) finish(IC<4>{});
-  if constexpr (MYQ > 5) finish(IC<5>{});
-  if constexpr (MYQ > 6) finish(IC<6>{});
-  if constexpr (MYQ > 7) finish(IC<7>{});
 }
 
 bool at_multiple(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
@@ -653,7 +694,10 @@ hipError_t launch_tile(GemmArgs& g, hipStream_t stream) {
   const int64_t total = (int64_t)g.ntm * g.ntn;
   if (total * G::NT >= (int64_t(1) << 32)) return hipErrorInvalidValue;
   g.total = (int)total;
-  hipLaunchKernelGGL(fp8_gemm_kernel<G>, dim3(g.total), dim3(G::NT), 0, stream, g);
+  if (g.a.drop > 0 && g.a.y_on)
+    hipLaunchKernelGGL((fp8_gemm_kernel<G, true>), dim3(g.total), dim3(G::NT), 0, stream, g);
+  else
+    hipLaunchKernelGGL((fp8_gemm_kernel<G, false>), dim3(g.total), dim3(G::NT), 0, stream, g);
   return hipGetLastError();
 }
 
@@ -663,12 +707,11 @@ hipError_t launch_rows(GemmArgs& g, hipStream_t stream) {
   const auto tiles = [&](int tm, int tn) {
     return (int64_t)((g.a.M + tm - 1) / tm) * ((g.a.N + tn - 1) / tn);
   };
-  constexpr int D = WIDE ? 2 : 1;  // (a slab of bf16 rows holds half the values)
-  if (tiles(128, 256) >= 200) return launch_tile<Tile<WIDE, 128, 256, 64, 128, 1, 128 / D, WIDE ? 4 : 3>>(g, stream);
-  if (tiles(128, 128) >= 200) return launch_tile<Tile<WIDE, 128, 128, 64, 64, 2, 128 / D, 5>>(g, stream);
-  if (tiles(64, 128) >= 200) return launch_tile<Tile<WIDE, 64, 128, 64, 64, 2, 128 / D, 6>>(g, stream);
-  if (tiles(64, 64) >= 200) return launch_tile<Tile<WIDE, 64, 64, 32, 64, 4, 256 / D, 4>>(g, stream);
-  return launch_tile<Tile<WIDE, 32, 32, 32, 32, 4, 256 / D, 8>>(g, stream);
+  if (tiles(128, 256) >= 200) return launch_tile<Tile<WIDE, 128, 256, 64, 128, 1, 128, 3>>(g, stream);
+  if (tiles(128, 128) >= 200) return launch_tile<Tile<WIDE, 128, 128, 64, 64, 2, 128, 5>>(g, stream);
+  if (tiles(64, 128) >= 200) return launch_tile<Tile<WIDE, 64, 128, 64, 64, 2, 128, 6>>(g, stream);
+  if (tiles(64, 64) >= 200) return launch_tile<Tile<WIDE, 64, 64, 32, 64, 4, 256, 4>>(g, stream);
+  return launch_tile<Tile<WIDE, 32, 32, 32, 32, 4, 256, 8>>(g, stream);
 }
 
 template <int RP>
@@ -702,8 +745,6 @@ hipError_t launch_fp8_prep(const Fp8PrepArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-bool fp8_wide(int M, int y_type) { return M <= kFewRows || y_type == kF32; }
-
 hipError_t launch_fp8_linear(const Fp8LinearArgs& a, hipStream_t stream) {
   if (a.M <= kFewRows && !a.ts) {
     hipLaunchKernelGGL(fp8_stream_kernel<2>, dim3((a.N + 31) / 32), dim3(S_WAVES * 64), 0, stream, a);
@@ -714,10 +755,9 @@ hipError_t launch_fp8_linear(const Fp8LinearArgs& a, hipStream_t stream) {
   const int64_t kb = (a.K + kFp8Block - 1) / kFp8Block;
   g.xs_bytes = a.M * kb;
   g.ws_bytes = (int64_t)((a.N + kFp8Block - 1) / kFp8Block) * kb;
-  const uintptr_t four = a.y_type == kF32 ? 16 : 8;
-  g.vec4 = a.N % 4 == 0 && at_multiple(a.y_off, four) && at_multiple(a.y_on, four);
+  g.vec = a.N % (a.y_type == kF32 ? 4 : 8) == 0 && at_multiple(a.y_off, 16) && at_multiple(a.y_on, 16);
   g.bvec = a.r % 8 == 0 && a.ldb % 8 == 0 && at_multiple(a.B, 16);
-  return fp8_wide(a.M, a.y_type) ? launch_rows<true>(g, stream) : launch_rows<false>(g, stream);
+  return a.y_type == kF32 ? launch_rows<true>(g, stream) : launch_rows<false>(g, stream);
 }
 
 }  // namespace hydra

@@ -1178,9 +1178,8 @@ namespace {
 
 int64_t blocks128(int64_t n) { return (n + 127) / 128; }
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
-// Workspace of a product over an 8-bit weight: the rows' values in bf16, or their
-// bytes and scales in the same place.
-size_t fp8_rows_bytes(int64_t M, int64_t K) { return up256((size_t)M * K * 2) + up256((size_t)M * blocks128(K)); }
+// Workspace of a product over an 8-bit weight: the rows' bytes and their scales.
+size_t fp8_rows_bytes(int64_t M, int64_t K) { return up256((size_t)M * K) + up256((size_t)M * blocks128(K)); }
 
 hydra_status fp8_shape(int64_t M, int64_t N, int64_t K, int64_t r) {
   if (M < 1 || M > kMaxRows || N < 1 || N > kMaxCols || K < 1 || K > kMaxK || K % 16 != 0) return HYDRA_ERR_SHAPE;
@@ -1253,8 +1252,7 @@ hydra_status hydra_fp8_lora_linear(const uint16_t* x, const uint16_t* x_adapter,
   const int rp = lora ? hydra::padded_rank(int(r)) : 0;
   int nch = 0, kch = 0;
   hydra::fp8_prep_chunks(int(M), int(K), rp, nch, kch);
-  const bool wide = hydra::fp8_wide(int(M), y_type);
-  const size_t rows = xq && !wide ? 0 : fp8_rows_bytes(M, K), need = rows + (rp ? up256((size_t)nch * M * rp * 4) : 0);
+  const size_t rows = xq ? 0 : fp8_rows_bytes(M, K), need = rows + (rp ? up256((size_t)nch * M * rp * 4) : 0);
   if (need > 0) {
     if (!workspace) return HYDRA_ERR_NULL;
     if (workspace_bytes < need) return HYDRA_ERR_WORKSPACE;
@@ -1269,14 +1267,8 @@ hydra_status hydra_fp8_lora_linear(const uint16_t* x, const uint16_t* x_adapter,
   p.K = int(K);
   p.r = int(r);
   p.rp = rp;
-  if (wide) {
-    p.xh = reinterpret_cast<uint16_t*>(w);
-    p.q_in = xq;
-    p.s_in = x_scale;
-  } else {
-    p.xq = w;
-    p.xs = rows > 0 ? w + up256((size_t)M * K * 2) : nullptr;
-  }
+  p.xq = w;
+  p.xs = xq ? nullptr : w + up256((size_t)M * K);
   p.part = reinterpret_cast<float*>(w + rows);
   p.nch = nch;
   p.kch = kch;
@@ -1286,7 +1278,6 @@ hydra_status hydra_fp8_lora_linear(const uint16_t* x, const uint16_t* x_adapter,
     if (e != hipSuccess) return from_hip(e);
   }
   hydra::Fp8LinearArgs a{};
-  a.xh = p.xh;
   a.xq = xq ? xq : p.xq;
   a.xs = xq ? x_scale : p.xs;
   a.wq = Wq;
@@ -1347,12 +1338,8 @@ hydra_status hydra_fp8_lora_linear_backward(const uint16_t* x, const uint8_t* Wq
   if (!aligned(workspace, 16)) return HYDRA_ERR_ALIGN;
   uint8_t* const w = static_cast<uint8_t*>(workspace);
   hydra::Fp8LinearArgs g{};
-  if (hydra::fp8_wide(int(M), dx_type)) {
-    g.xh = reinterpret_cast<uint16_t*>(w);
-  } else {
-    g.xq = w;
-    g.xs = w + up256((size_t)M * N * 2);
-  }
+  g.xq = w;
+  g.xs = w + up256((size_t)M * N);
   g.wq = Wqt;
   g.ws = wt_scale;
   g.M = int(M);

@@ -295,9 +295,8 @@ hipError_t launch_fp8_quantize(const Fp8QuantArgs& a, hipStream_t stream);
 // hi and lo parts of s T [M x 2 rp].  drop > 0: the update goes through the
 // dropout mask of rng (an element's 16 bits below `drop`: 0, else times keep).
 struct Fp8LinearArgs {
-  const uint16_t* xh;  // [M x K] bf16 values of x (fp8_wide), or
-  const uint8_t* xq;   // [M x K] their bytes
-  const uint8_t* xs;   // [M x ceil(K / 128)] and scales
+  const uint8_t* xq;   // [M x K]
+  const uint8_t* xs;   // [M x ceil(K / 128)]
   const uint8_t* wq;   // [N x K]
   const uint8_t* ws;   // [ceil(N / 128) x ceil(K / 128)]
   int M, N, K;
@@ -315,19 +314,13 @@ struct Fp8LinearArgs {
   float keep;
   const uint64_t* rng;
 };
-// Whether the product takes the values of x as bf16, or bytes and scales.
-bool fp8_wide(int M, int y_type);
-// What the linear needs before its product: x quantized, as bytes and scales or
-// (xh) as the values that they stand for; or values from bytes (q_in, s_in) that
-// are there; and the partial sums of T = xa A^T (A nullptr: not).
+// What the linear needs before its product: x quantized (x nullptr: not), and the
+// partial sums of T = xa A^T (A nullptr: not).
 struct Fp8PrepArgs {
   const uint16_t* x;   // [M x K] bf16, or nullptr
-  const uint8_t* q_in; // [M x K], or nullptr
-  const uint8_t* s_in;
   const uint16_t* xa;  // [M x K] bf16: x itself, or the adapter's own input
   const uint16_t* A;   // [r x K] bf16
   int M, K, r, rp;
-  uint16_t* xh;
   uint8_t* xq;
   uint8_t* xs;
   float* part;         // [nch][M][rp]
@@ -389,7 +382,7 @@ struct BackwardArgs {
   float* dA;           // [r x K] or nullptr
   float* dB;           // [N x r] or nullptr
   // W in 8 bits: Wt and dx null, and what the product over it takes in their
-  // place (xh, or xq and xs: room for dy's; y_on: dx, of y_type; drop: the mask)
+  // place (xq, xs: room for dy's; y_on: dx, of y_type; drop: the mask)
   const Fp8LinearArgs* base8;
 };
 // Workspace bytes of the backward, and the launcher (which assumes a

@@ -353,7 +353,6 @@ hipError_t launch_lora_backward(const BackwardArgs& a, void* ws, hipStream_t str
     q.x = q.xa = a.dy;
     q.M = a.M;
     q.K = a.N;
-    q.xh = const_cast<uint16_t*>(g.xh);
     q.xq = const_cast<uint8_t*>(g.xq);
     q.xs = const_cast<uint8_t*>(g.xs);
     fp8_prep_chunks(q.M, q.K, 0, q.nch, q.kch);

@@ -12,8 +12,9 @@
 // Bound: memory for many rows (every logit once), launches for few.
 //  * verify_stats_kernel: maximum and sum of exponentials of every segment of
 //    every row that a sequence has;
-//  * verify_left_kernel: the rows' totals, the acceptances, and what the
-//    distribution of the next token has left in every segment;
+//  * verify_left_kernel: the rows' totals, the acceptances (every workgroup of a
+//    sequence forms them itself), the accepted tokens, and what the distribution of
+//    the next token has in every segment;
 //  * verify_sample_kernel: the segment in which the sample lies, and its place.
 #include "hydra_elem.h"
 
@@ -40,30 +41,31 @@ struct Decision {  // of one sequence
 };
 enum Kind : int { kPlain = 0, kMinus = 1, kWithout = 2, kNone = 3 };
 
-// e^x for x <= 0 to about 1e-14: 2^k P(r), x = k ln 2 + r, |r| <= ln 2 / 2, with
-// the exponential series to r^11 / 11! (the rest is below 1e-14).
-__device__ __forceinline__ double exp64(double x) {
-  x = fmax(x, -800.0);  // (below it e^x is 0 in 64 bits)
-  const double k = rint(x * 0x1.71547652b82fep+0);
-  double r = fma(-k, 0x1.62e42feep-1, x);  // ln 2 in two parts, the first of 32 bits
-  r = fma(-k, 0x1.a39ef35793c76p-33, r);
-  double s = 1.0 / 39916800;
-  s = fma(s, r, 1.0 / 3628800);
-  s = fma(s, r, 1.0 / 362880);
-  s = fma(s, r, 1.0 / 40320);
-  s = fma(s, r, 1.0 / 5040);
-  s = fma(s, r, 1.0 / 720);
-  s = fma(s, r, 1.0 / 120);
-  s = fma(s, r, 1.0 / 24);
+// e^x for x <= 0: 2^(k / 32) P(r), x = k ln 2 / 32 + r, |r| <= ln 2 / 64, with 2^(j / 32)
+// from a table (put_table) and the exponential series to r^5 / 5! (the rest is below
+// 3e-15): thirteen 64-bit operations where the series alone, to r^11, took twenty.
+// Below e^-700 it is 0.
+__device__ __forceinline__ void put_table(double* table) {
+  if (threadIdx.x < 32) table[threadIdx.x] = exp2(threadIdx.x * (1.0 / 32));
+}
+__device__ __forceinline__ double exp64(double x, const double* table) {
+  // k in the low bits of a sum whose last place is 1
+  const double big = 0x1.8p52;
+  const double t = fma(x, 0x1.71547652b82fep+5, big), k = t - big;  // 32 / ln 2
+  const double r = fma(-k, 0x1.62e42fefa39efp-6, x);
+  double s = fma(1.0 / 120, r, 1.0 / 24);
   s = fma(s, r, 1.0 / 6);
   s = fma(s, r, 0.5);
   s = fma(s, r, 1.0);
   s = fma(s, r, 1.0);
-  return ldexp(s, (int)k);
+  const int ki = (int)__double2loint(t);
+  s *= table[ki & 31];
+  const double v = __hiloint2double(__double2hiint(s) + ((ki >> 5) << 20), __double2loint(s));
+  return x < -700.0 ? 0.0 : v;
 }
 // e^((z - most) / T) of a logit that is no NaN, 0 for -inf.
-__device__ __forceinline__ double weight(float z, float most, double inv_t) {
-  return exp64(((double)z - (double)most) * inv_t);
+__device__ __forceinline__ double weight(float z, float most, double inv_t, const double* table) {
+  return exp64(((double)z - (double)most) * inv_t, table);
 }
 
 __device__ __forceinline__ double wave_sum64(double v) {
@@ -99,11 +101,12 @@ __device__ __forceinline__ int length_of(const VerifyArgs& a, int b) {
 }
 
 template <int T, bool VEC>
-__device__ __forceinline__ void stats(const void* row, const VerifyArgs& a, int seg, Part* out) {
+__device__ __forceinline__ void stats(const void* row, const VerifyArgs& a, int seg, Part* out, double* table) {
   __shared__ float rm[VT / 64];
   __shared__ double rs[VT / 64];
   __shared__ int rb[VT / 64];
   const int t = threadIdx.x;
+  put_table(table);
   float f[kPer];
   float most = -INFINITY;
   bool bad = false;
@@ -128,7 +131,7 @@ __device__ __forceinline__ void stats(const void* row, const VerifyArgs& a, int 
   double sum = 0;
   if (!none && !odd) {
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) sum += weight(f[i], most, a.inv_t);
+    for (int i = 0; i < kPer; ++i) sum += weight(f[i], most, a.inv_t, table);
   }
   sum = wave_sum64(sum);
   if ((t & 63) == 0) rs[t >> 6] = sum;
@@ -139,6 +142,7 @@ __device__ __forceinline__ void stats(const void* row, const VerifyArgs& a, int 
 // Rows [0, n (k + 1)) are the target's, the rest the draft's.
 template <int TZ, int TD, bool VEC>
 __global__ __launch_bounds__(VT) void verify_stats_kernel(VerifyArgs a, Part* parts, int nseg) {
+  __shared__ double table[32];
   const int64_t row = blockIdx.x / nseg;
   const int seg = (int)(blockIdx.x - row * nseg);
   const int64_t nt = (int64_t)a.n * (a.k + 1);
@@ -146,127 +150,166 @@ __global__ __launch_bounds__(VT) void verify_stats_kernel(VerifyArgs a, Part* pa
   if (row < nt) {
     const int b = (int)(row / (a.k + 1)), j = (int)(row - (int64_t)b * (a.k + 1));
     if (j > length_of(a, b)) return;
-    stats<TZ, VEC>(row_of<TZ>(a.z, row, a.ld), a, seg, out);
+    stats<TZ, VEC>(row_of<TZ>(a.z, row, a.ld), a, seg, out, table);
   } else {
     const int64_t d = row - nt;
     const int b = (int)(d / a.k), j = (int)(d - (int64_t)b * a.k);
     if (j >= length_of(a, b)) return;
-    stats<TD, VEC>(row_of<TD>(a.zd, d, a.ld_d), a, seg, out);
+    stats<TD, VEC>(row_of<TD>(a.zd, d, a.ld_d), a, seg, out, table);
   }
 }
 
-// The weight of a logit in the next token's distribution, relative to p's or (kMinus) as a probability.
+// What a logit has in the next token's distribution, as a probability.
 __device__ __forceinline__ double left_of(const Decision& d, float z, float zd, int64_t v, double inv_t, double p_inv,
-                                          double q_inv) {
-  double p = weight(z, d.p_most, inv_t) * p_inv;
-  if (d.kind == kMinus) p = fmax(p - weight(zd, d.q_most, inv_t) * q_inv, 0.0);
+                                          double q_inv, const double* table) {
+  double p = weight(z, d.p_most, inv_t, table) * p_inv;
+  if (d.kind == kMinus) p = fmax(p - weight(zd, d.q_most, inv_t, table) * q_inv, 0.0);
   if (d.kind == kWithout && v == d.token) p = 0;
   return p;
+}
+
+// ... and of a thread's logits of a segment, four at a time.
+template <int TZ, int TD, bool VEC>
+__device__ __forceinline__ void left_in(const VerifyArgs& a, const Decision& d, int b, int seg, const double* table,
+                                        double (&w)[kPer]) {
+  const void* zr = row_of<TZ>(a.z, (int64_t)b * (a.k + 1) + d.accepted, a.ld);
+  const bool minus = d.kind == kMinus;
+  const void* dr = minus ? row_of<TD>(a.zd, (int64_t)b * a.k + d.accepted, a.ld_d) : nullptr;
+  const double p_inv = 1.0 / d.p_sum, q_inv = minus ? 1.0 / d.q_sum : 0.0;
+  float z[kPer / 4][4], zd[kPer / 4][4];
+#pragma unroll
+  for (int i = 0; i < kPer / 4; ++i) {
+    const int64_t c = (int64_t)seg * kSeg + i * (VT * 4) + threadIdx.x * 4;
+    load4<TZ, VEC>(zr, c, a.V, z[i]);
+    if (minus) load4<TD, VEC>(dr, c, a.V, zd[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < kPer / 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int64_t c = (int64_t)seg * kSeg + i * (VT * 4) + threadIdx.x * 4 + j;
+      w[4 * i + j] = left_of(d, z[i][j], zd[i][j], c, a.inv_t, p_inv, q_inv, table);
+    }
 }
 
 template <int TZ, int TD, bool VEC>
 __global__ __launch_bounds__(VT) void verify_left_kernel(VerifyArgs a, const Part* parts, int nseg, Decision* decisions,
                                                          double* left) {
+  __shared__ double table[32];
   __shared__ float most[kMaxRows];
   __shared__ double sum[kMaxRows];
   __shared__ int accept[kMaxDrafts];
-  __shared__ Decision sd;
+  __shared__ int stop;
   __shared__ double rs[VT / 64];
   const int t = threadIdx.x;
   const int b = blockIdx.x / nseg, seg = blockIdx.x - b * nseg;
   const int len = length_of(a, b);
-  const int64_t nt = (int64_t)a.n * (a.k + 1);
+  const int64_t nt = (int64_t)a.n * (a.k + 1), base = (int64_t)b * (a.k + 1);
+  put_table(table);
+  // a thread's own draft (k <= VT) and its logits, requested ahead
+  static_assert(kMaxDrafts <= VT, "a draft a thread");
+  int tok = -1;
+  float z = 0.f, zd = 0.f, u = 0.f;
+  if (t < len) {
+    tok = a.drafts[(int64_t)b * a.k + t];
+    u = a.u[base + t];
+    if (tok >= 0 && tok < a.V) {
+      z = load_elem(row_of<TZ>(a.z, base + t, a.ld), TZ, tok);
+      if (a.zd) zd = load_elem(row_of<TD>(a.zd, (int64_t)b * a.k + t, a.ld_d), TD, tok);
+    }
+  }
+  __syncthreads();
   // rows 0 ... len are the target's, then the draft's: 16 lanes each
   const int rows = len + 1 + (a.zd ? len : 0);
   for (int r = t / 16; r < rows; r += VT / 16) {
-    const int64_t row = r <= len ? (int64_t)b * (a.k + 1) + r : nt + (int64_t)b * a.k + (r - len - 1);
+    const int64_t row = r <= len ? base + r : nt + (int64_t)b * a.k + (r - len - 1);
     const Part* p = parts + row * nseg;
     float m = -INFINITY;
+    double v = 0;
     bool bad = false;
     for (int s = t & 15; s < nseg; s += 16) {
-      m = fmaxf(m, p[s].most);
-      bad = bad || p[s].most != p[s].most;
+      const Part q = p[s];
+      bad = bad || q.most != q.most;
+      const float to = fmaxf(m, q.most);
+      if (to > -INFINITY && q.most == q.most)
+        v = (m > -INFINITY ? v * weight(m, to, a.inv_t, table) : 0.0) +
+            (q.most > -INFINITY ? q.sum * weight(q.most, to, a.inv_t, table) : 0.0);
+      m = to;
     }
+    float all = m;
 #pragma unroll
     for (int d = 8; d > 0; d >>= 1) {
-      m = fmaxf(m, __shfl_xor(m, d, 16));
+      all = fmaxf(all, __shfl_xor(all, d, 16));
       bad = __shfl_xor((int)bad, d, 16) || bad;
     }
-    double v = 0;
-    if (m > -INFINITY && !bad)
-      for (int s = t & 15; s < nseg; s += 16)
-        if (p[s].most > -INFINITY) v += p[s].sum * weight(p[s].most, m, a.inv_t);
+    v = m > -INFINITY ? v * weight(m, all, a.inv_t, table) : 0.0;
 #pragma unroll
     for (int d = 8; d > 0; d >>= 1) v += __shfl_xor(v, d, 16);
     if ((t & 15) == 0) {
-      most[r] = m;
+      most[r] = all;
       sum[r] = bad ? 0.0 : v;  // 0: no distribution
     }
   }
   __syncthreads();
   // 1: accepted, 0: not, 2: no draft that can be one (its token, its row), 3: no distribution of the target
-  for (int i = t; i < len; i += VT) {
-    const int tok = a.drafts[(int64_t)b * a.k + i];
+  double at_z = 0;  // ln p + ln sum of the draft
+  if (t < len) {
     int what = 0;
-    if (!(sum[i] > 0)) {
+    if (!(sum[t] > 0)) {
       what = 3;
-    } else if (tok < 0 || tok >= a.V || (a.zd && !(sum[len + 1 + i] > 0))) {
+    } else if (tok < 0 || tok >= a.V || (a.zd && !(sum[len + 1 + t] > 0))) {
       what = 2;
     } else {
-      const float z = load_elem(row_of<TZ>(a.z, (int64_t)b * (a.k + 1) + i, a.ld), TZ, tok);
-      const double p = weight(z, most[i], a.inv_t) / sum[i];
-      double q = 1;
-      if (a.zd) {
-        const float zd = load_elem(row_of<TD>(a.zd, (int64_t)b * a.k + i, a.ld_d), TD, tok);
-        q = weight(zd, most[len + 1 + i], a.inv_t) / sum[len + 1 + i];
-      }
-      what = (double)a.u[(int64_t)b * (a.k + 1) + i] * q < p;
+      at_z = ((double)z - (double)most[t]) * a.inv_t;
+      const double p = exp64(at_z, table) / sum[t];
+      const double q = a.zd ? weight(zd, most[len + 1 + t], a.inv_t, table) / sum[len + 1 + t] : 1.0;
+      what = (double)u * q < p;
     }
-    accept[i] = what;
+    accept[t] = what;
   }
   __syncthreads();
-  if (t == 0) {
-    int at = 0;
-    while (at < len && accept[at] == 1) ++at;
-    Decision d{};
-    d.accepted = at;
-    d.token = -1;
-    d.p_most = most[at];
-    d.p_sum = sum[at];
-    d.kind = kPlain;
-    if (!(sum[at] > 0)) {
-      d.kind = kNone;
-    } else if (at < len && accept[at] == 0) {
-      d.kind = a.zd ? kMinus : kWithout;
-      d.token = a.drafts[(int64_t)b * a.k + at];
-      if (a.zd) {
-        d.q_most = most[len + 1 + at];
-        d.q_sum = sum[len + 1 + at];
-      }
+  if (t < 64) {  // the first that is not accepted
+    int first = len;
+    for (int i = t; i < len; i += 64)
+      if (accept[i] != 1 && i < first) first = i;
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) first = min(first, __shfl_xor(first, d));
+    if (t == 0) stop = first;
+  }
+  __syncthreads();
+  Decision d{};
+  d.accepted = stop;
+  d.token = -1;
+  d.p_most = most[stop];
+  d.p_sum = sum[stop];
+  d.kind = !(d.p_sum > 0) ? kNone : kPlain;
+  const int what = stop < len ? accept[stop] : 1;
+  if (d.kind != kNone && what == 0) {
+    d.kind = a.zd ? kMinus : kWithout;
+    d.token = a.drafts[(int64_t)b * a.k + stop];
+    if (a.zd) {
+      d.q_most = most[len + 1 + stop];
+      d.q_sum = sum[len + 1 + stop];
     }
-    sd = d;
-    if (seg == 0) {
+  }
+  if (seg == 0) {
+    if (t == 0) {
       decisions[b] = d;
-      const bool odd = d.kind == kNone || (at < len && accept[at] == 2) || (a.lens && a.lens[b] != len);
-      if (odd && a.err) atomicOr(a.err, 1);
+      a.accepted[b] = stop;
+      if (a.err && (d.kind == kNone || what == 2 || (a.lens && a.lens[b] != len))) atomicOr(a.err, 1);
+    }
+    // the accepted drafts and what lies past the next token (and that one, where it has no distribution)
+    if (t <= a.k && (t != stop || d.kind == kNone)) {
+      a.tokens[base + t] = t < stop ? tok : -1;
+      if (a.lp) a.lp[base + t] = t < stop ? (float)(at_z - log(sum[t])) : t == stop ? __uint_as_float(0x7FC00000u) : 0.f;
     }
   }
-  __syncthreads();
-  const Decision d = sd;
   double v = 0;
   if (d.kind != kNone) {
-    const void* zr = row_of<TZ>(a.z, (int64_t)b * (a.k + 1) + d.accepted, a.ld);
-    const void* dr = d.kind == kMinus ? row_of<TD>(a.zd, (int64_t)b * a.k + d.accepted, a.ld_d) : nullptr;
-    const double p_inv = 1.0 / d.p_sum, q_inv = d.kind == kMinus ? 1.0 / d.q_sum : 0.0;
+    double w[kPer];
+    left_in<TZ, TD, VEC>(a, d, b, seg, table, w);
 #pragma unroll
-    for (int i = 0; i < kPer / 4; ++i) {
-      const int64_t c = (int64_t)seg * kSeg + i * (VT * 4) + t * 4;
-      float z[4], zd[4] = {0.f, 0.f, 0.f, 0.f};
-      load4<TZ, VEC>(zr, c, a.V, z);
-      if (dr) load4<TD, VEC>(dr, c, a.V, zd);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) v += left_of(d, z[j], zd[j], c + j, a.inv_t, p_inv, q_inv);
-    }
+    for (int i = 0; i < kPer; ++i) v += w[i];
   }
   v = wave_sum64(v);
   if ((t & 63) == 0) rs[t >> 6] = v;
@@ -274,123 +317,119 @@ __global__ __launch_bounds__(VT) void verify_left_kernel(VerifyArgs a, const Par
   if (t == 0) left[(int64_t)b * nseg + seg] = (rs[0] + rs[1]) + (rs[2] + rs[3]);
 }
 
+__device__ __forceinline__ double wave_scan64(double v, int lane) {
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) {
+    const double o = __shfl_up(v, s);
+    if (lane >= s) v += o;
+  }
+  return v;
+}
+
 template <int TZ, int TD, bool VEC>
 __global__ __launch_bounds__(VT) void verify_sample_kernel(VerifyArgs a, const Part* parts, int nseg,
                                                            const Decision* decisions, const double* left) {
-  __shared__ double wsum[VT / 64];
-  __shared__ int found, last;
-  __shared__ double before;
-  __shared__ int sseg;
-  __shared__ int skind;
-  __shared__ double goal;
+  constexpr int R = kPer / 4;  // rounds of four logits a thread
+  __shared__ double table[32];
+  __shared__ double wsum[R][VT / 64];
+  __shared__ int wfirst[VT / 64], wlast[VT / 64];
+  __shared__ double before, goal;
+  __shared__ int sseg, skind;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const int b = blockIdx.x;
   Decision d = decisions[b];
   const int64_t base = (int64_t)b * (a.k + 1);
-  // the accepted drafts, their log-probabilities, and what lies past the new token
-  for (int j = t; j <= a.k; j += VT) {
-    if (j == d.accepted) continue;
-    const bool in = j < d.accepted;
-    const int tok = in ? a.drafts[(int64_t)b * a.k + j] : -1;
-    a.tokens[base + j] = tok;
-    if (a.lp) {
-      float lp = 0.f;
-      if (in) {
-        const Part* p = parts + (base + j) * nseg;
-        float m = -INFINITY;
-        for (int s = 0; s < nseg; ++s) m = fmaxf(m, p[s].most);
-        double v = 0;
-        for (int s = 0; s < nseg; ++s)
-          if (p[s].most > -INFINITY) v += p[s].sum * weight(p[s].most, m, a.inv_t);
-        const float z = load_elem(row_of<TZ>(a.z, base + j, a.ld), TZ, tok);
-        lp = (float)(((double)z - (double)m) * a.inv_t - log(v));
-      }
-      a.lp[base + j] = lp;
-    }
-  }
-  if (t == 0) {
-    a.accepted[b] = d.accepted;
-    if (d.kind == kNone) {
-      a.tokens[base + d.accepted] = -1;
-      if (a.lp) a.lp[base + d.accepted] = __uint_as_float(0x7FC00000u);
-    }
-  }
   if (d.kind == kNone) return;
-  if (t == 0) {
+  const double u = a.u[base + a.k];
+  put_table(table);
+  __syncthreads();
+  if (wave == 0) {
     // the segment in which the running sum passes u of the total
     const double* l = left + (int64_t)b * nseg;
-    double all = 0;
-    for (int s = 0; s < nseg; ++s) all += l[s];
-    int kind = d.kind;
     const Part* p = parts + (base + d.accepted) * nseg;
-    // nothing left (p and q the same but for rounding): from p
-    if (!(all > 0)) {
+    int kind = d.kind;
+    const auto mass = [&](int s) {
+      if (s >= nseg) return 0.0;
+      if (kind == d.kind) return l[s];
+      return p[s].most > -INFINITY ? p[s].sum * weight(p[s].most, d.p_most, a.inv_t, table) / d.p_sum : 0.0;
+    };
+    double all = 0;
+    for (int s0 = 0; s0 < nseg; s0 += 64) all += wave_sum64(mass(s0 + lane));
+    if (!(all > 0)) {  // nothing left (p and q the same but for rounding): from p
       kind = kPlain;
       all = 0;
-      for (int s = 0; s < nseg; ++s)
-        if (p[s].most > -INFINITY) all += p[s].sum * weight(p[s].most, d.p_most, a.inv_t) / d.p_sum;
+      for (int s0 = 0; s0 < nseg; s0 += 64) all += wave_sum64(mass(s0 + lane));
     }
-    const double g = (double)a.u[base + a.k] * all;
+    const double g = u * all;
     double run = 0, at = 0;
     int seg = -1;
-    for (int s = 0; s < nseg; ++s) {
-      const double v = kind == d.kind ? l[s]
-                       : p[s].most > -INFINITY ? p[s].sum * weight(p[s].most, d.p_most, a.inv_t) / d.p_sum : 0.0;
-      if (v > 0) {
-        seg = s;  // (the last with anything in it, where rounding or u leaves none)
-        at = run;
-        if (run + v > g) break;
+    for (int s0 = 0; s0 < nseg; s0 += 64) {
+      const double v = mass(s0 + lane), to = run + wave_scan64(v, lane);
+      const uint64_t some = __ballot(v > 0), past = __ballot(v > 0 && to > g);
+      if (some) {  // the first that passes, or the last with anything in it, where rounding or u leaves none
+        const int src = past ? __ffsll((unsigned long long)past) - 1 : 63 - __clzll((long long)some);
+        seg = s0 + src;
+        at = __shfl(to - v, src);
       }
-      run += v;
+      if (past) break;
+      run = __shfl(to, 63);
     }
-    sseg = seg;
-    before = at;
-    skind = kind;
-    goal = g;
-    found = 0x7FFFFFFF;
-    last = -1;
+    if (lane == 0) {
+      sseg = seg;
+      before = at;
+      goal = g;
+      skind = kind;
+    }
   }
   __syncthreads();
   d.kind = skind;
-  const void* zr = row_of<TZ>(a.z, base + d.accepted, a.ld);
-  const void* dr = d.kind == kMinus ? row_of<TD>(a.zd, (int64_t)b * a.k + d.accepted, a.ld_d) : nullptr;
-  const double p_inv = 1.0 / d.p_sum, q_inv = d.kind == kMinus ? 1.0 / d.q_sum : 0.0;
-  double run = before;
+  const int seg = sseg;
   const double g = goal;
-  for (int i = 0; i < kPer / 4; ++i) {
-    const int64_t c = (int64_t)sseg * kSeg + i * (VT * 4) + t * 4;
-    float z[4], zd[4] = {0.f, 0.f, 0.f, 0.f};
-    load4<TZ, VEC>(zr, c, a.V, z);
-    if (dr) load4<TD, VEC>(dr, c, a.V, zd);
-    double w[4];
+  double w[kPer], scan[R];
+  left_in<TZ, TD, VEC>(a, d, b, seg, table, w);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = left_of(d, z[j], zd[j], c + j, a.inv_t, p_inv, q_inv);
-    double mine = (w[0] + w[1]) + (w[2] + w[3]), scan = mine;
+  for (int i = 0; i < R; ++i) {
+    scan[i] = wave_scan64((w[4 * i] + w[4 * i + 1]) + (w[4 * i + 2] + w[4 * i + 3]), lane);
+    if (lane == 63) wsum[i][wave] = scan[i];
+  }
+  __syncthreads();
+  int first = 0x7FFFFFFF, last = -1;
+  double run = before;
 #pragma unroll
-    for (int s = 1; s < 64; s <<= 1) {
-      const double o = __shfl_up(scan, s);
-      if (lane >= s) scan += o;
+  for (int i = 0; i < R; ++i) {
+    double to = run + (scan[i] - ((w[4 * i] + w[4 * i + 1]) + (w[4 * i + 2] + w[4 * i + 3])));
+#pragma unroll
+    for (int k = 0; k < VT / 64; ++k) {
+      if (k < wave) to += wsum[i][k];
+      run += wsum[i][k];
     }
-    if (lane == 63) wsum[wave] = scan;
-    __syncthreads();
-    double to = run + (scan - mine);
-    for (int k = 0; k < wave; ++k) to += wsum[k];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      to += w[j];
-      if (w[j] > 0) {
-        atomicMax(&last, (int)(c + j));
-        if (to > g) atomicMin(&found, (int)(c + j));
+      const int c = seg * kSeg + i * (VT * 4) + t * 4 + j;
+      to += w[4 * i + j];
+      if (w[4 * i + j] > 0) {
+        last = c;
+        if (to > g && c < first) first = c;
       }
     }
-    run += (wsum[0] + wsum[1]) + (wsum[2] + wsum[3]);
-    __syncthreads();
   }
+#pragma unroll
+  for (int s = 32; s > 0; s >>= 1) {
+    first = min(first, __shfl_xor(first, s));
+    last = max(last, __shfl_xor(last, s));
+  }
+  if (lane == 0) {
+    wfirst[wave] = first;
+    wlast[wave] = last;
+  }
+  __syncthreads();
   if (t == 0) {
-    const int tok = found != 0x7FFFFFFF ? found : last;
+    first = min(min(wfirst[0], wfirst[1]), min(wfirst[2], wfirst[3]));
+    last = max(max(wlast[0], wlast[1]), max(wlast[2], wlast[3]));
+    const int tok = first != 0x7FFFFFFF ? first : last;
     a.tokens[base + d.accepted] = tok;
     if (a.lp) {
-      const float z = load_elem(zr, TZ, tok);
+      const float z = load_elem(row_of<TZ>(a.z, base + d.accepted, a.ld), TZ, tok);
       a.lp[base + d.accepted] = (float)(((double)z - (double)d.p_most) * a.inv_t - log(d.p_sum));
     }
   }

@@ -78,7 +78,7 @@ def backward_bounds(xa, W, A, B, s, dy, dx_type, factor):
     M, N = dy.shape
     K, r = W.shape[1], len(A)
     dq = dequantize_ref(*quantize_ref(dy, 1), 1)
-    wide = M <= 16 or dx_type == "f32"
+    wide = dx_type == "f32"
     u = abs(s) * (np.abs(dy) @ np.abs(B))
     t = abs(s) * (np.abs(xa) @ np.abs(A).T)
     r_u, r_t = (N + 2) * U + 2.0 ** -17, (K + 2) * U + 2.0 ** -17

@@ -129,7 +129,7 @@ def test_workspace_sizes():
     assert L.hydra_verify_drafts_workspace_bytes(8, 4, 64, None) == NULL
     for M, K, r in ((1, 16, 0), (8, 4096, 16), (2048, 11008, 128), (1 << 20, 4096, 16)):
         n = H.hydra_fp8_lora_linear_workspace_bytes(M, K, r)
-        assert 2 * M * K <= n <= 4 * M * K + 40 * M * 128 + (1 << 24)
+        assert M * K <= n <= 2 * M * K + 40 * M * 128 + (1 << 24)
     for n, k, V in ((1, 0, 1), (64, 7, 50272), (1, 128, 1 << 21)):
         assert 0 < H.hydra_verify_drafts_workspace_bytes(n, k, V) < 1 << 24
 
