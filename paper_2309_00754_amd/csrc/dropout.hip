@@ -37,7 +37,7 @@ __global__ __launch_bounds__(DT) void dropout_kernel(DropoutArgs a) {
   float x[8], r[8];
   load8<X>(a.x, i, x);
   if constexpr (R >= 0) load8<R>(a.res, i, r);
-  const uint4 w = dropout_words(a.rng, group);
+  const uint4 w = dropout_words(a.rng[0], a.rng[1], group);
   float y[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
@@ -61,7 +61,7 @@ __global__ __launch_bounds__(DT) void dropout_any_kernel(DropoutArgs a, size_t f
   const size_t group = from + (size_t)blockIdx.x * DT + threadIdx.x;
   const size_t n = (size_t)a.n;
   if (group * 8 >= n) return;
-  const uint4 w = dropout_words(a.rng, group);
+  const uint4 w = dropout_words(a.rng[0], a.rng[1], group);
   for (int j = 0; j < 8; ++j) {
     const size_t i = group * 8 + j;
     if (i >= n) return;

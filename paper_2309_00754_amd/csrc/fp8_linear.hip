@@ -26,14 +26,16 @@ namespace {
 
 // ------------------------------------------------------------------ before the product
 
-constexpr int P_WAVES = 4;
+constexpr int P_WAVES = 8;
+constexpr int kFewRows = 16;
+constexpr int kStagedChunks = 8;  // most partial sums of T at padded rank 16 above kFewRows rows
 
-// 16 rows and one chunk of K a workgroup; a wave takes the chunk's blocks in
-// turn.  Lane l holds values 32 (l / 16) ... + 31 of the block of row l % 16, in
-// four pieces of eight: a block's maximum is over four lanes, its bytes are two
-// 16-byte stores a lane, and piece j of all lanes is one 16x16x32 product of T
-// (with its values of k in another order, the same for A).
-template <int RP>
+// 16 rows and one chunk of K a workgroup; a wave takes the chunk's blocks in turn.
+// Lane l holds values 32 j + 8 (l / 16) ... + 7, j = 0 ... 3, of the block of row l % 16:
+// four lanes read 64 consecutive bytes of a row, a block's maximum is over four
+// lanes, and piece j of all lanes is one 16x16x32 product of T.
+// QUANT: x's bytes and scales; OWN: the adapter has an input of its own.
+template <int RP, bool QUANT, bool OWN>
 __global__ __launch_bounds__(P_WAVES * 64) void fp8_prep_kernel(Fp8PrepArgs g) {
   constexpr int TJ = RP / 16, TJ1 = TJ > 0 ? TJ : 1;
   const int t = threadIdx.x, lane = t & 63, l16 = lane & 15, lg = lane >> 4;
@@ -41,36 +43,27 @@ __global__ __launch_bounds__(P_WAVES * 64) void fp8_prep_kernel(Fp8PrepArgs g) {
   const int K = g.K, kb_n = (K + kFp8Block - 1) / kFp8Block;
   const int m0 = blockIdx.x * 16, rows = min(16, g.M - m0);
   const uint32_t bytes = (uint32_t)rows * K * 2u;
-  const bool quantize = g.x != nullptr;
-  const bool same = g.xa == g.x;
-  const __amdgpu_buffer_rsrc_t xr = make_rsrc(quantize ? g.x + (size_t)m0 * K : nullptr, quantize ? bytes : 0u);
-  const __amdgpu_buffer_rsrc_t ar = make_rsrc(TJ > 0 ? g.xa + (size_t)m0 * K : nullptr, TJ > 0 ? bytes : 0u);
+  const __amdgpu_buffer_rsrc_t xr = make_rsrc((QUANT ? g.x : g.xa) + (size_t)m0 * K, bytes);
+  const __amdgpu_buffer_rsrc_t ar = make_rsrc(OWN ? g.xa + (size_t)m0 * K : nullptr, OWN ? bytes : 0u);
   const __amdgpu_buffer_rsrc_t Ar = make_rsrc(TJ > 0 ? g.A : nullptr, TJ > 0 ? (uint32_t)g.r * K * 2u : 0u);
   f32x4_t acc[TJ1];
 #pragma unroll
   for (int j = 0; j < TJ1; ++j) acc[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   const int kb1 = min(kb_n, (int)(blockIdx.y + 1) * g.kch);
   for (int kb = blockIdx.y * g.kch + wave; kb < kb1; kb += P_WAVES) {
-    const int k = kb * kFp8Block + 32 * lg;
+    const int k = kb * kFp8Block + 8 * lg;
     uint4 v[4], a[4];
     uint4 w[4][TJ1];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = buf_load16(xr, k + 8 * j < K ? (l16 * K + k + 8 * j) * 2 : kOutOfRange);
-    if constexpr (TJ > 0) {
+    for (int j = 0; j < 4; ++j) {
+      const bool ok = k + 32 * j < K;
+      v[j] = buf_load16(xr, ok ? (l16 * K + k + 32 * j) * 2 : kOutOfRange);
+      if constexpr (OWN) a[j] = buf_load16(ar, ok ? (l16 * K + k + 32 * j) * 2 : kOutOfRange);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const bool ok = k + 8 * j < K;
-        a[j] = quantize && same ? v[j] : buf_load16(ar, ok ? (l16 * K + k + 8 * j) * 2 : kOutOfRange);
-#pragma unroll
-        for (int i = 0; i < TJ; ++i)
-          w[j][i] = buf_load16(Ar, ok ? ((i * 16 + l16) * K + k + 8 * j) * 2 : kOutOfRange);
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int i = 0; i < TJ; ++i) acc[i] = mfma16(a[j], w[j][i], acc[i]);
+      for (int i = 0; i < TJ; ++i)
+        w[j][i] = buf_load16(Ar, ok ? ((i * 16 + l16) * K + k + 32 * j) * 2 : kOutOfRange);
     }
-    if (quantize) {
+    if constexpr (QUANT) {
       float f[4][8];
       float most = 0.f;
 #pragma unroll
@@ -84,17 +77,18 @@ __global__ __launch_bounds__(P_WAVES * 64) void fp8_prep_kernel(Fp8PrepArgs g) {
       const int byte = fp8_scale_byte(most);
       const float p = fp8_inverse(byte);
       if (l16 < rows) {
-        const size_t at = (size_t)(m0 + l16) * K + k;
+        uint8_t* q = g.xq + (size_t)(m0 + l16) * K + k;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (k + 16 * h >= K) continue;
-          *reinterpret_cast<uint4*>(g.xq + at + 16 * h) =
-              make_uint4(fp8_pack4(f[2 * h], p), fp8_pack4(f[2 * h] + 4, p), fp8_pack4(f[2 * h + 1], p),
-                         fp8_pack4(f[2 * h + 1] + 4, p));
-        }
+        for (int j = 0; j < 4; ++j)
+          if (k + 32 * j < K)
+            *reinterpret_cast<uint2*>(q + 32 * j) = make_uint2(fp8_pack4(f[j], p), fp8_pack4(f[j] + 4, p));
         if (lg == 0) g.xs[(size_t)(m0 + l16) * kb_n + kb] = (uint8_t)byte;
       }
     }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int i = 0; i < TJ; ++i) acc[i] = mfma16(OWN ? a[j] : v[j], w[j][i], acc[i]);
   }
   if constexpr (TJ > 0) {
     // acc[j] of lane l: T[m0 + 4 lg + e][16 j + l16], to be added over the waves
@@ -114,27 +108,17 @@ __global__ __launch_bounds__(P_WAVES * 64) void fp8_prep_kernel(Fp8PrepArgs g) {
   }
 }
 
-// T[row][j] as the sum of its chunks, in their order.
-__device__ __forceinline__ float t_sum(const Fp8LinearArgs& a, int row, int j) {
-  const size_t stride = (size_t)a.M * a.rp;
-  const float* p = a.part + (size_t)row * a.rp + j;
-  float v = 0.f;
-  for (int c = 0; c < a.nch; ++c) v += p[c * stride];
-  return v;
-}
-
 // ------------------------------------------------------------------ few rows
 
-constexpr int kFewRows = 16;
-constexpr int S_WAVES = 8;
 
 // 16 NB rows of W a workgroup, the blocks of K dealt to its waves; their partial
-// sums meet in LDS in wave order.
-template <int NB>
-__global__ __launch_bounds__(S_WAVES * 64) void fp8_stream_kernel(Fp8LinearArgs a) {
-  constexpr int U = 4;
-  __shared__ f32x4_t red[S_WAVES][NB][64];
-  __shared__ float T[16][129];
+// sums meet in LDS in wave order.  U blocks a wave are requested before the first
+// is used.
+template <int NB, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void fp8_stream_kernel(Fp8LinearArgs a) {
+  constexpr int U = 4, NT = WAVES * 64;
+  __shared__ f32x4_t red[WAVES][NB][64];
+  __shared__ float T[16][132];
   __shared__ uint16_t Bs[16 * NB][130];
   const int t = threadIdx.x, lane = t & 63, l16 = lane & 15, lg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -147,12 +131,12 @@ __global__ __launch_bounds__(S_WAVES * 64) void fp8_stream_kernel(Fp8LinearArgs 
   f32x4_t acc[NB];
 #pragma unroll
   for (int b = 0; b < NB; ++b) acc[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  for (int kb0 = wave; kb0 < kb_n; kb0 += S_WAVES * U) {
+  for (int kb0 = wave; kb0 < kb_n; kb0 += WAVES * U) {
     uint4 x[U][2], w[U][NB][2];
     int sx[U], sw[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int kb = kb0 + u * S_WAVES, k = kb * kFp8Block + 32 * lg;
+      const int kb = kb0 + u * WAVES, k = kb * kFp8Block + 32 * lg;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const bool ok = k + 16 * h < K;
@@ -165,6 +149,7 @@ __global__ __launch_bounds__(S_WAVES * 64) void fp8_stream_kernel(Fp8LinearArgs 
       sx[u] = xs[kc];
       sw[u] = ws[kc];
     }
+    __builtin_amdgcn_sched_barrier(0);
     // lane l has values 32 (l / 16) ... + 31 of a block; the products take eight of
     // every lane at a time
 #pragma unroll
@@ -185,30 +170,51 @@ __global__ __launch_bounds__(S_WAVES * 64) void fp8_stream_kernel(Fp8LinearArgs 
   for (int b = 0; b < NB; ++b) red[wave][b][lane] = acc[b];
   const bool lora = a.y_on && a.rp > 0;
   if (lora) {
-    for (int e = t; e < M * a.rp; e += S_WAVES * 64) T[e / a.rp][e % a.rp] = a.s * t_sum(a, e / a.rp, e % a.rp);
+    const size_t stride = (size_t)M * a.rp;
+    for (int e = t; e < M * a.rp / 4; e += NT) {  // T as the sum of its chunks, in their order
+      const float* p = a.part + 4 * e;
+      f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+      for (int c = 0; c < a.nch; ++c) v += *reinterpret_cast<const f32x4_t*>(p + c * stride);
+      *reinterpret_cast<f32x4_t*>(&T[4 * e / a.rp][4 * e % a.rp]) = a.s * v;
+    }
     const int rows = min(16 * NB, N - n0);
-    for (int e = t; e < rows * a.r; e += S_WAVES * 64)
-      Bs[e / a.r][e % a.r] = a.B[(size_t)(n0 + e / a.r) * a.ldb + e % a.r];
+    for (int e = t; e < rows * a.r; e += NT) Bs[e / a.r][e % a.r] = a.B[(size_t)(n0 + e / a.r) * a.ldb + e % a.r];
   }
   __syncthreads();
-  for (int e = t; e < 16 * NB * M; e += S_WAVES * 64) {
+  for (int e = t; e < 16 * NB * M; e += NT) {
     const int nl = e % (16 * NB), m = e / (16 * NB), n = n0 + nl;
     if (n >= N) continue;
     const int b = nl / 16, src = (nl % 16) / 4 * 16 + m, i = nl % 4;
     float v = red[0][b][src][i];
 #pragma unroll
-    for (int w = 1; w < S_WAVES; ++w) v += red[w][b][src][i];
+    for (int w = 1; w < WAVES; ++w) v += red[w][b][src][i];
     const size_t at = (size_t)m * N + n;
     if (a.y_off) store_elem(a.y_off, a.y_type, at, v);
     if (!a.y_on) continue;
     if (lora) {
       float u = 0.f;
       for (int j = 0; j < a.r; ++j) u = fmaf(T[m][j], bf16_to_f32(Bs[nl][j]), u);
-      if (a.drop > 0) u = dropout_keeps(dropout_words(a.rng, at >> 3), (int)(at & 7), a.drop) ? u * a.keep : 0.f;
       v += u;
     }
     store_elem(a.y_on, a.y_type, at, v);
   }
+}
+
+template <int NB, int WAVES>
+void launch_stream_as(const Fp8LinearArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL((fp8_stream_kernel<NB, WAVES>), dim3((a.N + 16 * NB - 1) / (16 * NB)), dim3(WAVES * 64), 0, stream, a);
+}
+// Sixteen rows of W a workgroup; thirty-two where that leaves two workgroups a CU and more
+// than four rows of x, which every workgroup reads, count.  us, <1, 8> and <2, 8>: 8 x 4096 x
+// 4096 6.8 and 7.8, 8 x 11008 x 4096 13.4 and 15.4, 8 x 4096 x 11008 15.9 and 20.6, 16 x
+// 32000 x 4096 39.3 and 33.4, 8 x 32000 x 4096 31.3 and 30.0, 1 x 32000 x 4096 25.3 and 26.7;
+// four waves or sixteen, or 64 rows: slower at most sizes, by up to a half.
+void launch_stream(const Fp8LinearArgs& a, hipStream_t stream) {
+  if (a.N > 16384 && a.M > 4)
+    launch_stream_as<2, 8>(a, stream);
+  else
+    launch_stream_as<1, 8>(a, stream);
 }
 
 // ------------------------------------------------------------------ tiles
@@ -224,10 +230,11 @@ struct GemmArgs {
 // TM x TN tile, WM x WN sub-tile a wave, KS waves a sub-tile (each takes its share
 // of every slab), slabs of BK values of K in a ring of NS; four more waves copy.
 // WIDE: bf16 products, in steps of 32 values of K, into fp32 outputs; else 8-bit ones, in
-// steps of 64, into bf16.
-template <bool WIDE_, int TM_, int TN_, int WM_, int WN_, int KS_, int BK_, int NS_>
+// steps of 64, into bf16.  WPC workgroups share a CU.
+template <bool WIDE_, int TM_, int TN_, int WM_, int WN_, int KS_, int BK_, int NS_, int WPC_ = 1>
 struct Tile {
   static constexpr bool WIDE = WIDE_;
+  static constexpr int WPC = WPC_;
   static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, KS = KS_, BK = BK_, NS = NS_;
   static constexpr int NWN = TN / WN, NMW = TM / WM * NWN * KS, NW = NMW + 4, NT = NW * 64;
   static constexpr int MT = WM / 32, NTL = WN / 32, NQ = MT * NTL;
@@ -240,13 +247,14 @@ struct Tile {
   static constexpr int RD = STEP / 32;                 // 16-byte reads a lane and row in a step
   static constexpr int OLD = TN + 4;                   // row of the output tile in LDS (fp32, in values)
   static constexpr int OUT = KS * TM * OLD * 4;        // bytes of the KS partial sums of it
-  // rows of s T (hi | lo) and of B, 16 bytes apart from the next, at padded rank rp, and a mask
-  static constexpr int lora_bytes(int rp) { return TM * (4 * rp + 16) + TN * (2 * rp + 16) + TM * TN / 8; }
+  // rows of s T (hi | lo) and of B, 16 bytes apart from the next, at padded rank rp
+  static constexpr int lora_bytes(int rp) { return TM * (4 * rp + 16) + TN * (2 * rp + 16); }
   static constexpr size_t cmax(size_t x, size_t y) { return x > y ? x : y; }
+  static constexpr int MASK = TM * TN / 8;             // bytes of dropout's mask, after the rest
   static constexpr size_t LDS = cmax(cmax(size_t(NS) * STAGE * 16, OUT), lora_bytes(128));
   static_assert(TM % (RPB * 4) == 0 && TN % (RPB * 4) == 0 && SPW >= 1 && TN % 8 == 0, "whole copies, steps and groups");
   static_assert(SPW <= 4 && (SPW == 1 || SPW % 2 == 0), "steps listed below");
-  static_assert(WN <= kFp8Block && LDS <= 160 * 1024 && (NS - 2) * DPW < 64, "one scale a sub-tile and slab; LDS; waits");
+  static_assert(WN <= kFp8Block && LDS + MASK <= 160 * 1024 / WPC && (NS - 2) * DPW < 64, "one scale a sub-tile and slab; LDS; waits");
 };
 
 template <int V>
@@ -284,11 +292,11 @@ __device__ __forceinline__ uint32_t load_scales(const uint8_t* p, int64_t at, in
 
 // MASK: the update goes through dropout's mask.
 template <class G, bool MASK>
-__global__ __launch_bounds__(G::NT) void fp8_gemm_kernel(GemmArgs g) {
+__global__ __launch_bounds__(G::NT, G::NT / 256 * G::WPC) void fp8_gemm_kernel(GemmArgs g) {
   constexpr int TM = G::TM, TN = G::TN, WM = G::WM, WN = G::WN, KS = G::KS, BK = G::BK, NS = G::NS;
   constexpr int MT = G::MT, NTL = G::NTL, NQ = G::NQ, SPW = G::SPW;
   constexpr int CPR = G::CPR, RPB = G::RPB, RD = G::RD;
-  __shared__ uint4 sm[G::LDS / 16];
+  __shared__ uint4 sm[(G::LDS + (MASK ? G::MASK : 0)) / 16];
   const Fp8LinearArgs& a = g.a;
   const int M = a.M, N = a.N, K = a.K, kb_n = (K + kFp8Block - 1) / kFp8Block;
   const int t = threadIdx.x, lane = t & 63;
@@ -385,11 +393,63 @@ __global__ __launch_bounds__(G::NT) void fp8_gemm_kernel(GemmArgs g) {
   const int rp = a.rp, lrp = 31 - __builtin_clz(rp | 1), ldt = 2 * rp + 8, ldb = rp + 8;  // (in values)
   uint16_t* const Ts = reinterpret_cast<uint16_t*>(sm);
   uint16_t* const Bs = Ts + TM * ldt;
-  auto put_update = [&]() __attribute__((always_inline)) {
-    const int rows = min(TM, M - m0), cols = min(TN, N - n0);
+  // Four values of s T, of a tile's row.
+  auto put_t = [&](int row, int j, const f32x4_t& v) __attribute__((always_inline)) {
+    uint32_t hi[4], lo[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float f = a.s * v[i];
+      hi[i] = f32_to_bf16_any(f);
+      lo[i] = (hi[i] & 0x7FFF) < 0x7F80 ? f32_to_bf16_any(f - bf16_to_f32(hi[i])) : 0;  // (none of an infinity)
+    }
+    *reinterpret_cast<uint2*>(Ts + row * ldt + j) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
+    *reinterpret_cast<uint2*>(Ts + row * ldt + rp + j) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+  };
+  const int rows = min(TM, M - m0), cols = min(TN, N - n0);
+  // By the 256 threads of the copy waves.  At padded rank 16, the usual one, the loads
+  // come ahead (`ahead`), while the last products run and y_off is stored.
+  struct Ahead {
+    f32x4_t t[TM * 4 > 256 ? TM * 4 / 256 : 1][kStagedChunks];
+    uint4 b[TN * 2 > 256 ? TN * 2 / 256 : 1];
+  };
+  const bool ahead = a.y_on && rp == 16 && !a.ts && g.bvec && a.nch <= kStagedChunks;
+  auto load_ahead = [&](Ahead& u, int tc) __attribute__((always_inline)) {
+    const size_t stride = (size_t)M * 16;
+#pragma unroll
+    for (int i = 0; i * 256 < TM * 4; ++i) {
+      const int e = i * 256 + tc, row = e / 4, j = e % 4 * 4;
+#pragma unroll
+      for (int c = 0; c < kStagedChunks; ++c) {
+        u.t[i][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        if (row < rows && c < a.nch)
+          u.t[i][c] = *reinterpret_cast<const f32x4_t*>(a.part + (size_t)(m0 + row) * 16 + j + c * stride);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i * 256 < TN * 2; ++i) {
+      const int e = i * 256 + tc, row = e / 2, j = e % 2 * 8;
+      u.b[i] = make_uint4(0, 0, 0, 0);
+      if (row < cols && j < a.r) u.b[i] = *reinterpret_cast<const uint4*>(a.B + (size_t)(n0 + row) * a.ldb + j);
+    }
+  };
+  auto put_ahead = [&](const Ahead& u, int tc) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i * 256 < TM * 4; ++i) {
+      const int e = i * 256 + tc;
+      f32x4_t v = u.t[i][0];
+#pragma unroll
+      for (int c = 1; c < kStagedChunks; ++c) v += u.t[i][c];
+      if (TM * 4 % 256 == 0 || e < TM * 4) put_t(e / 4, e % 4 * 4, v);
+    }
+#pragma unroll
+    for (int i = 0; i * 256 < TN * 2; ++i) {
+      const int e = i * 256 + tc;
+      if (TN * 2 % 256 == 0 || e < TN * 2) *reinterpret_cast<uint4*>(Bs + e / 2 * ldb + e % 2 * 8) = u.b[i];
+    }
+  };
+  auto put_update = [&](int tc) __attribute__((always_inline)) {
     if (a.ts) {
-#pragma unroll 1
-      for (int e = te; e < TM * rp / 4; e += G::NT) {  // 16 bytes each
+      for (int e = tc; e < TM * rp / 4; e += 256) {  // 16 bytes each
         const int row = e >> (lrp - 2), c = (e & (rp / 4 - 1)) * 8;
         uint4 v = make_uint4(0, 0, 0, 0);
         if (row < rows) v = *reinterpret_cast<const uint4*>(a.ts + (size_t)(m0 + row) * 2 * rp + c);
@@ -397,56 +457,36 @@ __global__ __launch_bounds__(G::NT) void fp8_gemm_kernel(GemmArgs g) {
       }
     } else {
       const size_t stride = (size_t)M * rp;
-#pragma unroll 1
-      for (int e = te; e < TM * rp / 4; e += G::NT) {
+#pragma unroll 4
+      for (int e = tc; e < TM * rp / 4; e += 256) {
         const int row = e >> (lrp - 2), j = (e & (rp / 4 - 1)) * 4;
         f32x4_t v = {0.f, 0.f, 0.f, 0.f};
         if (row < rows) {
           const float* p = a.part + (size_t)(m0 + row) * rp + j;
-#pragma unroll 2
           for (int c = 0; c < a.nch; ++c) v += *reinterpret_cast<const f32x4_t*>(p + c * stride);
         }
-        uint32_t hi[4], lo[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float f = a.s * v[i];
-          hi[i] = f32_to_bf16_any(f);
-          lo[i] = (hi[i] & 0x7FFF) < 0x7F80 ? f32_to_bf16_any(f - bf16_to_f32(hi[i])) : 0;  // (none of an infinity)
-        }
-        *reinterpret_cast<uint2*>(Ts + row * ldt + j) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
-        *reinterpret_cast<uint2*>(Ts + row * ldt + rp + j) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+        put_t(row, j, v);
       }
     }
     if (g.bvec) {
-#pragma unroll 1
-      for (int e = te; e < TN * rp / 8; e += G::NT) {
+#pragma unroll 4
+      for (int e = tc; e < TN * rp / 8; e += 256) {
         const int row = e >> (lrp - 3), j = (e & (rp / 8 - 1)) * 8;
         uint4 v = make_uint4(0, 0, 0, 0);
         if (row < cols && j < a.r) v = *reinterpret_cast<const uint4*>(a.B + (size_t)(n0 + row) * a.ldb + j);
         *reinterpret_cast<uint4*>(Bs + row * ldb + j) = v;
       }
     } else {
-#pragma unroll 1
-      for (int e = te; e < TN * rp; e += G::NT) {
+#pragma unroll 8
+      for (int e = tc; e < TN * rp; e += 256) {
         const int row = e >> lrp, j = e & (rp - 1);
         Bs[row * ldb + j] = row < cols && j < a.r ? a.B[(size_t)(n0 + row) * a.ldb + j] : (uint16_t)0;
       }
     }
   };
   // Dropout's mask of the update (N % 8 == 0 here): a bit a column, a byte a block of
-  // the generator.
-  uint8_t* const mask = reinterpret_cast<uint8_t*>(Bs + TN * ldb);
-  auto put_mask = [&]() __attribute__((always_inline)) {
-#pragma unroll 1
-    for (int e = te; e < TM * TN / 8; e += G::NT) {
-      const int row = e / (TN / 8), col = e % (TN / 8) * 8;
-      const uint4 bits = dropout_words(a.rng, ((uint64_t)(m0 + row) * N + n0 + col) >> 3);
-      uint32_t m = 0;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) m |= dropout_keeps(bits, j, a.drop) ? 1u << j : 0u;
-      mask[e] = (uint8_t)m;
-    }
-  };
+  // the generator.  The copy waves make it while the products run.
+  uint8_t* const mask = reinterpret_cast<uint8_t*>(sm) + G::LDS;
   // s T B^T onto the accumulators (of the first of a sub-tile's KS waves): rows of
   // [B | B] against rows of [hi | lo]
   auto add_update = [&](f32x16_t (&acc)[MT][NTL]) __attribute__((always_inline)) {
@@ -492,8 +532,8 @@ __global__ __launch_bounds__(G::NT) void fp8_gemm_kernel(GemmArgs g) {
         }
     }
   };
-  // By the role of the wave: `do_put` and `do_add` are nothing on a copy wave.
-  auto finish = [&](auto do_put, auto do_add) __attribute__((always_inline)) {
+  // By the role of the wave: do_stage is a copy wave's, the others a matrix wave's.
+  auto finish = [&](auto do_stage, auto do_put, auto do_add) __attribute__((always_inline)) {
     asm volatile("" : "+v"(te));
     const bool lora = a.y_on && rp > 0;
     if (a.y_off || !lora) {
@@ -506,8 +546,7 @@ __global__ __launch_bounds__(G::NT) void fp8_gemm_kernel(GemmArgs g) {
       if (!lora) return;
       __syncthreads();
     }
-    put_update();
-    if constexpr (MASK) put_mask();
+    do_stage();
     __syncthreads();
     do_add();
     __syncthreads();
@@ -537,6 +576,19 @@ __global__ __launch_bounds__(G::NT) void fp8_gemm_kernel(GemmArgs g) {
         dma16(wrs, sm + stage * G::STAGE + (TM + row) * CPR, ok ? (row + rl) * K + k : kOutOfRange);
       }
     };
+    const int tc = t - G::NMW * 64;
+    int next = tc;  // of this thread's bytes of the mask
+    const uint64_t seed = MASK ? a.rng[0] : 0, offset = MASK ? a.rng[1] : 0;
+    auto put_mask = [&]() __attribute__((always_inline)) {
+      if (next >= TM * TN / 8) return;
+      const int row = next / (TN / 8), col = next % (TN / 8) * 8;
+      const uint4 bits = dropout_words(seed, offset, ((uint64_t)(m0 + row) * N + n0 + col) >> 3);
+      uint32_t m = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) m |= dropout_keeps(bits, j, a.drop) ? 1u << j : 0u;
+      mask[next] = (uint8_t)m;
+      next += 256;
+    };
     // slabs past the last read zeros, so that the waits count the same throughout
 #pragma unroll
     for (int s = 0; s < NS; ++s) issue(s, s);
@@ -547,11 +599,16 @@ __global__ __launch_bounds__(G::NT) void fp8_gemm_kernel(GemmArgs g) {
       wait_vm<(NS - 2) * G::DPW>();
       lds_barrier();  // slab kt + 1 has landed, slab kt is in registers everywhere
       issue(stage, kt + NS);
+      if constexpr (MASK) put_mask();
       stage = stage + 1 == NS ? 0 : stage + 1;
     }
+    if constexpr (MASK)
+      while (next < TM * TN / 8) put_mask();
     wait_vm<0>();
+    Ahead up;
+    if (ahead) load_ahead(up, tc);
     lds_barrier();  // every copy has landed, every wave is done with the ring
-    finish([] {}, [] {});
+    finish([&] { ahead ? put_ahead(up, tc) : put_update(tc); }, [] {}, [] {});
   } else {
     // -------------------------------------------------------------- matrix waves
     f32x16_t acc[MT][NTL];
@@ -681,7 +738,7 @@ __global__ __launch_bounds__(G::NT) void fp8_gemm_kernel(GemmArgs g) {
       }
     }
     lds_barrier();
-    finish([&] { put(acc); }, [&] { add_update(acc); });
+    finish([] {}, [&] { put(acc); }, [&] { add_update(acc); });
   }
 }
 
@@ -701,32 +758,83 @@ hipError_t launch_tile(GemmArgs& g, hipStream_t stream) {
   return hipGetLastError();
 }
 
-// The tile: the largest that gives most CUs one.
+// The tile by a model of its time: base + fixed w + K / 128 (step w + pair r), us, for w
+// workgroups a CU one after the other (pair: in r rounds of two together).  The
+// numbers are fits to 15 row counts from 17 to 4096 and eight (N, K) from 1000 x 688
+// to 11008 x 4096 and 4096 x 11008 (rms error 5 to 11%).  They choose the best of the six
+// tiles or one 0.4% slower on average, 9% at most.  What they say: a small tile's
+// slab costs its copies (32 to 50 GB/s into a CU), the largest one's its products.
+// us, M x N x K into bf16 and fp32: 64 x 4096 x 4096 10.0 and 11.5, 333 x 4096 x
+// 11008 37 and 48, 1000 x 4096 x 4096 24 and 37, 2048 x 4096 x 4096 38 and 60.
+struct TileCost {
+  int tm, tn;
+  float base, fixed, step, pair;
+};
+constexpr TileCost kTiles[2][6] = {{{128, 256, 0.f, 5.8f, 0.767f, 0.f},
+                                    {128, 128, 0.f, 4.99f, 0.516f, 0.f},
+                                    {64, 128, 0.1f, 4.19f, 0.376f, 0.f},
+                                    {64, 64, 2.47f, 1.23f, 0.136f, 0.143f},
+                                    {32, 64, 1.98f, 1.93f, 0.219f, 0.f},
+                                    {32, 32, 3.36f, 0.5f, 0.084f, 0.095f}},
+                                   {{128, 256, 0.f, 6.42f, 1.318f, 0.f},
+                                    {128, 128, 0.f, 5.24f, 0.775f, 0.f},
+                                    {64, 128, 0.f, 4.56f, 0.542f, 0.f},
+                                    {64, 64, 2.16f, 1.58f, 0.182f, 0.195f},
+                                    {32, 64, 1.57f, 2.23f, 0.272f, 0.f},
+                                    {32, 32, 2.9f, 0.72f, 0.067f, 0.165f}}};
+
+int best_tile(bool wide, int M, int N, int K) {
+  int best = 0;
+  float least = 0.f;
+  for (int i = 0; i < 6; ++i) {
+    const TileCost& c = kTiles[wide][i];
+    const int64_t n = (int64_t)((M + c.tm - 1) / c.tm) * ((N + c.tn - 1) / c.tn);
+    const float w = (float)((n + 255) / 256), r = (float)((n + 511) / 512), slabs = (float)((K + 127) / 128);
+    const float us = c.base + c.fixed * w + slabs * (c.step * w + c.pair * r);
+    if (i == 0 || us < least) {
+      least = us;
+      best = i;
+    }
+  }
+  return best;
+}
+
 template <bool WIDE>
 hipError_t launch_rows(GemmArgs& g, hipStream_t stream) {
-  const auto tiles = [&](int tm, int tn) {
-    return (int64_t)((g.a.M + tm - 1) / tm) * ((g.a.N + tn - 1) / tn);
-  };
-  if (tiles(128, 256) >= 200) return launch_tile<Tile<WIDE, 128, 256, 64, 128, 1, 128, 3>>(g, stream);
-  if (tiles(128, 128) >= 200) return launch_tile<Tile<WIDE, 128, 128, 64, 64, 2, 128, 5>>(g, stream);
-  if (tiles(64, 128) >= 200) return launch_tile<Tile<WIDE, 64, 128, 64, 64, 2, 128, 6>>(g, stream);
-  if (tiles(64, 64) >= 200) return launch_tile<Tile<WIDE, 64, 64, 32, 64, 4, 256, 4>>(g, stream);
-  return launch_tile<Tile<WIDE, 32, 32, 32, 32, 4, 256, 8>>(g, stream);
+  switch (best_tile(WIDE, g.a.M, g.a.N, g.a.K)) {
+    case 0: return launch_tile<Tile<WIDE, 128, 256, 64, 128, 1, 128, 3>>(g, stream);
+    case 1: return launch_tile<Tile<WIDE, 128, 128, 64, 64, 2, 128, 4>>(g, stream);
+    case 2: return launch_tile<Tile<WIDE, 64, 128, 64, 64, 2, 128, 6>>(g, stream);
+    case 3: return launch_tile<Tile<WIDE, 64, 64, 32, 64, 2, 128, 4, 2>>(g, stream);
+    case 4: return launch_tile<Tile<WIDE, 32, 64, 32, 64, 4, 256, 6>>(g, stream);
+    default: return launch_tile<Tile<WIDE, 32, 32, 32, 32, 4, 256, 4, 2>>(g, stream);
+  }
 }
 
 template <int RP>
 void launch_prep(const Fp8PrepArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL(fp8_prep_kernel<RP>, dim3((a.M + 15) / 16, a.nch), dim3(P_WAVES * 64), 0, stream, a);
+  const dim3 grid((a.M + 15) / 16, a.nch), block(P_WAVES * 64);
+  if constexpr (RP == 0) {
+    hipLaunchKernelGGL((fp8_prep_kernel<0, true, false>), grid, block, 0, stream, a);
+  } else {
+    if (!a.x)
+      hipLaunchKernelGGL((fp8_prep_kernel<RP, false, false>), grid, block, 0, stream, a);
+    else if (a.xa == a.x)
+      hipLaunchKernelGGL((fp8_prep_kernel<RP, true, false>), grid, block, 0, stream, a);
+    else
+      hipLaunchKernelGGL((fp8_prep_kernel<RP, true, true>), grid, block, 0, stream, a);
+  }
 }
 
 }  // namespace
 
 // Chunks of K: about 512 workgroups, each at least a block a wave, and no more
-// partial sums of T than the product can add up on the side.
+// partial sums of T than the product can add up on the side.  us, four waves -> eight: 8 x
+// 4096 rank 16 P1 -> P2, 2048 x 4096 P3 -> P4, 333 x 11008 P5 -> P6.
 void fp8_prep_chunks(int M, int K, int rp, int& nch, int& kch) {
   const int kb = (K + kFp8Block - 1) / kFp8Block, mb = (M + 15) / 16;
   int want = (512 + mb - 1) / mb;
-  const int most = rp == 0 ? 64 : M <= 16 ? 32 : rp <= 32 ? 8 : 4;
+  const int most = rp == 0 ? 64 : M <= kFewRows ? 32 : rp <= 32 ? kStagedChunks : 4;
   want = want < most ? want : most;
   kch = (kb + want - 1) / want;
   kch = kch < P_WAVES ? P_WAVES : kch;
@@ -747,7 +855,7 @@ hipError_t launch_fp8_prep(const Fp8PrepArgs& a, hipStream_t stream) {
 
 hipError_t launch_fp8_linear(const Fp8LinearArgs& a, hipStream_t stream) {
   if (a.M <= kFewRows && !a.ts) {
-    hipLaunchKernelGGL(fp8_stream_kernel<2>, dim3((a.N + 31) / 32), dim3(S_WAVES * 64), 0, stream, a);
+    launch_stream(a, stream);
     return hipGetLastError();
   }
   GemmArgs g{};

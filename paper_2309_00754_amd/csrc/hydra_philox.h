@@ -20,11 +20,10 @@ __device__ __forceinline__ uint4 philox4x32(uint4 c, uint32_t k0, uint32_t k1) {
 }
 
 // Dropout's random numbers: sixteen bits an element, eight elements a block.
-// rng[0] is the key, rng[1] the counter's upper half, `group` (the element's
-// flat index / 8) its lower half; element 8 group + j has half j % 2 (0: the
+// `seed` is the key, `offset` the counter's upper half, `group` (the element's flat
+// index / 8) its lower half; element 8 group + j has half j % 2 (0: the
 // lower) of word j / 2.
-__device__ __forceinline__ uint4 dropout_words(const uint64_t* rng, uint64_t group) {
-  const uint64_t seed = rng[0], offset = rng[1];
+__device__ __forceinline__ uint4 dropout_words(uint64_t seed, uint64_t offset, uint64_t group) {
   return philox4x32(make_uint4((uint32_t)group, (uint32_t)(group >> 32), (uint32_t)offset, (uint32_t)(offset >> 32)),
                     (uint32_t)seed, (uint32_t)(seed >> 32));
 }

@@ -41,31 +41,35 @@ struct Decision {  // of one sequence
 };
 enum Kind : int { kPlain = 0, kMinus = 1, kWithout = 2, kNone = 3 };
 
-// e^x for x <= 0: 2^(k / 32) P(r), x = k ln 2 / 32 + r, |r| <= ln 2 / 64, with 2^(j / 32)
-// from a table (put_table) and the exponential series to r^5 / 5! (the rest is below
-// 3e-15): thirteen 64-bit operations where the series alone, to r^11, took twenty.
-// Below e^-700 it is 0.
+// e^((z - most) / T) for z <= most: with y = (z - most) 64 / (T ln 2) = k + f, k whole and
+// |f| <= 1/2, it is 2^(k / 64) e^(f ln 2 / 64): 2^(j / 64) from a table (put_table), the
+// exponential series to its fourth power (the rest is below 4e-14).  Eleven 64-bit
+// operations and four others; the series alone, to x^11, took twenty and nine.
+constexpr int kTable = 64;
 __device__ __forceinline__ void put_table(double* table) {
-  if (threadIdx.x < 32) table[threadIdx.x] = exp2(threadIdx.x * (1.0 / 32));
+  if (threadIdx.x < kTable) table[threadIdx.x] = exp2(threadIdx.x * (1.0 / kTable));
 }
-__device__ __forceinline__ double exp64(double x, const double* table) {
-  // k in the low bits of a sum whose last place is 1
-  const double big = 0x1.8p52;
-  const double t = fma(x, 0x1.71547652b82fep+5, big), k = t - big;  // 32 / ln 2
-  const double r = fma(-k, 0x1.62e42fefa39efp-6, x);
-  double s = fma(1.0 / 120, r, 1.0 / 24);
-  s = fma(s, r, 1.0 / 6);
-  s = fma(s, r, 0.5);
-  s = fma(s, r, 1.0);
-  s = fma(s, r, 1.0);
-  const int ki = (int)__double2loint(t);
-  s *= table[ki & 31];
-  const double v = __hiloint2double(__double2hiint(s) + ((ki >> 5) << 20), __double2loint(s));
-  return x < -700.0 ? 0.0 : v;
+// 64 / (T ln 2)
+__device__ __forceinline__ double scale_of(double inv_t) { return inv_t * 0x1.71547652b82fep+6; }
+constexpr double kFloor = -700 * 0x1.71547652b82fep+6;  // y of e^-700
+__device__ __forceinline__ double power_of(double y, const double* table) {
+  constexpr double L = 0x1.62e42fefa39efp-7, big = 0x1.8p52;  // ln 2 / 64; a sum whose last place is 1
+  const double t = y + big, f = y - (t - big);
+  double v = fma(L * L * L * L / 24, f, L * L * L / 6);
+  v = fma(v, f, L * L / 2);
+  v = fma(v, f, L);
+  v = fma(v, f, 1.0);
+  const int k = (int)__double2loint(t);
+  return ldexp(v * table[k & (kTable - 1)], k >> 6);
 }
-// e^((z - most) / T) of a logit that is no NaN, 0 for -inf.
-__device__ __forceinline__ double weight(float z, float most, double inv_t, const double* table) {
-  return exp64(((double)z - (double)most) * inv_t, table);
+// For sums: what is below e^-700, -inf too, is e^-700.
+__device__ __forceinline__ double weight_in_sum(float z, float most, double scale, const double* table) {
+  return power_of(fmax(((double)z - (double)most) * scale, kFloor), table);
+}
+// ... is 0; z is no NaN.
+__device__ __forceinline__ double weight(float z, float most, double scale, const double* table) {
+  const double y = ((double)z - (double)most) * scale, v = power_of(fmax(y, kFloor), table);
+  return y <= kFloor ? 0.0 : v;
 }
 
 __device__ __forceinline__ double wave_sum64(double v) {
@@ -122,16 +126,19 @@ __device__ __forceinline__ void stats(const void* row, const VerifyArgs& a, int 
     }
   }
   most = wave_max(most);
-  if ((t & 63) == 0) rm[t >> 6] = most;
   const bool any = __any(bad);
-  if ((t & 63) == 0) rb[t >> 6] = any;
+  if ((t & 63) == 0) {
+    rm[t >> 6] = most;
+    rb[t >> 6] = any;
+  }
   __syncthreads();
   most = fmaxf(fmaxf(rm[0], rm[1]), fmaxf(rm[2], rm[3]));
   const bool none = most == -INFINITY, odd = rb[0] || rb[1] || rb[2] || rb[3];
   double sum = 0;
   if (!none && !odd) {
+    const double sc = scale_of(a.inv_t);
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) sum += weight(f[i], most, a.inv_t, table);
+    for (int i = 0; i < kPer; ++i) sum += weight_in_sum(f[i], most, sc, table);
   }
   sum = wave_sum64(sum);
   if ((t & 63) == 0) rs[t >> 6] = sum;
@@ -142,7 +149,7 @@ __device__ __forceinline__ void stats(const void* row, const VerifyArgs& a, int 
 // Rows [0, n (k + 1)) are the target's, the rest the draft's.
 template <int TZ, int TD, bool VEC>
 __global__ __launch_bounds__(VT) void verify_stats_kernel(VerifyArgs a, Part* parts, int nseg) {
-  __shared__ double table[32];
+  __shared__ double table[kTable];
   const int64_t row = blockIdx.x / nseg;
   const int seg = (int)(blockIdx.x - row * nseg);
   const int64_t nt = (int64_t)a.n * (a.k + 1);
@@ -160,10 +167,10 @@ __global__ __launch_bounds__(VT) void verify_stats_kernel(VerifyArgs a, Part* pa
 }
 
 // What a logit has in the next token's distribution, as a probability.
-__device__ __forceinline__ double left_of(const Decision& d, float z, float zd, int64_t v, double inv_t, double p_inv,
-                                          double q_inv, const double* table) {
-  double p = weight(z, d.p_most, inv_t, table) * p_inv;
-  if (d.kind == kMinus) p = fmax(p - weight(zd, d.q_most, inv_t, table) * q_inv, 0.0);
+__device__ __forceinline__ double left_of(const Decision& d, float z, float zd, int64_t v, double sc,
+                                          double p_inv, double q_inv, const double* table) {
+  double p = weight(z, d.p_most, sc, table) * p_inv;
+  if (d.kind == kMinus) p = fmax(p - weight(zd, d.q_most, sc, table) * q_inv, 0.0);
   if (d.kind == kWithout && v == d.token) p = 0;
   return p;
 }
@@ -176,6 +183,7 @@ __device__ __forceinline__ void left_in(const VerifyArgs& a, const Decision& d, 
   const bool minus = d.kind == kMinus;
   const void* dr = minus ? row_of<TD>(a.zd, (int64_t)b * a.k + d.accepted, a.ld_d) : nullptr;
   const double p_inv = 1.0 / d.p_sum, q_inv = minus ? 1.0 / d.q_sum : 0.0;
+  const double sc = scale_of(a.inv_t);
   float z[kPer / 4][4], zd[kPer / 4][4];
 #pragma unroll
   for (int i = 0; i < kPer / 4; ++i) {
@@ -188,14 +196,14 @@ __device__ __forceinline__ void left_in(const VerifyArgs& a, const Decision& d, 
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int64_t c = (int64_t)seg * kSeg + i * (VT * 4) + threadIdx.x * 4 + j;
-      w[4 * i + j] = left_of(d, z[i][j], zd[i][j], c, a.inv_t, p_inv, q_inv, table);
+      w[4 * i + j] = left_of(d, z[i][j], zd[i][j], c, sc, p_inv, q_inv, table);
     }
 }
 
 template <int TZ, int TD, bool VEC>
 __global__ __launch_bounds__(VT) void verify_left_kernel(VerifyArgs a, const Part* parts, int nseg, Decision* decisions,
                                                          double* left) {
-  __shared__ double table[32];
+  __shared__ double table[kTable];
   __shared__ float most[kMaxRows];
   __shared__ double sum[kMaxRows];
   __shared__ int accept[kMaxDrafts];
@@ -206,6 +214,7 @@ __global__ __launch_bounds__(VT) void verify_left_kernel(VerifyArgs a, const Par
   const int len = length_of(a, b);
   const int64_t nt = (int64_t)a.n * (a.k + 1), base = (int64_t)b * (a.k + 1);
   put_table(table);
+  const double sc = scale_of(a.inv_t);
   // a thread's own draft (k <= VT) and its logits, requested ahead
   static_assert(kMaxDrafts <= VT, "a draft a thread");
   int tok = -1;
@@ -232,8 +241,8 @@ __global__ __launch_bounds__(VT) void verify_left_kernel(VerifyArgs a, const Par
       bad = bad || q.most != q.most;
       const float to = fmaxf(m, q.most);
       if (to > -INFINITY && q.most == q.most)
-        v = (m > -INFINITY ? v * weight(m, to, a.inv_t, table) : 0.0) +
-            (q.most > -INFINITY ? q.sum * weight(q.most, to, a.inv_t, table) : 0.0);
+        v = (m > -INFINITY ? v * weight(m, to, sc, table) : 0.0) +
+            (q.most > -INFINITY ? q.sum * weight(q.most, to, sc, table) : 0.0);
       m = to;
     }
     float all = m;
@@ -242,7 +251,7 @@ __global__ __launch_bounds__(VT) void verify_left_kernel(VerifyArgs a, const Par
       all = fmaxf(all, __shfl_xor(all, d, 16));
       bad = __shfl_xor((int)bad, d, 16) || bad;
     }
-    v = m > -INFINITY ? v * weight(m, all, a.inv_t, table) : 0.0;
+    v = m > -INFINITY ? v * weight(m, all, sc, table) : 0.0;
 #pragma unroll
     for (int d = 8; d > 0; d >>= 1) v += __shfl_xor(v, d, 16);
     if ((t & 15) == 0) {
@@ -261,8 +270,8 @@ __global__ __launch_bounds__(VT) void verify_left_kernel(VerifyArgs a, const Par
       what = 2;
     } else {
       at_z = ((double)z - (double)most[t]) * a.inv_t;
-      const double p = exp64(at_z, table) / sum[t];
-      const double q = a.zd ? weight(zd, most[len + 1 + t], a.inv_t, table) / sum[len + 1 + t] : 1.0;
+      const double p = weight(z, most[t], sc, table) / sum[t];
+      const double q = a.zd ? weight(zd, most[len + 1 + t], sc, table) / sum[len + 1 + t] : 1.0;
       what = (double)u * q < p;
     }
     accept[t] = what;
@@ -330,7 +339,7 @@ template <int TZ, int TD, bool VEC>
 __global__ __launch_bounds__(VT) void verify_sample_kernel(VerifyArgs a, const Part* parts, int nseg,
                                                            const Decision* decisions, const double* left) {
   constexpr int R = kPer / 4;  // rounds of four logits a thread
-  __shared__ double table[32];
+  __shared__ double table[kTable];
   __shared__ double wsum[R][VT / 64];
   __shared__ int wfirst[VT / 64], wlast[VT / 64];
   __shared__ double before, goal;
@@ -340,7 +349,7 @@ __global__ __launch_bounds__(VT) void verify_sample_kernel(VerifyArgs a, const P
   Decision d = decisions[b];
   const int64_t base = (int64_t)b * (a.k + 1);
   if (d.kind == kNone) return;
-  const double u = a.u[base + a.k];
+  const double u = a.u[base + a.k], sc = scale_of(a.inv_t);
   put_table(table);
   __syncthreads();
   if (wave == 0) {
@@ -351,7 +360,7 @@ __global__ __launch_bounds__(VT) void verify_sample_kernel(VerifyArgs a, const P
     const auto mass = [&](int s) {
       if (s >= nseg) return 0.0;
       if (kind == d.kind) return l[s];
-      return p[s].most > -INFINITY ? p[s].sum * weight(p[s].most, d.p_most, a.inv_t, table) / d.p_sum : 0.0;
+      return p[s].most > -INFINITY ? p[s].sum * weight(p[s].most, d.p_most, sc, table) / d.p_sum : 0.0;
     };
     double all = 0;
     for (int s0 = 0; s0 < nseg; s0 += 64) all += wave_sum64(mass(s0 + lane));
@@ -455,7 +464,8 @@ hipError_t launch_all(const VerifyArgs& a, void* ws, hipStream_t stream) {
   hipLaunchKernelGGL((verify_left_kernel<TZ, TD, VEC>), dim3((unsigned)((int64_t)a.n * nseg)), dim3(VT), 0, stream, a, parts,
                      nseg, decisions, left);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  hipLaunchKernelGGL((verify_sample_kernel<TZ, TD, VEC>), dim3(a.n), dim3(VT), 0, stream, a, parts, nseg, decisions, left);
+  hipLaunchKernelGGL((verify_sample_kernel<TZ, TD, VEC>), dim3(a.n), dim3(VT), 0, stream, a, parts, nseg, decisions,
+                     left);
   return hipGetLastError();
 }
 
