@@ -765,9 +765,10 @@ hydra_status hydra_fp8_quantize(const void* x, hydra_dtype x_type, int64_t M, in
                                 uint8_t* scale, uint8_t* qt, uint8_t* scale_t, void* stream);
 
 /* hydra_fp8_lora_linear_workspace_bytes -- device workspace that hydra_fp8_lora_linear
- * needs at most for M rows, K inputs and rank r (writes *bytes).  HYDRA_ERR_NULL for a
- * NULL `bytes`, HYDRA_ERR_SHAPE for sizes outside that call's limits. */
-hydra_status hydra_fp8_lora_linear_workspace_bytes(int64_t M, int64_t K, int64_t r, size_t* bytes);
+ * needs at most for up to M rows, N outputs, K inputs and rank r (writes *bytes; less is
+ * never asked for more rows, so the largest call's workspace serves all).  HYDRA_ERR_NULL
+ * for a NULL `bytes`, HYDRA_ERR_SHAPE for sizes outside that call's limits. */
+hydra_status hydra_fp8_lora_linear_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t r, size_t* bytes);
 
 /*
  * hydra_fp8_lora_linear -- hydra_lora_linear over a frozen weight in 8 bits:
@@ -783,8 +784,8 @@ hydra_status hydra_fp8_lora_linear_workspace_bytes(int64_t M, int64_t K, int64_t
  *   A, B, s   as in hydra_lora_linear
  *   y_off, y_on  [M x N] bf16 or fp32 (y_type, both)   out, each optional, at least one
  *   workspace, workspace_bytes  device, 16-byte aligned, contents ignored and
- *             overwritten; hydra_fp8_lora_linear_workspace_bytes(M, K, r) bytes are
- *             always enough (NULL allowed where xq is given and no update is computed)
+ *             overwritten; hydra_fp8_lora_linear_workspace_bytes(M, N, K, r) bytes are
+ *             always enough
  * x, x_adapter, xq, Wq and A 16-byte aligned, B 2-byte, outputs at their element's
  * alignment.  Into fp32 outputs, and up to 16 rows, every product is exact and
  * added in fp32; into bf16 outputs of more rows the 8-bit matrix instructions run,

@@ -180,7 +180,7 @@ def lib() -> ctypes.CDLL:
             ("hydra_grad_norm", [_i64, _pp, _i32p, _i64p, _vp, _vp, _size, _vp]),
             ("hydra_grad_clip", [_i64, _pp, _i32p, _i64p, _f32, _vp, _pp, _i32p, _vp, _size, _vp, _vp]),
             ("hydra_fp8_quantize", [_vp, _int, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp]),
-            ("hydra_fp8_lora_linear_workspace_bytes", [_i64, _i64, _i64, _sizep]),
+            ("hydra_fp8_lora_linear_workspace_bytes", [_i64, _i64, _i64, _i64, _sizep]),
             ("hydra_fp8_lora_linear", [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _f32, _i64, _i64, _i64, _i64, _vp, _vp, _int,
                                        _vp, _size, _vp]),
             ("hydra_fp8_lora_linear_backward_workspace_bytes", [_i64, _i64, _i64, _i64, _sizep]),
@@ -1138,9 +1138,9 @@ def _hydra_fp8_quantize(x, q, scale, block_rows, qt, scale_t, stream) -> None:
         _ptr(x), _type(x), M, K, rows, _ptr(q), _ptr(scale), _ptr(qt), _ptr(scale_t), st))
 
 
-def hydra_fp8_lora_linear_workspace_bytes(M: int, K: int, r: int) -> int:
+def hydra_fp8_lora_linear_workspace_bytes(M: int, N: int, K: int, r: int) -> int:
     out = ctypes.c_size_t(0)
-    _check(lib().hydra_fp8_lora_linear_workspace_bytes(int(M), int(K), int(r), ctypes.byref(out)),
+    _check(lib().hydra_fp8_lora_linear_workspace_bytes(int(M), int(N), int(K), int(r), ctypes.byref(out)),
            "hydra_fp8_lora_linear_workspace_bytes")
     return int(out.value)
 
@@ -1187,7 +1187,7 @@ def _hydra_fp8_lora_linear(x, Wq, w_scale, A, B, s, y_off, y_on, x_adapter, xq, 
             lambda ws, n, st: lib().hydra_fp8_lora_linear(
                 _ptr(x), _ptr(x_adapter), _ptr(xq), _ptr(x_scale), _ptr(Wq), _ptr(w_scale), _ptr(A), _ptr(B), float(s), M,
                 N, K, r, _ptr(y_off), _ptr(y_on), y_type, ws, n, st),
-            workspace, hydra_fp8_lora_linear_workspace_bytes(M, K, r))
+            workspace, hydra_fp8_lora_linear_workspace_bytes(M, N, K, r))
 
 
 def hydra_fp8_lora_linear_backward_workspace_bytes(M: int, N: int, K: int, r: int) -> int:

@@ -30,10 +30,30 @@ constexpr int P_WAVES = 8;
 constexpr int kFewRows = 16;
 constexpr int kStagedChunks = 8;  // most partial sums of T at padded rank 16 above kFewRows rows
 
+// The pieces of four lanes 16 apart, transposed: v[j] of lane group g becomes v[g] of
+// lane group j.
+__device__ __forceinline__ void transpose4(uint32_t (&v)[4]) {
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const auto r = __builtin_amdgcn_permlane32_swap(v[j], v[j + 2], false, false);
+    v[j] = r[0];
+    v[j + 2] = r[1];
+  }
+#pragma unroll
+  for (int j = 0; j < 4; j += 2) {
+    const auto r = __builtin_amdgcn_permlane16_swap(v[j], v[j + 1], false, false);
+    v[j] = r[0];
+    v[j + 1] = r[1];
+  }
+}
+
 // 16 rows and one chunk of K a workgroup; a wave takes the chunk's blocks in turn.
 // Lane l holds values 32 j + 8 (l / 16) ... + 7, j = 0 ... 3, of the block of row l % 16:
 // four lanes read 64 consecutive bytes of a row, a block's maximum is over four
-// lanes, and piece j of all lanes is one 16x16x32 product of T.
+// lanes, and piece j of all lanes is one 16x16x32 product of T.  The bytes change lanes
+// for stores of 128 consecutive bytes a row.  2048 x 4096 at rank 16, x quantized: 8.5 us
+// (with each lane's eight bytes a store of their own 11.2; with 32 rows a workgroup, for
+// half the reads of A, 10.2, with 64 12.9: fewer waves to hide the loads behind).
 // QUANT: x's bytes and scales; OWN: the adapter has an input of its own.
 template <int RP, bool QUANT, bool OWN>
 __global__ __launch_bounds__(P_WAVES * 64) void fp8_prep_kernel(Fp8PrepArgs g) {
@@ -52,8 +72,7 @@ __global__ __launch_bounds__(P_WAVES * 64) void fp8_prep_kernel(Fp8PrepArgs g) {
   const int kb1 = min(kb_n, (int)(blockIdx.y + 1) * g.kch);
   for (int kb = blockIdx.y * g.kch + wave; kb < kb1; kb += P_WAVES) {
     const int k = kb * kFp8Block + 8 * lg;
-    uint4 v[4], a[4];
-    uint4 w[4][TJ1];
+    uint4 v[4], a[4], w[4][TJ1];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const bool ok = k + 32 * j < K;
@@ -76,12 +95,19 @@ __global__ __launch_bounds__(P_WAVES * 64) void fp8_prep_kernel(Fp8PrepArgs g) {
       most = fmaxf(most, __shfl_xor(most, 32));
       const int byte = fp8_scale_byte(most);
       const float p = fp8_inverse(byte);
-      if (l16 < rows) {
-        uint8_t* q = g.xq + (size_t)(m0 + l16) * K + k;
+      uint32_t lo[4], hi[4];  // values 32 j + 8 lg ... + 3 and + 4 ... + 7; then 32 lg + 8 j ...
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (k + 32 * j < K)
-            *reinterpret_cast<uint2*>(q + 32 * j) = make_uint2(fp8_pack4(f[j], p), fp8_pack4(f[j] + 4, p));
+      for (int j = 0; j < 4; ++j) {
+        lo[j] = fp8_pack4(f[j], p);
+        hi[j] = fp8_pack4(f[j] + 4, p);
+      }
+      transpose4(lo);
+      transpose4(hi);
+      const int kq = kb * kFp8Block + 32 * lg;
+      if (l16 < rows) {
+        uint8_t* q = g.xq + (size_t)(m0 + l16) * K + kq;
+        if (kq < K) *reinterpret_cast<uint4*>(q) = make_uint4(lo[0], hi[0], lo[1], hi[1]);
+        if (kq + 16 < K) *reinterpret_cast<uint4*>(q + 16) = make_uint4(lo[2], hi[2], lo[3], hi[3]);
         if (lg == 0) g.xs[(size_t)(m0 + l16) * kb_n + kb] = (uint8_t)byte;
       }
     }
@@ -225,7 +251,13 @@ struct GemmArgs {
   int vec;    // outputs in 16-byte stores
   int bvec;   // B in 16-byte loads
   int64_t xs_bytes, ws_bytes;
+  int nsplit, per;  // K in nsplit parts of `per` slabs (PART, JOIN)
 };
+
+// WHOLE: a tile's outputs.  PART: the base product of one part of K (blockIdx.y) to
+// a.split, [nsplit][M][N] fp32; JOIN: their sum in the order of K, and what WHOLE does
+// after its own.
+enum Phase { WHOLE, PART, JOIN };
 
 // TM x TN tile, WM x WN sub-tile a wave, KS waves a sub-tile (each takes its share
 // of every slab), slabs of BK values of K in a ring of NS; four more waves copy.
@@ -291,7 +323,7 @@ __device__ __forceinline__ uint32_t load_scales(const uint8_t* p, int64_t at, in
 }
 
 // MASK: the update goes through dropout's mask.
-template <class G, bool MASK>
+template <class G, bool MASK, Phase PH>
 __global__ __launch_bounds__(G::NT, G::NT / 256 * G::WPC) void fp8_gemm_kernel(GemmArgs g) {
   constexpr int TM = G::TM, TN = G::TN, WM = G::WM, WN = G::WN, KS = G::KS, BK = G::BK, NS = G::NS;
   constexpr int MT = G::MT, NTL = G::NTL, NQ = G::NQ, SPW = G::SPW;
@@ -315,7 +347,9 @@ __global__ __launch_bounds__(G::NT, G::NT / 256 * G::WPC) void fp8_gemm_kernel(G
     tni = in / gsize;
   }
   const int m0 = __builtin_amdgcn_readfirstlane(tmi * TM), n0 = __builtin_amdgcn_readfirstlane(tni * TN);
-  const int nkt = (K + BK - 1) / BK;
+  // slabs [kt0, nkt) of this workgroup
+  const int kt0 = PH == PART ? (int)blockIdx.y * g.per : 0;
+  const int nkt = PH == JOIN ? 0 : PH == PART ? min((K + BK - 1) / BK, kt0 + g.per) : (K + BK - 1) / BK;
 
   // LDS chunk of (row, 16-byte chunk c): c is XOR-ed with bits of the row, so that
   // 16 consecutive rows' chunks c lie in different banks.  W's rows follow x's.
@@ -350,6 +384,29 @@ __global__ __launch_bounds__(G::NT, G::NT / 256 * G::WPC) void fp8_gemm_kernel(G
               f32x4_t{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
         }
   };
+  // The base product from its parts (N % 4 == 0: four at a time).
+  auto add_parts = [&](float* v, int row, int col) __attribute__((always_inline)) {
+    if (m0 + row >= M) return;
+    const float* p = a.split + (size_t)(m0 + row) * N + n0 + col;
+    const size_t stride = (size_t)M * N;
+    constexpr int W = G::WIDE ? 4 : 8;
+    f32x4_t sum[W / 4];
+#pragma unroll
+    for (int q = 0; q < W / 4; ++q) sum[q] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < g.nsplit; ++k, p += stride)
+#pragma unroll
+      for (int q = 0; q < W / 4; ++q) {
+        if (N % 4 == 0) {
+          if (n0 + col + 4 * q < N) sum[q] += *reinterpret_cast<const f32x4_t*>(p + 4 * q);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (n0 + col + 4 * q + e < N) sum[q][e] += p[4 * q + e];
+        }
+      }
+#pragma unroll
+    for (int e = 0; e < W; ++e) v[e] += sum[e / 4][e % 4];
+  };
   // A thread's groups of consecutive columns, 16 bytes of the output: f(values, row, column).
   constexpr int w = G::WIDE ? 4 : 8;
   auto each = [&](auto f) __attribute__((always_inline)) {
@@ -369,6 +426,7 @@ __global__ __launch_bounds__(G::NT, G::NT / 256 * G::WPC) void fp8_gemm_kernel(G
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[4 * q + e] = s[e];
       }
+      if constexpr (PH == JOIN) add_parts(v, row, col);
       f(v, row, col);
     }
   };
@@ -535,6 +593,27 @@ __global__ __launch_bounds__(G::NT, G::NT / 256 * G::WPC) void fp8_gemm_kernel(G
   // By the role of the wave: do_stage is a copy wave's, the others a matrix wave's.
   auto finish = [&](auto do_stage, auto do_put, auto do_add) __attribute__((always_inline)) {
     asm volatile("" : "+v"(te));
+    if constexpr (PH == PART) {
+      do_put();
+      __syncthreads();
+      float* const part = a.split + (size_t)blockIdx.y * M * N;
+      each([&](const float* v, int row, int col) __attribute__((always_inline)) {
+        if (m0 + row >= M) return;
+        float* p = part + (size_t)(m0 + row) * N + n0 + col;
+#pragma unroll
+        for (int q = 0; q < w / 4; ++q) {
+          if (N % 4 == 0) {
+            if (n0 + col + 4 * q < N)
+              *reinterpret_cast<f32x4_t*>(p + 4 * q) = f32x4_t{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (n0 + col + 4 * q + e < N) p[4 * q + e] = v[4 * q + e];
+          }
+        }
+      });
+      return;
+    }
     const bool lora = a.y_on && rp > 0;
     if (a.y_off || !lora) {
       do_put();
@@ -564,7 +643,7 @@ __global__ __launch_bounds__(G::NT, G::NT / 256 * G::WPC) void fp8_gemm_kernel(G
     const i32x4_t wrs = make_rsrc_raw(a.wq + (size_t)n0 * K, (uint32_t)min(TN, N - n0) * K);
     auto issue = [&](int stage, int kt) __attribute__((always_inline)) {
       const int k = kt * BK + c * 16;
-      const bool ok = k < K;
+      const bool ok = k < K && (PH != PART || kt < nkt);
 #pragma unroll
       for (int j = 0; j < G::XJ; ++j) {
         const int row = (cw + 4 * j) * RPB;
@@ -590,12 +669,14 @@ __global__ __launch_bounds__(G::NT, G::NT / 256 * G::WPC) void fp8_gemm_kernel(G
       next += 256;
     };
     // slabs past the last read zeros, so that the waits count the same throughout
+    if constexpr (PH != JOIN) {
 #pragma unroll
-    for (int s = 0; s < NS; ++s) issue(s, s);
-    wait_vm<(NS - 1) * G::DPW < 63 ? (NS - 1) * G::DPW : 63>();
-    lds_barrier();  // slab 0 is in LDS
+      for (int s = 0; s < NS; ++s) issue(s, kt0 + s);
+      wait_vm<(NS - 1) * G::DPW < 63 ? (NS - 1) * G::DPW : 63>();
+      lds_barrier();  // the first slab is in LDS
+    }
     int stage = 0;
-    for (int kt = 0; kt < nkt; ++kt) {
+    for (int kt = kt0; kt < nkt; ++kt) {
       wait_vm<(NS - 2) * G::DPW>();
       lds_barrier();  // slab kt + 1 has landed, slab kt is in registers everywhere
       issue(stage, kt + NS);
@@ -663,7 +744,8 @@ __global__ __launch_bounds__(G::NT, G::NT / 256 * G::WPC) void fp8_gemm_kernel(G
       sw = swn;
       load_four(4 * f + 4);
     };
-    load_four(0);
+    const int kb_first = (kt0 * (BK / G::STEP) + kg * SPW) / (kFp8Block / G::STEP);
+    if constexpr (PH != JOIN) load_four(kb_first & ~3);
     auto kstep = [&](auto S, const Frag& fc, Frag& fn, int st, int kt) __attribute__((always_inline)) {
       constexpr int sp = decltype(S)::value;
       constexpr bool last = sp == SPW - 1;
@@ -716,13 +798,15 @@ __global__ __launch_bounds__(G::NT, G::NT / 256 * G::WPC) void fp8_gemm_kernel(G
         }
       }
     };
-    lds_barrier();  // slab 0 is in LDS
+    if constexpr (PH != JOIN) {
+      lds_barrier();  // the first slab is in LDS
 #pragma unroll
-    for (int r = 0; r < NR; ++r) read(F[0], 0, 0, r);
+      for (int r = 0; r < NR; ++r) read(F[0], 0, 0, r);
+    }
     // Past the last slab the reads fill registers that are never used.
     constexpr int UN = SPW % 2 && !ONE ? 2 : 1;  // slabs until the two fragment sets are back in place
     int stage = 0;
-    for (int kt = 0; kt < nkt; kt += UN) {
+    for (int kt = kt0; kt < nkt; kt += UN) {
 #pragma unroll
       for (int u = 0; u < UN; ++u) {
         if (u > 0 && kt + u >= nkt) break;
@@ -744,18 +828,31 @@ __global__ __launch_bounds__(G::NT, G::NT / 256 * G::WPC) void fp8_gemm_kernel(G
 
 bool at_multiple(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
-template <class G>
-hipError_t launch_tile(GemmArgs& g, hipStream_t stream) {
+template <class G, bool MASK, Phase PH>
+hipError_t launch_phase(GemmArgs& g, hipStream_t stream) {
   g.ntm = (g.a.M + G::TM - 1) / G::TM;
   g.ntn = (g.a.N + G::TN - 1) / G::TN;
   const int64_t total = (int64_t)g.ntm * g.ntn;
   if (total * G::NT >= (int64_t(1) << 32)) return hipErrorInvalidValue;
   g.total = (int)total;
-  if (g.a.drop > 0 && g.a.y_on)
-    hipLaunchKernelGGL((fp8_gemm_kernel<G, true>), dim3(g.total), dim3(G::NT), 0, stream, g);
-  else
-    hipLaunchKernelGGL((fp8_gemm_kernel<G, false>), dim3(g.total), dim3(G::NT), 0, stream, g);
+  hipLaunchKernelGGL((fp8_gemm_kernel<G, MASK, PH>), dim3(g.total, PH == PART ? g.nsplit : 1), dim3(G::NT), 0, stream, g);
   return hipGetLastError();
+}
+template <class G, Phase PH>
+hipError_t launch_masked(GemmArgs& g, hipStream_t stream) {
+  return g.a.drop > 0 && g.a.y_on ? launch_phase<G, true, PH>(g, stream) : launch_phase<G, false, PH>(g, stream);
+}
+template <class G>
+hipError_t launch_tile(GemmArgs& g, hipStream_t stream) {
+  return launch_masked<G, WHOLE>(g, stream);
+}
+template <class G>
+hipError_t launch_split(GemmArgs& g, int nsplit, hipStream_t stream) {
+  g.per = ((g.a.K + G::BK - 1) / G::BK + nsplit - 1) / nsplit;
+  g.nsplit = ((g.a.K + G::BK - 1) / G::BK + g.per - 1) / g.per;
+  const hipError_t e = launch_phase<G, false, PART>(g, stream);
+  if (e != hipSuccess) return e;
+  return launch_masked<Tile<G::WIDE, 32, 64, 32, 64, 1, 128, 2, 2>, JOIN>(g, stream);
 }
 
 // The tile by a model of its time: base + fixed w + K / 128 (step w + pair r), us, for w
@@ -783,17 +880,33 @@ constexpr TileCost kTiles[2][6] = {{{128, 256, 0.f, 5.8f, 0.767f, 0.f},
                                     {32, 64, 1.57f, 2.23f, 0.272f, 0.f},
                                     {32, 32, 2.9f, 0.72f, 0.067f, 0.165f}}};
 
-int best_tile(bool wide, int M, int N, int K) {
-  int best = 0;
+// K in parts (tiles 1, 2 and 4): few rows and a long K leave CUs without a tile.  The
+// parts' sums go through memory, and a second launch joins them, for 3.9 us and the
+// sums written and read at 6.75 TB/s (a fit to 330 cases, rms error 9%).  us, whole ->
+// in parts, fp32: 17 x 2048 x 8192 17.9 -> 11.4, 64 x 4096 x 11008 25.3 -> 21.8, 200 x 4096 x
+// 11008 38.6 -> 32.7; below K = 4096 never faster.
+constexpr int kMaxSplit = 8, kMaxParts = 512;
+struct Plan {
+  int tile, nsplit;
+};
+Plan plan_of(bool wide, int M, int N, int K) {
+  Plan best{0, 1};
   float least = 0.f;
   for (int i = 0; i < 6; ++i) {
     const TileCost& c = kTiles[wide][i];
-    const int64_t n = (int64_t)((M + c.tm - 1) / c.tm) * ((N + c.tn - 1) / c.tn);
-    const float w = (float)((n + 255) / 256), r = (float)((n + 511) / 512), slabs = (float)((K + 127) / 128);
-    const float us = c.base + c.fixed * w + slabs * (c.step * w + c.pair * r);
-    if (i == 0 || us < least) {
-      least = us;
-      best = i;
+    const int64_t tiles = (int64_t)((M + c.tm - 1) / c.tm) * ((N + c.tn - 1) / c.tn);
+    const int slabs = (K + 127) / 128;
+    const bool may = (i == 1 || i == 2 || i == 4) && tiles < 256;
+    for (int s = 1; s <= (may ? kMaxSplit : 1) && s * 4 <= (s == 1 ? 4 : slabs); ++s) {
+      const int64_t n = tiles * s;
+      if (s > 1 && n > kMaxParts) break;
+      const float w = (float)((n + 255) / 256), r = (float)((n + 511) / 512), sl = (float)((slabs + s - 1) / s);
+      float us = c.base + c.fixed * w + sl * (c.step * w + c.pair * r);
+      if (s > 1) us += 3.9f + (float)s * 8.f * (float)M * (float)N / 6.75e6f;
+      if ((i == 0 && s == 1) || us < least) {
+        least = us;
+        best = Plan{i, s};
+      }
     }
   }
   return best;
@@ -801,12 +914,23 @@ int best_tile(bool wide, int M, int N, int K) {
 
 template <bool WIDE>
 hipError_t launch_rows(GemmArgs& g, hipStream_t stream) {
-  switch (best_tile(WIDE, g.a.M, g.a.N, g.a.K)) {
+  const Plan p = plan_of(WIDE, g.a.M, g.a.N, g.a.K);
+  using T1 = Tile<WIDE, 128, 128, 64, 64, 2, 128, 4>;
+  using T2 = Tile<WIDE, 64, 128, 64, 64, 2, 128, 6>;
+  using T4 = Tile<WIDE, 32, 64, 32, 64, 4, 256, 6>;
+  if (p.nsplit > 1) {
+    switch (p.tile) {
+      case 1: return launch_split<T1>(g, p.nsplit, stream);
+      case 2: return launch_split<T2>(g, p.nsplit, stream);
+      default: return launch_split<T4>(g, p.nsplit, stream);
+    }
+  }
+  switch (p.tile) {
     case 0: return launch_tile<Tile<WIDE, 128, 256, 64, 128, 1, 128, 3>>(g, stream);
-    case 1: return launch_tile<Tile<WIDE, 128, 128, 64, 64, 2, 128, 4>>(g, stream);
-    case 2: return launch_tile<Tile<WIDE, 64, 128, 64, 64, 2, 128, 6>>(g, stream);
+    case 1: return launch_tile<T1>(g, stream);
+    case 2: return launch_tile<T2>(g, stream);
     case 3: return launch_tile<Tile<WIDE, 64, 64, 32, 64, 2, 128, 4, 2>>(g, stream);
-    case 4: return launch_tile<Tile<WIDE, 32, 64, 32, 64, 4, 256, 6>>(g, stream);
+    case 4: return launch_tile<T4>(g, stream);
     default: return launch_tile<Tile<WIDE, 32, 32, 32, 32, 4, 256, 4, 2>>(g, stream);
   }
 }
@@ -829,8 +953,8 @@ void launch_prep(const Fp8PrepArgs& a, hipStream_t stream) {
 }  // namespace
 
 // Chunks of K: about 512 workgroups, each at least a block a wave, and no more
-// partial sums of T than the product can add up on the side.  us, four waves -> eight: 8 x
-// 4096 rank 16 P1 -> P2, 2048 x 4096 P3 -> P4, 333 x 11008 P5 -> P6.
+// partial sums of T than the product can add up on the side.  2048 x 4096 at rank 16 takes
+// 8.5 to 9.1 us with 256, 512, 768 or 1024 workgroups and with 4, 8 or 16 waves.
 void fp8_prep_chunks(int M, int K, int rp, int& nch, int& kch) {
   const int kb = (K + kFp8Block - 1) / kFp8Block, mb = (M + 15) / 16;
   int want = (512 + mb - 1) / mb;
@@ -851,6 +975,19 @@ hipError_t launch_fp8_prep(const Fp8PrepArgs& a, hipStream_t stream) {
     default: return hipErrorInvalidValue;
   }
   return hipGetLastError();
+}
+
+size_t fp8_split_most(int M, int N, int K) {
+  if (K <= 128 * 7) return 0;
+  const size_t all = (size_t)kMaxSplit * M * N, parts = (size_t)kMaxParts * 128 * 128;
+  return (all < parts ? all : parts) * 4;
+}
+size_t fp8_prep_most(int M, int rp) {
+  if (rp == 0) return 0;
+  const size_t few = (size_t)32 * (M < kFewRows ? M : kFewRows);
+  const size_t by_rows = (size_t)(rp <= 32 ? kStagedChunks : 4) * M, by_grid = (size_t)(512 + 1) * 16 + M;
+  const size_t many = M <= kFewRows ? 0 : by_rows < by_grid ? by_rows : by_grid;
+  return (few > many ? few : many) * rp * 4;
 }
 
 hipError_t launch_fp8_linear(const Fp8LinearArgs& a, hipStream_t stream) {

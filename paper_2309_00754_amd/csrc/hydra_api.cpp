@@ -1219,14 +1219,13 @@ hydra_status hydra_fp8_quantize(const void* x, hydra_dtype x_type, int64_t M, in
   return from_hip(hydra::launch_fp8_quantize(a, reinterpret_cast<hipStream_t>(stream)));
 }
 
-hydra_status hydra_fp8_lora_linear_workspace_bytes(int64_t M, int64_t K, int64_t r, size_t* bytes) {
+hydra_status hydra_fp8_lora_linear_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t r, size_t* bytes) {
   if (!bytes) return HYDRA_ERR_NULL;
-  const hydra_status chk = fp8_shape(M, 1, K, r);
+  const hydra_status chk = fp8_shape(M, N, K, r);
   if (chk != HYDRA_OK) return chk;
-  int nch = 0, kch = 0;
-  const int rp = hydra::padded_rank(int(r));
-  hydra::fp8_prep_chunks(int(M), int(K), rp, nch, kch);
-  *bytes = fp8_rows_bytes(M, K) + (rp ? up256((size_t)nch * M * rp * 4) : 0);
+  // (what the largest of the calls with up to M rows needs)
+  *bytes = fp8_rows_bytes(M, K) + up256(hydra::fp8_prep_most(int(M), hydra::padded_rank(int(r)))) +
+           up256(hydra::fp8_split_most(int(M), int(N), int(K)));
   return HYDRA_OK;
 }
 
@@ -1252,7 +1251,8 @@ hydra_status hydra_fp8_lora_linear(const uint16_t* x, const uint16_t* x_adapter,
   const int rp = lora ? hydra::padded_rank(int(r)) : 0;
   int nch = 0, kch = 0;
   hydra::fp8_prep_chunks(int(M), int(K), rp, nch, kch);
-  const size_t rows = xq ? 0 : fp8_rows_bytes(M, K), need = rows + (rp ? up256((size_t)nch * M * rp * 4) : 0);
+  const size_t rows = xq ? 0 : fp8_rows_bytes(M, K), part = up256(hydra::fp8_prep_most(int(M), rp));
+  const size_t need = rows + part + up256(hydra::fp8_split_most(int(M), int(N), int(K)));
   if (need > 0) {
     if (!workspace) return HYDRA_ERR_NULL;
     if (workspace_bytes < need) return HYDRA_ERR_WORKSPACE;
@@ -1273,7 +1273,7 @@ hydra_status hydra_fp8_lora_linear(const uint16_t* x, const uint16_t* x_adapter,
   p.nch = nch;
   p.kch = kch;
   const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-  if (need > 0) {
+  if (rows + part > 0) {
     const hipError_t e = hydra::launch_fp8_prep(p, st);
     if (e != hipSuccess) return from_hip(e);
   }
@@ -1292,6 +1292,7 @@ hydra_status hydra_fp8_lora_linear(const uint16_t* x, const uint16_t* x_adapter,
   a.rp = rp;
   a.s = s;
   a.part = p.part;
+  a.split = reinterpret_cast<float*>(w + rows + part);
   a.nch = nch;
   a.B = B;
   a.ldb = int(r);
@@ -1303,7 +1304,8 @@ hydra_status hydra_fp8_lora_linear_backward_workspace_bytes(int64_t M, int64_t N
   const hydra_status chk = fp8_shape(M, K, N, r);
   if (chk != HYDRA_OK) return chk;
   if (K % 16 != 0) return HYDRA_ERR_SHAPE;
-  *bytes = fp8_rows_bytes(M, N) + hydra::backward_ws_bytes(int(M), int(N), int(K), hydra::padded_rank(int(r)));
+  *bytes = fp8_rows_bytes(M, N) + up256(hydra::fp8_split_most(int(M), int(K), int(N))) +
+           hydra::backward_ws_bytes(int(M), int(N), int(K), hydra::padded_rank(int(r)));
   return HYDRA_OK;
 }
 
@@ -1332,7 +1334,8 @@ hydra_status hydra_fp8_lora_linear_backward(const uint16_t* x, const uint8_t* Wq
       !aligned(dx, type_align(dx_type)) || !aligned(dA, 4) || !aligned(dB, 4))
     return HYDRA_ERR_ALIGN;
   const int rp = hydra::padded_rank(int(r));
-  const size_t rows = fp8_rows_bytes(M, N), need = rows + hydra::backward_ws_bytes(int(M), int(N), int(K), rp);
+  const size_t rows = fp8_rows_bytes(M, N), split = up256(hydra::fp8_split_most(int(M), int(K), int(N)));
+  const size_t need = rows + split + hydra::backward_ws_bytes(int(M), int(N), int(K), rp);
   if (!workspace) return HYDRA_ERR_NULL;
   if (workspace_bytes < need) return HYDRA_ERR_WORKSPACE;
   if (!aligned(workspace, 16)) return HYDRA_ERR_ALIGN;
@@ -1340,6 +1343,7 @@ hydra_status hydra_fp8_lora_linear_backward(const uint16_t* x, const uint8_t* Wq
   hydra::Fp8LinearArgs g{};
   g.xq = w;
   g.xs = w + up256((size_t)M * N);
+  g.split = reinterpret_cast<float*>(w + rows);
   g.wq = Wqt;
   g.ws = wt_scale;
   g.M = int(M);
@@ -1364,7 +1368,7 @@ hydra_status hydra_fp8_lora_linear_backward(const uint16_t* x, const uint8_t* Wq
   a.dA = dA;
   a.dB = dB;
   a.base8 = dx ? &g : nullptr;
-  return from_hip(hydra::launch_lora_backward(a, w + rows, reinterpret_cast<hipStream_t>(stream)));
+  return from_hip(hydra::launch_lora_backward(a, w + rows + split, reinterpret_cast<hipStream_t>(stream)));
 }
 
 hydra_status hydra_dropout(const void* x, hydra_dtype x_type, const void* residual, hydra_dtype residual_type, double p,

@@ -313,7 +313,12 @@ struct Fp8LinearArgs {
   uint32_t drop;
   float keep;
   const uint64_t* rng;
+  float* split;        // fp8_split_most(M, N, K) of room
 };
+// Room that any call with up to M rows can do with: for partial sums of the base product
+// (0 where K is never split), and of T.
+size_t fp8_split_most(int M, int N, int K);
+size_t fp8_prep_most(int M, int rp);
 // What the linear needs before its product: x quantized (x nullptr: not), and the
 // partial sums of T = xa A^T (A nullptr: not).
 struct Fp8PrepArgs {

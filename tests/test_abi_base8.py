@@ -54,7 +54,7 @@ LIN = dict(x=at(0), xa=None, xq=None, xs=None, W=at(1), ws=at(2), A=at(3), B=at(
 ])
 def test_linear_rejects(kw, code):
     a = {**LIN, **kw}
-    nb = H.hydra_fp8_lora_linear_workspace_bytes(40, 64, 8) - 1 if a["nb"] < 0 else a["nb"]
+    nb = H.hydra_fp8_lora_linear_workspace_bytes(40, 64, 64, 8) - 1 if a["nb"] < 0 else a["nb"]
     assert H.lib().hydra_fp8_lora_linear(a["x"], a["xa"], a["xq"], a["xs"], a["W"], a["ws"], a["A"], a["B"], 1.0, a["M"],
                                          a["N"], a["K"], a["r"], a["off"], a["on"], a["yt"], a["w"], nb, None) == code
 
@@ -119,19 +119,25 @@ def test_verify_drafts_rejects(kw, code):
 def test_workspace_sizes():
     b = ctypes.c_size_t(0)
     L = H.lib()
-    assert L.hydra_fp8_lora_linear_workspace_bytes(0, 64, 8, ctypes.byref(b)) == SHAPE
-    assert L.hydra_fp8_lora_linear_workspace_bytes(8, 72, 8, ctypes.byref(b)) == SHAPE
-    assert L.hydra_fp8_lora_linear_workspace_bytes(8, 64, 129, ctypes.byref(b)) == SHAPE
-    assert L.hydra_fp8_lora_linear_workspace_bytes(8, 64, 8, None) == NULL
+    assert L.hydra_fp8_lora_linear_workspace_bytes(0, 64, 64, 8, ctypes.byref(b)) == SHAPE
+    assert L.hydra_fp8_lora_linear_workspace_bytes(8, 64, 72, 8, ctypes.byref(b)) == SHAPE
+    assert L.hydra_fp8_lora_linear_workspace_bytes(8, 64, 64, 129, ctypes.byref(b)) == SHAPE
+    assert L.hydra_fp8_lora_linear_workspace_bytes(8, 64, 64, 8, None) == NULL
     assert L.hydra_fp8_lora_linear_backward_workspace_bytes(8, 64, 72, 8, ctypes.byref(b)) == SHAPE
     assert L.hydra_fp8_lora_linear_backward_workspace_bytes(8, 64, 64, 8, None) == NULL
     assert L.hydra_verify_drafts_workspace_bytes(8, 129, 64, ctypes.byref(b)) == SHAPE
     assert L.hydra_verify_drafts_workspace_bytes(8, 4, 64, None) == NULL
     for M, K, r in ((1, 16, 0), (8, 4096, 16), (2048, 11008, 128), (1 << 20, 4096, 16)):
-        n = H.hydra_fp8_lora_linear_workspace_bytes(M, K, r)
-        assert M * K <= n <= 2 * M * K + 40 * M * 128 + (1 << 24)
+        n = H.hydra_fp8_lora_linear_workspace_bytes(M, 4096, K, r)
+        assert M * K <= n <= 2 * M * K + 40 * M * 128 + (1 << 26)
     for n, k, V in ((1, 0, 1), (64, 7, 50272), (1, 128, 1 << 21)):
         assert 0 < H.hydra_verify_drafts_workspace_bytes(n, k, V) < 1 << 24
+
+
+@pytest.mark.parametrize("N,K,r", [(16, 16, 1), (4096, 4096, 16), (4096, 11008, 64), (50272, 512, 128), (130, 32768, 0)])
+def test_the_largest_calls_workspace_serves_fewer_rows(N, K, r):
+    got = [H.hydra_fp8_lora_linear_workspace_bytes(M, N, K, r) for M in list(range(1, 300)) + list(range(300, 20000, 97))]
+    assert got == sorted(got)
 
 
 def test_host_tensors_are_refused():

@@ -61,6 +61,30 @@ def test_linear(dev, M, N, K, r, y_type):
     c.check(c.forward(y_type), y_type)
 
 
+# Few rows and a long K, which is taken in parts; and 16384 and more outputs of few rows.
+LONG = [(17, 300, 8192, 16), (40, 1030, 4112, 8), (30, 35, 32768, 64), (64, 514, 8208, 0), (100, 2050, 8192, 16),
+        (33, 4100, 4096, 20), (300, 40, 16000, 128), (9, 16500, 64, 16), (5, 16389, 1040, 3), (16, 16400, 16, 0)]
+
+
+@pytest.mark.parametrize("M,N,K,r", LONG)
+@pytest.mark.parametrize("y_type", ["f32", "bf16"])
+def test_linear_in_parts(dev, M, N, K, r, y_type):
+    import torch
+    say("fp8_lora_linear", M, N, K, r, y_type)
+    c = Linear(M * 7 + N, M, N, K, r, dev, shift=1)
+    n = H.hydra_fp8_lora_linear_workspace_bytes(M, N, K, r)
+    y = c.forward(y_type, workspace=torch.full((n,), 0xFF, dtype=torch.uint8, device=dev))
+    c.check(y, y_type)
+    alone = c.forward(y_type, off=False)  # (and again, from another workspace)
+    assert np.array_equal(f64(alone[1]), f64(y[1]))
+
+
+def test_tiles_of_128_rows_in_parts(dev):
+    c = Linear(0, 112, 4100, 6000, 16, dev)
+    for y_type in ("f32", "bf16"):
+        c.check(c.forward(y_type), y_type)
+
+
 @pytest.mark.parametrize("M", [4, 40, 300])
 def test_one_output_and_another_input_for_the_adapter(dev, M):
     c = Linear(M, M, 200, 384, 12, dev, shift=1)  # (B at an odd multiple of two bytes)
@@ -97,7 +121,7 @@ def test_inputs_already_quantized(dev, M, y_type):
 def test_repeated_calls_and_old_workspaces(dev, M):
     import torch
     c = Linear(M + 2, M, 520, 528, 16, dev)
-    n = H.hydra_fp8_lora_linear_workspace_bytes(M, 528, 16)
+    n = H.hydra_fp8_lora_linear_workspace_bytes(M, 520, 528, 16)
     first = c.forward("f32", workspace=torch.zeros(n, dtype=torch.uint8, device=dev))
     again = c.forward("f32", workspace=torch.full((n,), 0xFF, dtype=torch.uint8, device=dev))
     for a, b in zip(first, again):
@@ -164,7 +188,9 @@ def test_update_of_nothing_is_exact(dev):
 
 
 BACK = [(1, 16, 16, 1), (3, 64, 48, 8), (16, 160, 272, 128), (17, 128, 64, 16), (40, 144, 400, 5), (130, 528, 256, 64),
-        (333, 272, 640, 16), (1030, 256, 2064, 16), (70, 64, 96, 0)]
+        (333, 272, 640, 16), (1030, 256, 2064, 16), (70, 64, 96, 0),
+        (40, 8192, 304, 8), (3, 8192, 256, 16), (64, 4112, 144, 128), (1100, 144, 2608, 16), (2100, 64, 2608, 8),
+        (600, 48, 3312, 20), (2100, 64, 2608, 0)]
 
 
 @pytest.mark.parametrize("M,N,K,r", BACK)
@@ -236,7 +262,7 @@ def test_a_replayed_graph_on_new_inputs(dev, M):
     y = [empty((M, 256), "bf16", dev) for _ in range(2)]
     dx, dA, dB = empty((M, 512), "f32", dev), empty((16, 512), "f32", dev), empty((256, 16), "f32", dev)
     rng = rng_of(3, 1, dev)
-    ws = torch.empty(max(H.hydra_fp8_lora_linear_workspace_bytes(M, 512, 16),
+    ws = torch.empty(max(H.hydra_fp8_lora_linear_workspace_bytes(M, 256, 512, 16),
                          H.hydra_fp8_lora_linear_backward_workspace_bytes(M, 256, 512, 16)), dtype=torch.uint8, device=dev)
 
     def step():
