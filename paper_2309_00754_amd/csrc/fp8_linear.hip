@@ -141,7 +141,7 @@ __global__ __launch_bounds__(P_WAVES * 64) void fp8_prep_kernel(Fp8PrepArgs g) {
 // sums meet in LDS in wave order.  U blocks a wave are requested before the first
 // is used.
 template <int NB, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void fp8_stream_kernel(Fp8LinearArgs a) {
+__global__ __launch_bounds__(WAVES * 64, 4) void fp8_stream_kernel(Fp8LinearArgs a) {
   constexpr int U = 4, NT = WAVES * 64;
   __shared__ f32x4_t red[WAVES][NB][64];
   __shared__ float T[16][132];
@@ -157,7 +157,45 @@ __global__ __launch_bounds__(WAVES * 64) void fp8_stream_kernel(Fp8LinearArgs a)
   f32x4_t acc[NB];
 #pragma unroll
   for (int b = 0; b < NB; ++b) acc[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  for (int kb0 = wave; kb0 < kb_n; kb0 += WAVES * U) {
+  // T as the sum of its chunks in their order, and these rows of B: with 16 rows of W asked
+  // for before W and put into LDS while W is on its way (8 x 11008 x 4096 22.3 -> 18.5 us, 1 x
+  // 32000 x 4096 33.0 -> 30.6; 32 rows leave no registers for it)
+  constexpr int UT = 4;
+  const bool lora = a.y_on && a.rp > 0;
+  const int lr = lora ? __builtin_ctz(a.rp) : 0, items = lora ? (M << lr) / 4 : 0;
+  const int b_n = lora ? min(16 * NB, N - n0) << lr : 0;
+  const float* const part = a.part + 4 * t;
+  const uint32_t stride = (uint32_t)M << lr;
+  f32x4_t tv[UT];
+  uint16_t bv = 0;
+  auto b_at = [&](int i) {
+    const int n = i >> lr, j = i & (a.rp - 1);
+    return j < a.r ? a.B[(size_t)(n0 + n) * a.ldb + j] : (uint16_t)0;
+  };
+  auto ask = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < UT; ++i)
+      tv[i] = t < items && i < a.nch ? *reinterpret_cast<const f32x4_t*>(part + i * stride) : f32x4_t{0.f, 0.f, 0.f, 0.f};
+    if (t < b_n) bv = b_at(t);
+  };
+  auto stage = [&]() __attribute__((always_inline)) {
+    if (t < items) {
+      f32x4_t v = tv[0];
+#pragma unroll
+      for (int i = 1; i < UT; ++i) v += tv[i];
+#pragma unroll 4
+      for (int c = UT; c < a.nch; ++c) v += *reinterpret_cast<const f32x4_t*>(part + c * stride);
+      *reinterpret_cast<f32x4_t*>(&T[4 * t >> lr][4 * t & (a.rp - 1)]) = a.s * v;
+    }
+    if (t < b_n) Bs[t >> lr][t & (a.rp - 1)] = bv;
+    for (int i = t + NT; i < b_n; i += NT) Bs[i >> lr][i & (a.rp - 1)] = b_at(i);
+  };
+  static_assert(NT >= 16 * 128 / 4, "a thread for every four values of T");
+  if constexpr (NB == 1) {
+    ask();
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  for (int kb0 = wave; kb0 < kb_n || kb0 == wave; kb0 += WAVES * U) {
     uint4 x[U][2], w[U][NB][2];
     int sx[U], sw[U];
 #pragma unroll
@@ -176,6 +214,8 @@ __global__ __launch_bounds__(WAVES * 64) void fp8_stream_kernel(Fp8LinearArgs a)
       sw[u] = ws[kc];
     }
     __builtin_amdgcn_sched_barrier(0);
+    if constexpr (NB == 1)
+      if (kb0 == wave) stage();
     // lane l has values 32 (l / 16) ... + 31 of a block; the products take eight of
     // every lane at a time
 #pragma unroll
@@ -194,18 +234,9 @@ __global__ __launch_bounds__(WAVES * 64) void fp8_stream_kernel(Fp8LinearArgs a)
   }
 #pragma unroll
   for (int b = 0; b < NB; ++b) red[wave][b][lane] = acc[b];
-  const bool lora = a.y_on && a.rp > 0;
-  if (lora) {
-    const size_t stride = (size_t)M * a.rp;
-    for (int e = t; e < M * a.rp / 4; e += NT) {  // T as the sum of its chunks, in their order
-      const float* p = a.part + 4 * e;
-      f32x4_t v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-      for (int c = 0; c < a.nch; ++c) v += *reinterpret_cast<const f32x4_t*>(p + c * stride);
-      *reinterpret_cast<f32x4_t*>(&T[4 * e / a.rp][4 * e % a.rp]) = a.s * v;
-    }
-    const int rows = min(16 * NB, N - n0);
-    for (int e = t; e < rows * a.r; e += NT) Bs[e / a.r][e % a.r] = a.B[(size_t)(n0 + e / a.r) * a.ldb + e % a.r];
+  if constexpr (NB > 1) {
+    ask();
+    stage();
   }
   __syncthreads();
   for (int e = t; e < 16 * NB * M; e += NT) {
@@ -232,10 +263,11 @@ void launch_stream_as(const Fp8LinearArgs& a, hipStream_t stream) {
   hipLaunchKernelGGL((fp8_stream_kernel<NB, WAVES>), dim3((a.N + 16 * NB - 1) / (16 * NB)), dim3(WAVES * 64), 0, stream, a);
 }
 // Sixteen rows of W a workgroup; thirty-two where that leaves two workgroups a CU and more
-// than four rows of x, which every workgroup reads, count.  us, <1, 8> and <2, 8>: 8 x 4096 x
-// 4096 6.8 and 7.8, 8 x 11008 x 4096 13.4 and 15.4, 8 x 4096 x 11008 15.9 and 20.6, 16 x
-// 32000 x 4096 39.3 and 33.4, 8 x 32000 x 4096 31.3 and 30.0, 1 x 32000 x 4096 25.3 and 26.7;
-// four waves or sixteen, or 64 rows: slower at most sizes, by up to a half.
+// than four rows of x, which every workgroup reads, count.  us at rank 16, x quantized in
+// the call, <1, 8> and <2, 8>: 16 x 32000 x 4096 46.0 and 39.4, 8 x 32000 x 4096 37.7 and 34.9,
+// 12 x 16400 x 4096 27.6 and 25.4; the product alone: 8 x 4096 x 4096 6.8 and 7.8, 8 x 11008 x
+// 4096 13.4 and 15.4, 1 x 32000 x 4096 25.3 and 26.7.  Four waves or sixteen, or 64 rows:
+// slower at most sizes, by up to a half.
 void launch_stream(const Fp8LinearArgs& a, hipStream_t stream) {
   if (a.N > 16384 && a.M > 4)
     launch_stream_as<2, 8>(a, stream);
@@ -952,16 +984,19 @@ void launch_prep(const Fp8PrepArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-// Chunks of K: about 512 workgroups, each at least a block a wave, and no more
-// partial sums of T than the product can add up on the side.  2048 x 4096 at rank 16 takes
-// 8.5 to 9.1 us with 256, 512, 768 or 1024 workgroups and with 4, 8 or 16 waves.
+// Chunks of K: about 512 workgroups, each at least a block a wave (few rows at a rank
+// above 16: fewer, as A's rows take the time; 1 x 4096 x 4096 at rank 128 18.1 -> 13.6 us, 8 x
+// 8192 x 4096 at 64 19.7 -> 17.9), and no more partial sums of T than the product can
+// add up on the side.  2048 x 4096 at rank 16 takes 8.5 to 9.1 us with 256, 512, 768 or
+// 1024 workgroups and with 4, 8 or 16 waves.
 void fp8_prep_chunks(int M, int K, int rp, int& nch, int& kch) {
   const int kb = (K + kFp8Block - 1) / kFp8Block, mb = (M + 15) / 16;
   int want = (512 + mb - 1) / mb;
   const int most = rp == 0 ? 64 : M <= kFewRows ? 32 : rp <= 32 ? kStagedChunks : 4;
   want = want < most ? want : most;
   kch = (kb + want - 1) / want;
-  kch = kch < P_WAVES ? P_WAVES : kch;
+  const int least = M <= kFewRows && rp > 16 ? 256 / rp : P_WAVES;
+  kch = kch < least ? least : kch;
   nch = (kb + kch - 1) / kch;
 }
 
