@@ -912,11 +912,12 @@ constexpr TileCost kTiles[2][6] = {{{128, 256, 0.f, 5.8f, 0.767f, 0.f},
                                     {32, 64, 1.57f, 2.23f, 0.272f, 0.f},
                                     {32, 32, 2.9f, 0.72f, 0.067f, 0.165f}}};
 
-// K in parts (tiles 1, 2 and 4): few rows and a long K leave CUs without a tile.  The
+// K in parts (tiles 0, 1, 2 and 4): few rows and a long K leave CUs without a tile.  The
 // parts' sums go through memory, and a second launch joins them, for 3.9 us and the
 // sums written and read at 6.75 TB/s (a fit to 330 cases, rms error 9%).  us, whole ->
 // in parts, fp32: 17 x 2048 x 8192 17.9 -> 11.4, 64 x 4096 x 11008 25.3 -> 21.8, 200 x 4096 x
-// 11008 38.6 -> 32.7; below K = 4096 never faster.
+// 11008 38.6 -> 32.7; with tile 0 among them 333 x 4096 x 11008 59.3 -> 57.1 (bf16 51.2 ->
+// 47.8), rank 16 and x quantized in the call.  Below K = 4096 never faster.
 constexpr int kMaxSplit = 8, kMaxParts = 512;
 struct Plan {
   int tile, nsplit;
@@ -928,7 +929,7 @@ Plan plan_of(bool wide, int M, int N, int K) {
     const TileCost& c = kTiles[wide][i];
     const int64_t tiles = (int64_t)((M + c.tm - 1) / c.tm) * ((N + c.tn - 1) / c.tn);
     const int slabs = (K + 127) / 128;
-    const bool may = (i == 1 || i == 2 || i == 4) && tiles < 256;
+    const bool may = (i <= 2 || i == 4) && tiles < 256;
     for (int s = 1; s <= (may ? kMaxSplit : 1) && s * 4 <= (s == 1 ? 4 : slabs); ++s) {
       const int64_t n = tiles * s;
       if (s > 1 && n > kMaxParts) break;
@@ -947,18 +948,20 @@ Plan plan_of(bool wide, int M, int N, int K) {
 template <bool WIDE>
 hipError_t launch_rows(GemmArgs& g, hipStream_t stream) {
   const Plan p = plan_of(WIDE, g.a.M, g.a.N, g.a.K);
+  using T0 = Tile<WIDE, 128, 256, 64, 128, 1, 128, 3>;
   using T1 = Tile<WIDE, 128, 128, 64, 64, 2, 128, 4>;
   using T2 = Tile<WIDE, 64, 128, 64, 64, 2, 128, 6>;
   using T4 = Tile<WIDE, 32, 64, 32, 64, 4, 256, 6>;
   if (p.nsplit > 1) {
     switch (p.tile) {
+      case 0: return launch_split<T0>(g, p.nsplit, stream);
       case 1: return launch_split<T1>(g, p.nsplit, stream);
       case 2: return launch_split<T2>(g, p.nsplit, stream);
       default: return launch_split<T4>(g, p.nsplit, stream);
     }
   }
   switch (p.tile) {
-    case 0: return launch_tile<Tile<WIDE, 128, 256, 64, 128, 1, 128, 3>>(g, stream);
+    case 0: return launch_tile<T0>(g, stream);
     case 1: return launch_tile<T1>(g, stream);
     case 2: return launch_tile<T2>(g, stream);
     case 3: return launch_tile<Tile<WIDE, 64, 64, 32, 64, 2, 128, 4, 2>>(g, stream);

@@ -79,8 +79,9 @@ def test_linear_in_parts(dev, M, N, K, r, y_type):
     assert np.array_equal(f64(alone[1]), f64(y[1]))
 
 
-def test_tiles_of_128_rows_in_parts(dev):
-    c = Linear(0, 112, 4100, 6000, 16, dev)
+@pytest.mark.parametrize("M,N,K", [(112, 4100, 6000), (653, 1966, 8192)])
+def test_tiles_of_128_rows_in_parts(dev, M, N, K):
+    c = Linear(0, M, N, K, 16, dev)
     for y_type in ("f32", "bf16"):
         c.check(c.forward(y_type), y_type)
 
