@@ -728,7 +728,7 @@ bool backward_shape_ok(int64_t M, int64_t N, int64_t K, int64_t r) {
 hydra_status hydra_lora_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t r, size_t* bytes) {
   if (!bytes) return HYDRA_ERR_NULL;
   if (!backward_shape_ok(M, N, K, r)) return HYDRA_ERR_SHAPE;
-  *bytes = hydra::backward_ws_bytes(int(M), int(N), int(K), hydra::padded_rank(int(r)));
+  *bytes = hydra::backward_ws_bytes(int(M), int(N), int(K), hydra::padded_rank(int(r)), 2);
   return HYDRA_OK;
 }
 
@@ -744,13 +744,14 @@ hydra_status hydra_lora_linear_backward(const uint16_t* x, const uint16_t* Wt, c
   if (!aligned(dy, 16) || (x && !aligned(x, 16)) || (dx && !aligned(Wt, 16))) return HYDRA_ERR_ALIGN;
   if (r > 0 && (!aligned(A, 16) || !aligned(B, 2))) return HYDRA_ERR_ALIGN;
   if ((dx && !aligned(dx, 4)) || (dA && !aligned(dA, 4)) || (dB && !aligned(dB, 4))) return HYDRA_ERR_ALIGN;
-  const size_t need = hydra::backward_ws_bytes(int(M), int(N), int(K), hydra::padded_rank(int(r)));
+  const size_t need = hydra::backward_ws_bytes(int(M), int(N), int(K), hydra::padded_rank(int(r)), 2);
   if (need > 0) {
     if (!workspace) return HYDRA_ERR_NULL;
     if (workspace_bytes < need) return HYDRA_ERR_WORKSPACE;
     if (!aligned(workspace, 16)) return HYDRA_ERR_ALIGN;
   }
   hydra::BackwardArgs a{};
+  a.planes = 2;
   a.x = x;
   a.Wt = Wt;
   a.A = A;
@@ -1181,6 +1182,10 @@ size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 // Workspace of a product over an 8-bit weight: the rows' bytes and their scales.
 size_t fp8_rows_bytes(int64_t M, int64_t K) { return up256((size_t)M * K) + up256((size_t)M * blocks128(K)); }
 
+// Parts of s U and s T in the sums of dA and dB: 24 bits of them.  (Two, as in
+// hydra_lora_linear_backward, leave an error of 2^-17, ten times that of the fp32 sums.)
+constexpr int kFp8Planes = 3;
+
 hydra_status fp8_shape(int64_t M, int64_t N, int64_t K, int64_t r) {
   if (M < 1 || M > kMaxRows || N < 1 || N > kMaxCols || K < 1 || K > kMaxK || K % 16 != 0) return HYDRA_ERR_SHAPE;
   if (r < 0 || r > HYDRA_MAX_RANK) return HYDRA_ERR_SHAPE;
@@ -1305,7 +1310,7 @@ hydra_status hydra_fp8_lora_linear_backward_workspace_bytes(int64_t M, int64_t N
   if (chk != HYDRA_OK) return chk;
   if (K % 16 != 0) return HYDRA_ERR_SHAPE;
   *bytes = fp8_rows_bytes(M, N) + up256(hydra::fp8_split_most(int(M), int(K), int(N))) +
-           hydra::backward_ws_bytes(int(M), int(N), int(K), hydra::padded_rank(int(r)));
+           hydra::backward_ws_bytes(int(M), int(N), int(K), hydra::padded_rank(int(r)), kFp8Planes);
   return HYDRA_OK;
 }
 
@@ -1335,7 +1340,7 @@ hydra_status hydra_fp8_lora_linear_backward(const uint16_t* x, const uint8_t* Wq
     return HYDRA_ERR_ALIGN;
   const int rp = hydra::padded_rank(int(r));
   const size_t rows = fp8_rows_bytes(M, N), split = up256(hydra::fp8_split_most(int(M), int(K), int(N)));
-  const size_t need = rows + split + hydra::backward_ws_bytes(int(M), int(N), int(K), rp);
+  const size_t need = rows + split + hydra::backward_ws_bytes(int(M), int(N), int(K), rp, kFp8Planes);
   if (!workspace) return HYDRA_ERR_NULL;
   if (workspace_bytes < need) return HYDRA_ERR_WORKSPACE;
   if (!aligned(workspace, 16)) return HYDRA_ERR_ALIGN;
@@ -1367,6 +1372,7 @@ hydra_status hydra_fp8_lora_linear_backward(const uint16_t* x, const uint8_t* Wq
   a.r = int(r);
   a.dA = dA;
   a.dB = dB;
+  a.planes = kFp8Planes;
   a.base8 = dx ? &g : nullptr;
   return from_hip(hydra::launch_lora_backward(a, w + rows + split, reinterpret_cast<hipStream_t>(stream)));
 }

@@ -74,7 +74,8 @@ struct TpreArgs {
   uint16_t* ts;       // [M x 2 RP] hi | lo of s T, or nullptr
   uint16_t* bp;       // used only when B itself cannot serve (r != RP or B not 16-byte aligned)
   float* part;        // [kTpreMaxChunks x M x RP] fp32 partial sums over K chunks
-  uint16_t* tT;       // [2][RP][Mp] bf16 hi and lo planes of (s T)^T, rows M..Mp zero, or nullptr
+  uint16_t* tT;       // [2 or 3][RP][Mp] bf16 planes of (s T)^T, rows M..Mp zero, or nullptr
+  int planes;         // 3: the third plane of tT too
   int Mp;             // leading dimension of tT (M rounded up to 32)
   // jobs that may or may not run together: the longest K and the sum of K over
   // both, which the choice of kernel and chunks looks at (0: K)
@@ -386,13 +387,14 @@ struct BackwardArgs {
   float* dx;           // [M x K] or nullptr
   float* dA;           // [r x K] or nullptr
   float* dB;           // [N x r] or nullptr
+  int planes;          // parts of s U and s T in dA and dB: 2 or 3
   // W in 8 bits: Wt and dx null, and what the product over it takes in their
   // place (xq, xs: room for dy's; y_on: dx, of y_type; drop: the mask)
   const Fp8LinearArgs* base8;
 };
 // Workspace bytes of the backward, and the launcher (which assumes a
 // workspace of at least that size, 16-byte aligned).
-size_t backward_ws_bytes(int M, int N, int K, int rp);
+size_t backward_ws_bytes(int M, int N, int K, int rp, int planes);
 hipError_t launch_lora_backward(const BackwardArgs& a, void* ws, hipStream_t stream);
 // dst [Cp x Rp] bf16: dst[c][q] = src[q][c] for c < C, q < R (src [R x C]), else 0.
 hipError_t launch_transpose_pad(const uint16_t* src, int R, int C, uint16_t* dst, int Rp, int Cp, hipStream_t stream);

@@ -81,9 +81,10 @@ constexpr int O_KS = 32;           // rows per k-step (the k of one 16x16x32 MFM
 constexpr int O_LD = O_COLS + 4;   // LDS row stride in bf16 (130 dwords; see outer_part)
 constexpr int O_TARGET_WG = 256;   // workgroups the chunking aims for (both products together: twice that)
 constexpr int O_MIN_ROWS = 128;    // fewest rows per chunk
+constexpr int O_MIN_ROWS_3 = 64;   // ... with three planes of P (which give each chunk more to do)
 
 struct OuterArgs {
-  const uint16_t* PT;  // [2][RP][Mp] bf16: hi and lo planes of P^T (P = s U or s T)
+  const uint16_t* PT;  // [NP][RP][Mp] bf16: planes of P^T (P = s U or s T), hi and lo, or the next part too
   const uint16_t* Q;   // [M x C] bf16
   float* part;         // [nch x RP x C] (jc) or [nch x C x RP] fp32
   float* out;          // [r x C] (jc) or [C x r] fp32
@@ -96,14 +97,14 @@ struct OuterArgs {
 // Partial out[j][c] = sum_m P[m][j] Q[m][c] over the rows of one chunk, for
 // every j and the 256 columns of one tile (b = tile + tiles * chunk), on
 // v_mfma_f32_16x16x32_bf16: A operand = 16 j x 32 m of P^T (its hi plane,
-// then its lo plane: ~16 significant bits of P), B operand = 32 m x 16
+// then its lo plane: ~16 significant bits of P; NP = 3: 24), B operand = 32 m x 16
 // columns of Q.  The MFMA wants eight consecutive m per lane, but m is Q's
 // row index, so each 32-row slab of Q goes through LDS (row-major, double
 // buffered, one barrier per slab) and every lane gathers its column's eight
 // values with 16-bit reads.  With a row stride of 130 dwords the four row
 // groups of one read land in disjoint bank windows.  Each wave owns 64
 // columns and all RP j, so one slab in LDS serves every 16-wide j group.
-template <int RP>
+template <int RP, int NP>
 __device__ __forceinline__ void outer_part(const OuterArgs& a, int b) {
   constexpr int JG = RP / 16;
   __shared__ uint16_t qs[2][O_KS][O_LD];
@@ -148,14 +149,14 @@ __device__ __forceinline__ void outer_part(const OuterArgs& a, int b) {
   // Up to padded rank 32 they are requested a slab ahead, so that their latency overlaps the previous slab's
   // MFMAs; at higher ranks the second set of registers would cost occupancy, and they are requested in the slab.
   constexpr bool PF = JG <= 2;
-  uint4 ap[JG][2], an[PF ? JG : 1][2];
-  auto load_p = [&](int ks, uint4 (&d)[JG][2]) __attribute__((always_inline)) {
+  uint4 ap[JG][NP], an[PF ? JG : 1][NP];
+  auto load_p = [&](int ks, uint4 (&d)[JG][NP]) __attribute__((always_inline)) {
     const int m0 = m_begin + ks * O_KS;
 #pragma unroll
     for (int g = 0; g < JG; ++g) {
       const uint16_t* p = a.PT + (size_t)(g * 16 + l16) * a.Mp + m0 + 8 * lg;
-      d[g][0] = *reinterpret_cast<const uint4*>(p);
-      d[g][1] = *reinterpret_cast<const uint4*>(p + (size_t)a.RP * a.Mp);
+#pragma unroll
+      for (int n = 0; n < NP; ++n) d[g][n] = *reinterpret_cast<const uint4*>(p + n * (size_t)a.RP * a.Mp);
     }
   };
   if constexpr (PF) load_p(0, ap);
@@ -184,8 +185,8 @@ __device__ __forceinline__ void outer_part(const OuterArgs& a, int b) {
     for (int g = 0; g < JG; ++g)
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
-        acc[g][s] = mfma16(ap[g][0], bq[s], acc[g][s]);
-        acc[g][s] = mfma16(ap[g][1], bq[s], acc[g][s]);
+#pragma unroll
+        for (int n = 0; n < NP; ++n) acc[g][s] = mfma16(ap[g][n], bq[s], acc[g][s]);
       }
     if (ks + 1 < nks) {
       store(st ^ 1);  // stage st ^ 1 was last read before the previous barrier
@@ -193,8 +194,8 @@ __device__ __forceinline__ void outer_part(const OuterArgs& a, int b) {
       if constexpr (PF) {
 #pragma unroll
         for (int g = 0; g < JG; ++g) {
-          ap[g][0] = an[g][0];
-          ap[g][1] = an[g][1];
+#pragma unroll
+          for (int n = 0; n < NP; ++n) ap[g][n] = an[g][n];
         }
       }
     }
@@ -221,13 +222,13 @@ __device__ __forceinline__ void outer_part(const OuterArgs& a, int b) {
 }
 
 // dA's and dB's partials in one launch: workgroups [0, n0) for o0, the rest o1.
-template <int RP>
+template <int RP, int NP>
 __global__ __launch_bounds__(O_WAVES * 64) void lora_outer_part_kernel(OuterArgs o0, int n0, OuterArgs o1) {
   const int b = blockIdx.x;
   if (b < n0)
-    outer_part<RP>(o0, b);
+    outer_part<RP, NP>(o0, b);
   else
-    outer_part<RP>(o1, b - n0);
+    outer_part<RP, NP>(o1, b - n0);
 }
 
 constexpr int F_UNROLL = 8;
@@ -262,39 +263,47 @@ __global__ __launch_bounds__(256) void lora_outer_finish_kernel(OuterArgs o0, in
 
 // Rows per chunk and number of chunks of the outer products over M rows and
 // C columns: enough chunks for about O_TARGET_WG workgroups, each chunk a
-// multiple of O_KS rows and at least O_MIN_ROWS.
-void outer_chunks(int M, int C, int& mch, int& nch) {
+// multiple of O_KS rows and at least O_MIN_ROWS (by which chunk the sums are joined
+// is part of the result: three planes have chunks of their own.  The backward over an
+// 8-bit weight, us with chunks of at least 128, 64, 32 rows: 250 x 8192 x 2048 at rank
+// 128 70.7, 66.8, 69.3; 1000 x 2048 x 2048 at 128 70.1, 66.8, 75.3; 512 x 4096 x 4096 at 64 63.1,
+// 61.2, 64.1; two planes and 128 rows 66.3, 64.0, 60.8).
+void outer_chunks(int M, int C, int planes, int& mch, int& nch) {
   const int64_t tiles = (C + O_COLS - 1) / O_COLS;
   const int64_t want = std::max<int64_t>(1, (O_TARGET_WG + tiles - 1) / tiles);
   int64_t rows = (M + want - 1) / want;
-  rows = std::max<int64_t>(O_MIN_ROWS, (rows + O_KS - 1) / O_KS * O_KS);
+  rows = std::max<int64_t>(planes == 3 ? O_MIN_ROWS_3 : O_MIN_ROWS, (rows + O_KS - 1) / O_KS * O_KS);
   mch = (int)rows;
   nch = (int)((M + rows - 1) / rows);
 }
 
 int padded_rows(int M) { return (M + O_KS - 1) / O_KS * O_KS; }
 
-OuterArgs outer_job(const uint16_t* PT, const uint16_t* Q, int M, int C, int rp, int r, float* part, float* out,
-                    bool jc, int& parts, int& finishes) {
+OuterArgs outer_job(const uint16_t* PT, const uint16_t* Q, int M, int C, int rp, int r, int planes, float* part,
+                    float* out, bool jc, int& parts, int& finishes) {
   OuterArgs o{PT, Q, part, out, M, padded_rows(M), C, rp, r, 0, 0, jc ? 1 : 0, (C + O_COLS - 1) / O_COLS};
-  outer_chunks(M, C, o.mch, o.nch);
+  outer_chunks(M, C, planes, o.mch, o.nch);
   parts = o.tiles * o.nch;
   finishes = (int)(((size_t)r * C + 255) / 256);
   return o;
 }
 
 template <int RP>
-void launch_outer_rp(const OuterArgs& o0, int p0, const OuterArgs& o1, int p1, hipStream_t stream) {
-  hipLaunchKernelGGL((lora_outer_part_kernel<RP>), dim3(p0 + p1), dim3(O_WAVES * 64), 0, stream, o0, p0, o1);
+void launch_outer_rp(const OuterArgs& o0, int p0, const OuterArgs& o1, int p1, int planes, hipStream_t stream) {
+  const dim3 grid(p0 + p1), block(O_WAVES * 64);
+  if (planes == 3)
+    hipLaunchKernelGGL((lora_outer_part_kernel<RP, 3>), grid, block, 0, stream, o0, p0, o1);
+  else
+    hipLaunchKernelGGL((lora_outer_part_kernel<RP, 2>), grid, block, 0, stream, o0, p0, o1);
 }
 
 hipError_t launch_outer(const OuterArgs& o0, int p0, int f0, const OuterArgs& o1, int p1, int f1, int rp,
-                        hipStream_t stream) {
+                        int planes, hipStream_t stream) {
   switch (rp) {
-    case 16: launch_outer_rp<16>(o0, p0, o1, p1, stream); break;
-    case 32: launch_outer_rp<32>(o0, p0, o1, p1, stream); break;
-    case 64: launch_outer_rp<64>(o0, p0, o1, p1, stream); break;
-    case 128: launch_outer_rp<128>(o0, p0, o1, p1, stream); break;
+    case 16: launch_outer_rp<16>(o0, p0, o1, p1, planes, stream); break;
+    case 32: launch_outer_rp<32>(o0, p0, o1, p1, planes, stream); break;
+    case 64: launch_outer_rp<64>(o0, p0, o1, p1, planes, stream); break;
+    case 128: launch_outer_rp<128>(o0, p0, o1, p1, planes, stream); break;
     default: return hipErrorInvalidValue;
   }
   hipError_t e = hipGetLastError();
@@ -310,20 +319,20 @@ struct BwdLayout {
   size_t bt, at, tsu, uT, tT, tpart, tpart2, opa, opb, total;
 };
 
-BwdLayout layout(int M, int N, int K, int rp) {
+BwdLayout layout(int M, int N, int K, int rp, int planes) {
   BwdLayout l{};
   size_t o = 0;
   l.bt = o;    o += up256((size_t)rp * N * 2);                      // B^T [RP x N] bf16
   l.at = o;    o += up256((size_t)K * rp * 2);                      // A^T [K x RP] bf16
   l.tsu = o;   o += up256((size_t)M * 2 * rp * 2);                  // hi | lo of s U [M x 2 RP] bf16
   const size_t Mp = (size_t)padded_rows(M);
-  l.uT = o;    o += up256(2 * (size_t)rp * Mp * 2);                 // hi | lo planes of (s U)^T [2][RP][Mp] bf16
-  l.tT = o;    o += up256(2 * (size_t)rp * Mp * 2);                 // hi | lo planes of (s T)^T [2][RP][Mp] bf16
+  l.uT = o;    o += up256(planes * (size_t)rp * Mp * 2);            // planes of (s U)^T, [planes][RP][Mp] bf16
+  l.tT = o;    o += up256(planes * (size_t)rp * Mp * 2);            // planes of (s T)^T, [planes][RP][Mp] bf16
   l.tpart = o; o += up256((size_t)kTpreMaxChunks * M * rp * 4);     // pre-pass partials (s U)
   l.tpart2 = o; o += up256((size_t)kTpreMaxChunks * M * rp * 4);    // pre-pass partials (s T)
   int mch, nch_a, nch_b;
-  outer_chunks(M, K, mch, nch_a);
-  outer_chunks(M, N, mch, nch_b);
+  outer_chunks(M, K, planes, mch, nch_a);
+  outer_chunks(M, N, planes, mch, nch_b);
   const size_t oa = (size_t)nch_a * rp * K, ob = (size_t)nch_b * rp * N;
   l.opa = o;   o += up256(oa * 4);                                  // dA's outer-product partials
   l.opb = o;   o += up256(ob * 4);                                  // dB's outer-product partials
@@ -341,7 +350,9 @@ hipError_t launch_transpose_pad(const uint16_t* src, int R, int C, uint16_t* dst
   return hipGetLastError();
 }
 
-size_t backward_ws_bytes(int M, int N, int K, int rp) { return rp == 0 ? 0 : layout(M, N, K, rp).total; }
+size_t backward_ws_bytes(int M, int N, int K, int rp, int planes) {
+  return rp == 0 ? 0 : layout(M, N, K, rp, planes).total;
+}
 
 hipError_t launch_lora_backward(const BackwardArgs& a, void* ws, hipStream_t stream) {
   const int rp = padded_rank(a.r);
@@ -375,7 +386,7 @@ hipError_t launch_lora_backward(const BackwardArgs& a, void* ws, hipStream_t str
     g.y_off = a.dx;
     return launch_lora_gemm(g, stream);
   }
-  const BwdLayout l = layout(a.M, a.N, a.K, rp);
+  const BwdLayout l = layout(a.M, a.N, a.K, rp, a.planes);
   uint8_t* w = static_cast<uint8_t*>(ws);
   uint16_t* bt = reinterpret_cast<uint16_t*>(w + l.bt);
   uint16_t* at = reinterpret_cast<uint16_t*>(w + l.at);
@@ -408,6 +419,7 @@ hipError_t launch_lora_backward(const BackwardArgs& a, void* ws, hipStream_t str
   u.part = reinterpret_cast<float*>(w + l.tpart);
   u.tT = a.dA ? reinterpret_cast<uint16_t*>(w + l.uT) : nullptr;
   u.Mp = padded_rows(a.M);
+  u.planes = tt.planes = a.planes;
   tt.x = a.x;
   tt.A = a.A;
   tt.s = a.s;
@@ -441,11 +453,11 @@ hipError_t launch_lora_backward(const BackwardArgs& a, void* ws, hipStream_t str
   int p0 = 0, f0 = 0, p1 = 0, f1 = 0;
   OuterArgs o0{}, o1{};
   if (a.dA)
-    o0 = outer_job(u.tT, a.x, a.M, a.K, rp, a.r, reinterpret_cast<float*>(w + l.opa), a.dA, true, p0, f0);
+    o0 = outer_job(u.tT, a.x, a.M, a.K, rp, a.r, a.planes, reinterpret_cast<float*>(w + l.opa), a.dA, true, p0, f0);
   if (a.dB)
-    o1 = outer_job(tt.tT, a.dy, a.M, a.N, rp, a.r, reinterpret_cast<float*>(w + l.opb), a.dB, false, p1, f1);
+    o1 = outer_job(tt.tT, a.dy, a.M, a.N, rp, a.r, a.planes, reinterpret_cast<float*>(w + l.opb), a.dB, false, p1, f1);
   if (p0 + p1 > 0)
-    if ((e = launch_outer(o0, p0, f0, o1, p1, f1, rp, stream)) != hipSuccess) return e;
+    if ((e = launch_outer(o0, p0, f0, o1, p1, f1, rp, a.planes, stream)) != hipSuccess) return e;
   return hipSuccess;
 }
 

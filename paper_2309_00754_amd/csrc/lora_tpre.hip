@@ -117,7 +117,7 @@ __device__ __forceinline__ void pad_b(const TpreArgs& a, size_t block, size_t bl
   }
 }
 
-// hi and lo bf16 parts of s * T[row][j], written row-major (ts) and / or
+// hi and lo bf16 parts of s * T[row][j] (and what they leave, to tT), written row-major (ts) and / or
 // transposed (tT, whose rows M..Mp are written as zeros: v = 0 there).
 __device__ __forceinline__ void t_store(const TpreArgs& a, int rp, size_t row, size_t j, float v) {
   v *= a.s;
@@ -130,6 +130,8 @@ __device__ __forceinline__ void t_store(const TpreArgs& a, int rp, size_t row, s
   if (a.tT) {
     a.tT[j * a.Mp + row] = (uint16_t)hi;
     a.tT[(rp + j) * a.Mp + row] = (uint16_t)lo;
+    if (a.planes == 3)
+      a.tT[(2 * rp + j) * a.Mp + row] = (uint16_t)f32_to_bf16_rne(v - bf16_to_f32(hi) - bf16_to_f32(lo));
   }
 }
 

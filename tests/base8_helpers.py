@@ -81,8 +81,9 @@ def backward_bounds(xa, W, A, B, s, dy, dx_type, factor):
     wide = dx_type == "f32"
     u = abs(s) * (np.abs(dy) @ np.abs(B))
     t = abs(s) * (np.abs(xa) @ np.abs(A).T)
-    r_u, r_t = (N + 2) * U + 2.0 ** -17, (K + 2) * U + 2.0 ** -17
-    dx = product_bound(dq, W.T, wide) + (r_u + (2 * r + 4) * U) * (u @ np.abs(A)) * np.maximum(factor, 0)
-    dA = (r_u + (2 * M + 2) * U) * (u.T @ np.abs(xa))
-    dB = (r_t + (2 * M + 2) * U) * (np.abs(dy).T @ t)
+    # (dx takes two bf16 parts of s U, dA and dB three, which are within 2^-25 of it)
+    r_u, r_t = (N + 2.5) * U, (K + 2.5) * U
+    dx = product_bound(dq, W.T, wide) + (r_u + 2.0 ** -17 + (2 * r + 4) * U) * (u @ np.abs(A)) * np.maximum(factor, 0)
+    dA = (r_u + (3 * M + 2) * U) * (u.T @ np.abs(xa))
+    dB = (r_t + (3 * M + 2) * U) * (np.abs(dy).T @ t)
     return dx, dA + 1e-40, dB + 1e-40
