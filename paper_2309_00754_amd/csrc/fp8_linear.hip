@@ -416,37 +416,39 @@ __global__ __launch_bounds__(G::NT, G::NT / 256 * G::WPC) void fp8_gemm_kernel(G
               f32x4_t{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
         }
   };
-  // The base product from its parts (N % 4 == 0: four at a time).
-  auto add_parts = [&](float* v, int row, int col) __attribute__((always_inline)) {
-    if (m0 + row >= M) return;
-    const float* p = a.split + (size_t)(m0 + row) * N + n0 + col;
-    const size_t stride = (size_t)M * N;
-    constexpr int W = G::WIDE ? 4 : 8;
-    f32x4_t sum[W / 4];
-#pragma unroll
-    for (int q = 0; q < W / 4; ++q) sum[q] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < g.nsplit; ++k, p += stride)
-#pragma unroll
-      for (int q = 0; q < W / 4; ++q) {
-        if (N % 4 == 0) {
-          if (n0 + col + 4 * q < N) sum[q] += *reinterpret_cast<const f32x4_t*>(p + 4 * q);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (n0 + col + 4 * q + e < N) sum[q][e] += p[4 * q + e];
-        }
-      }
-#pragma unroll
-    for (int e = 0; e < W; ++e) v[e] += sum[e / 4][e % 4];
-  };
   // A thread's groups of consecutive columns, 16 bytes of the output: f(values, row, column).
-  constexpr int w = G::WIDE ? 4 : 8;
-  auto each = [&](auto f) __attribute__((always_inline)) {
-    constexpr int per_row = TN / w, n = TM * per_row;
+  constexpr int w = G::WIDE ? 4 : 8, per_row = TN / w, groups = TM * per_row, rounds = (groups + G::NT - 1) / G::NT;
+  // JOIN: the base product of these groups, from its parts (N % 4 == 0: four at a time)
+  f32x4_t base[PH == JOIN ? rounds : 1][w / 4];
+  if constexpr (PH == JOIN) {
+    const size_t stride = (size_t)M * N;
+#pragma unroll
+    for (int i = 0; i < rounds; ++i) {
+      const int at = i * G::NT + t, row = at / per_row, col = at % per_row * w;
+      const bool ok = at < groups && m0 + row < M;
+      const float* p = a.split + (size_t)(m0 + row) * N + n0 + col;
+#pragma unroll
+      for (int q = 0; q < w / 4; ++q) base[i][q] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-    for (int i = 0; i < (n + G::NT - 1) / G::NT; ++i) {
+      for (int k = 0; k < g.nsplit; ++k, p += stride)
+#pragma unroll
+        for (int q = 0; q < w / 4; ++q) {
+          if (N % 4 == 0) {
+            if (ok && n0 + col + 4 * q < N) base[i][q] += *reinterpret_cast<const f32x4_t*>(p + 4 * q);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (ok && n0 + col + 4 * q + e < N) base[i][q][e] += p[4 * q + e];
+          }
+        }
+    }
+  }
+  auto each = [&](auto f) __attribute__((always_inline)) {
+    constexpr int un = PH == JOIN ? rounds : 4;
+#pragma unroll un
+    for (int i = 0; i < rounds; ++i) {
       const int at = i * G::NT + te;
-      if (n % G::NT != 0 && at >= n) break;
+      if (groups % G::NT != 0 && at >= groups) break;
       const int row = at / per_row, col = at % per_row * w;
       float v[w];
 #pragma unroll
@@ -455,10 +457,10 @@ __global__ __launch_bounds__(G::NT, G::NT / 256 * G::WPC) void fp8_gemm_kernel(G
 #pragma unroll
         for (int k = 1; k < KS; ++k)
           s += *reinterpret_cast<const f32x4_t*>(out + (k * TM + row) * OLD + col + 4 * q);
+        if constexpr (PH == JOIN) s += base[i][q];
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[4 * q + e] = s[e];
       }
-      if constexpr (PH == JOIN) add_parts(v, row, col);
       f(v, row, col);
     }
   };
