@@ -30,6 +30,18 @@ constexpr int P_WAVES = 8;
 constexpr int kFewRows = 16;
 constexpr int kStagedChunks = 8;  // most partial sums of T at padded rank 16 above kFewRows rows
 
+// Four values as bf16 and, in bf16 too, what that leaves of them.
+__device__ __forceinline__ void two_parts(const f32x4_t& v, uint2& hi, uint2& lo) {
+  uint32_t h[4], l[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    h[i] = f32_to_bf16_any(v[i]);
+    l[i] = (h[i] & 0x7FFF) < 0x7F80 ? f32_to_bf16_any(v[i] - bf16_to_f32(h[i])) : 0;  // (none of an infinity)
+  }
+  hi = make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
+  lo = make_uint2(l[0] | l[1] << 16, l[2] | l[3] << 16);
+}
+
 // The pieces of four lanes 16 apart, transposed: v[j] of lane group g becomes v[g] of
 // lane group j.
 __device__ __forceinline__ void transpose4(uint32_t (&v)[4]) {
@@ -132,6 +144,22 @@ __global__ __launch_bounds__(P_WAVES * 64) void fp8_prep_kernel(Fp8PrepArgs g) {
       g.part[((size_t)blockIdx.y * g.M + m0 + row) * RP + j] = sum;
     }
   }
+}
+
+// s T as its bf16 parts [M][hi rp | lo rp], which tiles at a rank above 16 read in place of
+// the chunks' sums: four values a thread.
+__global__ __launch_bounds__(256) void fp8_t_finish_kernel(Fp8PrepArgs g, int lrp) {
+  const size_t e = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4, all = (size_t)g.M << lrp;
+  if (e >= all) return;
+  f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int c = 0; c < g.nch; ++c) v += *reinterpret_cast<const f32x4_t*>(g.part + c * all + e);
+  uint2 hi, lo;
+  two_parts(g.s * v, hi, lo);
+  const size_t row = e >> lrp;
+  uint16_t* const o = g.ts + (row << (lrp + 1)) + (e - (row << lrp));
+  *reinterpret_cast<uint2*>(o) = hi;
+  *reinterpret_cast<uint2*>(o + g.rp) = lo;
 }
 
 // ------------------------------------------------------------------ few rows
@@ -487,15 +515,10 @@ __global__ __launch_bounds__(G::NT, G::NT / 256 * G::WPC) void fp8_gemm_kernel(G
   uint16_t* const Bs = Ts + TM * ldt;
   // Four values of s T, of a tile's row.
   auto put_t = [&](int row, int j, const f32x4_t& v) __attribute__((always_inline)) {
-    uint32_t hi[4], lo[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float f = a.s * v[i];
-      hi[i] = f32_to_bf16_any(f);
-      lo[i] = (hi[i] & 0x7FFF) < 0x7F80 ? f32_to_bf16_any(f - bf16_to_f32(hi[i])) : 0;  // (none of an infinity)
-    }
-    *reinterpret_cast<uint2*>(Ts + row * ldt + j) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
-    *reinterpret_cast<uint2*>(Ts + row * ldt + rp + j) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+    uint2 hi, lo;
+    two_parts(a.s * v, hi, lo);
+    *reinterpret_cast<uint2*>(Ts + row * ldt + j) = hi;
+    *reinterpret_cast<uint2*>(Ts + row * ldt + rp + j) = lo;
   };
   const int rows = min(TM, M - m0), cols = min(TN, N - n0);
   // By the 256 threads of the copy waves.  At padded rank 16, the usual one, the loads
@@ -541,6 +564,7 @@ __global__ __launch_bounds__(G::NT, G::NT / 256 * G::WPC) void fp8_gemm_kernel(G
   };
   auto put_update = [&](int tc) __attribute__((always_inline)) {
     if (a.ts) {
+#pragma unroll 8
       for (int e = tc; e < TM * rp / 4; e += 256) {  // 16 bytes each
         const int row = e >> (lrp - 2), c = (e & (rp / 4 - 1)) * 8;
         uint4 v = make_uint4(0, 0, 0, 0);
@@ -561,7 +585,7 @@ __global__ __launch_bounds__(G::NT, G::NT / 256 * G::WPC) void fp8_gemm_kernel(G
       }
     }
     if (g.bvec) {
-#pragma unroll 4
+#pragma unroll 8
       for (int e = tc; e < TN * rp / 8; e += 256) {
         const int row = e >> (lrp - 3), j = (e & (rp / 8 - 1)) * 8;
         uint4 v = make_uint4(0, 0, 0, 0);
@@ -989,6 +1013,12 @@ void launch_prep(const Fp8PrepArgs& a, hipStream_t stream) {
 
 }  // namespace
 
+// A tile's partial sums of T at a high rank are many, and another launch pays that adds
+// them up once.  us without and with it: 2048 x 11008 x 4096 at rank 128 into bf16 198.6 and
+// 161.6, 1024 x 4096 x 4096 64.7 and 53.4, 250 x 2048 x 8192 46.8 and 37.4, 40 x 1024 x 1024 17.8 and
+// 19.2; 2048 x 4096 x 4096 at 64 64.0 and 60.9, 512 38.9 and 38.3, 64 21.9 and 22.8; 2048 at 32
+// 54.3 and 53.8, 512 33.9 and 35.1.
+bool fp8_finishes_t(int M, int rp) { return rp > 16 && M > kFewRows && (int64_t)M * rp >= 24576; }
 // Chunks of K: about 512 workgroups, each at least a block a wave (few rows at a rank
 // above 16: fewer, as A's rows take the time; 1 x 4096 x 4096 at rank 128 18.1 -> 13.6 us, 8 x
 // 8192 x 4096 at 64 19.7 -> 17.9), and no more partial sums of T than the product can
@@ -997,7 +1027,7 @@ void launch_prep(const Fp8PrepArgs& a, hipStream_t stream) {
 void fp8_prep_chunks(int M, int K, int rp, int& nch, int& kch) {
   const int kb = (K + kFp8Block - 1) / kFp8Block, mb = (M + 15) / 16;
   int want = (512 + mb - 1) / mb;
-  const int most = rp == 0 ? 64 : M <= kFewRows ? 32 : rp <= 32 ? kStagedChunks : 4;
+  const int most = rp == 0 ? 64 : M <= kFewRows ? 32 : rp <= 32 || fp8_finishes_t(M, rp) ? kStagedChunks : 4;
   want = want < most ? want : most;
   kch = (kb + want - 1) / want;
   const int least = M <= kFewRows && rp > 16 ? 256 / rp : P_WAVES;
@@ -1014,6 +1044,10 @@ hipError_t launch_fp8_prep(const Fp8PrepArgs& a, hipStream_t stream) {
     case 128: launch_prep<128>(a, stream); break;
     default: return hipErrorInvalidValue;
   }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !a.ts) return e;
+  const size_t blocks = ((size_t)a.M * a.rp / 4 + 255) / 256;
+  hipLaunchKernelGGL(fp8_t_finish_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, a, 31 - __builtin_clz(a.rp));
   return hipGetLastError();
 }
 
@@ -1025,7 +1059,7 @@ size_t fp8_split_most(int M, int N, int K) {
 size_t fp8_prep_most(int M, int rp) {
   if (rp == 0) return 0;
   const size_t few = (size_t)32 * (M < kFewRows ? M : kFewRows);
-  const size_t by_rows = (size_t)(rp <= 32 ? kStagedChunks : 4) * M, by_grid = (size_t)(512 + 1) * 16 + M;
+  const size_t by_rows = (size_t)kStagedChunks * M, by_grid = (size_t)(512 + 1) * 16 + M;
   const size_t many = M <= kFewRows ? 0 : by_rows < by_grid ? by_rows : by_grid;
   return (few > many ? few : many) * rp * 4;
 }

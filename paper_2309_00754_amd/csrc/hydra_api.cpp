@@ -1229,7 +1229,9 @@ hydra_status hydra_fp8_lora_linear_workspace_bytes(int64_t M, int64_t N, int64_t
   const hydra_status chk = fp8_shape(M, N, K, r);
   if (chk != HYDRA_OK) return chk;
   // (what the largest of the calls with up to M rows needs)
-  *bytes = fp8_rows_bytes(M, K) + up256(hydra::fp8_prep_most(int(M), hydra::padded_rank(int(r)))) +
+  const int rp = hydra::padded_rank(int(r));
+  *bytes = fp8_rows_bytes(M, K) + up256(hydra::fp8_prep_most(int(M), rp)) +
+           (hydra::fp8_finishes_t(int(M), rp) ? up256((size_t)M * 2 * rp * 2) : 0) +
            up256(hydra::fp8_split_most(int(M), int(N), int(K)));
   return HYDRA_OK;
 }
@@ -1257,7 +1259,8 @@ hydra_status hydra_fp8_lora_linear(const uint16_t* x, const uint16_t* x_adapter,
   int nch = 0, kch = 0;
   hydra::fp8_prep_chunks(int(M), int(K), rp, nch, kch);
   const size_t rows = xq ? 0 : fp8_rows_bytes(M, K), part = up256(hydra::fp8_prep_most(int(M), rp));
-  const size_t need = rows + part + up256(hydra::fp8_split_most(int(M), int(N), int(K)));
+  const size_t ts_bytes = hydra::fp8_finishes_t(int(M), rp) ? up256((size_t)M * 2 * rp * 2) : 0;
+  const size_t need = rows + part + ts_bytes + up256(hydra::fp8_split_most(int(M), int(N), int(K)));
   if (need > 0) {
     if (!workspace) return HYDRA_ERR_NULL;
     if (workspace_bytes < need) return HYDRA_ERR_WORKSPACE;
@@ -1277,6 +1280,8 @@ hydra_status hydra_fp8_lora_linear(const uint16_t* x, const uint16_t* x_adapter,
   p.part = reinterpret_cast<float*>(w + rows);
   p.nch = nch;
   p.kch = kch;
+  p.s = s;
+  p.ts = ts_bytes ? reinterpret_cast<uint16_t*>(w + rows + part) : nullptr;
   const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   if (rows + part > 0) {
     const hipError_t e = hydra::launch_fp8_prep(p, st);
@@ -1297,7 +1302,8 @@ hydra_status hydra_fp8_lora_linear(const uint16_t* x, const uint16_t* x_adapter,
   a.rp = rp;
   a.s = s;
   a.part = p.part;
-  a.split = reinterpret_cast<float*>(w + rows + part);
+  a.ts = p.ts;
+  a.split = reinterpret_cast<float*>(w + rows + part + ts_bytes);
   a.nch = nch;
   a.B = B;
   a.ldb = int(r);

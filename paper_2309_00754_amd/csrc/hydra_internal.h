@@ -331,7 +331,11 @@ struct Fp8PrepArgs {
   uint8_t* xs;
   float* part;         // [nch][M][rp]
   int nch, kch;        // chunks of K, of kch blocks of 128
+  float s;
+  uint16_t* ts;        // [M][2 rp] bf16 hi | lo of s T, or nullptr (fp8_finishes_t)
 };
+// Whether the product takes s T as ts, else the partial sums.
+bool fp8_finishes_t(int M, int rp);
 void fp8_prep_chunks(int M, int K, int rp, int& nch, int& kch);
 hipError_t launch_fp8_prep(const Fp8PrepArgs& a, hipStream_t stream);
 hipError_t launch_fp8_linear(const Fp8LinearArgs& a, hipStream_t stream);

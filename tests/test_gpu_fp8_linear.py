@@ -50,7 +50,8 @@ class Linear:
 SIZES = [(1, 16, 16, 1), (1, 48, 160, 16), (2, 100, 272, 8), (7, 33, 1040, 5), (8, 512, 2048, 16), (16, 130, 4096, 128),
          (16, 64, 112, 64), (17, 64, 128, 16), (31, 97, 400, 3), (33, 256, 144, 32), (64, 300, 1024, 16), (65, 129, 640, 128),
          (127, 512, 528, 16), (200, 1000, 256, 64), (333, 260, 2064, 16), (130, 8200, 128, 8), (520, 3300, 144, 16),
-         (1100, 2052, 272, 20), (2100, 2600, 128, 16), (40, 36, 64, 0), (5, 20, 48, 0)]
+         (1100, 2052, 272, 20), (2100, 2600, 128, 16), (40, 36, 64, 0), (5, 20, 48, 0), (230, 300, 400, 100), (401, 130, 272, 41),
+        (2050, 72, 64, 128)]
 
 
 @pytest.mark.parametrize("M,N,K,r", SIZES)
