@@ -261,6 +261,132 @@ __global__ __launch_bounds__(256) void lora_outer_finish_kernel(OuterArgs o0, in
     outer_finish(o1, (size_t)(b - n0) * 256 + threadIdx.x);
 }
 
+// ... over all rows in one workgroup and 64 columns of the output, with no partial sums: for
+// few rows.  Four waves share out the 16-wide j groups, and where those are fewer than
+// four the 32-row slabs of a step, whose sums meet in LDS in wave order.
+constexpr int W_COLS = 64, W_ROWS = 128, W_LD = W_COLS + 4;
+template <int RP>
+__device__ __forceinline__ void outer_whole(const OuterArgs& a, int b) {
+  constexpr int NP = 3, JG = RP / 16, JW = JG < 4 ? JG : 4, JGW = JG / JW, SW = 4 / JW, SS = W_ROWS / O_KS / SW;
+  __shared__ __attribute__((aligned(16))) uint16_t qs[2][W_ROWS][W_LD];
+  const int t = threadIdx.x, lane = t & 63, l16 = lane & 15, lg = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(t >> 6), jw = wave % JW, sw = wave / JW;
+  const int c0 = b * W_COLS, nks = a.Mp / O_KS, nst = (a.Mp + W_ROWS - 1) / W_ROWS;
+  const int lr = t >> 3, lc = (t & 7) * 8;
+  uint4 qv[4];
+  auto load = [&](int st) __attribute__((always_inline)) {
+    const int m0 = st * W_ROWS, rows = min(W_ROWS, a.M - m0);
+    const __amdgpu_buffer_rsrc_t qrs = make_rsrc(a.Q + (size_t)m0 * a.C, (uint32_t)rows * a.C * 2u);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int row = lr + 32 * u;
+      qv[u] = buf_load16(qrs, (row < rows && c0 + lc < a.C) ? (row * a.C + c0 + lc) * 2 : kOutOfRange);
+    }
+  };
+  auto store = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      uint2* d = reinterpret_cast<uint2*>(&qs[buf][lr + 32 * u][lc]);
+      d[0] = uint2{qv[u].x, qv[u].y};
+      d[1] = uint2{qv[u].z, qv[u].w};
+    }
+  };
+  f32x4_t acc[JGW][4];
+#pragma unroll
+  for (int g = 0; g < JGW; ++g)
+#pragma unroll
+    for (int s = 0; s < 4; ++s) acc[g][s] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  load(0);
+  uint4 ap[SS][JGW][NP];
+  auto load_p = [&](int st) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < SS; ++i) {
+      const int ks = st * (W_ROWS / O_KS) + i * SW + sw;
+#pragma unroll
+      for (int g = 0; g < JGW; ++g) {
+        const uint16_t* p = a.PT + (size_t)((jw * JGW + g) * 16 + l16) * a.Mp + ks * O_KS + 8 * lg;
+#pragma unroll
+        for (int n = 0; n < NP; ++n)
+          ap[i][g][n] = ks < nks ? *reinterpret_cast<const uint4*>(p + n * (size_t)a.RP * a.Mp) : uint4{0, 0, 0, 0};
+      }
+    }
+  };
+  load_p(0);
+  store(0);
+  if (nst > 1) load(1);
+  __syncthreads();
+  for (int st = 0; st < nst; ++st) {
+    if (st > 0) load_p(st);
+#pragma unroll
+    for (int i = 0; i < SS; ++i) {
+      uint4 bq[4];  // column 16 s + l16, rows 8 lg ... + 7 of the slab
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const uint16_t* q = &qs[st & 1][(i * SW + sw) * O_KS + 8 * lg][s * 16 + l16];
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = (uint32_t)q[2 * e * W_LD] | ((uint32_t)q[(2 * e + 1) * W_LD] << 16);
+        bq[s] = uint4{w[0], w[1], w[2], w[3]};
+      }
+#pragma unroll
+      for (int g = 0; g < JGW; ++g)
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+          for (int n = 0; n < NP; ++n) acc[g][s] = mfma16(ap[i][g][n], bq[s], acc[g][s]);
+    }
+    if (st + 1 < nst) {
+      store((st + 1) & 1);
+      if (st + 2 < nst) load(st + 2);
+    }
+    __syncthreads();
+  }
+  if constexpr (SW > 1) {
+    f32x4_t* red = reinterpret_cast<f32x4_t*>(&qs[0][0][0]);  // [4][JGW][4][64]
+    static_assert(4 * JGW * 4 * 64 * 16 <= (int)sizeof(qs), "the sums of the waves");
+#pragma unroll
+    for (int g = 0; g < JGW; ++g)
+#pragma unroll
+      for (int s = 0; s < 4; ++s) red[((wave * JGW + g) * 4 + s) * 64 + lane] = acc[g][s];
+    __syncthreads();
+    if (sw > 0) return;
+#pragma unroll
+    for (int g = 0; g < JGW; ++g)
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int w = 1; w < SW; ++w) acc[g][s] += red[(((w * JW + jw) * JGW + g) * 4 + s) * 64 + lane];
+  }
+#pragma unroll
+  for (int s = 0; s < 4; ++s) {
+    const int c = c0 + s * 16 + l16;
+    if (c >= a.C) continue;
+#pragma unroll
+    for (int g = 0; g < JGW; ++g)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int j = (jw * JGW + g) * 16 + 4 * lg + e;
+        if (j < a.r) a.out[a.jc ? (size_t)j * a.C + c : (size_t)c * a.r + j] = acc[g][s][e];
+      }
+  }
+}
+
+template <int RP>
+__global__ __launch_bounds__(O_WAVES * 64) void lora_outer_whole_kernel(OuterArgs o0, int n0, OuterArgs o1) {
+  const int b = blockIdx.x;
+  if (b < n0)
+    outer_whole<RP>(o0, b);
+  else
+    outer_whole<RP>(o1, b - n0);
+}
+
+// Whether the outer products take all rows in one workgroup.  The backward over an 8-bit
+// weight, us in chunks and in one: 250 x 8192 x 2048 at rank 128 68.0 and 61.9, 128 x 4096 x
+// 4096 at 128 52.4 and 44.0, 64 x 4096 x 4096 at 16 30.3 and 28.2, 300 x 11008 x 4096 at 64 85.5 and
+// 77.4, 512 x 4096 x 4096 at 16, 64, 128 48.6, 59.6, 73.4 and 47.8, 59.6, 73.1, 1000 x 2048 x 2048 at
+// 128 66.3 and 83.4.  (Two planes keep their chunks, and with them their bits.)
+bool outer_in_one(int M, int planes) { return planes == 3 && M <= 512; }
+
 // Rows per chunk and number of chunks of the outer products over M rows and
 // C columns: enough chunks for about O_TARGET_WG workgroups, each chunk a
 // multiple of O_KS rows and at least O_MIN_ROWS (by which chunk the sums are joined
@@ -283,31 +409,34 @@ OuterArgs outer_job(const uint16_t* PT, const uint16_t* Q, int M, int C, int rp,
                     float* out, bool jc, int& parts, int& finishes) {
   OuterArgs o{PT, Q, part, out, M, padded_rows(M), C, rp, r, 0, 0, jc ? 1 : 0, (C + O_COLS - 1) / O_COLS};
   outer_chunks(M, C, planes, o.mch, o.nch);
-  parts = o.tiles * o.nch;
+  parts = outer_in_one(M, planes) ? (C + W_COLS - 1) / W_COLS : o.tiles * o.nch;
   finishes = (int)(((size_t)r * C + 255) / 256);
   return o;
 }
 
 template <int RP>
-void launch_outer_rp(const OuterArgs& o0, int p0, const OuterArgs& o1, int p1, int planes, hipStream_t stream) {
+void launch_outer_rp(const OuterArgs& o0, int p0, const OuterArgs& o1, int p1, int M, int planes,
+                     hipStream_t stream) {
   const dim3 grid(p0 + p1), block(O_WAVES * 64);
-  if (planes == 3)
+  if (outer_in_one(M, planes))
+    hipLaunchKernelGGL((lora_outer_whole_kernel<RP>), grid, block, 0, stream, o0, p0, o1);
+  else if (planes == 3)
     hipLaunchKernelGGL((lora_outer_part_kernel<RP, 3>), grid, block, 0, stream, o0, p0, o1);
   else
     hipLaunchKernelGGL((lora_outer_part_kernel<RP, 2>), grid, block, 0, stream, o0, p0, o1);
 }
 
 hipError_t launch_outer(const OuterArgs& o0, int p0, int f0, const OuterArgs& o1, int p1, int f1, int rp,
-                        int planes, hipStream_t stream) {
+                        int M, int planes, hipStream_t stream) {
   switch (rp) {
-    case 16: launch_outer_rp<16>(o0, p0, o1, p1, planes, stream); break;
-    case 32: launch_outer_rp<32>(o0, p0, o1, p1, planes, stream); break;
-    case 64: launch_outer_rp<64>(o0, p0, o1, p1, planes, stream); break;
-    case 128: launch_outer_rp<128>(o0, p0, o1, p1, planes, stream); break;
+    case 16: launch_outer_rp<16>(o0, p0, o1, p1, M, planes, stream); break;
+    case 32: launch_outer_rp<32>(o0, p0, o1, p1, M, planes, stream); break;
+    case 64: launch_outer_rp<64>(o0, p0, o1, p1, M, planes, stream); break;
+    case 128: launch_outer_rp<128>(o0, p0, o1, p1, M, planes, stream); break;
     default: return hipErrorInvalidValue;
   }
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || outer_in_one(M, planes)) return e;
   hipLaunchKernelGGL(lora_outer_finish_kernel, dim3(f0 + f1), dim3(256), 0, stream, o0, f0, o1);
   return hipGetLastError();
 }
@@ -457,7 +586,7 @@ hipError_t launch_lora_backward(const BackwardArgs& a, void* ws, hipStream_t str
   if (a.dB)
     o1 = outer_job(tt.tT, a.dy, a.M, a.N, rp, a.r, a.planes, reinterpret_cast<float*>(w + l.opb), a.dB, false, p1, f1);
   if (p0 + p1 > 0)
-    if ((e = launch_outer(o0, p0, f0, o1, p1, f1, rp, a.planes, stream)) != hipSuccess) return e;
+    if ((e = launch_outer(o0, p0, f0, o1, p1, f1, rp, a.M, a.planes, stream)) != hipSuccess) return e;
   return hipSuccess;
 }
 
