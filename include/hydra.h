@@ -902,7 +902,7 @@ hydra_status hydra_verify_drafts_workspace_bytes(int64_t n, int64_t k, int64_t V
  * Exponentials and sums are 64-bit, in a fixed order (e^-700 of the largest of a row and
  * less count as 0); where rounding leaves nothing of p_a - q_a, the next token is drawn
  * from p_a.  Requires n >= 1, 0 <= k <= HYDRA_MAX_DRAFTS,
- * n (k + 1) <= 2^20, 1 <= V <= 2^21, n (2 k + 1) ceil(V / 4096) < 2^24, ld <= 2^31 - 1; logits at their
+ * n (k + 1) <= 2^20, 1 <= V <= 2^21, n (2 k + 1) ceil(V / 2048) < 2^24, ld <= 2^31 - 1; logits at their
  * element's alignment; outputs distinct (HYDRA_ERR_SHAPE).  Calls that share a workspace on
  * different streams race.
  */

@@ -1415,8 +1415,8 @@ namespace {
 hydra_status verify_shape(int64_t n, int64_t k, int64_t V) {
   if (n < 1 || k < 0 || k > HYDRA_MAX_DRAFTS || V < 1 || V > kMaxCols || n > kMaxRows || n * (k + 1) > kMaxRows)
     return HYDRA_ERR_SHAPE;
-  // (one dispatch of 256 threads a row and 4096 logits)
-  return n * (2 * k + 1) * ((V + 4095) / 4096) < (int64_t(1) << 24) ? HYDRA_OK : HYDRA_ERR_SHAPE;
+  // (one dispatch of 256 threads a row and 2048 logits)
+  return n * (2 * k + 1) * ((V + 2047) / 2048) < (int64_t(1) << 24) ? HYDRA_OK : HYDRA_ERR_SHAPE;
 }
 
 }  // namespace

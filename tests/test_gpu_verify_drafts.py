@@ -59,7 +59,8 @@ class Case:
 
 
 @pytest.mark.parametrize("n,k,V", [(1, 0, 1), (1, 1, 1), (3, 2, 2), (2, 5, 1000), (5, 3, 4096), (3, 7, 4097), (2, 4, 8191),
-                                   (1, 5, 32000), (2, 3, 50272), (40, 1, 300), (1, 128, 64), (2, 1, 70001)])
+                                   (1, 5, 32000), (2, 3, 50272), (40, 1, 300), (1, 128, 64), (2, 1, 70001), (4, 2, 2048), (3, 3, 2049),
+                                   (1, 2, 140001), (1, 1, 300000)])
 @pytest.mark.parametrize("draft", [True, False])
 def test_verify(dev, n, k, V, draft):
     say("verify", n, k, V, draft)
