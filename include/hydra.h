@@ -825,6 +825,9 @@ hydra_status hydra_fp8_lora_linear_backward_workspace_bytes(int64_t M, int64_t N
  *   workspace, workspace_bytes  device, 16-byte aligned, at least
  *            hydra_fp8_lora_linear_backward_workspace_bytes(M, N, K, r) bytes,
  *            contents ignored and overwritten
+ * dx: into fp32 every product of the base is exact and added in fp32, into bf16 the
+ * 8-bit matrix instructions run at every M; its update enters as two bf16 parts of s (dy B)
+ * (2^-17 of it).  dA and dB take 24 bits of s (dy B) and s (xa A^T).
  * The quantized x of the forward's base product counts as x itself (its
  * rounding has no gradient).  Requires N and K multiples of 16, other limits as in
  * hydra_fp8_lora_linear with N and K exchanged.  At least one output

@@ -92,6 +92,7 @@ struct OuterArgs {
   int mch, nch;        // rows per chunk (multiple of O_KS), chunks
   int jc;              // partials and output j-major
   int tiles;           // column tiles of O_COLS
+  int vec;             // outer_whole: [C x r] outputs in 16-byte stores
 };
 
 // Partial out[j][c] = sum_m P[m][j] Q[m][c] over the rows of one chunk, for
@@ -362,12 +363,16 @@ __device__ __forceinline__ void outer_whole(const OuterArgs& a, int b) {
     const int c = c0 + s * 16 + l16;
     if (c >= a.C) continue;
 #pragma unroll
-    for (int g = 0; g < JGW; ++g)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int j = (jw * JGW + g) * 16 + 4 * lg + e;
-        if (j < a.r) a.out[a.jc ? (size_t)j * a.C + c : (size_t)c * a.r + j] = acc[g][s][e];
+    for (int g = 0; g < JGW; ++g) {
+      const int j = (jw * JGW + g) * 16 + 4 * lg;
+      if (a.vec) {
+        if (j < a.r) *reinterpret_cast<f32x4_t*>(a.out + (size_t)c * a.r + j) = acc[g][s];
+        continue;
       }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (j + e < a.r) a.out[a.jc ? (size_t)(j + e) * a.C + c : (size_t)c * a.r + j + e] = acc[g][s][e];
+    }
   }
 }
 
@@ -381,9 +386,9 @@ __global__ __launch_bounds__(O_WAVES * 64) void lora_outer_whole_kernel(OuterArg
 }
 
 // Whether the outer products take all rows in one workgroup.  The backward over an 8-bit
-// weight, us in chunks and in one: 250 x 8192 x 2048 at rank 128 68.0 and 61.9, 128 x 4096 x
-// 4096 at 128 52.4 and 44.0, 64 x 4096 x 4096 at 16 30.3 and 28.2, 300 x 11008 x 4096 at 64 85.5 and
-// 77.4, 512 x 4096 x 4096 at 16, 64, 128 48.6, 59.6, 73.4 and 47.8, 59.6, 73.1, 1000 x 2048 x 2048 at
+// weight, us in chunks and in one: 250 x 8192 x 2048 at rank 128 68.0 and 58.0, 128 x 4096 x
+// 4096 at 128 52.4 and 42.6, 64 x 4096 x 4096 at 16 30.3 and 28.3, 300 x 11008 x 4096 at 64 85.5 and
+// 76.1, 512 x 4096 x 4096 at 16, 64, 128 48.6, 59.6, 73.4 and 48.0, 58.9, 71.4, 1000 x 2048 x 2048 at
 // 128 66.3 and 83.4.  (Two planes keep their chunks, and with them their bits.)
 bool outer_in_one(int M, int planes) { return planes == 3 && M <= 512; }
 
@@ -408,6 +413,7 @@ int padded_rows(int M) { return (M + O_KS - 1) / O_KS * O_KS; }
 OuterArgs outer_job(const uint16_t* PT, const uint16_t* Q, int M, int C, int rp, int r, int planes, float* part,
                     float* out, bool jc, int& parts, int& finishes) {
   OuterArgs o{PT, Q, part, out, M, padded_rows(M), C, rp, r, 0, 0, jc ? 1 : 0, (C + O_COLS - 1) / O_COLS};
+  o.vec = !jc && r % 4 == 0 && (reinterpret_cast<uintptr_t>(out) & 15) == 0;
   outer_chunks(M, C, planes, o.mch, o.nch);
   parts = outer_in_one(M, planes) ? (C + W_COLS - 1) / W_COLS : o.tiles * o.nch;
   finishes = (int)(((size_t)r * C + 255) / 256);

@@ -16,6 +16,8 @@
 //    sequence forms them itself), the accepted tokens, and what the distribution of
 //    the next token has in every segment;
 //  * verify_sample_kernel: the segment in which the sample lies, and its place.
+// 1 sequence of 5 drafts, V 32000, 16 us: three launches of dependent steps; 64 of up to 7,
+// V 50272, 52 us: some 30 of them for the sums over 26 million logits.
 #include "hydra_elem.h"
 
 namespace hydra {
