@@ -169,15 +169,14 @@ __global__ __launch_bounds__(256) void fp8_t_finish_kernel(Fp8PrepArgs g, int lr
 
 // ------------------------------------------------------------------ few rows
 
-
 // 16 NB rows of W a workgroup, the blocks of K dealt to its waves; their partial
 // sums meet in LDS in wave order.  U blocks a wave are requested before the first
-// is used.
+// is used (two of them and three workgroups a CU: 0 to 15% slower).
 template <int NB, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, 4) void fp8_stream_kernel(Fp8LinearArgs a) {
   constexpr int U = 4, NT = WAVES * 64;
   __shared__ f32x4_t red[WAVES][NB][64];
-  __shared__ float T[16][132];
+  __shared__ __align__(16) float T[16][132];
   __shared__ uint16_t Bs[16 * NB][130];
   const int t = threadIdx.x, lane = t & 63, l16 = lane & 15, lg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
