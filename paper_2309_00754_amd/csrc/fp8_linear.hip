@@ -24,6 +24,7 @@
 #include <type_traits>
 
 #include "hydra_fp8.h"
+#include "hydra_fp8_plan.h"
 #include "hydra_philox.h"
 
 namespace hydra {
@@ -32,8 +33,6 @@ namespace {
 // ------------------------------------------------------------------ before the product
 
 constexpr int P_WAVES = 8;
-constexpr int kFewRows = 16;
-constexpr int kStagedChunks = 8;  // most partial sums of T at padded rank 16 above kFewRows rows
 
 // Four values as bf16 and, in bf16 too, what that leaves of them.
 __device__ __forceinline__ void two_parts(const f32x4_t& v, uint2& hi, uint2& lo) {
@@ -909,94 +908,34 @@ hipError_t launch_tile(GemmArgs& g, hipStream_t stream) {
   return launch_masked<G, WHOLE>(g, stream);
 }
 template <class G>
-hipError_t launch_split(GemmArgs& g, int nsplit, hipStream_t stream) {
-  g.per = ((g.a.K + G::BK - 1) / G::BK + nsplit - 1) / nsplit;
-  g.nsplit = ((g.a.K + G::BK - 1) / G::BK + g.per - 1) / g.per;
+hipError_t launch_split(GemmArgs& g, const Fp8Plan& p, hipStream_t stream) {
+  if (p.split_values(g.a.M, g.a.N) * 4 > g.a.split_bytes) return hipErrorInvalidValue;
+  g.per = p.per;
+  g.nsplit = p.nsplit;
   const hipError_t e = launch_phase<G, false, PART>(g, stream);
   if (e != hipSuccess) return e;
   return launch_masked<Tile<G::WIDE, 32, 64, 32, 64, 1, 128, 2, 2>, JOIN>(g, stream);
 }
-
-// The tile by a model of its time: base + fixed w + K / 128 (step w + pair r), us, for w
-// workgroups a CU one after the other (pair: in r rounds of two together).  The
-// numbers are fits to 15 row counts from 17 to 4096 and eight (N, K) from 1000 x 688
-// to 11008 x 4096 and 4096 x 11008 (rms error 5 to 11%).  They choose the best of the six
-// tiles or one 0.4% slower on average, 9% at most.  What they say: a small tile's
-// slab costs its copies (32 to 50 GB/s into a CU), the largest one's its products.
-// us, M x N x K into bf16 and fp32: 64 x 4096 x 4096 10.0 and 11.5, 333 x 4096 x
-// 11008 37 and 48, 1000 x 4096 x 4096 24 and 37, 2048 x 4096 x 4096 38 and 60.
-struct TileCost {
-  int tm, tn;
-  float base, fixed, step, pair;
-};
-constexpr TileCost kTiles[2][6] = {{{128, 256, 0.f, 5.8f, 0.767f, 0.f},
-                                    {128, 128, 0.f, 4.99f, 0.516f, 0.f},
-                                    {64, 128, 0.1f, 4.19f, 0.376f, 0.f},
-                                    {64, 64, 2.47f, 1.23f, 0.136f, 0.143f},
-                                    {32, 64, 1.98f, 1.93f, 0.219f, 0.f},
-                                    {32, 32, 3.36f, 0.5f, 0.084f, 0.095f}},
-                                   {{128, 256, 0.f, 6.42f, 1.318f, 0.f},
-                                    {128, 128, 0.f, 5.24f, 0.775f, 0.f},
-                                    {64, 128, 0.f, 4.56f, 0.542f, 0.f},
-                                    {64, 64, 2.16f, 1.58f, 0.182f, 0.195f},
-                                    {32, 64, 1.57f, 2.23f, 0.272f, 0.f},
-                                    {32, 32, 2.9f, 0.72f, 0.067f, 0.165f}}};
-
-// K in parts (tiles 0, 1, 2 and 4): few rows and a long K leave CUs without a tile.  The
-// parts' sums go through memory, and a second launch joins them, for 3.9 us and the
-// sums written and read at 6.75 TB/s (a fit to 330 cases, rms error 9%).  us, whole ->
-// in parts, fp32: 17 x 2048 x 8192 17.9 -> 11.4, 64 x 4096 x 11008 25.3 -> 21.8, 200 x 4096 x
-// 11008 38.6 -> 32.7; with tile 0 among them 333 x 4096 x 11008 59.3 -> 57.1 (bf16 51.2 ->
-// 47.8), rank 16 and x quantized in the call.  Below K = 4096 never faster.
-constexpr int kMaxSplit = 8, kMaxParts = 512;
-struct Plan {
-  int tile, nsplit;
-};
-Plan plan_of(bool wide, int M, int N, int K) {
-  Plan best{0, 1};
-  float least = 0.f;
-  for (int i = 0; i < 6; ++i) {
-    const TileCost& c = kTiles[wide][i];
-    const int64_t tiles = (int64_t)((M + c.tm - 1) / c.tm) * ((N + c.tn - 1) / c.tn);
-    const int slabs = (K + 127) / 128;
-    const bool may = (i <= 2 || i == 4) && tiles < 256;
-    for (int s = 1; s <= (may ? kMaxSplit : 1) && s * 4 <= (s == 1 ? 4 : slabs); ++s) {
-      const int64_t n = tiles * s;
-      if (s > 1 && n > kMaxParts) break;
-      const float w = (float)((n + 255) / 256), r = (float)((n + 511) / 512), sl = (float)((slabs + s - 1) / s);
-      float us = c.base + c.fixed * w + sl * (c.step * w + c.pair * r);
-      if (s > 1) us += 3.9f + (float)s * 8.f * (float)M * (float)N / 6.75e6f;
-      if ((i == 0 && s == 1) || us < least) {
-        least = us;
-        best = Plan{i, s};
-      }
-    }
+template <class G, int I>
+hipError_t launch_planned(GemmArgs& g, const Fp8Plan& p, hipStream_t stream) {
+  constexpr Fp8TileCost c = kFp8TileCosts[G::WIDE][I];
+  static_assert(G::TM == c.tm && G::TN == c.tn && G::BK == c.bk, "the tile that the plan is of");
+  if constexpr (c.parts) {
+    if (p.nsplit > 1) return launch_split<G>(g, p, stream);
   }
-  return best;
+  return launch_tile<G>(g, stream);
 }
 
 template <bool WIDE>
 hipError_t launch_rows(GemmArgs& g, hipStream_t stream) {
-  const Plan p = plan_of(WIDE, g.a.M, g.a.N, g.a.K);
-  using T0 = Tile<WIDE, 128, 256, 64, 128, 1, 128, 3>;
-  using T1 = Tile<WIDE, 128, 128, 64, 64, 2, 128, 4>;
-  using T2 = Tile<WIDE, 64, 128, 64, 64, 2, 128, 6>;
-  using T4 = Tile<WIDE, 32, 64, 32, 64, 4, 256, 6>;
-  if (p.nsplit > 1) {
-    switch (p.tile) {
-      case 0: return launch_split<T0>(g, p.nsplit, stream);
-      case 1: return launch_split<T1>(g, p.nsplit, stream);
-      case 2: return launch_split<T2>(g, p.nsplit, stream);
-      default: return launch_split<T4>(g, p.nsplit, stream);
-    }
-  }
+  const Fp8Plan p = fp8_plan(WIDE, g.a.M, g.a.N, g.a.K);
   switch (p.tile) {
-    case 0: return launch_tile<T0>(g, stream);
-    case 1: return launch_tile<T1>(g, stream);
-    case 2: return launch_tile<T2>(g, stream);
-    case 3: return launch_tile<Tile<WIDE, 64, 64, 32, 64, 2, 128, 4, 2>>(g, stream);
-    case 4: return launch_tile<T4>(g, stream);
-    default: return launch_tile<Tile<WIDE, 32, 32, 32, 32, 4, 256, 4, 2>>(g, stream);
+    case 0: return launch_planned<Tile<WIDE, 128, 256, 64, 128, 1, 128, 3>, 0>(g, p, stream);
+    case 1: return launch_planned<Tile<WIDE, 128, 128, 64, 64, 2, 128, 4>, 1>(g, p, stream);
+    case 2: return launch_planned<Tile<WIDE, 64, 128, 64, 64, 2, 128, 6>, 2>(g, p, stream);
+    case 3: return launch_planned<Tile<WIDE, 64, 64, 32, 64, 2, 128, 4, 2>, 3>(g, p, stream);
+    case 4: return launch_planned<Tile<WIDE, 32, 64, 32, 64, 4, 256, 6>, 4>(g, p, stream);
+    default: return launch_planned<Tile<WIDE, 32, 32, 32, 32, 4, 256, 4, 2>, 5>(g, p, stream);
   }
 }
 
@@ -1017,28 +956,6 @@ void launch_prep(const Fp8PrepArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-// A tile's partial sums of T at a high rank are many, and another launch pays that adds
-// them up once.  us without and with it: 2048 x 11008 x 4096 at rank 128 into bf16 198.6 and
-// 161.6, 1024 x 4096 x 4096 64.7 and 53.4, 250 x 2048 x 8192 46.8 and 37.4, 40 x 1024 x 1024 17.8 and
-// 19.2; 2048 x 4096 x 4096 at 64 64.0 and 60.9, 512 38.9 and 38.3, 64 21.9 and 22.8; 2048 at 32
-// 54.3 and 53.8, 512 33.9 and 35.1.
-bool fp8_finishes_t(int M, int rp) { return rp > 16 && M > kFewRows && (int64_t)M * rp >= 24576; }
-// Chunks of K: about 512 workgroups, each at least a block a wave (few rows at a rank
-// above 16: fewer, as A's rows take the time; 1 x 4096 x 4096 at rank 128 18.1 -> 13.6 us, 8 x
-// 8192 x 4096 at 64 19.7 -> 17.9), and no more partial sums of T than the product can
-// add up on the side.  2048 x 4096 at rank 16 takes 8.5 to 9.1 us with 256, 512, 768 or
-// 1024 workgroups and with 4, 8 or 16 waves.
-void fp8_prep_chunks(int M, int K, int rp, int& nch, int& kch) {
-  const int kb = (K + kFp8Block - 1) / kFp8Block, mb = (M + 15) / 16;
-  int want = (512 + mb - 1) / mb;
-  const int most = rp == 0 ? 64 : M <= kFewRows ? 32 : rp <= 32 || fp8_finishes_t(M, rp) ? kStagedChunks : 4;
-  want = want < most ? want : most;
-  kch = (kb + want - 1) / want;
-  const int least = M <= kFewRows && rp > 16 ? 256 / rp : P_WAVES;
-  kch = kch < least ? least : kch;
-  nch = (kb + kch - 1) / kch;
-}
-
 hipError_t launch_fp8_prep(const Fp8PrepArgs& a, hipStream_t stream) {
   switch (a.A ? a.rp : 0) {
     case 0: launch_prep<0>(a, stream); break;
@@ -1053,19 +970,6 @@ hipError_t launch_fp8_prep(const Fp8PrepArgs& a, hipStream_t stream) {
   const size_t blocks = ((size_t)a.M * a.rp / 4 + 255) / 256;
   hipLaunchKernelGGL(fp8_t_finish_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, a, 31 - __builtin_clz(a.rp));
   return hipGetLastError();
-}
-
-size_t fp8_split_most(int M, int N, int K) {
-  if (K <= 128 * 7) return 0;
-  const size_t all = (size_t)kMaxSplit * M * N, parts = (size_t)kMaxParts * 128 * 128;
-  return (all < parts ? all : parts) * 4;
-}
-size_t fp8_prep_most(int M, int rp) {
-  if (rp == 0) return 0;
-  const size_t few = (size_t)32 * (M < kFewRows ? M : kFewRows);
-  const size_t by_rows = (size_t)kStagedChunks * M, by_grid = (size_t)(512 + 1) * 16 + M;
-  const size_t many = M <= kFewRows ? 0 : by_rows < by_grid ? by_rows : by_grid;
-  return (few > many ? few : many) * rp * 4;
 }
 
 hipError_t launch_fp8_linear(const Fp8LinearArgs& a, hipStream_t stream) {

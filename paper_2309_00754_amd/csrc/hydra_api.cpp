@@ -8,6 +8,7 @@
 #include <algorithm>
 #include <mutex>
 
+#include "hydra_fp8_plan.h"
 #include "hydra_internal.h"
 
 namespace {
@@ -1260,7 +1261,8 @@ hydra_status hydra_fp8_lora_linear(const uint16_t* x, const uint16_t* x_adapter,
   hydra::fp8_prep_chunks(int(M), int(K), rp, nch, kch);
   const size_t rows = xq ? 0 : fp8_rows_bytes(M, K), part = up256(hydra::fp8_prep_most(int(M), rp));
   const size_t ts_bytes = hydra::fp8_finishes_t(int(M), rp) ? up256((size_t)M * 2 * rp * 2) : 0;
-  const size_t need = rows + part + ts_bytes + up256(hydra::fp8_split_most(int(M), int(N), int(K)));
+  const size_t split = up256(hydra::fp8_split_most(int(M), int(N), int(K)));
+  const size_t need = rows + part + ts_bytes + split;
   if (need > 0) {
     if (!workspace) return HYDRA_ERR_NULL;
     if (workspace_bytes < need) return HYDRA_ERR_WORKSPACE;
@@ -1304,6 +1306,7 @@ hydra_status hydra_fp8_lora_linear(const uint16_t* x, const uint16_t* x_adapter,
   a.part = p.part;
   a.ts = p.ts;
   a.split = reinterpret_cast<float*>(w + rows + part + ts_bytes);
+  a.split_bytes = split;
   a.nch = nch;
   a.B = B;
   a.ldb = int(r);
@@ -1355,6 +1358,7 @@ hydra_status hydra_fp8_lora_linear_backward(const uint16_t* x, const uint8_t* Wq
   g.xq = w;
   g.xs = w + up256((size_t)M * N);
   g.split = reinterpret_cast<float*>(w + rows);
+  g.split_bytes = split;
   g.wq = Wqt;
   g.ws = wt_scale;
   g.M = int(M);

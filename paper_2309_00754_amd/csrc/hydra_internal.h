@@ -314,12 +314,9 @@ struct Fp8LinearArgs {
   uint32_t drop;
   float keep;
   const uint64_t* rng;
-  float* split;        // fp8_split_most(M, N, K) of room
+  float* split;        // room for the sums of parts of K
+  size_t split_bytes;  // ... of this size: fp8_split_most(M, N, K)
 };
-// Room that any call with up to M rows can do with: for partial sums of the base product
-// (0 where K is never split), and of T.
-size_t fp8_split_most(int M, int N, int K);
-size_t fp8_prep_most(int M, int rp);
 // What the linear needs before its product: x quantized (x nullptr: not), and the
 // partial sums of T = xa A^T (A nullptr: not).
 struct Fp8PrepArgs {
@@ -334,9 +331,6 @@ struct Fp8PrepArgs {
   float s;
   uint16_t* ts;        // [M][2 rp] bf16 hi | lo of s T, or nullptr (fp8_finishes_t)
 };
-// Whether the product takes s T as ts, else the partial sums.
-bool fp8_finishes_t(int M, int rp);
-void fp8_prep_chunks(int M, int K, int rp, int& nch, int& kch);
 hipError_t launch_fp8_prep(const Fp8PrepArgs& a, hipStream_t stream);
 hipError_t launch_fp8_linear(const Fp8LinearArgs& a, hipStream_t stream);
 

@@ -21,6 +21,7 @@
 #include <algorithm>
 
 #include "hydra_device.h"
+#include "hydra_fp8_plan.h"
 #include "hydra_internal.h"
 
 namespace hydra {
