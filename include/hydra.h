@@ -757,7 +757,7 @@ hydra_status hydra_grad_clip(int64_t n, const void* const* grads, const int32_t*
  *   scale_t  [ceil(K / 128) x ceil(M / 128)] bytes   out, NULL iff qt is: scale transposed
  * Values below 2^-10 of the scale become 0; NaN and infinities become NaN and
  * do not count for the scale.  Requires 1 <= M, K <= 2^21 (no multiple of
- * anything) and M ceil(K / 128) < 2^28, or ceil(M / 128) ceil(K / 128) < 2^24;
+ * anything) and M ceil(K / 128) <= 2^28 - 16, or ceil(M / 128) ceil(K / 128) < 2^24;
  * x at its element's alignment (K % 8 == 0 and 16-byte aligned: faster).
  * HYDRA_ERR_UNSUPPORTED for another block_rows, or qt with block_rows 1.
  */

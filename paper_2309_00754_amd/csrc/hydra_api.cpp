@@ -1205,9 +1205,9 @@ hydra_status hydra_fp8_quantize(const void* x, hydra_dtype x_type, int64_t M, in
   if (block_rows != 1 && block_rows != 128) return HYDRA_ERR_UNSUPPORTED;
   if (qt && block_rows != 128) return HYDRA_ERR_UNSUPPORTED;
   if (M < 1 || M > kMaxCols || K < 1 || K > kMaxK) return HYDRA_ERR_SHAPE;
-  // (one dispatch: 16 lanes a block of 128 values, 256 a block of 128 x 128)
-  if (block_rows == 1 ? M * blocks128(K) >= (int64_t(1) << 28) : blocks128(M) * blocks128(K) >= (int64_t(1) << 24))
-    return HYDRA_ERR_SHAPE;
+  // (one dispatch: workgroups of 256 threads for 16 blocks of 128 values, or for one of 128 x 128)
+  const int64_t groups = block_rows == 1 ? (M * blocks128(K) + 15) / 16 : blocks128(M) * blocks128(K);
+  if (groups >= (int64_t(1) << 24)) return HYDRA_ERR_SHAPE;
   const void* const outs[4] = {q, scale, qt, scale_t};
   const void* const ins[1] = {x};
   if (!distinct(outs, ins)) return HYDRA_ERR_SHAPE;
