@@ -729,7 +729,7 @@ bool backward_shape_ok(int64_t M, int64_t N, int64_t K, int64_t r) {
 hydra_status hydra_lora_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t r, size_t* bytes) {
   if (!bytes) return HYDRA_ERR_NULL;
   if (!backward_shape_ok(M, N, K, r)) return HYDRA_ERR_SHAPE;
-  *bytes = hydra::backward_ws_bytes(int(M), int(N), int(K), hydra::padded_rank(int(r)), 2);
+  *bytes = hydra::backward_ws_bytes(int(M), int(N), int(K), hydra::padded_rank(int(r)), 2, 0);
   return HYDRA_OK;
 }
 
@@ -745,7 +745,7 @@ hydra_status hydra_lora_linear_backward(const uint16_t* x, const uint16_t* Wt, c
   if (!aligned(dy, 16) || (x && !aligned(x, 16)) || (dx && !aligned(Wt, 16))) return HYDRA_ERR_ALIGN;
   if (r > 0 && (!aligned(A, 16) || !aligned(B, 2))) return HYDRA_ERR_ALIGN;
   if ((dx && !aligned(dx, 4)) || (dA && !aligned(dA, 4)) || (dB && !aligned(dB, 4))) return HYDRA_ERR_ALIGN;
-  const size_t need = hydra::backward_ws_bytes(int(M), int(N), int(K), hydra::padded_rank(int(r)), 2);
+  const size_t need = hydra::backward_ws_bytes(int(M), int(N), int(K), hydra::padded_rank(int(r)), 2, 0);
   if (need > 0) {
     if (!workspace) return HYDRA_ERR_NULL;
     if (workspace_bytes < need) return HYDRA_ERR_WORKSPACE;
@@ -1318,8 +1318,8 @@ hydra_status hydra_fp8_lora_linear_backward_workspace_bytes(int64_t M, int64_t N
   const hydra_status chk = fp8_shape(M, K, N, r);
   if (chk != HYDRA_OK) return chk;
   if (K % 16 != 0) return HYDRA_ERR_SHAPE;
-  *bytes = fp8_rows_bytes(M, N) + up256(hydra::fp8_split_most(int(M), int(K), int(N))) +
-           hydra::backward_ws_bytes(int(M), int(N), int(K), hydra::padded_rank(int(r)), kFp8Planes);
+  *bytes = fp8_rows_bytes(M, N) + hydra::backward_ws_bytes(int(M), int(N), int(K), hydra::padded_rank(int(r)), kFp8Planes,
+                                                           hydra::fp8_split_most(int(M), int(K), int(N)));
   return HYDRA_OK;
 }
 
@@ -1348,8 +1348,8 @@ hydra_status hydra_fp8_lora_linear_backward(const uint16_t* x, const uint8_t* Wq
       !aligned(dx, type_align(dx_type)) || !aligned(dA, 4) || !aligned(dB, 4))
     return HYDRA_ERR_ALIGN;
   const int rp = hydra::padded_rank(int(r));
-  const size_t rows = fp8_rows_bytes(M, N), split = up256(hydra::fp8_split_most(int(M), int(K), int(N)));
-  const size_t need = rows + split + hydra::backward_ws_bytes(int(M), int(N), int(K), rp, kFp8Planes);
+  const size_t rows = fp8_rows_bytes(M, N), split = hydra::fp8_split_most(int(M), int(K), int(N));
+  const size_t need = rows + hydra::backward_ws_bytes(int(M), int(N), int(K), rp, kFp8Planes, split);
   if (!workspace) return HYDRA_ERR_NULL;
   if (workspace_bytes < need) return HYDRA_ERR_WORKSPACE;
   if (!aligned(workspace, 16)) return HYDRA_ERR_ALIGN;
@@ -1357,7 +1357,6 @@ hydra_status hydra_fp8_lora_linear_backward(const uint16_t* x, const uint8_t* Wq
   hydra::Fp8LinearArgs g{};
   g.xq = w;
   g.xs = w + up256((size_t)M * N);
-  g.split = reinterpret_cast<float*>(w + rows);
   g.split_bytes = split;
   g.wq = Wqt;
   g.ws = wt_scale;
@@ -1384,7 +1383,7 @@ hydra_status hydra_fp8_lora_linear_backward(const uint16_t* x, const uint8_t* Wq
   a.dB = dB;
   a.planes = kFp8Planes;
   a.base8 = dx ? &g : nullptr;
-  return from_hip(hydra::launch_lora_backward(a, w + rows + split, reinterpret_cast<hipStream_t>(stream)));
+  return from_hip(hydra::launch_lora_backward(a, w + rows, reinterpret_cast<hipStream_t>(stream)));
 }
 
 hydra_status hydra_dropout(const void* x, hydra_dtype x_type, const void* residual, hydra_dtype residual_type, double p,

@@ -387,12 +387,14 @@ struct BackwardArgs {
   float* dB;           // [N x r] or nullptr
   int planes;          // parts of s U and s T in dA and dB: 2 or 3
   // W in 8 bits: Wt and dx null, and what the product over it takes in their
-  // place (xq, xs: room for dy's; y_on: dx, of y_type; drop: the mask)
+  // place (xq, xs: room for dy's; y_on: dx, of y_type; drop: the mask; split_bytes: that of the
+  // workspace below)
   const Fp8LinearArgs* base8;
 };
-// Workspace bytes of the backward, and the launcher (which assumes a
+// Workspace bytes of the backward (split: fp8_split_most of dx's product over W in 8 bits,
+// else 0), and the launcher (which assumes a
 // workspace of at least that size, 16-byte aligned).
-size_t backward_ws_bytes(int M, int N, int K, int rp, int planes);
+size_t backward_ws_bytes(int M, int N, int K, int rp, int planes, size_t split);
 hipError_t launch_lora_backward(const BackwardArgs& a, void* ws, hipStream_t stream);
 // dst [Cp x Rp] bf16: dst[c][q] = src[q][c] for c < C, q < R (src [R x C]), else 0.
 hipError_t launch_transpose_pad(const uint16_t* src, int R, int C, uint16_t* dst, int Rp, int Cp, hipStream_t stream);

@@ -397,9 +397,8 @@ bool outer_in_one(int M, int planes) { return planes == 3 && M <= 512; }
 // C columns: enough chunks for about O_TARGET_WG workgroups, each chunk a
 // multiple of O_KS rows and at least O_MIN_ROWS (by which chunk the sums are joined
 // is part of the result: three planes have chunks of their own.  The backward over an
-// 8-bit weight, us with chunks of at least 128, 64, 32 rows: 250 x 8192 x 2048 at rank
-// 128 70.7, 66.8, 69.3; 1000 x 2048 x 2048 at 128 70.1, 66.8, 75.3; 512 x 4096 x 4096 at 64 63.1,
-// 61.2, 64.1; two planes and 128 rows 66.3, 64.0, 60.8).
+// 8-bit weight, us with chunks of at least 128, 64, 32 rows: 1000 x 2048 x 2048 at 128
+// 70.1, 66.8, 75.3; with two planes and 128 rows 64.0).
 void outer_chunks(int M, int C, int planes, int& mch, int& nch) {
   const int64_t tiles = (C + O_COLS - 1) / O_COLS;
   const int64_t want = std::max<int64_t>(1, (O_TARGET_WG + tiles - 1) / tiles);
@@ -452,10 +451,11 @@ hipError_t launch_outer(const OuterArgs& o0, int p0, int f0, const OuterArgs& o1
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
 struct BwdLayout {
-  size_t bt, at, tsu, uT, tT, tpart, tpart2, opa, opb, total;
+  size_t bt, at, tsu, uT, tT, tpart, tpart2, split, opa, opb, total;
 };
 
-BwdLayout layout(int M, int N, int K, int rp, int planes) {
+// (split: bytes for the partial sums of dx's product over an 8-bit weight)
+BwdLayout layout(int M, int N, int K, int rp, int planes, size_t split) {
   BwdLayout l{};
   size_t o = 0;
   l.bt = o;    o += up256((size_t)rp * N * 2);                      // B^T [RP x N] bf16
@@ -469,10 +469,12 @@ BwdLayout layout(int M, int N, int K, int rp, int planes) {
   int mch, nch_a, nch_b;
   outer_chunks(M, K, planes, mch, nch_a);
   outer_chunks(M, N, planes, mch, nch_b);
-  const size_t oa = (size_t)nch_a * rp * K, ob = (size_t)nch_b * rp * N;
-  l.opa = o;   o += up256(oa * 4);                                  // dA's outer-product partials
-  l.opb = o;   o += up256(ob * 4);                                  // dB's outer-product partials
-  l.total = o;
+  const bool one = outer_in_one(M, planes);  // (no partials)
+  const size_t oa = one ? 0 : (size_t)nch_a * rp * K, ob = one ? 0 : (size_t)nch_b * rp * N;
+  l.opa = o;                                                        // dA's outer-product partials
+  l.opb = o + up256(oa * 4);                                        // dB's outer-product partials
+  l.split = o;                                                      // dx's, which is there before them
+  l.total = o + std::max(up256(oa * 4) + up256(ob * 4), up256(split));
   return l;
 }
 
@@ -486,16 +488,19 @@ hipError_t launch_transpose_pad(const uint16_t* src, int R, int C, uint16_t* dst
   return hipGetLastError();
 }
 
-size_t backward_ws_bytes(int M, int N, int K, int rp, int planes) {
-  return rp == 0 ? 0 : layout(M, N, K, rp, planes).total;
+size_t backward_ws_bytes(int M, int N, int K, int rp, int planes, size_t split) {
+  return rp == 0 ? up256(split) : layout(M, N, K, rp, planes, split).total;
 }
 
 hipError_t launch_lora_backward(const BackwardArgs& a, void* ws, hipStream_t stream) {
   const int rp = padded_rank(a.r);
   hipError_t e;
+  uint8_t* const w = static_cast<uint8_t*>(ws);
+  const size_t split = a.base8 ? a.base8->split_bytes : 0;
   // dx over a weight in 8 bits: dy's bytes, then the product with its update
-  auto dx_over_8 = [&](const uint16_t* ts, const uint16_t* at) {
+  auto dx_over_8 = [&](const uint16_t* ts, const uint16_t* at, size_t split_at) {
     Fp8LinearArgs g = *a.base8;
+    g.split = reinterpret_cast<float*>(w + split_at);
     Fp8PrepArgs q{};
     q.x = q.xa = a.dy;
     q.M = a.M;
@@ -510,7 +515,7 @@ hipError_t launch_lora_backward(const BackwardArgs& a, void* ws, hipStream_t str
     g.r = g.rp = g.ldb = rp;
     return launch_fp8_linear(g, stream);
   };
-  if (rp == 0 && a.base8) return dx_over_8(nullptr, nullptr);
+  if (rp == 0 && a.base8) return dx_over_8(nullptr, nullptr, 0);
   if (rp == 0) {  // no adapter: dx = dy W only
     if (!a.dx) return hipSuccess;
     LinearArgs g{};
@@ -522,8 +527,7 @@ hipError_t launch_lora_backward(const BackwardArgs& a, void* ws, hipStream_t str
     g.y_off = a.dx;
     return launch_lora_gemm(g, stream);
   }
-  const BwdLayout l = layout(a.M, a.N, a.K, rp, a.planes);
-  uint8_t* w = static_cast<uint8_t*>(ws);
+  const BwdLayout l = layout(a.M, a.N, a.K, rp, a.planes, split);
   uint16_t* bt = reinterpret_cast<uint16_t*>(w + l.bt);
   uint16_t* at = reinterpret_cast<uint16_t*>(w + l.at);
   const bool want_dx = a.dx || a.base8;
@@ -572,7 +576,7 @@ hipError_t launch_lora_backward(const BackwardArgs& a, void* ws, hipStream_t str
   if (e != hipSuccess) return e;
   // 3. dx = dy W + s U A: the GEMM over W^T with slabs ([hi | lo](s U), A^T)
   if (a.base8) {
-    if ((e = dx_over_8(u.ts, at)) != hipSuccess) return e;
+    if ((e = dx_over_8(u.ts, at, l.split)) != hipSuccess) return e;
   } else if (a.dx) {
     LinearArgs g{};
     g.x = a.dy;
