@@ -793,8 +793,8 @@ hydra_status hydra_fp8_lora_linear_workspace_bytes(int64_t M, int64_t N, int64_t
  * fp32 up to 16 rows, above as two bf16 parts (2^-17 of s x A^T).  Outputs are
  * rounded once, to nearest even.  A scale byte 255 stands for NaN; a value whose bytes
  * stand for 2^128 (above 1.94 2^127 in x) counts as infinite where products are exact.
- * NaN and infinities in x make their row's outputs NaN.  With r == 0 y_on equals
- * y_off.  Requires 1 <= M <= 2^20, 1 <= N <= 2^21, 16 <= K <= 2^21, K % 16 == 0,
+ * NaN and infinities in x make their row's outputs NaN; in x_adapter alone they go
+ * through the update as fp32 takes them.  With r == 0 y_on equals y_off.  Requires 1 <= M <= 2^20, 1 <= N <= 2^21, 16 <= K <= 2^21, K % 16 == 0,
  * 0 <= r <= HYDRA_MAX_RANK, ceil(M / 128) ceil(N / 256) < 2^23; outputs distinct
  * (HYDRA_ERR_SHAPE).  Repeated calls give the same bits.  Calls that share a
  * workspace on different streams race.

@@ -145,7 +145,8 @@ __global__ __launch_bounds__(P_WAVES * 64) void fp8_prep_kernel(Fp8PrepArgs g) {
       float sum = red[0][row][j];
 #pragma unroll
       for (int w = 1; w < P_WAVES; ++w) sum += red[w][row][j];
-      g.part[((size_t)blockIdx.y * g.M + m0 + row) * RP + j] = sum;
+      // (an infinity times the zeros of a row that A does not have is no number)
+      g.part[((size_t)blockIdx.y * g.M + m0 + row) * RP + j] = j < g.r ? sum : 0.f;
     }
   }
 }
