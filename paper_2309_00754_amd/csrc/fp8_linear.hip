@@ -34,16 +34,25 @@ namespace {
 
 constexpr int P_WAVES = 8;
 
-// Four values as bf16 and, in bf16 too, what that leaves of them.
-__device__ __forceinline__ void two_parts(const f32x4_t& v, uint2& hi, uint2& lo) {
-  uint32_t h[4], l[4];
+// Two values as NP bf16 parts, a pair of each part.  Three add up to the values: the upper
+// half of their bits, that of what it leaves, and what is left then (at most eight bits).
+// Two, rounded, are within 2^-17 of them.  An infinity's other parts are zero.
+template <int NP>
+__device__ __forceinline__ void bf16_parts(float a, float b, uint32_t (&p)[NP]) {
+  const bool ia = __builtin_isinf(a), ib = __builtin_isinf(b);
+  if constexpr (NP == 2) {
+    p[0] = f32_to_bf16_pair(a, b);
+    p[1] = f32_to_bf16_pair(ia ? 0.f : a - __uint_as_float(p[0] << 16), ib ? 0.f : b - __uint_as_float(p[0] & 0xFFFF0000u));
+  } else {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    h[i] = f32_to_bf16_any(v[i]);
-    l[i] = (h[i] & 0x7FFF) < 0x7F80 ? f32_to_bf16_any(v[i] - bf16_to_f32(h[i])) : 0;  // (none of an infinity)
+    for (int n = 0; n < 3; ++n) {
+      const uint32_t ua = __float_as_uint(a), ub = __float_as_uint(b);
+      p[n] = __builtin_amdgcn_perm(ub, ua, 0x07060302u);
+      a -= __uint_as_float(ua & 0xFFFF0000u);
+      b -= __uint_as_float(ub & 0xFFFF0000u);
+      if (n == 0) a = ia ? 0.f : a, b = ib ? 0.f : b;
+    }
   }
-  hi = make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
-  lo = make_uint2(l[0] | l[1] << 16, l[2] | l[3] << 16);
 }
 
 // The pieces of four lanes 16 apart, transposed: v[j] of lane group g becomes v[g] of
@@ -151,20 +160,15 @@ __global__ __launch_bounds__(P_WAVES * 64) void fp8_prep_kernel(Fp8PrepArgs g) {
   }
 }
 
-// s T as its bf16 parts [M][hi rp | lo rp], which tiles at a rank above 16 read in place of
-// the chunks' sums: four values a thread.
-__global__ __launch_bounds__(256) void fp8_t_finish_kernel(Fp8PrepArgs g, int lrp) {
-  const size_t e = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4, all = (size_t)g.M << lrp;
+// s T, which tiles at a rank above 16 read in place of the chunks' sums: four values a
+// thread.
+__global__ __launch_bounds__(256) void fp8_t_finish_kernel(Fp8PrepArgs g) {
+  const size_t e = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4, all = (size_t)g.M * g.rp;
   if (e >= all) return;
   f32x4_t v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
   for (int c = 0; c < g.nch; ++c) v += *reinterpret_cast<const f32x4_t*>(g.part + c * all + e);
-  uint2 hi, lo;
-  two_parts(g.s * v, hi, lo);
-  const size_t row = e >> lrp;
-  uint16_t* const o = g.ts + (row << (lrp + 1)) + (e - (row << lrp));
-  *reinterpret_cast<uint2*>(o) = hi;
-  *reinterpret_cast<uint2*>(o + g.rp) = lo;
+  *reinterpret_cast<f32x4_t*>(g.ts + e) = g.s * v;
 }
 
 // ------------------------------------------------------------------ few rows
@@ -343,7 +347,7 @@ struct Tile {
   static constexpr int RD = STEP / 32;                 // 16-byte reads a lane and row in a step
   static constexpr int OLD = TN + 4;                   // row of the output tile in LDS (fp32, in values)
   static constexpr int OUT = KS * TM * OLD * 4;        // bytes of the KS partial sums of it
-  // rows of s T (hi | lo) and of B, 16 bytes apart from the next, at padded rank rp
+  // rows of s T (fp32) and of B, 16 bytes apart from the next, at padded rank rp
   static constexpr int lora_bytes(int rp) { return TM * (4 * rp + 16) + TN * (2 * rp + 16); }
   static constexpr size_t cmax(size_t x, size_t y) { return x > y ? x : y; }
   static constexpr int MASK = TM * TN / 8;             // bytes of dropout's mask, after the rest
@@ -512,17 +516,13 @@ __global__ __launch_bounds__(G::NT, G::NT / 256 * G::WPC) void fp8_gemm_kernel(G
         if (n0 + col + e < N) store_elem(y, w == 4 ? kF32 : kBf16, at + e, v[e]);
     }
   };
-  // The rows of s T as bf16 hi and lo parts (2^-17 of a value together) and those
-  // of B, zero padded to rp, to LDS.
-  const int rp = a.rp, lrp = 31 - __builtin_clz(rp | 1), ldt = 2 * rp + 8, ldb = rp + 8;  // (in values)
-  uint16_t* const Ts = reinterpret_cast<uint16_t*>(sm);
-  uint16_t* const Bs = Ts + TM * ldt;
+  // The rows of s T and those of B, zero padded to rp, to LDS.
+  const int rp = a.rp, lrp = 31 - __builtin_clz(rp | 1), ldt = rp + 4, ldb = rp + 8;  // (in values)
+  float* const Ts = reinterpret_cast<float*>(sm);
+  uint16_t* const Bs = reinterpret_cast<uint16_t*>(Ts + TM * ldt);
   // Four values of s T, of a tile's row.
   auto put_t = [&](int row, int j, const f32x4_t& v) __attribute__((always_inline)) {
-    uint2 hi, lo;
-    two_parts(a.s * v, hi, lo);
-    *reinterpret_cast<uint2*>(Ts + row * ldt + j) = hi;
-    *reinterpret_cast<uint2*>(Ts + row * ldt + rp + j) = lo;
+    *reinterpret_cast<f32x4_t*>(Ts + row * ldt + j) = v;
   };
   const int rows = min(TM, M - m0), cols = min(TN, N - n0);
   // By the 256 threads of the copy waves.  At padded rank 16, the usual one, the loads
@@ -558,7 +558,7 @@ __global__ __launch_bounds__(G::NT, G::NT / 256 * G::WPC) void fp8_gemm_kernel(G
       f32x4_t v = u.t[i][0];
 #pragma unroll
       for (int c = 1; c < kStagedChunks; ++c) v += u.t[i][c];
-      if (TM * 4 % 256 == 0 || e < TM * 4) put_t(e / 4, e % 4 * 4, v);
+      if (TM * 4 % 256 == 0 || e < TM * 4) put_t(e / 4, e % 4 * 4, a.s * v);
     }
 #pragma unroll
     for (int i = 0; i * 256 < TN * 2; ++i) {
@@ -569,11 +569,11 @@ __global__ __launch_bounds__(G::NT, G::NT / 256 * G::WPC) void fp8_gemm_kernel(G
   auto put_update = [&](int tc) __attribute__((always_inline)) {
     if (a.ts) {
 #pragma unroll 8
-      for (int e = tc; e < TM * rp / 4; e += 256) {  // 16 bytes each
-        const int row = e >> (lrp - 2), c = (e & (rp / 4 - 1)) * 8;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (row < rows) v = *reinterpret_cast<const uint4*>(a.ts + (size_t)(m0 + row) * 2 * rp + c);
-        *reinterpret_cast<uint4*>(Ts + row * ldt + c) = v;
+      for (int e = tc; e < TM * rp / 4; e += 256) {
+        const int row = e >> (lrp - 2), j = (e & (rp / 4 - 1)) * 4;
+        f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+        if (row < rows) v = *reinterpret_cast<const f32x4_t*>(a.ts + (size_t)(m0 + row) * rp + j);
+        put_t(row, j, v);
       }
     } else {
       const size_t stride = (size_t)M * rp;
@@ -585,7 +585,7 @@ __global__ __launch_bounds__(G::NT, G::NT / 256 * G::WPC) void fp8_gemm_kernel(G
           const float* p = a.part + (size_t)(m0 + row) * rp + j;
           for (int c = 0; c < a.nch; ++c) v += *reinterpret_cast<const f32x4_t*>(p + c * stride);
         }
-        put_t(row, j, v);
+        put_t(row, j, a.s * v);
       }
     }
     if (g.bvec) {
@@ -607,13 +607,31 @@ __global__ __launch_bounds__(G::NT, G::NT / 256 * G::WPC) void fp8_gemm_kernel(G
   // Dropout's mask of the update (N % 8 == 0 here): a bit a column, a byte a block of
   // the generator.  The copy waves make it while the products run.
   uint8_t* const mask = reinterpret_cast<uint8_t*>(sm) + G::LDS;
-  // s T B^T onto the accumulators (of the first of a sub-tile's KS waves): rows of
-  // [B | B] against rows of [hi | lo]
+  // s T B^T onto the accumulators (of the first of a sub-tile's KS waves): rows of B
+  // against rows of s T, whose bf16 parts are made on the way in: three into fp32, all that
+  // s T holds; two into bf16, whose own rounding is two hundred times theirs.  us with two
+  // and three into fp32: 333 x 4096 x 11008 at rank 16 56.0 and 56.2, 1024 x 4096 x 4096 at 128
+  // 60.9 and 63.4; dx of 2048 x 4096 x 4096 under a mask, with dA and dB, at 16 100.8 and 102.0, at
+  // 128 176.6 and 180.5.  (Three planes of s T in LDS, split as they are put there: 1 to 2% slower
+  // still at rank 128, for they take its columns in two halves.)
+  constexpr int NP = G::WIDE ? 3 : 2;
   auto add_update = [&](f32x16_t (&acc)[MT][NTL]) __attribute__((always_inline)) {
     if (KS > 1 && kg != 0) return;
     const int l32 = te & 31, lh = te >> 5 & 1;
-    const uint16_t* const tr = Ts + (wr * WM + l32) * ldt + 8 * lh;
+    const float* const tr = Ts + (wr * WM + l32) * ldt + 8 * lh;
     const uint16_t* const br = Bs + (wc * WN + l32) * ldb + 8 * lh;
+    auto parts = [&](int mi, int k0, uint4 (&p)[NP]) __attribute__((always_inline)) {
+      const float* const f = tr + mi * 32 * ldt + k0;
+      const f32x4_t a = *reinterpret_cast<const f32x4_t*>(f), b = *reinterpret_cast<const f32x4_t*>(f + 4);
+      uint32_t v[4][NP];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        bf16_parts<NP>(a[2 * i], a[2 * i + 1], v[i]);
+        bf16_parts<NP>(b[2 * i], b[2 * i + 1], v[2 + i]);
+      }
+#pragma unroll
+      for (int n = 0; n < NP; ++n) p[n] = make_uint4(v[0][n], v[1][n], v[2][n], v[3][n]);
+    };
     if constexpr (!MASK) {
       for (int k0 = 0; k0 < rp; k0 += 16) {
         uint4 bf[NTL];
@@ -621,34 +639,46 @@ __global__ __launch_bounds__(G::NT, G::NT / 256 * G::WPC) void fp8_gemm_kernel(G
         for (int ni = 0; ni < NTL; ++ni) bf[ni] = *reinterpret_cast<const uint4*>(br + ni * 32 * ldb + k0);
 #pragma unroll
         for (int mi = 0; mi < MT; ++mi) {
-          const uint4 hi = *reinterpret_cast<const uint4*>(tr + mi * 32 * ldt + k0);
-          const uint4 lo = *reinterpret_cast<const uint4*>(tr + mi * 32 * ldt + rp + k0);
+          uint4 p[NP];
+          parts(mi, k0, p);
 #pragma unroll
-          for (int ni = 0; ni < NTL; ++ni) acc[mi][ni] = mfma32(bf[ni], hi, acc[mi][ni]);
+          for (int n = 0; n < NP; ++n)
 #pragma unroll
-          for (int ni = 0; ni < NTL; ++ni) acc[mi][ni] = mfma32(bf[ni], lo, acc[mi][ni]);
+            for (int ni = 0; ni < NTL; ++ni) acc[mi][ni] = mfma32(bf[ni], p[n], acc[mi][ni]);
         }
       }
     } else {
+      // blocks whose update is in registers at a time
+      constexpr int PAIR = G::WIDE && NTL > 1 ? 2 : 1;
 #pragma unroll
       for (int mi = 0; mi < MT; ++mi)
 #pragma unroll
-        for (int ni = 0; ni < NTL; ++ni) {
-          f32x16_t L;
+        for (int b0 = 0; b0 < NTL; b0 += PAIR) {
+          f32x16_t L[PAIR];
 #pragma unroll
-          for (int e = 0; e < 16; ++e) L[e] = 0.f;
+          for (int q = 0; q < PAIR; ++q)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) L[q][e] = 0.f;
           for (int k0 = 0; k0 < rp; k0 += 16) {
-            const uint4 bf = *reinterpret_cast<const uint4*>(br + ni * 32 * ldb + k0);
-            L = mfma32(bf, *reinterpret_cast<const uint4*>(tr + mi * 32 * ldt + k0), L);
-            L = mfma32(bf, *reinterpret_cast<const uint4*>(tr + mi * 32 * ldt + rp + k0), L);
-          }
-          // the block's four bytes of this lane's row; elements 4 i + e: bit 4 lh + e of byte i
-          const int at = ((wr * WM + mi * 32 + l32) * TN + wc * WN + ni * 32) / 8;
-          const uint32_t bits = *reinterpret_cast<const uint32_t*>(mask + at) >> (4 * lh);
+            uint4 p[NP];
+            parts(mi, k0, p);
 #pragma unroll
-          for (int e = 0; e < 16; ++e)
-            acc[mi][ni][e] += (bits >> (8 * (e / 4) + e % 4)) & 1 ? L[e] * a.keep : 0.f;
-          __builtin_amdgcn_sched_barrier(0);  // (one block's L at a time)
+            for (int q = 0; q < PAIR; ++q) {
+              const uint4 bf = *reinterpret_cast<const uint4*>(br + (b0 + q) * 32 * ldb + k0);
+#pragma unroll
+              for (int n = 0; n < NP; ++n) L[q] = mfma32(bf, p[n], L[q]);
+            }
+          }
+          // a block's four bytes of this lane's row; elements 4 i + e: bit 4 lh + e of byte i
+#pragma unroll
+          for (int q = 0; q < PAIR; ++q) {
+            const int at = ((wr * WM + mi * 32 + l32) * TN + wc * WN + (b0 + q) * 32) / 8;
+            const uint32_t bits = *reinterpret_cast<const uint32_t*>(mask + at) >> (4 * lh);
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              acc[mi][b0 + q][e] += (bits >> (8 * (e / 4) + e % 4)) & 1 ? L[q][e] * a.keep : 0.f;
+          }
+          __builtin_amdgcn_sched_barrier(0);  // (PAIR blocks at a time)
         }
     }
   };
@@ -969,7 +999,7 @@ hipError_t launch_fp8_prep(const Fp8PrepArgs& a, hipStream_t stream) {
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.ts) return e;
   const size_t blocks = ((size_t)a.M * a.rp / 4 + 255) / 256;
-  hipLaunchKernelGGL(fp8_t_finish_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, a, 31 - __builtin_clz(a.rp));
+  hipLaunchKernelGGL(fp8_t_finish_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 

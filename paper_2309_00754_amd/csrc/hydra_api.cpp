@@ -1232,7 +1232,7 @@ hydra_status hydra_fp8_lora_linear_workspace_bytes(int64_t M, int64_t N, int64_t
   // (what the largest of the calls with up to M rows needs)
   const int rp = hydra::padded_rank(int(r));
   *bytes = fp8_rows_bytes(M, K) + up256(hydra::fp8_prep_most(int(M), rp)) +
-           (hydra::fp8_finishes_t(int(M), rp) ? up256((size_t)M * 2 * rp * 2) : 0) +
+           (hydra::fp8_finishes_t(int(M), rp) ? up256((size_t)M * rp * 4) : 0) +
            up256(hydra::fp8_split_most(int(M), int(N), int(K)));
   return HYDRA_OK;
 }
@@ -1260,7 +1260,7 @@ hydra_status hydra_fp8_lora_linear(const uint16_t* x, const uint16_t* x_adapter,
   int nch = 0, kch = 0;
   hydra::fp8_prep_chunks(int(M), int(K), rp, nch, kch);
   const size_t rows = xq ? 0 : fp8_rows_bytes(M, K), part = up256(hydra::fp8_prep_most(int(M), rp));
-  const size_t ts_bytes = hydra::fp8_finishes_t(int(M), rp) ? up256((size_t)M * 2 * rp * 2) : 0;
+  const size_t ts_bytes = hydra::fp8_finishes_t(int(M), rp) ? up256((size_t)M * rp * 4) : 0;
   const size_t split = up256(hydra::fp8_split_most(int(M), int(N), int(K)));
   const size_t need = rows + part + ts_bytes + split;
   if (need > 0) {
@@ -1283,7 +1283,7 @@ hydra_status hydra_fp8_lora_linear(const uint16_t* x, const uint16_t* x_adapter,
   p.nch = nch;
   p.kch = kch;
   p.s = s;
-  p.ts = ts_bytes ? reinterpret_cast<uint16_t*>(w + rows + part) : nullptr;
+  p.ts = ts_bytes ? reinterpret_cast<float*>(w + rows + part) : nullptr;
   const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   if (rows + part > 0) {
     const hipError_t e = hydra::launch_fp8_prep(p, st);

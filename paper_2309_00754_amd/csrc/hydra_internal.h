@@ -72,6 +72,7 @@ struct TpreArgs {
   float s;
   int M, N, K, r;
   uint16_t* ts;       // [M x 2 RP] hi | lo of s T, or nullptr
+  float* tv;          // [M x RP] s T itself, or nullptr
   uint16_t* bp;       // used only when B itself cannot serve (r != RP or B not 16-byte aligned)
   float* part;        // [kTpreMaxChunks x M x RP] fp32 partial sums over K chunks
   uint16_t* tT;       // [2 or 3][RP][Mp] bf16 planes of (s T)^T, rows M..Mp zero, or nullptr
@@ -293,7 +294,7 @@ hipError_t launch_fp8_quantize(const Fp8QuantArgs& a, hipStream_t stream);
 
 // The dual-output linear over an 8-bit weight (fp8_linear.hip).  Where the LoRA
 // update's s T comes from: `part`, nch partial sums [nch][M][rp] of T, or `ts`,
-// hi and lo parts of s T [M x 2 rp].  drop > 0: the update goes through the
+// s T in fp32 [M x rp].  drop > 0: the update goes through the
 // dropout mask of rng (an element's 16 bits below `drop`: 0, else times keep).
 struct Fp8LinearArgs {
   const uint8_t* xq;   // [M x K]
@@ -308,7 +309,7 @@ struct Fp8LinearArgs {
   float s;
   const float* part;
   int nch;
-  const uint16_t* ts;
+  const float* ts;
   const uint16_t* B;   // [N x ldb], the first r columns
   int ldb;
   uint32_t drop;
@@ -329,7 +330,7 @@ struct Fp8PrepArgs {
   float* part;         // [nch][M][rp]
   int nch, kch;        // chunks of K, of kch blocks of 128
   float s;
-  uint16_t* ts;        // [M][2 rp] bf16 hi | lo of s T, or nullptr (fp8_finishes_t)
+  float* ts;           // [M][rp] s T, or nullptr (fp8_finishes_t)
 };
 hipError_t launch_fp8_prep(const Fp8PrepArgs& a, hipStream_t stream);
 hipError_t launch_fp8_linear(const Fp8LinearArgs& a, hipStream_t stream);

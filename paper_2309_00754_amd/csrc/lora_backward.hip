@@ -460,7 +460,7 @@ BwdLayout layout(int M, int N, int K, int rp, int planes, size_t split) {
   size_t o = 0;
   l.bt = o;    o += up256((size_t)rp * N * 2);                      // B^T [RP x N] bf16
   l.at = o;    o += up256((size_t)K * rp * 2);                      // A^T [K x RP] bf16
-  l.tsu = o;   o += up256((size_t)M * 2 * rp * 2);                  // hi | lo of s U [M x 2 RP] bf16
+  l.tsu = o;   o += up256((size_t)M * 2 * rp * 2);                  // hi | lo of s U [M x 2 RP] bf16, or s U [M x RP] fp32
   const size_t Mp = (size_t)padded_rows(M);
   l.uT = o;    o += up256(planes * (size_t)rp * Mp * 2);            // planes of (s U)^T, [planes][RP][Mp] bf16
   l.tT = o;    o += up256(planes * (size_t)rp * Mp * 2);            // planes of (s T)^T, [planes][RP][Mp] bf16
@@ -498,7 +498,7 @@ hipError_t launch_lora_backward(const BackwardArgs& a, void* ws, hipStream_t str
   uint8_t* const w = static_cast<uint8_t*>(ws);
   const size_t split = a.base8 ? a.base8->split_bytes : 0;
   // dx over a weight in 8 bits: dy's bytes, then the product with its update
-  auto dx_over_8 = [&](const uint16_t* ts, const uint16_t* at, size_t split_at) {
+  auto dx_over_8 = [&](const float* ts, const uint16_t* at, size_t split_at) {
     Fp8LinearArgs g = *a.base8;
     g.split = reinterpret_cast<float*>(w + split_at);
     Fp8PrepArgs q{};
@@ -555,7 +555,8 @@ hipError_t launch_lora_backward(const BackwardArgs& a, void* ws, hipStream_t str
   u.r = a.r;
   u.Kform = tt.Kform = std::max(a.N, a.K);
   u.Kall = tt.Kall = a.N + a.K;
-  u.ts = want_dx ? reinterpret_cast<uint16_t*>(w + l.tsu) : nullptr;
+  u.ts = a.dx ? reinterpret_cast<uint16_t*>(w + l.tsu) : nullptr;
+  u.tv = a.base8 ? reinterpret_cast<float*>(w + l.tsu) : nullptr;
   u.part = reinterpret_cast<float*>(w + l.tpart);
   u.tT = a.dA ? reinterpret_cast<uint16_t*>(w + l.uT) : nullptr;
   u.Mp = padded_rows(a.M);
@@ -576,7 +577,7 @@ hipError_t launch_lora_backward(const BackwardArgs& a, void* ws, hipStream_t str
   if (e != hipSuccess) return e;
   // 3. dx = dy W + s U A: the GEMM over W^T with slabs ([hi | lo](s U), A^T)
   if (a.base8) {
-    if ((e = dx_over_8(u.ts, at, l.split)) != hipSuccess) return e;
+    if ((e = dx_over_8(u.tv, at, l.split)) != hipSuccess) return e;
   } else if (a.dx) {
     LinearArgs g{};
     g.x = a.dy;

@@ -118,7 +118,7 @@ __device__ __forceinline__ void pad_b(const TpreArgs& a, size_t block, size_t bl
 }
 
 // hi and lo bf16 parts of s * T[row][j] (and what they leave, to tT), written row-major (ts) and / or
-// transposed (tT, whose rows M..Mp are written as zeros: v = 0 there).
+// transposed (tT, whose rows M..Mp are written as zeros: v = 0 there), or s * T itself row-major (tv).
 __device__ __forceinline__ void t_store(const TpreArgs& a, int rp, size_t row, size_t j, float v) {
   v *= a.s;
   const uint32_t hi = f32_to_bf16_rne(v);
@@ -127,6 +127,7 @@ __device__ __forceinline__ void t_store(const TpreArgs& a, int rp, size_t row, s
     a.ts[row * 2 * rp + j] = (uint16_t)hi;
     a.ts[row * 2 * rp + rp + j] = (uint16_t)lo;
   }
+  if (a.tv && row < (size_t)a.M) a.tv[row * rp + j] = v;
   if (a.tT) {
     a.tT[j * a.Mp + row] = (uint16_t)hi;
     a.tT[(rp + j) * a.Mp + row] = (uint16_t)lo;
