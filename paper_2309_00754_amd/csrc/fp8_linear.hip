@@ -34,24 +34,23 @@ namespace {
 
 constexpr int P_WAVES = 8;
 
-// Two values as NP bf16 parts, a pair of each part.  Three add up to the values: the upper
-// half of their bits, that of what it leaves, and what is left then (at most eight bits).
-// Two, rounded, are within 2^-17 of them.  An infinity's other parts are zero.
-template <int NP>
-__device__ __forceinline__ void bf16_parts(float a, float b, uint32_t (&p)[NP]) {
+// Two values as bf16 parts, a pair of each.  Two, rounded, are within 2^-17 of them.
+// Three add up to them: the upper half of their bits, that of what it leaves, and what is
+// left then (at most eight bits).  An infinity's other parts are zero.
+__device__ __forceinline__ void two_parts(float a, float b, uint32_t& hi, uint32_t& lo) {
+  hi = f32_to_bf16_pair(a, b);
+  lo = f32_to_bf16_pair(__builtin_isinf(a) ? 0.f : a - __uint_as_float(hi << 16),
+                        __builtin_isinf(b) ? 0.f : b - __uint_as_float(hi & 0xFFFF0000u));
+}
+__device__ __forceinline__ void three_parts(float a, float b, uint32_t (&p)[3]) {
   const bool ia = __builtin_isinf(a), ib = __builtin_isinf(b);
-  if constexpr (NP == 2) {
-    p[0] = f32_to_bf16_pair(a, b);
-    p[1] = f32_to_bf16_pair(ia ? 0.f : a - __uint_as_float(p[0] << 16), ib ? 0.f : b - __uint_as_float(p[0] & 0xFFFF0000u));
-  } else {
 #pragma unroll
-    for (int n = 0; n < 3; ++n) {
-      const uint32_t ua = __float_as_uint(a), ub = __float_as_uint(b);
-      p[n] = __builtin_amdgcn_perm(ub, ua, 0x07060302u);
-      a -= __uint_as_float(ua & 0xFFFF0000u);
-      b -= __uint_as_float(ub & 0xFFFF0000u);
-      if (n == 0) a = ia ? 0.f : a, b = ib ? 0.f : b;
-    }
+  for (int n = 0; n < 3; ++n) {
+    const uint32_t ua = __float_as_uint(a), ub = __float_as_uint(b);
+    p[n] = __builtin_amdgcn_perm(ub, ua, 0x07060302u);
+    a -= __uint_as_float(ua & 0xFFFF0000u);
+    b -= __uint_as_float(ub & 0xFFFF0000u);
+    if (n == 0) a = ia ? 0.f : a, b = ib ? 0.f : b;
   }
 }
 
@@ -160,15 +159,27 @@ __global__ __launch_bounds__(P_WAVES * 64) void fp8_prep_kernel(Fp8PrepArgs g) {
   }
 }
 
-// s T, which tiles at a rank above 16 read in place of the chunks' sums: four values a
-// thread.
-__global__ __launch_bounds__(256) void fp8_t_finish_kernel(Fp8PrepArgs g) {
-  const size_t e = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4, all = (size_t)g.M * g.rp;
+// s T, which tiles at a rank above 16 read in place of the chunks' sums, as they hold it: in
+// fp32, or (PARTS) as two bf16 parts [M][hi rp | lo rp].  Four values a thread.
+template <bool PARTS>
+__global__ __launch_bounds__(256) void fp8_t_finish_kernel(Fp8PrepArgs g, int lrp) {
+  const size_t e = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4, all = (size_t)g.M << lrp;
   if (e >= all) return;
   f32x4_t v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
   for (int c = 0; c < g.nch; ++c) v += *reinterpret_cast<const f32x4_t*>(g.part + c * all + e);
-  *reinterpret_cast<f32x4_t*>(g.ts + e) = g.s * v;
+  v *= g.s;
+  if constexpr (PARTS) {
+    uint2 hi, lo;
+    two_parts(v[0], v[1], hi.x, lo.x);
+    two_parts(v[2], v[3], hi.y, lo.y);
+    const size_t row = e >> lrp;
+    uint16_t* const o = static_cast<uint16_t*>(g.ts) + (row << (lrp + 1)) + (e - (row << lrp));
+    *reinterpret_cast<uint2*>(o) = hi;
+    *reinterpret_cast<uint2*>(o + g.rp) = lo;
+  } else {
+    *reinterpret_cast<f32x4_t*>(static_cast<float*>(g.ts) + e) = v;
+  }
 }
 
 // ------------------------------------------------------------------ few rows
@@ -347,7 +358,7 @@ struct Tile {
   static constexpr int RD = STEP / 32;                 // 16-byte reads a lane and row in a step
   static constexpr int OLD = TN + 4;                   // row of the output tile in LDS (fp32, in values)
   static constexpr int OUT = KS * TM * OLD * 4;        // bytes of the KS partial sums of it
-  // rows of s T (fp32) and of B, 16 bytes apart from the next, at padded rank rp
+  // rows of s T (fp32, or two bf16 parts) and of B, 16 bytes apart from the next, at padded rank rp
   static constexpr int lora_bytes(int rp) { return TM * (4 * rp + 16) + TN * (2 * rp + 16); }
   static constexpr size_t cmax(size_t x, size_t y) { return x > y ? x : y; }
   static constexpr int MASK = TM * TN / 8;             // bytes of dropout's mask, after the rest
@@ -516,13 +527,22 @@ __global__ __launch_bounds__(G::NT, G::NT / 256 * G::WPC) void fp8_gemm_kernel(G
         if (n0 + col + e < N) store_elem(y, w == 4 ? kF32 : kBf16, at + e, v[e]);
     }
   };
-  // The rows of s T and those of B, zero padded to rp, to LDS.
-  const int rp = a.rp, lrp = 31 - __builtin_clz(rp | 1), ldt = rp + 4, ldb = rp + 8;  // (in values)
-  float* const Ts = reinterpret_cast<float*>(sm);
-  uint16_t* const Bs = reinterpret_cast<uint16_t*>(Ts + TM * ldt);
+  // The rows of s T and those of B, zero padded to rp, to LDS: s T as it is where it goes
+  // into fp32, else as its two parts [hi rp | lo rp].
+  const int rp = a.rp, lrp = 31 - __builtin_clz(rp | 1), ldt = 2 * rp + 8, ldb = rp + 8;  // (in 16 bits)
+  uint16_t* const Ts = reinterpret_cast<uint16_t*>(sm);
+  uint16_t* const Bs = Ts + TM * ldt;
   // Four values of s T, of a tile's row.
   auto put_t = [&](int row, int j, const f32x4_t& v) __attribute__((always_inline)) {
-    *reinterpret_cast<f32x4_t*>(Ts + row * ldt + j) = v;
+    if constexpr (G::WIDE) {
+      *reinterpret_cast<f32x4_t*>(Ts + row * ldt + 2 * j) = v;
+    } else {
+      uint2 hi, lo;
+      two_parts(v[0], v[1], hi.x, lo.x);
+      two_parts(v[2], v[3], hi.y, lo.y);
+      *reinterpret_cast<uint2*>(Ts + row * ldt + j) = hi;
+      *reinterpret_cast<uint2*>(Ts + row * ldt + rp + j) = lo;
+    }
   };
   const int rows = min(TM, M - m0), cols = min(TN, N - n0);
   // By the 256 threads of the copy waves.  At padded rank 16, the usual one, the loads
@@ -568,12 +588,13 @@ __global__ __launch_bounds__(G::NT, G::NT / 256 * G::WPC) void fp8_gemm_kernel(G
   };
   auto put_update = [&](int tc) __attribute__((always_inline)) {
     if (a.ts) {
+      const uint16_t* const ts = static_cast<const uint16_t*>(a.ts);
 #pragma unroll 8
-      for (int e = tc; e < TM * rp / 4; e += 256) {
-        const int row = e >> (lrp - 2), j = (e & (rp / 4 - 1)) * 4;
-        f32x4_t v = {0.f, 0.f, 0.f, 0.f};
-        if (row < rows) v = *reinterpret_cast<const f32x4_t*>(a.ts + (size_t)(m0 + row) * rp + j);
-        put_t(row, j, v);
+      for (int e = tc; e < TM * rp / 4; e += 256) {  // 16 bytes each
+        const int row = e >> (lrp - 2), c = (e & (rp / 4 - 1)) * 8;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (row < rows) v = *reinterpret_cast<const uint4*>(ts + (size_t)(m0 + row) * 2 * rp + c);
+        *reinterpret_cast<uint4*>(Ts + row * ldt + c) = v;
       }
     } else {
       const size_t stride = (size_t)M * rp;
@@ -608,29 +629,34 @@ __global__ __launch_bounds__(G::NT, G::NT / 256 * G::WPC) void fp8_gemm_kernel(G
   // the generator.  The copy waves make it while the products run.
   uint8_t* const mask = reinterpret_cast<uint8_t*>(sm) + G::LDS;
   // s T B^T onto the accumulators (of the first of a sub-tile's KS waves): rows of B
-  // against rows of s T, whose bf16 parts are made on the way in: three into fp32, all that
-  // s T holds; two into bf16, whose own rounding is two hundred times theirs.  us with two
-  // and three into fp32: 333 x 4096 x 11008 at rank 16 56.0 and 56.2, 1024 x 4096 x 4096 at 128
-  // 60.9 and 63.4; dx of 2048 x 4096 x 4096 under a mask, with dA and dB, at 16 100.8 and 102.0, at
-  // 128 176.6 and 180.5.  (Three planes of s T in LDS, split as they are put there: 1 to 2% slower
-  // still at rank 128, for they take its columns in two halves.)
+  // against those of the parts of s T: three into fp32, all that s T holds, made on the way
+  // in; two into bf16, whose own rounding is two hundred times theirs.  us with two and
+  // three into fp32: 333 x 4096 x 11008 at rank 16 56.0 and 56.2, 1024 x 4096 x 4096 at 128 60.9 and
+  // 63.4; dx of 2048 x 4096 x 4096 under a mask, with dA and dB, at 16 100.8 and 102.0, at 128 176.6
+  // and 180.5.  (Three planes in LDS, split as they are put there: 1 to 2% slower still at
+  // rank 128, for the largest tile takes its columns in two halves then.)
   constexpr int NP = G::WIDE ? 3 : 2;
   auto add_update = [&](f32x16_t (&acc)[MT][NTL]) __attribute__((always_inline)) {
     if (KS > 1 && kg != 0) return;
     const int l32 = te & 31, lh = te >> 5 & 1;
-    const float* const tr = Ts + (wr * WM + l32) * ldt + 8 * lh;
+    const uint16_t* const tr = Ts + (wr * WM + l32) * ldt + (G::WIDE ? 16 : 8) * lh;
     const uint16_t* const br = Bs + (wc * WN + l32) * ldb + 8 * lh;
     auto parts = [&](int mi, int k0, uint4 (&p)[NP]) __attribute__((always_inline)) {
-      const float* const f = tr + mi * 32 * ldt + k0;
-      const f32x4_t a = *reinterpret_cast<const f32x4_t*>(f), b = *reinterpret_cast<const f32x4_t*>(f + 4);
-      uint32_t v[4][NP];
+      const uint16_t* const row = tr + mi * 32 * ldt;
+      if constexpr (G::WIDE) {
+        const f32x4_t a = *reinterpret_cast<const f32x4_t*>(row + 2 * k0);
+        const f32x4_t b = *reinterpret_cast<const f32x4_t*>(row + 2 * k0 + 8);
+        uint32_t v[4][3];
+        three_parts(a[0], a[1], v[0]);
+        three_parts(a[2], a[3], v[1]);
+        three_parts(b[0], b[1], v[2]);
+        three_parts(b[2], b[3], v[3]);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        bf16_parts<NP>(a[2 * i], a[2 * i + 1], v[i]);
-        bf16_parts<NP>(b[2 * i], b[2 * i + 1], v[2 + i]);
+        for (int n = 0; n < NP; ++n) p[n] = make_uint4(v[0][n], v[1][n], v[2][n], v[3][n]);
+      } else {
+#pragma unroll
+        for (int n = 0; n < NP; ++n) p[n] = *reinterpret_cast<const uint4*>(row + n * rp + k0);
       }
-#pragma unroll
-      for (int n = 0; n < NP; ++n) p[n] = make_uint4(v[0][n], v[1][n], v[2][n], v[3][n]);
     };
     if constexpr (!MASK) {
       for (int k0 = 0; k0 < rp; k0 += 16) {
@@ -999,7 +1025,11 @@ hipError_t launch_fp8_prep(const Fp8PrepArgs& a, hipStream_t stream) {
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.ts) return e;
   const size_t blocks = ((size_t)a.M * a.rp / 4 + 255) / 256;
-  hipLaunchKernelGGL(fp8_t_finish_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, a);
+  const int lrp = 31 - __builtin_clz(a.rp);
+  if (a.parts)
+    hipLaunchKernelGGL((fp8_t_finish_kernel<true>), dim3((unsigned)blocks), dim3(256), 0, stream, a, lrp);
+  else
+    hipLaunchKernelGGL((fp8_t_finish_kernel<false>), dim3((unsigned)blocks), dim3(256), 0, stream, a, lrp);
   return hipGetLastError();
 }
 

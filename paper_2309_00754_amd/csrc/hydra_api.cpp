@@ -1283,7 +1283,8 @@ hydra_status hydra_fp8_lora_linear(const uint16_t* x, const uint16_t* x_adapter,
   p.nch = nch;
   p.kch = kch;
   p.s = s;
-  p.ts = ts_bytes ? reinterpret_cast<float*>(w + rows + part) : nullptr;
+  p.ts = ts_bytes ? w + rows + part : nullptr;
+  p.parts = y_type != HYDRA_F32;
   const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   if (rows + part > 0) {
     const hipError_t e = hydra::launch_fp8_prep(p, st);

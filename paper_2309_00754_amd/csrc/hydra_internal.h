@@ -294,8 +294,9 @@ hipError_t launch_fp8_quantize(const Fp8QuantArgs& a, hipStream_t stream);
 
 // The dual-output linear over an 8-bit weight (fp8_linear.hip).  Where the LoRA
 // update's s T comes from: `part`, nch partial sums [nch][M][rp] of T, or `ts`,
-// s T in fp32 [M x rp].  drop > 0: the update goes through the
-// dropout mask of rng (an element's 16 bits below `drop`: 0, else times keep).
+// s T [M x rp] in fp32 or, where y is bf16, its hi and lo parts [M x 2 rp].  drop > 0:
+// the update goes through the dropout mask of rng (an element's 16 bits below `drop`: 0,
+// else times keep).
 struct Fp8LinearArgs {
   const uint8_t* xq;   // [M x K]
   const uint8_t* xs;   // [M x ceil(K / 128)]
@@ -309,7 +310,7 @@ struct Fp8LinearArgs {
   float s;
   const float* part;
   int nch;
-  const float* ts;
+  const void* ts;
   const uint16_t* B;   // [N x ldb], the first r columns
   int ldb;
   uint32_t drop;
@@ -330,7 +331,8 @@ struct Fp8PrepArgs {
   float* part;         // [nch][M][rp]
   int nch, kch;        // chunks of K, of kch blocks of 128
   float s;
-  float* ts;           // [M][rp] s T, or nullptr (fp8_finishes_t)
+  void* ts;            // s T as the product takes it, or nullptr (fp8_finishes_t)
+  bool parts;          // ... as hi and lo parts
 };
 hipError_t launch_fp8_prep(const Fp8PrepArgs& a, hipStream_t stream);
 hipError_t launch_fp8_linear(const Fp8LinearArgs& a, hipStream_t stream);

@@ -498,7 +498,7 @@ hipError_t launch_lora_backward(const BackwardArgs& a, void* ws, hipStream_t str
   uint8_t* const w = static_cast<uint8_t*>(ws);
   const size_t split = a.base8 ? a.base8->split_bytes : 0;
   // dx over a weight in 8 bits: dy's bytes, then the product with its update
-  auto dx_over_8 = [&](const float* ts, const uint16_t* at, size_t split_at) {
+  auto dx_over_8 = [&](const void* ts, const uint16_t* at, size_t split_at) {
     Fp8LinearArgs g = *a.base8;
     g.split = reinterpret_cast<float*>(w + split_at);
     Fp8PrepArgs q{};
@@ -555,8 +555,9 @@ hipError_t launch_lora_backward(const BackwardArgs& a, void* ws, hipStream_t str
   u.r = a.r;
   u.Kform = tt.Kform = std::max(a.N, a.K);
   u.Kall = tt.Kall = a.N + a.K;
-  u.ts = a.dx ? reinterpret_cast<uint16_t*>(w + l.tsu) : nullptr;
-  u.tv = a.base8 ? reinterpret_cast<float*>(w + l.tsu) : nullptr;
+  const bool whole = a.base8 && a.base8->y_type == kF32;  // (s U in fp32, else as two parts)
+  u.ts = want_dx && !whole ? reinterpret_cast<uint16_t*>(w + l.tsu) : nullptr;
+  u.tv = whole ? reinterpret_cast<float*>(w + l.tsu) : nullptr;
   u.part = reinterpret_cast<float*>(w + l.tpart);
   u.tT = a.dA ? reinterpret_cast<uint16_t*>(w + l.uT) : nullptr;
   u.Mp = padded_rows(a.M);
@@ -577,7 +578,7 @@ hipError_t launch_lora_backward(const BackwardArgs& a, void* ws, hipStream_t str
   if (e != hipSuccess) return e;
   // 3. dx = dy W + s U A: the GEMM over W^T with slabs ([hi | lo](s U), A^T)
   if (a.base8) {
-    if ((e = dx_over_8(u.tv, at, l.split)) != hipSuccess) return e;
+    if ((e = dx_over_8(w + l.tsu, at, l.split)) != hipSuccess) return e;
   } else if (a.dx) {
     LinearArgs g{};
     g.x = a.dy;
