@@ -34,13 +34,22 @@ namespace {
 
 constexpr int P_WAVES = 8;
 
-// Two values as bf16 parts, a pair of each.  Two, rounded, are within 2^-17 of them.
-// Three add up to them: the upper half of their bits, that of what it leaves, and what is
-// left then (at most eight bits).  An infinity's other parts are zero.
+// Two values as bf16 parts, a pair of each.  Two, rounded, are within 2^-17 of them (the
+// first cut, not rounded, where rounding would make it infinite).  Three add up to them: the
+// upper half of their bits, that of what it leaves, and what is left then (at most eight
+// bits).  An infinity's other parts are zero.
 __device__ __forceinline__ void two_parts(float a, float b, uint32_t& hi, uint32_t& lo) {
-  hi = f32_to_bf16_pair(a, b);
-  lo = f32_to_bf16_pair(__builtin_isinf(a) ? 0.f : a - __uint_as_float(hi << 16),
-                        __builtin_isinf(b) ? 0.f : b - __uint_as_float(hi & 0xFFFF0000u));
+  const float f[2] = {a, b};
+  uint32_t h[2];
+  float rest[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    h[i] = f32_to_bf16_any(f[i]);
+    if ((h[i] & 0x7FFF) == 0x7F80) h[i] = __float_as_uint(f[i]) >> 16;
+    rest[i] = __builtin_isinf(f[i]) ? 0.f : f[i] - bf16_to_f32(h[i]);
+  }
+  hi = h[0] | h[1] << 16;
+  lo = f32_to_bf16_pair(rest[0], rest[1]);
 }
 __device__ __forceinline__ void three_parts(float a, float b, uint32_t (&p)[3]) {
   const bool ia = __builtin_isinf(a), ib = __builtin_isinf(b);

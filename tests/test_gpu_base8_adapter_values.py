@@ -26,3 +26,23 @@ def test_the_largest_and_infinite_updates(dev, M, N, K, r):
     H.hydra_fp8_lora_linear(x, W, w, A, put(B, "bf16", dev), 1.9921875, None, on, x_adapter=put(xa, "bf16", dev))
     ref = 1.9921875 * xa[:, K - 1:].astype(np.float64) @ B.T
     near(f64(on), ref, 4 * U * np.abs(ref), "y_on")
+
+
+@pytest.mark.parametrize("M,N,K,r", [(3, 40, 128, 1), (40, 300, 256, 1), (1100, 264, 128, 32), (20, 64, 8192, 3)])
+@pytest.mark.parametrize("y_type", ["f32", "bf16"])
+def test_updates_above_the_largest_bf16(dev, M, N, K, r, y_type):
+    """s T between bf16's largest number and fp32's, times a half."""
+    import torch
+    say("updates above the largest bf16", M, N, K, r, y_type)
+    big = float(torch.finfo(torch.bfloat16).max)
+    s = float(np.float32(1.003))  # (s T is past the middle between bf16's largest and 2^128, and below fp32's largest)
+    xa = np.zeros((M, K), np.float32)
+    xa[:, 0] = np.where(np.arange(M) % 2 == 0, big, -big)
+    A, B = np.zeros((r, K), np.float32), np.zeros((N, r), np.float32)
+    A[r - 1], B[:, r - 1] = 1, 0.5
+    W, w = torch.zeros((N, K), dtype=torch.uint8, device=dev), torch.full((-(-N // 128), -(-K // 128)), 127, dtype=torch.uint8, device=dev)
+    on = empty((M, N), y_type, dev)
+    H.hydra_fp8_lora_linear(put(np.ones((M, K)), "bf16", dev), W, w, put(A, "bf16", dev), put(B, "bf16", dev), s, None, on,
+                            x_adapter=put(xa, "bf16", dev))
+    ref = np.repeat(0.5 * s * xa[:, :1].astype(np.float64), N, 1)
+    near(f64(on), ref, (4 * U + (2.0 ** -8 if y_type == "bf16" else 0)) * np.abs(ref), "y_on")
