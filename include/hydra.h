@@ -789,13 +789,16 @@ hydra_status hydra_fp8_lora_linear_workspace_bytes(int64_t M, int64_t N, int64_t
  * x, x_adapter, xq, Wq and A 16-byte aligned, B 2-byte, outputs at their element's
  * alignment.  Into fp32 outputs, and up to 16 rows, every product is exact and
  * added in fp32; into bf16 outputs of more rows the 8-bit matrix instructions run,
- * whose sums are about 2e-5 off (a step of bf16 is 8e-3).  The update takes all that
- * fp32 holds of s x A^T, but into bf16 outputs of more than 16 rows, where it takes two
- * bf16 parts (2^-17 of it).  Outputs are rounded once, to nearest even.  A scale byte 255 stands for NaN; a value whose bytes
- * stand for 2^128 (above 1.94 2^127 in x) counts as infinite where products are exact.
- * NaN and infinities in x make their row's outputs NaN; in x_adapter alone they go
- * through the update as fp32 takes them.  With r == 0 y_on equals y_off.  Requires 1 <= M <= 2^20, 1 <= N <= 2^21, 16 <= K <= 2^21, K % 16 == 0,
- * 0 <= r <= HYDRA_MAX_RANK, ceil(M / 128) ceil(N / 256) < 2^23; outputs distinct
+ * which keep of every eight products with consecutive k what lies above 2^-12 of the
+ * largest: typical sums are 2e-5 off (a step of bf16 is 8e-3), a sum whose products
+ * cancel keeps more of its digits in fp32 outputs.  The update takes all that fp32
+ * holds of s x A^T, but into bf16 outputs of more than 16 rows, where it takes two
+ * bf16 parts (2^-17 of it).  Outputs are rounded once, to nearest even.  A scale byte
+ * 255 stands for NaN; a value whose bytes stand for 2^128 (above 1.94 2^127 in x)
+ * counts as infinite where products are exact.  NaN and infinities in x make their
+ * row's outputs NaN; in x_adapter alone they go through the update as fp32 takes them.
+ * With r == 0 y_on equals y_off.  Requires 1 <= M <= 2^20, 1 <= N <= 2^21, 16 <= K <= 2^21,
+ * K % 16 == 0, 0 <= r <= HYDRA_MAX_RANK, ceil(M / 128) ceil(N / 256) < 2^23; outputs distinct
  * (HYDRA_ERR_SHAPE).  Repeated calls give the same bits.  Calls that share a
  * workspace on different streams race.
  */
@@ -827,8 +830,10 @@ hydra_status hydra_fp8_lora_linear_backward_workspace_bytes(int64_t M, int64_t N
  *            hydra_fp8_lora_linear_backward_workspace_bytes(M, N, K, r) bytes,
  *            contents ignored and overwritten
  * dx: into fp32 every product of the base is exact and added in fp32, into bf16 the
- * 8-bit matrix instructions run at every M; its update takes all that fp32 holds of s (dy B),
- * into bf16 two bf16 parts (2^-17 of it).  dA and dB take 24 bits of s (dy B) and s (xa A^T).
+ * 8-bit matrix instructions run (but with r == 0 up to 16 rows, where products are exact
+ * too); its update takes all that fp32 holds of s (dy B), into bf16 two bf16 parts (2^-17
+ * of it).  dA and dB take 24 bits of s (dy B) and s (xa A^T).  What a NaN or an infinity
+ * reaches is NaN or infinite.
  * The quantized x of the forward's base product counts as x itself (its
  * rounding has no gradient).  Requires N and K multiples of 16, other limits as in
  * hydra_fp8_lora_linear with N and K exchanged.  At least one output

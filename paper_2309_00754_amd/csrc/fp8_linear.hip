@@ -19,8 +19,9 @@
 //    4096 15.2 us, 3.0 TB/s, behind 3.8 us of x and T);
 //  * fp8_gemm_kernel (more rows): tiles through LDS, four waves copying ahead of those that
 //    multiply; K in parts where few rows leave CUs without a tile.  Bound by the matrix cores
-//    from some 1000 rows on: 2048 x 11008 x 4096 into one bf16 output 118 us with all
-//    launches, 1.6 PFLOP/s, into fp32 169, 1.1; below by the copies into LDS.
+//    from some 1000 rows on: 2048 x 11008 x 4096 into one bf16 output 118 to 124 us with all
+//    launches, 1.5 PFLOP/s, into fp32 181, 1.0; below by the copies into LDS.
+// Which tile, how many parts and how much room they take: hydra_fp8_plan.h.
 #include <type_traits>
 
 #include "hydra_fp8.h"

@@ -78,7 +78,8 @@ constexpr Fp8TileCost kFp8TileCosts[2][kFp8Tiles] = {{{128, 256, 128, true, 0.f,
 // sums written and read at 6.75 TB/s (a fit to 330 cases, rms error 9%).  us, whole ->
 // in parts, fp32: 17 x 2048 x 8192 17.9 -> 11.4, 64 x 4096 x 11008 25.3 -> 21.8, 200 x 4096 x
 // 11008 38.6 -> 32.7; with tile 0 among them 333 x 4096 x 11008 59.3 -> 57.1 (bf16 51.2 ->
-// 47.8), rank 16 and x quantized in the call.  Below K = 4096 never faster.
+// 47.8), rank 16 and x quantized in the call; 54 to 56 (42) with the joining launch that asks
+// for the parts' sums first.  Below K = 4096 never faster.
 constexpr int kFp8MaxSplit = 8, kFp8MaxParts = 512;
 
 struct Fp8Plan {

@@ -8,9 +8,11 @@
 //  2. the LoRA pre-pass of the forward GEMM (lora_tpre.hip) twice, in one
 //     pair of launches: s U from dy against the rows of B^T, s T from x
 //     against A, each as bf16 hi and lo parts (row-major for step 3,
-//     transposed for step 4);
+//     transposed for step 4); over a weight in 8 bits as three parts for step
+//     4, and s U in fp32 for step 3 into an fp32 dx;
 //  3. dx by the forward's MFMA GEMM run on (dy, W^T), its LoRA slabs being
-//     [hi | lo](s U) against rows of A^T: one pass over W^T, as in the forward;
+//     [hi | lo](s U) against rows of A^T: one pass over W^T, as in the forward
+//     (over a weight in 8 bits: fp8_linear.hip);
 //  4. dA and dB as sums of outer products over the rows m:
 //     out[j][c] = sum_m P[m][j] Q[m][c] with (P, Q) = (s U, x) and (s T, dy),
 //     on MFMAs (lora_outer_part_kernel: per row chunk partials, laid out like

@@ -9,7 +9,9 @@
 // running sums is lost in 32 bits (their errors, 1e-7 each, against steps of
 // 1e-5: one sample in a hundred another token).
 //
-// Bound: memory for many rows (every logit once), launches for few.
+// Bound: vector instructions for many rows (64 sequences of up to 7: 35 for each logit of the
+// sums, the tables below among them, which keep the vector units busy for 24 of that launch's 33
+// us; its logits are 16 us of memory), launches for few.
 //  * verify_stats_kernel: maximum and sum of exponentials of every segment of
 //    every row that a sequence has;
 //  * verify_left_kernel: the rows' totals, the acceptances (every workgroup of a
